@@ -88,8 +88,9 @@ def valid_edges(src, dst, rel, type_offsets, rels) -> np.ndarray:
     rs = np.array([r[0] for r in rels] + [-1], np.int64)
     rt = np.array([r[1] for r in rels] + [-1], np.int64)
     rr = np.where(ok, rel, len(rels))
-    ok &= node_type(np.where(ok, src, 0), type_offsets) == rs[rr]
-    ok &= node_type(np.where(ok, dst, 0), type_offsets) == rt[rr]
+    types = node_type(np.arange(max(n, 1)), type_offsets).astype(np.int8)
+    ok &= types[np.where(ok, src, 0)] == rs[rr]
+    ok &= types[np.where(ok, dst, 0)] == rt[rr]
     return ok
 
 
@@ -266,6 +267,13 @@ def layer_backward(csr: list, type_offsets, rels, params: dict, H, dH_out, act: 
 # ----------------------------------------------------------------------------------------------
 # sampled forms for full-size checks: the same definitions, evaluated only where asked
 # ----------------------------------------------------------------------------------------------
+def _places(rows_sorted, ids, n):
+    """Index of each id in the sorted list of node ids, -1 where it is not in it (ids in [0, n))."""
+    table = np.full(max(n, 1), -1, np.int32)
+    table[rows_sorted] = np.arange(rows_sorted.shape[0], dtype=np.int32)
+    return table[ids]
+
+
 def _row_aggregates(src, dst, rel, valid, rows_sorted, H, R, chunk=1 << 20):
     """For sorted node ids `rows_sorted`: S[k, r] = sum of H[src] over valid in-edges of relation r
     into rows_sorted[k], and deg[k, r] their count."""
@@ -273,10 +281,8 @@ def _row_aggregates(src, dst, rel, valid, rows_sorted, H, R, chunk=1 << 20):
     d = H.shape[1]
     S = np.zeros((n, R, d), F64)
     deg = np.zeros((n, R), np.int64)
-    pos = np.searchsorted(rows_sorted, dst)
-    pos_c = np.minimum(pos, n - 1)
-    hit = valid & (rows_sorted[pos_c] == dst)
-    e = np.flatnonzero(hit)
+    pos_c = _places(rows_sorted, np.where(valid, dst, 0), H.shape[0])
+    e = np.flatnonzero(valid & (pos_c >= 0))
     np.add.at(deg, (pos_c[e], rel[e]), 1)
     for s in range(0, e.shape[0], chunk):
         ec = e[s:s + chunk]
@@ -366,11 +372,10 @@ def layer_backward_rows(src, dst, rel, type_offsets, rels, params, H, S_rows, dH
     ins = S_rows[kc] == query_rows
     out[ins] += dY[kc[ins]]
     valid = valid_edges(src, dst, rel, type_offsets, rels)
-    qpos = np.searchsorted(query_rows, src)
-    qc = np.minimum(qpos, query_rows.shape[0] - 1)
-    spos = np.searchsorted(S_rows, dst)
-    sc = np.minimum(spos, S_rows.shape[0] - 1)
-    e = np.flatnonzero(valid & (query_rows[qc] == src) & (S_rows[sc] == dst))
+    N = int(type_offsets[-1])
+    qc = _places(query_rows, np.where(valid, src, 0), N)
+    sc = _places(S_rows, np.where(valid, dst, 0), N)
+    e = np.flatnonzero(valid & (qc >= 0) & (sc >= 0))
     np.add.at(out, qc[e], dMs[sc[e], rel[e]])
     return out, g
 
