@@ -56,7 +56,8 @@ typedef enum {
 } hg_status;
 
 typedef enum { HG_F32 = 0, HG_BF16 = 1 } hg_dtype;
-typedef enum { HG_ACT_RELU = 0, HG_ACT_GELU_TANH = 1, HG_ACT_NONE = 2 } hg_act;
+/* HG_ACT_SILU (x * sigmoid(x)) is taken by the gated feed-forward block (hg_ffn_*) only. */
+typedef enum { HG_ACT_RELU = 0, HG_ACT_GELU_TANH = 1, HG_ACT_NONE = 2, HG_ACT_SILU = 3 } hg_act;
 
 /* Relation r connects a source node of type src_type to a destination node of type dst_type
  * (the meta-relation triplet <tau(i), phi(e), tau(j)> of Section 2.2). */
@@ -499,6 +500,142 @@ hg_status hg_temporal_fwd(const hg_temporal_params* params, const void* X, const
 hg_status hg_temporal_bwd(const hg_temporal_params* params, const void* X, const void* C, int64_t n,
                           const void* saved, const void* dH_out, void* dX, const hg_temporal_grads* grads,
                           void* scratch, hg_stream stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* History encoder: operators over a node's whole history (a sequence of snapshots or events),   */
+/* beside the temporal module's window of w states.  The paper has no counterpart.               */
+/* Queries and keys are normed and turned by their positions (hg_qkrot_*), a causal linear        */
+/* attention with a decay for each head mixes the history (hg_decay_*: whole histories, or one    */
+/* new snapshot from a carried state), a gated feed-forward block mixes the features (hg_ffn_*).  */
+/* ------------------------------------------------------------------------------------------- */
+
+/* Heads of width d_h in {16, 32, 64, 128}, 1 to 64 of them.  A row of heads is heads * d_h contiguous
+ * values of the storage type; rows lie `stride` values apart (for hg_seq: row t of sequence i at
+ * p + i * stride_n + t * stride_t), so a slice of a wider projection row can be passed as it is.  p must
+ * be 16-byte aligned and each stride a multiple of 16 bytes, non-negative, and (for arrays written) such
+ * that no two rows overlap; a stride that no second row uses is not looked at. */
+typedef struct {
+  void* p;
+  int64_t stride;
+} hg_rows;
+typedef struct {
+  void* p;
+  int64_t stride_n;
+  int64_t stride_t;
+} hg_seq;
+
+/* Norm and rotation of queries and keys.  For each head x (d_h values) of a row at position pos:
+ *   y = x / sqrt(mean(x^2) + eps) * gamma       (gamma_q [d_h] for queries, gamma_k [d_h] for keys, storage
+ *                                                type, NULL = ones)
+ *   each pair i < rot / 2 of y is turned by the angle  pos * base^(-2 i / rot):
+ *     (a, b) -> (a cos - b sin, b cos + a sin),
+ *   a pair is (i, i + rot / 2), or (2 i, 2 i + 1) when interleaved; features from rot on are left as y.
+ * rot: a multiple of 16, 0 <= rot <= d_h (0: the norm alone).  eps > 0, base >= 1, both finite.  heads_k
+ * may differ from heads_q (queries that share keys); heads_k = 0 leaves the keys out. */
+typedef struct {
+  int32_t heads_q;
+  int32_t heads_k;
+  int32_t d_h;
+  int32_t rot;
+  int32_t interleaved;
+  hg_dtype dtype;
+  float eps;
+  double base;
+  const void* gamma_q;
+  const void* gamma_k;
+} hg_qkrot_params;
+
+/* Scratch of hg_qkrot_bwd for n rows (the forward needs none). */
+hg_status hg_qkrot_workspace_size(const hg_qkrot_params* params, int64_t n, size_t* scratch_bytes);
+
+/* q_out, k_out = normed and turned rows of q, k (n rows each).  pos: device int64 [n], or NULL for
+ * pos[i] = i; any value is taken (negative ones turn backwards), the angle is reduced exactly in 64-bit
+ * fixed point and is within 4e-7 of the definition for |pos| < 2^31.  Computed in fp32, rounded once.
+ * An output may be its own input (same pointer and stride); other overlaps are not allowed. */
+hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* q, const hg_rows* k, const int64_t* pos,
+                       int64_t n, const hg_rows* q_out, const hg_rows* k_out, hg_stream stream);
+
+/* Gradients for the upstream gradients dq_out, dk_out: dq, dk (OVERWRITTEN, may be dq_out, dk_out
+ * themselves) and dgamma_q, dgamma_k (device fp32 [d_h], OVERWRITTEN; NULL = not wanted).  q, k, pos are
+ * those of the forward (its inputs: nothing is saved).  The gains' sums have a fixed order. */
+hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* q, const hg_rows* k, const int64_t* pos,
+                       int64_t n, const hg_rows* dq_out, const hg_rows* dk_out, const hg_rows* dq,
+                       const hg_rows* dk, float* dgamma_q, float* dgamma_k, void* scratch, hg_stream stream);
+
+/* Causal linear attention with a decay for each head.  Per sequence and head, gamma = exp(log_decay[head]):
+ *   S_t = gamma S_(t-1) + k_t v_t^T   (d_h x d_h, fp32; S_(-1) = S_in, or zero),   o_t = scale q_t S_t.
+ * log_decay: device fp32 [heads], a constant of the model (no gradient); a value that is not below zero
+ * counts as 0 (no decay), one below -200 as -200. */
+typedef struct {
+  int32_t heads;
+  int32_t d_h;
+  hg_dtype dtype;
+  float scale;
+  const float* log_decay;
+} hg_decay_params;
+
+/* Scratch of hg_decay_fwd and hg_decay_bwd for n sequences of up to T positions. */
+hg_status hg_decay_workspace_size(const hg_decay_params* params, int64_t n, int64_t T, size_t* fwd_bytes,
+                                  size_t* bwd_bytes);
+
+/* Whole histories.  q, k, v, o: n sequences of T rows of heads.  lens: device int32 [n], the positions in
+ * use of each sequence (values outside [0, T] are taken as the nearer end), or NULL = T.  Rows from a
+ * sequence's length on are not read and get zero in o.  S_in, S_out: device fp32 [n][heads][d_h][d_h]
+ * (key feature x value feature); S_in NULL = zero, S_out NULL = not wanted; S_out (the state after the last
+ * position in use; S_in for an empty sequence) may be S_in itself.  o overlaps none of q, k, v. */
+hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
+                       const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* o, float* S_out,
+                       void* scratch, hg_stream stream);
+
+/* Gradients of hg_decay_fwd on the same q, k, v, lens, S_in, for the upstream gradients d_o and dS_out
+ * (NULL = zero): dq, dk, dv (OVERWRITTEN; zero rows from a sequence's length on) and dS_in (fp32,
+ * OVERWRITTEN; NULL = not wanted; may be dS_out itself).  Nothing is saved by the forward. */
+hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
+                       const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* d_o,
+                       const float* dS_out, const hg_seq* dq, const hg_seq* dk, const hg_seq* dv, float* dS_in,
+                       void* scratch, hg_stream stream);
+
+/* One new snapshot of n nodes: S_out = gamma S_in + k v^T and o = scale q S_out per node and head (rows
+ * and states as above; one row a node).  live: device int32 [n] or NULL; a node whose entry is not
+ * positive keeps its state and gets a zero row.  S_out may be S_in (updated in place). */
+hg_status hg_decay_step(const hg_decay_params* params, const hg_rows* q, const hg_rows* k, const hg_rows* v,
+                        const int32_t* live, int64_t n, const float* S_in, const hg_rows* o, float* S_out,
+                        hg_stream stream);
+
+/* Gated feed-forward block, device pointers of the storage type: W_gate, W_up [d x f], W_down [f x d]
+ * (input x output, row-major, 16-byte aligned); d in {64, 128, 256}, f a positive multiple of 8 up to
+ * 16384; residual != 0 adds X:
+ *   Y = (act(X W_gate) * (X W_up)) W_down (+ X). */
+typedef struct {
+  int32_t d;
+  int32_t f;
+  hg_dtype dtype;
+  hg_act act;
+  int32_t residual;
+  const void* W_gate;
+  const void* W_up;
+  const void* W_down;
+} hg_ffn_params;
+
+/* Gradients, device fp32, OVERWRITTEN: dW_gate, dW_up [d x f], dW_down [f x d]. */
+typedef struct {
+  float* dW_gate;
+  float* dW_up;
+  float* dW_down;
+} hg_ffn_grads;
+
+/* Scratch of hg_ffn_fwd and hg_ffn_bwd for n rows. */
+hg_status hg_ffn_workspace_size(const hg_ffn_params* params, int64_t n, size_t* fwd_bytes, size_t* bwd_bytes);
+
+/* X, Y: n x d, row-major, storage type, 16-byte aligned; Y does not overlap X. */
+hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int64_t n, void* Y, void* scratch,
+                     hg_stream stream);
+
+/* Gradients for the upstream gradient dY (n x d): dX (n x d, OVERWRITTEN; NULL = skip; overlaps neither X
+ * nor dY) and the weights' (grads NULL = skip).  The hidden rows are formed again from X: nothing is
+ * saved by the forward.  Sums over rows have a fixed order. */
+hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
+                     const hg_ffn_grads* grads, void* scratch, hg_stream stream);
 
 /* ------------------------------------------------------------------------------------------- */
 /* Kernel timing (measurement support; off by default)                                          */

@@ -1,0 +1,507 @@
+// Causal linear attention with a decay for each head: entry points, the CUDA-core scan (fp32 storage), the
+// join of segments, and the step of one snapshot.
+//
+//   S_t = gamma S_(t-1) + k_t v_t^T,  o_t = c q_t S_t;  the gradients are three scans of the same form
+//   (decay_kernels.cuh).
+//
+// CUDA-core scan: a lane owns one value feature of a head, so its column of the state (d_h numbers) stays in
+// registers and o_t needs no exchange; the keys and queries of a few positions are laid in shared memory
+// for their warp, where all lanes read the same 16 bytes at once.  2 d_h FMA a position and lane: at d_h = 32
+// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it.
+// Long histories of few sequences: the histories are cut into segments; a first pass finds each segment's own
+// state, a join runs through them, and the scan then starts each segment from its true state.
+//
+// The step reads and writes the state once (16-byte rows of it across the lanes): bound by HBM.
+#include <algorithm>
+
+#include "decay_kernels.cuh"
+
+namespace hg {
+
+namespace {
+
+constexpr int kMaxHeads = 64;
+constexpr int kWarps = 4;
+constexpr int kSms = 152;
+
+template <int DH>
+struct SimtCfg {
+  static constexpr int W = DH < 32 ? 32 : DH;     // values of a staged row: the heads of 32 columns
+  static constexpr int TC = DH <= 32 ? 16 : 8;    // positions staged at a time
+};
+
+// blockIdx.x * kWarps + warp = ((sequence * nseg) + segment) * column blocks + column block
+template <typename T, int DH, bool kLocal>
+__global__ void __launch_bounds__(32 * kWarps) scan_simt(ScanArgs a) {
+  pdl_begin();
+  using C = SimtCfg<DH>;
+  constexpr int W = C::W, TC = C::TC, VEC = VecTraits<T>::kElems;
+  __shared__ __align__(16) float sk[kWarps][TC][W];
+  __shared__ __align__(16) float sq[kLocal ? 1 : kWarps][kLocal ? 1 : TC][W];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int width = a.heads * DH;
+  const int ncb = (width + 31) / 32;
+  const int64_t item = (int64_t)blockIdx.x * kWarps + warp;
+  const int64_t seq = item / (ncb * a.nseg);
+  if (seq >= a.n) return;
+  const int cb = (int)(item % ncb), segi = (int)(item / ncb % a.nseg);
+  const int col = cb * 32 + lane;
+  const bool on = col < width;
+  const int head = on ? col / DH : a.heads - 1, j = col % DH;
+  const int row0 = cb * 32 / DH * DH;                 // first staged value of a row
+  const int rw = min(W, width - row0);                // staged values of a row (a multiple of 16)
+  const int hoff = on ? (head * DH - row0) : 0;       // this lane's head within them
+  const int64_t len = scan_len(a, seq);
+  const int64_t t0 = segi * a.seg_len;
+  const int64_t tend = min(t0 + a.seg_len, a.T);
+  const int64_t t1 = min(tend, len);
+  if (kLocal && segi == a.nseg - 1) return;
+  const float ld = clamp_ld(a.ld[head]);
+  float S[DH];
+#pragma unroll
+  for (int i = 0; i < DH; ++i) S[i] = 0.f;
+  const int64_t st0 = (seq * a.heads + head) * (int64_t)DH * DH;
+  if (!kLocal && on) {
+    if (a.nseg > 1) {
+      const float* src = a.seg + ((seq * a.heads + head) * a.nseg + segi) * (int64_t)DH * DH + j;
+#pragma unroll
+      for (int i = 0; i < DH; ++i) S[i] = src[i * DH];
+    } else if (a.init) {
+#pragma unroll
+      for (int i = 0; i < DH; ++i) S[i] = a.init[st0 + (a.init_t ? j * DH + i : i * DH + j)];
+    }
+  }
+  int base = 0;  // frame base, in positions from t0
+  const T* qp = static_cast<const T*>(a.q.p) + seq * a.q.sn + row0;
+  const T* kp = static_cast<const T*>(a.k.p) + seq * a.k.sn + row0;
+  const T* vp = static_cast<const T*>(a.v.p) + seq * a.v.sn;
+  T* op = static_cast<T*>(const_cast<void*>(a.o.p)) + seq * a.o.sn;
+  for (int64_t tc = t0; tc < t1; tc += TC) {
+    const int m = (int)min((int64_t)TC, t1 - tc);
+    __syncwarp();
+    for (int x = lane; x < m * (rw / VEC); x += 32) {
+      const int r = x / (rw / VEC), c = x % (rw / VEC) * VEC;
+      const int64_t t = a.reverse ? len - 1 - (tc + r) : tc + r;
+      float f[VEC];
+      unpack(ld16(kp + t * a.k.st + c), f, T());
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sk[warp][r][c + e] = f[e];
+      if (!kLocal) {
+        unpack(ld16(qp + t * a.q.st + c), f, T());
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sq[warp][r][c + e] = f[e];
+      }
+    }
+    float v[TC];
+#pragma unroll
+    for (int r = 0; r < TC; ++r) {
+      const int64_t t = a.reverse ? len - 1 - (tc + r) : tc + r;
+      v[r] = on && r < m ? to_f32(vp[t * a.v.st + col]) : 0.f;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < TC; ++r) {
+      if (r >= m) break;
+      const int64_t t = tc + r;
+      const int tau = (int)(t - t0) + a.shift;
+      const bool move = (float)(base - tau) * ld > kFrame;
+      if (__any_sync(0xffffffffu, move)) {
+        const float g = move ? expf(ld * (float)(tau - base)) : 1.f;
+#pragma unroll
+        for (int i = 0; i < DH; ++i) S[i] *= g;
+        if (move) base = tau;
+      }
+      const float vin = a.c_in * expf(ld * (float)(base - tau)) * v[r];
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int i = 0; i < DH; i += 4) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&sk[warp][r][hoff + i]);
+        S[i] = fmaf(k4.x, vin, S[i]);
+        S[i + 1] = fmaf(k4.y, vin, S[i + 1]);
+        S[i + 2] = fmaf(k4.z, vin, S[i + 2]);
+        S[i + 3] = fmaf(k4.w, vin, S[i + 3]);
+        if (!kLocal) {
+          const float4 q4 = *reinterpret_cast<const float4*>(&sq[warp][r][hoff + i]);
+          s0 = fmaf(q4.x, S[i], s0);
+          s1 = fmaf(q4.y, S[i + 1], s1);
+          s0 = fmaf(q4.z, S[i + 2], s0);
+          s1 = fmaf(q4.w, S[i + 3], s1);
+        }
+      }
+      if (!kLocal && on) {
+        const int64_t row = a.reverse ? len - 1 - t : t;
+        op[row * a.o.st + col] = from_f32<T>(a.c_out * expf(ld * (float)(tau - base)) * (s0 + s1));
+      }
+    }
+  }
+  if (!kLocal && on)
+    for (int64_t t = max(t0, len); t < tend; ++t) op[t * a.o.st + col] = from_f32<T>(0.f);
+  if (!on) return;
+  const float g = expf(ld * (float)((int)(max(t1, t0) - t0) - base));
+  if (kLocal) {
+    float* dst = a.seg + ((seq * a.heads + head) * a.nseg + segi) * (int64_t)DH * DH + j;
+#pragma unroll
+    for (int i = 0; i < DH; ++i) dst[i * DH] = S[i] * g;
+  } else if (a.last && segi == (len > 0 ? (len - 1) / a.seg_len : 0)) {
+#pragma unroll
+    for (int i = 0; i < DH; ++i) a.last[st0 + i * DH + j] = S[i] * g;
+  }
+}
+
+// seg[s] (segment s's own state, for s < nseg - 1) -> the state at segment s's start: one thread an element.
+__global__ void __launch_bounds__(256) scan_join(ScanArgs a, int dh) {
+  pdl_begin();
+  const int64_t dd = (int64_t)dh * dh, total = a.n * a.heads * dd;
+  const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (x >= total) return;
+  const int64_t sh = x / dd, e = x % dd, i = e / dh, j = e % dh;
+  const int64_t len = scan_len(a, sh / a.heads);
+  const float ld = clamp_ld(a.ld[sh % a.heads]);
+  float run = a.init ? a.init[sh * dd + (a.init_t ? j * dh + i : e)] : 0.f;
+  float* seg = a.seg + sh * a.nseg * dd + e;
+  for (int s = 0; s < a.nseg; ++s) {
+    const float own = s + 1 < a.nseg ? seg[s * dd] : 0.f;
+    seg[s * dd] = run;
+    const int64_t m = min(a.seg_len, max(len - s * a.seg_len, (int64_t)0));
+    run = fmaf(run, expf(ld * (float)m), own);
+  }
+}
+
+// One row a node.  A warp takes one head: DH / 4 lanes (32 of them hold 4 columns each at DH = 128) span a row
+// of the state, the others the next rows, and the rows' sums meet by shuffles.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q, int64_t sq, const T* __restrict__ k,
+                                                         int64_t sk, const T* __restrict__ v, int64_t sv,
+                                                         const int32_t* __restrict__ live, const float* __restrict__ ld,
+                                                         int64_t n, int heads, float scale, const float* S_in, T* o,
+                                                         int64_t so, float* S_out) {
+  pdl_begin();
+  constexpr int LR = DH / 4;       // lanes of a row
+  constexpr int RW = 32 / LR;      // rows at a time
+  constexpr int NR = DH / RW;      // rounds
+  constexpr int U = NR < 8 ? NR : 8;
+  const int lane = threadIdx.x & 31;
+  const int64_t item = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  if (item >= n * heads) return;
+  const int64_t i = item / heads;
+  const int h = (int)(item % heads);
+  const int c = lane % LR * 4, r0 = lane / LR;
+  const float* src = S_in + item * (DH * DH) + c;
+  float* dst = S_out + item * (DH * DH) + c;
+  T* orow = o + i * so + h * DH;
+  if (live && live[i] <= 0) {
+    if (S_in != S_out)
+      for (int r = r0; r < DH; r += RW)
+        *reinterpret_cast<float4*>(dst + r * DH) = *reinterpret_cast<const float4*>(src + r * DH);
+    for (int x = lane; x < DH; x += 32) orow[x] = from_f32<T>(0.f);
+    return;
+  }
+  const float g = expf(clamp_ld(ld[h]));
+  const T* qr = q + i * sq + h * DH;
+  const T* kr = k + i * sk + h * DH;
+  const T* vr = v + i * sv + h * DH + c;
+  const float4 vv = make_float4(to_f32(vr[0]), to_f32(vr[1]), to_f32(vr[2]), to_f32(vr[3]));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int b = 0; b < NR; b += U) {
+    float4 s[U];
+    float kk[U], qq[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = (b + u) * RW + r0;
+      s[u] = *reinterpret_cast<const float4*>(src + r * DH);
+      kk[u] = to_f32(kr[r]);
+      qq[u] = to_f32(qr[r]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = (b + u) * RW + r0;
+      float4 y = s[u];
+      y.x = fmaf(kk[u], vv.x, g * y.x);
+      y.y = fmaf(kk[u], vv.y, g * y.y);
+      y.z = fmaf(kk[u], vv.z, g * y.z);
+      y.w = fmaf(kk[u], vv.w, g * y.w);
+      *reinterpret_cast<float4*>(dst + r * DH) = y;
+      acc.x = fmaf(qq[u], y.x, acc.x);
+      acc.y = fmaf(qq[u], y.y, acc.y);
+      acc.z = fmaf(qq[u], y.z, acc.z);
+      acc.w = fmaf(qq[u], y.w, acc.w);
+    }
+  }
+#pragma unroll
+  for (int x = LR; x < 32; x <<= 1) {
+    acc.x += __shfl_xor_sync(0xffffffffu, acc.x, x);
+    acc.y += __shfl_xor_sync(0xffffffffu, acc.y, x);
+    acc.z += __shfl_xor_sync(0xffffffffu, acc.z, x);
+    acc.w += __shfl_xor_sync(0xffffffffu, acc.w, x);
+  }
+  if (lane < LR) {
+    orow[c] = from_f32<T>(scale * acc.x);
+    orow[c + 1] = from_f32<T>(scale * acc.y);
+    orow[c + 2] = from_f32<T>(scale * acc.z);
+    orow[c + 3] = from_f32<T>(scale * acc.w);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------
+int scan_warps(const hg_decay_params* p) { return (p->heads * p->d_h + 31) / 32; }
+
+// Segments: as many as fill the GPU with warps (16 an SM), none shorter than kMinSeg positions, where the
+// second reading of keys and values costs more than the warps gain.
+constexpr int64_t kMinSeg = 256;
+void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int* nseg, int64_t* seg_len) {
+  const int64_t warps = std::max<int64_t>(n, 1) * scan_warps(p);
+  const int64_t want = std::min<int64_t>(kSms * 16 / warps, T / kMinSeg);
+  *nseg = 1;
+  *seg_len = std::max<int64_t>(T, 1);
+  if (want < 2) return;
+  *seg_len = (int64_t)align_up((size_t)ceil_div(T, want), 16);
+  *nseg = (int)ceil_div(T, *seg_len);
+}
+
+template <typename T, int DH>
+hg_status scan_simt_t(const ScanArgs& a, bool local, cudaStream_t s) {
+  const int64_t items = a.n * a.nseg * (int64_t)((a.heads * DH + 31) / 32);
+  const dim3 grid((unsigned)ceil_div(items, kWarps));
+  if (local) return launch("decay_scan_local", scan_simt<T, DH, true>, grid, dim3(32 * kWarps), 0, s, a);
+  return launch("decay_scan", scan_simt<T, DH, false>, grid, dim3(32 * kWarps), 0, s, a);
+}
+
+template <typename T>
+hg_status scan_pass(const ScanArgs& a, int dh, bool local, cudaStream_t s) {
+  if (dh == 16) return scan_simt_t<T, 16>(a, local, s);
+  if (dh == 32) return scan_simt_t<T, 32>(a, local, s);
+  if (dh == 64) return scan_simt_t<T, 64>(a, local, s);
+  return scan_simt_t<T, 128>(a, local, s);
+}
+
+hg_status scan_dtype(const ScanArgs& a, const hg_decay_params* p, bool local, cudaStream_t s) {
+  if (p->dtype == HG_F32) return scan_pass<float>(a, p->d_h, local, s);
+  return scan_pass<__nv_bfloat16>(a, p->d_h, local, s);
+}
+
+hg_status scan(const ScanArgs& a, const hg_decay_params* p, cudaStream_t s) {
+  if (a.nseg > 1) {
+    HG_TRY(scan_dtype(a, p, true, s));
+    HG_TRY(launch("decay_scan_join", scan_join,
+                  dim3((unsigned)ceil_div(a.n * a.heads * (int64_t)p->d_h * p->d_h, 256)), dim3(256), 0, s, a, p->d_h));
+  }
+  return scan_dtype(a, p, false, s);
+}
+
+hg_status check_params(const hg_decay_params* p, int64_t n, int64_t T) {
+  HG_REQUIRE(p != nullptr, "params must be non-null");
+  if (!(p->d_h == 16 || p->d_h == 32 || p->d_h == 64 || p->d_h == 128) ||
+      !(p->dtype == HG_F32 || p->dtype == HG_BF16)) {
+    set_error("unsupported d_h=%d / dtype=%d", p->d_h, (int)p->dtype);
+    return HG_ERR_UNSUPPORTED;
+  }
+  HG_REQUIRE(p->heads >= 1 && p->heads <= kMaxHeads, "heads must be in [1, %d]", kMaxHeads);
+  HG_REQUIRE(n >= 0 && n * p->heads < (int64_t(1) << 28), "n * heads must be in [0, 2^28)");
+  HG_REQUIRE(T >= 0 && T < (int64_t(1) << 30), "T must be in [0, 2^30)");
+  return HG_OK;
+}
+
+hg_status check_seq(const hg_seq* r, const char* name, int64_t n, int64_t T, int64_t width, size_t esz, bool written) {
+  HG_REQUIRE(r != nullptr && r->p != nullptr, "%s must be non-null", name);
+  HG_REQUIRE(((uintptr_t)r->p & 15) == 0, "%s must be 16-byte aligned", name);
+  const int64_t lim = int64_t(1) << 40, st = r->stride_t, sn = r->stride_n, u = 16 / (int64_t)esz;
+  HG_REQUIRE(T < 2 || (st >= 0 && st < lim && st % u == 0),
+             "%s: stride_t must be a non-negative multiple of 16 bytes", name);
+  HG_REQUIRE(n < 2 || (sn >= 0 && sn < lim && sn % u == 0),
+             "%s: stride_n must be a non-negative multiple of 16 bytes", name);
+  if (written) {  // rows nest: positions within sequences, or sequences within positions
+    const bool ok_t = T < 2 || st >= width, ok_n = n < 2 || sn >= width;
+    const bool nest = n < 2 || T < 2 || sn >= (T - 1) * st + width || st >= (n - 1) * sn + width;
+    HG_REQUIRE(ok_t && ok_n && nest, "%s: rows that are written must not overlap", name);
+  }
+  return HG_OK;
+}
+
+hg_status check_buffers(const hg_decay_params* p, const void* scratch, bool needed) {
+  HG_REQUIRE(p->log_decay != nullptr, "log_decay must be non-null");
+  HG_REQUIRE(!needed || scratch != nullptr, "scratch must be non-null");
+  HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
+  return HG_OK;
+}
+
+ScanRows rows_of(const hg_seq* r, int64_t n, int64_t T) {
+  return {r->p, n < 2 ? 0 : r->stride_n, T < 2 ? 0 : r->stride_t};
+}
+
+size_t seg_bytes(const hg_decay_params* p, int64_t n, int64_t T) {
+  int nseg;
+  int64_t seg_len;
+  plan_segments(p, n, T, &nseg, &seg_len);
+  return nseg > 1 ? align_up(sizeof(float) * (size_t)n * p->heads * nseg * p->d_h * p->d_h) : 0;
+}
+
+}  // namespace
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" hg_status hg_decay_workspace_size(const hg_decay_params* params, int64_t n, int64_t T, size_t* fwd_bytes,
+                                             size_t* bwd_bytes) {
+  clear_error();
+  HG_REQUIRE(fwd_bytes && bwd_bytes, "fwd_bytes and bwd_bytes must be non-null");
+  HG_TRY(check_params(params, n, T));
+  *fwd_bytes = *bwd_bytes = seg_bytes(params, n, T);
+  return HG_OK;
+}
+
+extern "C" hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
+                                  const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* o,
+                                  float* S_out, void* scratch, hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check_params(params, n, T));
+  const size_t need = seg_bytes(params, n, T);
+  HG_TRY(check_buffers(params, scratch, need > 0));
+  if (n == 0) return HG_OK;
+  const size_t esz = params->dtype == HG_BF16 ? 2 : 4;
+  const int64_t w = (int64_t)params->heads * params->d_h;
+  ScanArgs a{};
+  if (T > 0) {
+    HG_TRY(check_seq(q, "q", n, T, w, esz, false));
+    HG_TRY(check_seq(k, "k", n, T, w, esz, false));
+    HG_TRY(check_seq(v, "v", n, T, w, esz, false));
+    HG_TRY(check_seq(o, "o", n, T, w, esz, true));
+    a.q = rows_of(q, n, T);
+    a.k = rows_of(k, n, T);
+    a.v = rows_of(v, n, T);
+    a.o = rows_of(o, n, T);
+  }
+  a.lens = lens;
+  a.ld = params->log_decay;
+  a.init = S_in;
+  a.last = S_out;
+  a.seg = static_cast<float*>(scratch);
+  a.n = n;
+  a.T = T;
+  plan_segments(params, n, T, &a.nseg, &a.seg_len);
+  a.heads = params->heads;
+  a.shift = 1;
+  a.c_in = 1.f;
+  a.c_out = params->scale;
+  return scan(a, params, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
+                                  const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* d_o,
+                                  const float* dS_out, const hg_seq* dq, const hg_seq* dk, const hg_seq* dv,
+                                  float* dS_in, void* scratch, hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check_params(params, n, T));
+  const size_t need = seg_bytes(params, n, T);
+  HG_TRY(check_buffers(params, scratch, need > 0));
+  if (n == 0) return HG_OK;
+  const size_t esz = params->dtype == HG_BF16 ? 2 : 4;
+  const int64_t w = (int64_t)params->heads * params->d_h;
+  ScanArgs a{};
+  ScanRows rq{}, rk{}, rv{}, ro{}, gq{}, gk{}, gv{};
+  if (T > 0) {
+    HG_TRY(check_seq(q, "q", n, T, w, esz, false));
+    HG_TRY(check_seq(k, "k", n, T, w, esz, false));
+    HG_TRY(check_seq(v, "v", n, T, w, esz, false));
+    HG_TRY(check_seq(d_o, "d_o", n, T, w, esz, false));
+    HG_TRY(check_seq(dq, "dq", n, T, w, esz, true));
+    HG_TRY(check_seq(dk, "dk", n, T, w, esz, true));
+    HG_TRY(check_seq(dv, "dv", n, T, w, esz, true));
+    rq = rows_of(q, n, T);
+    rk = rows_of(k, n, T);
+    rv = rows_of(v, n, T);
+    ro = rows_of(d_o, n, T);
+    gq = rows_of(dq, n, T);
+    gk = rows_of(dk, n, T);
+    gv = rows_of(dv, n, T);
+  }
+  a.lens = lens;
+  a.ld = params->log_decay;
+  a.seg = static_cast<float*>(scratch);
+  a.n = n;
+  a.T = T;
+  plan_segments(params, n, T, &a.nseg, &a.seg_len);
+  a.heads = params->heads;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  // dq
+  a.q = ro;
+  a.k = rv;
+  a.v = rk;
+  a.o = gq;
+  a.init = S_in;
+  a.init_t = 1;
+  a.last = nullptr;
+  a.shift = 1;
+  a.c_in = 1.f;
+  a.c_out = params->scale;
+  if (T > 0) HG_TRY(scan(a, params, s));
+  // dk (before dv, whose run may overwrite dS_out with dS_in)
+  a.q = rv;
+  a.k = ro;
+  a.v = rq;
+  a.o = gk;
+  a.init = dS_out;
+  a.shift = 0;
+  a.reverse = 1;
+  a.c_in = params->scale;
+  a.c_out = 1.f;
+  if (T > 0) HG_TRY(scan(a, params, s));
+  a.q = rk;
+  a.k = rq;
+  a.v = ro;
+  a.o = gv;
+  a.init_t = 0;
+  a.last = dS_in;
+  return scan(a, params, s);
+}
+
+namespace hg {
+namespace {
+
+template <typename T, int DH>
+hg_status step_t(const hg_decay_params* p, const hg_rows* q, const hg_rows* k, const hg_rows* v, const int32_t* live,
+                 int64_t n, const float* S_in, const hg_rows* o, float* S_out, cudaStream_t s) {
+  return launch("decay_step", decay_step_kernel<T, DH>, dim3((unsigned)ceil_div(n * p->heads, 8)), dim3(256), 0, s,
+                (const T*)q->p, q->stride, (const T*)k->p, k->stride, (const T*)v->p, v->stride, live, p->log_decay, n,
+                p->heads, p->scale, S_in, (T*)o->p, o->stride, S_out);
+}
+
+template <typename T>
+hg_status step_w(const hg_decay_params* p, const hg_rows* q, const hg_rows* k, const hg_rows* v, const int32_t* live,
+                 int64_t n, const float* S_in, const hg_rows* o, float* S_out, cudaStream_t s) {
+  if (p->d_h == 16) return step_t<T, 16>(p, q, k, v, live, n, S_in, o, S_out, s);
+  if (p->d_h == 32) return step_t<T, 32>(p, q, k, v, live, n, S_in, o, S_out, s);
+  if (p->d_h == 64) return step_t<T, 64>(p, q, k, v, live, n, S_in, o, S_out, s);
+  return step_t<T, 128>(p, q, k, v, live, n, S_in, o, S_out, s);
+}
+
+}  // namespace
+}  // namespace hg
+
+extern "C" hg_status hg_decay_step(const hg_decay_params* params, const hg_rows* q, const hg_rows* k, const hg_rows* v,
+                                   const int32_t* live, int64_t n, const float* S_in, const hg_rows* o, float* S_out,
+                                   hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check_params(params, n, 1));
+  HG_REQUIRE(params->log_decay != nullptr, "log_decay must be non-null");
+  if (n == 0) return HG_OK;
+  const size_t esz = params->dtype == HG_BF16 ? 2 : 4;
+  const int64_t w = (int64_t)params->heads * params->d_h;
+  const hg_rows* in[4] = {q, k, v, o};
+  const char* names[4] = {"q", "k", "v", "o"};
+  for (int x = 0; x < 4; ++x) {
+    HG_REQUIRE(in[x] != nullptr, "%s must be non-null", names[x]);
+    const hg_seq r{in[x]->p, in[x]->stride, 0};
+    HG_TRY(check_seq(&r, names[x], n, 1, w, esz, x == 3));
+  }
+  HG_REQUIRE(S_in && S_out, "S_in and S_out must be non-null");
+  HG_REQUIRE((((uintptr_t)S_in | (uintptr_t)S_out) & 15) == 0, "S_in and S_out must be 16-byte aligned");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (params->dtype == HG_F32) return step_w<float>(params, q, k, v, live, n, S_in, o, S_out, s);
+  return step_w<__nv_bfloat16>(params, q, k, v, live, n, S_in, o, S_out, s);
+}

@@ -1,0 +1,391 @@
+// Gated feed-forward block: entry points and the CUDA-core path (fp32 storage).
+//
+//   G = X W_gate, U = X W_up, H = act(G) * U, Y = H W_down (+ X)
+//   dH = dY W_down^T, dG = dH * U * act'(G), dU = dH * act(G)
+//   dX = dG W_gate^T + dU W_up^T (+ dY), dW_gate = X^T dG, dW_up = X^T dU, dW_down = H^T dY
+//
+// CUDA-core path: 128 x 64 tiles, 8 x 4 results a thread, operands in shared memory by k; the two
+// projections (and dH) share a pass over k, their gate is applied to the sums in registers, and H, dG and dU
+// go to scratch.  The weights' gradients split the rows; the splits are added in order.  Bound by the FMA rate.
+#include <algorithm>
+
+#include "ffn_kernels.cuh"
+#include "layer_kernels.cuh"
+
+namespace hg {
+
+namespace {
+
+constexpr int kBm = 128, kBn = 64, kBk = 16, kThr = 256;
+constexpr int kSms = 152;
+constexpr int kMaxF = 16384;
+
+// One operand as the tile loaders see it: element (r, c) at p[r * ld + c], rows r < nr, columns c < nc.
+template <typename T>
+struct Mat {
+  const T* p;
+  int64_t ld, nr, nc;
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) {
+  return *reinterpret_cast<const float4*>(p);
+}
+template <>
+__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                     __uint_as_float(v.y & 0xffff0000u));
+}
+
+// dst[k][x] for kBk of k and X of x (row stride X + 4) from an operand whose rows are x and columns k
+// (kByRow) or whose rows are k and columns x.  Zero outside.  nr, nc and the starts are such that four
+// neighbouring columns are all inside or all outside.
+template <typename T, int X, bool kByRow>
+__device__ __forceinline__ void stage(float* dst, const Mat<T>& a, int64_t x0, int64_t k0) {
+  constexpr int PER = X * kBk / 4 / kThr;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x + i * kThr;
+    const int r = kByRow ? e / (kBk / 4) : e / (X / 4);
+    const int c = (kByRow ? e % (kBk / 4) : e % (X / 4)) * 4;
+    const int64_t row = (kByRow ? x0 : k0) + r, col = (kByRow ? k0 : x0) + c;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row < a.nr && col < a.nc) v = load4(a.p + row * a.ld + col);
+    if (kByRow) {
+      dst[(c + 0) * (X + 4) + r] = v.x;
+      dst[(c + 1) * (X + 4) + r] = v.y;
+      dst[(c + 2) * (X + 4) + r] = v.z;
+      dst[(c + 3) * (X + 4) + r] = v.w;
+    } else {
+      *reinterpret_cast<float4*>(dst + r * (X + 4) + c) = v;
+    }
+  }
+}
+
+struct Acc {
+  float v[8][4];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+  }
+};
+
+// thread (ty, tx) holds rows ty * 4 + {0..3}, 64 + ty * 4 + {0..3} and columns tx * 4 + {0..3}
+__device__ __forceinline__ int acc_row(int i) { return (i < 4 ? 0 : 64) + (threadIdx.x / 16) * 4 + (i & 3); }
+
+__device__ __forceinline__ void mul(const float* A, const float* B, Acc& acc) {
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+#pragma unroll
+  for (int k = 0; k < kBk; ++k) {
+    const float4 a0 = *reinterpret_cast<const float4*>(A + k * (kBm + 4) + ty * 4);
+    const float4 a1 = *reinterpret_cast<const float4*>(A + k * (kBm + 4) + 64 + ty * 4);
+    const float4 b = *reinterpret_cast<const float4*>(B + k * (kBn + 4) + tx * 4);
+    const float av[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+    const float bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc.v[i][j] = fmaf(av[i], bv[j], acc.v[i][j]);
+  }
+}
+
+// H = act(X W_gate) * (X W_up), a tile a block, the column tiles of a row tile one after another; with kBwd also
+// dH = dY W_down^T, and dG, dU.
+template <typename T, int kAct, bool kBwd>
+__global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat<T> X, Mat<T> Wg, Mat<T> Wu, Mat<T> dY, Mat<T> Wd,
+                                                        float* __restrict__ H, float* __restrict__ dG,
+                                                        float* __restrict__ dU) {
+  pdl_begin();
+  __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)], Cs[kBk * (kBn + 4)];
+  __shared__ __align__(16) float Ds[kBwd ? kBk * (kBm + 4) : 4], Es[kBwd ? kBk * (kBn + 4) : 4];
+  const int ctiles = (int)((Wg.nc + kBn - 1) / kBn);
+  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * kBm, c0 = (int64_t)(blockIdx.x % ctiles) * kBn;
+  Acc g, u, h;
+  g.zero();
+  u.zero();
+  h.zero();
+  for (int64_t k0 = 0; k0 < X.nc; k0 += kBk) {
+    stage<T, kBm, true>(As, X, r0, k0);
+    stage<T, kBn, false>(Bs, Wg, c0, k0);
+    stage<T, kBn, false>(Cs, Wu, c0, k0);
+    if (kBwd) {
+      stage<T, kBm, true>(Ds, dY, r0, k0);
+      stage<T, kBn, true>(Es, Wd, c0, k0);
+    }
+    __syncthreads();
+    mul(As, Bs, g);
+    mul(As, Cs, u);
+    if (kBwd) mul(Ds, Es, h);
+    __syncthreads();
+  }
+  const int64_t col = c0 + threadIdx.x % 16 * 4;
+  if (col >= Wg.nc) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = r0 + acc_row(i);
+    if (row >= X.nr) continue;
+    float hv[4], gv[4], uv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (kBwd) {
+        float d;
+        const float a = gate_grad<kAct>(g.v[i][j], &d);
+        hv[j] = a * u.v[i][j];
+        gv[j] = h.v[i][j] * u.v[i][j] * d;
+        uv[j] = h.v[i][j] * a;
+      } else {
+        hv[j] = gate<kAct>(g.v[i][j]) * u.v[i][j];
+      }
+    }
+    const int64_t at = row * Wg.nc + col;
+    *reinterpret_cast<float4*>(H + at) = make_float4(hv[0], hv[1], hv[2], hv[3]);
+    if (kBwd) {
+      *reinterpret_cast<float4*>(dG + at) = make_float4(gv[0], gv[1], gv[2], gv[3]);
+      *reinterpret_cast<float4*>(dU + at) = make_float4(uv[0], uv[1], uv[2], uv[3]);
+    }
+  }
+}
+
+// out = A B (+ A2 B2) (+ add): the second product when A2.p is set; kTransB: B given by its transpose.
+template <typename T, bool kTransB>
+__global__ void __launch_bounds__(kThr) ffn_out_simt(Mat<float> A, Mat<T> B, Mat<float> A2, Mat<T> B2, const T* add,
+                                                     T* __restrict__ out, int64_t nc) {
+  pdl_begin();
+  __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
+  const int ctiles = (int)((nc + kBn - 1) / kBn);
+  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * kBm, c0 = (int64_t)(blockIdx.x % ctiles) * kBn;
+  Acc acc;
+  acc.zero();
+  for (int half = 0; half < (A2.p ? 2 : 1); ++half) {
+    for (int64_t k0 = 0; k0 < A.nc; k0 += kBk) {
+      stage<float, kBm, true>(As, half ? A2 : A, r0, k0);
+      stage<T, kBn, kTransB>(Bs, half ? B2 : B, c0, k0);
+      __syncthreads();
+      mul(As, Bs, acc);
+      __syncthreads();
+    }
+  }
+  const int64_t col = c0 + threadIdx.x % 16 * 4;
+  if (col >= nc) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = r0 + acc_row(i);
+    if (row >= A.nr) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t at = row * nc + col + j;
+      out[at] = from_f32<T>(acc.v[i][j] + (add ? to_f32(add[at]) : 0.f));
+    }
+  }
+}
+
+// part[blockIdx.z] = A^T B over the split's rows (A: rows x mc, B: rows x nc).
+template <typename TA, typename TB>
+__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat<TA> A, Mat<TB> B, int64_t rows, float* __restrict__ part) {
+  pdl_begin();
+  __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
+  const int64_t m0 = (int64_t)blockIdx.y * kBm, c0 = (int64_t)blockIdx.x * kBn;
+  const int64_t k1 = min(A.nr, (int64_t)(blockIdx.z + 1) * rows);
+  Mat<TA> Ae = A;
+  Mat<TB> Be = B;
+  Ae.nr = Be.nr = k1;
+  Acc acc;
+  acc.zero();
+  for (int64_t k0 = (int64_t)blockIdx.z * rows; k0 < k1; k0 += kBk) {
+    stage<TA, kBm, false>(As, Ae, m0, k0);
+    stage<TB, kBn, false>(Bs, Be, c0, k0);
+    __syncthreads();
+    mul(As, Bs, acc);
+    __syncthreads();
+  }
+  const int64_t col = c0 + threadIdx.x % 16 * 4;
+  if (col >= B.nc) return;
+  float* out = part + blockIdx.z * A.nc * B.nc;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t m = m0 + acc_row(i);
+    if (m < A.nc)
+      *reinterpret_cast<float4*>(out + m * B.nc + col) =
+          make_float4(acc.v[i][0], acc.v[i][1], acc.v[i][2], acc.v[i][3]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------
+// Splits of the rows: tiles enough for two waves, none shorter than 256 rows.
+int wg_splits(int64_t n, int d, int f) {
+  const int64_t tiles = ceil_div(d, kBm) * ceil_div(f, kBn);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(2 * kSms, tiles), n / 256));
+}
+
+struct FfnLayout {
+  float* H;
+  float* dG;
+  float* dU;
+  float* part;
+  float* tmp;
+};
+
+void carve_simt(void* scratch, const hg_ffn_params* p, int64_t n, bool bwd, FfnLayout* L, size_t* bytes) {
+  Carve k(scratch);
+  const size_t nf = (size_t)std::max<int64_t>(n, 1) * p->f;
+  *L = FfnLayout{};
+  L->H = k.take<float>(nf);
+  if (bwd) {
+    L->dG = k.take<float>(nf);
+    L->dU = k.take<float>(nf);
+    const int sp = wg_splits(n, p->d, p->f);
+    L->part = k.take<float>((size_t)sp * p->d * p->f);
+    L->tmp = k.take<float>(reduce_tmp_floats(sp, (int64_t)p->d * p->f));
+  }
+  if (bytes) *bytes = k.used;
+}
+
+template <typename T, int kAct, bool kBwd>
+hg_status hidden(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, const FfnLayout& L, cudaStream_t s) {
+  const int64_t d = p->d, f = p->f;
+  const Mat<T> x{(const T*)X, d, n, d}, g{(const T*)p->W_gate, f, d, f}, u{(const T*)p->W_up, f, d, f},
+      dy{(const T*)dY, d, n, d}, w{(const T*)p->W_down, d, f, d};
+  return launch(kBwd ? "ffn_hidden_bwd_simt" : "ffn_hidden_simt", ffn_hidden_simt<T, kAct, kBwd>,
+                dim3((unsigned)(ceil_div(f, kBn) * ceil_div(n, kBm))), dim3(kThr), 0, s, x, g, u, dy, w, L.H,
+                L.dG, L.dU);
+}
+
+template <typename T, bool kBwd>
+hg_status hidden_act(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, const FfnLayout& L,
+                     cudaStream_t s) {
+  if (p->act == HG_ACT_RELU) return hidden<T, HG_ACT_RELU, kBwd>(p, X, n, dY, L, s);
+  if (p->act == HG_ACT_GELU_TANH) return hidden<T, HG_ACT_GELU_TANH, kBwd>(p, X, n, dY, L, s);
+  if (p->act == HG_ACT_SILU) return hidden<T, HG_ACT_SILU, kBwd>(p, X, n, dY, L, s);
+  return hidden<T, HG_ACT_NONE, kBwd>(p, X, n, dY, L, s);
+}
+
+template <typename TA, typename TB>
+hg_status wgrad(const TA* A, int64_t mc, const TB* B, int64_t nc, int64_t n, const FfnLayout& L, int splits, float* out,
+                cudaStream_t s) {
+  const Mat<TA> a{A, mc, n, mc};
+  const Mat<TB> b{B, nc, n, nc};
+  const int64_t rows = (int64_t)align_up((size_t)ceil_div(n, splits), kBk);
+  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt<TA, TB>,
+                dim3((unsigned)ceil_div(nc, kBn), (unsigned)ceil_div(mc, kBm), (unsigned)splits), dim3(kThr), 0, s, a,
+                b, rows, L.part));
+  return reduce_partials(L.part, mc * nc, splits, mc * nc, out, L.tmp, s);
+}
+
+template <typename T>
+hg_status fwd_simt(const hg_ffn_params* p, const void* X, int64_t n, void* Y, const FfnLayout& L, cudaStream_t s) {
+  const int64_t d = p->d, f = p->f;
+  HG_TRY((hidden_act<T, false>(p, X, n, nullptr, L, s)));
+  const Mat<float> h{L.H, f, n, f}, none{};
+  const Mat<T> w{(const T*)p->W_down, d, f, d};
+  return launch("ffn_out_simt", ffn_out_simt<T, false>, dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))),
+                dim3(kThr), 0, s, h, w, none, w, (const T*)(p->residual ? X : nullptr), (T*)Y, d);
+}
+
+template <typename T>
+hg_status bwd_simt(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
+                   const FfnLayout& L, cudaStream_t s) {
+  const int64_t d = p->d, f = p->f;
+  HG_TRY((hidden_act<T, true>(p, X, n, dY, L, s)));
+  if (dX) {
+    const Mat<float> a{L.dG, f, n, f}, a2{L.dU, f, n, f};
+    const Mat<T> b{(const T*)p->W_gate, f, d, f}, b2{(const T*)p->W_up, f, d, f};
+    HG_TRY(launch("ffn_dx_simt", ffn_out_simt<T, true>,
+                  dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))), dim3(kThr), 0, s, a, b, a2, b2,
+                  (const T*)(p->residual ? dY : nullptr), (T*)dX, d));
+  }
+  if (!g) return HG_OK;
+  const int sp = wg_splits(n, p->d, p->f);
+  HG_TRY(wgrad((const T*)X, d, L.dG, f, n, L, sp, g->dW_gate, s));
+  HG_TRY(wgrad((const T*)X, d, L.dU, f, n, L, sp, g->dW_up, s));
+  return wgrad(L.H, f, (const T*)dY, d, n, L, sp, g->dW_down, s);
+}
+
+hg_status check_params(const hg_ffn_params* p, int64_t n) {
+  HG_REQUIRE(p != nullptr, "params must be non-null");
+  if (!(p->d == 64 || p->d == 128 || p->d == 256) || !(p->dtype == HG_F32 || p->dtype == HG_BF16)) {
+    set_error("unsupported d=%d / dtype=%d", p->d, (int)p->dtype);
+    return HG_ERR_UNSUPPORTED;
+  }
+  HG_REQUIRE(p->f >= 8 && p->f <= kMaxF && p->f % 8 == 0, "f must be a multiple of 8 in [8, %d]", kMaxF);
+  HG_REQUIRE(p->act == HG_ACT_RELU || p->act == HG_ACT_GELU_TANH || p->act == HG_ACT_NONE || p->act == HG_ACT_SILU,
+             "unknown activation %d", (int)p->act);
+  HG_REQUIRE(n >= 0 && n < (int64_t(1) << 31) && ceil_div(n, kBm) * ceil_div(p->f, kBn) < (int64_t(1) << 31),
+             "n must be in [0, 2^31), n * f below 2^44");
+  return HG_OK;
+}
+
+hg_status check_weights(const hg_ffn_params* p) {
+  HG_REQUIRE(p->W_gate && p->W_up && p->W_down, "every weight pointer must be non-null");
+  HG_REQUIRE((((uintptr_t)p->W_gate | (uintptr_t)p->W_up | (uintptr_t)p->W_down) & 15) == 0,
+             "weights must be 16-byte aligned");
+  return HG_OK;
+}
+
+}  // namespace
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" hg_status hg_ffn_workspace_size(const hg_ffn_params* params, int64_t n, size_t* fwd_bytes,
+                                           size_t* bwd_bytes) {
+  clear_error();
+  HG_REQUIRE(fwd_bytes && bwd_bytes, "fwd_bytes and bwd_bytes must be non-null");
+  HG_TRY(check_params(params, n));
+  FfnLayout L;
+  carve_simt(nullptr, params, n, false, &L, fwd_bytes);
+  carve_simt(nullptr, params, n, true, &L, bwd_bytes);
+  return HG_OK;
+}
+
+extern "C" hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int64_t n, void* Y, void* scratch,
+                                hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check_params(params, n));
+  HG_TRY(check_weights(params));
+  if (n == 0) return HG_OK;
+  HG_REQUIRE(X && Y && scratch, "X, Y and scratch must be non-null");
+  HG_REQUIRE((((uintptr_t)X | (uintptr_t)Y) & 15) == 0, "X and Y must be 16-byte aligned");
+  HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  FfnLayout L;
+  carve_simt(scratch, params, n, false, &L, nullptr);
+  if (params->dtype == HG_F32) return fwd_simt<float>(params, X, n, Y, L, s);
+  return fwd_simt<__nv_bfloat16>(params, X, n, Y, L, s);
+}
+
+extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
+                                const hg_ffn_grads* grads, void* scratch, hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check_params(params, n));
+  HG_TRY(check_weights(params));
+  HG_REQUIRE(!grads || (grads->dW_gate && grads->dW_up && grads->dW_down), "every gradient pointer must be non-null");
+  HG_REQUIRE(!grads || (((uintptr_t)grads->dW_gate | (uintptr_t)grads->dW_up | (uintptr_t)grads->dW_down) & 15) == 0,
+             "gradients must be 16-byte aligned");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const size_t wbytes = sizeof(float) * (size_t)params->d * params->f;
+  if (n == 0) {
+    if (grads) {
+      HG_CUDA(cudaMemsetAsync(grads->dW_gate, 0, wbytes, s));
+      HG_CUDA(cudaMemsetAsync(grads->dW_up, 0, wbytes, s));
+      HG_CUDA(cudaMemsetAsync(grads->dW_down, 0, wbytes, s));
+    }
+    return HG_OK;
+  }
+  HG_REQUIRE(X && dY && scratch, "X, dY and scratch must be non-null");
+  HG_REQUIRE((((uintptr_t)X | (uintptr_t)dY | (uintptr_t)dX) & 15) == 0, "X, dY and dX must be 16-byte aligned");
+  HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
+  if (!dX && !grads) return HG_OK;
+  FfnLayout L;
+  carve_simt(scratch, params, n, true, &L, nullptr);
+  if (params->dtype == HG_F32) return bwd_simt<float>(params, X, n, dY, dX, grads, L, s);
+  return bwd_simt<__nv_bfloat16>(params, X, n, dY, dX, grads, L, s);
+}

@@ -8,17 +8,18 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+from ctypes import (POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64,
+                    c_void_p)
 
 import torch
 
 from . import build as _build
 
 HG_F32, HG_BF16 = 0, 1
-HG_ACT_RELU, HG_ACT_GELU_TANH, HG_ACT_NONE = 0, 1, 2
+HG_ACT_RELU, HG_ACT_GELU_TANH, HG_ACT_NONE, HG_ACT_SILU = 0, 1, 2, 3
 DTYPES = {"f32": HG_F32, "bf16": HG_BF16}
 TORCH_DTYPES = {HG_F32: torch.float32, HG_BF16: torch.bfloat16}
-ACTS = {"relu": HG_ACT_RELU, "gelu_tanh": HG_ACT_GELU_TANH, "none": HG_ACT_NONE}
+ACTS = {"relu": HG_ACT_RELU, "gelu_tanh": HG_ACT_GELU_TANH, "none": HG_ACT_NONE, "silu": HG_ACT_SILU}
 
 
 class hg_rel_desc(Structure):
@@ -80,6 +81,34 @@ class hg_temporal_grads(Structure):
                 ("db_h", c_void_p)]
 
 
+class hg_rows(Structure):
+    _fields_ = [("p", c_void_p), ("stride", c_int64)]
+
+
+class hg_seq(Structure):
+    _fields_ = [("p", c_void_p), ("stride_n", c_int64), ("stride_t", c_int64)]
+
+
+class hg_qkrot_params(Structure):
+    _fields_ = [("heads_q", c_int32), ("heads_k", c_int32), ("d_h", c_int32), ("rot", c_int32),
+                ("interleaved", c_int32), ("dtype", c_int32), ("eps", c_float), ("base", c_double),
+                ("gamma_q", c_void_p), ("gamma_k", c_void_p)]
+
+
+class hg_decay_params(Structure):
+    _fields_ = [("heads", c_int32), ("d_h", c_int32), ("dtype", c_int32), ("scale", c_float),
+                ("log_decay", c_void_p)]
+
+
+class hg_ffn_params(Structure):
+    _fields_ = [("d", c_int32), ("f", c_int32), ("dtype", c_int32), ("act", c_int32), ("residual", c_int32),
+                ("W_gate", c_void_p), ("W_up", c_void_p), ("W_down", c_void_p)]
+
+
+class hg_ffn_grads(Structure):
+    _fields_ = [("dW_gate", c_void_p), ("dW_up", c_void_p), ("dW_down", c_void_p)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "hg_status_string": (c_char_p, [c_int32]),
@@ -133,6 +162,25 @@ EXPORTS = {
     "hg_hgt_fwd": (c_int32, [c_void_p, POINTER(hg_hgt_params), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "hg_hgt_bwd": (c_int32, [c_void_p, POINTER(hg_hgt_params), c_void_p, c_void_p, c_void_p, c_void_p,
                              POINTER(hg_hgt_grads), c_void_p, c_void_p]),
+    "hg_qkrot_workspace_size": (c_int32, [POINTER(hg_qkrot_params), c_int64, POINTER(c_size_t)]),
+    "hg_qkrot_fwd": (c_int32, [POINTER(hg_qkrot_params), POINTER(hg_rows), POINTER(hg_rows), c_void_p, c_int64,
+                               POINTER(hg_rows), POINTER(hg_rows), c_void_p]),
+    "hg_qkrot_bwd": (c_int32, [POINTER(hg_qkrot_params), POINTER(hg_rows), POINTER(hg_rows), c_void_p, c_int64,
+                               POINTER(hg_rows), POINTER(hg_rows), POINTER(hg_rows), POINTER(hg_rows), c_void_p,
+                               c_void_p, c_void_p, c_void_p]),
+    "hg_decay_workspace_size": (c_int32, [POINTER(hg_decay_params), c_int64, c_int64, POINTER(c_size_t),
+                                          POINTER(c_size_t)]),
+    "hg_decay_fwd": (c_int32, [POINTER(hg_decay_params), POINTER(hg_seq), POINTER(hg_seq), POINTER(hg_seq), c_void_p,
+                               c_int64, c_int64, c_void_p, POINTER(hg_seq), c_void_p, c_void_p, c_void_p]),
+    "hg_decay_bwd": (c_int32, [POINTER(hg_decay_params), POINTER(hg_seq), POINTER(hg_seq), POINTER(hg_seq), c_void_p,
+                               c_int64, c_int64, c_void_p, POINTER(hg_seq), c_void_p, POINTER(hg_seq), POINTER(hg_seq),
+                               POINTER(hg_seq), c_void_p, c_void_p, c_void_p]),
+    "hg_decay_step": (c_int32, [POINTER(hg_decay_params), POINTER(hg_rows), POINTER(hg_rows), POINTER(hg_rows),
+                                c_void_p, c_int64, c_void_p, POINTER(hg_rows), c_void_p, c_void_p]),
+    "hg_ffn_workspace_size": (c_int32, [POINTER(hg_ffn_params), c_int64, POINTER(c_size_t), POINTER(c_size_t)]),
+    "hg_ffn_fwd": (c_int32, [POINTER(hg_ffn_params), c_void_p, c_int64, c_void_p, c_void_p, c_void_p]),
+    "hg_ffn_bwd": (c_int32, [POINTER(hg_ffn_params), c_void_p, c_int64, c_void_p, c_void_p, POINTER(hg_ffn_grads),
+                             c_void_p, c_void_p]),
     "hg_timing_enable": (c_int32, [c_int32]),
     "hg_timing_report": (c_int32, [c_char_p, c_size_t]),
 }
@@ -573,3 +621,196 @@ def hg_hgt_bwd(g: Graph, params: HgtParams, H_in, saved, dH_out, dH_in, grads: d
     gr = hg_hgt_grads(*(_ptr(grads.get(k)) for k in HGT_KEYS))
     _check(lib().hg_hgt_bwd(g.handle, byref(p), _ptr(H_in), _ptr(saved), _ptr(dH_out), _ptr(dH_in), byref(gr),
                             _ptr(scratch), _stream(stream)), "hg_hgt_bwd")
+
+
+# ------------------------------------------------------------------------------------------------
+# history encoder: norm and rotation of queries and keys, linear attention with decay, gated block
+# ------------------------------------------------------------------------------------------------
+def _storage(dtype) -> int:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"storage types are float32 and bfloat16; got {dtype}")
+    return HG_F32 if dtype == torch.float32 else HG_BF16
+
+
+def _want(t, name: str, dtype, shape):
+    """A contiguous device tensor of this type and shape (None passes NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}; got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _heads_of(t, name: str, dtype, shape):
+    """A device tensor [..., heads, d_h] whose rows of heads are contiguous; the other strides are free."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}; got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"libhg takes device memory; {name} is on {t.device}")
+    if (shape[-1] > 1 and t.stride(-1) != 1) or (shape[-2] > 1 and t.stride(-2) != shape[-1]):
+        raise ValueError(f"{name}: a row's heads must be contiguous; got strides {t.stride()}")
+
+
+def _row_arg(t, name: str, dtype, shape):
+    _heads_of(t, name, dtype, shape)
+    return byref(hg_rows(t.data_ptr(), t.stride(0)))
+
+
+def _seq_arg(t, name: str, dtype, shape):
+    _heads_of(t, name, dtype, shape)
+    return byref(hg_seq(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def _work_ptr(t, need: int, name: str):
+    """Workspace of at least `need` bytes (None is allowed where none is needed)."""
+    have = 0 if t is None else t.numel() * t.element_size()
+    if have < need:
+        raise ValueError(f"{name}: {need} bytes are needed, {have} given (see the *_workspace_size call)")
+    return _ptr(t)
+
+
+class QkRotParams:
+    """Parameters of the norm and rotation (see hg_qkrot_params): gains [d_h] in the storage type, or None with
+    d_h and dtype given."""
+
+    def __init__(self, gamma_q, gamma_k, heads_q: int, heads_k: int, rot: int | None = None, base: float = 10000.0,
+                 eps: float = 1e-6, interleaved: bool = False, d_h: int | None = None, dtype=None):
+        some = gamma_q if gamma_q is not None else gamma_k
+        if some is not None:
+            d_h, dtype = int(some.numel()), some.dtype
+        self.t = [x.contiguous() if x is not None else None for x in (gamma_q, gamma_k)]
+        for x, name in zip(self.t, ("gamma_q", "gamma_k")):
+            _want(x, name, dtype, (d_h,))
+        self.heads_q, self.heads_k, self.d_h, self.dtype = int(heads_q), int(heads_k), int(d_h), dtype
+        self._c = hg_qkrot_params(self.heads_q, self.heads_k, self.d_h, self.d_h if rot is None else int(rot),
+                                  1 if interleaved else 0, _storage(dtype), float(eps), float(base),
+                                  *(_ptr(x) for x in self.t))
+
+    def c(self) -> hg_qkrot_params:
+        return self._c
+
+
+def hg_qkrot_workspace_size(params: QkRotParams, n: int) -> int:
+    b = c_size_t(0)
+    _check(lib().hg_qkrot_workspace_size(byref(params.c()), int(n), byref(b)), "hg_qkrot_workspace_size")
+    return b.value
+
+
+def _qkrot_rows(p: QkRotParams, n: int, qk):
+    out = []
+    for q, k, tag in qk:
+        out.append(_row_arg(q, tag % "q", p.dtype, (n, p.heads_q, p.d_h)))
+        out.append(_row_arg(k, tag % "k", p.dtype, (n, p.heads_k, p.d_h)) if p.heads_k else None)
+    return out
+
+
+def hg_qkrot_fwd(params: QkRotParams, q, k, pos, q_out, k_out, stream=None):
+    """q [n, heads_q, d_h], k [n, heads_k, d_h] (None when heads_k is 0); pos int64 [n] or None."""
+    n = q.shape[0]
+    a = _qkrot_rows(params, n, ((q, k, "%s"), (q_out, k_out, "%s_out")))
+    _check(lib().hg_qkrot_fwd(byref(params.c()), a[0], a[1], _want(pos, "pos", torch.int64, (n,)), n, a[2], a[3],
+                              _stream(stream)), "hg_qkrot_fwd")
+
+
+def hg_qkrot_bwd(params: QkRotParams, q, k, pos, dq_out, dk_out, dq, dk, grads: dict, scratch, stream=None):
+    """grads: gamma_q, gamma_k (fp32 [d_h]; a missing one is not computed)."""
+    n = q.shape[0]
+    a = _qkrot_rows(params, n, ((q, k, "%s"), (dq_out, dk_out, "d%s_out"), (dq, dk, "d%s")))
+    g = [_want(grads.get(x), x, torch.float32, (params.d_h,)) for x in ("gamma_q", "gamma_k")]
+    w = _work_ptr(scratch, hg_qkrot_workspace_size(params, n) if n else 0, "scratch")
+    _check(lib().hg_qkrot_bwd(byref(params.c()), a[0], a[1], _want(pos, "pos", torch.int64, (n,)), n, a[2], a[3], a[4],
+                              a[5], g[0], g[1], w, _stream(stream)), "hg_qkrot_bwd")
+
+
+class DecayParams:
+    """Parameters of the linear attention with decay (see hg_decay_params); log_decay fp32 [heads]."""
+
+    def __init__(self, log_decay, d_h: int, dtype, scale: float = 1.0):
+        self.log_decay = log_decay.contiguous()
+        self.heads, self.d_h, self.dtype = int(log_decay.numel()), int(d_h), dtype
+        self._c = hg_decay_params(self.heads, self.d_h, _storage(dtype), float(scale),
+                                  _want(self.log_decay, "log_decay", torch.float32, (self.heads,)))
+
+    def c(self) -> hg_decay_params:
+        return self._c
+
+
+def hg_decay_workspace_size(params: DecayParams, n: int, T: int) -> tuple:
+    f, b = c_size_t(0), c_size_t(0)
+    _check(lib().hg_decay_workspace_size(byref(params.c()), int(n), int(T), byref(f), byref(b)),
+           "hg_decay_workspace_size")
+    return f.value, b.value
+
+
+def hg_decay_fwd(params: DecayParams, q, k, v, lens, S_in, o, S_out, scratch, stream=None):
+    """q, k, v, o [n, T, heads, d_h]; lens int32 [n] or None; S_in, S_out fp32 [n, heads, d_h, d_h] or None."""
+    n, T, h, dh = q.shape[0], q.shape[1], params.heads, params.d_h
+    r = [_seq_arg(t, x, params.dtype, (n, T, h, dh)) for t, x in ((q, "q"), (k, "k"), (v, "v"), (o, "o"))]
+    st = [_want(t, x, torch.float32, (n, h, dh, dh)) for t, x in ((S_in, "S_in"), (S_out, "S_out"))]
+    w = _work_ptr(scratch, hg_decay_workspace_size(params, n, T)[0] if n else 0, "scratch")
+    _check(lib().hg_decay_fwd(byref(params.c()), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
+                              r[3], st[1], w, _stream(stream)), "hg_decay_fwd")
+
+
+def hg_decay_bwd(params: DecayParams, q, k, v, lens, S_in, d_o, dS_out, dq, dk, dv, dS_in, scratch, stream=None):
+    n, T, h, dh = q.shape[0], q.shape[1], params.heads, params.d_h
+    r = [_seq_arg(t, x, params.dtype, (n, T, h, dh))
+         for t, x in ((q, "q"), (k, "k"), (v, "v"), (d_o, "d_o"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
+    st = [_want(t, x, torch.float32, (n, h, dh, dh))
+          for t, x in ((S_in, "S_in"), (dS_out, "dS_out"), (dS_in, "dS_in"))]
+    w = _work_ptr(scratch, hg_decay_workspace_size(params, n, T)[1] if n else 0, "scratch")
+    _check(lib().hg_decay_bwd(byref(params.c()), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
+                              r[3], st[1], r[4], r[5], r[6], st[2], w, _stream(stream)), "hg_decay_bwd")
+
+
+def hg_decay_step(params: DecayParams, q, k, v, live, S_in, o, S_out=None, stream=None):
+    """One snapshot: q, k, v, o [n, heads, d_h]; live int32 [n] or None; S_out None updates S_in in place."""
+    n, h, dh = q.shape[0], params.heads, params.d_h
+    r = [_row_arg(t, x, params.dtype, (n, h, dh)) for t, x in ((q, "q"), (k, "k"), (v, "v"), (o, "o"))]
+    S_out = S_in if S_out is None else S_out
+    st = [_want(t, x, torch.float32, (n, h, dh, dh)) for t, x in ((S_in, "S_in"), (S_out, "S_out"))]
+    _check(lib().hg_decay_step(byref(params.c()), r[0], r[1], r[2], _want(live, "live", torch.int32, (n,)), n, st[0],
+                               r[3], st[1], _stream(stream)), "hg_decay_step")
+
+
+class FfnParams:
+    """Weights of the gated feed-forward block (see hg_ffn_params): W_gate, W_up [d, f], W_down [f, d]."""
+
+    def __init__(self, W_gate, W_up, W_down, act: str = "silu", residual: bool = False):
+        self.t = [x.contiguous() for x in (W_gate, W_up, W_down)]
+        self.d, self.f = (int(x) for x in W_gate.shape)
+        self.dtype = W_gate.dtype
+        shapes = ((self.d, self.f), (self.d, self.f), (self.f, self.d))
+        ptrs = [_want(x, name, self.dtype, shape)
+                for x, name, shape in zip(self.t, ("W_gate", "W_up", "W_down"), shapes)]
+        self._c = hg_ffn_params(self.d, self.f, _storage(self.dtype), ACTS[act], 1 if residual else 0, *ptrs)
+
+    def c(self) -> hg_ffn_params:
+        return self._c
+
+
+def hg_ffn_workspace_size(params: FfnParams, n: int) -> tuple:
+    f, b = c_size_t(0), c_size_t(0)
+    _check(lib().hg_ffn_workspace_size(byref(params.c()), int(n), byref(f), byref(b)), "hg_ffn_workspace_size")
+    return f.value, b.value
+
+
+def hg_ffn_fwd(params: FfnParams, X, Y, scratch, stream=None):
+    n, shape = X.shape[0], (X.shape[0], params.d)
+    w = _work_ptr(scratch, hg_ffn_workspace_size(params, n)[0] if n else 0, "scratch")
+    _check(lib().hg_ffn_fwd(byref(params.c()), _want(X, "X", params.dtype, shape), n,
+                            _want(Y, "Y", params.dtype, shape), w, _stream(stream)), "hg_ffn_fwd")
+
+
+def hg_ffn_bwd(params: FfnParams, X, dY, dX, grads: dict | None, scratch, stream=None):
+    """dX None or grads None skips that part; grads: W_gate, W_up, W_down (fp32)."""
+    n, shape = X.shape[0], (X.shape[0], params.d)
+    gr = None
+    if grads is not None:
+        df, fd = (params.d, params.f), (params.f, params.d)
+        gr = byref(hg_ffn_grads(*(_want(grads[k], k, torch.float32, s)
+                                  for k, s in (("W_gate", df), ("W_up", df), ("W_down", fd)))))
+    w = _work_ptr(scratch, hg_ffn_workspace_size(params, n)[1] if n else 0, "scratch")
+    _check(lib().hg_ffn_bwd(byref(params.c()), _want(X, "X", params.dtype, shape), n,
+                            _want(dY, "dY", params.dtype, shape), _want(dX, "dX", params.dtype, shape), gr, w,
+                            _stream(stream)), "hg_ffn_bwd")

@@ -1,0 +1,254 @@
+"""Oracle of the history encoder's operators against differences and identities, and the refusals of their entry
+points and binding (CPU only: fake aligned addresses stand in for device buffers, nothing is dereferenced)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import history as OH
+
+A = 1 << 20  # a 256-byte-aligned stand-in address
+
+
+@pytest.fixture(scope="module")
+def hg():
+    from paper_2608_02168_gb300 import build
+    build.build()
+    from paper_2608_02168_gb300 import hg as binding
+    return binding
+
+
+def central(f, x, dy, h=1e-5):
+    """d <f(x), dy> / dx by central differences."""
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        keep = x[i]
+        x[i] = keep + h
+        up = (f() * dy).sum()
+        x[i] = keep - h
+        g[i] = (up - (f() * dy).sum()) / (2 * h)
+        x[i] = keep
+    return g
+
+
+def close(a, b, tol=1e-7):
+    # central differences of step 1e-5: truncation h^2 and rounding 2^-53 / h, both below 1e-9 of these values
+    assert np.abs(a - b).max() <= tol * max(1.0, np.abs(b).max()), np.abs(a - b).max()
+
+
+@pytest.mark.parametrize("rot,interleaved", [(16, False), (16, True), (32, False), (0, False)])
+def test_rotation_gradients(rot, interleaved):
+    rng = np.random.default_rng(rot)
+    x, g, dy = rng.standard_normal((3, 2, 32)), rng.standard_normal(32), rng.standard_normal((3, 2, 32))
+    pos = np.array([0, 5, -7])
+    f = lambda: OH.qkrot_forward(x, g, pos, rot, 100.0, 1e-3, interleaved)  # noqa: E731
+    dx, dg = OH.qkrot_backward(x, g, pos, rot, 100.0, 1e-3, interleaved, dy)
+    close(dx, central(f, x, dy))
+    close(dg, central(f, g, dy))
+
+
+def test_rotation_depends_on_the_distance_alone():
+    rng = np.random.default_rng(1)
+    q, k = rng.standard_normal((2, 1, 1, 32))
+    one = np.ones(32)
+    dots = []
+    for a, b in ((3, 1), (1003, 1001)):
+        y = [OH.qkrot_forward(x, one, [p], 32, 1e4, 1e-6, False)[0, 0] for x, p in ((q, a), (k, b))]
+        dots.append(y[0] @ y[1])
+    close(np.array(dots[0]), np.array(dots[1]), 1e-10)
+
+
+@pytest.mark.parametrize("lens", [None, [0, 1, 4], [4, 3, 2]])
+def test_decay_gradients(lens):
+    rng = np.random.default_rng(3)
+    n, T, h, d = 3, 4, 2, 3
+    q, k, v, do = rng.standard_normal((4, n, T, h, d))
+    S, dS = rng.standard_normal((2, n, h, d, d))
+    ld = np.array([-0.3, -2.0])
+    lens = None if lens is None else np.array(lens)
+
+    def both():
+        o, last = OH.decay_forward(q, k, v, ld, 0.7, lens, S)
+        return np.concatenate([o.ravel(), last.ravel()])
+
+    dy = np.concatenate([do.ravel(), dS.ravel()])
+    got = OH.decay_backward(q, k, v, ld, 0.7, do, lens, S, dS)
+    for x, g in zip((q, k, v, S), got):
+        close(g, central(both, x, dy))
+
+
+def test_decay_is_the_masked_product():
+    rng = np.random.default_rng(4)
+    T, d = 9, 5
+    q, k, v = rng.standard_normal((3, T, d))
+    ld = -0.2
+    gap = np.arange(T)[:, None] - np.arange(T)
+    want = 0.5 * (np.where(gap >= 0, np.exp(ld * np.maximum(gap, 0)), 0.0) * (q @ k.T)) @ v
+    o, S = OH.decay_forward(q[None, :, None], k[None, :, None], v[None, :, None], np.array([ld]), 0.5)
+    close(o[0, :, 0], want, 1e-12)
+    a, S1 = OH.decay_forward(*(x[None, :4, None] for x in (q, k, v)), np.array([ld]), 0.5)
+    b, S2 = OH.decay_forward(*(x[None, 4:, None] for x in (q, k, v)), np.array([ld]), 0.5, S_in=S1)
+    close(np.concatenate([a, b], 1), o, 1e-12)
+    close(S2, S, 1e-12)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu_tanh", "relu", "none"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_ffn_gradients(kind, residual):
+    rng = np.random.default_rng(5)
+    X, dY = rng.standard_normal((2, 4, 6))
+    Wg, Wu = rng.standard_normal((2, 6, 8))
+    Wd = rng.standard_normal((8, 6))
+    f = lambda: OH.ffn_forward(X, Wg, Wu, Wd, kind, residual)  # noqa: E731
+    for x, g in zip((X, Wg, Wu, Wd), OH.ffn_backward(X, Wg, Wu, Wd, kind, residual, dY)):
+        close(g, central(f, x, dY))
+
+
+def test_gelu_is_torch_gelu():
+    x = np.linspace(-6, 6, 101)
+    want = torch.nn.functional.gelu(torch.from_numpy(x), approximate="tanh").numpy()
+    close(OH.act(x, "gelu_tanh")[0], want, 1e-12)
+
+
+# ---------------------------------------------------------------------------------------------- refusals
+def rows(hg, p=A, stride=128):
+    return ctypes.byref(hg.hg_rows(p, stride))
+
+
+def seq(hg, p=A, sn=4096, st=128):
+    return ctypes.byref(hg.hg_seq(p, sn, st))
+
+
+def test_qkrot_refusals(hg):
+    so = hg.lib()
+
+    def params(hq=4, hk=4, dh=32, rot=32, inter=0, dt=1, eps=1e-6, base=1e4):
+        return ctypes.byref(hg.hg_qkrot_params(hq, hk, dh, rot, inter, dt, eps, base, None, None))
+
+    size = ctypes.c_size_t()
+
+    def query(n=10, **k):
+        return so.hg_qkrot_workspace_size(params(**k), n, ctypes.byref(size))
+
+    assert query() == 0 and size.value > 0 and query(0) == 0
+    assert query(dh=48) == 2 and query(dt=2) == 2 and query(dt=-1) == 2
+    assert query(hq=0) == query(hq=65) == query(hk=-1) == query(hk=65) == 1
+    assert query(rot=8) == query(rot=48) == query(rot=-16) == 1
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        assert query(eps=bad) == 1
+    for bad in (0.5, float("nan"), float("inf")):
+        assert query(base=bad) == 1
+    assert query(-1) == 1 and so.hg_qkrot_workspace_size(None, 1, ctypes.byref(size)) == 1
+    assert so.hg_qkrot_workspace_size(params(), 1, None) == 1
+
+    def fwd(q=None, k=None, qo=None, ko=None, n=10, **kw):
+        z = [rows(hg) if x is None else x for x in (q, k, qo, ko)]
+        return so.hg_qkrot_fwd(params(**kw), z[0], z[1], None, n, z[2], z[3], None)
+
+    null = ctypes.POINTER(hg.hg_rows)()
+    assert fwd(q=null) == fwd(k=null) == fwd(qo=null) == fwd(ko=null) == 1
+    assert fwd(q=rows(hg, A + 2)) == fwd(ko=rows(hg, A + 8)) == 1           # alignment
+    assert fwd(q=rows(hg, stride=132)) == fwd(q=rows(hg, stride=-128)) == 1  # stride
+    assert fwd(qo=rows(hg, stride=64)) == fwd(ko=rows(hg, stride=0)) == 1    # written rows overlap
+    assert fwd(q=null, n=0) == 0
+
+    def bwd(n=10, scratch=A, dq=None, **kw):
+        r = rows(hg)
+        return so.hg_qkrot_bwd(params(**kw), r, r, None, n, r, r, r if dq is None else dq, r, A, A, scratch, None)
+
+    assert bwd(scratch=None) == bwd(scratch=A + 16) == bwd(dq=rows(hg, stride=32)) == bwd(n=-1) == 1
+
+
+def test_decay_refusals(hg):
+    so = hg.lib()
+
+    def params(h=4, dh=32, dt=1, ld=A):
+        return ctypes.byref(hg.hg_decay_params(h, dh, dt, 1.0, ld))
+
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+
+    def query(n=3, T=5, **k):
+        return so.hg_decay_workspace_size(params(**k), n, T, ctypes.byref(f), ctypes.byref(b))
+
+    assert query() == 0 and f.value == b.value == 0
+    assert query(1, 1 << 16) == 0 and f.value >= 4 * 4 * 32 * 32 * 2 and b.value >= f.value  # segments' states
+    assert query(dh=24) == 2 and query(dt=7) == 2
+    assert query(h=0) == query(h=65) == query(n=-1) == query(T=-1) == query(T=1 << 30) == query(n=1 << 26) == 1
+    assert so.hg_decay_workspace_size(params(), 1, 1, None, ctypes.byref(b)) == 1
+
+    def fwd(n=3, T=5, o=None, q=None, scratch=None, **kw):
+        s = seq(hg)
+        return so.hg_decay_fwd(params(**kw), s if q is None else q, s, s, None, n, T, None, s if o is None else o, None,
+                               scratch, None)
+
+    null = ctypes.POINTER(hg.hg_seq)()
+    assert fwd(ld=None) == fwd(q=null) == fwd(o=null) == 1
+    assert fwd(q=seq(hg, A + 4)) == fwd(q=seq(hg, st=-128)) == fwd(q=seq(hg, sn=4100)) == 1
+    assert fwd(o=seq(hg, st=64)) == fwd(o=seq(hg, sn=512)) == fwd(o=seq(hg, sn=0)) == 1  # written rows overlap
+    assert fwd(o=seq(hg, sn=128, st=256)) == 1
+    assert fwd(n=1, T=1 << 16) == 1                                                      # segments need scratch
+    assert fwd(n=1, T=1 << 16, scratch=A + 64) == 1
+    assert fwd(n=0, q=null) == 0
+
+    def bwd(dk=None, n=3, T=5):
+        s = seq(hg)
+        return so.hg_decay_bwd(params(), s, s, s, None, n, T, None, s, None, s, s if dk is None else dk, s, None, None,
+                               None)
+
+    assert bwd(dk=null) == bwd(dk=seq(hg, st=0)) == bwd(T=-1) == 1
+
+    def step(q=None, S=A, So=A, n=3, o=None, **kw):
+        r = rows(hg)
+        return so.hg_decay_step(params(**kw), r if q is None else q, r, r, None, n, S, r if o is None else o, So, None)
+
+    nullr = ctypes.POINTER(hg.hg_rows)()
+    assert step(q=nullr) == step(S=None) == step(So=None) == step(So=A + 4) == step(o=rows(hg, stride=32)) == 1
+    assert step(ld=None) == step(n=-1) == 1 and step(dh=20) == 2 and step(n=0, q=nullr) == 0
+
+
+def test_ffn_refusals(hg):
+    so = hg.lib()
+
+    def params(d=64, f=96, dt=1, act=3, wg=A, wu=A, wd=A):
+        return ctypes.byref(hg.hg_ffn_params(d, f, dt, act, 1, wg, wu, wd))
+
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+
+    def query(n=10, **k):
+        return so.hg_ffn_workspace_size(params(**k), n, ctypes.byref(f), ctypes.byref(b))
+
+    assert query() == 0 and query(0) == 0
+    assert query(d=96) == query(dt=3) == 2
+    assert query(f=0) == query(f=12) == query(f=16392) == query(act=4) == query(act=-1) == query(-1) == 1
+    assert query(1 << 31) == 1
+
+    def fwd(X=A, Y=A, n=10, scratch=A, **kw):
+        return so.hg_ffn_fwd(params(**kw), X, n, Y, scratch, None)
+
+    assert fwd(X=None) == fwd(Y=None) == fwd(X=A + 8) == fwd(wg=None) == fwd(wd=A + 2) == 1
+    assert fwd(scratch=A + 16) == 1 and fwd(X=None, n=0) == 0
+
+    def bwd(X=A, dY=A, dX=A, n=10, g=(A, A, A), scratch=A):
+        gr = None if g is None else ctypes.byref(hg.hg_ffn_grads(*g))
+        return so.hg_ffn_bwd(params(), X, n, dY, dX, gr, scratch, None)
+
+    assert bwd(g=(A, None, A)) == bwd(g=(A, A, A + 4)) == bwd(dY=None) == bwd(dX=A + 2) == bwd(scratch=None) == 1
+    assert bwd(n=-1) == 1 and bwd(dX=None, g=None) == 0
+
+
+def test_binding_refuses_shapes_types_and_host_tensors(hg):
+    t = torch.empty(3, 2, 32)
+    with pytest.raises(ValueError, match="device memory"):
+        hg._heads_of(t, "q", torch.float32, (3, 2, 32))
+    with pytest.raises(ValueError, match="shape"):
+        hg._heads_of(t, "q", torch.float32, (3, 2, 16))
+    with pytest.raises(ValueError, match="shape"):
+        hg._heads_of(t, "q", torch.bfloat16, (3, 2, 32))
+    with pytest.raises(ValueError, match="shape"):
+        hg._want(torch.empty(3, dtype=torch.int64), "lens", torch.int32, (3,))
+    with pytest.raises(ValueError, match="storage types"):
+        hg._storage(torch.float16)
+    with pytest.raises(ValueError, match="bytes are needed"):
+        hg._work_ptr(None, 16, "scratch")
+    assert hg._work_ptr(None, 0, "scratch") is None
