@@ -31,9 +31,10 @@ struct SimtCfg {
 };
 
 // blockIdx.x * kWarps + warp = ((sequence * nseg) + segment) * column blocks + column block
-template <typename T, int DH, bool kLocal>
+template <int DH, bool kLocal>
 __global__ void __launch_bounds__(32 * kWarps) scan_simt(ScanArgs a) {
   pdl_begin();
+  using T = float;
   using C = SimtCfg<DH>;
   constexpr int W = C::W, TC = C::TC, VEC = VecTraits<T>::kElems;
   __shared__ __align__(16) float sk[kWarps][TC][W];
@@ -246,14 +247,14 @@ __global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-int scan_warps(const hg_decay_params* p) { return (p->heads * p->d_h + 31) / 32; }
-
-// Segments: as many as fill the GPU with warps (16 an SM), none shorter than kMinSeg positions, where the
-// second reading of keys and values costs more than the warps gain.
+// Segments: as many as fill the GPU with warps, none shorter than kMinSeg positions, where the second
+// reading of keys and values costs more than the warps gain.
 constexpr int64_t kMinSeg = 256;
 void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int* nseg, int64_t* seg_len) {
-  const int64_t warps = std::max<int64_t>(n, 1) * scan_warps(p);
-  const int64_t want = std::min<int64_t>(kSms * 16 / warps, T / kMinSeg);
+  const bool mma = p->dtype == HG_BF16;
+  const int64_t each = mma ? scan_mma_warps(p->heads, p->d_h) : (p->heads * p->d_h + 31) / 32;
+  const int64_t full = kSms * (mma ? scan_mma_resident(p->d_h) : 16);
+  const int64_t want = std::min<int64_t>(full / (std::max<int64_t>(n, 1) * each), T / kMinSeg);
   *nseg = 1;
   *seg_len = std::max<int64_t>(T, 1);
   if (want < 2) return;
@@ -261,34 +262,29 @@ void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int* nseg, in
   *nseg = (int)ceil_div(T, *seg_len);
 }
 
-template <typename T, int DH>
+template <int DH>
 hg_status scan_simt_t(const ScanArgs& a, bool local, cudaStream_t s) {
   const int64_t items = a.n * a.nseg * (int64_t)((a.heads * DH + 31) / 32);
   const dim3 grid((unsigned)ceil_div(items, kWarps));
-  if (local) return launch("decay_scan_local", scan_simt<T, DH, true>, grid, dim3(32 * kWarps), 0, s, a);
-  return launch("decay_scan", scan_simt<T, DH, false>, grid, dim3(32 * kWarps), 0, s, a);
+  if (local) return launch("decay_scan_local", scan_simt<DH, true>, grid, dim3(32 * kWarps), 0, s, a);
+  return launch("decay_scan", scan_simt<DH, false>, grid, dim3(32 * kWarps), 0, s, a);
 }
 
-template <typename T>
-hg_status scan_pass(const ScanArgs& a, int dh, bool local, cudaStream_t s) {
-  if (dh == 16) return scan_simt_t<T, 16>(a, local, s);
-  if (dh == 32) return scan_simt_t<T, 32>(a, local, s);
-  if (dh == 64) return scan_simt_t<T, 64>(a, local, s);
-  return scan_simt_t<T, 128>(a, local, s);
-}
-
-hg_status scan_dtype(const ScanArgs& a, const hg_decay_params* p, bool local, cudaStream_t s) {
-  if (p->dtype == HG_F32) return scan_pass<float>(a, p->d_h, local, s);
-  return scan_pass<__nv_bfloat16>(a, p->d_h, local, s);
+hg_status scan_pass(const ScanArgs& a, const hg_decay_params* p, bool local, cudaStream_t s) {
+  if (p->dtype == HG_BF16) return scan_mma(a, p->d_h, local, s);
+  if (p->d_h == 16) return scan_simt_t<16>(a, local, s);
+  if (p->d_h == 32) return scan_simt_t<32>(a, local, s);
+  if (p->d_h == 64) return scan_simt_t<64>(a, local, s);
+  return scan_simt_t<128>(a, local, s);
 }
 
 hg_status scan(const ScanArgs& a, const hg_decay_params* p, cudaStream_t s) {
   if (a.nseg > 1) {
-    HG_TRY(scan_dtype(a, p, true, s));
+    HG_TRY(scan_pass(a, p, true, s));
     HG_TRY(launch("decay_scan_join", scan_join,
                   dim3((unsigned)ceil_div(a.n * a.heads * (int64_t)p->d_h * p->d_h, 256)), dim3(256), 0, s, a, p->d_h));
   }
-  return scan_dtype(a, p, false, s);
+  return scan_pass(a, p, false, s);
 }
 
 hg_status check_params(const hg_decay_params* p, int64_t n, int64_t T) {

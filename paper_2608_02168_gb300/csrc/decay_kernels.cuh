@@ -47,7 +47,8 @@ constexpr float kFrame = 11.f;
 
 // bf16 scan on the tensor cores (decay_mma.cu); local: the segments' own states into a.seg, no rows.
 hg_status scan_mma(const ScanArgs& a, int d_h, bool local, cudaStream_t s);
-// warps that scan_mma runs for one sequence and segment
+// warps that scan_mma runs for one sequence and segment, and warps that an SM holds
 int scan_mma_warps(int heads, int d_h);
+int scan_mma_resident(int d_h);
 
 }  // namespace hg

@@ -1,0 +1,390 @@
+// Scan of the linear attention with decay for bf16 rows on the warp-level tensor instructions.
+//
+// Chunks of 16 positions.  With F the state in its frame (decay_kernels.cuh), r, j positions of a chunk:
+//   rows    o_r = sum_(j <= r) gamma^(r - j) c (q_r . k_j) v_j  +  c_out gamma^(tau_r - b) q_r F
+//   state   F += sum_j c_in gamma^(b - tau_j) k_j v_j^T
+// A warp owns one head of one sequence (or of one segment of it) and a slice of DS <= 32 value features, and keeps
+// F^T (DS x d_h, fp32) in registers as the accumulator of m16n8k16 products: the accumulator's layout is the
+// layout in which the next product wants its second operand, so the state goes from sum to operand without
+// leaving the registers; likewise the chunk's weights from q k^T to the product with v.  No warp waits for
+// another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand.  The
+// scaled values that are added to the state are split into two bf16 numbers (16 bits), since a state is an fp32
+// result that gathers them.
+//
+// Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high and histories
+// are often shorter than one tile; at d_h = 32 a position moves 256 bytes and needs 9 kFLOP, which the warp
+// instructions deliver at the HBM rate.
+//
+// Loads: cp.async, 16 bytes a lane, into a ring of chunks that runs ahead across the warp's items, so short
+// histories follow one another without a pause.  Pieces of a row are XORed with the row so that ldmatrix is
+// free of bank conflicts.
+#include <algorithm>
+
+#include "decay_kernels.cuh"
+#include "tc_util.cuh"
+
+namespace hg {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kC = 16;  // positions of a chunk
+constexpr int kSms = 152;
+
+template <int DH>
+struct Cfg {
+  static constexpr int DS = DH < 32 ? DH : 32;       // value features of a warp
+  static constexpr int SL = DH / DS;                 // slices of a head
+  static constexpr int ST = DH == 128 ? 2 : 3;       // chunks in the ring
+  static constexpr int W = 4;                        // warps of a CTA
+  static constexpr int kRow = DH * 2, kVRow = DS * 2;
+  static constexpr int kQ = kC * kRow, kV = kC * kVRow;
+  static constexpr int kStage = 2 * kQ + kV;
+  static constexpr int kSmem = W * ST * kStage;
+  static constexpr int kBlocks = DH == 16 ? 6 : DH == 32 ? 4 : DH == 64 ? 3 : 2;  // resident CTAs of an SM
+};
+
+// Byte offset of 16-byte piece c of row r, N pieces a row.
+template <int N>
+__device__ __forceinline__ uint32_t piece(int r, int c) {
+  constexpr int sh = N == 2 ? 2 : N == 4 ? 1 : 0;
+  constexpr int mask = (N < 8 ? N : 8) - 1;
+  return (uint32_t)(r * N + (c ^ ((r >> sh) & mask))) * 16u;
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// d += A (16 x 16) B (16 x 8)
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// One warp's piece of work and its place in it.
+struct Item {
+  int64_t id;       // past the last: none
+  int64_t seq, len;
+  int head, slice, segi;
+  int64_t t0, t1;   // positions of the scan: [t0, t1) in use
+};
+
+template <int DH, bool kLocal>
+__device__ __forceinline__ void locate(const ScanArgs& a, int64_t items, Item& it) {
+  if (it.id >= items) {
+    it.t0 = it.t1 = 0;
+    return;
+  }
+  constexpr int SL = Cfg<DH>::SL;
+  const uint32_t segs = kLocal ? a.nseg - 1 : a.nseg;
+  it.slice = (int)(it.id % SL);
+  uint64_t x = (uint64_t)it.id / SL;
+  it.head = (int)(x % (uint32_t)a.heads);
+  x /= (uint32_t)a.heads;
+  it.segi = 0;
+  if (segs > 1) {
+    it.segi = (int)(x % segs);
+    x /= segs;
+  }
+  it.seq = (int64_t)x;
+  it.len = scan_len(a, it.seq);
+  it.t0 = it.segi * a.seg_len;
+  it.t1 = max(it.t0, min(it.t0 + a.seg_len, it.len));
+}
+
+template <int DH, bool kLocal>
+__device__ __forceinline__ void load_chunk(const ScanArgs& a, const Item& it, int64_t c0, uint8_t* stage, int lane) {
+  using C = Cfg<DH>;
+  constexpr int N = DH / 8, NV = C::DS / 8;
+  const int m = (int)min((int64_t)kC, it.t1 - c0);
+  const __nv_bfloat16* q = (const __nv_bfloat16*)a.q.p + it.seq * a.q.sn + it.head * DH;
+  const __nv_bfloat16* k = (const __nv_bfloat16*)a.k.p + it.seq * a.k.sn + it.head * DH;
+  const __nv_bfloat16* v = (const __nv_bfloat16*)a.v.p + it.seq * a.v.sn + it.head * DH + it.slice * C::DS;
+#pragma unroll
+  for (int x = lane; x < kC * N; x += 32) {
+    const int r = x / N, c = x % N;
+    const bool ok = r < m;
+    const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
+    const int64_t row = ok ? t : (a.reverse ? it.len - 1 - c0 : c0);
+    cp_async16(stage + C::kQ + piece<N>(r, c), k + row * a.k.st + c * 8, ok);
+    if (!kLocal) cp_async16(stage + piece<N>(r, c), q + row * a.q.st + c * 8, ok);
+  }
+#pragma unroll
+  for (int x = lane; x < kC * NV; x += 32) {
+    const int r = x / NV, c = x % NV;
+    const bool ok = r < m;
+    const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
+    const int64_t row = ok ? t : (a.reverse ? it.len - 1 - c0 : c0);
+    cp_async16(stage + 2 * C::kQ + piece<NV>(r, c), v + row * a.v.st + c * 8, ok);
+  }
+}
+
+// x (a pair of bf16) times (f0, f1) as a sum hi + lo of bf16 pairs
+__device__ __forceinline__ void scale_split(uint32_t x, float f0, float f1, uint32_t& hi, uint32_t& lo) {
+  const float y0 = __uint_as_float(x << 16) * f0, y1 = __uint_as_float(x & 0xffff0000u) * f1;
+  hi = pack2_bf16(y0, y1);
+  lo = pack2_bf16(y0 - __uint_as_float(hi << 16), y1 - __uint_as_float(hi & 0xffff0000u));
+}
+
+template <int DH, bool kLocal>
+__global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_kernel(const __grid_constant__ ScanArgs a) {
+  pdl_begin();
+  using C = Cfg<DH>;
+  constexpr int DS = C::DS, MT = DS / 16, NT = DH / 8, KS = DH / 16, NV = DS / 8, ST = C::ST;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  uint8_t* ring = smem + warp * (ST * C::kStage);
+  const int64_t items = a.n * (kLocal ? a.nseg - 1 : a.nseg) * a.heads * C::SL;
+  const int64_t stride = (int64_t)gridDim.x * C::W;
+  // lane addresses inside a tile of 16 x 16 for ldmatrix: rows by lane & 15 / pieces by lane >> 4, and the other order
+  const int r16 = lane & 15, c16 = lane >> 4;
+  const int r8 = (lane & 7) + ((lane >> 4) << 3), c8 = (lane >> 3) & 1;
+
+  Item it, nx;
+  it.id = (int64_t)blockIdx.x * C::W + warp;
+  locate<DH, kLocal>(a, items, it);
+  nx = it;
+  int64_t nc = nx.t0;  // the next chunk to load: position nc of item nx
+  auto advance = [&](uint8_t* stage) {
+    while (nx.id < items && nc >= nx.t1) {
+      nx.id += stride;
+      locate<DH, kLocal>(a, items, nx);
+      nc = nx.t0;
+    }
+    if (nx.id < items) {
+      load_chunk<DH, kLocal>(a, nx, nc, stage, lane);
+      nc += kC;
+    }
+    cp_async_commit();
+  };
+  int put = 0, get = 0;
+#pragma unroll
+  for (int s = 0; s < ST - 1; ++s) {
+    advance(ring + put * C::kStage);
+    put = put + 1 == ST ? 0 : put + 1;
+  }
+  for (; it.id < items; it.id += stride, locate<DH, kLocal>(a, items, it)) {
+    const float ld = clamp_ld(a.ld[it.head]);
+    const int64_t sh = it.seq * a.heads + it.head;
+    float F[MT][NT][4];
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+      for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) F[x][y][e] = 0.f;
+    // element e of F[x][y]: value feature 16 x + g + 8 (e / 2) of the slice, key feature 8 y + 2 t4 + e % 2
+    const int v0 = it.slice * DS + g, k0 = 2 * t4;
+    bool some = false;  // the state is not zero
+    if (!kLocal && (a.nseg > 1 || a.init)) {
+      const float* src = a.nseg > 1 ? a.seg + (sh * a.nseg + it.segi) * (int64_t)(DH * DH) : a.init + sh * (DH * DH);
+      const bool tr = a.nseg > 1 ? false : a.init_t != 0;
+      some = true;
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int vi = v0 + 16 * x + 8 * (e >> 1), ki = k0 + 8 * y + (e & 1);
+            F[x][y][e] = tr ? src[vi * DH + ki] : src[ki * DH + vi];
+          }
+    }
+    // weights gamma^(r - j) of the chunk's products: rows g, g + 8, columns 2 t4, 2 t4 + 1 (+ 8)
+    float w[4];
+    bool keep[2];  // column j is not past row g
+    const float cc = a.c_in * a.c_out;
+    if (!kLocal) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = 2 * t4 + e, gap = g - j;
+        keep[e] = gap >= 0;
+        w[e] = keep[e] ? expf(ld * (float)gap) * cc : 0.f;  // row g, column j; row g + 8, column j + 8
+        w[2 + e] = expf(ld * (float)(gap + 8)) * cc;        // row g + 8, column j
+      }
+    }
+    int base = 0;  // positions from t0
+    const bool leave = kLocal || (a.last && it.segi == (it.len > 0 ? (it.len - 1) / a.seg_len : 0));
+    __nv_bfloat16* out = (__nv_bfloat16*)const_cast<void*>(a.o.p) + it.seq * a.o.sn + it.head * DH + it.slice * DS;
+    for (int64_t c0 = it.t0; c0 < it.t1; c0 += kC) {
+      cp_async_wait<ST - 2>();
+      __syncwarp();
+      advance(ring + put * C::kStage);
+      put = put + 1 == ST ? 0 : put + 1;
+      uint8_t* stage = ring + get * C::kStage;
+      get = get + 1 == ST ? 0 : get + 1;
+      const uint32_t sq = smem_u32(stage), sk = sq + C::kQ, sv = sk + C::kQ;
+      const int m = (int)min((int64_t)kC, it.t1 - c0);
+      const int tau0 = (int)(c0 - it.t0) + a.shift;
+      uint32_t vt[MT][4];  // v, positions by pairs: [0], [2] positions 0..7 / 8..15 of features 0..7; [1], [3] of 8..15
+#pragma unroll
+      for (int x = 0; x < MT; ++x) {
+        uint32_t b[4];
+        ldsm4t(sv + piece<NV>(r16, 2 * x + c16), b);
+        vt[x][0] = b[0];
+        vt[x][2] = b[1];
+        vt[x][1] = b[2];
+        vt[x][3] = b[3];
+      }
+      if (!kLocal) {
+        float o[NV][4], p0[4] = {0.f, 0.f, 0.f, 0.f}, p1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < NV; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[y][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          uint32_t qa[4], kb[4];
+          ldsm4(sq + piece<DH / 8>(r16, 2 * s + c16), qa);
+          ldsm4(sk + piece<DH / 8>(r8, 2 * s + c8), kb);
+          mma(p0, qa[0], qa[1], qa[2], qa[3], kb[0], kb[1]);
+          mma(p1, qa[0], qa[1], qa[2], qa[3], kb[2], kb[3]);
+          if (some) {
+#pragma unroll
+            for (int y = 0; y < NV; ++y) {
+              const float* f0 = F[y >> 1][2 * s];
+              const float* f1 = F[y >> 1][2 * s + 1];
+              const int e = (y & 1) * 2;
+              mma(o[y], qa[0], qa[1], qa[2], qa[3], pack2_bf16(f0[e], f0[e + 1]), pack2_bf16(f1[e], f1[e + 1]));
+            }
+          }
+        }
+        if (some) {
+          const float f0 = a.c_out * expf(ld * (float)(tau0 + g - base));
+          const float f1 = a.c_out * expf(ld * (float)(tau0 + g + 8 - base));
+#pragma unroll
+          for (int y = 0; y < NV; ++y) {
+            o[y][0] *= f0;
+            o[y][1] *= f0;
+            o[y][2] *= f1;
+            o[y][3] *= f1;
+          }
+        }
+        const uint32_t a0 = pack2_bf16(keep[0] ? p0[0] * w[0] : 0.f, keep[1] ? p0[1] * w[1] : 0.f);
+        const uint32_t a1 = pack2_bf16(p0[2] * w[2], p0[3] * w[3]);
+        const uint32_t a3 = pack2_bf16(keep[0] ? p1[2] * w[0] : 0.f, keep[1] ? p1[3] * w[1] : 0.f);
+#pragma unroll
+        for (int y = 0; y < NV; ++y) mma(o[y], a0, a1, 0u, a3, vt[y >> 1][y & 1], vt[y >> 1][2 + (y & 1)]);
+        // rows out through the place of q, 16 bytes a lane
+        __syncwarp();
+#pragma unroll
+        for (int y = 0; y < NV; ++y) {
+          *reinterpret_cast<uint32_t*>(stage + piece<NV>(g, y) + t4 * 4) = pack2_bf16(o[y][0], o[y][1]);
+          *reinterpret_cast<uint32_t*>(stage + piece<NV>(g + 8, y) + t4 * 4) = pack2_bf16(o[y][2], o[y][3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int x = lane; x < kC * NV; x += 32) {
+          const int r = x / NV, c = x % NV;
+          if (r < m) {
+            const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
+            st16(out + t * a.o.st + c * 8, ld16(stage + piece<NV>(r, c)));
+          }
+        }
+      }
+      if (leave || c0 + kC < it.t1) {
+        const int target = tau0 + m - 1;
+        if ((float)(base - target) * ld > kFrame) {
+          const float f = expf(ld * (float)(target - base));
+#pragma unroll
+          for (int x = 0; x < MT; ++x)
+#pragma unroll
+            for (int y = 0; y < NT; ++y)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) F[x][y][e] *= f;
+          base = target;
+        }
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 2 * t4 + (e & 1) + 8 * (e >> 1);
+          f[e] = r < m ? a.c_in * expf(ld * (float)(base - tau0 - r)) : 0.f;
+        }
+        uint32_t hi[MT][4], lo[MT][4];
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], lo[x][e]);
+#pragma unroll
+        for (int y = 0; y < NT; y += 2) {
+          uint32_t kb[4];
+          ldsm4t(sk + piece<DH / 8>(r16, y + c16), kb);
+#pragma unroll
+          for (int x = 0; x < MT; ++x) {
+            mma(F[x][y], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[0], kb[1]);
+            mma(F[x][y + 1], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[2], kb[3]);
+            mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
+            mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
+          }
+        }
+        some = true;
+      }
+    }
+    if (!kLocal) {
+      const int64_t tend = min(it.t0 + a.seg_len, a.T), first = max(it.t0, it.len);
+      const int64_t pieces = max((tend - first) * NV, (int64_t)0);
+      for (int64_t x = lane; x < pieces; x += 32)
+        st16(out + (first + x / NV) * a.o.st + x % NV * 8, make_uint4(0u, 0u, 0u, 0u));
+    }
+    if (leave) {
+      const float f = expf(ld * (float)((int)(it.t1 - it.t0) - base));
+      float* dst = kLocal ? a.seg + (sh * a.nseg + it.segi) * (int64_t)(DH * DH) : a.last + sh * (DH * DH);
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            dst[(k0 + 8 * y + (e & 1)) * DH + v0 + 16 * x + 8 * (e >> 1)] = F[x][y][e] * f;
+    }
+  }
+  cp_async_wait<0>();
+}
+
+template <int DH, bool kLocal>
+hg_status scan_mma_t(const ScanArgs& a, cudaStream_t s) {
+  using C = Cfg<DH>;
+  static bool done = false;
+  if (!done) {
+    HG_CUDA(cudaFuncSetAttribute(scan_mma_kernel<DH, kLocal>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    done = true;
+  }
+  const int64_t items = a.n * (kLocal ? a.nseg - 1 : a.nseg) * a.heads * C::SL;
+  const int64_t grid = std::min<int64_t>(ceil_div(items, C::W), kSms * C::kBlocks);
+  return launch(kLocal ? "decay_scan_local_mma" : "decay_scan_mma", scan_mma_kernel<DH, kLocal>, dim3((unsigned)grid),
+                dim3(32 * C::W), C::kSmem, s, a);
+}
+
+}  // namespace
+
+hg_status scan_mma(const ScanArgs& a, int d_h, bool local, cudaStream_t s) {
+  if (d_h == 16) return local ? scan_mma_t<16, true>(a, s) : scan_mma_t<16, false>(a, s);
+  if (d_h == 32) return local ? scan_mma_t<32, true>(a, s) : scan_mma_t<32, false>(a, s);
+  if (d_h == 64) return local ? scan_mma_t<64, true>(a, s) : scan_mma_t<64, false>(a, s);
+  return local ? scan_mma_t<128, true>(a, s) : scan_mma_t<128, false>(a, s);
+}
+
+int scan_mma_warps(int heads, int d_h) { return heads * (d_h <= 32 ? 1 : d_h / 32); }
+
+int scan_mma_resident(int d_h) {
+  if (d_h == 16) return Cfg<16>::W * Cfg<16>::kBlocks;
+  if (d_h == 32) return Cfg<32>::W * Cfg<32>::kBlocks;
+  if (d_h == 64) return Cfg<64>::W * Cfg<64>::kBlocks;
+  return Cfg<128>::W * Cfg<128>::kBlocks;
+}
+
+}  // namespace hg
