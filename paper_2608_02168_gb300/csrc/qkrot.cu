@@ -273,10 +273,11 @@ void fill_args(RotArgs* a, const hg_qkrot_params* p, const int64_t* pos, int64_t
   a->heads = p->heads_q + p->heads_k;
   a->rot = p->rot;
   a->eps = p->eps;
-  for (int i = 0; i < p->rot / 2; ++i) {
-    const long double turns = powl((long double)p->base, -2.0L * i / p->rot) / 6.28318530717958647692528676655900577L;
-    a->freq[i] = (uint64_t)(turns * 18446744073709551616.0L + 0.5L);
-  }
+  if (p->rot == 0) return;
+  // powers by products: 64 of them stay within 2^-57 of their value, and powl is slow where it is emulated
+  const long double ratio = powl((long double)p->base, -2.0L / p->rot);
+  long double turns = 18446744073709551616.0L / 6.28318530717958647692528676655900577L;
+  for (int i = 0; i < p->rot / 2; ++i, turns *= ratio) a->freq[i] = (uint64_t)(turns + 0.5L);
 }
 
 }  // namespace
