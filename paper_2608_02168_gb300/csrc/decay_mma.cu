@@ -8,8 +8,8 @@
 // layout in which the next product wants its second operand, so the state goes from sum to operand without
 // leaving the registers; likewise the chunk's weights from q k^T to the product with v.  No warp waits for
 // another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand.  The
-// scaled values that are added to the state are split into two bf16 numbers (16 bits), since a state is an fp32
-// result that gathers them.
+// scaled values that are added to the state are split into two bf16 numbers (16 bits, far below the rows'
+// rounding), and into three (24 bits) where the state left behind, an fp32 result, is asked for.
 //
 // Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high and histories
 // are often shorter than one tile; at d_h = 32 a position moves 256 bytes and needs 9 kFLOP, which the warp
@@ -133,11 +133,14 @@ __device__ __forceinline__ void load_chunk(const ScanArgs& a, const Item& it, in
   }
 }
 
-// x (a pair of bf16) times (f0, f1) as a sum hi + lo of bf16 pairs
-__device__ __forceinline__ void scale_split(uint32_t x, float f0, float f1, uint32_t& hi, uint32_t& lo) {
-  const float y0 = __uint_as_float(x << 16) * f0, y1 = __uint_as_float(x & 0xffff0000u) * f1;
+// x (a pair of bf16) times (f0, f1) as a sum of three bf16 pairs
+__device__ __forceinline__ void scale_split(uint32_t x, float f0, float f1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  float y0 = __uint_as_float(x << 16) * f0, y1 = __uint_as_float(x & 0xffff0000u) * f1;
   hi = pack2_bf16(y0, y1);
-  lo = pack2_bf16(y0 - __uint_as_float(hi << 16), y1 - __uint_as_float(hi & 0xffff0000u));
+  y0 -= __uint_as_float(hi << 16);
+  y1 -= __uint_as_float(hi & 0xffff0000u);
+  mid = pack2_bf16(y0, y1);
+  lo = pack2_bf16(y0 - __uint_as_float(mid << 16), y1 - __uint_as_float(mid & 0xffff0000u));
 }
 
 template <int DH, bool kLocal>
@@ -314,11 +317,11 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
           const int r = 2 * t4 + (e & 1) + 8 * (e >> 1);
           f[e] = r < m ? a.c_in * expf(ld * (float)(base - tau0 - r)) : 0.f;
         }
-        uint32_t hi[MT][4], lo[MT][4];
+        uint32_t hi[MT][4], mid[MT][4], lo[MT][4];
 #pragma unroll
         for (int x = 0; x < MT; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], lo[x][e]);
+          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
 #pragma unroll
         for (int y = 0; y < NT; y += 2) {
           uint32_t kb[4];
@@ -327,8 +330,12 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
           for (int x = 0; x < MT; ++x) {
             mma(F[x][y], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[0], kb[1]);
             mma(F[x][y + 1], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[2], kb[3]);
-            mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
-            mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
+            mma(F[x][y], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[0], kb[1]);
+            mma(F[x][y + 1], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[2], kb[3]);
+            if (a.last) {
+              mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
+              mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
+            }
           }
         }
         some = true;

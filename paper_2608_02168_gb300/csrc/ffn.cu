@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
+#include "ffn_tc.cuh"
 #include "layer_kernels.cuh"
 
 namespace hg {
@@ -21,30 +22,16 @@ constexpr int kSms = 152;
 constexpr int kMaxF = 16384;
 
 // One operand as the tile loaders see it: element (r, c) at p[r * ld + c], rows r < nr, columns c < nc.
-template <typename T>
 struct Mat {
-  const T* p;
+  const float* p;
   int64_t ld, nr, nc;
 };
-
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) {
-  return *reinterpret_cast<const float4*>(p);
-}
-template <>
-__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
-                     __uint_as_float(v.y & 0xffff0000u));
-}
 
 // dst[k][x] for kBk of k and X of x (row stride X + 4) from an operand whose rows are x and columns k
 // (kByRow) or whose rows are k and columns x.  Zero outside.  nr, nc and the starts are such that four
 // neighbouring columns are all inside or all outside.
-template <typename T, int X, bool kByRow>
-__device__ __forceinline__ void stage(float* dst, const Mat<T>& a, int64_t x0, int64_t k0) {
+template <int X, bool kByRow>
+__device__ __forceinline__ void stage(float* dst, const Mat& a, int64_t x0, int64_t k0) {
   constexpr int PER = X * kBk / 4 / kThr;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -53,7 +40,7 @@ __device__ __forceinline__ void stage(float* dst, const Mat<T>& a, int64_t x0, i
     const int c = (kByRow ? e % (kBk / 4) : e % (X / 4)) * 4;
     const int64_t row = (kByRow ? x0 : k0) + r, col = (kByRow ? k0 : x0) + c;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < a.nr && col < a.nc) v = load4(a.p + row * a.ld + col);
+    if (row < a.nr && col < a.nc) v = *reinterpret_cast<const float4*>(a.p + row * a.ld + col);
     if (kByRow) {
       dst[(c + 0) * (X + 4) + r] = v.x;
       dst[(c + 1) * (X + 4) + r] = v.y;
@@ -96,9 +83,8 @@ __device__ __forceinline__ void mul(const float* A, const float* B, Acc& acc) {
 
 // H = act(X W_gate) * (X W_up), a tile a block, the column tiles of a row tile one after another; with kBwd also
 // dH = dY W_down^T, and dG, dU.
-template <typename T, int kAct, bool kBwd>
-__global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat<T> X, Mat<T> Wg, Mat<T> Wu, Mat<T> dY, Mat<T> Wd,
-                                                        float* __restrict__ H, float* __restrict__ dG,
+template <int kAct, bool kBwd>
+__global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, Mat dY, Mat Wd, float* __restrict__ H, float* __restrict__ dG,
                                                         float* __restrict__ dU) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)], Cs[kBk * (kBn + 4)];
@@ -110,12 +96,12 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat<T> X, Mat<T> Wg, Mat
   u.zero();
   h.zero();
   for (int64_t k0 = 0; k0 < X.nc; k0 += kBk) {
-    stage<T, kBm, true>(As, X, r0, k0);
-    stage<T, kBn, false>(Bs, Wg, c0, k0);
-    stage<T, kBn, false>(Cs, Wu, c0, k0);
+    stage<kBm, true>(As, X, r0, k0);
+    stage<kBn, false>(Bs, Wg, c0, k0);
+    stage<kBn, false>(Cs, Wu, c0, k0);
     if (kBwd) {
-      stage<T, kBm, true>(Ds, dY, r0, k0);
-      stage<T, kBn, true>(Es, Wd, c0, k0);
+      stage<kBm, true>(Ds, dY, r0, k0);
+      stage<kBn, true>(Es, Wd, c0, k0);
     }
     __syncthreads();
     mul(As, Bs, g);
@@ -152,9 +138,9 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat<T> X, Mat<T> Wg, Mat
 }
 
 // out = A B (+ A2 B2) (+ add): the second product when A2.p is set; kTransB: B given by its transpose.
-template <typename T, bool kTransB>
-__global__ void __launch_bounds__(kThr) ffn_out_simt(Mat<float> A, Mat<T> B, Mat<float> A2, Mat<T> B2, const T* add,
-                                                     T* __restrict__ out, int64_t nc) {
+template <bool kTransB>
+__global__ void __launch_bounds__(kThr) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B2, const float* add,
+                                                     float* __restrict__ out, int64_t nc) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
   const int ctiles = (int)((nc + kBn - 1) / kBn);
@@ -163,8 +149,8 @@ __global__ void __launch_bounds__(kThr) ffn_out_simt(Mat<float> A, Mat<T> B, Mat
   acc.zero();
   for (int half = 0; half < (A2.p ? 2 : 1); ++half) {
     for (int64_t k0 = 0; k0 < A.nc; k0 += kBk) {
-      stage<float, kBm, true>(As, half ? A2 : A, r0, k0);
-      stage<T, kBn, kTransB>(Bs, half ? B2 : B, c0, k0);
+      stage<kBm, true>(As, half ? A2 : A, r0, k0);
+      stage<kBn, kTransB>(Bs, half ? B2 : B, c0, k0);
       __syncthreads();
       mul(As, Bs, acc);
       __syncthreads();
@@ -176,29 +162,26 @@ __global__ void __launch_bounds__(kThr) ffn_out_simt(Mat<float> A, Mat<T> B, Mat
   for (int i = 0; i < 8; ++i) {
     const int64_t row = r0 + acc_row(i);
     if (row >= A.nr) continue;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t at = row * nc + col + j;
-      out[at] = from_f32<T>(acc.v[i][j] + (add ? to_f32(add[at]) : 0.f));
-    }
+    const int64_t at = row * nc + col;
+    const float4 x = add ? *reinterpret_cast<const float4*>(add + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<float4*>(out + at) =
+        make_float4(acc.v[i][0] + x.x, acc.v[i][1] + x.y, acc.v[i][2] + x.z, acc.v[i][3] + x.w);
   }
 }
 
 // part[blockIdx.z] = A^T B over the split's rows (A: rows x mc, B: rows x nc).
-template <typename TA, typename TB>
-__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat<TA> A, Mat<TB> B, int64_t rows, float* __restrict__ part) {
+__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat A, Mat B, int64_t rows, float* __restrict__ part) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
   const int64_t m0 = (int64_t)blockIdx.y * kBm, c0 = (int64_t)blockIdx.x * kBn;
   const int64_t k1 = min(A.nr, (int64_t)(blockIdx.z + 1) * rows);
-  Mat<TA> Ae = A;
-  Mat<TB> Be = B;
+  Mat Ae = A, Be = B;
   Ae.nr = Be.nr = k1;
   Acc acc;
   acc.zero();
   for (int64_t k0 = (int64_t)blockIdx.z * rows; k0 < k1; k0 += kBk) {
-    stage<TA, kBm, false>(As, Ae, m0, k0);
-    stage<TB, kBn, false>(Bs, Be, c0, k0);
+    stage<kBm, false>(As, Ae, m0, k0);
+    stage<kBn, false>(Bs, Be, c0, k0);
     __syncthreads();
     mul(As, Bs, acc);
     __syncthreads();
@@ -247,64 +230,66 @@ void carve_simt(void* scratch, const hg_ffn_params* p, int64_t n, bool bwd, FfnL
   if (bytes) *bytes = k.used;
 }
 
-template <typename T, int kAct, bool kBwd>
+template <int kAct, bool kBwd>
 hg_status hidden(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, const FfnLayout& L, cudaStream_t s) {
   const int64_t d = p->d, f = p->f;
-  const Mat<T> x{(const T*)X, d, n, d}, g{(const T*)p->W_gate, f, d, f}, u{(const T*)p->W_up, f, d, f},
-      dy{(const T*)dY, d, n, d}, w{(const T*)p->W_down, d, f, d};
-  return launch(kBwd ? "ffn_hidden_bwd_simt" : "ffn_hidden_simt", ffn_hidden_simt<T, kAct, kBwd>,
+  const Mat x{(const float*)X, d, n, d}, g{(const float*)p->W_gate, f, d, f}, u{(const float*)p->W_up, f, d, f},
+      dy{(const float*)dY, d, n, d}, w{(const float*)p->W_down, d, f, d};
+  return launch(kBwd ? "ffn_hidden_bwd_simt" : "ffn_hidden_simt", ffn_hidden_simt<kAct, kBwd>,
                 dim3((unsigned)(ceil_div(f, kBn) * ceil_div(n, kBm))), dim3(kThr), 0, s, x, g, u, dy, w, L.H,
                 L.dG, L.dU);
 }
 
-template <typename T, bool kBwd>
+template <bool kBwd>
 hg_status hidden_act(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, const FfnLayout& L,
                      cudaStream_t s) {
-  if (p->act == HG_ACT_RELU) return hidden<T, HG_ACT_RELU, kBwd>(p, X, n, dY, L, s);
-  if (p->act == HG_ACT_GELU_TANH) return hidden<T, HG_ACT_GELU_TANH, kBwd>(p, X, n, dY, L, s);
-  if (p->act == HG_ACT_SILU) return hidden<T, HG_ACT_SILU, kBwd>(p, X, n, dY, L, s);
-  return hidden<T, HG_ACT_NONE, kBwd>(p, X, n, dY, L, s);
+  if (p->act == HG_ACT_RELU) return hidden<HG_ACT_RELU, kBwd>(p, X, n, dY, L, s);
+  if (p->act == HG_ACT_GELU_TANH) return hidden<HG_ACT_GELU_TANH, kBwd>(p, X, n, dY, L, s);
+  if (p->act == HG_ACT_SILU) return hidden<HG_ACT_SILU, kBwd>(p, X, n, dY, L, s);
+  return hidden<HG_ACT_NONE, kBwd>(p, X, n, dY, L, s);
 }
 
-template <typename TA, typename TB>
-hg_status wgrad(const TA* A, int64_t mc, const TB* B, int64_t nc, int64_t n, const FfnLayout& L, int splits, float* out,
-                cudaStream_t s) {
-  const Mat<TA> a{A, mc, n, mc};
-  const Mat<TB> b{B, nc, n, nc};
+hg_status wgrad(const float* A, int64_t mc, const float* B, int64_t nc, int64_t n, const FfnLayout& L, int splits,
+                float* out, cudaStream_t s) {
+  const Mat a{A, mc, n, mc}, b{B, nc, n, nc};
   const int64_t rows = (int64_t)align_up((size_t)ceil_div(n, splits), kBk);
-  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt<TA, TB>,
+  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt,
                 dim3((unsigned)ceil_div(nc, kBn), (unsigned)ceil_div(mc, kBm), (unsigned)splits), dim3(kThr), 0, s, a,
                 b, rows, L.part));
   return reduce_partials(L.part, mc * nc, splits, mc * nc, out, L.tmp, s);
 }
 
-template <typename T>
 hg_status fwd_simt(const hg_ffn_params* p, const void* X, int64_t n, void* Y, const FfnLayout& L, cudaStream_t s) {
   const int64_t d = p->d, f = p->f;
-  HG_TRY((hidden_act<T, false>(p, X, n, nullptr, L, s)));
-  const Mat<float> h{L.H, f, n, f}, none{};
-  const Mat<T> w{(const T*)p->W_down, d, f, d};
-  return launch("ffn_out_simt", ffn_out_simt<T, false>, dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))),
-                dim3(kThr), 0, s, h, w, none, w, (const T*)(p->residual ? X : nullptr), (T*)Y, d);
+  HG_TRY((hidden_act<false>(p, X, n, nullptr, L, s)));
+  const Mat h{L.H, f, n, f}, w{(const float*)p->W_down, d, f, d}, none{};
+  return launch("ffn_out_simt", ffn_out_simt<false>, dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))), dim3(kThr),
+                0, s, h, w, none, w, (const float*)(p->residual ? X : nullptr), (float*)Y, d);
 }
 
-template <typename T>
 hg_status bwd_simt(const hg_ffn_params* p, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
                    const FfnLayout& L, cudaStream_t s) {
   const int64_t d = p->d, f = p->f;
-  HG_TRY((hidden_act<T, true>(p, X, n, dY, L, s)));
+  HG_TRY((hidden_act<true>(p, X, n, dY, L, s)));
   if (dX) {
-    const Mat<float> a{L.dG, f, n, f}, a2{L.dU, f, n, f};
-    const Mat<T> b{(const T*)p->W_gate, f, d, f}, b2{(const T*)p->W_up, f, d, f};
-    HG_TRY(launch("ffn_dx_simt", ffn_out_simt<T, true>,
-                  dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))), dim3(kThr), 0, s, a, b, a2, b2,
-                  (const T*)(p->residual ? dY : nullptr), (T*)dX, d));
+    const Mat a{L.dG, f, n, f}, a2{L.dU, f, n, f}, b{(const float*)p->W_gate, f, d, f},
+        b2{(const float*)p->W_up, f, d, f};
+    HG_TRY(launch("ffn_dx_simt", ffn_out_simt<true>, dim3((unsigned)(ceil_div(d, kBn) * ceil_div(n, kBm))), dim3(kThr),
+                  0, s, a, b, a2, b2, (const float*)(p->residual ? dY : nullptr), (float*)dX, d));
   }
   if (!g) return HG_OK;
   const int sp = wg_splits(n, p->d, p->f);
-  HG_TRY(wgrad((const T*)X, d, L.dG, f, n, L, sp, g->dW_gate, s));
-  HG_TRY(wgrad((const T*)X, d, L.dU, f, n, L, sp, g->dW_up, s));
-  return wgrad(L.H, f, (const T*)dY, d, n, L, sp, g->dW_down, s);
+  HG_TRY(wgrad((const float*)X, d, L.dG, f, n, L, sp, g->dW_gate, s));
+  HG_TRY(wgrad((const float*)X, d, L.dU, f, n, L, sp, g->dW_up, s));
+  return wgrad(L.H, f, (const float*)dY, d, n, L, sp, g->dW_down, s);
+}
+
+size_t scratch_bytes(const hg_ffn_params* p, int64_t n, bool bwd) {
+  if (p->dtype == HG_BF16) return bwd ? ffn_bwd_tc_scratch(p, n) : 0;
+  FfnLayout L;
+  size_t bytes = 0;
+  carve_simt(nullptr, p, n, bwd, &L, &bytes);
+  return bytes;
 }
 
 hg_status check_params(const hg_ffn_params* p, int64_t n) {
@@ -338,9 +323,8 @@ extern "C" hg_status hg_ffn_workspace_size(const hg_ffn_params* params, int64_t 
   clear_error();
   HG_REQUIRE(fwd_bytes && bwd_bytes, "fwd_bytes and bwd_bytes must be non-null");
   HG_TRY(check_params(params, n));
-  FfnLayout L;
-  carve_simt(nullptr, params, n, false, &L, fwd_bytes);
-  carve_simt(nullptr, params, n, true, &L, bwd_bytes);
+  *fwd_bytes = scratch_bytes(params, n, false);
+  *bwd_bytes = scratch_bytes(params, n, true);
   return HG_OK;
 }
 
@@ -351,14 +335,14 @@ extern "C" hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int6
   HG_TRY(check_params(params, n));
   HG_TRY(check_weights(params));
   if (n == 0) return HG_OK;
-  HG_REQUIRE(X && Y && scratch, "X, Y and scratch must be non-null");
+  HG_REQUIRE(X && Y && (scratch || params->dtype == HG_BF16), "X, Y and scratch must be non-null");
   HG_REQUIRE((((uintptr_t)X | (uintptr_t)Y) & 15) == 0, "X and Y must be 16-byte aligned");
   HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (params->dtype == HG_BF16) return ffn_fwd_tc(params, X, n, Y, s);
   FfnLayout L;
   carve_simt(scratch, params, n, false, &L, nullptr);
-  if (params->dtype == HG_F32) return fwd_simt<float>(params, X, n, Y, L, s);
-  return fwd_simt<__nv_bfloat16>(params, X, n, Y, L, s);
+  return fwd_simt(params, X, n, Y, L, s);
 }
 
 extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
@@ -384,8 +368,8 @@ extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int6
   HG_REQUIRE((((uintptr_t)X | (uintptr_t)dY | (uintptr_t)dX) & 15) == 0, "X, dY and dX must be 16-byte aligned");
   HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
   if (!dX && !grads) return HG_OK;
+  if (params->dtype == HG_BF16) return ffn_bwd_tc(params, X, n, dY, dX, grads, scratch, s);
   FfnLayout L;
   carve_simt(scratch, params, n, true, &L, nullptr);
-  if (params->dtype == HG_F32) return bwd_simt<float>(params, X, n, dY, dX, grads, L, s);
-  return bwd_simt<__nv_bfloat16>(params, X, n, dY, dX, grads, L, s);
+  return bwd_simt(params, X, n, dY, dX, grads, L, s);
 }

@@ -1,0 +1,725 @@
+// Gated feed-forward block on the tensor cores (bf16 storage, fp32 accumulation), backward.
+//
+//   [G | U] = X [W_gate | W_up] and dH = dY W_down^T again, chunk by chunk of the hidden features
+//   dG = dH * U * act'(G), dU = dH * act(G), H = act(G) * U
+//   dX = dG W_gate^T + dU W_up^T (+ dY)                               (ffn_dx_tc)
+//   dW_gate = X^T dG, dW_up = X^T dU, dW_down^T = dY^T H              (ffn_wgrad_tc)
+//
+// The hidden rows are formed twice, once in each kernel, instead of being stored: three of the five and of the
+// nine products are theirs, but n x f values written and read would take an order of magnitude longer.
+//
+// ffn_dx_tc: as the forward (ffn_tc.cu), one 128-row tile at a time.  The weights' pieces serve twice, as
+// MN-major operands of [G | U] and as K-major operands of dX.  dG and dU are rounded to bf16.  At d = 256
+// X, dY and a chunk's weights fill the shared memory, so dG and dU go back to tensor memory, as the products'
+// first operand.
+//
+// ffn_wgrad_tc: a CTA owns a chunk of hidden features, keeps its weights in shared memory and its gradients
+// in tensor memory, and takes a share of the row tiles.  The gradients are fp32 results, so dG, dU and H enter
+// as sums of two bf16 numbers (16 bits): one rounding would leave them with three digits.  The tensor pipe's own
+// additions cut their results short, which shrinks a long sum (3.8e-5 of it over 16000 rows): each tile's products
+// are therefore drained into registers and added there.  The shares' sums are added in order.  With d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the
+// products is not used: a 64-wide one would run at half the rate).
+//
+// Bound by the tensor pipe (16 d f flops a row are needed; 28 are run).
+#include <algorithm>
+
+#include "ffn_kernels.cuh"
+#include "ffn_tc.cuh"
+#include "layer_kernels.cuh"
+#include "tc_util.cuh"
+
+namespace hg {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kRows = 128;
+constexpr int kBlk = kRows * 128;  // a 64-column block of a 128-row tile
+constexpr int kThreads = 384;      // warps 0..3: TMA, MMA issue, tensor memory, idle; two warpgroups for the gates
+constexpr int kSms = 152;
+
+__device__ __forceinline__ void ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// eight 32-bit columns of this thread's lane
+__device__ __forceinline__ void st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D += A[tmem] B[smem]: A's lane = row, each 32-bit column two bf16 along K
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ uint8_t* align1024(uint8_t* p) {
+  return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~uintptr_t(1023));
+}
+
+// A bounded wait of a role: false, and the give-up recorded once, when it runs out.
+struct Waiter {
+  int* status;
+  bool ok = true;
+  __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity) {
+    if (ok && !mbar_wait(b, parity)) {
+      ok = false;
+      record_device_error(status, kErrTimeout);
+    }
+    if (ok) fence_after_sync();
+    return ok;
+  }
+};
+
+// ---------------------------------------------------------------------------------------------
+// dX
+// ---------------------------------------------------------------------------------------------
+template <int D>
+struct DxCfg {
+  static constexpr int HC = 64;
+  static constexpr int NB = D / 64;
+  static constexpr bool kTs = D == 256;              // dG, dU in tensor memory
+  static constexpr int SLOTS = kTs ? 1 : 2;
+  static constexpr int NG = D == 256 ? 1 : 3;        // ring of [W_gate | W_up]
+  static constexpr int ND = D == 256 ? 1 : 2;        // ring of W_down
+  static constexpr int kGu = D * 128 * 2, kDown = HC * D * 2;
+  static constexpr int kX = NB * kBlk;
+  static constexpr int kOps = kTs ? 0 : 2 * kBlk;    // dG, dU: 64 columns each
+  static constexpr int kSmem = 2 * kX + NG * kGu + ND * kDown + kOps + 512 + 1024;
+  static constexpr int PR = D < 128 ? D : 128;       // rows of a TMA box of [W_gate | W_up]
+  // tensor memory: dX, the slots ([G | U | dH], 192 columns), dG and dU (kTs)
+  static constexpr uint32_t kSlot = D, kSlotCols = 192, kOpsCol = 448;
+};
+
+struct DxP {
+  int64_t n;
+  int nch;
+  int64_t tiles;
+  const __nv_bfloat16* res;  // dY, or null without the residual
+  __nv_bfloat16* dX;
+  int* status;
+};
+
+template <int D, int kAct>
+__global__ void __launch_bounds__(kThreads, 1)
+    ffn_dx_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_dY,
+                     const __grid_constant__ CUtensorMap tm_G, const __grid_constant__ CUtensorMap tm_U,
+                     const __grid_constant__ CUtensorMap tm_W, DxP p) {
+  pdl_begin();
+  using C = DxCfg<D>;
+  constexpr int NB = C::NB, HC = C::HC, NG = C::NG, ND = C::ND, SLOTS = C::SLOTS;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* Xs = align1024(smem_raw);
+  uint8_t* Ys = Xs + C::kX;
+  uint8_t* Gs = Ys + C::kX;
+  uint8_t* Ds = Gs + NG * C::kGu;
+  uint8_t* Os = Ds + ND * C::kDown;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + C::kOps);
+  uint64_t *wfull = bars, *wfree = wfull + NG, *dfull = wfree + NG, *dfree = dfull + ND, *xfull = dfree + ND,
+           *xfree = xfull + 1, *gfull = xfree + 1, *ofull = gfull + 2, *ofree = ofull + 1, *yfull = ofree + 1,
+           *yfree = yfull + 1, *quit = yfree + 1;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NG; ++i) {
+      mbar_init(&wfull[i], 1);
+      mbar_init(&wfree[i], 1);
+    }
+    for (int i = 0; i < ND; ++i) {
+      mbar_init(&dfull[i], 1);
+      mbar_init(&dfree[i], 1);
+    }
+    mbar_init(xfull, 1);
+    mbar_init(xfree, 1);
+    mbar_init(&gfull[0], 1);
+    mbar_init(&gfull[1], 1);
+    mbar_init(ofull, SLOTS == 2 ? 128 : 256);
+    mbar_init(ofree, 1);
+    mbar_init(yfull, 1);
+    mbar_init(yfree, 256);
+    mbar_init(quit, 1);
+    fence_mbar_init();
+  }
+  if (warp == 2) tmem_alloc(tslot, 512);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *tslot;
+  const int nch = p.nch;
+
+  if (warp == 0 && lane == 0) {
+    Waiter wait{p.status};
+    uint32_t q = 0, xn = 0;  // chunks and tiles asked for
+    for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x) {
+      if (xn >= 1 && !wait(xfree, (xn - 1) & 1)) break;
+      mbar_expect_tx(xfull, 2 * C::kX);
+      for (int b = 0; b < NB; ++b) {
+        tma_load_2d(Xs + b * kBlk, &tm_X, b * 64, (int)(tile * kRows), xfull);
+        tma_load_2d(Ys + b * kBlk, &tm_dY, b * 64, (int)(tile * kRows), xfull);
+      }
+      ++xn;
+      for (int c = 0; c < nch; ++c, ++q) {
+        const uint32_t sg = q % NG, sd = q % ND;
+        if (q >= ND && !wait(&dfree[sd], (q / ND - 1) & 1)) break;
+        mbar_expect_tx(&dfull[sd], C::kDown);
+        for (int b = 0; b < NB; ++b)
+          tma_load_2d(Ds + sd * C::kDown + b * HC * 128, &tm_W, b * 64, c * HC, &dfull[sd]);
+        if (q >= NG && !wait(&wfree[sg], (q / NG - 1) & 1)) {
+          mbar_wait(&dfull[sd], (q / ND) & 1);
+          break;
+        }
+        mbar_expect_tx(&wfull[sg], C::kGu);
+        uint8_t* dst = Gs + sg * C::kGu;
+        for (int r = 0; r < D; r += C::PR) {
+          tma_load_2d(dst + r * 128, &tm_G, c * HC, r, &wfull[sg]);
+          tma_load_2d(dst + D * 128 + r * 128, &tm_U, c * HC, r, &wfull[sg]);
+        }
+      }
+    }
+    if (!wait.ok) {  // what was asked for lands before the CTA ends
+      if (xn) mbar_wait(xfull, (xn - 1) & 1);
+      drain_rounds(dfull, ND, q);
+      drain_rounds(wfull, NG, q);
+    }
+  } else if (warp == 1 && lane == 0) {
+    Waiter wait{p.status};
+    uint32_t q = 0, ti = 0;  // q: chunks whose [G | U | dH] was issued
+    const uint32_t xs = smem_u32(Xs), ys = smem_u32(Ys), gs = smem_u32(Gs), ds = smem_u32(Ds), os = smem_u32(Os);
+    constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_h = idesc_bf16(128, 64, false, false),
+                       id_dx = idesc_bf16(128, D, false, false);
+    auto hidden = [&](int s) {
+      const uint32_t sg = q % NG, sd = q % ND;
+      if (!wait(&wfull[sg], (q / NG) & 1) || !wait(&dfull[sd], (q / ND) & 1)) return;
+      const uint32_t w = gs + sg * C::kGu, w2 = ds + sd * C::kDown, t = tmem + C::kSlot + s * C::kSlotCols;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        mma_bf16(t, desc_sw128(xs + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
+                 desc_sw128(w + j * 2048, D * 128, 1024), id_gu, j > 0 ? 1u : 0u);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        mma_bf16(t + 128, desc_sw128(ys + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
+                 desc_sw128(w2 + (j >> 2) * (HC * 128) + (j & 3) * 32, 16, 1024), id_h, j > 0 ? 1u : 0u);
+      mma_commit(&gfull[s]);
+      mma_commit(&dfree[sd]);
+      ++q;
+    };
+    uint32_t done = 0;  // chunks whose dX was issued
+    for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
+      if (!wait(xfull, ti & 1)) break;
+      for (int c = 0; wait.ok && c < SLOTS && c < nch; ++c) hidden(c % SLOTS);
+      if (wait.ok && nch <= SLOTS) mma_commit(xfree);
+      for (int c = 0; wait.ok && c < nch; ++c) {
+        if (!wait(ofull, done & 1)) break;
+        if (c == 0 && ti >= 1 && !wait(yfree, (ti - 1) & 1)) break;
+        const uint32_t w = gs + done % NG * C::kGu;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int j = 0; j < HC / 16; ++j) {
+            const uint64_t b = desc_sw128(w + half * D * 128 + j * 32, 16, 1024);
+            const uint32_t acc = (c > 0 || half > 0 || j > 0) ? 1u : 0u;
+            if (C::kTs)
+              mma_bf16_ts(tmem, tmem + C::kOpsCol + half * 32 + j * 8, b, id_dx, acc);
+            else
+              mma_bf16(tmem, desc_sw128(os + half * kBlk + j * 32, 16, 1024), b, id_dx, acc);
+          }
+        mma_commit(ofree);
+        mma_commit(&wfree[done % NG]);
+        ++done;
+        if (c == nch - 1) mma_commit(yfull);
+        if (c + SLOTS < nch) {
+          hidden((c + SLOTS) % SLOTS);
+          if (wait.ok && c + SLOTS == nch - 1) mma_commit(xfree);
+        }
+      }
+    }
+    if (!wait.ok) drain_mma(quit, 0);
+  } else if (warp >= 4) {
+    const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const int s = SLOTS == 2 ? wg : 0;
+    const uint32_t t0 = tmem + C::kSlot + s * C::kSlotCols + lane_off;
+    constexpr int HW = SLOTS == 2 ? HC : HC / 2;  // hidden features of a warpgroup
+    const int h0 = SLOTS == 2 ? 0 : wg * HW;
+    Waiter one{p.status};
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      one(b, parity);
+      one.ok = __all_sync(0xffffffffu, one.ok);
+      return one.ok;
+    };
+    uint32_t k = 0, done = 0, ti = 0;  // chunks of this slot, of all slots; tiles
+    for (int64_t tile = blockIdx.x; one.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
+      for (int c = 0; one.ok && c < nch; ++c, ++done) {
+        if (SLOTS == 2 && (c & 1) != s) continue;
+        if (!wait(&gfull[s], k & 1)) break;
+        ++k;
+        uint32_t dg[HW / 2], du[HW / 2];
+#pragma unroll
+        for (int x = 0; x < HW; x += 16) {
+          uint32_t g[16], u[16], h[16];
+          ld16_issue(t0 + h0 + x, g);
+          ld16_issue(t0 + 64 + h0 + x, u);
+          ld16_issue(t0 + 128 + h0 + x, h);
+          ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            float a0, a1, d0, d1;
+            gate_grad2<kAct>(__uint_as_float(g[e]), __uint_as_float(g[e + 1]), &a0, &a1, &d0, &d1);
+            const float y0 = __uint_as_float(h[e]), y1 = __uint_as_float(h[e + 1]);
+            dg[(x + e) / 2] = pack2_bf16(y0 * __uint_as_float(u[e]) * d0, y1 * __uint_as_float(u[e + 1]) * d1);
+            du[(x + e) / 2] = pack2_bf16(y0 * a0, y1 * a1);
+          }
+        }
+        if (done >= 1 && !wait(ofree, (done - 1) & 1)) break;
+        if (C::kTs) {
+#pragma unroll
+          for (int x = 0; x < HW / 2; x += 8) {
+            st8(tmem + C::kOpsCol + lane_off + h0 / 2 + x, dg + x);
+            st8(tmem + C::kOpsCol + 32 + lane_off + h0 / 2 + x, du + x);
+          }
+          st_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < HW / 8; ++e) {
+            st16(Os + sw128_offset(row, e * 16), make_uint4(dg[4 * e], dg[4 * e + 1], dg[4 * e + 2], dg[4 * e + 3]));
+            st16(Os + kBlk + sw128_offset(row, e * 16),
+                 make_uint4(du[4 * e], du[4 * e + 1], du[4 * e + 2], du[4 * e + 3]));
+          }
+          fence_async_smem();
+        }
+        fence_before_sync();
+        mbar_arrive(ofull);
+      }
+      if (!one.ok) break;
+      constexpr int CW = D / 2;
+      const int64_t r = tile * kRows + row;
+      const bool live = r < p.n;
+      if (!wait(yfull, ti & 1)) break;
+#pragma unroll
+      for (int c = 0; c < CW; c += 16) {
+        uint32_t y[16];
+        ld16_issue(tmem + lane_off + wg * CW + c, y);
+        uint4 x[2];
+        if (p.res && live) {
+          x[0] = ldg16(p.res + r * D + wg * CW + c);
+          x[1] = ldg16(p.res + r * D + wg * CW + c + 8);
+        }
+        ld_wait();
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float v[8];
+            if (p.res) {
+              unpack(x[e], v, __nv_bfloat16());
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(y[e * 8 + i]);
+            st16(p.dX + r * D + wg * CW + c + e * 8, pack(v, __nv_bfloat16()));
+          }
+        }
+      }
+      fence_before_sync();
+      mbar_arrive(yfree);
+    }
+  }
+  fence_before_sync();
+  __syncthreads();
+  if (warp == 2) tmem_dealloc(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------------------------
+// weight gradients
+// ---------------------------------------------------------------------------------------------
+template <int D>
+struct WgCfg {
+  static constexpr int HC = D == 256 ? 32 : 64;
+  static constexpr int NB = D / 64;
+  static constexpr int MB = D == 256 ? 2 : 1;         // 128-row blocks of the gradients
+  static constexpr int XS = D == 64 ? 2 : 1;          // row tiles in flight
+  static constexpr int kX = NB * kBlk;
+  static constexpr int N2 = 2 * HC;                   // columns of [dG | dU] and of [H hi | H lo]
+  static constexpr int OB = N2 / 64;                  // their 64-column blocks
+  static constexpr int kW = N2 * D * 2, kDown = HC * D * 2;
+  static constexpr int kOps = OB * kBlk;
+  static constexpr int kSmem = XS * 2 * kX + kW + kDown + 3 * kOps + 512 + 1024;
+  // tensor memory: gradients ([dG | dU] of each block, then [H hi | H lo]), then [G | U | dH]
+  static constexpr uint32_t kAcc2 = MB * N2, kHid = 2 * MB * N2;
+};
+
+struct WgP {
+  int64_t n, tiles;
+  int f, splits, chunks;
+  float* part;  // [splits][3 d f]
+  int* status;
+};
+
+template <int D, int kAct>
+__global__ void __launch_bounds__(kThreads, 1)
+    ffn_wgrad_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_dY,
+                        const __grid_constant__ CUtensorMap tm_Wt, const __grid_constant__ CUtensorMap tm_W, WgP p) {
+  pdl_begin();
+  using C = WgCfg<D>;
+  constexpr int NB = C::NB, HC = C::HC, XS = C::XS, MB = C::MB, N2 = C::N2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* Xs = align1024(smem_raw);               // [XS] (X tile, dY tile)
+  uint8_t* Ws = Xs + XS * 2 * C::kX;
+  uint8_t* Ds = Ws + C::kW;
+  uint8_t* Os = Ds + C::kDown;                     // [dG | dU] hi, lo, [H hi | H lo]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + 3 * C::kOps);
+  uint64_t *wfull = bars, *xfull = bars + 1, *xfree = xfull + 2, *gfull = xfree + 2, *ofull = gfull + 1,
+           *ofree = ofull + 1, *quit = ofree + 1;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(wfull, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&xfull[i], 1);
+      mbar_init(&xfree[i], 1);
+    }
+    mbar_init(gfull, 1);
+    mbar_init(ofull, 256);
+    mbar_init(ofree, 1);
+    mbar_init(quit, 1);
+    fence_mbar_init();
+  }
+  if (warp == 2) tmem_alloc(tslot, 512);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *tslot;
+  const int chunk = blockIdx.x % p.chunks, split = blockIdx.x / p.chunks;
+  const int64_t tile0 = p.tiles * split / p.splits, tile1 = p.tiles * (split + 1) / p.splits;
+  const int count = (int)(tile1 - tile0);  // at least one
+
+  if (warp == 0 && lane == 0) {
+    Waiter wait{p.status};
+    mbar_expect_tx(wfull, C::kW + C::kDown);
+    for (int b = 0; b < NB; ++b) {
+      tma_load_2d(Ws + b * N2 * 128, &tm_Wt, b * 64, chunk * N2, wfull);
+      tma_load_2d(Ds + b * HC * 128, &tm_W, b * 64, chunk * HC, wfull);
+    }
+    uint32_t q = 0;
+    for (; q < (uint32_t)count; ++q) {
+      const uint32_t s = q % XS;
+      if (q >= XS && !wait(&xfree[s], (q / XS - 1) & 1)) break;
+      mbar_expect_tx(&xfull[s], 2 * C::kX);
+      uint8_t* dst = Xs + s * 2 * C::kX;
+      const int r = (int)((tile0 + q) * kRows);
+      for (int b = 0; b < NB; ++b) {
+        tma_load_2d(dst + b * kBlk, &tm_X, b * 64, r, &xfull[s]);
+        tma_load_2d(dst + C::kX + b * kBlk, &tm_dY, b * 64, r, &xfull[s]);
+      }
+    }
+    if (!wait.ok) {
+      mbar_wait(wfull, 0);
+      drain_rounds(xfull, XS, q);
+    }
+  } else if (warp == 1 && lane == 0) {
+    Waiter wait{p.status};
+    const uint32_t xs = smem_u32(Xs), ws = smem_u32(Ws), ds = smem_u32(Ds), os = smem_u32(Os);
+    constexpr uint32_t id_gu = idesc_bf16(128, N2, false, false), id_h = idesc_bf16(128, HC, false, false),
+                       id_w = idesc_bf16(128, N2, true, true);
+    wait(wfull, 0);
+    for (int i = 0; wait.ok && i < count; ++i) {
+      const int s = i % XS;
+      if (!wait(&xfull[s], (i / XS) & 1)) break;
+      if (i >= 1 && !wait(ofull, (i - 1) & 1)) break;  // the hidden sums of the tile before were read
+      const uint32_t x = xs + s * 2 * C::kX, y = x + C::kX, hid = tmem + C::kHid;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        mma_bf16(hid, desc_sw128(x + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
+                 desc_sw128(ws + (j >> 2) * (N2 * 128) + (j & 3) * 32, 16, 1024), id_gu, j > 0 ? 1u : 0u);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        mma_bf16(hid + N2, desc_sw128(y + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
+                 desc_sw128(ds + (j >> 2) * (HC * 128) + (j & 3) * 32, 16, 1024), id_h, j > 0 ? 1u : 0u);
+      mma_commit(gfull);
+      if (!wait(ofull, i & 1)) break;
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        // d = 64: X and dY side by side are the 128 rows of both gradients
+        const uint32_t ax = x + m * 2 * kBlk, ay = D == 64 ? x : y + m * 2 * kBlk;
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            mma_bf16(tmem + m * N2, desc_sw128(ax + j * 2048, kBlk, 1024),
+                     desc_sw128(os + part * C::kOps + j * 2048, kBlk, 1024), id_w, (part > 0 || j > 0) ? 1u : 0u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          mma_bf16(tmem + C::kAcc2 + m * N2, desc_sw128(ay + j * 2048, kBlk, 1024),
+                   desc_sw128(os + 2 * C::kOps + j * 2048, kBlk, 1024), id_w, j > 0 ? 1u : 0u);
+      }
+      mma_commit(&xfree[s]);
+      mma_commit(ofree);
+    }
+    if (!wait.ok) drain_mma(quit, 0);
+  } else if (warp >= 4) {
+    const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    constexpr int HW = HC / 2;  // hidden features of a warpgroup
+    const int h0 = wg * HW;
+    const uint32_t hid = tmem + C::kHid + lane_off;
+    Waiter one{p.status};
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      one(b, parity);
+      one.ok = __all_sync(0xffffffffu, one.ok);
+      return one.ok;
+    };
+    // 16 bytes (8 features from column c of an operand block pair) of this row
+    auto put = [&](uint8_t* o, int c, const uint32_t* v) {
+      st16(o + (c >> 6) * kBlk + sw128_offset(row, (c & 63) * 2), make_uint4(v[0], v[1], v[2], v[3]));
+    };
+    // This thread's 96 sums, six pieces of 16 columns of its row: at d = 256 a warpgroup takes a block of 128
+    // rows (64 columns of [dG | dU], 32 of H), else the first one 96 columns of [dG | dU] and the second the
+    // other 32 and H's 64.  H's two halves are added.
+    float sum[96];
+#pragma unroll
+    for (int e = 0; e < 96; ++e) sum[e] = 0.f;
+    auto place = [&](int b, bool* pair) -> uint32_t {  // columns of piece b: [dG | dU] from 0, or H from kAcc2
+      const int gb = D == 256 ? b : wg * 6 + b, first = N2 / 16;
+      const int m = D == 256 ? wg : 0;
+      *pair = gb >= first;
+      return (gb < first ? gb * 16 : C::kAcc2 + (gb - first) * 16) + m * N2;
+    };
+    auto drain = [&]() {
+#pragma unroll
+      for (int b = 0; b < 6; ++b) {
+        bool pair;
+        const uint32_t col = tmem + lane_off + place(b, &pair);
+        uint32_t v[16];
+        ld16_issue(col, v);
+        ld_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[b * 16 + e] += __uint_as_float(v[e]);
+        if (pair) {
+          ld16_issue(col + HC, v);
+          ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[b * 16 + e] += __uint_as_float(v[e]);
+        }
+      }
+    };
+    for (int i = 0; i < count; ++i) {
+      if (!wait(gfull, i & 1)) break;
+      if (i >= 1) {
+        if (!wait(ofree, (i - 1) & 1)) break;
+        drain();
+      }
+#pragma unroll
+      for (int x = 0; x < HW; x += 8) {
+        float g[8], u[8], h[8];
+        tmem_ld8(hid + h0 + x, g);
+        tmem_ld8(hid + HC + h0 + x, u);
+        tmem_ld8(hid + N2 + h0 + x, h);
+        uint32_t hi[3][4], lo[3][4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float a0, a1, d0, d1;
+          gate_grad2<kAct>(g[e], g[e + 1], &a0, &a1, &d0, &d1);
+          const float v[3][2] = {{h[e] * u[e] * d0, h[e + 1] * u[e + 1] * d1},
+                                 {h[e] * a0, h[e + 1] * a1},
+                                 {a0 * u[e], a1 * u[e + 1]}};
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const uint32_t w = pack2_bf16(v[k][0], v[k][1]);
+            hi[k][e / 2] = w;
+            lo[k][e / 2] = pack2_bf16(v[k][0] - __uint_as_float(w << 16), v[k][1] - __uint_as_float(w & 0xffff0000u));
+          }
+        }
+        const int c = h0 + x;
+        put(Os, c, hi[0]);
+        put(Os, HC + c, hi[1]);
+        put(Os + C::kOps, c, lo[0]);
+        put(Os + C::kOps, HC + c, lo[1]);
+        put(Os + 2 * C::kOps, c, hi[2]);
+        put(Os + 2 * C::kOps, HC + c, lo[2]);
+      }
+      fence_async_smem();
+      fence_before_sync();
+      mbar_arrive(ofull);
+    }
+    // the sums of this share: part[split] = [dW_gate d x f | dW_up d x f | dW_down f x d]
+    if (one.ok && wait(ofree, (count - 1) & 1)) {
+      drain();
+      float* out = p.part + (int64_t)split * 3 * D * p.f;
+      const int64_t df = (int64_t)D * p.f;
+      const int m = D == 256 ? wg : 0, dr = m * 128 + row;
+#pragma unroll
+      for (int b = 0; b < 6; ++b) {
+        bool pair;
+        const int col = (int)place(b, &pair) - m * N2;
+        if (!pair) {
+          const int hcol = chunk * HC + col % HC;
+          if (dr < D) {
+            float* o = out + (col / HC) * df + (int64_t)dr * p.f + hcol;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+              if (hcol + e < p.f) st16(o + e, pack(sum + b * 16 + e, 0.f));
+          }
+        } else {
+          const int r = D == 64 ? row - 64 : dr;  // d = 64: the lower half is dY's
+          const int hcol = chunk * HC + col - (int)C::kAcc2;
+          if (r >= 0) {
+            float* o = out + 2 * df + (int64_t)hcol * D + r;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (hcol + e < p.f) o[(int64_t)e * D] = sum[b * 16 + e];
+          }
+        }
+      }
+    }
+  }
+  fence_before_sync();
+  __syncthreads();
+  if (warp == 2) tmem_dealloc(tmem, 512);
+}
+
+// out[((c * 2 + w) * hc + j) * d + k] = W_w[k][c * hc + j] (W_0 = W_gate, W_1 = W_up; zero from f on): the
+// weights of a chunk of hidden features as rows along d.  32 x 32 tiles through shared memory.
+__global__ void __launch_bounds__(256) ffn_pack_weights(const __nv_bfloat16* __restrict__ Wg,
+                                                        const __nv_bfloat16* __restrict__ Wu, int d, int f, int hc,
+                                                        __nv_bfloat16* __restrict__ out) {
+  pdl_begin();
+  __shared__ __nv_bfloat16 t[32][34];
+  const __nv_bfloat16* W = blockIdx.z ? Wu : Wg;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int h0 = blockIdx.x * 32, k0 = blockIdx.y * 32;
+#pragma unroll
+  for (int r = y; r < 32; r += 8) t[r][x] = h0 + x < f ? W[(int64_t)(k0 + r) * f + h0 + x] : __float2bfloat16(0.f);
+  __syncthreads();
+#pragma unroll
+  for (int r = y; r < 32; r += 8) {
+    const int h = h0 + r, c = h / hc, j = h % hc;
+    out[((int64_t)(c * 2 + blockIdx.z) * hc + j) * d + k0 + x] = t[x][r];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------
+template <int D, int kAct>
+hg_status dx_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, cudaStream_t s) {
+  using C = DxCfg<D>;
+  static bool done = false;
+  if (!done) {
+    HG_CUDA(cudaFuncSetAttribute(ffn_dx_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    done = true;
+  }
+  CUtensorMap tm_X, tm_dY, tm_G, tm_U, tm_W;
+  HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
+  HG_TRY(make_tmap_bf16(&tm_dY, dY, (uint64_t)n, D, kRows));
+  HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, C::PR));
+  HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, C::PR));
+  HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, C::HC));
+  DxP p{n, (int)ceil_div(w->f, C::HC), ceil_div(n, kRows), w->residual ? (const __nv_bfloat16*)dY : nullptr,
+        (__nv_bfloat16*)dX, device_status_ptr()};
+  return launch("ffn_dx_tc", ffn_dx_tc_kernel<D, kAct>, dim3((unsigned)std::min<int64_t>(p.tiles, kSms)),
+                dim3(kThreads), C::kSmem, s, tm_X, tm_dY, tm_G, tm_U, tm_W, p);
+}
+
+int hidden_chunk(int d) { return d == 256 ? WgCfg<256>::HC : WgCfg<128>::HC; }
+
+// Shares of the row tiles: the count that makes the longest SM's work shortest (whole waves of chunks x shares).
+int wg_splits(int64_t n, int d, int f) {
+  const int64_t tiles = ceil_div(n, kRows), chunks = ceil_div(f, hidden_chunk(d));
+  int64_t best = 1, best_cost = INT64_MAX;
+  for (int64_t sp = 1; sp <= std::min<int64_t>(tiles, kSms); ++sp) {
+    // a CTA's fixed cost (weights in, gradients out) is about four tiles' time
+    const int64_t cost = ceil_div(chunks * sp, kSms) * (ceil_div(tiles, sp) + 4);
+    if (cost < best_cost) {
+      best = sp;
+      best_cost = cost;
+    }
+  }
+  return (int)best;
+}
+
+struct WgLayout {
+  void* Wt;
+  float* part;
+};
+void carve_wg(void* scratch, const hg_ffn_params* w, int64_t n, WgLayout* L, size_t* bytes) {
+  Carve k(scratch);
+  const int hc = hidden_chunk(w->d);
+  L->Wt = k.take<__nv_bfloat16>((size_t)ceil_div(w->f, hc) * 2 * hc * w->d);
+  L->part = k.take<float>((size_t)wg_splits(std::max<int64_t>(n, 1), w->d, w->f) * 3 * w->d * w->f);
+  if (bytes) *bytes = k.used;
+}
+
+template <int D, int kAct>
+hg_status wg_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, const hg_ffn_grads* g,
+               const WgLayout& L, cudaStream_t s) {
+  using C = WgCfg<D>;
+  static bool done = false;
+  if (!done) {
+    HG_CUDA(cudaFuncSetAttribute(ffn_wgrad_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    done = true;
+  }
+  const int chunks = (int)ceil_div(w->f, C::HC), splits = wg_splits(n, D, w->f);
+  HG_TRY(launch("ffn_pack_weights", ffn_pack_weights, dim3(chunks * C::HC / 32, D / 32, 2), dim3(256), 0, s,
+                (const __nv_bfloat16*)w->W_gate, (const __nv_bfloat16*)w->W_up, D, w->f, C::HC, (__nv_bfloat16*)L.Wt));
+  CUtensorMap tm_X, tm_dY, tm_Wt, tm_W;
+  HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
+  HG_TRY(make_tmap_bf16(&tm_dY, dY, (uint64_t)n, D, kRows));
+  HG_TRY(make_tmap_bf16(&tm_Wt, L.Wt, (uint64_t)chunks * C::N2, D, C::N2));
+  HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, C::HC));
+  WgP p{n, ceil_div(n, kRows), w->f, splits, chunks, L.part, device_status_ptr()};
+  HG_TRY(launch("ffn_wgrad_tc", ffn_wgrad_tc_kernel<D, kAct>, dim3((unsigned)(chunks * splits)), dim3(kThreads),
+                C::kSmem, s, tm_X, tm_dY, tm_Wt, tm_W, p));
+  const int64_t df = (int64_t)D * w->f;
+  return reduce_partials3(L.part, 3 * df, splits, df, g->dW_gate, g->dW_up, g->dW_down, s);
+}
+
+template <int D, int kAct>
+hg_status bwd_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
+                void* scratch, cudaStream_t s) {
+  if (dX) HG_TRY((dx_t<D, kAct>(w, X, n, dY, dX, s)));
+  if (!g) return HG_OK;
+  WgLayout L;
+  carve_wg(scratch, w, n, &L, nullptr);
+  return wg_t<D, kAct>(w, X, n, dY, g, L, s);
+}
+
+template <int D>
+hg_status bwd_d(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
+                void* scratch, cudaStream_t s) {
+  if (w->act == HG_ACT_RELU) return bwd_t<D, HG_ACT_RELU>(w, X, n, dY, dX, g, scratch, s);
+  if (w->act == HG_ACT_GELU_TANH) return bwd_t<D, HG_ACT_GELU_TANH>(w, X, n, dY, dX, g, scratch, s);
+  if (w->act == HG_ACT_SILU) return bwd_t<D, HG_ACT_SILU>(w, X, n, dY, dX, g, scratch, s);
+  return bwd_t<D, HG_ACT_NONE>(w, X, n, dY, dX, g, scratch, s);
+}
+
+}  // namespace
+
+size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n) {
+  WgLayout L;
+  size_t bytes = 0;
+  carve_wg(nullptr, w, n, &L, &bytes);
+  return bytes;
+}
+
+hg_status ffn_bwd_tc(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
+                     void* scratch, cudaStream_t s) {
+  if (w->d == 64) return bwd_d<64>(w, X, n, dY, dX, g, scratch, s);
+  if (w->d == 128) return bwd_d<128>(w, X, n, dY, dX, g, scratch, s);
+  return bwd_d<256>(w, X, n, dY, dX, g, scratch, s);
+}
+
+}  // namespace hg

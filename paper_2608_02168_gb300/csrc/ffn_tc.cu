@@ -1,0 +1,372 @@
+// Gated feed-forward block on the tensor cores (bf16 storage, fp32 accumulation), forward.
+//
+//   [G | U] = X [W_gate | W_up],  H = act(G) * U (rounded to bf16: the operand of the next product),
+//   Y = H W_down (+ X)
+//
+// One persistent CTA an SM.  A group of two 128-row tiles (d <= 128; one at d = 256, whose Y fills half of the
+// tensor memory) stays in shared memory while the hidden features pass by in chunks of 64: the weights'
+// pieces arrive by TMA in a ring, in the stored layout (MN-major operands), [G | U] of a chunk goes to
+// one of two tensor-memory slots, a warpgroup turns it into H (one row a thread) in shared memory, and the
+// product with W_down adds into Y.  The hidden rows never leave the chip.  The slots take turns (the two
+// tiles, or even and odd chunks): one's gates are computed while the other's products run, so the tensor pipe
+// waits only for the slower of the two.  The gate's reciprocals are taken for two features at once, since the
+// special-function rate (e^x and 1/x of every hidden feature) is as scarce as the tensor rate at d = 128.
+// Bound by the tensor pipe (6 d f flops a row against 4 d bytes).
+#include <algorithm>
+
+#include "ffn_kernels.cuh"
+#include "ffn_tc.cuh"
+#include "layer_kernels.cuh"
+#include "tc_util.cuh"
+
+namespace hg {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kRows = 128;
+constexpr int kHc = 64;              // hidden features of a chunk
+constexpr int kBlk = kRows * 128;    // a 64-column block of a 128-row tile
+constexpr int kThreads = 384;        // warps 0..3: TMA, MMA issue, tensor memory, idle; two warpgroups for the gates
+constexpr int kSms = 152;
+
+template <int D>
+struct FCfg {
+  static constexpr int NB = D / 64;
+  static constexpr int NT = D == 256 ? 1 : 2;                // row tiles of a group
+  static constexpr int KP = D == 256 ? 2 : 1;                // pieces of [W_gate | W_up] (by rows)
+  static constexpr int PR = D / KP;                          // their rows
+  static constexpr int kPiece = PR * 128 * 2;                // bytes; W_down's piece is 64 D 2 <= kPiece
+  static constexpr int kDown = kHc * D * 2;
+  static constexpr int NS = D == 64 ? 6 : 4;                 // ring slots
+  static constexpr int kX = NT * NB * kBlk;
+  static constexpr int kH = kRows * 128;
+  static constexpr int kSmem = kX + NS * kPiece + 2 * kH + 512 + 1024;
+  static constexpr uint32_t kYCol = 0, kGuCol = 256;         // tensor memory: Y (tile x at x D), slots of 128
+};
+
+struct FwdP {
+  int64_t n;
+  int nch;
+  int64_t groups;
+  const __nv_bfloat16* res;  // X, or null without the residual
+  __nv_bfloat16* Y;
+  int* status;
+};
+
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+template <int D, int kAct>
+__global__ void __launch_bounds__(kThreads, 1)
+    ffn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_G,
+                      const __grid_constant__ CUtensorMap tm_U, const __grid_constant__ CUtensorMap tm_W, FwdP p) {
+  pdl_begin();
+  using C = FCfg<D>;
+  constexpr int NB = C::NB, NT = C::NT, NS = C::NS, KP = C::KP;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* Xs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* Ws = Xs + C::kX;
+  uint8_t* Hs = Ws + NS * C::kPiece;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Hs + 2 * C::kH);
+  uint64_t *wfull = bars, *wfree = bars + NS, *xfull = bars + 2 * NS, *xfree = xfull + 1, *gfull = xfull + 2,
+           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yfree = yfull + 2, *quit = yfree + 2;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&wfull[i], 1);
+      mbar_init(&wfree[i], 1);
+    }
+    mbar_init(xfull, 1);
+    mbar_init(xfree, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&gfull[i], 1);
+      mbar_init(&hfull[i], 128);
+      mbar_init(&hfree[i], 1);
+      mbar_init(&yfull[i], 1);
+      mbar_init(&yfree[i], NT == 2 ? 128 : 256);
+    }
+    mbar_init(quit, 1);
+    fence_mbar_init();
+  }
+  if (warp == 2) tmem_alloc(tslot, 512);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *tslot;
+  const int nch = p.nch;
+
+  if (warp == 0 && lane == 0) {
+    // ---------------------------------------------------------------- loads
+    bool ok = true;
+    uint32_t q = 0, xn = 0;  // pieces and row groups asked for
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      if (ok && !mbar_wait(b, parity)) {
+        ok = false;
+        record_device_error(p.status, kErrTimeout);
+      }
+      return ok;
+    };
+    auto slot = [&](uint32_t bytes) -> uint8_t* {
+      const uint32_t s = q % NS;
+      if (q >= NS && !wait(&wfree[s], (q / NS - 1) & 1)) return nullptr;
+      mbar_expect_tx(&wfull[s], bytes);
+      ++q;
+      return Ws + s * C::kPiece;
+    };
+    auto load_gu = [&](int c) {
+      for (int k = 0; ok && k < KP; ++k) {
+        uint8_t* dst = slot(C::kPiece);
+        if (!dst) return;
+        uint64_t* b = &wfull[(q - 1) % NS];
+        tma_load_2d(dst, &tm_G, c * kHc, k * C::PR, b);
+        tma_load_2d(dst + C::PR * 128, &tm_U, c * kHc, k * C::PR, b);
+      }
+    };
+    auto load_down = [&](int c) {
+      uint8_t* dst = ok ? slot(C::kDown) : nullptr;
+      if (!dst) return;
+      for (int b = 0; b < NB; ++b) tma_load_2d(dst + b * kHc * 128, &tm_W, b * 64, c * kHc, &wfull[(q - 1) % NS]);
+    };
+    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x) {
+      if (xn >= 1 && !wait(xfree, (xn - 1) & 1)) break;
+      mbar_expect_tx(xfull, C::kX);
+      for (int t = 0; t < NT; ++t)
+        for (int b = 0; b < NB; ++b)
+          tma_load_2d(Xs + (t * NB + b) * kBlk, &tm_X, b * 64, (int)((gr * NT + t) * kRows), xfull);
+      ++xn;
+      load_gu(0);
+      if (NT == 1 && nch > 1) load_gu(1);
+      for (int c = 0; ok && c < nch; ++c) {
+        load_down(c);
+        if (c + 3 - NT < nch) load_gu(c + 3 - NT);
+      }
+    }
+    if (!ok) {  // what was asked for lands before the CTA ends
+      if (xn) mbar_wait(xfull, (xn - 1) & 1);
+      drain_rounds(wfull, NS, q);
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---------------------------------------------------------------- products
+    bool ok = true;
+    uint32_t q = 0, gi = 0;
+    uint32_t hk[2] = {0, 0};  // chunks of each slot so far
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      if (ok && !mbar_wait(b, parity)) {
+        ok = false;
+        record_device_error(p.status, kErrTimeout);
+      }
+      if (ok) fence_after_sync();
+      return ok;
+    };
+    const uint32_t xs = smem_u32(Xs), ws = smem_u32(Ws), hs = smem_u32(Hs);
+    constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_y = idesc_bf16(128, D, false, true);
+    // pieces q0 .. q0 + KP - 1 times tile t into slot s
+    auto gu = [&](uint32_t q0, int t, int s) {
+#pragma unroll
+      for (int k = 0; k < KP; ++k) {
+        if (t == 0 && !wait(&wfull[(q0 + k) % NS], ((q0 + k) / NS) & 1)) return;
+        const uint32_t w = ws + (q0 + k) % NS * C::kPiece;
+#pragma unroll
+        for (int j = 0; j < C::PR / 16; ++j) {
+          const int jj = k * (C::PR / 16) + j;
+          mma_bf16(tmem + C::kGuCol + s * 128,
+                   desc_sw128(xs + (t * NB + (jj >> 2)) * kBlk + (jj & 3) * 32, 16, 1024),
+                   desc_sw128(w + j * 2048, C::PR * 128, 1024), id_gu, jj > 0 ? 1u : 0u);
+        }
+      }
+      mma_commit(&gfull[s]);
+    };
+    auto down = [&](uint32_t qd, int c, int s) {
+      const int t = NT == 2 ? s : 0;
+      if (!wait(&hfull[s], hk[s] & 1)) return;
+      if (c == 0 && gi >= 1 && !wait(&yfree[t], (gi - 1) & 1)) return;
+      ++hk[s];
+      const uint32_t w = ws + qd % NS * C::kPiece;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        mma_bf16(tmem + C::kYCol + t * D, desc_sw128(hs + s * C::kH + j * 32, 16, 1024),
+                 desc_sw128(w + j * 2048, kHc * 128, 1024), id_y, (c > 0 || j > 0) ? 1u : 0u);
+      mma_commit(&hfree[s]);
+      if (c == nch - 1) mma_commit(&yfull[t]);
+    };
+    auto release = [&](uint32_t q0, int count) {
+      for (int i = 0; i < count; ++i) mma_commit(&wfree[(q0 + i) % NS]);
+    };
+    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x, ++gi) {
+      if (!wait(xfull, gi & 1)) break;
+      if (NT == 2) {
+        for (int t = 0; ok && t < 2; ++t) gu(q, t, t);
+        if (!ok) break;
+        release(q, KP);
+        q += KP;
+        if (nch == 1) mma_commit(xfree);
+        for (int c = 0; ok && c < nch; ++c) {
+          const bool more = c + 1 < nch;
+          if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
+          for (int s = 0; ok && s < 2; ++s) {
+            down(q, c, s);
+            if (ok && more) gu(q + 1, s, s);
+          }
+          if (!ok) break;
+          release(q, 1 + (more ? KP : 0));
+          q += 1 + (more ? KP : 0);
+          if (c + 2 == nch) mma_commit(xfree);
+        }
+      } else {
+        for (int c = 0; ok && c < 2 && c < nch; ++c) {
+          gu(q, 0, c);
+          if (!ok) break;
+          release(q, KP);
+          q += KP;
+        }
+        if (ok && nch <= 2) mma_commit(xfree);
+        for (int c = 0; ok && c < nch; ++c) {
+          if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
+          down(q, c, c & 1);
+          if (!ok) break;
+          release(q, 1);
+          ++q;
+          if (c + 2 < nch) {
+            gu(q, 0, c & 1);
+            if (!ok) break;
+            release(q, KP);
+            q += KP;
+            if (c + 3 == nch) mma_commit(xfree);
+          }
+        }
+      }
+    }
+    if (!ok) drain_mma(quit, 0);
+  } else if (warp >= 4) {
+    // ---------------------------------------------------------------- gates and rows out
+    const int s = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t gcol = tmem + C::kGuCol + s * 128 + lane_off;
+    uint8_t* H = Hs + s * C::kH;
+    bool ok = true;
+    uint32_t k = 0, gi = 0;
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      if (ok && !mbar_wait(b, parity)) {
+        ok = false;
+        record_device_error(p.status, kErrTimeout);
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) fence_after_sync();
+      return ok;
+    };
+    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x, ++gi) {
+      for (int c = NT == 2 ? 0 : s; ok && c < nch; c += 3 - NT, ++k) {
+        if (!wait(&gfull[s], k & 1)) break;
+        uint32_t h[32];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t g[32], u[32];
+          tmem_ld32_issue(gcol + half * 32, g);
+          tmem_ld32_issue(gcol + 64 + half * 32, u);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            float a0, a1;
+            gate2<kAct>(__uint_as_float(g[e]), __uint_as_float(g[e + 1]), &a0, &a1);
+            h[half * 16 + e / 2] = pack2_bf16(a0 * __uint_as_float(u[e]), a1 * __uint_as_float(u[e + 1]));
+          }
+        }
+        if (k >= 1 && !wait(&hfree[s], (k - 1) & 1)) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          st16(H + sw128_offset(row, e * 16), make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]));
+        fence_async_smem();
+        fence_before_sync();
+        mbar_arrive(&hfull[s]);
+      }
+      if (!ok) break;
+      const int t = NT == 2 ? s : 0;
+      constexpr int CW = NT == 2 ? D : D / 2;  // columns of a warpgroup
+      const int col0 = NT == 2 ? 0 : s * CW;
+      const int64_t r = (gr * NT + t) * kRows + row;
+      const bool live = r < p.n;
+      if (!wait(&yfull[t], gi & 1)) break;
+#pragma unroll
+      for (int c = 0; c < CW; c += 32) {
+        uint32_t y[32];
+        tmem_ld32_issue(tmem + C::kYCol + t * D + lane_off + col0 + c, y);
+        uint4 x[4];
+        if (p.res && live) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = ldg16(p.res + r * D + col0 + c + e * 8);
+        }
+        tmem_ld_wait();
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float v[8];
+            if (p.res) {
+              unpack(x[e], v, __nv_bfloat16());
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(y[e * 8 + i]);
+            st16(p.Y + r * D + col0 + c + e * 8, pack(v, __nv_bfloat16()));
+          }
+        }
+      }
+      fence_before_sync();
+      mbar_arrive(&yfree[t]);
+    }
+  }
+  fence_before_sync();
+  __syncthreads();
+  if (warp == 2) tmem_dealloc(tmem, 512);
+}
+
+template <int D, int kAct>
+hg_status fwd_t(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
+  using C = FCfg<D>;
+  static bool done = false;
+  if (!done) {
+    HG_CUDA(cudaFuncSetAttribute(ffn_fwd_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    done = true;
+  }
+  CUtensorMap tm_X, tm_G, tm_U, tm_W;
+  HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
+  HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, C::PR));
+  HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, C::PR));
+  HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, kHc));
+  FwdP p{n, (int)ceil_div(w->f, kHc), ceil_div(n, (int64_t)kRows * C::NT),
+         w->residual ? (const __nv_bfloat16*)X : nullptr, (__nv_bfloat16*)Y, device_status_ptr()};
+  const int grid = (int)std::min<int64_t>(p.groups, kSms);
+  return launch("ffn_fwd_tc", ffn_fwd_tc_kernel<D, kAct>, dim3(grid), dim3(kThreads), C::kSmem, s, tm_X, tm_G, tm_U,
+                tm_W, p);
+}
+
+template <int D>
+hg_status fwd_d(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
+  if (w->act == HG_ACT_RELU) return fwd_t<D, HG_ACT_RELU>(w, X, n, Y, s);
+  if (w->act == HG_ACT_GELU_TANH) return fwd_t<D, HG_ACT_GELU_TANH>(w, X, n, Y, s);
+  if (w->act == HG_ACT_SILU) return fwd_t<D, HG_ACT_SILU>(w, X, n, Y, s);
+  return fwd_t<D, HG_ACT_NONE>(w, X, n, Y, s);
+}
+
+}  // namespace
+
+hg_status ffn_fwd_tc(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
+  if (w->d == 64) return fwd_d<64>(w, X, n, Y, s);
+  if (w->d == 128) return fwd_d<128>(w, X, n, Y, s);
+  return fwd_d<256>(w, X, n, Y, s);
+}
+
+}  // namespace hg

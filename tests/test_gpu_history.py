@@ -194,7 +194,7 @@ def past(x, lens):
 
 
 # Rows: bf16 rounds the weights of a chunk (the products q k of its positions times their decay) and the state that
-# enters it once each, the terms of a state at most 2^-16: r = 2 u.  States are fp32 sums: the terms' split 2^-16.
+# enters it once each, the terms of a state at most 2^-16: r = 2 u.  States are fp32 sums of terms split to 2^-16.
 # e: sums of at most T d_h terms in chunks (T + 2 d_h), decays exp(x) with |x| <= 11 + rounding 2^-22, 4 of them.
 def decay_rel(dt, T, dh, out):
     e = (T + 2 * dh + 80) * F32
