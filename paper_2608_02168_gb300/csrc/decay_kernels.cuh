@@ -42,8 +42,9 @@ __device__ __forceinline__ int64_t scan_len(const ScanArgs& a, int64_t i) {
 
 // A state is kept in a frame: S = gamma^(tau - b) F with a base time b, so that no position multiplies it;
 // additions are scaled by gamma^(b - tau), at most e^kFrame.  Beyond that the frame moves on.
-// A state multiplied at each of thousands of positions would gather the rounding of gamma itself.
-constexpr float kFrame = 11.f;
+// A state multiplied at each of thousands of positions would gather the rounding of gamma itself; a wider frame
+// would magnify the rounding of the exponents.
+constexpr float kFrame = 5.f;
 
 // bf16 scan on the tensor cores (decay_mma.cu); local: the segments' own states into a.seg, no rows.
 hg_status scan_mma(const ScanArgs& a, int d_h, bool local, cudaStream_t s);

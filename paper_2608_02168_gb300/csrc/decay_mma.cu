@@ -42,7 +42,7 @@ struct Cfg {
   static constexpr int kQ = kC * kRow, kV = kC * kVRow;
   static constexpr int kStage = 2 * kQ + kV;
   static constexpr int kSmem = W * ST * kStage;
-  static constexpr int kBlocks = DH == 16 ? 6 : DH == 32 ? 4 : DH == 64 ? 3 : 2;  // resident CTAs of an SM
+  static constexpr int kBlocks = DH == 16 ? 5 : DH == 32 ? 4 : DH == 64 ? 3 : 2;  // resident CTAs of an SM
 };
 
 // Byte offset of 16-byte piece c of row r, N pieces a row.
@@ -75,24 +75,23 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// One warp's piece of work and its place in it.
+// One warp's piece of work: positions [t0, t1) of the scan of a head (segment segi), value features slice * DS on.
 struct Item {
-  int64_t id;       // past the last: none
-  int64_t seq, len;
+  uint32_t id;  // at or past the number of items: none
+  uint32_t seq;
   int head, slice, segi;
-  int64_t t0, t1;   // positions of the scan: [t0, t1) in use
+  int64_t len, t0, t1;
 };
 
-template <int DH, bool kLocal>
-__device__ __forceinline__ void locate(const ScanArgs& a, int64_t items, Item& it) {
+template <int DH>
+__device__ __forceinline__ void locate(const ScanArgs& a, uint32_t items, uint32_t segs, Item& it) {
   if (it.id >= items) {
     it.t0 = it.t1 = 0;
     return;
   }
-  constexpr int SL = Cfg<DH>::SL;
-  const uint32_t segs = kLocal ? a.nseg - 1 : a.nseg;
+  constexpr uint32_t SL = Cfg<DH>::SL;
   it.slice = (int)(it.id % SL);
-  uint64_t x = (uint64_t)it.id / SL;
+  uint32_t x = it.id / SL;
   it.head = (int)(x % (uint32_t)a.heads);
   x /= (uint32_t)a.heads;
   it.segi = 0;
@@ -100,37 +99,41 @@ __device__ __forceinline__ void locate(const ScanArgs& a, int64_t items, Item& i
     it.segi = (int)(x % segs);
     x /= segs;
   }
-  it.seq = (int64_t)x;
-  it.len = scan_len(a, it.seq);
+  it.seq = x;
+  it.len = scan_len(a, x);
   it.t0 = it.segi * a.seg_len;
   it.t1 = max(it.t0, min(it.t0 + a.seg_len, it.len));
 }
 
-template <int DH, bool kLocal>
-__device__ __forceinline__ void load_chunk(const ScanArgs& a, const Item& it, int64_t c0, uint8_t* stage, int lane) {
-  using C = Cfg<DH>;
-  constexpr int N = DH / 8, NV = C::DS / 8;
-  const int m = (int)min((int64_t)kC, it.t1 - c0);
-  const __nv_bfloat16* q = (const __nv_bfloat16*)a.q.p + it.seq * a.q.sn + it.head * DH;
-  const __nv_bfloat16* k = (const __nv_bfloat16*)a.k.p + it.seq * a.k.sn + it.head * DH;
-  const __nv_bfloat16* v = (const __nv_bfloat16*)a.v.p + it.seq * a.v.sn + it.head * DH + it.slice * C::DS;
+// Where a lane's 16-byte pieces of an array's rows start and how far apart the rows of the scan lie, in bytes
+// (negative in reverse).  P pieces a row: the lane takes piece lane % P of rows lane / P + i (32 / P).
+template <int P>
+__device__ __forceinline__ const uint8_t* lane_rows(const ScanRows& r, const ScanArgs& a, const Item& it, int64_t t,
+                                                    int col, int lane) {
+  const int64_t row = a.reverse ? it.len - 1 - t - lane / P : t + lane / P;
+  return static_cast<const uint8_t*>(r.p) + 2 * ((int64_t)it.seq * r.sn + row * r.st + col + lane % P * 8);
+}
+__device__ __forceinline__ int64_t row_step(const ScanRows& r, const ScanArgs& a) {
+  return a.reverse ? -2 * r.st : 2 * r.st;
+}
+
+// The lane's pieces of kC rows, m of them in use (the others become zero), to dst.
+template <int P>
+__device__ __forceinline__ void load_rows(uint8_t* dst, const uint8_t* src, int64_t step, int m, int lane) {
+  constexpr int RS = 32 / P;
 #pragma unroll
-  for (int x = lane; x < kC * N; x += 32) {
-    const int r = x / N, c = x % N;
-    const bool ok = r < m;
-    const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
-    const int64_t row = ok ? t : (a.reverse ? it.len - 1 - c0 : c0);
-    cp_async16(stage + C::kQ + piece<N>(r, c), k + row * a.k.st + c * 8, ok);
-    if (!kLocal) cp_async16(stage + piece<N>(r, c), q + row * a.q.st + c * 8, ok);
+  for (int i = 0; i < kC / RS; ++i) {
+    const int r = lane / P + i * RS;
+    // a row that is not in use is not read; its address is that of the first row
+    const int64_t off = (r < m ? i * RS : -(lane / P)) * step;
+    cp_async16(dst + piece<P>(r, lane % P), src + off, r < m);
   }
-#pragma unroll
-  for (int x = lane; x < kC * NV; x += 32) {
-    const int r = x / NV, c = x % NV;
-    const bool ok = r < m;
-    const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
-    const int64_t row = ok ? t : (a.reverse ? it.len - 1 - c0 : c0);
-    cp_async16(stage + 2 * C::kQ + piece<NV>(r, c), v + row * a.v.st + c * 8, ok);
-  }
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // x (a pair of bf16) times (f0, f1) as a sum of three bf16 pairs
@@ -147,29 +150,47 @@ template <int DH, bool kLocal>
 __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_kernel(const __grid_constant__ ScanArgs a) {
   pdl_begin();
   using C = Cfg<DH>;
-  constexpr int DS = C::DS, MT = DS / 16, NT = DH / 8, KS = DH / 16, NV = DS / 8, ST = C::ST;
+  constexpr int DS = C::DS, MT = DS / 16, NT = DH / 8, KS = DH / 16, NV = DS / 8, N = DH / 8, ST = C::ST;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   uint8_t* ring = smem + warp * (ST * C::kStage);
-  const int64_t items = a.n * (kLocal ? a.nseg - 1 : a.nseg) * a.heads * C::SL;
-  const int64_t stride = (int64_t)gridDim.x * C::W;
+  const uint32_t segs = kLocal ? a.nseg - 1 : a.nseg;
+  const uint32_t items = (uint32_t)a.n * segs * a.heads * C::SL;
+  const uint32_t stride = gridDim.x * C::W;
+  const int64_t qs = row_step(a.q, a), ks = row_step(a.k, a), vs = row_step(a.v, a), os = row_step(a.o, a);
   // lane addresses inside a tile of 16 x 16 for ldmatrix: rows by lane & 15 / pieces by lane >> 4, and the other order
   const int r16 = lane & 15, c16 = lane >> 4;
   const int r8 = (lane & 7) + ((lane >> 4) << 3), c8 = (lane >> 3) & 1;
 
-  Item it, nx;
-  it.id = (int64_t)blockIdx.x * C::W + warp;
-  locate<DH, kLocal>(a, items, it);
+  Item it{}, nx{};
+  it.id = blockIdx.x * C::W + warp;
+  locate<DH>(a, items, segs, it);
+  // the loads run ahead: position nc of item nx is the next chunk to ask for
+  const uint8_t *qp = nullptr, *kp = nullptr, *vp = nullptr;
+  int64_t nc = 0;
+  auto begin = [&]() {
+    nc = nx.t0;
+    if (nx.id >= items || nx.t0 >= nx.t1) return;
+    if (!kLocal) qp = lane_rows<N>(a.q, a, nx, nc, nx.head * DH, lane);
+    kp = lane_rows<N>(a.k, a, nx, nc, nx.head * DH, lane);
+    vp = lane_rows<NV>(a.v, a, nx, nc, nx.head * DH + nx.slice * DS, lane);
+  };
   nx = it;
-  int64_t nc = nx.t0;  // the next chunk to load: position nc of item nx
+  begin();
   auto advance = [&](uint8_t* stage) {
     while (nx.id < items && nc >= nx.t1) {
       nx.id += stride;
-      locate<DH, kLocal>(a, items, nx);
-      nc = nx.t0;
+      locate<DH>(a, items, segs, nx);
+      begin();
     }
     if (nx.id < items) {
-      load_chunk<DH, kLocal>(a, nx, nc, stage, lane);
+      const int m = (int)min((int64_t)kC, nx.t1 - nc);
+      if (!kLocal) load_rows<N>(stage, qp, qs, m, lane);
+      load_rows<N>(stage + C::kQ, kp, ks, m, lane);
+      load_rows<NV>(stage + 2 * C::kQ, vp, vs, m, lane);
+      qp += kC * qs;
+      kp += kC * ks;
+      vp += kC * vs;
       nc += kC;
     }
     cp_async_commit();
@@ -180,16 +201,10 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
     advance(ring + put * C::kStage);
     put = put + 1 == ST ? 0 : put + 1;
   }
-  for (; it.id < items; it.id += stride, locate<DH, kLocal>(a, items, it)) {
-    const float ld = clamp_ld(a.ld[it.head]);
-    const int64_t sh = it.seq * a.heads + it.head;
+  for (; it.id < items; it.id += stride, locate<DH>(a, items, segs, it)) {
+    const float ld = clamp_ld(a.ld[it.head]), ld2 = ld * 1.4426950408889634f;
+    const int64_t sh = (int64_t)it.seq * a.heads + it.head;
     float F[MT][NT][4];
-#pragma unroll
-    for (int x = 0; x < MT; ++x)
-#pragma unroll
-      for (int y = 0; y < NT; ++y)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) F[x][y][e] = 0.f;
     // element e of F[x][y]: value feature 16 x + g + 8 (e / 2) of the slice, key feature 8 y + 2 t4 + e % 2
     const int v0 = it.slice * DS + g, k0 = 2 * t4;
     bool some = false;  // the state is not zero
@@ -206,24 +221,32 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
             const int vi = v0 + 16 * x + 8 * (e >> 1), ki = k0 + 8 * y + (e & 1);
             F[x][y][e] = tr ? src[vi * DH + ki] : src[ki * DH + vi];
           }
+    } else {
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) F[x][y][e] = 0.f;
     }
     // weights gamma^(r - j) of the chunk's products: rows g, g + 8, columns 2 t4, 2 t4 + 1 (+ 8)
     float w[4];
-    bool keep[2];  // column j is not past row g
-    const float cc = a.c_in * a.c_out;
+    const bool keep0 = g >= 2 * t4, keep1 = g >= 2 * t4 + 1;  // the column is not past row g
     if (!kLocal) {
+      const float cc = a.c_in * a.c_out;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int j = 2 * t4 + e, gap = g - j;
-        keep[e] = gap >= 0;
-        w[e] = keep[e] ? expf(ld * (float)gap) * cc : 0.f;  // row g, column j; row g + 8, column j + 8
-        w[2 + e] = expf(ld * (float)(gap + 8)) * cc;        // row g + 8, column j
+        const float gap = (float)(g - 2 * t4 - e);
+        w[e] = (e ? keep1 : keep0) ? ex2(ld2 * gap) * cc : 0.f;  // row g, column j; row g + 8, column j + 8
+        w[2 + e] = ex2(ld2 * (gap + 8.f)) * cc;                  // row g + 8, column j
       }
     }
     int base = 0;  // positions from t0
-    const bool leave = kLocal || (a.last && it.segi == (it.len > 0 ? (it.len - 1) / a.seg_len : 0));
-    __nv_bfloat16* out = (__nv_bfloat16*)const_cast<void*>(a.o.p) + it.seq * a.o.sn + it.head * DH + it.slice * DS;
-    for (int64_t c0 = it.t0; c0 < it.t1; c0 += kC) {
+    const bool leave = kLocal || (a.last && it.segi == (it.len > 0 ? (int)((it.len - 1) / a.seg_len) : 0));
+    uint8_t* op = nullptr;
+    if (!kLocal) op = const_cast<uint8_t*>(lane_rows<NV>(a.o, a, it, it.t0, it.head * DH + it.slice * DS, lane));
+    const int count = (int)(it.t1 - it.t0);
+    for (int c0 = 0; c0 < count; c0 += kC) {
       cp_async_wait<ST - 2>();
       __syncwarp();
       advance(ring + put * C::kStage);
@@ -231,8 +254,8 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
       uint8_t* stage = ring + get * C::kStage;
       get = get + 1 == ST ? 0 : get + 1;
       const uint32_t sq = smem_u32(stage), sk = sq + C::kQ, sv = sk + C::kQ;
-      const int m = (int)min((int64_t)kC, it.t1 - c0);
-      const int tau0 = (int)(c0 - it.t0) + a.shift;
+      const int m = min(kC, count - c0);
+      const int tau0 = c0 + a.shift;
       uint32_t vt[MT][4];  // v, positions by pairs: [0], [2] positions 0..7 / 8..15 of features 0..7; [1], [3] of 8..15
 #pragma unroll
       for (int x = 0; x < MT; ++x) {
@@ -252,8 +275,8 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           uint32_t qa[4], kb[4];
-          ldsm4(sq + piece<DH / 8>(r16, 2 * s + c16), qa);
-          ldsm4(sk + piece<DH / 8>(r8, 2 * s + c8), kb);
+          ldsm4(sq + piece<N>(r16, 2 * s + c16), qa);
+          ldsm4(sk + piece<N>(r8, 2 * s + c8), kb);
           mma(p0, qa[0], qa[1], qa[2], qa[3], kb[0], kb[1]);
           mma(p1, qa[0], qa[1], qa[2], qa[3], kb[2], kb[3]);
           if (some) {
@@ -267,8 +290,8 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
           }
         }
         if (some) {
-          const float f0 = a.c_out * expf(ld * (float)(tau0 + g - base));
-          const float f1 = a.c_out * expf(ld * (float)(tau0 + g + 8 - base));
+          const float x = (float)(tau0 + g - base);
+          const float f0 = a.c_out * ex2(ld2 * x), f1 = a.c_out * ex2(ld2 * (x + 8.f));
 #pragma unroll
           for (int y = 0; y < NV; ++y) {
             o[y][0] *= f0;
@@ -277,9 +300,9 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
             o[y][3] *= f1;
           }
         }
-        const uint32_t a0 = pack2_bf16(keep[0] ? p0[0] * w[0] : 0.f, keep[1] ? p0[1] * w[1] : 0.f);
+        const uint32_t a0 = pack2_bf16(keep0 ? p0[0] * w[0] : 0.f, keep1 ? p0[1] * w[1] : 0.f);
         const uint32_t a1 = pack2_bf16(p0[2] * w[2], p0[3] * w[3]);
-        const uint32_t a3 = pack2_bf16(keep[0] ? p1[2] * w[0] : 0.f, keep[1] ? p1[3] * w[1] : 0.f);
+        const uint32_t a3 = pack2_bf16(keep0 ? p1[2] * w[0] : 0.f, keep1 ? p1[3] * w[1] : 0.f);
 #pragma unroll
         for (int y = 0; y < NV; ++y) mma(o[y], a0, a1, 0u, a3, vt[y >> 1][y & 1], vt[y >> 1][2 + (y & 1)]);
         // rows out through the place of q, 16 bytes a lane
@@ -291,41 +314,42 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
         }
         __syncwarp();
 #pragma unroll
-        for (int x = lane; x < kC * NV; x += 32) {
-          const int r = x / NV, c = x % NV;
-          if (r < m) {
-            const int64_t t = a.reverse ? it.len - 1 - (c0 + r) : c0 + r;
-            st16(out + t * a.o.st + c * 8, ld16(stage + piece<NV>(r, c)));
-          }
+        for (int i = 0; i < kC * NV / 32; ++i) {
+          const int r = lane / NV + i * (32 / NV);
+          if (r < m) st16(op + i * (32 / NV) * os, ld16(stage + piece<NV>(r, lane % NV)));
         }
+        op += kC * os;
       }
-      if (leave || c0 + kC < it.t1) {
+      if (leave || c0 + kC < count) {
         const int target = tau0 + m - 1;
         if ((float)(base - target) * ld > kFrame) {
-          const float f = expf(ld * (float)(target - base));
+          if (some) {
+            const float f = ex2(ld2 * (float)(target - base));
 #pragma unroll
-          for (int x = 0; x < MT; ++x)
+            for (int x = 0; x < MT; ++x)
 #pragma unroll
-            for (int y = 0; y < NT; ++y)
+              for (int y = 0; y < NT; ++y)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) F[x][y][e] *= f;
+                for (int e = 0; e < 4; ++e) F[x][y][e] *= f;
+          }
           base = target;
         }
         float f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 2 * t4 + (e & 1) + 8 * (e >> 1);
-          f[e] = r < m ? a.c_in * expf(ld * (float)(base - tau0 - r)) : 0.f;
+          f[e] = r < m ? a.c_in * ex2(ld2 * (float)(base - tau0 - r)) : 0.f;
         }
         uint32_t hi[MT][4], mid[MT][4], lo[MT][4];
 #pragma unroll
         for (int x = 0; x < MT; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
+          for (int e = 0; e < 4; ++e)
+            scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
 #pragma unroll
         for (int y = 0; y < NT; y += 2) {
           uint32_t kb[4];
-          ldsm4t(sk + piece<DH / 8>(r16, y + c16), kb);
+          ldsm4t(sk + piece<N>(r16, y + c16), kb);
 #pragma unroll
           for (int x = 0; x < MT; ++x) {
             mma(F[x][y], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[0], kb[1]);
@@ -343,12 +367,14 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
     }
     if (!kLocal) {
       const int64_t tend = min(it.t0 + a.seg_len, a.T), first = max(it.t0, it.len);
-      const int64_t pieces = max((tend - first) * NV, (int64_t)0);
-      for (int64_t x = lane; x < pieces; x += 32)
-        st16(out + (first + x / NV) * a.o.st + x % NV * 8, make_uint4(0u, 0u, 0u, 0u));
+      uint8_t* zp = static_cast<uint8_t*>(const_cast<void*>(a.o.p)) +
+                    2 * ((int64_t)it.seq * a.o.sn + (first + lane / NV) * a.o.st + it.head * DH + it.slice * DS +
+                         lane % NV * 8);
+      for (int64_t t = first + lane / NV; t < tend; t += 32 / NV, zp += (32 / NV) * 2 * a.o.st)
+        st16(zp, make_uint4(0u, 0u, 0u, 0u));
     }
     if (leave) {
-      const float f = expf(ld * (float)((int)(it.t1 - it.t0) - base));
+      const float f = ex2(ld2 * (float)(count - base));
       float* dst = kLocal ? a.seg + (sh * a.nseg + it.segi) * (int64_t)(DH * DH) : a.last + sh * (DH * DH);
 #pragma unroll
       for (int x = 0; x < MT; ++x)

@@ -36,18 +36,9 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kBlk = kRows * 128;  // a 64-column block of a 128-row tile
-constexpr int kThreads = 384;      // warps 0..3: TMA, MMA issue, tensor memory, idle; two warpgroups for the gates
+constexpr int kThreads = 640;      // warps 0..3: TMA, MMA issue, tensor memory, idle; four warpgroups for the gates
 constexpr int kSms = 152;
 
-__device__ __forceinline__ void ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
-      "[%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // eight 32-bit columns of this thread's lane
 __device__ __forceinline__ void st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
@@ -146,10 +137,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(xfree, 1);
     mbar_init(&gfull[0], 1);
     mbar_init(&gfull[1], 1);
-    mbar_init(ofull, SLOTS == 2 ? 128 : 256);
+    mbar_init(ofull, SLOTS == 2 ? 256 : 512);
     mbar_init(ofree, 1);
     mbar_init(yfull, 1);
-    mbar_init(yfree, 256);
+    mbar_init(yfree, 512);
     mbar_init(quit, 1);
     fence_mbar_init();
   }
@@ -250,10 +241,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-    const int s = SLOTS == 2 ? wg : 0;
+    const int s = SLOTS == 2 ? wg >> 1 : 0;
     const uint32_t t0 = tmem + C::kSlot + s * C::kSlotCols + lane_off;
-    constexpr int HW = SLOTS == 2 ? HC : HC / 2;  // hidden features of a warpgroup
-    const int h0 = SLOTS == 2 ? 0 : wg * HW;
+    constexpr int HW = HC * SLOTS / 4;  // hidden features of a warpgroup
+    const int h0 = (SLOTS == 2 ? wg & 1 : wg) * HW;
     Waiter one{p.status};
     auto wait = [&](uint64_t* b, uint32_t parity) {
       one(b, parity);
@@ -294,8 +285,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else {
 #pragma unroll
           for (int e = 0; e < HW / 8; ++e) {
-            st16(Os + sw128_offset(row, e * 16), make_uint4(dg[4 * e], dg[4 * e + 1], dg[4 * e + 2], dg[4 * e + 3]));
-            st16(Os + kBlk + sw128_offset(row, e * 16),
+            st16(Os + sw128_offset(row, h0 * 2 + e * 16), make_uint4(dg[4 * e], dg[4 * e + 1], dg[4 * e + 2], dg[4 * e + 3]));
+            st16(Os + kBlk + sw128_offset(row, h0 * 2 + e * 16),
                  make_uint4(du[4 * e], du[4 * e + 1], du[4 * e + 2], du[4 * e + 3]));
           }
           fence_async_smem();
@@ -304,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(ofull);
       }
       if (!one.ok) break;
-      constexpr int CW = D / 2;
+      constexpr int CW = D / 4;
       const int64_t r = tile * kRows + row;
       const bool live = r < p.n;
       if (!wait(yfull, ti & 1)) break;
@@ -393,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&xfree[i], 1);
     }
     mbar_init(gfull, 1);
-    mbar_init(ofull, 256);
+    mbar_init(ofull, 512);
     mbar_init(ofree, 1);
     mbar_init(quit, 1);
     fence_mbar_init();
@@ -473,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-    constexpr int HW = HC / 2;  // hidden features of a warpgroup
+    constexpr int HW = HC / 4;  // hidden features of a warpgroup
     const int h0 = wg * HW;
     const uint32_t hid = tmem + C::kHid + lane_off;
     Waiter one{p.status};
@@ -486,23 +477,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto put = [&](uint8_t* o, int c, const uint32_t* v) {
       st16(o + (c >> 6) * kBlk + sw128_offset(row, (c & 63) * 2), make_uint4(v[0], v[1], v[2], v[3]));
     };
-    // This thread's 96 sums, six pieces of 16 columns of its row: at d = 256 a warpgroup takes a block of 128
-    // rows (64 columns of [dG | dU], 32 of H), else the first one 96 columns of [dG | dU] and the second the
-    // other 32 and H's 64.  H's two halves are added.
-    float sum[96];
+    // This thread's 48 sums, three pieces of 16 columns of its row.  The twelve pieces of a row (at d = 256: six
+    // of each block of 128 rows) are first those of [dG | dU], then H's, whose two halves are added.
+    float sum[48];
 #pragma unroll
-    for (int e = 0; e < 96; ++e) sum[e] = 0.f;
-    auto place = [&](int b, bool* pair) -> uint32_t {  // columns of piece b: [dG | dU] from 0, or H from kAcc2
-      const int gb = D == 256 ? b : wg * 6 + b, first = N2 / 16;
-      const int m = D == 256 ? wg : 0;
+    for (int e = 0; e < 48; ++e) sum[e] = 0.f;
+    const int m = MB == 2 ? wg >> 1 : 0;
+    auto place = [&](int b, bool* pair) -> uint32_t {  // columns of piece b, from the block's first
+      const int gb = (MB == 2 ? wg & 1 : wg) * 3 + b, first = N2 / 16;
       *pair = gb >= first;
-      return (gb < first ? gb * 16 : C::kAcc2 + (gb - first) * 16) + m * N2;
+      return gb < first ? gb * 16 : C::kAcc2 + (gb - first) * 16;
     };
     auto drain = [&]() {
 #pragma unroll
-      for (int b = 0; b < 6; ++b) {
+      for (int b = 0; b < 3; ++b) {
         bool pair;
-        const uint32_t col = tmem + lane_off + place(b, &pair);
+        const uint32_t col = tmem + lane_off + m * N2 + place(b, &pair);
         uint32_t v[16];
         ld16_issue(col, v);
         ld_wait();
@@ -560,11 +550,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain();
       float* out = p.part + (int64_t)split * 3 * D * p.f;
       const int64_t df = (int64_t)D * p.f;
-      const int m = D == 256 ? wg : 0, dr = m * 128 + row;
+      const int dr = m * 128 + row;
 #pragma unroll
-      for (int b = 0; b < 6; ++b) {
+      for (int b = 0; b < 3; ++b) {
         bool pair;
-        const int col = (int)place(b, &pair) - m * N2;
+        const int col = (int)place(b, &pair);
         if (!pair) {
           const int hcol = chunk * HC + col % HC;
           if (dr < D) {
@@ -609,6 +599,39 @@ __global__ void __launch_bounds__(256) ffn_pack_weights(const __nv_bfloat16* __r
     const int h = h0 + r, c = h / hc, j = h % hc;
     out[((int64_t)(c * 2 + blockIdx.z) * hc + j) * d + k0 + x] = t[x][r];
   }
+}
+
+// out = the shares' sums in order: 32 float4 columns x 8 runs of shares a block, then the runs in order.
+__global__ void __launch_bounds__(256) ffn_sum_shares(const float* __restrict__ part, int splits, int64_t df,
+                                                      float* __restrict__ o0, float* __restrict__ o1,
+                                                      float* __restrict__ o2) {
+  pdl_begin();
+  __shared__ float4 red[8][32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t total = 3 * df, c = ((int64_t)blockIdx.x * 32 + lane) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < total) {
+#pragma unroll 4
+    for (int k = splits * w / 8; k < splits * (w + 1) / 8; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(part + k * total + c);
+      s.x += v.x;
+      s.y += v.y;
+      s.z += v.z;
+      s.w += v.w;
+    }
+  }
+  red[w][lane] = s;
+  __syncthreads();
+  if (w > 0 || c >= total) return;
+  for (int k = 1; k < 8; ++k) {
+    const float4 v = red[k][lane];
+    s.x += v.x;
+    s.y += v.y;
+    s.z += v.z;
+    s.w += v.w;
+  }
+  float* o = c < df ? o0 : c < 2 * df ? o1 : o2;
+  *reinterpret_cast<float4*>(o + c % df) = s;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -684,7 +707,8 @@ hg_status wg_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
   HG_TRY(launch("ffn_wgrad_tc", ffn_wgrad_tc_kernel<D, kAct>, dim3((unsigned)(chunks * splits)), dim3(kThreads),
                 C::kSmem, s, tm_X, tm_dY, tm_Wt, tm_W, p));
   const int64_t df = (int64_t)D * w->f;
-  return reduce_partials3(L.part, 3 * df, splits, df, g->dW_gate, g->dW_up, g->dW_down, s);
+  return launch("ffn_sum_shares", ffn_sum_shares, dim3((unsigned)ceil_div(3 * df, 128)), dim3(256), 0, s,
+                (const float*)L.part, splits, df, g->dW_gate, g->dW_up, g->dW_down);
 }
 
 template <int D, int kAct>

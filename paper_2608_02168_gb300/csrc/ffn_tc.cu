@@ -28,7 +28,9 @@ namespace {
 constexpr int kRows = 128;
 constexpr int kHc = 64;              // hidden features of a chunk
 constexpr int kBlk = kRows * 128;    // a 64-column block of a 128-row tile
-constexpr int kThreads = 384;        // warps 0..3: TMA, MMA issue, tensor memory, idle; two warpgroups for the gates
+// warps 0..3: TMA, MMA issue, tensor memory, idle; then two warpgroups for the gates of each slot: with one, a
+// scheduler's single warp of a slot waits out every latency of its own (1M rows, d = 256: 1370 us)
+constexpr int kThreads = 640;
 constexpr int kSms = 152;
 
 template <int D>
@@ -55,18 +57,6 @@ struct FwdP {
   int* status;
 };
 
-__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
 template <int D, int kAct>
 __global__ void __launch_bounds__(kThreads, 1)
     ffn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_G,
@@ -92,10 +82,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(xfree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&gfull[i], 1);
-      mbar_init(&hfull[i], 128);
+      mbar_init(&hfull[i], 256);
       mbar_init(&hfree[i], 1);
       mbar_init(&yfull[i], 1);
-      mbar_init(&yfree[i], NT == 2 ? 128 : 256);
+      mbar_init(&yfree[i], NT == 2 ? 256 : 512);
     }
     mbar_init(quit, 1);
     fence_mbar_init();
@@ -251,9 +241,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) drain_mma(quit, 0);
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- gates and rows out
-    const int s = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+    // half of the slot's hidden features (and of its tile's columns) for each warpgroup
+    const int s = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t gcol = tmem + C::kGuCol + s * 128 + lane_off;
+    const uint32_t gcol = tmem + C::kGuCol + s * 128 + half * 32 + lane_off;
     uint8_t* H = Hs + s * C::kH;
     bool ok = true;
     uint32_t k = 0, gi = 0;
@@ -269,48 +260,48 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x, ++gi) {
       for (int c = NT == 2 ? 0 : s; ok && c < nch; c += 3 - NT, ++k) {
         if (!wait(&gfull[s], k & 1)) break;
-        uint32_t h[32];
+        uint32_t h[16];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t g[32], u[32];
-          tmem_ld32_issue(gcol + half * 32, g);
-          tmem_ld32_issue(gcol + 64 + half * 32, u);
-          tmem_ld_wait();
+        for (int x = 0; x < 32; x += 16) {
+          uint32_t g[16], u[16];
+          ld16_issue(gcol + x, g);
+          ld16_issue(gcol + 64 + x, u);
+          ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
+          for (int e = 0; e < 16; e += 2) {
             float a0, a1;
             gate2<kAct>(__uint_as_float(g[e]), __uint_as_float(g[e + 1]), &a0, &a1);
-            h[half * 16 + e / 2] = pack2_bf16(a0 * __uint_as_float(u[e]), a1 * __uint_as_float(u[e + 1]));
+            h[(x + e) / 2] = pack2_bf16(a0 * __uint_as_float(u[e]), a1 * __uint_as_float(u[e + 1]));
           }
         }
         if (k >= 1 && !wait(&hfree[s], (k - 1) & 1)) break;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          st16(H + sw128_offset(row, e * 16), make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]));
+        for (int e = 0; e < 4; ++e)
+          st16(H + sw128_offset(row, half * 64 + e * 16), make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]));
         fence_async_smem();
         fence_before_sync();
         mbar_arrive(&hfull[s]);
       }
       if (!ok) break;
       const int t = NT == 2 ? s : 0;
-      constexpr int CW = NT == 2 ? D : D / 2;  // columns of a warpgroup
-      const int col0 = NT == 2 ? 0 : s * CW;
+      constexpr int CW = NT == 2 ? D / 2 : D / 4;  // columns of a warpgroup
+      const int col0 = (NT == 2 ? half : s * 2 + half) * CW;
       const int64_t r = (gr * NT + t) * kRows + row;
       const bool live = r < p.n;
       if (!wait(&yfull[t], gi & 1)) break;
 #pragma unroll
-      for (int c = 0; c < CW; c += 32) {
-        uint32_t y[32];
-        tmem_ld32_issue(tmem + C::kYCol + t * D + lane_off + col0 + c, y);
-        uint4 x[4];
+      for (int c = 0; c < CW; c += 16) {
+        uint32_t y[16];
+        ld16_issue(tmem + C::kYCol + t * D + lane_off + col0 + c, y);
+        uint4 x[2];
         if (p.res && live) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = ldg16(p.res + r * D + col0 + c + e * 8);
+          x[0] = ldg16(p.res + r * D + col0 + c);
+          x[1] = ldg16(p.res + r * D + col0 + c + 8);
         }
-        tmem_ld_wait();
+        ld_wait();
         if (live) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 2; ++e) {
             float v[8];
             if (p.res) {
               unpack(x[e], v, __nv_bfloat16());

@@ -25,8 +25,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHeads = 64;
-constexpr int kBlocksPerSm = 4;
 constexpr int kSms = 152;
+
+// CTAs of an SM.  A run has no more of them, since a second wave would find a part of the SMs' room empty.
+constexpr int resident(bool bwd) { return bwd ? 2 : 3; }
 
 struct RotRows {
   const void* x;
@@ -60,7 +62,7 @@ __device__ __forceinline__ void turn_sincos(uint64_t phase, float* s, float* c) 
 }
 
 template <typename T, int DH, bool kInter, bool kBwd>
-__global__ void __launch_bounds__(kThreads) qkrot_kernel(const __grid_constant__ RotArgs a) {
+__global__ void __launch_bounds__(kThreads, resident(kBwd)) qkrot_kernel(const __grid_constant__ RotArgs a) {
   pdl_begin();
   constexpr int V = VecTraits<T>::kElems;
   constexpr int L = DH / (2 * V);
@@ -101,12 +103,13 @@ __global__ void __launch_bounds__(kThreads) qkrot_kernel(const __grid_constant__
   const int64_t step = groups / a.heads;
   const int64_t iters = (a.n + step - 1) / step;
   int64_t i = gid < groups ? gid / a.heads : a.n;
-  for (int64_t it = 0; it < iters; ++it, i += step) {
-    const bool live = i < a.n;
-    float x[2 * V], y[2 * V];
-    uint4 v0 = make_uint4(0, 0, 0, 0), v1 = v0, w0 = v0, w1 = v0;
-    int64_t p = 0;
-    if (live) {
+  // the next row's loads run ahead of this row's arithmetic
+  uint4 v0, v1, w0, w1;
+  int64_t p;
+  auto fetch = [&]() {
+    v0 = v1 = w0 = w1 = make_uint4(0, 0, 0, 0);
+    p = 0;
+    if (i < a.n) {
       const T* src = static_cast<const T*>(rows.x) + i * rows.sx + h * DH;
       v0 = ld16(src + o0);
       v1 = ld16(src + o1);
@@ -117,18 +120,27 @@ __global__ void __launch_bounds__(kThreads) qkrot_kernel(const __grid_constant__
       }
       p = a.pos ? a.pos[i] : i;
     }
+  };
+  fetch();
+  for (int64_t it = 0; it < iters; ++it) {
+    const int64_t row = i;
+    const uint64_t at = (uint64_t)p;
+    float x[2 * V], y[2 * V];
     unpack(v0, x, T());
     unpack(v1, x + V, T());
+    if (kBwd) {
+      unpack(w0, y, T());
+      unpack(w1, y + V, T());
+    }
+    i += step;
+    fetch();
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     const float rn = rsqrtf(ss * (1.f / DH) + a.eps);
-    if (kBwd) {
-      unpack(w0, y, T());
-      unpack(w1, y + V, T());
-    } else {
+    if (!kBwd) {
 #pragma unroll
       for (int e = 0; e < 2 * V; ++e) y[e] = x[e] * rn * gm[e];
     }
@@ -136,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) qkrot_kernel(const __grid_constant__
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         float s, c;
-        turn_sincos<kExact>((uint64_t)p * fr[e], &s, &c);
+        turn_sincos<kExact>(at * fr[e], &s, &c);
         if (kBwd) s = -s;
         const int ia = kInter ? 2 * e : e, ib = kInter ? 2 * e + 1 : V + e;
         const float ya = y[ia], yb = y[ib];
@@ -160,8 +172,8 @@ __global__ void __launch_bounds__(kThreads) qkrot_kernel(const __grid_constant__
 #pragma unroll
       for (int e = 0; e < 2 * V; ++e) y[e] = rn * (y[e] - x[e] * m);
     }
-    if (live) {
-      T* dst = static_cast<T*>(rows.out) + i * rows.sout + h * DH;
+    if (row < a.n) {
+      T* dst = static_cast<T*>(rows.out) + row * rows.sout + h * DH;
       st16(dst + o0, pack(y, T()));
       st16(dst + o1, pack(y + V, T()));
     }
@@ -211,10 +223,11 @@ __global__ void __launch_bounds__(256) qkrot_gains(const float* __restrict__ par
 
 // Blocks of a run: enough for every head of every row, at least one block per row's heads, at most a
 // resident set.
-int rot_grid(int64_t n, int heads, int dh, int v) {
-  const int64_t groups = kThreads / (dh / (2 * v));
+int rot_grid(int64_t n, int heads, int dh, hg_dtype dt, bool bwd) {
+  const int bytes = dt == HG_BF16 ? 2 : 4;
+  const int64_t groups = kThreads / (dh * bytes / 32);
   const int64_t want = ceil_div(n * heads, groups);
-  return (int)std::max(ceil_div(heads, groups), std::min<int64_t>(want, kSms * kBlocksPerSm));
+  return (int)std::max(ceil_div(heads, groups), std::min<int64_t>(want, kSms * resident(bwd)));
 }
 
 template <typename T, int DH, bool kBwd>
@@ -259,8 +272,8 @@ hg_status check_rows(const hg_rows* r, const char* name, int64_t n, int64_t widt
 }
 
 size_t rot_scratch(const hg_qkrot_params* p, int64_t n) {
-  const int v = p->dtype == HG_BF16 ? 8 : 4;
-  return align_up(sizeof(float) * 2 * p->d_h * (size_t)rot_grid(std::max<int64_t>(n, 1), p->heads_q + p->heads_k, p->d_h, v));
+  return align_up(sizeof(float) * 2 * p->d_h *
+                  (size_t)rot_grid(std::max<int64_t>(n, 1), p->heads_q + p->heads_k, p->d_h, p->dtype, true));
 }
 
 void fill_args(RotArgs* a, const hg_qkrot_params* p, const int64_t* pos, int64_t n) {
@@ -313,9 +326,9 @@ extern "C" hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* 
   if (wk) a.k = {k->p, nullptr, k_out->p, k->stride, 0, k_out->stride};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool inter = params->interleaved != 0;
-  if (params->dtype == HG_F32)
-    return rot_width<float, false>(a, params->d_h, rot_grid(n, a.heads, params->d_h, 4), inter, s);
-  return rot_width<__nv_bfloat16, false>(a, params->d_h, rot_grid(n, a.heads, params->d_h, 8), inter, s);
+  const int grid = rot_grid(n, a.heads, params->d_h, params->dtype, false);
+  if (params->dtype == HG_F32) return rot_width<float, false>(a, params->d_h, grid, inter, s);
+  return rot_width<__nv_bfloat16, false>(a, params->d_h, grid, inter, s);
 }
 
 extern "C" hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* q, const hg_rows* k, const int64_t* pos,
@@ -348,7 +361,7 @@ extern "C" hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* 
   if (wk) a.k = {k->p, dk_out->p, dk->p, k->stride, dk_out->stride, dk->stride};
   a.part = static_cast<float*>(scratch);
   const bool inter = params->interleaved != 0;
-  const int grid = rot_grid(n, a.heads, params->d_h, params->dtype == HG_BF16 ? 8 : 4);
+  const int grid = rot_grid(n, a.heads, params->d_h, params->dtype, true);
   if (params->dtype == HG_F32)
     HG_TRY((rot_width<float, true>(a, params->d_h, grid, inter, s)));
   else
