@@ -46,17 +46,6 @@ __device__ __forceinline__ void st8(uint32_t taddr, const uint32_t* r) {
                : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D += A[tmem] B[smem]: A's lane = row, each 32-bit column two bf16 along K
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
 __device__ __forceinline__ uint8_t* align1024(uint8_t* p) {
   return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~uintptr_t(1023));
 }
@@ -90,6 +79,7 @@ struct DxCfg {
   static constexpr int kX = NB * kBlk;
   static constexpr int kOps = kTs ? 0 : 2 * kBlk;    // dG, dU: 64 columns each
   static constexpr int kSmem = 2 * kX + NG * kGu + ND * kDown + kOps + 512 + 1024;
+  static constexpr int kStoreThreads = D == 64 ? 512 : D == 128 ? 256 : 128;  // that fill a 64-column block of dX
   static constexpr int PR = D < 128 ? D : 128;       // rows of a TMA box of [W_gate | W_up]
   // tensor memory: dX, the slots ([G | U | dH], 192 columns), dG and dU (kTs)
   static constexpr uint32_t kSlot = D, kSlotCols = 192, kOpsCol = 448;
@@ -99,8 +89,7 @@ struct DxP {
   int64_t n;
   int nch;
   int64_t tiles;
-  const __nv_bfloat16* res;  // dY, or null without the residual
-  __nv_bfloat16* dX;
+  int residual;
   int* status;
 };
 
@@ -108,7 +97,7 @@ template <int D, int kAct>
 __global__ void __launch_bounds__(kThreads, 1)
     ffn_dx_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_dY,
                      const __grid_constant__ CUtensorMap tm_G, const __grid_constant__ CUtensorMap tm_U,
-                     const __grid_constant__ CUtensorMap tm_W, DxP p) {
+                     const __grid_constant__ CUtensorMap tm_W, const __grid_constant__ CUtensorMap tm_dX, DxP p) {
   pdl_begin();
   using C = DxCfg<D>;
   constexpr int NB = C::NB, HC = C::HC, NG = C::NG, ND = C::ND, SLOTS = C::SLOTS;
@@ -121,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(Os + C::kOps);
   uint64_t *wfull = bars, *wfree = wfull + NG, *dfull = wfree + NG, *dfree = dfull + ND, *xfull = dfree + ND,
            *xfree = xfull + 1, *gfull = xfree + 1, *ofull = gfull + 2, *ofree = ofull + 1, *yfull = ofree + 1,
-           *yfree = yfull + 1, *quit = yfree + 1;
+           *yfree = yfull + 1, *sfull = yfree + 1, *quit = sfull + 4;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -134,7 +123,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&dfree[i], 1);
     }
     mbar_init(xfull, 1);
-    mbar_init(xfree, 1);
+    mbar_init(xfree, 512 / C::kStoreThreads);
+    for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads);
     mbar_init(&gfull[0], 1);
     mbar_init(&gfull[1], 1);
     mbar_init(ofull, SLOTS == 2 ? 256 : 512);
@@ -185,59 +175,58 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_rounds(dfull, ND, q);
       drain_rounds(wfull, NG, q);
     }
-  } else if (warp == 1 && lane == 0) {
-    Waiter wait{p.status};
+  } else if (warp == 1) {
+    const Issuer issue;
+    WarpWaiter wait{p.status};
     uint32_t q = 0, ti = 0;  // q: chunks whose [G | U | dH] was issued
-    const uint32_t xs = smem_u32(Xs), ys = smem_u32(Ys), gs = smem_u32(Gs), ds = smem_u32(Ds), os = smem_u32(Os);
+    const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), yd = desc_sw128(smem_u32(Ys), 16, 1024);
+    const uint64_t gd = desc_sw128(smem_u32(Gs), D * 128, 1024), gkd = desc_sw128(smem_u32(Gs), 16, 1024);
+    const uint64_t dd = desc_sw128(smem_u32(Ds), 16, 1024), od = desc_sw128(smem_u32(Os), 16, 1024);
     constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_h = idesc_bf16(128, 64, false, false),
                        id_dx = idesc_bf16(128, D, false, false);
     auto hidden = [&](int s) {
       const uint32_t sg = q % NG, sd = q % ND;
       if (!wait(&wfull[sg], (q / NG) & 1) || !wait(&dfull[sd], (q / ND) & 1)) return;
-      const uint32_t w = gs + sg * C::kGu, w2 = ds + sd * C::kDown, t = tmem + C::kSlot + s * C::kSlotCols;
+      const uint64_t w = desc_at(gd, sg * C::kGu), w2 = desc_at(dd, sd * C::kDown);
+      const uint32_t t = tmem + C::kSlot + s * C::kSlotCols;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
-        mma_bf16(t, desc_sw128(xs + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
-                 desc_sw128(w + j * 2048, D * 128, 1024), id_gu, j > 0 ? 1u : 0u);
+        issue.mma(t, desc_at(xd, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w, j * 2048), id_gu, j > 0 ? 1u : 0u);
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
-        mma_bf16(t + 128, desc_sw128(ys + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
-                 desc_sw128(w2 + (j >> 2) * (HC * 128) + (j & 3) * 32, 16, 1024), id_h, j > 0 ? 1u : 0u);
-      mma_commit(&gfull[s]);
-      mma_commit(&dfree[sd]);
+        issue.mma(t + 128, desc_at(yd, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w2, (j >> 2) * (HC * 128) + (j & 3) * 32),
+                 id_h, j > 0 ? 1u : 0u);
+      issue.commit(&gfull[s]);
+      issue.commit(&dfree[sd]);
       ++q;
     };
     uint32_t done = 0;  // chunks whose dX was issued
     for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
       if (!wait(xfull, ti & 1)) break;
       for (int c = 0; wait.ok && c < SLOTS && c < nch; ++c) hidden(c % SLOTS);
-      if (wait.ok && nch <= SLOTS) mma_commit(xfree);
       for (int c = 0; wait.ok && c < nch; ++c) {
         if (!wait(ofull, done & 1)) break;
         if (c == 0 && ti >= 1 && !wait(yfree, (ti - 1) & 1)) break;
-        const uint32_t w = gs + done % NG * C::kGu;
+        const uint64_t w = desc_at(gkd, done % NG * C::kGu);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < HC / 16; ++j) {
-            const uint64_t b = desc_sw128(w + half * D * 128 + j * 32, 16, 1024);
+            const uint64_t b = desc_at(w, half * D * 128 + j * 32);
             const uint32_t acc = (c > 0 || half > 0 || j > 0) ? 1u : 0u;
             if (C::kTs)
-              mma_bf16_ts(tmem, tmem + C::kOpsCol + half * 32 + j * 8, b, id_dx, acc);
+              issue.mma_ts(tmem, tmem + C::kOpsCol + half * 32 + j * 8, b, id_dx, acc);
             else
-              mma_bf16(tmem, desc_sw128(os + half * kBlk + j * 32, 16, 1024), b, id_dx, acc);
+              issue.mma(tmem, desc_at(od, half * kBlk + j * 32), b, id_dx, acc);
           }
-        mma_commit(ofree);
-        mma_commit(&wfree[done % NG]);
+        issue.commit(ofree);
+        issue.commit(&wfree[done % NG]);
         ++done;
-        if (c == nch - 1) mma_commit(yfull);
-        if (c + SLOTS < nch) {
-          hidden((c + SLOTS) % SLOTS);
-          if (wait.ok && c + SLOTS == nch - 1) mma_commit(xfree);
-        }
+        if (c == nch - 1) issue.commit(yfull);
+        if (c + SLOTS < nch) hidden((c + SLOTS) % SLOTS);
       }
     }
-    if (!wait.ok) drain_mma(quit, 0);
+    if (!wait.ok) issue.drain(quit);
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
@@ -245,15 +234,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t0 = tmem + C::kSlot + s * C::kSlotCols + lane_off;
     constexpr int HW = HC * SLOTS / 4;  // hidden features of a warpgroup
     const int h0 = (SLOTS == 2 ? wg & 1 : wg) * HW;
-    Waiter one{p.status};
-    auto wait = [&](uint64_t* b, uint32_t parity) {
-      one(b, parity);
-      one.ok = __all_sync(0xffffffffu, one.ok);
-      return one.ok;
-    };
+    WarpWaiter wait{p.status};
     uint32_t k = 0, done = 0, ti = 0;  // chunks of this slot, of all slots; tiles
-    for (int64_t tile = blockIdx.x; one.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
-      for (int c = 0; one.ok && c < nch; ++c, ++done) {
+    for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
+      for (int c = 0; wait.ok && c < nch; ++c, ++done) {
         if (SLOTS == 2 && (c & 1) != s) continue;
         if (!wait(&gfull[s], k & 1)) break;
         ++k;
@@ -294,40 +278,45 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before_sync();
         mbar_arrive(ofull);
       }
-      if (!one.ok) break;
+      if (!wait.ok) break;
+      // rows out: dY's place takes dX (+ dY), and a TMA store each 64 columns (it leaves out the rows past n)
       constexpr int CW = D / 4;
-      const int64_t r = tile * kRows + row;
-      const bool live = r < p.n;
-      if (!wait(yfull, ti & 1)) break;
+      const int col0 = wg * CW;
+      uint8_t* yb = Ys + col0 / 64 * kBlk;
+      if (!wait(xfull, ti & 1) || !wait(yfull, ti & 1)) break;
 #pragma unroll
       for (int c = 0; c < CW; c += 16) {
         uint32_t y[16];
-        ld16_issue(tmem + lane_off + wg * CW + c, y);
-        uint4 x[2];
-        if (p.res && live) {
-          x[0] = ldg16(p.res + r * D + wg * CW + c);
-          x[1] = ldg16(p.res + r * D + wg * CW + c + 8);
-        }
+        ld16_issue(tmem + lane_off + col0 + c, y);
+        uint4* x0 = reinterpret_cast<uint4*>(yb + sw128_offset(row, (col0 % 64 + c) * 2));
+        uint4* x1 = reinterpret_cast<uint4*>(yb + sw128_offset(row, (col0 % 64 + c) * 2 + 16));
+        float v[16];
+        unpack(p.residual ? *x0 : make_uint4(0u, 0u, 0u, 0u), v, __nv_bfloat16());
+        unpack(p.residual ? *x1 : make_uint4(0u, 0u, 0u, 0u), v + 8, __nv_bfloat16());
         ld_wait();
-        if (live) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v[8];
-            if (p.res) {
-              unpack(x[e], v, __nv_bfloat16());
-            } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(y[e * 8 + i]);
-            st16(p.dX + r * D + wg * CW + c + e * 8, pack(v, __nv_bfloat16()));
-          }
-        }
+        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(y[i]);
+        *x0 = pack(v, __nv_bfloat16());
+        *x1 = pack(v + 8, __nv_bfloat16());
       }
+      fence_async_smem();
       fence_before_sync();
       mbar_arrive(yfree);
+      uint64_t* sb = &sfull[(threadIdx.x - 128) / C::kStoreThreads];
+      mbar_arrive(sb);
+      if ((threadIdx.x - 128) % C::kStoreThreads == 0) {
+        if (mbar_wait(sb, ti & 1)) {
+          tma_store_2d(&tm_dX, yb, col0 / 64 * 64, (int)(tile * kRows));
+          bulk_commit();
+          bulk_wait_read();
+        } else {
+          record_device_error(p.status, kErrTimeout);
+        }
+        mbar_arrive(xfree);
+      }
+      __syncwarp();
     }
+    bulk_wait();
   }
   fence_before_sync();
   __syncthreads();
@@ -421,9 +410,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(wfull, 0);
       drain_rounds(xfull, XS, q);
     }
-  } else if (warp == 1 && lane == 0) {
-    Waiter wait{p.status};
-    const uint32_t xs = smem_u32(Xs), ws = smem_u32(Ws), ds = smem_u32(Ds), os = smem_u32(Os);
+  } else if (warp == 1) {
+    const Issuer issue;
+    WarpWaiter wait{p.status};
+    const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), xmd = desc_sw128(smem_u32(Xs), kBlk, 1024);
+    const uint64_t wd = desc_sw128(smem_u32(Ws), 16, 1024), dd = desc_sw128(smem_u32(Ds), 16, 1024);
+    const uint64_t od = desc_sw128(smem_u32(Os), kBlk, 1024);
     constexpr uint32_t id_gu = idesc_bf16(128, N2, false, false), id_h = idesc_bf16(128, HC, false, false),
                        id_w = idesc_bf16(128, N2, true, true);
     wait(wfull, 0);
@@ -431,48 +423,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int s = i % XS;
       if (!wait(&xfull[s], (i / XS) & 1)) break;
       if (i >= 1 && !wait(ofull, (i - 1) & 1)) break;  // the hidden sums of the tile before were read
-      const uint32_t x = xs + s * 2 * C::kX, y = x + C::kX, hid = tmem + C::kHid;
+      const uint64_t x = desc_at(xd, s * 2 * C::kX), xm = desc_at(xmd, s * 2 * C::kX);
+      const uint32_t hid = tmem + C::kHid;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
-        mma_bf16(hid, desc_sw128(x + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
-                 desc_sw128(ws + (j >> 2) * (N2 * 128) + (j & 3) * 32, 16, 1024), id_gu, j > 0 ? 1u : 0u);
+        issue.mma(hid, desc_at(x, (j >> 2) * kBlk + (j & 3) * 32), desc_at(wd, (j >> 2) * (N2 * 128) + (j & 3) * 32),
+                 id_gu, j > 0 ? 1u : 0u);
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
-        mma_bf16(hid + N2, desc_sw128(y + (j >> 2) * kBlk + (j & 3) * 32, 16, 1024),
-                 desc_sw128(ds + (j >> 2) * (HC * 128) + (j & 3) * 32, 16, 1024), id_h, j > 0 ? 1u : 0u);
-      mma_commit(gfull);
+        issue.mma(hid + N2, desc_at(x, C::kX + (j >> 2) * kBlk + (j & 3) * 32),
+                 desc_at(dd, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
+      issue.commit(gfull);
       if (!wait(ofull, i & 1)) break;
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         // d = 64: X and dY side by side are the 128 rows of both gradients
-        const uint32_t ax = x + m * 2 * kBlk, ay = D == 64 ? x : y + m * 2 * kBlk;
+        const uint32_t ax = m * 2 * kBlk, ay = (D == 64 ? 0 : C::kX) + m * 2 * kBlk;
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            mma_bf16(tmem + m * N2, desc_sw128(ax + j * 2048, kBlk, 1024),
-                     desc_sw128(os + part * C::kOps + j * 2048, kBlk, 1024), id_w, (part > 0 || j > 0) ? 1u : 0u);
+            issue.mma(tmem + m * N2, desc_at(xm, ax + j * 2048), desc_at(od, part * C::kOps + j * 2048), id_w, (part > 0 || j > 0) ? 1u : 0u);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          mma_bf16(tmem + C::kAcc2 + m * N2, desc_sw128(ay + j * 2048, kBlk, 1024),
-                   desc_sw128(os + 2 * C::kOps + j * 2048, kBlk, 1024), id_w, j > 0 ? 1u : 0u);
+          issue.mma(tmem + C::kAcc2 + m * N2, desc_at(xm, ay + j * 2048), desc_at(od, 2 * C::kOps + j * 2048), id_w, j > 0 ? 1u : 0u);
       }
-      mma_commit(&xfree[s]);
-      mma_commit(ofree);
+      issue.commit(&xfree[s]);
+      issue.commit(ofree);
     }
-    if (!wait.ok) drain_mma(quit, 0);
+    if (!wait.ok) issue.drain(quit);
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     constexpr int HW = HC / 4;  // hidden features of a warpgroup
     const int h0 = wg * HW;
     const uint32_t hid = tmem + C::kHid + lane_off;
-    Waiter one{p.status};
-    auto wait = [&](uint64_t* b, uint32_t parity) {
-      one(b, parity);
-      one.ok = __all_sync(0xffffffffu, one.ok);
-      return one.ok;
-    };
+    WarpWaiter wait{p.status};
     // 16 bytes (8 features from column c of an operand block pair) of this row
     auto put = [&](uint8_t* o, int c, const uint32_t* v) {
       st16(o + (c >> 6) * kBlk + sw128_offset(row, (c & 63) * 2), make_uint4(v[0], v[1], v[2], v[3]));
@@ -546,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_arrive(ofull);
     }
     // the sums of this share: part[split] = [dW_gate d x f | dW_up d x f | dW_down f x d]
-    if (one.ok && wait(ofree, (count - 1) & 1)) {
+    if (wait.ok && wait(ofree, (count - 1) & 1)) {
       drain();
       float* out = p.part + (int64_t)split * 3 * D * p.f;
       const int64_t df = (int64_t)D * p.f;
@@ -645,16 +631,16 @@ hg_status dx_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
     HG_CUDA(cudaFuncSetAttribute(ffn_dx_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     done = true;
   }
-  CUtensorMap tm_X, tm_dY, tm_G, tm_U, tm_W;
+  CUtensorMap tm_X, tm_dY, tm_G, tm_U, tm_W, tm_dX;
   HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
   HG_TRY(make_tmap_bf16(&tm_dY, dY, (uint64_t)n, D, kRows));
   HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, C::PR));
   HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, C::PR));
   HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, C::HC));
-  DxP p{n, (int)ceil_div(w->f, C::HC), ceil_div(n, kRows), w->residual ? (const __nv_bfloat16*)dY : nullptr,
-        (__nv_bfloat16*)dX, device_status_ptr()};
+  HG_TRY(make_tmap_bf16(&tm_dX, dX, (uint64_t)n, D, kRows));
+  DxP p{n, (int)ceil_div(w->f, C::HC), ceil_div(n, kRows), w->residual != 0, device_status_ptr()};
   return launch("ffn_dx_tc", ffn_dx_tc_kernel<D, kAct>, dim3((unsigned)std::min<int64_t>(p.tiles, kSms)),
-                dim3(kThreads), C::kSmem, s, tm_X, tm_dY, tm_G, tm_U, tm_W, p);
+                dim3(kThreads), C::kSmem, s, tm_X, tm_dY, tm_G, tm_U, tm_W, tm_dX, p);
 }
 
 int hidden_chunk(int d) { return d == 256 ? WgCfg<256>::HC : WgCfg<128>::HC; }

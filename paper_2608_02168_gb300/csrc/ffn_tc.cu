@@ -45,6 +45,7 @@ struct FCfg {
   static constexpr int kX = NT * NB * kBlk;
   static constexpr int kH = kRows * 128;
   static constexpr int kSmem = kX + NS * kPiece + 2 * kH + 512 + 1024;
+  static constexpr int kStoreThreads = D == 64 ? 256 : 128;  // that fill one 64-column block of the rows out
   static constexpr uint32_t kYCol = 0, kGuCol = 256;         // tensor memory: Y (tile x at x D), slots of 128
 };
 
@@ -52,15 +53,15 @@ struct FwdP {
   int64_t n;
   int nch;
   int64_t groups;
-  const __nv_bfloat16* res;  // X, or null without the residual
-  __nv_bfloat16* Y;
+  int residual;
   int* status;
 };
 
 template <int D, int kAct>
 __global__ void __launch_bounds__(kThreads, 1)
     ffn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_G,
-                      const __grid_constant__ CUtensorMap tm_U, const __grid_constant__ CUtensorMap tm_W, FwdP p) {
+                      const __grid_constant__ CUtensorMap tm_U, const __grid_constant__ CUtensorMap tm_W,
+                      const __grid_constant__ CUtensorMap tm_Y, FwdP p) {
   pdl_begin();
   using C = FCfg<D>;
   constexpr int NB = C::NB, NT = C::NT, NS = C::NS, KP = C::KP;
@@ -70,7 +71,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* Hs = Ws + NS * C::kPiece;
   uint64_t* bars = reinterpret_cast<uint64_t*>(Hs + 2 * C::kH);
   uint64_t *wfull = bars, *wfree = bars + NS, *xfull = bars + 2 * NS, *xfree = xfull + 1, *gfull = xfull + 2,
-           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yfree = yfull + 2, *quit = yfree + 2;
+           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yfree = yfull + 2, *sfull = yfree + 2,
+           *quit = sfull + 4;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&wfree[i], 1);
     }
     mbar_init(xfull, 1);
-    mbar_init(xfree, 1);
+    mbar_init(xfree, 512 / C::kStoreThreads);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&gfull[i], 1);
       mbar_init(&hfull[i], 256);
@@ -87,6 +89,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&yfull[i], 1);
       mbar_init(&yfree[i], NT == 2 ? 256 : 512);
     }
+    for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads);
     mbar_init(quit, 1);
     fence_mbar_init();
   }
@@ -147,98 +150,86 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (xn) mbar_wait(xfull, (xn - 1) & 1);
       drain_rounds(wfull, NS, q);
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     // ---------------------------------------------------------------- products
-    bool ok = true;
+    const Issuer issue;
+    WarpWaiter wait{p.status};
     uint32_t q = 0, gi = 0;
     uint32_t hk[2] = {0, 0};  // chunks of each slot so far
-    auto wait = [&](uint64_t* b, uint32_t parity) {
-      if (ok && !mbar_wait(b, parity)) {
-        ok = false;
-        record_device_error(p.status, kErrTimeout);
-      }
-      if (ok) fence_after_sync();
-      return ok;
-    };
-    const uint32_t xs = smem_u32(Xs), ws = smem_u32(Ws), hs = smem_u32(Hs);
+    const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), hd = desc_sw128(smem_u32(Hs), 16, 1024);
+    const uint64_t gd = desc_sw128(smem_u32(Ws), C::PR * 128, 1024), wd = desc_sw128(smem_u32(Ws), kHc * 128, 1024);
     constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_y = idesc_bf16(128, D, false, true);
     // pieces q0 .. q0 + KP - 1 times tile t into slot s
     auto gu = [&](uint32_t q0, int t, int s) {
 #pragma unroll
       for (int k = 0; k < KP; ++k) {
         if (t == 0 && !wait(&wfull[(q0 + k) % NS], ((q0 + k) / NS) & 1)) return;
-        const uint32_t w = ws + (q0 + k) % NS * C::kPiece;
+        const uint64_t w = desc_at(gd, (q0 + k) % NS * C::kPiece), x = desc_at(xd, t * NB * kBlk);
 #pragma unroll
         for (int j = 0; j < C::PR / 16; ++j) {
           const int jj = k * (C::PR / 16) + j;
-          mma_bf16(tmem + C::kGuCol + s * 128,
-                   desc_sw128(xs + (t * NB + (jj >> 2)) * kBlk + (jj & 3) * 32, 16, 1024),
-                   desc_sw128(w + j * 2048, C::PR * 128, 1024), id_gu, jj > 0 ? 1u : 0u);
+          issue.mma(tmem + C::kGuCol + s * 128, desc_at(x, (jj >> 2) * kBlk + (jj & 3) * 32), desc_at(w, j * 2048),
+                   id_gu, jj > 0 ? 1u : 0u);
         }
       }
-      mma_commit(&gfull[s]);
+      issue.commit(&gfull[s]);
     };
     auto down = [&](uint32_t qd, int c, int s) {
       const int t = NT == 2 ? s : 0;
       if (!wait(&hfull[s], hk[s] & 1)) return;
       if (c == 0 && gi >= 1 && !wait(&yfree[t], (gi - 1) & 1)) return;
       ++hk[s];
-      const uint32_t w = ws + qd % NS * C::kPiece;
+      const uint64_t w = desc_at(wd, qd % NS * C::kPiece), h = desc_at(hd, s * C::kH);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        mma_bf16(tmem + C::kYCol + t * D, desc_sw128(hs + s * C::kH + j * 32, 16, 1024),
-                 desc_sw128(w + j * 2048, kHc * 128, 1024), id_y, (c > 0 || j > 0) ? 1u : 0u);
-      mma_commit(&hfree[s]);
-      if (c == nch - 1) mma_commit(&yfull[t]);
+        issue.mma(tmem + C::kYCol + t * D, desc_at(h, j * 32), desc_at(w, j * 2048), id_y, (c > 0 || j > 0) ? 1u : 0u);
+      issue.commit(&hfree[s]);
+      if (c == nch - 1) issue.commit(&yfull[t]);
     };
     auto release = [&](uint32_t q0, int count) {
-      for (int i = 0; i < count; ++i) mma_commit(&wfree[(q0 + i) % NS]);
+      for (int i = 0; i < count; ++i) issue.commit(&wfree[(q0 + i) % NS]);
     };
-    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x, ++gi) {
+    for (int64_t gr = blockIdx.x; wait.ok && gr < p.groups; gr += gridDim.x, ++gi) {
       if (!wait(xfull, gi & 1)) break;
       if (NT == 2) {
-        for (int t = 0; ok && t < 2; ++t) gu(q, t, t);
-        if (!ok) break;
+        for (int t = 0; wait.ok && t < 2; ++t) gu(q, t, t);
+        if (!wait.ok) break;
         release(q, KP);
         q += KP;
-        if (nch == 1) mma_commit(xfree);
-        for (int c = 0; ok && c < nch; ++c) {
+        for (int c = 0; wait.ok && c < nch; ++c) {
           const bool more = c + 1 < nch;
           if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
-          for (int s = 0; ok && s < 2; ++s) {
+          for (int s = 0; wait.ok && s < 2; ++s) {
             down(q, c, s);
-            if (ok && more) gu(q + 1, s, s);
+            if (wait.ok && more) gu(q + 1, s, s);
           }
-          if (!ok) break;
+          if (!wait.ok) break;
           release(q, 1 + (more ? KP : 0));
           q += 1 + (more ? KP : 0);
-          if (c + 2 == nch) mma_commit(xfree);
         }
       } else {
-        for (int c = 0; ok && c < 2 && c < nch; ++c) {
+        for (int c = 0; wait.ok && c < 2 && c < nch; ++c) {
           gu(q, 0, c);
-          if (!ok) break;
+          if (!wait.ok) break;
           release(q, KP);
           q += KP;
         }
-        if (ok && nch <= 2) mma_commit(xfree);
-        for (int c = 0; ok && c < nch; ++c) {
+        for (int c = 0; wait.ok && c < nch; ++c) {
           if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
           down(q, c, c & 1);
-          if (!ok) break;
+          if (!wait.ok) break;
           release(q, 1);
           ++q;
           if (c + 2 < nch) {
             gu(q, 0, c & 1);
-            if (!ok) break;
+            if (!wait.ok) break;
             release(q, KP);
             q += KP;
-            if (c + 3 == nch) mma_commit(xfree);
           }
         }
       }
     }
-    if (!ok) drain_mma(quit, 0);
+    if (!wait.ok) issue.drain(quit);
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- gates and rows out
     // half of the slot's hidden features (and of its tile's columns) for each warpgroup
@@ -246,19 +237,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t gcol = tmem + C::kGuCol + s * 128 + half * 32 + lane_off;
     uint8_t* H = Hs + s * C::kH;
-    bool ok = true;
+    WarpWaiter wait{p.status};
     uint32_t k = 0, gi = 0;
-    auto wait = [&](uint64_t* b, uint32_t parity) {
-      if (ok && !mbar_wait(b, parity)) {
-        ok = false;
-        record_device_error(p.status, kErrTimeout);
-      }
-      ok = __all_sync(0xffffffffu, ok);
-      if (ok) fence_after_sync();
-      return ok;
-    };
-    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x, ++gi) {
-      for (int c = NT == 2 ? 0 : s; ok && c < nch; c += 3 - NT, ++k) {
+    for (int64_t gr = blockIdx.x; wait.ok && gr < p.groups; gr += gridDim.x, ++gi) {
+      for (int c = NT == 2 ? 0 : s; wait.ok && c < nch; c += 3 - NT, ++k) {
         if (!wait(&gfull[s], k & 1)) break;
         uint32_t h[16];
 #pragma unroll
@@ -282,42 +264,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before_sync();
         mbar_arrive(&hfull[s]);
       }
-      if (!ok) break;
+      if (!wait.ok) break;
+      // rows out: X's place takes Y (+ X), and a TMA store each 64 columns (it leaves out the rows past n)
       const int t = NT == 2 ? s : 0;
       constexpr int CW = NT == 2 ? D / 2 : D / 4;  // columns of a warpgroup
-      const int col0 = (NT == 2 ? half : s * 2 + half) * CW;
-      const int64_t r = (gr * NT + t) * kRows + row;
-      const bool live = r < p.n;
-      if (!wait(&yfull[t], gi & 1)) break;
+      const int col0 = (NT == 2 ? half : s * 2 + half) * CW, blk = col0 / 64;
+      const int64_t r0 = (gr * NT + t) * kRows;
+      uint8_t* xb = Xs + (t * NB + blk) * kBlk;
+      if (!wait(xfull, gi & 1) || !wait(&yfull[t], gi & 1)) break;
 #pragma unroll
       for (int c = 0; c < CW; c += 16) {
         uint32_t y[16];
         ld16_issue(tmem + C::kYCol + t * D + lane_off + col0 + c, y);
-        uint4 x[2];
-        if (p.res && live) {
-          x[0] = ldg16(p.res + r * D + col0 + c);
-          x[1] = ldg16(p.res + r * D + col0 + c + 8);
-        }
+        uint4* x0 = reinterpret_cast<uint4*>(xb + sw128_offset(row, (col0 % 64 + c) * 2));
+        uint4* x1 = reinterpret_cast<uint4*>(xb + sw128_offset(row, (col0 % 64 + c) * 2 + 16));
+        float v[16];
+        unpack(p.residual ? *x0 : make_uint4(0u, 0u, 0u, 0u), v, __nv_bfloat16());
+        unpack(p.residual ? *x1 : make_uint4(0u, 0u, 0u, 0u), v + 8, __nv_bfloat16());
         ld_wait();
-        if (live) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v[8];
-            if (p.res) {
-              unpack(x[e], v, __nv_bfloat16());
-            } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(y[e * 8 + i]);
-            st16(p.Y + r * D + col0 + c + e * 8, pack(v, __nv_bfloat16()));
-          }
-        }
+        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(y[i]);
+        *x0 = pack(v, __nv_bfloat16());
+        *x1 = pack(v + 8, __nv_bfloat16());
       }
+      fence_async_smem();
       fence_before_sync();
       mbar_arrive(&yfree[t]);
+      uint64_t* sb = &sfull[(threadIdx.x - 128) / C::kStoreThreads];
+      mbar_arrive(sb);
+      if ((threadIdx.x - 128) % C::kStoreThreads == 0) {
+        if (mbar_wait(sb, gi & 1)) {
+          if (r0 < p.n) tma_store_2d(&tm_Y, xb, blk * 64, (int)r0);
+          bulk_commit();
+          bulk_wait_read();
+        } else {
+          record_device_error(p.status, kErrTimeout);
+        }
+        mbar_arrive(xfree);
+      }
+      __syncwarp();
     }
+    bulk_wait();
   }
   fence_before_sync();
   __syncthreads();
@@ -332,16 +319,17 @@ hg_status fwd_t(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaS
     HG_CUDA(cudaFuncSetAttribute(ffn_fwd_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     done = true;
   }
-  CUtensorMap tm_X, tm_G, tm_U, tm_W;
+  CUtensorMap tm_X, tm_G, tm_U, tm_W, tm_Y;
   HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
   HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, C::PR));
   HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, C::PR));
   HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, kHc));
+  HG_TRY(make_tmap_bf16(&tm_Y, Y, (uint64_t)n, D, kRows));
   FwdP p{n, (int)ceil_div(w->f, kHc), ceil_div(n, (int64_t)kRows * C::NT),
-         w->residual ? (const __nv_bfloat16*)X : nullptr, (__nv_bfloat16*)Y, device_status_ptr()};
+         w->residual != 0, device_status_ptr()};
   const int grid = (int)std::min<int64_t>(p.groups, kSms);
   return launch("ffn_fwd_tc", ffn_fwd_tc_kernel<D, kAct>, dim3(grid), dim3(kThreads), C::kSmem, s, tm_X, tm_G, tm_U,
-                tm_W, p);
+                tm_W, tm_Y, p);
 }
 
 template <int D>

@@ -23,4 +23,59 @@ hg_status ffn_bwd_tc(const hg_ffn_params* w, const void* X, int64_t n, const voi
                      void* scratch, cudaStream_t s);
 size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n);
 
+// A descriptor `bytes` further on.
+__device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+
+// The issuing warp: all its lanes run the role, so that descriptors are warp-uniform values, and one elected
+// lane issues.
+struct Issuer {
+  uint32_t lead;
+  __device__ __forceinline__ Issuer() {
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(lead));
+  }
+  // D[tmem] (+)= A[smem] B[smem]
+  __device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                      uint32_t accumulate) const {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+        : "memory");
+  }
+  // D += A[tmem] B[smem]: A's lane = row, each 32-bit column two bf16 along K
+  __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                         uint32_t accumulate) const {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+        : "memory");
+  }
+  __device__ __forceinline__ void commit(uint64_t* bar) const {
+    if (lead) tc::mma_commit(bar);
+  }
+  __device__ __forceinline__ void drain(uint64_t* bar) const {
+    if (lead) tc::drain_mma(bar, 0);
+  }
+};
+
+// A warp's bounded wait: false on every lane, and the give-up recorded, once it has run out on one of them.
+struct WarpWaiter {
+  int* status;
+  bool ok = true;
+  __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity) {
+    if (ok && !tc::mbar_wait(b, parity)) {
+      ok = false;
+      record_device_error(status, tc::kErrTimeout);
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    if (ok) tc::fence_after_sync();
+    return ok;
+  }
+};
+
 }  // namespace hg
