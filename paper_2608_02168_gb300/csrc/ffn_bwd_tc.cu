@@ -45,7 +45,6 @@ __device__ __forceinline__ void st8(uint32_t taddr, const uint32_t* r) {
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint8_t* align1024(uint8_t* p) {
   return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~uintptr_t(1023));
 }
@@ -251,8 +250,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           ld_wait();
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
-            float a0, a1, d0, d1;
-            gate_grad2<kAct>(__uint_as_float(g[e]), __uint_as_float(g[e + 1]), &a0, &a1, &d0, &d1);
+            float d0, d1;
+            const float a0 = gate_grad<kAct>(__uint_as_float(g[e]), &d0);
+            const float a1 = gate_grad<kAct>(__uint_as_float(g[e + 1]), &d1);
             const float y0 = __uint_as_float(h[e]), y1 = __uint_as_float(h[e + 1]);
             dg[(x + e) / 2] = pack2_bf16(y0 * __uint_as_float(u[e]) * d0, y1 * __uint_as_float(u[e + 1]) * d1);
             du[(x + e) / 2] = pack2_bf16(y0 * a0, y1 * a1);
@@ -507,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t hi[3][4], lo[3][4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          float a0, a1, d0, d1;
-          gate_grad2<kAct>(g[e], g[e + 1], &a0, &a1, &d0, &d1);
+          float d0, d1;
+          const float a0 = gate_grad<kAct>(g[e], &d0), a1 = gate_grad<kAct>(g[e + 1], &d1);
           const float v[3][2] = {{h[e] * u[e] * d0, h[e + 1] * u[e + 1] * d1},
                                  {h[e] * a0, h[e + 1] * a1},
                                  {a0 * u[e], a1 * u[e + 1]}};

@@ -45,7 +45,6 @@ struct FCfg {
   static constexpr int kX = NT * NB * kBlk;
   static constexpr int kH = kRows * 128;
   static constexpr int kSmem = kX + NS * kPiece + 2 * kH + 512 + 1024;
-  static constexpr int kStoreThreads = D == 64 ? 256 : 128;  // that fill one 64-column block of the rows out
   static constexpr uint32_t kYCol = 0, kGuCol = 256;         // tensor memory: Y (tile x at x D), slots of 128
 };
 
@@ -71,8 +70,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* Hs = Ws + NS * C::kPiece;
   uint64_t* bars = reinterpret_cast<uint64_t*>(Hs + 2 * C::kH);
   uint64_t *wfull = bars, *wfree = bars + NS, *xfull = bars + 2 * NS, *xfree = xfull + 1, *gfull = xfull + 2,
-           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yfree = yfull + 2, *sfull = yfree + 2,
-           *quit = sfull + 4;
+           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yready = yfull + 2, *sfull = yready + 2,
+           *sdone = sfull + 2, *quit = sdone + 2;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -81,15 +80,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&wfree[i], 1);
     }
     mbar_init(xfull, 1);
-    mbar_init(xfree, 512 / C::kStoreThreads);
+    mbar_init(xfree, p.residual ? 513 : 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&gfull[i], 1);
       mbar_init(&hfull[i], 256);
       mbar_init(&hfree[i], 1);
       mbar_init(&yfull[i], 1);
-      mbar_init(&yfree[i], NT == 2 ? 256 : 512);
+      mbar_init(&yready[i], NT == 2 ? 256 : 512);
+      mbar_init(&sfull[i], 256);
+      mbar_init(&sdone[i], 1);
     }
-    for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads);
     mbar_init(quit, 1);
     fence_mbar_init();
   }
@@ -177,12 +177,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto down = [&](uint32_t qd, int c, int s) {
       const int t = NT == 2 ? s : 0;
       if (!wait(&hfull[s], hk[s] & 1)) return;
-      if (c == 0 && gi >= 1 && !wait(&yfree[t], (gi - 1) & 1)) return;
+      if (c == 0 && !wait(&yready[t], gi & 1)) return;
       ++hk[s];
       const uint64_t w = desc_at(wd, qd % NS * C::kPiece), h = desc_at(hd, s * C::kH);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        issue.mma(tmem + C::kYCol + t * D, desc_at(h, j * 32), desc_at(w, j * 2048), id_y, (c > 0 || j > 0) ? 1u : 0u);
+        issue.mma(tmem + C::kYCol + t * D, desc_at(h, j * 32), desc_at(w, j * 2048), id_y, (c > 0 || j > 0 || p.residual) ? 1u : 0u);
       issue.commit(&hfree[s]);
       if (c == nch - 1) issue.commit(&yfull[t]);
     };
@@ -196,6 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait.ok) break;
         release(q, KP);
         q += KP;
+        if (nch == 1) issue.commit(xfree);
         for (int c = 0; wait.ok && c < nch; ++c) {
           const bool more = c + 1 < nch;
           if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
@@ -206,6 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!wait.ok) break;
           release(q, 1 + (more ? KP : 0));
           q += 1 + (more ? KP : 0);
+          if (c + 2 == nch) issue.commit(xfree);
         }
       } else {
         for (int c = 0; wait.ok && c < 2 && c < nch; ++c) {
@@ -214,6 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           release(q, KP);
           q += KP;
         }
+        if (wait.ok && nch <= 2) issue.commit(xfree);
         for (int c = 0; wait.ok && c < nch; ++c) {
           if (!wait(&wfull[q % NS], (q / NS) & 1)) break;
           down(q, c, c & 1);
@@ -225,6 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!wait.ok) break;
             release(q, KP);
             q += KP;
+            if (c + 3 == nch) issue.commit(xfree);
           }
         }
       }
@@ -239,24 +243,47 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* H = Hs + s * C::kH;
     WarpWaiter wait{p.status};
     uint32_t k = 0, gi = 0;
+    // the slot's columns of Y: NT == 2 all of its tile's, else half of the tile's; 64 of them a round
+    const int t = NT == 2 ? s : 0;
+    constexpr int RN = (NT == 2 ? D : D / 2) / 64;
+    const int blk0 = NT == 2 ? 0 : s * RN;
+    const uint32_t ycol = tmem + C::kYCol + t * D + lane_off + blk0 * 64 + half * 32;
+    uint32_t rounds = 0;
     for (int64_t gr = blockIdx.x; wait.ok && gr < p.groups; gr += gridDim.x, ++gi) {
-      for (int c = NT == 2 ? 0 : s; wait.ok && c < nch; c += 3 - NT, ++k) {
-        if (!wait(&gfull[s], k & 1)) break;
-        uint32_t h[16];
+      if (p.residual) {  // Y starts at X, so that X's place can take the next group while this one is finished
+        if (!wait(xfull, gi & 1)) break;
 #pragma unroll
-        for (int x = 0; x < 32; x += 16) {
-          uint32_t g[16], u[16];
-          ld16_issue(gcol + x, g);
-          ld16_issue(gcol + 64 + x, u);
-          ld_wait();
+        for (int b = 0; b < RN; ++b) {
+          const uint8_t* xb = Xs + (t * NB + blk0 + b) * kBlk;
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            float a0, a1;
-            gate2<kAct>(__uint_as_float(g[e]), __uint_as_float(g[e + 1]), &a0, &a1);
-            h[(x + e) / 2] = pack2_bf16(a0 * __uint_as_float(u[e]), a1 * __uint_as_float(u[e + 1]));
+          for (int x = 0; x < 32; x += 16) {
+            float v[16];
+            unpack(ld16(xb + sw128_offset(row, half * 64 + x * 2)), v, __nv_bfloat16());
+            unpack(ld16(xb + sw128_offset(row, half * 64 + x * 2 + 16)), v + 8, __nv_bfloat16());
+            st16_issue(ycol + b * 64 + x, v);
           }
         }
+        st_wait();
+        mbar_arrive(xfree);
+      }
+      fence_before_sync();
+      mbar_arrive(&yready[t]);
+      bool first = rounds > 0;  // the rows of the group before leave through H's place
+      for (int c = NT == 2 ? 0 : s; wait.ok && c < nch; c += 3 - NT, ++k) {
+        if (!wait(&gfull[s], k & 1)) break;
+        uint32_t g[32], u[32], h[16];
+        ld16_issue(gcol, reinterpret_cast<uint32_t(&)[16]>(g[0]));
+        ld16_issue(gcol + 64, reinterpret_cast<uint32_t(&)[16]>(u[0]));
+        ld16_issue(gcol + 16, reinterpret_cast<uint32_t(&)[16]>(g[16]));
+        ld16_issue(gcol + 80, reinterpret_cast<uint32_t(&)[16]>(u[16]));
+        ld_wait();
+#pragma unroll
+        for (int e = 0; e < 32; e += 2)
+          h[e / 2] = pack2_bf16(gate<kAct>(__uint_as_float(g[e])) * __uint_as_float(u[e]),
+                                gate<kAct>(__uint_as_float(g[e + 1])) * __uint_as_float(u[e + 1]));
         if (k >= 1 && !wait(&hfree[s], (k - 1) & 1)) break;
+        if (first && !wait(&sdone[s], (rounds - 1) & 1)) break;
+        first = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           st16(H + sw128_offset(row, half * 64 + e * 16), make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]));
@@ -265,44 +292,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(&hfull[s]);
       }
       if (!wait.ok) break;
-      // rows out: X's place takes Y (+ X), and a TMA store each 64 columns (it leaves out the rows past n)
-      const int t = NT == 2 ? s : 0;
-      constexpr int CW = NT == 2 ? D / 2 : D / 4;  // columns of a warpgroup
-      const int col0 = (NT == 2 ? half : s * 2 + half) * CW, blk = col0 / 64;
+      // rows out, 64 columns a round: through H's place, and by a TMA store (it leaves out the rows past n)
       const int64_t r0 = (gr * NT + t) * kRows;
-      uint8_t* xb = Xs + (t * NB + blk) * kBlk;
-      if (!wait(xfull, gi & 1) || !wait(&yfull[t], gi & 1)) break;
-#pragma unroll
-      for (int c = 0; c < CW; c += 16) {
-        uint32_t y[16];
-        ld16_issue(tmem + C::kYCol + t * D + lane_off + col0 + c, y);
-        uint4* x0 = reinterpret_cast<uint4*>(xb + sw128_offset(row, (col0 % 64 + c) * 2));
-        uint4* x1 = reinterpret_cast<uint4*>(xb + sw128_offset(row, (col0 % 64 + c) * 2 + 16));
-        float v[16];
-        unpack(p.residual ? *x0 : make_uint4(0u, 0u, 0u, 0u), v, __nv_bfloat16());
-        unpack(p.residual ? *x1 : make_uint4(0u, 0u, 0u, 0u), v + 8, __nv_bfloat16());
+      if (!wait(&yfull[t], gi & 1)) break;
+#pragma unroll 1
+      for (int b = 0; b < RN; ++b, ++rounds) {
+        uint32_t y[32];
+        ld16_issue(ycol + b * 64, reinterpret_cast<uint32_t(&)[16]>(y[0]));
+        ld16_issue(ycol + b * 64 + 16, reinterpret_cast<uint32_t(&)[16]>(y[16]));
         ld_wait();
+        // a slot without a chunk (one chunk, odd slot) has not waited for its last rows to leave yet
+        if ((b > 0 || first) && !wait(&sdone[s], (rounds - 1) & 1)) break;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(y[i]);
-        *x0 = pack(v, __nv_bfloat16());
-        *x1 = pack(v + 8, __nv_bfloat16());
-      }
-      fence_async_smem();
-      fence_before_sync();
-      mbar_arrive(&yfree[t]);
-      uint64_t* sb = &sfull[(threadIdx.x - 128) / C::kStoreThreads];
-      mbar_arrive(sb);
-      if ((threadIdx.x - 128) % C::kStoreThreads == 0) {
-        if (mbar_wait(sb, gi & 1)) {
-          if (r0 < p.n) tma_store_2d(&tm_Y, xb, blk * 64, (int)r0);
-          bulk_commit();
-          bulk_wait_read();
-        } else {
-          record_device_error(p.status, kErrTimeout);
+        for (int e = 0; e < 4; ++e)
+          st16(H + sw128_offset(row, half * 64 + e * 16), pack(reinterpret_cast<float*>(y) + 8 * e, __nv_bfloat16()));
+        fence_async_smem();
+        mbar_arrive(&sfull[s]);
+        if ((threadIdx.x - 128) % 256 == 0) {
+          if (mbar_wait(&sfull[s], rounds & 1)) {
+            if (r0 < p.n) tma_store_2d(&tm_Y, H, (blk0 + b) * 64, (int)r0);
+            bulk_commit();
+            bulk_wait_read();
+          } else {
+            record_device_error(p.status, kErrTimeout);
+          }
+          mbar_arrive(&sdone[s]);
         }
-        mbar_arrive(xfree);
+        __syncwarp();
       }
-      __syncwarp();
     }
     bulk_wait();
   }
