@@ -16,16 +16,14 @@ __device__ __forceinline__ float gate_rcp(float x) {
   return y;
 }
 
-// The logistic function as s r and its complement as t r, from s = e^(z / 2), t = e^(-z / 2), r = 1 / (s + t): the
-// exponents are halved, so a gate as small as the smallest fp32 number comes out as it is and none of the factors
-// leaves the range.  (Above z = 277 both are at their limits.)
+// The logistic function of z as s (s r) and its complement as r, from s = e^(z / 2), r = 1 / (1 + s^2): the
+// exponent is halved, so a gate as small as the smallest fp32 number comes out as it is.  Above z = 41 the
+// logistic function is 1 to the last bit.
 struct Logistic {
-  float s, t, r;
+  float s, r;
   __device__ __forceinline__ explicit Logistic(float half_log2) {
-    const float h = fminf(half_log2, 100.f);
-    s = gate_ex2(h);
-    t = gate_ex2(-h);
-    r = gate_rcp(s + t);
+    s = gate_ex2(fminf(half_log2, 30.f));
+    r = gate_rcp(fmaf(s, s, 1.f));
   }
 };
 
@@ -46,7 +44,7 @@ __device__ __forceinline__ float gate(float x) {
   if (kAct == HG_ACT_RELU) return x > 0.f ? x : 0.f;
   if (kAct == HG_ACT_NONE) return x;
   const Logistic l(gate_half<kAct>(x));
-  return x * l.s * l.r;
+  return (x * l.s) * (l.s * l.r);
 }
 
 // The gate's value and derivative.
@@ -61,11 +59,11 @@ __device__ __forceinline__ float gate_grad(float x, float* d) {
     return x;
   }
   const Logistic l(gate_half<kAct>(x));
-  const float p = l.s * l.r;
-  float k = x * (l.t * l.r);
+  const float sr = l.s * l.r, p = l.s * sr;
+  float k = x * l.r;
   if (kAct == HG_ACT_GELU_TANH) k *= fmaf(x * x, 3.f * 0.044715f * 1.5957691216057308f, 1.5957691216057308f);
   *d = fmaf(p, k, p);
-  return x * p;
+  return (x * l.s) * sr;
 }
 
 }  // namespace hg
