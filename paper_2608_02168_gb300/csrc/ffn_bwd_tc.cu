@@ -13,8 +13,10 @@
 // X, dY and a chunk's weights fill the shared memory, so dG and dU go back to tensor memory, as the products'
 // first operand.
 //
-// ffn_wgrad_tc: a CTA owns a chunk of hidden features, keeps its weights in shared memory and its gradients
-// in tensor memory, and takes a share of the row tiles.  The gradients are fp32 results, so dG, dU and H enter
+// ffn_wgrad_tc: a CTA owns 32 hidden features, keeps their weights in shared memory and takes a share of the row
+// tiles.  At d <= 128 two row tiles fit, and a tile's hidden rows are formed while the gates of the one before are
+// computed and multiplied.  (64 hidden features would use the tensor pipe better, but leave room for one tile: 200k rows, d =
+// 128: 278 us.)  The gradients are fp32 results, so dG, dU and H enter
 // as sums of two bf16 numbers (16 bits): one rounding would leave them with three digits.  The tensor pipe's own
 // additions cut their results short, which shrinks a long sum (3.8e-5 of it over 16000 rows): each tile's products
 // are therefore drained into registers and added there.  The shares' sums are added in order.  With d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the
@@ -48,20 +50,6 @@ __device__ __forceinline__ void st8(uint32_t taddr, const uint32_t* r) {
 __device__ __forceinline__ uint8_t* align1024(uint8_t* p) {
   return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~uintptr_t(1023));
 }
-
-// A bounded wait of a role: false, and the give-up recorded once, when it runs out.
-struct Waiter {
-  int* status;
-  bool ok = true;
-  __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity) {
-    if (ok && !mbar_wait(b, parity)) {
-      ok = false;
-      record_device_error(status, kErrTimeout);
-    }
-    if (ok) fence_after_sync();
-    return ok;
-  }
-};
 
 // ---------------------------------------------------------------------------------------------
 // dX
@@ -123,13 +111,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(xfull, 1);
     mbar_init(xfree, 512 / C::kStoreThreads);
-    for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads);
+    for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads / 32);
     mbar_init(&gfull[0], 1);
     mbar_init(&gfull[1], 1);
-    mbar_init(ofull, SLOTS == 2 ? 256 : 512);
+    mbar_init(ofull, SLOTS == 2 ? 8 : 16);
     mbar_init(ofree, 1);
     mbar_init(yfull, 1);
-    mbar_init(yfree, 512);
+    mbar_init(yfree, 16);
     mbar_init(quit, 1);
     fence_mbar_init();
   }
@@ -276,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           fence_async_smem();
         }
         fence_before_sync();
-        mbar_arrive(ofull);
+        warp_arrive(ofull);
       }
       if (!wait.ok) break;
       // rows out: dY's place takes dX (+ dY), and a TMA store each 64 columns (it leaves out the rows past n)
@@ -301,9 +289,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       fence_async_smem();
       fence_before_sync();
-      mbar_arrive(yfree);
+      warp_arrive(yfree);
       uint64_t* sb = &sfull[(threadIdx.x - 128) / C::kStoreThreads];
-      mbar_arrive(sb);
+      warp_arrive(sb);
       if ((threadIdx.x - 128) % C::kStoreThreads == 0) {
         if (mbar_wait(sb, ti & 1)) {
           tma_store_2d(&tm_dX, yb, col0 / 64 * 64, (int)(tile * kRows));
@@ -328,18 +316,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------------------------
 template <int D>
 struct WgCfg {
-  static constexpr int HC = D == 256 ? 32 : 64;
+  static constexpr int HC = 32;                       // hidden features of a CTA
   static constexpr int NB = D / 64;
   static constexpr int MB = D == 256 ? 2 : 1;         // 128-row blocks of the gradients
-  static constexpr int XS = D == 64 ? 2 : 1;          // row tiles in flight
+  static constexpr int XS = D == 256 ? 1 : 2;         // row tiles in shared memory
   static constexpr int kX = NB * kBlk;
-  static constexpr int N2 = 2 * HC;                   // columns of [dG | dU] and of [H hi | H lo]
-  static constexpr int OB = N2 / 64;                  // their 64-column blocks
+  static constexpr int N2 = 2 * HC;                   // columns of [G | U], of [dG | dU] and of [H hi | H lo]
   static constexpr int kW = N2 * D * 2, kDown = HC * D * 2;
-  static constexpr int kOps = OB * kBlk;
-  static constexpr int kSmem = XS * 2 * kX + kW + kDown + 3 * kOps + 512 + 1024;
-  // tensor memory: gradients ([dG | dU] of each block, then [H hi | H lo]), then [G | U | dH]
-  static constexpr uint32_t kAcc2 = MB * N2, kHid = 2 * MB * N2;
+  static constexpr int kSmem = XS * 2 * kX + kW + kDown + 3 * kBlk + 512 + 1024;
+  // tensor memory: gradients ([dG | dU] of each block, then [H hi | H lo]), then two slots of [G | U | dH]
+  static constexpr uint32_t kAcc2 = MB * N2, kHid = 2 * MB * N2, kHidCols = N2 + HC;
+  static constexpr int PC = MB == 2 ? 6 : 3;          // pieces of 8 columns whose sums a warpgroup keeps
 };
 
 struct WgP {
@@ -361,8 +348,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* Ws = Xs + XS * 2 * C::kX;
   uint8_t* Ds = Ws + C::kW;
   uint8_t* Os = Ds + C::kDown;                     // [dG | dU] hi, lo, [H hi | H lo]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + 3 * C::kOps);
-  uint64_t *wfull = bars, *xfull = bars + 1, *xfree = xfull + 2, *gfull = xfree + 2, *ofull = gfull + 1,
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + 3 * kBlk);
+  uint64_t *wfull = bars, *xfull = bars + 1, *xfree = xfull + 2, *gfull = xfree + 2, *ofull = gfull + 2,
            *ofree = ofull + 1, *quit = ofree + 1;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -372,8 +359,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&xfull[i], 1);
       mbar_init(&xfree[i], 1);
     }
-    mbar_init(gfull, 1);
-    mbar_init(ofull, 512);
+    mbar_init(&gfull[0], 1);
+    mbar_init(&gfull[1], 1);
+    mbar_init(ofull, 16);
     mbar_init(ofree, 1);
     mbar_init(quit, 1);
     fence_mbar_init();
@@ -418,23 +406,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t od = desc_sw128(smem_u32(Os), kBlk, 1024);
     constexpr uint32_t id_gu = idesc_bf16(128, N2, false, false), id_h = idesc_bf16(128, HC, false, false),
                        id_w = idesc_bf16(128, N2, true, true);
-    wait(wfull, 0);
-    for (int i = 0; wait.ok && i < count; ++i) {
-      const int s = i % XS;
-      if (!wait(&xfull[s], (i / XS) & 1)) break;
-      if (i >= 1 && !wait(ofull, (i - 1) & 1)) break;  // the hidden sums of the tile before were read
-      const uint64_t x = desc_at(xd, s * 2 * C::kX), xm = desc_at(xmd, s * 2 * C::kX);
-      const uint32_t hid = tmem + C::kHid;
+    // [G | U | dH] of tile i into slot i & 1, whose last contents were read before the operands of tile i - 2 were full
+    auto hidden = [&](int i) {
+      if (!wait(&xfull[i % XS], (i / XS) & 1)) return;
+      const uint64_t x = desc_at(xd, i % XS * 2 * C::kX);
+      const uint32_t hid = tmem + C::kHid + (i & 1) * C::kHidCols;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
         issue.mma(hid, desc_at(x, (j >> 2) * kBlk + (j & 3) * 32), desc_at(wd, (j >> 2) * (N2 * 128) + (j & 3) * 32),
-                 id_gu, j > 0 ? 1u : 0u);
+                  id_gu, j > 0 ? 1u : 0u);
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
         issue.mma(hid + N2, desc_at(x, C::kX + (j >> 2) * kBlk + (j & 3) * 32),
-                 desc_at(dd, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
-      issue.commit(gfull);
+                  desc_at(dd, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
+      issue.commit(&gfull[i & 1]);
+    };
+    if (wait(wfull, 0)) hidden(0);
+    for (int i = 0; wait.ok && i < count; ++i) {
+      // the next tile's hidden rows go ahead where it has a place of its own
+      if (XS == 2 && i + 1 < count) hidden(i + 1);
       if (!wait(ofull, i & 1)) break;
+      const uint64_t xm = desc_at(xmd, i % XS * 2 * C::kX);
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         // d = 64: X and dY side by side are the 128 rows of both gradients
@@ -443,93 +435,90 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int part = 0; part < 2; ++part)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            issue.mma(tmem + m * N2, desc_at(xm, ax + j * 2048), desc_at(od, part * C::kOps + j * 2048), id_w, (part > 0 || j > 0) ? 1u : 0u);
+            issue.mma(tmem + m * N2, desc_at(xm, ax + j * 2048), desc_at(od, part * kBlk + j * 2048), id_w,
+                      (part > 0 || j > 0) ? 1u : 0u);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          issue.mma(tmem + C::kAcc2 + m * N2, desc_at(xm, ay + j * 2048), desc_at(od, 2 * C::kOps + j * 2048), id_w, j > 0 ? 1u : 0u);
+          issue.mma(tmem + C::kAcc2 + m * N2, desc_at(xm, ay + j * 2048), desc_at(od, 2 * kBlk + j * 2048), id_w,
+                    j > 0 ? 1u : 0u);
       }
-      issue.commit(&xfree[s]);
+      issue.commit(&xfree[i % XS]);
       issue.commit(ofree);
+      if (XS == 1 && i + 1 < count) hidden(i + 1);
     }
     if (!wait.ok) issue.drain(quit);
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-    constexpr int HW = HC / 4;  // hidden features of a warpgroup
+    constexpr int HW = HC / 4, PC = C::PC;  // hidden features of a warpgroup
     const int h0 = wg * HW;
-    const uint32_t hid = tmem + C::kHid + lane_off;
     WarpWaiter wait{p.status};
-    // 16 bytes (8 features from column c of an operand block pair) of this row
-    auto put = [&](uint8_t* o, int c, const uint32_t* v) {
-      st16(o + (c >> 6) * kBlk + sw128_offset(row, (c & 63) * 2), make_uint4(v[0], v[1], v[2], v[3]));
-    };
-    // This thread's 48 sums, three pieces of 16 columns of its row.  The twelve pieces of a row (at d = 256: six
-    // of each block of 128 rows) are first those of [dG | dU], then H's, whose two halves are added.
-    float sum[48];
+    // This thread's sums: PC pieces of 8 columns of its row.  The twelve pieces of a row of a block are first those of
+    // [dG | dU], then H's, whose two halves are added; at d = 256 two warpgroups share a block.
+    float sum[PC * 8];
 #pragma unroll
-    for (int e = 0; e < 48; ++e) sum[e] = 0.f;
+    for (int e = 0; e < PC * 8; ++e) sum[e] = 0.f;
     const int m = MB == 2 ? wg >> 1 : 0;
     auto place = [&](int b, bool* pair) -> uint32_t {  // columns of piece b, from the block's first
-      const int gb = (MB == 2 ? wg & 1 : wg) * 3 + b, first = N2 / 16;
+      const int gb = (MB == 2 ? wg & 1 : wg) * PC + b, first = N2 / 8;
       *pair = gb >= first;
-      return gb < first ? gb * 16 : C::kAcc2 + (gb - first) * 16;
+      return gb < first ? gb * 8 : C::kAcc2 + (gb - first) * 8;
     };
     auto drain = [&]() {
 #pragma unroll
-      for (int b = 0; b < 3; ++b) {
+      for (int b = 0; b < PC; ++b) {
         bool pair;
         const uint32_t col = tmem + lane_off + m * N2 + place(b, &pair);
-        uint32_t v[16];
-        ld16_issue(col, v);
-        ld_wait();
+        float v[8];
+        tmem_ld8(col, v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum[b * 16 + e] += __uint_as_float(v[e]);
+        for (int e = 0; e < 8; ++e) sum[b * 8 + e] += v[e];
         if (pair) {
-          ld16_issue(col + HC, v);
-          ld_wait();
+          tmem_ld8(col + HC, v);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum[b * 16 + e] += __uint_as_float(v[e]);
+          for (int e = 0; e < 8; ++e) sum[b * 8 + e] += v[e];
         }
       }
     };
     for (int i = 0; i < count; ++i) {
-      if (!wait(gfull, i & 1)) break;
+      if (!wait(&gfull[i & 1], (i >> 1) & 1)) break;
+      const uint32_t hid = tmem + C::kHid + (i & 1) * C::kHidCols + lane_off + h0;
+      float g[8], u[8], h[8];
+      tmem_ld8(hid, g);
+      tmem_ld8(hid + HC, u);
+      tmem_ld8(hid + N2, h);
+      uint32_t hi[3][4], lo[3][4];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        float d0, d1;
+        const float a0 = gate_grad<kAct>(g[e], &d0), a1 = gate_grad<kAct>(g[e + 1], &d1);
+        const float v[3][2] = {{h[e] * u[e] * d0, h[e + 1] * u[e + 1] * d1},
+                               {h[e] * a0, h[e + 1] * a1},
+                               {a0 * u[e], a1 * u[e + 1]}};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const uint32_t w = pack2_bf16(v[k][0], v[k][1]);
+          hi[k][e / 2] = w;
+          lo[k][e / 2] = pack2_bf16(v[k][0] - __uint_as_float(w << 16), v[k][1] - __uint_as_float(w & 0xffff0000u));
+        }
+      }
       if (i >= 1) {
         if (!wait(ofree, (i - 1) & 1)) break;
         drain();
       }
-#pragma unroll
-      for (int x = 0; x < HW; x += 8) {
-        float g[8], u[8], h[8];
-        tmem_ld8(hid + h0 + x, g);
-        tmem_ld8(hid + HC + h0 + x, u);
-        tmem_ld8(hid + N2 + h0 + x, h);
-        uint32_t hi[3][4], lo[3][4];
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          float d0, d1;
-          const float a0 = gate_grad<kAct>(g[e], &d0), a1 = gate_grad<kAct>(g[e + 1], &d1);
-          const float v[3][2] = {{h[e] * u[e] * d0, h[e + 1] * u[e + 1] * d1},
-                                 {h[e] * a0, h[e + 1] * a1},
-                                 {a0 * u[e], a1 * u[e + 1]}};
-#pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const uint32_t w = pack2_bf16(v[k][0], v[k][1]);
-            hi[k][e / 2] = w;
-            lo[k][e / 2] = pack2_bf16(v[k][0] - __uint_as_float(w << 16), v[k][1] - __uint_as_float(w & 0xffff0000u));
-          }
-        }
-        const int c = h0 + x;
-        put(Os, c, hi[0]);
-        put(Os, HC + c, hi[1]);
-        put(Os + C::kOps, c, lo[0]);
-        put(Os + C::kOps, HC + c, lo[1]);
-        put(Os + 2 * C::kOps, c, hi[2]);
-        put(Os + 2 * C::kOps, HC + c, lo[2]);
-      }
+      // 16 bytes of this row: feature h0 on, of the first or the second half of the columns
+      auto put = [&](uint8_t* o, int c, const uint32_t* v) {
+        st16(o + sw128_offset(row, (c + h0) * 2), make_uint4(v[0], v[1], v[2], v[3]));
+      };
+      put(Os, 0, hi[0]);
+      put(Os, HC, hi[1]);
+      put(Os + kBlk, 0, lo[0]);
+      put(Os + kBlk, HC, lo[1]);
+      put(Os + 2 * kBlk, 0, hi[2]);
+      put(Os + 2 * kBlk, HC, lo[2]);
       fence_async_smem();
       fence_before_sync();
-      mbar_arrive(ofull);
+      warp_arrive(ofull);
     }
     // the sums of this share: part[split] = [dW_gate d x f | dW_up d x f | dW_down f x d]
     if (wait.ok && wait(ofree, (count - 1) & 1)) {
@@ -538,25 +527,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t df = (int64_t)D * p.f;
       const int dr = m * 128 + row;
 #pragma unroll
-      for (int b = 0; b < 3; ++b) {
+      for (int b = 0; b < PC; ++b) {
         bool pair;
         const int col = (int)place(b, &pair);
         if (!pair) {
           const int hcol = chunk * HC + col % HC;
-          if (dr < D) {
+          if (dr < D && hcol < p.f) {
             float* o = out + (col / HC) * df + (int64_t)dr * p.f + hcol;
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-              if (hcol + e < p.f) st16(o + e, pack(sum + b * 16 + e, 0.f));
+            st16(o, pack(sum + b * 8, 0.f));
+            st16(o + 4, pack(sum + b * 8 + 4, 0.f));
           }
         } else {
           const int r = D == 64 ? row - 64 : dr;  // d = 64: the lower half is dY's
           const int hcol = chunk * HC + col - (int)C::kAcc2;
-          if (r >= 0) {
+          if (r >= 0 && hcol < p.f) {
             float* o = out + 2 * df + (int64_t)hcol * D + r;
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (hcol + e < p.f) o[(int64_t)e * D] = sum[b * 16 + e];
+            for (int e = 0; e < 8; ++e) o[(int64_t)e * D] = sum[b * 8 + e];
           }
         }
       }
@@ -643,11 +630,11 @@ hg_status dx_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
                 dim3(kThreads), C::kSmem, s, tm_X, tm_dY, tm_G, tm_U, tm_W, tm_dX, p);
 }
 
-int hidden_chunk(int d) { return d == 256 ? WgCfg<256>::HC : WgCfg<128>::HC; }
+constexpr int kWgHc = WgCfg<128>::HC;
 
 // Shares of the row tiles: the count that makes the longest SM's work shortest (whole waves of chunks x shares).
-int wg_splits(int64_t n, int d, int f) {
-  const int64_t tiles = ceil_div(n, kRows), chunks = ceil_div(f, hidden_chunk(d));
+int wg_splits(int64_t n, int f) {
+  const int64_t tiles = ceil_div(n, kRows), chunks = ceil_div(f, kWgHc);
   int64_t best = 1, best_cost = INT64_MAX;
   for (int64_t sp = 1; sp <= std::min<int64_t>(tiles, kSms); ++sp) {
     // a CTA's fixed cost (weights in, gradients out) is about four tiles' time
@@ -666,9 +653,8 @@ struct WgLayout {
 };
 void carve_wg(void* scratch, const hg_ffn_params* w, int64_t n, WgLayout* L, size_t* bytes) {
   Carve k(scratch);
-  const int hc = hidden_chunk(w->d);
-  L->Wt = k.take<__nv_bfloat16>((size_t)ceil_div(w->f, hc) * 2 * hc * w->d);
-  L->part = k.take<float>((size_t)wg_splits(std::max<int64_t>(n, 1), w->d, w->f) * 3 * w->d * w->f);
+  L->Wt = k.take<__nv_bfloat16>((size_t)ceil_div(w->f, kWgHc) * 2 * kWgHc * w->d);
+  L->part = k.take<float>((size_t)wg_splits(std::max<int64_t>(n, 1), w->f) * 3 * w->d * w->f);
   if (bytes) *bytes = k.used;
 }
 
@@ -681,7 +667,7 @@ hg_status wg_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
     HG_CUDA(cudaFuncSetAttribute(ffn_wgrad_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     done = true;
   }
-  const int chunks = (int)ceil_div(w->f, C::HC), splits = wg_splits(n, D, w->f);
+  const int chunks = (int)ceil_div(w->f, C::HC), splits = wg_splits(n, w->f);
   HG_TRY(launch("ffn_pack_weights", ffn_pack_weights, dim3(chunks * C::HC / 32, D / 32, 2), dim3(256), 0, s,
                 (const __nv_bfloat16*)w->W_gate, (const __nv_bfloat16*)w->W_up, D, w->f, C::HC, (__nv_bfloat16*)L.Wt));
   CUtensorMap tm_X, tm_dY, tm_Wt, tm_W;

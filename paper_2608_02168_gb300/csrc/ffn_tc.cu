@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t gk[2] = {0, 0};  // [G | U] of each slot so far
     // tile t times the chunk's pieces q .. q + KP - 1 into slot s, once the gates have read what it held
     auto gu = [&](int t, int s) {
-      if (gk[s] >= 1 && !wait(&gfree[s], (gk[s] - 1) & 1)) return;
+      if (NT == 2 && gk[s] >= 1 && !wait(&gfree[s], (gk[s] - 1) & 1)) return;
 #pragma unroll
       for (int k = 0; k < KP; ++k) {
         if (!wait(&wfull[(q + k) % NS], ((q + k) / NS) & 1)) return;
@@ -260,8 +260,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         ld16_issue(gcol + 16, reinterpret_cast<uint32_t(&)[16]>(g[16]));
         ld16_issue(gcol + 80, reinterpret_cast<uint32_t(&)[16]>(u[16]));
         ld_wait();
-        fence_before_sync();
-        mbar_arrive(&gfree[s]);  // the next [G | U] runs while these gates are computed
+        if (NT == 2) {  // the next [G | U] runs while these gates are computed
+          fence_before_sync();
+          mbar_arrive(&gfree[s]);
+        }
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
           h[e / 2] = pack2_bf16(gate<kAct>(__uint_as_float(g[e])) * __uint_as_float(u[e]),

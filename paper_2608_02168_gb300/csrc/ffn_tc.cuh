@@ -36,6 +36,12 @@ __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.
 // A descriptor `bytes` further on.
 __device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
 
+// One arrival for the warp, after what all its lanes did before.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) tc::mbar_arrive(bar);
+}
+
 // The issuing warp: all its lanes run the role, so that descriptors are warp-uniform values, and one elected
 // lane issues.
 struct Issuer {
@@ -70,6 +76,20 @@ struct Issuer {
   }
   __device__ __forceinline__ void drain(uint64_t* bar) const {
     if (lead) tc::drain_mma(bar, 0);
+  }
+};
+
+// A bounded wait of a role: false, and the give-up recorded once, when it runs out.
+struct Waiter {
+  int* status;
+  bool ok = true;
+  __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity) {
+    if (ok && !tc::mbar_wait(b, parity)) {
+      ok = false;
+      record_device_error(status, tc::kErrTimeout);
+    }
+    if (ok) tc::fence_after_sync();
+    return ok;
   }
 };
 
