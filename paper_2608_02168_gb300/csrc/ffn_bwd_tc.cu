@@ -13,10 +13,8 @@
 // X, dY and a chunk's weights fill the shared memory, so dG and dU go back to tensor memory, as the products'
 // first operand.
 //
-// ffn_wgrad_tc: a CTA owns 32 hidden features, keeps their weights in shared memory and takes a share of the row
-// tiles.  At d <= 128 two row tiles fit, and a tile's hidden rows are formed while the gates of the one before are
-// computed and multiplied.  (64 hidden features would use the tensor pipe better, but leave room for one tile: 200k rows, d =
-// 128: 278 us.)  The gradients are fp32 results, so dG, dU and H enter
+// ffn_wgrad_tc: a CTA owns a chunk of hidden features, keeps its weights in shared memory and its gradients
+// in tensor memory, and takes a share of the row tiles.  The gradients are fp32 results, so dG, dU and H enter
 // as sums of two bf16 numbers (16 bits): one rounding would leave them with three digits.  The tensor pipe's own
 // additions cut their results short, which shrinks a long sum (3.8e-5 of it over 16000 rows): each tile's products
 // are therefore drained into registers and added there.  The shares' sums are added in order.  With d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the
@@ -316,17 +314,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------------------------
 template <int D>
 struct WgCfg {
-  static constexpr int HC = 32;                       // hidden features of a CTA
+  static constexpr int HC = D == 256 ? 32 : 64;       // hidden features of a CTA
   static constexpr int NB = D / 64;
   static constexpr int MB = D == 256 ? 2 : 1;         // 128-row blocks of the gradients
-  static constexpr int XS = D == 256 ? 1 : 2;         // row tiles in shared memory
+  static constexpr int XS = D == 64 ? 2 : 1;          // row tiles in shared memory
   static constexpr int kX = NB * kBlk;
   static constexpr int N2 = 2 * HC;                   // columns of [G | U], of [dG | dU] and of [H hi | H lo]
   static constexpr int kW = N2 * D * 2, kDown = HC * D * 2;
-  static constexpr int kSmem = XS * 2 * kX + kW + kDown + 3 * kBlk + 512 + 1024;
-  // tensor memory: gradients ([dG | dU] of each block, then [H hi | H lo]), then two slots of [G | U | dH]
-  static constexpr uint32_t kAcc2 = MB * N2, kHid = 2 * MB * N2, kHidCols = N2 + HC;
-  static constexpr int PC = MB == 2 ? 6 : 3;          // pieces of 8 columns whose sums a warpgroup keeps
+  static constexpr int kOps = N2 / 64 * kBlk;
+  static constexpr int kSmem = XS * 2 * kX + kW + kDown + 3 * kOps + 512 + 1024;
+  // tensor memory: gradients ([dG | dU] of each block, then [H hi | H lo]), then [G | U | dH]
+  static constexpr uint32_t kAcc2 = MB * N2, kHid = 2 * MB * N2;
+  static constexpr int PC = 6;                        // pieces of 8 columns whose sums a warpgroup keeps
 };
 
 struct WgP {
@@ -348,19 +347,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* Ws = Xs + XS * 2 * C::kX;
   uint8_t* Ds = Ws + C::kW;
   uint8_t* Os = Ds + C::kDown;                     // [dG | dU] hi, lo, [H hi | H lo]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + 3 * kBlk);
-  uint64_t *wfull = bars, *xfull = bars + 1, *xfree = xfull + 2, *gfull = xfree + 2, *ofull = gfull + 2,
-           *ofree = ofull + 1, *quit = ofree + 1;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(Os + 3 * C::kOps);
+  uint64_t *wfull = bars, *xfull = bars + 1, *xfree = xfull + XS, *yfull = xfree + XS, *yfree = yfull + XS,
+           *gfull = yfree + XS, *ofull = gfull + 1, *ofree = ofull + 1, *quit = ofree + 1;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(wfull, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < XS; ++i) {
       mbar_init(&xfull[i], 1);
       mbar_init(&xfree[i], 1);
+      mbar_init(&yfull[i], 1);
+      mbar_init(&yfree[i], 1);
     }
-    mbar_init(&gfull[0], 1);
-    mbar_init(&gfull[1], 1);
+    mbar_init(gfull, 1);
     mbar_init(ofull, 16);
     mbar_init(ofree, 1);
     mbar_init(quit, 1);
@@ -382,21 +382,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       tma_load_2d(Ws + b * N2 * 128, &tm_Wt, b * 64, chunk * N2, wfull);
       tma_load_2d(Ds + b * HC * 128, &tm_W, b * 64, chunk * HC, wfull);
     }
-    uint32_t q = 0;
+    uint32_t q = 0, qy = 0;  // X and dY tiles asked for
     for (; q < (uint32_t)count; ++q) {
       const uint32_t s = q % XS;
-      if (q >= XS && !wait(&xfree[s], (q / XS - 1) & 1)) break;
-      mbar_expect_tx(&xfull[s], 2 * C::kX);
-      uint8_t* dst = Xs + s * 2 * C::kX;
       const int r = (int)((tile0 + q) * kRows);
-      for (int b = 0; b < NB; ++b) {
-        tma_load_2d(dst + b * kBlk, &tm_X, b * 64, r, &xfull[s]);
-        tma_load_2d(dst + C::kX + b * kBlk, &tm_dY, b * 64, r, &xfull[s]);
+      uint8_t* dst = Xs + s * 2 * C::kX;
+      if (q >= XS && !wait(&xfree[s], (q / XS - 1) & 1)) break;
+      mbar_expect_tx(&xfull[s], C::kX);
+      for (int b = 0; b < NB; ++b) tma_load_2d(dst + b * kBlk, &tm_X, b * 64, r, &xfull[s]);
+      if (q >= XS && !wait(&yfree[s], (q / XS - 1) & 1)) {
+        ++q;
+        break;
       }
+      mbar_expect_tx(&yfull[s], C::kX);
+      for (int b = 0; b < NB; ++b) tma_load_2d(dst + C::kX + b * kBlk, &tm_dY, b * 64, r, &yfull[s]);
+      ++qy;
     }
     if (!wait.ok) {
       mbar_wait(wfull, 0);
       drain_rounds(xfull, XS, q);
+      drain_rounds(yfull, XS, qy);
     }
   } else if (warp == 1) {
     const Issuer issue;
@@ -406,45 +411,42 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t od = desc_sw128(smem_u32(Os), kBlk, 1024);
     constexpr uint32_t id_gu = idesc_bf16(128, N2, false, false), id_h = idesc_bf16(128, HC, false, false),
                        id_w = idesc_bf16(128, N2, true, true);
-    // [G | U | dH] of tile i into slot i & 1, whose last contents were read before the operands of tile i - 2 were full
-    auto hidden = [&](int i) {
-      if (!wait(&xfull[i % XS], (i / XS) & 1)) return;
-      const uint64_t x = desc_at(xd, i % XS * 2 * C::kX);
-      const uint32_t hid = tmem + C::kHid + (i & 1) * C::kHidCols;
+    wait(wfull, 0);
+    for (int i = 0; wait.ok && i < count; ++i) {
+      const int s = i % XS;
+      if (!wait(&xfull[s], (i / XS) & 1)) break;
+      const uint64_t x = desc_at(xd, s * 2 * C::kX), xm = desc_at(xmd, s * 2 * C::kX);
+      const uint32_t hid = tmem + C::kHid;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
         issue.mma(hid, desc_at(x, (j >> 2) * kBlk + (j & 3) * 32), desc_at(wd, (j >> 2) * (N2 * 128) + (j & 3) * 32),
                   id_gu, j > 0 ? 1u : 0u);
+      if (!wait(&yfull[s], (i / XS) & 1)) break;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
         issue.mma(hid + N2, desc_at(x, C::kX + (j >> 2) * kBlk + (j & 3) * 32),
                   desc_at(dd, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
-      issue.commit(&gfull[i & 1]);
-    };
-    if (wait(wfull, 0)) hidden(0);
-    for (int i = 0; wait.ok && i < count; ++i) {
-      // the next tile's hidden rows go ahead where it has a place of its own
-      if (XS == 2 && i + 1 < count) hidden(i + 1);
+      issue.commit(gfull);
       if (!wait(ofull, i & 1)) break;
-      const uint64_t xm = desc_at(xmd, i % XS * 2 * C::kX);
+      // X's products first: its place takes the next tile while dY's run
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        // d = 64: X and dY side by side are the 128 rows of both gradients
-        const uint32_t ax = m * 2 * kBlk, ay = (D == 64 ? 0 : C::kX) + m * 2 * kBlk;
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            issue.mma(tmem + m * N2, desc_at(xm, ax + j * 2048), desc_at(od, part * kBlk + j * 2048), id_w,
+            issue.mma(tmem + m * N2, desc_at(xm, m * 2 * kBlk + j * 2048), desc_at(od, part * C::kOps + j * 2048), id_w,
                       (part > 0 || j > 0) ? 1u : 0u);
+      if (D != 64) issue.commit(&xfree[s]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          issue.mma(tmem + C::kAcc2 + m * N2, desc_at(xm, ay + j * 2048), desc_at(od, 2 * kBlk + j * 2048), id_w,
-                    j > 0 ? 1u : 0u);
-      }
-      issue.commit(&xfree[i % XS]);
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)  // d = 64: X and dY side by side are the 128 rows of both gradients
+          issue.mma(tmem + C::kAcc2 + m * N2, desc_at(xm, (D == 64 ? 0 : C::kX) + m * 2 * kBlk + j * 2048),
+                    desc_at(od, 2 * C::kOps + j * 2048), id_w, j > 0 ? 1u : 0u);
+      if (D == 64) issue.commit(&xfree[s]);
+      issue.commit(&yfree[s]);
       issue.commit(ofree);
-      if (XS == 1 && i + 1 < count) hidden(i + 1);
     }
     if (!wait.ok) issue.drain(quit);
   } else if (warp >= 4) {
@@ -452,9 +454,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     constexpr int HW = HC / 4, PC = C::PC;  // hidden features of a warpgroup
     const int h0 = wg * HW;
+    const uint32_t hid = tmem + C::kHid + lane_off + h0;
     WarpWaiter wait{p.status};
-    // This thread's sums: PC pieces of 8 columns of its row.  The twelve pieces of a row of a block are first those of
-    // [dG | dU], then H's, whose two halves are added; at d = 256 two warpgroups share a block.
+    // This thread's sums: six pieces of 8 columns of its row.  The pieces of a row of a block (24; 12 at d = 256, where
+    // two warpgroups share a block) are first those of [dG | dU], then H's, whose two halves are added.
     float sum[PC * 8];
 #pragma unroll
     for (int e = 0; e < PC * 8; ++e) sum[e] = 0.f;
@@ -469,53 +472,55 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int b = 0; b < PC; ++b) {
         bool pair;
         const uint32_t col = tmem + lane_off + m * N2 + place(b, &pair);
-        float v[8];
-        tmem_ld8(col, v);
+        uint32_t v[8], w[8];
+        ld8_issue(col, v);
+        ld8_issue(pair ? col + HC : col, w);
+        ld_wait();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[b * 8 + e] += v[e];
-        if (pair) {
-          tmem_ld8(col + HC, v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum[b * 8 + e] += v[e];
-        }
+        for (int e = 0; e < 8; ++e) sum[b * 8 + e] += __uint_as_float(v[e]) + (pair ? __uint_as_float(w[e]) : 0.f);
       }
     };
     for (int i = 0; i < count; ++i) {
-      if (!wait(&gfull[i & 1], (i >> 1) & 1)) break;
-      const uint32_t hid = tmem + C::kHid + (i & 1) * C::kHidCols + lane_off + h0;
-      float g[8], u[8], h[8];
-      tmem_ld8(hid, g);
-      tmem_ld8(hid + HC, u);
-      tmem_ld8(hid + N2, h);
-      uint32_t hi[3][4], lo[3][4];
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float d0, d1;
-        const float a0 = gate_grad<kAct>(g[e], &d0), a1 = gate_grad<kAct>(g[e + 1], &d1);
-        const float v[3][2] = {{h[e] * u[e] * d0, h[e + 1] * u[e + 1] * d1},
-                               {h[e] * a0, h[e + 1] * a1},
-                               {a0 * u[e], a1 * u[e + 1]}};
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          const uint32_t w = pack2_bf16(v[k][0], v[k][1]);
-          hi[k][e / 2] = w;
-          lo[k][e / 2] = pack2_bf16(v[k][0] - __uint_as_float(w << 16), v[k][1] - __uint_as_float(w & 0xffff0000u));
-        }
-      }
-      if (i >= 1) {
+      if (i >= 1) {  // while the next tile is loaded and its hidden rows are formed
         if (!wait(ofree, (i - 1) & 1)) break;
         drain();
       }
-      // 16 bytes of this row: feature h0 on, of the first or the second half of the columns
-      auto put = [&](uint8_t* o, int c, const uint32_t* v) {
-        st16(o + sw128_offset(row, (c + h0) * 2), make_uint4(v[0], v[1], v[2], v[3]));
-      };
-      put(Os, 0, hi[0]);
-      put(Os, HC, hi[1]);
-      put(Os + kBlk, 0, lo[0]);
-      put(Os + kBlk, HC, lo[1]);
-      put(Os + 2 * kBlk, 0, hi[2]);
-      put(Os + 2 * kBlk, HC, lo[2]);
+      if (!wait(gfull, i & 1)) break;
+#pragma unroll
+      for (int x = 0; x < HW; x += 8) {
+        uint32_t g[8], u[8], h[8];
+        ld8_issue(hid + x, g);
+        ld8_issue(hid + HC + x, u);
+        ld8_issue(hid + N2 + x, h);
+        ld_wait();
+        uint32_t hi[3][4], lo[3][4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float d0, d1;
+          const float a0 = gate_grad<kAct>(__uint_as_float(g[e]), &d0);
+          const float a1 = gate_grad<kAct>(__uint_as_float(g[e + 1]), &d1);
+          const float u0 = __uint_as_float(u[e]), u1 = __uint_as_float(u[e + 1]);
+          const float y0 = __uint_as_float(h[e]), y1 = __uint_as_float(h[e + 1]);
+          const float v[3][2] = {{y0 * u0 * d0, y1 * u1 * d1}, {y0 * a0, y1 * a1}, {a0 * u0, a1 * u1}};
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const uint32_t w = pack2_bf16(v[k][0], v[k][1]);
+            hi[k][e / 2] = w;
+            lo[k][e / 2] = pack2_bf16(v[k][0] - __uint_as_float(w << 16), v[k][1] - __uint_as_float(w & 0xffff0000u));
+          }
+        }
+        // 16 bytes of this row: feature h0 + x on, of the first or the second half of the columns
+        auto put = [&](uint8_t* o, int c, const uint32_t* v) {
+          c += h0 + x;
+          st16(o + (c >> 6) * kBlk + sw128_offset(row, (c & 63) * 2), make_uint4(v[0], v[1], v[2], v[3]));
+        };
+        put(Os, 0, hi[0]);
+        put(Os, HC, hi[1]);
+        put(Os + C::kOps, 0, lo[0]);
+        put(Os + C::kOps, HC, lo[1]);
+        put(Os + 2 * C::kOps, 0, hi[2]);
+        put(Os + 2 * C::kOps, HC, lo[2]);
+      }
       fence_async_smem();
       fence_before_sync();
       warp_arrive(ofull);
@@ -630,11 +635,11 @@ hg_status dx_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
                 dim3(kThreads), C::kSmem, s, tm_X, tm_dY, tm_G, tm_U, tm_W, tm_dX, p);
 }
 
-constexpr int kWgHc = WgCfg<128>::HC;
+int wg_chunk(int d) { return d == 256 ? WgCfg<256>::HC : WgCfg<128>::HC; }
 
 // Shares of the row tiles: the count that makes the longest SM's work shortest (whole waves of chunks x shares).
-int wg_splits(int64_t n, int f) {
-  const int64_t tiles = ceil_div(n, kRows), chunks = ceil_div(f, kWgHc);
+int wg_splits(int64_t n, int d, int f) {
+  const int64_t tiles = ceil_div(n, kRows), chunks = ceil_div(f, wg_chunk(d));
   int64_t best = 1, best_cost = INT64_MAX;
   for (int64_t sp = 1; sp <= std::min<int64_t>(tiles, kSms); ++sp) {
     // a CTA's fixed cost (weights in, gradients out) is about four tiles' time
@@ -653,8 +658,9 @@ struct WgLayout {
 };
 void carve_wg(void* scratch, const hg_ffn_params* w, int64_t n, WgLayout* L, size_t* bytes) {
   Carve k(scratch);
-  L->Wt = k.take<__nv_bfloat16>((size_t)ceil_div(w->f, kWgHc) * 2 * kWgHc * w->d);
-  L->part = k.take<float>((size_t)wg_splits(std::max<int64_t>(n, 1), w->f) * 3 * w->d * w->f);
+  const int hc = wg_chunk(w->d);
+  L->Wt = k.take<__nv_bfloat16>((size_t)ceil_div(w->f, hc) * 2 * hc * w->d);
+  L->part = k.take<float>((size_t)wg_splits(std::max<int64_t>(n, 1), w->d, w->f) * 3 * w->d * w->f);
   if (bytes) *bytes = k.used;
 }
 
@@ -667,7 +673,7 @@ hg_status wg_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
     HG_CUDA(cudaFuncSetAttribute(ffn_wgrad_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     done = true;
   }
-  const int chunks = (int)ceil_div(w->f, C::HC), splits = wg_splits(n, w->f);
+  const int chunks = (int)ceil_div(w->f, C::HC), splits = wg_splits(n, D, w->f);
   HG_TRY(launch("ffn_pack_weights", ffn_pack_weights, dim3(chunks * C::HC / 32, D / 32, 2), dim3(256), 0, s,
                 (const __nv_bfloat16*)w->W_gate, (const __nv_bfloat16*)w->W_up, D, w->f, C::HC, (__nv_bfloat16*)L.Wt));
   CUtensorMap tm_X, tm_dY, tm_Wt, tm_W;
