@@ -25,6 +25,7 @@ struct ScanArgs {
   const float* init;  // [n][heads][d_h][d_h] or null
   int init_t;         // read transposed
   float* last;        // state left behind, or null
+  uint32_t* claims;   // counter, zero before the launch: items are claimed instead of dealt out (null: dealt out)
   float* seg;         // [n][heads][nseg][d_h][d_h]: states of the segments (nseg > 1)
   int64_t n, T, seg_len;
   int nseg, heads;

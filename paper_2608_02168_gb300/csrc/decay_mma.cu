@@ -8,8 +8,8 @@
 // layout in which the next product wants its second operand, so the state goes from sum to operand without
 // leaving the registers; likewise the chunk's weights from q k^T to the product with v.  No warp waits for
 // another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand.  The
-// scaled values that are added to the state are split into two bf16 numbers (16 bits, far below the rows'
-// rounding), and into three (24 bits) where the state left behind, an fp32 result, is asked for.
+// scaled values that are added to the state are split into three bf16 numbers, since a state is an fp32 result that
+// gathers them (two left it 2.5e-6 off).
 //
 // Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high and histories
 // are often shorter than one tile; at d_h = 32 a position moves 256 bytes and needs 9 kFLOP, which the warp
@@ -41,7 +41,7 @@ struct Cfg {
   static constexpr int kRow = DH * 2, kVRow = DS * 2;
   static constexpr int kQ = kC * kRow, kV = kC * kVRow;
   static constexpr int kStage = 2 * kQ + kV;
-  static constexpr int kSmem = W * ST * kStage;
+  static constexpr int kSmem = W * (ST * kStage + 16);
   static constexpr int kBlocks = DH == 16 ? 5 : DH == 32 ? 4 : DH == 64 ? 3 : 2;  // resident CTAs of an SM
 };
 
@@ -162,10 +162,26 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
   const int r16 = lane & 15, c16 = lane >> 4;
   const int r8 = (lane & 7) + ((lane >> 4) << 3), c8 = (lane >> 3) & 1;
 
+  // Items by turns, or, where a counter is given, as they are claimed: the loads run ahead, so the claimed numbers
+  // wait in a queue for the arithmetic.
+  uint32_t* queue = reinterpret_cast<uint32_t*>(smem + C::W * ST * C::kStage) + warp * 4;
+  uint32_t queued = 0, taken = 0;
+  auto next_id = [&](uint32_t id) -> uint32_t {
+    if (!a.claims) return id + stride;
+    uint32_t x = 0;
+    if (lane == 0) x = atomicAdd(a.claims, 1u);
+    x = __shfl_sync(0xffffffffu, x, 0) + stride;
+    if (lane == 0) queue[queued & 3] = x;
+    ++queued;
+    __syncwarp();
+    return x;
+  };
+  auto follow = [&](uint32_t id) -> uint32_t { return a.claims ? queue[taken++ & 3] : id + stride; };
   Item it{}, nx{};
   it.id = blockIdx.x * C::W + warp;
   locate<DH>(a, items, segs, it);
-  // the loads run ahead: position nc of item nx is the next chunk to ask for
+  // The loads run ahead: position nc of item nx is the next chunk to ask for.  An item without positions passes as one
+  // empty chunk, so the loads are at most a ring ahead of the arithmetic.
   const uint8_t *qp = nullptr, *kp = nullptr, *vp = nullptr;
   int64_t nc = 0;
   auto begin = [&]() {
@@ -178,20 +194,22 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
   nx = it;
   begin();
   auto advance = [&](uint8_t* stage) {
-    while (nx.id < items && nc >= nx.t1) {
-      nx.id += stride;
+    if (nx.id < items && nc >= max(nx.t1, nx.t0 + 1)) {
+      nx.id = next_id(nx.id);
       locate<DH>(a, items, segs, nx);
       begin();
     }
     if (nx.id < items) {
       const int m = (int)min((int64_t)kC, nx.t1 - nc);
-      if (!kLocal) load_rows<N>(stage, qp, qs, m, lane);
-      load_rows<N>(stage + C::kQ, kp, ks, m, lane);
-      load_rows<NV>(stage + 2 * C::kQ, vp, vs, m, lane);
-      qp += kC * qs;
-      kp += kC * ks;
-      vp += kC * vs;
       nc += kC;
+      if (m > 0) {
+        if (!kLocal) load_rows<N>(stage, qp, qs, m, lane);
+        load_rows<N>(stage + C::kQ, kp, ks, m, lane);
+        load_rows<NV>(stage + 2 * C::kQ, vp, vs, m, lane);
+        qp += kC * qs;
+        kp += kC * ks;
+        vp += kC * vs;
+      }
     }
     cp_async_commit();
   };
@@ -201,7 +219,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
     advance(ring + put * C::kStage);
     put = put + 1 == ST ? 0 : put + 1;
   }
-  for (; it.id < items; it.id += stride, locate<DH>(a, items, segs, it)) {
+  for (; it.id < items; it.id = follow(it.id), locate<DH>(a, items, segs, it)) {
     const float ld = clamp_ld(a.ld[it.head]), ld2 = ld * 1.4426950408889634f;
     const int64_t sh = (int64_t)it.seq * a.heads + it.head;
     float F[MT][NT][4];
@@ -246,7 +264,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
     uint8_t* op = nullptr;
     if (!kLocal) op = const_cast<uint8_t*>(lane_rows<NV>(a.o, a, it, it.t0, it.head * DH + it.slice * DS, lane));
     const int count = (int)(it.t1 - it.t0);
-    for (int c0 = 0; c0 < count; c0 += kC) {
+    for (int c0 = 0; c0 < max(count, 1); c0 += kC) {
       cp_async_wait<ST - 2>();
       __syncwarp();
       advance(ring + put * C::kStage);
@@ -255,6 +273,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
       get = get + 1 == ST ? 0 : get + 1;
       const uint32_t sq = smem_u32(stage), sk = sq + C::kQ, sv = sk + C::kQ;
       const int m = min(kC, count - c0);
+      if (m <= 0) break;
       const int tau0 = c0 + a.shift;
       uint32_t vt[MT][4];  // v, positions by pairs: [0], [2] positions 0..7 / 8..15 of features 0..7; [1], [3] of 8..15
 #pragma unroll
@@ -344,8 +363,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
 #pragma unroll
         for (int x = 0; x < MT; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
+          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
 #pragma unroll
         for (int y = 0; y < NT; y += 2) {
           uint32_t kb[4];
@@ -356,10 +374,8 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
             mma(F[x][y + 1], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[2], kb[3]);
             mma(F[x][y], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[0], kb[1]);
             mma(F[x][y + 1], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[2], kb[3]);
-            if (a.last) {
-              mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
-              mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
-            }
+            mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
+            mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
           }
         }
         some = true;
