@@ -95,8 +95,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(Os + C::kOps);
   uint64_t *wfull = bars, *wfree = wfull + NG, *dfull = wfree + NG, *dfree = dfull + ND, *xfull = dfree + ND,
            *xfree = xfull + 1, *gfull = xfree + 1, *ofull = gfull + 2, *ofree = ofull + 1, *yfull = ofree + 1,
-           *yfree = yfull + 1, *sfull = yfree + 1, *quit = sfull + 4;
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
+           *yfree = yfull + 1, *sfull = yfree + 1,
+           *gfree = sfull + 4, *quit = gfree + 2;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < NG; ++i) {
@@ -116,7 +117,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(ofree, 1);
     mbar_init(yfull, 1);
     mbar_init(yfree, 16);
-    mbar_init(quit, 1);
+    mbar_init(&gfree[0], SLOTS == 2 ? 8 : 16);
+    mbar_init(&gfree[1], 8);
+    mbar_init(&quit[0], 1);
+    mbar_init(&quit[1], 1);
     fence_mbar_init();
   }
   if (warp == 2) tmem_alloc(tslot, 512);
@@ -161,57 +165,67 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_rounds(wfull, NG, q);
     }
   } else if (warp == 1) {
-    const Issuer issue;
+    // [G | U | dH]
+    const Issuer<1> issue;
     WarpWaiter wait{p.status};
-    uint32_t q = 0, ti = 0;  // q: chunks whose [G | U | dH] was issued
+    uint32_t q = 0, ti = 0;
+    uint32_t gk[2] = {0, 0};  // chunks of each slot so far
     const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), yd = desc_sw128(smem_u32(Ys), 16, 1024);
-    const uint64_t gd = desc_sw128(smem_u32(Gs), D * 128, 1024), gkd = desc_sw128(smem_u32(Gs), 16, 1024);
-    const uint64_t dd = desc_sw128(smem_u32(Ds), 16, 1024), od = desc_sw128(smem_u32(Os), 16, 1024);
-    constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_h = idesc_bf16(128, 64, false, false),
-                       id_dx = idesc_bf16(128, D, false, false);
-    auto hidden = [&](int s) {
-      const uint32_t sg = q % NG, sd = q % ND;
-      if (!wait(&wfull[sg], (q / NG) & 1) || !wait(&dfull[sd], (q / ND) & 1)) return;
-      const uint64_t w = desc_at(gd, sg * C::kGu), w2 = desc_at(dd, sd * C::kDown);
-      const uint32_t t = tmem + C::kSlot + s * C::kSlotCols;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-        issue.mma(t, desc_at(xd, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w, j * 2048), id_gu, j > 0 ? 1u : 0u);
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-        issue.mma(t + 128, desc_at(yd, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w2, (j >> 2) * (HC * 128) + (j & 3) * 32),
-                 id_h, j > 0 ? 1u : 0u);
-      issue.commit(&gfull[s]);
-      issue.commit(&dfree[sd]);
-      ++q;
-    };
-    uint32_t done = 0;  // chunks whose dX was issued
+    const uint64_t gd = desc_sw128(smem_u32(Gs), D * 128, 1024), dd = desc_sw128(smem_u32(Ds), 16, 1024);
+    constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_h = idesc_bf16(128, 64, false, false);
     for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
       if (!wait(xfull, ti & 1)) break;
-      for (int c = 0; wait.ok && c < SLOTS && c < nch; ++c) hidden(c % SLOTS);
-      for (int c = 0; wait.ok && c < nch; ++c) {
-        if (!wait(ofull, done & 1)) break;
-        if (c == 0 && ti >= 1 && !wait(yfree, (ti - 1) & 1)) break;
-        const uint64_t w = desc_at(gkd, done % NG * C::kGu);
+      for (int c = 0; c < nch; ++c, ++q) {
+        const uint32_t sg = q % NG, sd = q % ND;
+        const int s = c % SLOTS;
+        // once the gates have read what the slot held
+        if (gk[s] >= 1 && !wait(&gfree[s], (gk[s] - 1) & 1)) break;
+        if (!wait(&wfull[sg], (q / NG) & 1) || !wait(&dfull[sd], (q / ND) & 1)) break;
+        ++gk[s];
+        const uint64_t w = desc_at(gd, sg * C::kGu), w2 = desc_at(dd, sd * C::kDown);
+        const uint32_t t = tmem + C::kSlot + s * C::kSlotCols;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+          issue.mma(t, desc_at(xd, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w, j * 2048), id_gu, j > 0 ? 1u : 0u);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+          issue.mma(t + 128, desc_at(yd, (j >> 2) * kBlk + (j & 3) * 32),
+                    desc_at(w2, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
+        issue.commit(&gfull[s]);
+        issue.commit(&dfree[sd]);
+      }
+    }
+    if (!wait.ok) issue.drain(&quit[0]);
+  } else if (warp == 3) {
+    // dX, by a warp of its own (see the forward)
+    const Issuer<1> issue;
+    WarpWaiter wait{p.status};
+    uint32_t done = 0, ti = 0;
+    const uint64_t gkd = desc_sw128(smem_u32(Gs), 16, 1024), od = desc_sw128(smem_u32(Os), 16, 1024);
+    constexpr uint32_t id_dx = idesc_bf16(128, D, false, false);
+    for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
+      if (ti >= 1 && !wait(yfree, (ti - 1) & 1)) break;
+      for (int c = 0; c < nch; ++c, ++done) {
+        const uint32_t sg = done % NG;
+        if (!wait(&wfull[sg], (done / NG) & 1) || !wait(ofull, done & 1)) break;
+        const uint64_t w = desc_at(gkd, sg * C::kGu);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < HC / 16; ++j) {
             const uint64_t b = desc_at(w, half * D * 128 + j * 32);
             const uint32_t acc = (c > 0 || half > 0 || j > 0) ? 1u : 0u;
-            if (C::kTs)
+            if constexpr (C::kTs)
               issue.mma_ts(tmem, tmem + C::kOpsCol + half * 32 + j * 8, b, id_dx, acc);
             else
               issue.mma(tmem, desc_at(od, half * kBlk + j * 32), b, id_dx, acc);
           }
         issue.commit(ofree);
-        issue.commit(&wfree[done % NG]);
-        ++done;
+        issue.commit(&wfree[sg]);
         if (c == nch - 1) issue.commit(yfull);
-        if (c + SLOTS < nch) hidden((c + SLOTS) % SLOTS);
       }
     }
-    if (!wait.ok) issue.drain(quit);
+    if (!wait.ok) issue.drain(&quit[1]);
   } else if (warp >= 4) {
     const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
@@ -234,6 +248,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           ld16_issue(t0 + 64 + h0 + x, u);
           ld16_issue(t0 + 128 + h0 + x, h);
           ld_wait();
+          if (x + 16 == HW) {  // the slot's next products run while these gates are computed
+            fence_before_sync();
+            warp_arrive(&gfree[s]);
+          }
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
             float d0, d1;
@@ -404,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_rounds(yfull, XS, qy);
     }
   } else if (warp == 1) {
-    const Issuer issue;
+    const Issuer<1> issue;
     WarpWaiter wait{p.status};
     const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), xmd = desc_sw128(smem_u32(Xs), kBlk, 1024);
     const uint64_t wd = desc_sw128(smem_u32(Ws), 16, 1024), dd = desc_sw128(smem_u32(Ds), 16, 1024);

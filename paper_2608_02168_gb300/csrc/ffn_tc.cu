@@ -5,7 +5,8 @@
 //
 // One persistent CTA an SM.  A group of two 128-row tiles (d <= 128; one at d = 256, whose Y fills half of the
 // tensor memory) stays in shared memory while the hidden features pass by in chunks of 64: the weights'
-// pieces arrive by TMA in a ring, in the stored layout (MN-major operands), [G | U] of a chunk goes to
+// pieces arrive by TMA in two rings, in the stored layout (MN-major operands), half of each piece fetched by each
+// CTA of a pair for both (at d = 256 a lone CTA's weights, 96 KB a chunk, ask more of L2 than it gives), [G | U] of a chunk goes to
 // one of two tensor-memory slots, a warpgroup turns it into H (one row a thread) in shared memory, and the
 // product with W_down adds into Y.  The hidden rows never leave the chip.  The slots take turns (the two
 // tiles, or even and odd chunks): one's gates are computed while the other's products run, so the tensor pipe
@@ -36,15 +37,17 @@ constexpr int kSms = 152;
 template <int D>
 struct FCfg {
   static constexpr int NB = D / 64;
-  static constexpr int NT = D == 256 ? 1 : 2;                // row tiles of a group
-  static constexpr int KP = D == 256 ? 2 : 1;                // pieces of [W_gate | W_up] (by rows)
-  static constexpr int PR = D / KP;                          // their rows
-  static constexpr int kPiece = PR * 128 * 2;                // bytes; W_down's piece is 64 D 2 <= kPiece
-  static constexpr int kDown = kHc * D * 2;
-  static constexpr int NS = D == 64 ? 6 : 4;                 // ring slots
+  static constexpr int NT = D == 256 ? 1 : 2;                // row tiles of a CTA's group
+  // CTAs that share the weights: at d = 256 a lone CTA's operands, read at 8 KB a 64-cycle product and written at 96 KB a
+  // chunk, ask more of shared memory than it gives (300k rows: 284 us; a pair, whose products read half of the weights
+  // from each, 226 us); at d = 128 two tiles share them already (a pair 93 us, one CTA 88 us)
+  static constexpr int CL = D == 256 ? 2 : 1;
+  // a CTA's part of a chunk's weights: of a pair W_gate's or W_up's columns, and half of W_down's
+  static constexpr int kPiece = D * 128 * 2 / CL, kDown = kHc * D * 2 / CL;
+  static constexpr int NG = D == 64 ? 4 : 3, ND = D == 64 ? 4 : 2;  // ring slots
   static constexpr int kX = NT * NB * kBlk;
   static constexpr int kH = kRows * 128;
-  static constexpr int kSmem = kX + NS * kPiece + 2 * kH + 512 + 1024;
+  static constexpr int kSmem = kX + NG * kPiece + ND * kDown + 2 * kH + 512 + 1024;
   static constexpr uint32_t kYCol = 0, kGuCol = 256;         // tensor memory: Y (tile x at x D), slots of 128
 };
 
@@ -57,83 +60,89 @@ struct FwdP {
 };
 
 template <int D, int kAct>
-__global__ void __launch_bounds__(kThreads, 1)
+__cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 1)
     ffn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_G,
                       const __grid_constant__ CUtensorMap tm_U, const __grid_constant__ CUtensorMap tm_W,
                       const __grid_constant__ CUtensorMap tm_Y, FwdP p) {
   pdl_begin();
   using C = FCfg<D>;
-  constexpr int NB = C::NB, NT = C::NT, NS = C::NS, KP = C::KP;
+  constexpr int NB = C::NB, NT = C::NT, NG = C::NG, ND = C::ND, CL = C::CL;
+  using I = Issuer<CL>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* Xs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* Ws = Xs + C::kX;
-  uint8_t* Hs = Ws + NS * C::kPiece;
+  uint8_t* Ds = Ws + NG * C::kPiece;
+  uint8_t* Hs = Ds + ND * C::kDown;
   uint64_t* bars = reinterpret_cast<uint64_t*>(Hs + 2 * C::kH);
-  uint64_t *wfull = bars, *wfree = bars + NS, *xfull = bars + 2 * NS, *xfree = xfull + 1, *gfull = xfull + 2,
-           *hfull = gfull + 2, *hfree = hfull + 2, *yfull = hfree + 2, *yready = yfull + 2, *sfull = yready + 2,
-           *sdone = sfull + 2, *gfree = sdone + 2, *quit = gfree + 2;
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 1);
+  uint64_t *wfull = bars, *wfree = wfull + NG, *dfull = wfree + NG, *dfree = dfull + ND, *xfull = dfree + ND,
+           *xfree = xfull + 1, *xpeer = xfree + 1, *gfull = xpeer + 1, *hfull = gfull + 2, *hfree = hfull + 2,
+           *yfull = hfree + 2, *yready = yfull + 2, *sfull = yready + 2, *sdone = sfull + 2, *gfree = sdone + 2,
+           *quit = gfree + 2;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NS; ++i) {
+    for (int i = 0; i < NG; ++i) {
       mbar_init(&wfull[i], 1);
       mbar_init(&wfree[i], 1);
     }
+    for (int i = 0; i < ND; ++i) {
+      mbar_init(&dfull[i], 1);
+      mbar_init(&dfree[i], 1);
+    }
     mbar_init(xfull, 1);
-    mbar_init(xfree, p.residual ? 513 : 1);
+    mbar_init(xfree, p.residual ? 17 : 1);
+    mbar_init(xpeer, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&gfull[i], 1);
-      mbar_init(&gfree[i], 256);
-      mbar_init(&hfull[i], 256);
+      mbar_init(&gfree[i], 8 * CL);
+      mbar_init(&hfull[i], 8 * CL);
       mbar_init(&hfree[i], 1);
       mbar_init(&yfull[i], 1);
-      mbar_init(&yready[i], NT == 2 ? 256 : 512);
-      mbar_init(&sfull[i], 256);
+      mbar_init(&yready[i], (NT == 2 ? 8 : 16) * CL);
+      mbar_init(&sfull[i], 8);
       mbar_init(&sdone[i], 1);
     }
-    mbar_init(quit, 1);
+    mbar_init(&quit[0], 1);
+    mbar_init(&quit[1], 1);
     fence_mbar_init();
   }
-  if (warp == 2) tmem_alloc(tslot, 512);
+  if (warp == 2) I::alloc(tslot, 512);
   fence_before_sync();
-  __syncthreads();
+  I::sync_all();
   fence_after_sync();
   const uint32_t tmem = *tslot;
   const int nch = p.nch;
+  // A pair's CTAs take neighbouring groups at the same pace (one past the last is rows past n).  The first one issues the
+  // products of both; its barriers gather both CTAs' arrivals, its commits arrive in both.
+  const uint32_t rank = I::rank();
+  const int64_t gr0 = blockIdx.x, gend = (p.groups + CL - 1) / CL * CL;
 
   if (warp == 0 && lane == 0) {
     // ---------------------------------------------------------------- loads
-    bool ok = true;
-    uint32_t q = 0, xn = 0;  // pieces and row groups asked for
-    auto wait = [&](uint64_t* b, uint32_t parity) {
-      if (ok && !mbar_wait(b, parity)) {
-        ok = false;
-        record_device_error(p.status, kErrTimeout);
-      }
-      return ok;
-    };
-    auto slot = [&](uint32_t bytes) -> uint8_t* {
-      const uint32_t s = q % NS;
-      if (q >= NS && !wait(&wfree[s], (q / NS - 1) & 1)) return nullptr;
-      mbar_expect_tx(&wfull[s], bytes);
-      ++q;
-      return Ws + s * C::kPiece;
-    };
+    Waiter wait{p.status};
+    uint32_t q = 0, qd = 0, xn = 0;  // pieces of the two rings and row groups asked for
     auto load_gu = [&](int c) {
-      for (int k = 0; ok && k < KP; ++k) {
-        uint8_t* dst = slot(C::kPiece);
-        if (!dst) return;
-        uint64_t* b = &wfull[(q - 1) % NS];
-        tma_load_2d(dst, &tm_G, c * kHc, k * C::PR, b);
-        tma_load_2d(dst + C::PR * 128, &tm_U, c * kHc, k * C::PR, b);
+      const uint32_t s = q % NG;
+      if (!wait.ok || (q >= NG && !wait(&wfree[s], (q / NG - 1) & 1))) return;
+      if (rank == 0) mbar_expect_tx(&wfull[s], C::kPiece * CL);
+      ++q;
+      uint8_t* dst = Ws + s * C::kPiece;
+      if (CL == 2) {
+        I::load(dst, rank ? &tm_U : &tm_G, c * kHc, 0, &wfull[s]);
+      } else {
+        I::load(dst, &tm_G, c * kHc, 0, &wfull[s]);
+        I::load(dst + D * 128, &tm_U, c * kHc, 0, &wfull[s]);
       }
     };
     auto load_down = [&](int c) {
-      uint8_t* dst = ok ? slot(C::kDown) : nullptr;
-      if (!dst) return;
-      for (int b = 0; b < NB; ++b) tma_load_2d(dst + b * kHc * 128, &tm_W, b * 64, c * kHc, &wfull[(q - 1) % NS]);
+      const uint32_t s = qd % ND;
+      if (!wait.ok || (qd >= ND && !wait(&dfree[s], (qd / ND - 1) & 1))) return;
+      if (rank == 0) mbar_expect_tx(&dfull[s], C::kDown * CL);
+      ++qd;
+      for (int b = 0; b < NB / CL; ++b)
+        I::load(Ds + s * C::kDown + b * kHc * 128, &tm_W, (rank * (NB / CL) + b) * 64, c * kHc, &dfull[s]);
     };
-    for (int64_t gr = blockIdx.x; ok && gr < p.groups; gr += gridDim.x) {
+    for (int64_t gr = gr0; wait.ok && gr < gend; gr += gridDim.x) {
       if (xn >= 1 && !wait(xfree, (xn - 1) & 1)) break;
       mbar_expect_tx(xfull, C::kX);
       for (int t = 0; t < NT; ++t)
@@ -141,82 +150,87 @@ __global__ void __launch_bounds__(kThreads, 1)
           tma_load_2d(Xs + (t * NB + b) * kBlk, &tm_X, b * 64, (int)((gr * NT + t) * kRows), xfull);
       ++xn;
       load_gu(0);
-      if (NT == 1 && nch > 1) load_gu(1);
-      for (int c = 0; ok && c < nch; ++c) {
-        if (NT == 2 && c + 1 < nch) load_gu(c + 1);
+      for (int c = 0; wait.ok && c < nch; ++c) {
+        if (c + 1 < nch) load_gu(c + 1);
         load_down(c);
-        if (NT == 1 && c + 2 < nch) load_gu(c + 2);
       }
     }
-    if (!ok) {  // what was asked for lands before the CTA ends
+    // The last arrivals from the other CTA land before this one is gone; so do, after a give-up, the loads asked for.
+    drain_rounds(wfree, NG, q);
+    drain_rounds(dfree, ND, qd);
+    if (xn) mbar_wait(xfree, (xn - 1) & 1);
+    if (!wait.ok) {
       if (xn) mbar_wait(xfull, (xn - 1) & 1);
-      drain_rounds(wfull, NS, q);
+      if (rank == 0) {
+        drain_rounds(wfull, NG, q);
+        drain_rounds(dfull, ND, qd);
+      }
     }
+  } else if (warp == 1 && rank != 0) {
+    // ---------------------------------------------------------------- X is there, for the issuing CTA
+    WarpWaiter wait{p.status};
+    uint32_t gi = 0;
+    for (int64_t gr = gr0; gr < gend && wait(xfull, gi & 1); gr += gridDim.x, ++gi) I::arrive(xpeer);
   } else if (warp == 1) {
-    // ---------------------------------------------------------------- products
-    const Issuer issue;
+    // ---------------------------------------------------------------- [G | U]
+    const I issue;
+    WarpWaiter wait{p.status};
+    uint32_t q = 0, gi = 0;
+    uint32_t gk[2] = {0, 0};  // [G | U] of each slot so far
+    const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), gd = desc_sw128(smem_u32(Ws), D * 128, 1024);
+    constexpr uint32_t id_gu = idesc_bf16(128 * CL, 128, false, true);
+    for (int64_t gr = gr0; wait.ok && gr < gend; gr += gridDim.x, ++gi) {
+      if (!wait(xfull, gi & 1) || (CL == 2 && !wait(xpeer, gi & 1))) break;
+      for (int c = 0; wait.ok && c < nch; ++c, ++q) {
+        if (!wait(&wfull[q % NG], (q / NG) & 1)) break;
+        const uint64_t w = desc_at(gd, q % NG * C::kPiece);
+        for (int t = 0; wait.ok && t < NT; ++t) {
+          const int s = NT == 2 ? t : c & 1;
+          // once the gates have read what the slot held
+          if (gk[s] >= 1 && !wait(&gfree[s], (gk[s] - 1) & 1)) break;
+          const uint64_t x = desc_at(xd, t * NB * kBlk);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+            issue.mma(tmem + C::kGuCol + s * 128, desc_at(x, (j >> 2) * kBlk + (j & 3) * 32), desc_at(w, j * 2048), id_gu,
+                      j > 0 ? 1u : 0u);
+          ++gk[s];
+          issue.commit(&gfull[s]);
+        }
+        if (!wait.ok) break;
+        issue.commit(&wfree[q % NG]);
+        if (c == nch - 1) issue.commit(xfree);
+      }
+    }
+    if (!wait.ok) issue.drain(&quit[0]);
+  } else if (warp == 3 && rank == 0) {
+    // ---------------------------------------------------------------- H W_down, by a warp of its own: a wait or a commit takes
+    // this role some hundred cycles beside the gates' warps, and neither product should stand behind the other's
+    const I issue;
     WarpWaiter wait{p.status};
     uint32_t q = 0, gi = 0;
     uint32_t hk[2] = {0, 0};  // chunks of each slot so far
-    const uint64_t xd = desc_sw128(smem_u32(Xs), 16, 1024), hd = desc_sw128(smem_u32(Hs), 16, 1024);
-    const uint64_t gd = desc_sw128(smem_u32(Ws), C::PR * 128, 1024), wd = desc_sw128(smem_u32(Ws), kHc * 128, 1024);
-    constexpr uint32_t id_gu = idesc_bf16(128, 128, false, true), id_y = idesc_bf16(128, D, false, true);
-    uint32_t gk[2] = {0, 0};  // [G | U] of each slot so far
-    // tile t times the chunk's pieces q .. q + KP - 1 into slot s, once the gates have read what it held
-    auto gu = [&](int t, int s) {
-      if (NT == 2 && gk[s] >= 1 && !wait(&gfree[s], (gk[s] - 1) & 1)) return;
+    const uint64_t hd = desc_sw128(smem_u32(Hs), 16, 1024), wd = desc_sw128(smem_u32(Ds), kHc * 128, 1024);
+    constexpr uint32_t id_y = idesc_bf16(128 * CL, D, false, true);
+    for (int64_t gr = gr0; wait.ok && gr < gend; gr += gridDim.x, ++gi) {
+      for (int c = 0; wait.ok && c < nch; ++c, ++q) {
+        if (!wait(&dfull[q % ND], (q / ND) & 1)) break;
+        const uint64_t w = desc_at(wd, q % ND * C::kDown);
+        for (int t = 0; wait.ok && t < NT; ++t) {
+          const int s = NT == 2 ? t : c & 1;
+          if ((c == 0 && !wait(&yready[t], gi & 1)) || !wait(&hfull[s], hk[s] & 1)) break;
+          ++hk[s];
+          const uint64_t h = desc_at(hd, s * C::kH);
 #pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        if (!wait(&wfull[(q + k) % NS], ((q + k) / NS) & 1)) return;
-        const uint64_t w = desc_at(gd, (q + k) % NS * C::kPiece), x = desc_at(xd, t * NB * kBlk);
-#pragma unroll
-        for (int j = 0; j < C::PR / 16; ++j) {
-          const int jj = k * (C::PR / 16) + j;
-          issue.mma(tmem + C::kGuCol + s * 128, desc_at(x, (jj >> 2) * kBlk + (jj & 3) * 32), desc_at(w, j * 2048),
-                    id_gu, jj > 0 ? 1u : 0u);
+          for (int j = 0; j < 4; ++j)
+            issue.mma(tmem + C::kYCol + t * D, desc_at(h, j * 32), desc_at(w, j * 2048), id_y,
+                      (c > 0 || j > 0 || p.residual) ? 1u : 0u);
+          issue.commit(&hfree[s]);
+          if (c == nch - 1) issue.commit(&yfull[t]);
         }
-      }
-      ++gk[s];
-      issue.commit(&gfull[s]);
-    };
-    // the hidden rows of slot s times W_down's piece q into its tile's Y
-    auto down = [&](int c, int s) {
-      const int t = NT == 2 ? s : 0;
-      if (!wait(&wfull[q % NS], (q / NS) & 1) || !wait(&hfull[s], hk[s] & 1)) return;
-      if (c == 0 && !wait(&yready[t], gi & 1)) return;
-      ++hk[s];
-      const uint64_t w = desc_at(wd, q % NS * C::kPiece), h = desc_at(hd, s * C::kH);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        issue.mma(tmem + C::kYCol + t * D, desc_at(h, j * 32), desc_at(w, j * 2048), id_y,
-                  (c > 0 || j > 0 || p.residual) ? 1u : 0u);
-      issue.commit(&hfree[s]);
-      if (c == nch - 1) issue.commit(&yfull[t]);
-    };
-    auto release = [&](int count) {
-      for (int i = 0; i < count; ++i, ++q) issue.commit(&wfree[q % NS]);
-    };
-    // chunk c's [G | U] of every tile of the group
-    auto hidden = [&](int c) {
-      for (int t = 0; wait.ok && t < NT; ++t) gu(t, NT == 2 ? t : c & 1);
-      if (!wait.ok) return;
-      release(KP);
-      if (c == nch - 1) issue.commit(xfree);
-    };
-    for (int64_t gr = blockIdx.x; wait.ok && gr < p.groups; gr += gridDim.x, ++gi) {
-      if (!wait(xfull, gi & 1)) break;
-      for (int c = 0; wait.ok && c < 3 - NT && c < nch; ++c) hidden(c);
-      for (int c = 0; wait.ok && c < nch; ++c) {
-        // two tiles: the next [G | U] of both goes ahead, it is wanted first; one tile: the other slot's [G | U]
-        // is under way, and the next one would only stand before this product (300k rows, d = 256: 275 -> 317 us)
-        if (NT == 2 && c + 1 < nch) hidden(c + 1);
-        for (int t = 0; wait.ok && t < NT; ++t) down(c, NT == 2 ? t : c & 1);
-        if (!wait.ok) break;
-        release(1);
-        if (NT == 1 && c + 2 < nch) hidden(c + 2);
+        if (wait.ok) issue.commit(&dfree[q % ND]);
       }
     }
-    if (!wait.ok) issue.drain(quit);
+    if (!wait.ok) issue.drain(&quit[1]);
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- gates and rows out
     // half of the slot's hidden features (and of its tile's columns) for each warpgroup
@@ -232,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int blk0 = NT == 2 ? 0 : s * RN;
     const uint32_t ycol = tmem + C::kYCol + t * D + lane_off + blk0 * 64 + half * 32;
     uint32_t rounds = 0;
-    for (int64_t gr = blockIdx.x; wait.ok && gr < p.groups; gr += gridDim.x, ++gi) {
+    for (int64_t gr = gr0; wait.ok && gr < gend; gr += gridDim.x, ++gi) {
       if (p.residual) {  // Y starts at X, so that X's place can take the next group while this one is finished
         if (!wait(xfull, gi & 1)) break;
 #pragma unroll
@@ -247,10 +261,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         st_wait();
-        mbar_arrive(xfree);
+        warp_arrive(xfree);
       }
       fence_before_sync();
-      mbar_arrive(&yready[t]);
+      I::arrive(&yready[t]);
       bool first = rounds > 0;  // the rows of the group before leave through H's place
       for (int c = NT == 2 ? 0 : s; wait.ok && c < nch; c += 3 - NT, ++k) {
         if (!wait(&gfull[s], k & 1)) break;
@@ -260,10 +274,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         ld16_issue(gcol + 16, reinterpret_cast<uint32_t(&)[16]>(g[16]));
         ld16_issue(gcol + 80, reinterpret_cast<uint32_t(&)[16]>(u[16]));
         ld_wait();
-        if (NT == 2) {  // the next [G | U] runs while these gates are computed
-          fence_before_sync();
-          mbar_arrive(&gfree[s]);
-        }
+        fence_before_sync();
+        I::arrive(&gfree[s]);  // the next [G | U] runs while these gates are computed
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
           h[e / 2] = pack2_bf16(gate<kAct>(__uint_as_float(g[e])) * __uint_as_float(u[e]),
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           st16(H + sw128_offset(row, half * 64 + e * 16), make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]));
         fence_async_smem();
         fence_before_sync();
-        mbar_arrive(&hfull[s]);
+        I::arrive(&hfull[s]);
       }
       if (!wait.ok) break;
       // rows out, 64 columns a round: through H's place, and by a TMA store (it leaves out the rows past n)
@@ -294,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int e = 0; e < 4; ++e)
           st16(H + sw128_offset(row, half * 64 + e * 16), pack(reinterpret_cast<float*>(y) + 8 * e, __nv_bfloat16()));
         fence_async_smem();
-        mbar_arrive(&sfull[s]);
+        warp_arrive(&sfull[s]);
         if ((threadIdx.x - 128) % 256 == 0) {
           if (mbar_wait(&sfull[s], rounds & 1)) {
             if (r0 < p.n) tma_store_2d(&tm_Y, H, (blk0 + b) * 64, (int)r0);
@@ -308,11 +320,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       }
     }
+    if (k >= 1) wait(&hfree[s], (k - 1) & 1);
     bulk_wait();
   }
   fence_before_sync();
-  __syncthreads();
-  if (warp == 2) tmem_dealloc(tmem, 512);
+  I::sync_all();
+  if (warp == 2) I::dealloc(tmem, 512);
 }
 
 template <int D, int kAct>
@@ -325,13 +338,13 @@ hg_status fwd_t(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaS
   }
   CUtensorMap tm_X, tm_G, tm_U, tm_W, tm_Y;
   HG_TRY(make_tmap_bf16(&tm_X, X, (uint64_t)n, D, kRows));
-  HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, C::PR));
-  HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, C::PR));
+  HG_TRY(make_tmap_bf16(&tm_G, w->W_gate, D, (uint64_t)w->f, D));
+  HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, D));
   HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, kHc));
   HG_TRY(make_tmap_bf16(&tm_Y, Y, (uint64_t)n, D, kRows));
   FwdP p{n, (int)ceil_div(w->f, kHc), ceil_div(n, (int64_t)kRows * C::NT),
          w->residual != 0, device_status_ptr()};
-  const int grid = (int)std::min<int64_t>(p.groups, kSms);
+  const int grid = (int)std::min<int64_t>(ceil_div(p.groups, C::CL) * C::CL, kSms / C::CL * C::CL);
   return launch("ffn_fwd_tc", ffn_fwd_tc_kernel<D, kAct>, dim3(grid), dim3(kThreads), C::kSmem, s, tm_X, tm_G, tm_U,
                 tm_W, tm_Y, p);
 }

@@ -47,8 +47,11 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
   if ((threadIdx.x & 31) == 0) tc::mbar_arrive(bar);
 }
 
-// The issuing warp: all its lanes run the role, so that descriptors are warp-uniform values, and one elected
-// lane issues.
+// The issuing warp of a CTA (CL = 1) or of a pair of CTAs (CL = 2, a cluster): all its lanes run the role, so that
+// descriptors are warp-uniform values, and one elected lane issues.  A pair's product has 256 rows, 128 of each CTA from
+// the same places of its shared memory to the same columns of its tensor memory; the second operand lies half in each.
+// The first CTA issues, and a commit arrives at the same barrier of both.
+template <int CL>
 struct Issuer {
   uint32_t lead;
   __device__ __forceinline__ Issuer() {
@@ -57,17 +60,27 @@ struct Issuer {
   // D[tmem] (+)= A[smem] B[smem]
   __device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
                                       uint32_t accumulate) const {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "setp.ne.b32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
-        : "memory");
+    if constexpr (CL == 1)
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.ne.b32 p, %4, 0;\n\t"
+          "setp.ne.b32 q, %5, 0;\n\t"
+          "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+          ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+          : "memory");
+    else
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.ne.b32 p, %4, 0;\n\t"
+          "setp.ne.b32 q, %5, 0;\n\t"
+          "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+          ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+          : "memory");
   }
   // D += A[tmem] B[smem]: A's lane = row, each 32-bit column two bf16 along K
   __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                          uint32_t accumulate) const {
+    static_assert(CL == 1);
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
@@ -77,10 +90,75 @@ struct Issuer {
         : "memory");
   }
   __device__ __forceinline__ void commit(uint64_t* bar) const {
-    if (lead) tc::mma_commit(bar);
+    if (!lead) return;
+    if constexpr (CL == 1)
+      tc::mma_commit(bar);
+    else
+      asm volatile(
+          "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+              tc::smem_u32(bar)),
+          "h"((uint16_t)3)
+          : "memory");
   }
   __device__ __forceinline__ void drain(uint64_t* bar) const {
-    if (lead) tc::drain_mma(bar, 0);
+    commit(bar);
+    if (lead) tc::mbar_wait(bar, 0);
+  }
+
+  // The other roles of the CTAs.
+  static __device__ __forceinline__ uint32_t rank() {
+    if constexpr (CL == 1) return 0;
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+  }
+  static __device__ __forceinline__ void sync_all() {
+    if constexpr (CL == 1)
+      __syncthreads();
+    else
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // address of the first CTA's barrier
+  static __device__ __forceinline__ uint32_t first(uint64_t* bar) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(tc::smem_u32(bar)));
+    return a;
+  }
+  // one arrival for the warp at the first CTA's barrier, after what all its lanes did before
+  static __device__ __forceinline__ void arrive(uint64_t* bar) {
+    if constexpr (CL == 1) {
+      warp_arrive(bar);
+    } else {
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0)
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(first(bar)) : "memory");
+    }
+  }
+  // tile load into this CTA's shared memory, counted on the first CTA's barrier
+  static __device__ __forceinline__ void load(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+    if constexpr (CL == 1)
+      tc::tma_load_2d(dst, map, x, y, bar);
+    else
+      asm volatile(
+          "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
+          "%3}], [%4];" ::"r"(tc::smem_u32(dst)),
+          "l"(map), "r"(x), "r"(y), "r"(first(bar))
+          : "memory");
+  }
+  static __device__ __forceinline__ void alloc(uint32_t* slot, uint32_t ncols) {
+    if constexpr (CL == 1) {
+      tc::tmem_alloc(slot, ncols);
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(slot)), "r"(ncols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+  }
+  static __device__ __forceinline__ void dealloc(uint32_t taddr, uint32_t ncols) {
+    if constexpr (CL == 1)
+      tc::tmem_dealloc(taddr, ncols);
+    else
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
   }
 };
 
