@@ -94,9 +94,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* Os = Ds + ND * C::kDown;
   uint64_t* bars = reinterpret_cast<uint64_t*>(Os + C::kOps);
   uint64_t *wfull = bars, *wfree = wfull + NG, *dfull = wfree + NG, *dfree = dfull + ND, *xfull = dfree + ND,
-           *xfree = xfull + 1, *gfull = xfree + 1, *ofull = gfull + 2, *ofree = ofull + 1, *yfull = ofree + 1,
+           *xfree = xfull + 1, *gfull = xfree + 1, *ofull = gfull + 2, *ofree = ofull + 1, *yfull = ofree + 2,
            *yfree = yfull + 1, *sfull = yfree + 1,
-           *gfree = sfull + 4, *quit = gfree + 2;
+           *sdone = sfull + 4, *gfree = sdone + 1, *quit = gfree + 2;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(quit + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -109,12 +109,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&dfree[i], 1);
     }
     mbar_init(xfull, 1);
-    mbar_init(xfree, 512 / C::kStoreThreads);
+    mbar_init(xfree, C::kTs ? 512 / C::kStoreThreads : p.residual ? 17 : 1);
+    mbar_init(sdone, 512 / C::kStoreThreads);
     for (int i = 0; i < 512 / C::kStoreThreads; ++i) mbar_init(&sfull[i], C::kStoreThreads / 32);
     mbar_init(&gfull[0], 1);
     mbar_init(&gfull[1], 1);
     mbar_init(ofull, SLOTS == 2 ? 8 : 16);
-    mbar_init(ofree, 1);
+    mbar_init(&ofree[0], 1);
+    mbar_init(&ofree[1], 1);
     mbar_init(yfull, 1);
     mbar_init(yfree, 16);
     mbar_init(&gfree[0], SLOTS == 2 ? 8 : 16);
@@ -193,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     desc_at(w2, (j >> 2) * (HC * 128) + (j & 3) * 32), id_h, j > 0 ? 1u : 0u);
         issue.commit(&gfull[s]);
         issue.commit(&dfree[sd]);
+        if (!C::kTs && c == nch - 1) issue.commit(xfree);
       }
     }
     if (!wait.ok) issue.drain(&quit[0]);
@@ -204,7 +207,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t gkd = desc_sw128(smem_u32(Gs), 16, 1024), od = desc_sw128(smem_u32(Os), 16, 1024);
     constexpr uint32_t id_dx = idesc_bf16(128, D, false, false);
     for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
-      if (ti >= 1 && !wait(yfree, (ti - 1) & 1)) break;
+      // kTs: the sums of the tile before were read; else dX is ready to be added to
+      if (C::kTs ? ti >= 1 && !wait(yfree, (ti - 1) & 1) : !wait(yfree, ti & 1)) break;
       for (int c = 0; c < nch; ++c, ++done) {
         const uint32_t sg = done % NG;
         if (!wait(&wfull[sg], (done / NG) & 1) || !wait(ofull, done & 1)) break;
@@ -214,13 +218,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < HC / 16; ++j) {
             const uint64_t b = desc_at(w, half * D * 128 + j * 32);
-            const uint32_t acc = (c > 0 || half > 0 || j > 0) ? 1u : 0u;
+            const uint32_t acc = (c > 0 || half > 0 || j > 0 || (!C::kTs && p.residual)) ? 1u : 0u;
             if constexpr (C::kTs)
               issue.mma_ts(tmem, tmem + C::kOpsCol + half * 32 + j * 8, b, id_dx, acc);
             else
               issue.mma(tmem, desc_at(od, half * kBlk + j * 32), b, id_dx, acc);
           }
-        issue.commit(ofree);
+        issue.commit(&ofree[done & 1]);
         issue.commit(&wfree[sg]);
         if (c == nch - 1) issue.commit(yfull);
       }
@@ -235,7 +239,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int h0 = (SLOTS == 2 ? wg & 1 : wg) * HW;
     WarpWaiter wait{p.status};
     uint32_t k = 0, done = 0, ti = 0;  // chunks of this slot, of all slots; tiles
+    constexpr int CW = D / 4;  // columns of dX of a warpgroup
+    const int col0 = wg * CW;
     for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
+      if (!C::kTs) {
+        if (p.residual) {  // dX starts at dY, so that X's and dY's places can take the next tile while this one is finished
+          if (!wait(xfull, ti & 1)) break;
+#pragma unroll
+          for (int c = 0; c < CW; c += 16) {
+            const uint8_t* yb = Ys + col0 / 64 * kBlk;
+            float v[16];
+            unpack(ld16(yb + sw128_offset(row, (col0 % 64 + c) * 2)), v, __nv_bfloat16());
+            unpack(ld16(yb + sw128_offset(row, (col0 % 64 + c) * 2 + 16)), v + 8, __nv_bfloat16());
+            st16_issue(tmem + lane_off + col0 + c, v);
+          }
+          st_wait();
+          warp_arrive(xfree);
+        }
+        fence_before_sync();
+        warp_arrive(yfree);
+      }
+      bool first = ti > 0;  // the rows of the tile before leave through the operands' place
       for (int c = 0; wait.ok && c < nch; ++c, ++done) {
         if (SLOTS == 2 && (c & 1) != s) continue;
         if (!wait(&gfull[s], k & 1)) break;
@@ -262,7 +286,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             du[(x + e) / 2] = pack2_bf16(y0 * a0, y1 * a1);
           }
         }
-        if (done >= 1 && !wait(ofree, (done - 1) & 1)) break;
+        // The product before has read the operands.  A slot looks at every other product, so even and odd ones have
+        // barriers of their own: no phase of one passes unseen.
+        if (done >= 1 && !wait(&ofree[(done - 1) & 1], ((done - 1) >> 1) & 1)) break;
         if (C::kTs) {
 #pragma unroll
           for (int x = 0; x < HW / 2; x += 8) {
@@ -271,6 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           st_wait();
         } else {
+          if (first && !wait(sdone, (ti - 1) & 1)) break;
+          first = false;
 #pragma unroll
           for (int e = 0; e < HW / 8; ++e) {
             st16(Os + sw128_offset(row, h0 * 2 + e * 16), make_uint4(dg[4 * e], dg[4 * e + 1], dg[4 * e + 2], dg[4 * e + 3]));
@@ -283,20 +311,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         warp_arrive(ofull);
       }
       if (!wait.ok) break;
-      // rows out: dY's place takes dX (+ dY), and a TMA store each 64 columns (it leaves out the rows past n)
-      constexpr int CW = D / 4;
-      const int col0 = wg * CW;
-      uint8_t* yb = Ys + col0 / 64 * kBlk;
-      if (!wait(xfull, ti & 1) || !wait(yfull, ti & 1)) break;
+      // Rows out, a TMA store each 64 columns (it leaves out the rows past n): through the operands' place, which the last
+      // product has read; kTs: dY's place takes dX (+ dY).
+      uint8_t* ob = (C::kTs ? Ys : Os) + col0 / 64 * kBlk;
+      if ((C::kTs && !wait(xfull, ti & 1)) || !wait(yfull, ti & 1)) break;
+      if (!C::kTs && first && !wait(sdone, (ti - 1) & 1)) break;
 #pragma unroll
       for (int c = 0; c < CW; c += 16) {
         uint32_t y[16];
         ld16_issue(tmem + lane_off + col0 + c, y);
-        uint4* x0 = reinterpret_cast<uint4*>(yb + sw128_offset(row, (col0 % 64 + c) * 2));
-        uint4* x1 = reinterpret_cast<uint4*>(yb + sw128_offset(row, (col0 % 64 + c) * 2 + 16));
+        uint4* x0 = reinterpret_cast<uint4*>(ob + sw128_offset(row, (col0 % 64 + c) * 2));
+        uint4* x1 = reinterpret_cast<uint4*>(ob + sw128_offset(row, (col0 % 64 + c) * 2 + 16));
+        const bool add = C::kTs && p.residual;
         float v[16];
-        unpack(p.residual ? *x0 : make_uint4(0u, 0u, 0u, 0u), v, __nv_bfloat16());
-        unpack(p.residual ? *x1 : make_uint4(0u, 0u, 0u, 0u), v + 8, __nv_bfloat16());
+        unpack(add ? *x0 : make_uint4(0u, 0u, 0u, 0u), v, __nv_bfloat16());
+        unpack(add ? *x1 : make_uint4(0u, 0u, 0u, 0u), v + 8, __nv_bfloat16());
         ld_wait();
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(y[i]);
@@ -305,18 +334,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       fence_async_smem();
       fence_before_sync();
-      warp_arrive(yfree);
+      if (C::kTs) warp_arrive(yfree);
       uint64_t* sb = &sfull[(threadIdx.x - 128) / C::kStoreThreads];
       warp_arrive(sb);
       if ((threadIdx.x - 128) % C::kStoreThreads == 0) {
         if (mbar_wait(sb, ti & 1)) {
-          tma_store_2d(&tm_dX, yb, col0 / 64 * 64, (int)(tile * kRows));
+          tma_store_2d(&tm_dX, ob, col0 / 64 * 64, (int)(tile * kRows));
           bulk_commit();
           bulk_wait_read();
         } else {
           record_device_error(p.status, kErrTimeout);
         }
-        mbar_arrive(xfree);
+        mbar_arrive(C::kTs ? xfree : sdone);
       }
       __syncwarp();
     }

@@ -414,12 +414,14 @@ def test_ffn_forward_and_backward(dt, n, d, f, act, res):
     assert all(torch.equal(again[k], g[k]) for k in g)
 
 
-@pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_ffn_many_row_tiles(dt):
-    """More row tiles than CTAs: every one of them is taken, and none twice."""
+@pytest.mark.parametrize("dt,d,f", [("f32", 64, 40), ("bf16", 64, 40), ("bf16", 64, 200), ("bf16", 128, 136),
+                                    ("bf16", 128, 256), ("bf16", 256, 72), ("bf16", 256, 320)])
+def test_ffn_many_row_tiles(dt, d, f):
+    """More row tiles than CTAs, with one to five chunks of hidden features: every tile is taken, none twice, and a
+    row's values do not depend on the tiles around it, whatever turn their chunks take."""
     need_gpu()
     hg = lib()
-    n, d, f = 45_001, 64, 40
+    n = 45_001
     td = tdtype(dt)
     X, Wg, Wu, Wd, dY = ffn_problem(dt, 129, d, f, 3)
     at = torch.arange(n, device="cuda") % 129
