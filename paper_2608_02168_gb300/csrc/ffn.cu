@@ -27,30 +27,42 @@ struct Mat {
   int64_t ld, nr, nc;
 };
 
-// dst[k][x] for kBk of k and X of x (row stride X + 4) from an operand whose rows are x and columns k
-// (kByRow) or whose rows are k and columns x.  Zero outside.  nr, nc and the starts are such that four
-// neighbouring columns are all inside or all outside.
+// A tile dst[k][x], kBk of k and X of x (row stride X + 4), of an operand whose rows are x and columns k (kByRow) or
+// whose rows are k and columns x.  Zero outside.  nr, nc and the starts are such that four neighbouring columns are
+// all inside or all outside.  fetch loads a thread's pieces, put lays them in shared memory: the loads of the next
+// tile run while this one is multiplied.
 template <int X, bool kByRow>
-__device__ __forceinline__ void stage(float* dst, const Mat& a, int64_t x0, int64_t k0) {
-  constexpr int PER = X * kBk / 4 / kThr;
+struct Piece {
+  static constexpr int PER = X * kBk / 4 / kThr;
+  float4 v[PER];
+  __device__ __forceinline__ void fetch(const Mat& a, int64_t x0, int64_t k0) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = threadIdx.x + i * kThr;
-    const int r = kByRow ? e / (kBk / 4) : e / (X / 4);
-    const int c = (kByRow ? e % (kBk / 4) : e % (X / 4)) * 4;
-    const int64_t row = (kByRow ? x0 : k0) + r, col = (kByRow ? k0 : x0) + c;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < a.nr && col < a.nc) v = *reinterpret_cast<const float4*>(a.p + row * a.ld + col);
-    if (kByRow) {
-      dst[(c + 0) * (X + 4) + r] = v.x;
-      dst[(c + 1) * (X + 4) + r] = v.y;
-      dst[(c + 2) * (X + 4) + r] = v.z;
-      dst[(c + 3) * (X + 4) + r] = v.w;
-    } else {
-      *reinterpret_cast<float4*>(dst + r * (X + 4) + c) = v;
+    for (int i = 0; i < PER; ++i) {
+      const int e = threadIdx.x + i * kThr;
+      const int r = kByRow ? e / (kBk / 4) : e / (X / 4);
+      const int c = (kByRow ? e % (kBk / 4) : e % (X / 4)) * 4;
+      const int64_t row = (kByRow ? x0 : k0) + r, col = (kByRow ? k0 : x0) + c;
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < a.nr && col < a.nc) v[i] = *reinterpret_cast<const float4*>(a.p + row * a.ld + col);
     }
   }
-}
+  __device__ __forceinline__ void put(float* dst) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = threadIdx.x + i * kThr;
+      const int r = kByRow ? e / (kBk / 4) : e / (X / 4);
+      const int c = (kByRow ? e % (kBk / 4) : e % (X / 4)) * 4;
+      if (kByRow) {
+        dst[(c + 0) * (X + 4) + r] = v[i].x;
+        dst[(c + 1) * (X + 4) + r] = v[i].y;
+        dst[(c + 2) * (X + 4) + r] = v[i].z;
+        dst[(c + 3) * (X + 4) + r] = v[i].w;
+      } else {
+        *reinterpret_cast<float4*>(dst + r * (X + 4) + c) = v[i];
+      }
+    }
+  }
+};
 
 struct Acc {
   float v[8][4];
@@ -95,19 +107,33 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, M
   g.zero();
   u.zero();
   h.zero();
-  for (int64_t k0 = 0; k0 < X.nc; k0 += kBk) {
-    stage<kBm, true>(As, X, r0, k0);
-    stage<kBn, false>(Bs, Wg, c0, k0);
-    stage<kBn, false>(Cs, Wu, c0, k0);
+  Piece<kBm, true> pa, pd;
+  Piece<kBn, false> pb, pc;
+  Piece<kBn, true> pe;
+  auto fetch = [&](int64_t k0) {
+    pa.fetch(X, r0, k0);
+    pb.fetch(Wg, c0, k0);
+    pc.fetch(Wu, c0, k0);
     if (kBwd) {
-      stage<kBm, true>(Ds, dY, r0, k0);
-      stage<kBn, true>(Es, Wd, c0, k0);
+      pd.fetch(dY, r0, k0);
+      pe.fetch(Wd, c0, k0);
+    }
+  };
+  fetch(0);
+  for (int64_t k0 = 0; k0 < X.nc; k0 += kBk) {
+    __syncthreads();
+    pa.put(As);
+    pb.put(Bs);
+    pc.put(Cs);
+    if (kBwd) {
+      pd.put(Ds);
+      pe.put(Es);
     }
     __syncthreads();
+    if (k0 + kBk < X.nc) fetch(k0 + kBk);
     mul(As, Bs, g);
     mul(As, Cs, u);
     if (kBwd) mul(Ds, Es, h);
-    __syncthreads();
   }
   const int64_t col = c0 + threadIdx.x % 16 * 4;
   if (col >= Wg.nc) return;
@@ -147,14 +173,23 @@ __global__ void __launch_bounds__(kThr) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B
   const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * kBm, c0 = (int64_t)(blockIdx.x % ctiles) * kBn;
   Acc acc;
   acc.zero();
-  for (int half = 0; half < (A2.p ? 2 : 1); ++half) {
-    for (int64_t k0 = 0; k0 < A.nc; k0 += kBk) {
-      stage<kBm, true>(As, half ? A2 : A, r0, k0);
-      stage<kBn, kTransB>(Bs, half ? B2 : B, c0, k0);
-      __syncthreads();
-      mul(As, Bs, acc);
-      __syncthreads();
-    }
+  Piece<kBm, true> pa;
+  Piece<kBn, kTransB> pb;
+  const int64_t steps = (A.nc + kBk - 1) / kBk, all = A2.p ? 2 * steps : steps;
+  auto fetch = [&](int64_t i) {
+    const bool second = i >= steps;
+    const int64_t k0 = (second ? i - steps : i) * kBk;
+    pa.fetch(second ? A2 : A, r0, k0);
+    pb.fetch(second ? B2 : B, c0, k0);
+  };
+  fetch(0);
+  for (int64_t i = 0; i < all; ++i) {
+    __syncthreads();
+    pa.put(As);
+    pb.put(Bs);
+    __syncthreads();
+    if (i + 1 < all) fetch(i + 1);
+    mul(As, Bs, acc);
   }
   const int64_t col = c0 + threadIdx.x % 16 * 4;
   if (col >= nc) return;
@@ -169,26 +204,40 @@ __global__ void __launch_bounds__(kThr) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B
   }
 }
 
-// part[blockIdx.z] = A^T B over the split's rows (A: rows x mc, B: rows x nc).
-__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat A, Mat B, int64_t rows, float* __restrict__ part) {
+// part[blockIdx.y] = [X^T dG | X^T dU | H^T dY] over the split's rows, a tile a block.
+__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat X, Mat dG, Mat dU, Mat H, Mat dY, int64_t rows,
+                                                       float* __restrict__ part) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
-  const int64_t m0 = (int64_t)blockIdx.y * kBm, c0 = (int64_t)blockIdx.x * kBn;
-  const int64_t k1 = min(A.nr, (int64_t)(blockIdx.z + 1) * rows);
-  Mat Ae = A, Be = B;
-  Ae.nr = Be.nr = k1;
+  const int64_t d = X.nc, f = H.nc;
+  const int tiles = (int)((d + kBm - 1) / kBm * ((f + kBn - 1) / kBn));  // of each of the first two
+  const int which = min((int)blockIdx.x / tiles, 2), x = blockIdx.x - which * tiles;
+  Mat A = which < 2 ? X : H, B = which == 0 ? dG : which == 1 ? dU : dY;
+  const int ct = (int)((B.nc + kBn - 1) / kBn);
+  const int64_t m0 = (int64_t)(x / ct) * kBm, c0 = (int64_t)(x % ct) * kBn;
+  const int64_t k1 = min(X.nr, (int64_t)(blockIdx.y + 1) * rows);
+  A.nr = B.nr = k1;
   Acc acc;
   acc.zero();
-  for (int64_t k0 = (int64_t)blockIdx.z * rows; k0 < k1; k0 += kBk) {
-    stage<kBm, false>(As, Ae, m0, k0);
-    stage<kBn, false>(Bs, Be, c0, k0);
+  Piece<kBm, false> pa;
+  Piece<kBn, false> pb;
+  int64_t k0 = (int64_t)blockIdx.y * rows;
+  pa.fetch(A, m0, k0);
+  pb.fetch(B, c0, k0);
+  for (; k0 < k1; k0 += kBk) {
     __syncthreads();
+    pa.put(As);
+    pb.put(Bs);
+    __syncthreads();
+    if (k0 + kBk < k1) {
+      pa.fetch(A, m0, k0 + kBk);
+      pb.fetch(B, c0, k0 + kBk);
+    }
     mul(As, Bs, acc);
-    __syncthreads();
   }
   const int64_t col = c0 + threadIdx.x % 16 * 4;
   if (col >= B.nc) return;
-  float* out = part + blockIdx.z * A.nc * B.nc;
+  float* out = part + (blockIdx.y * 3 + which) * d * f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t m = m0 + acc_row(i);
@@ -201,10 +250,12 @@ __global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat A, Mat B, int64_t row
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-// Splits of the rows: tiles enough for two waves, none shorter than 256 rows.
+// Splits of the rows: tiles enough for two rounds of three blocks an SM, none shorter than 128 rows.
+int wg_tiles(int d, int f) {
+  return (int)(2 * ceil_div(d, kBm) * ceil_div(f, kBn) + ceil_div(f, kBm) * ceil_div(d, kBn));
+}
 int wg_splits(int64_t n, int d, int f) {
-  const int64_t tiles = ceil_div(d, kBm) * ceil_div(f, kBn);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(2 * kSms, tiles), n / 256));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(6 * kSms, wg_tiles(d, f)), n / 128));
 }
 
 struct FfnLayout {
@@ -212,7 +263,6 @@ struct FfnLayout {
   float* dG;
   float* dU;
   float* part;
-  float* tmp;
 };
 
 void carve_simt(void* scratch, const hg_ffn_params* p, int64_t n, bool bwd, FfnLayout* L, size_t* bytes) {
@@ -224,8 +274,7 @@ void carve_simt(void* scratch, const hg_ffn_params* p, int64_t n, bool bwd, FfnL
     L->dG = k.take<float>(nf);
     L->dU = k.take<float>(nf);
     const int sp = wg_splits(n, p->d, p->f);
-    L->part = k.take<float>((size_t)sp * p->d * p->f);
-    L->tmp = k.take<float>(reduce_tmp_floats(sp, (int64_t)p->d * p->f));
+    L->part = k.take<float>((size_t)sp * 3 * p->d * p->f);
   }
   if (bytes) *bytes = k.used;
 }
@@ -249,16 +298,6 @@ hg_status hidden_act(const hg_ffn_params* p, const void* X, int64_t n, const voi
   return hidden<HG_ACT_NONE, kBwd>(p, X, n, dY, L, s);
 }
 
-hg_status wgrad(const float* A, int64_t mc, const float* B, int64_t nc, int64_t n, const FfnLayout& L, int splits,
-                float* out, cudaStream_t s) {
-  const Mat a{A, mc, n, mc}, b{B, nc, n, nc};
-  const int64_t rows = (int64_t)align_up((size_t)ceil_div(n, splits), kBk);
-  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt,
-                dim3((unsigned)ceil_div(nc, kBn), (unsigned)ceil_div(mc, kBm), (unsigned)splits), dim3(kThr), 0, s, a,
-                b, rows, L.part));
-  return reduce_partials(L.part, mc * nc, splits, mc * nc, out, L.tmp, s);
-}
-
 hg_status fwd_simt(const hg_ffn_params* p, const void* X, int64_t n, void* Y, const FfnLayout& L, cudaStream_t s) {
   const int64_t d = p->d, f = p->f;
   HG_TRY((hidden_act<false>(p, X, n, nullptr, L, s)));
@@ -279,9 +318,11 @@ hg_status bwd_simt(const hg_ffn_params* p, const void* X, int64_t n, const void*
   }
   if (!g) return HG_OK;
   const int sp = wg_splits(n, p->d, p->f);
-  HG_TRY(wgrad((const float*)X, d, L.dG, f, n, L, sp, g->dW_gate, s));
-  HG_TRY(wgrad((const float*)X, d, L.dU, f, n, L, sp, g->dW_up, s));
-  return wgrad(L.H, f, (const float*)dY, d, n, L, sp, g->dW_down, s);
+  const Mat x{(const float*)X, d, n, d}, dg{L.dG, f, n, f}, du{L.dU, f, n, f}, h{L.H, f, n, f},
+      dy{(const float*)dY, d, n, d};
+  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt, dim3((unsigned)wg_tiles(p->d, p->f), (unsigned)sp), dim3(kThr), 0, s, x,
+                dg, du, h, dy, (int64_t)align_up((size_t)ceil_div(n, sp), kBk), L.part));
+  return ffn_sum_shares(L.part, sp, d * f, g, s);
 }
 
 size_t scratch_bytes(const hg_ffn_params* p, int64_t n, bool bwd) {

@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(256) ffn_pack_weights(const __nv_bfloat16* __r
 }
 
 // out = the shares' sums in order: 32 float4 columns x 8 runs of shares a block, then the runs in order.
-__global__ void __launch_bounds__(256) ffn_sum_shares(const float* __restrict__ part, int splits, int64_t df,
+__global__ void __launch_bounds__(256) ffn_sum_shares_kernel(const float* __restrict__ part, int splits, int64_t df,
                                                       float* __restrict__ o0, float* __restrict__ o1,
                                                       float* __restrict__ o2) {
   pdl_begin();
@@ -732,8 +732,7 @@ hg_status wg_t(const hg_ffn_params* w, const void* X, int64_t n, const void* dY,
   HG_TRY(launch("ffn_wgrad_tc", ffn_wgrad_tc_kernel<D, kAct>, dim3((unsigned)(chunks * splits)), dim3(kThreads),
                 C::kSmem, s, tm_X, tm_dY, tm_Wt, tm_W, p));
   const int64_t df = (int64_t)D * w->f;
-  return launch("ffn_sum_shares", ffn_sum_shares, dim3((unsigned)ceil_div(3 * df, 128)), dim3(256), 0, s,
-                (const float*)L.part, splits, df, g->dW_gate, g->dW_up, g->dW_down);
+  return ffn_sum_shares(L.part, splits, df, g, s);
 }
 
 template <int D, int kAct>
@@ -756,6 +755,11 @@ hg_status bwd_d(const hg_ffn_params* w, const void* X, int64_t n, const void* dY
 }
 
 }  // namespace
+
+hg_status ffn_sum_shares(const float* part, int splits, int64_t df, const hg_ffn_grads* g, cudaStream_t s) {
+  return launch("ffn_sum_shares", ffn_sum_shares_kernel, dim3((unsigned)ceil_div(3 * df, 128)), dim3(256), 0, s, part,
+                splits, df, g->dW_gate, g->dW_up, g->dW_down);
+}
 
 size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n) {
   WgLayout L;

@@ -26,6 +26,8 @@ hg_status ffn_fwd_tc(const hg_ffn_params* w, const void* X, int64_t n, void* Y, 
 // dX null or g null: that part is left out
 hg_status ffn_bwd_tc(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
                      void* scratch, cudaStream_t s);
+// the weights' gradients from the row shares' sums, part[splits] = [dW_gate | dW_up | dW_down] of df values each
+hg_status ffn_sum_shares(const float* part, int splits, int64_t df, const hg_ffn_grads* g, cudaStream_t s);
 size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n);
 
 __device__ __forceinline__ void st16_issue(uint32_t taddr, const float* v) {
