@@ -64,40 +64,58 @@ struct Piece {
   }
 };
 
+// A thread's 8 x 4 sums; rows 2 i and 2 i + 1 lie in one register pair, for the FMA of two.
 struct Acc {
-  float v[8][4];
+  float2 v[4][4];
   __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) v[i][j] = make_float2(0.f, 0.f);
   }
+  __device__ __forceinline__ float at(int i, int j) const { return i & 1 ? v[i >> 1][j].y : v[i >> 1][j].x; }
 };
 
 // thread (ty, tx) holds rows ty * 4 + {0..3}, 64 + ty * 4 + {0..3} and columns tx * 4 + {0..3}
 __device__ __forceinline__ int acc_row(int i) { return (i < 4 ? 0 : 64) + (threadIdx.x / 16) * 4 + (i & 3); }
 
-__device__ __forceinline__ void mul(const float* A, const float* B, Acc& acc) {
+__device__ __forceinline__ void fma2(float2& c, float2 a, float b) {
+  asm("{\n\t.reg .b64 x, y, z;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%0, %1};\n\t"
+      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "+f"(c.x), "+f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b));
+}
+
+// acc += A B, and acc2 += A B2: an operand of both is read once
+__device__ __forceinline__ void mul(const float* A, const float* B, Acc& acc, const float* B2 = nullptr,
+                                    Acc* acc2 = nullptr) {
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
 #pragma unroll
   for (int k = 0; k < kBk; ++k) {
     const float4 a0 = *reinterpret_cast<const float4*>(A + k * (kBm + 4) + ty * 4);
     const float4 a1 = *reinterpret_cast<const float4*>(A + k * (kBm + 4) + 64 + ty * 4);
-    const float4 b = *reinterpret_cast<const float4*>(B + k * (kBn + 4) + tx * 4);
-    const float av[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
-    const float bv[4] = {b.x, b.y, b.z, b.w};
+    const float2 av[4] = {{a0.x, a0.y}, {a0.z, a0.w}, {a1.x, a1.y}, {a1.z, a1.w}};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int t = 0; t < 2; ++t) {
+      if (t && !B2) break;
+      const float4 b = *reinterpret_cast<const float4*>((t ? B2 : B) + k * (kBn + 4) + tx * 4);
+      const float bv[4] = {b.x, b.y, b.z, b.w};
+      Acc& c = t ? *acc2 : acc;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc.v[i][j] = fmaf(av[i], bv[j], acc.v[i][j]);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fma2(c.v[i][j], av[i], bv[j]);
+    }
   }
 }
 
 // H = act(X W_gate) * (X W_up), a tile a block, the column tiles of a row tile one after another; with kBwd also
 // dH = dY W_down^T, and dG, dU.
 template <int kAct, bool kBwd>
-__global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, Mat dY, Mat Wd, float* __restrict__ H, float* __restrict__ dG,
-                                                        float* __restrict__ dU) {
+__global__ void __launch_bounds__(kThr, kBwd ? 1 : 2)
+    ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, Mat dY, Mat Wd, float* __restrict__ H, float* __restrict__ dG,
+                    float* __restrict__ dU) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)], Cs[kBk * (kBn + 4)];
   __shared__ __align__(16) float Ds[kBwd ? kBk * (kBm + 4) : 4], Es[kBwd ? kBk * (kBn + 4) : 4];
@@ -131,8 +149,7 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, M
     }
     __syncthreads();
     if (k0 + kBk < X.nc) fetch(k0 + kBk);
-    mul(As, Bs, g);
-    mul(As, Cs, u);
+    mul(As, Bs, g, Cs, &u);
     if (kBwd) mul(Ds, Es, h);
   }
   const int64_t col = c0 + threadIdx.x % 16 * 4;
@@ -146,12 +163,12 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, M
     for (int j = 0; j < 4; ++j) {
       if (kBwd) {
         float d;
-        const float a = gate_grad<kAct>(g.v[i][j], &d);
-        hv[j] = a * u.v[i][j];
-        gv[j] = h.v[i][j] * u.v[i][j] * d;
-        uv[j] = h.v[i][j] * a;
+        const float a = gate_grad<kAct>(g.at(i, j), &d);
+        hv[j] = a * u.at(i, j);
+        gv[j] = h.at(i, j) * u.at(i, j) * d;
+        uv[j] = h.at(i, j) * a;
       } else {
-        hv[j] = gate<kAct>(g.v[i][j]) * u.v[i][j];
+        hv[j] = gate<kAct>(g.at(i, j)) * u.at(i, j);
       }
     }
     const int64_t at = row * Wg.nc + col;
@@ -165,7 +182,7 @@ __global__ void __launch_bounds__(kThr) ffn_hidden_simt(Mat X, Mat Wg, Mat Wu, M
 
 // out = A B (+ A2 B2) (+ add): the second product when A2.p is set; kTransB: B given by its transpose.
 template <bool kTransB>
-__global__ void __launch_bounds__(kThr) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B2, const float* add,
+__global__ void __launch_bounds__(kThr, 3) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B2, const float* add,
                                                      float* __restrict__ out, int64_t nc) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
@@ -200,12 +217,12 @@ __global__ void __launch_bounds__(kThr) ffn_out_simt(Mat A, Mat B, Mat A2, Mat B
     const int64_t at = row * nc + col;
     const float4 x = add ? *reinterpret_cast<const float4*>(add + at) : make_float4(0.f, 0.f, 0.f, 0.f);
     *reinterpret_cast<float4*>(out + at) =
-        make_float4(acc.v[i][0] + x.x, acc.v[i][1] + x.y, acc.v[i][2] + x.z, acc.v[i][3] + x.w);
+        make_float4(acc.at(i, 0) + x.x, acc.at(i, 1) + x.y, acc.at(i, 2) + x.z, acc.at(i, 3) + x.w);
   }
 }
 
 // part[blockIdx.y] = [X^T dG | X^T dU | H^T dY] over the split's rows, a tile a block.
-__global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat X, Mat dG, Mat dU, Mat H, Mat dY, int64_t rows,
+__global__ void __launch_bounds__(kThr, 3) ffn_wgrad_simt(Mat X, Mat dG, Mat dU, Mat H, Mat dY, int64_t rows,
                                                        float* __restrict__ part) {
   pdl_begin();
   __shared__ __align__(16) float As[kBk * (kBm + 4)], Bs[kBk * (kBn + 4)];
@@ -243,7 +260,7 @@ __global__ void __launch_bounds__(kThr) ffn_wgrad_simt(Mat X, Mat dG, Mat dU, Ma
     const int64_t m = m0 + acc_row(i);
     if (m < A.nc)
       *reinterpret_cast<float4*>(out + m * B.nc + col) =
-          make_float4(acc.v[i][0], acc.v[i][1], acc.v[i][2], acc.v[i][3]);
+          make_float4(acc.at(i, 0), acc.at(i, 1), acc.at(i, 2), acc.at(i, 3));
   }
 }
 
