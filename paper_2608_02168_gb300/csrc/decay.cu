@@ -13,6 +13,7 @@
 //
 // The step reads and writes the state once (16-byte rows of it across the lanes): bound by HBM.
 #include <algorithm>
+#include <initializer_list>
 
 #include "decay_kernels.cuh"
 
@@ -313,7 +314,7 @@ hg_status check_params(const hg_decay_params* p, int64_t n, int64_t T) {
     return HG_ERR_UNSUPPORTED;
   }
   HG_REQUIRE(p->heads >= 1 && p->heads <= kMaxHeads, "heads must be in [1, %d]", kMaxHeads);
-  HG_REQUIRE(n >= 0 && n * p->heads < (int64_t(1) << 28), "n * heads must be in [0, 2^28)");
+  HG_REQUIRE(n >= 0 && n < (int64_t(1) << 28) && n * p->heads < (int64_t(1) << 28), "n * heads must be in [0, 2^28)");
   HG_REQUIRE(T >= 0 && T < (int64_t(1) << 30), "T must be in [0, 2^30)");
   return HG_OK;
 }
@@ -328,9 +329,17 @@ hg_status check_seq(const hg_seq* r, const char* name, int64_t n, int64_t T, int
              "%s: stride_n must be a non-negative multiple of 16 bytes", name);
   if (written) {  // rows nest: positions within sequences, or sequences within positions
     const bool ok_t = T < 2 || st >= width, ok_n = n < 2 || sn >= width;
-    const bool nest = n < 2 || T < 2 || sn >= (T - 1) * st + width || st >= (n - 1) * sn + width;
+    // sn >= (T - 1) st + width, or st >= (n - 1) sn + width, without the products, which may pass 64 bits
+    const bool nest = n < 2 || T < 2 || (sn >= width && st <= (sn - width) / (T - 1)) ||
+                      (st >= width && sn <= (st - width) / (n - 1));
     HG_REQUIRE(ok_t && ok_n && nest, "%s: rows that are written must not overlap", name);
   }
+  return HG_OK;
+}
+
+// Rows that are written start at none of the rows that are read.
+hg_status check_apart(const hg_seq* out, const char* name, std::initializer_list<const hg_seq*> in) {
+  for (const hg_seq* r : in) HG_REQUIRE(out->p != r->p, "%s must not overlap an input", name);
   return HG_OK;
 }
 
@@ -346,6 +355,7 @@ ScanRows rows_of(const hg_seq* r, int64_t n, int64_t T) {
 }
 
 size_t seg_bytes(const hg_decay_params* p, int64_t n, int64_t T) {
+  if (n == 0) return 0;
   int nseg;
   int64_t seg_len;
   plan_segments(p, n, T, &nseg, &seg_len);
@@ -399,6 +409,7 @@ extern "C" hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q
     HG_TRY(check_seq(k, "k", n, T, w, esz, false));
     HG_TRY(check_seq(v, "v", n, T, w, esz, false));
     HG_TRY(check_seq(o, "o", n, T, w, esz, true));
+    HG_TRY(check_apart(o, "o", {q, k, v}));
     a.q = rows_of(q, n, T);
     a.k = rows_of(k, n, T);
     a.v = rows_of(v, n, T);
@@ -441,6 +452,9 @@ extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q
     HG_TRY(check_seq(dq, "dq", n, T, w, esz, true));
     HG_TRY(check_seq(dk, "dk", n, T, w, esz, true));
     HG_TRY(check_seq(dv, "dv", n, T, w, esz, true));
+    HG_TRY(check_apart(dq, "dq", {q, k, v, d_o, dk, dv}));
+    HG_TRY(check_apart(dk, "dk", {q, k, v, d_o, dv}));
+    HG_TRY(check_apart(dv, "dv", {q, k, v, d_o}));
     rq = rows_of(q, n, T);
     rk = rows_of(k, n, T);
     rv = rows_of(v, n, T);
@@ -527,6 +541,7 @@ extern "C" hg_status hg_decay_step(const hg_decay_params* params, const hg_rows*
     HG_REQUIRE(in[x] != nullptr, "%s must be non-null", names[x]);
     const hg_seq r{in[x]->p, in[x]->stride, 0};
     HG_TRY(check_seq(&r, names[x], n, 1, w, esz, x == 3));
+    HG_REQUIRE(x == 3 || !o || in[x]->p != o->p, "o must not overlap an input");
   }
   HG_REQUIRE(S_in && S_out, "S_in and S_out must be non-null");
   HG_REQUIRE((((uintptr_t)S_in | (uintptr_t)S_out) & 15) == 0, "S_in and S_out must be 16-byte aligned");

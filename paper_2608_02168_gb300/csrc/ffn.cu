@@ -364,6 +364,14 @@ hg_status check_params(const hg_ffn_params* p, int64_t n) {
   return HG_OK;
 }
 
+// Two arrays of n x d values share no byte.
+hg_status check_apart(const hg_ffn_params* p, int64_t n, const void* out, const void* in, const char* names) {
+  const size_t bytes = (size_t)n * p->d * (p->dtype == HG_BF16 ? 2 : 4);
+  const uintptr_t a = (uintptr_t)out, b = (uintptr_t)in;
+  HG_REQUIRE(a >= b + bytes || b >= a + bytes, "%s must not overlap", names);
+  return HG_OK;
+}
+
 hg_status check_weights(const hg_ffn_params* p) {
   HG_REQUIRE(p->W_gate && p->W_up && p->W_down, "every weight pointer must be non-null");
   HG_REQUIRE((((uintptr_t)p->W_gate | (uintptr_t)p->W_up | (uintptr_t)p->W_down) & 15) == 0,
@@ -395,6 +403,7 @@ extern "C" hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int6
   if (n == 0) return HG_OK;
   HG_REQUIRE(X && Y && (scratch || params->dtype == HG_BF16), "X, Y and scratch must be non-null");
   HG_REQUIRE((((uintptr_t)X | (uintptr_t)Y) & 15) == 0, "X and Y must be 16-byte aligned");
+  HG_TRY(check_apart(params, n, Y, X, "Y and X"));
   HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (params->dtype == HG_BF16) return ffn_fwd_tc(params, X, n, Y, s);
@@ -424,6 +433,10 @@ extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int6
   }
   HG_REQUIRE(X && dY && scratch, "X, dY and scratch must be non-null");
   HG_REQUIRE((((uintptr_t)X | (uintptr_t)dY | (uintptr_t)dX) & 15) == 0, "X, dY and dX must be 16-byte aligned");
+  if (dX) {
+    HG_TRY(check_apart(params, n, dX, X, "dX and X"));
+    HG_TRY(check_apart(params, n, dX, dY, "dX and dY"));
+  }
   HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
   if (!dX && !grads) return HG_OK;
   if (params->dtype == HG_BF16) return ffn_bwd_tc(params, X, n, dY, dX, grads, scratch, s);

@@ -102,9 +102,18 @@ struct Issuer {
           "h"((uint16_t)3)
           : "memory");
   }
+  // After a give-up: the products issued so far end (the arrival is this CTA's alone: the other one may be gone).
   __device__ __forceinline__ void drain(uint64_t* bar) const {
-    commit(bar);
-    if (lead) tc::mbar_wait(bar, 0);
+    if (!lead) return;
+    if constexpr (CL == 1)
+      tc::mma_commit(bar);
+    else
+      asm volatile(
+          "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+              tc::smem_u32(bar)),
+          "h"((uint16_t)1)
+          : "memory");
+    tc::mbar_wait(bar, 0);
   }
 
   // The other roles of the CTAs.
@@ -115,6 +124,7 @@ struct Issuer {
     return r;
   }
   static __device__ __forceinline__ void sync_all() {
+    __syncwarp();
     if constexpr (CL == 1)
       __syncthreads();
     else

@@ -16,6 +16,7 @@
 // written once.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "hg_internal.cuh"
 
@@ -271,6 +272,14 @@ hg_status check_rows(const hg_rows* r, const char* name, int64_t n, int64_t widt
   return HG_OK;
 }
 
+// An output may be its own input, rows at the same places; it starts at no other array's rows.
+hg_status check_apart(const hg_rows* out, const hg_rows* own, const char* name, int64_t n,
+                      std::initializer_list<const hg_rows*> others) {
+  HG_REQUIRE(out->p != own->p || n < 2 || out->stride == own->stride, "%s: in place, the strides must agree", name);
+  for (const hg_rows* r : others) HG_REQUIRE(!r || out->p != r->p, "%s must not overlap another array", name);
+  return HG_OK;
+}
+
 size_t rot_scratch(const hg_qkrot_params* p, int64_t n) {
   return align_up(sizeof(float) * 2 * p->d_h *
                   (size_t)rot_grid(std::max<int64_t>(n, 1), p->heads_q + p->heads_k, p->d_h, p->dtype, true));
@@ -319,6 +328,10 @@ extern "C" hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* 
   if (wk) {
     HG_TRY(check_rows(k, "k", n, wk, esz, false));
     HG_TRY(check_rows(k_out, "k_out", n, wk, esz, true));
+    HG_TRY(check_apart(q_out, q, "q_out", n, {k, k_out}));
+    HG_TRY(check_apart(k_out, k, "k_out", n, {q}));
+  } else {
+    HG_TRY(check_apart(q_out, q, "q_out", n, {}));
   }
   RotArgs a;
   fill_args(&a, params, pos, n);
@@ -353,6 +366,10 @@ extern "C" hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* 
     HG_TRY(check_rows(k, "k", n, wk, esz, false));
     HG_TRY(check_rows(dk_out, "dk_out", n, wk, esz, false));
     HG_TRY(check_rows(dk, "dk", n, wk, esz, true));
+    HG_TRY(check_apart(dq, dq_out, "dq", n, {q, k, dk_out, dk}));
+    HG_TRY(check_apart(dk, dk_out, "dk", n, {q, k, dq_out}));
+  } else {
+    HG_TRY(check_apart(dq, dq_out, "dq", n, {q}));
   }
   HG_REQUIRE(scratch != nullptr && ((uintptr_t)scratch & 255) == 0, "scratch must be non-null and 256-byte aligned");
   RotArgs a;

@@ -252,3 +252,71 @@ def test_binding_refuses_shapes_types_and_host_tensors(hg):
     with pytest.raises(ValueError, match="bytes are needed"):
         hg._work_ptr(None, 16, "scratch")
     assert hg._work_ptr(None, 0, "scratch") is None
+
+
+def test_arrays_that_share_memory_are_refused(hg):
+    """Outputs that start at another array's rows, each call's arrays far apart but for the one named."""
+    so = hg.lib()
+    P = [A + (i << 24) for i in range(8)]
+
+    def refused(status):
+        return status == 1 and b"overlap" in so.hg_last_error()
+
+    qp = ctypes.byref(hg.hg_qkrot_params(4, 4, 32, 32, 0, 1, 1e-6, 1e4, None, None))
+
+    def rot(q, k, qo, ko, so_stride=128):
+        return so.hg_qkrot_fwd(qp, rows(hg, q), rows(hg, k), None, 10, rows(hg, qo, so_stride), rows(hg, ko), None)
+
+    assert refused(rot(P[0], P[1], P[1], P[3])) and refused(rot(P[0], P[1], P[2], P[0]))
+    assert refused(rot(P[0], P[1], P[2], P[2]))
+    assert rot(P[0], P[1], P[0], P[3], so_stride=256) == 1 and b"in place" in so.hg_last_error()
+
+    def rot_bwd(q, k, dqo, dko, dq, dk):
+        r = [rows(hg, x) for x in (q, k, dqo, dko, dq, dk)]
+        return so.hg_qkrot_bwd(qp, r[0], r[1], None, 10, *r[2:], None, None, A, None)
+
+    assert refused(rot_bwd(*P[:4], P[0], P[5])) and refused(rot_bwd(*P[:4], P[4], P[1]))
+    assert refused(rot_bwd(*P[:4], P[3], P[5])) and refused(rot_bwd(*P[:4], P[4], P[4]))
+
+    dp = ctypes.byref(hg.hg_decay_params(4, 32, 1, 1.0, A))
+    for i in range(3):
+        s = [seq(hg, x) for x in P[:3]]
+        assert refused(so.hg_decay_fwd(dp, *s, None, 3, 5, None, seq(hg, P[i]), None, None, None))
+        r = [rows(hg, x) for x in P[:3]]
+        assert refused(so.hg_decay_step(dp, *r, None, 3, A, rows(hg, P[i]), A, None))
+    for i, j in ((4, 0), (5, 1), (6, 2), (4, 3), (5, 4), (6, 5)):
+        p = P[:7]
+        p[i] = P[j]
+        s = [seq(hg, x) for x in p]
+        assert refused(so.hg_decay_bwd(dp, *s[:3], None, 3, 5, None, s[3], None, *s[4:], None, None, None))
+
+    fp = ctypes.byref(hg.hg_ffn_params(64, 96, 1, 3, 1, A, A, A))
+    last = 9 * 128  # bytes to the last of ten rows
+    for y in (P[1], P[1] + last, P[1] - last):
+        assert refused(so.hg_ffn_fwd(fp, P[1], 10, y, A, None))
+        assert refused(so.hg_ffn_bwd(fp, P[1], 10, P[2], y, None, A, None))
+        assert refused(so.hg_ffn_bwd(fp, P[2], 10, P[1], y, None, A, None))
+
+
+def test_decay_sizes_that_pass_64_bits_are_refused(hg):
+    so = hg.lib()
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    p = ctypes.byref(hg.hg_decay_params(64, 32, 1, 1.0, A))
+    assert so.hg_decay_workspace_size(p, 1 << 58, 5, ctypes.byref(f), ctypes.byref(b)) == 1
+    # rows of the two sequences meet: the span of one, (T - 1) stride_t, is 2^66 values
+    far = seq(hg, A + (1 << 30), sn=1 << 39, st=1 << 38)
+    s = seq(hg)
+    T = (1 << 28) + 1
+    scratch = A
+    assert so.hg_decay_fwd(p, s, s, s, None, 2, T, None, far, None, scratch, None) == 1
+    assert b"overlap" in so.hg_last_error()
+
+
+def test_decay_of_no_sequences_needs_no_scratch(hg):
+    so = hg.lib()
+    f, b = ctypes.c_size_t(1), ctypes.c_size_t(1)
+    p = ctypes.byref(hg.hg_decay_params(4, 32, 1, 1.0, A))
+    assert so.hg_decay_workspace_size(p, 0, 500, ctypes.byref(f), ctypes.byref(b)) == 0
+    assert f.value == b.value == 0
+    null = ctypes.POINTER(hg.hg_seq)()
+    assert so.hg_decay_fwd(p, null, null, null, None, 0, 500, None, null, None, None, None) == 0
