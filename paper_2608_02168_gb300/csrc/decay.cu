@@ -150,9 +150,11 @@ __global__ void __launch_bounds__(32 * kWarps) scan_simt(ScanArgs a) {
   }
 }
 
-// seg[s] (segment s's own state, for s < nseg - 1) -> the state at segment s's start: one thread an element.
-__global__ void __launch_bounds__(256) scan_join(ScanArgs a, int dh) {
+// seg[s] (segment s's own state, for s < nseg - 1) -> the state at segment s's start: one thread an element,
+// blockIdx.y the scan.
+__global__ void __launch_bounds__(256) scan_join(const __grid_constant__ ScanBatch b, int dh) {
   pdl_begin();
+  const ScanArgs& a = b.s[blockIdx.y];
   const int64_t dd = (int64_t)dh * dh, total = a.n * a.heads * dd;
   const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (x >= total) return;
@@ -259,11 +261,11 @@ __global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q
 // Segments: as many as fill the GPU with warps, none shorter than kMinSeg positions, where the second
 // reading of keys and values costs more than the warps gain.
 constexpr int64_t kMinSeg = 256;
-void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int* nseg, int64_t* seg_len) {
+void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int scans, int* nseg, int64_t* seg_len) {
   const bool mma = p->dtype == HG_BF16;
   const int64_t each = mma ? scan_mma_warps(p->heads, p->d_h) : (p->heads * p->d_h + 31) / 32;
   const int64_t full = kSms * (mma ? scan_mma_resident(p->d_h) : 16);
-  const int64_t want = std::min<int64_t>(full / (std::max<int64_t>(n, 1) * each), T / kMinSeg);
+  const int64_t want = std::min<int64_t>(full / (std::max<int64_t>(n, 1) * each * scans), T / kMinSeg);
   *nseg = 1;
   *seg_len = std::max<int64_t>(T, 1);
   if (want < 2) return;
@@ -279,12 +281,15 @@ hg_status scan_simt_t(const ScanArgs& a, bool local, cudaStream_t s) {
   return launch("decay_scan", scan_simt<DH, false>, grid, dim3(32 * kWarps), 0, s, a);
 }
 
-hg_status scan_pass(const ScanArgs& a, const hg_decay_params* p, bool local, cudaStream_t s) {
-  if (p->dtype == HG_BF16) return scan_mma(a, p->d_h, local, s);
-  if (p->d_h == 16) return scan_simt_t<16>(a, local, s);
-  if (p->d_h == 32) return scan_simt_t<32>(a, local, s);
-  if (p->d_h == 64) return scan_simt_t<64>(a, local, s);
-  return scan_simt_t<128>(a, local, s);
+hg_status scan_pass(const ScanBatch& b, const hg_decay_params* p, bool local, cudaStream_t s) {
+  if (p->dtype == HG_BF16) return scan_mma(b, p->d_h, local, s);
+  for (int i = 0; i < b.count; ++i) {
+    if (p->d_h == 16) HG_TRY(scan_simt_t<16>(b.s[i], local, s));
+    if (p->d_h == 32) HG_TRY(scan_simt_t<32>(b.s[i], local, s));
+    if (p->d_h == 64) HG_TRY(scan_simt_t<64>(b.s[i], local, s));
+    if (p->d_h == 128) HG_TRY(scan_simt_t<128>(b.s[i], local, s));
+  }
+  return HG_OK;
 }
 
 // Scratch: counters of the claimed items, one for each launch of a call, then the segments' states.
@@ -294,16 +299,23 @@ constexpr int kClaims = 8;
 constexpr int64_t kClaimT = 128;
 bool scan_claims(const hg_decay_params* p, int64_t T) { return p->dtype == HG_BF16 && T >= kClaimT; }
 
-hg_status scan(ScanArgs& a, const hg_decay_params* p, cudaStream_t s) {
+// The scans [first, first + count) of a call, side by side.
+hg_status scan(const ScanArgs* first, int count, uint32_t*& claims, const hg_decay_params* p, cudaStream_t s) {
+  ScanBatch b{};
+  b.count = count;
+  auto pass = [&](bool local) -> hg_status {
+    for (int i = 0; i < count; ++i) b.s[i].claims = claims;
+    if (claims) ++claims;
+    return scan_pass(b, p, local, s);
+  };
+  for (int i = 0; i < count; ++i) b.s[i] = first[i];
+  const ScanArgs& a = b.s[0];
   if (a.nseg > 1) {
-    HG_TRY(scan_pass(a, p, true, s));
-    if (a.claims) ++a.claims;
-    HG_TRY(launch("decay_scan_join", scan_join,
-                  dim3((unsigned)ceil_div(a.n * a.heads * (int64_t)p->d_h * p->d_h, 256)), dim3(256), 0, s, a, p->d_h));
+    HG_TRY(pass(true));
+    const unsigned blocks = (unsigned)ceil_div(a.n * a.heads * (int64_t)p->d_h * p->d_h, 256);
+    HG_TRY(launch("decay_scan_join", scan_join, dim3(blocks, (unsigned)count), dim3(256), 0, s, b, p->d_h));
   }
-  HG_TRY(scan_pass(a, p, false, s));
-  if (a.claims) ++a.claims;
-  return HG_OK;
+  return pass(false);
 }
 
 hg_status check_params(const hg_decay_params* p, int64_t n, int64_t T) {
@@ -354,27 +366,35 @@ ScanRows rows_of(const hg_seq* r, int64_t n, int64_t T) {
   return {r->p, n < 2 ? 0 : r->stride_n, T < 2 ? 0 : r->stride_t};
 }
 
-size_t seg_bytes(const hg_decay_params* p, int64_t n, int64_t T) {
-  if (n == 0) return 0;
+// Scratch of a call's scans: the counters, then each scan's states.
+struct ScanLayout {
   int nseg;
   int64_t seg_len;
-  plan_segments(p, n, T, &nseg, &seg_len);
-  const size_t states = nseg > 1 ? align_up(sizeof(float) * (size_t)n * p->heads * nseg * p->d_h * p->d_h) : 0;
-  return states + (scan_claims(p, T) ? 256 : 0);
+  uint32_t* claims;
+  float* seg[3];
+};
+size_t carve_scans(void* scratch, const hg_decay_params* p, int64_t n, int64_t T, int scans, ScanLayout* L) {
+  *L = ScanLayout{};
+  plan_segments(p, n, T, scans, &L->nseg, &L->seg_len);
+  if (n == 0) return 0;
+  Carve c(scratch);
+  if (scan_claims(p, T)) L->claims = c.take<uint32_t>(kClaims);
+  const size_t states = L->nseg > 1 ? (size_t)n * p->heads * L->nseg * p->d_h * p->d_h : 0;
+  for (int i = 0; i < scans && states; ++i) L->seg[i] = c.take<float>(states);
+  return c.used;
 }
 
-// The scan's part of a call's scratch; counters zeroed.
-hg_status carve_scan(ScanArgs* a, const hg_decay_params* p, void* scratch, cudaStream_t s) {
-  Carve c(scratch);
-  if (scan_claims(p, a->T)) {
-    uint32_t* claims = c.take<uint32_t>(kClaims);
-    if (a->lens) {
-      HG_CUDA(cudaMemsetAsync(claims, 0, sizeof(uint32_t) * kClaims, s));
-      a->claims = claims;
-    }
+// The scans' part of a call: counters zeroed where the lengths are ragged.
+hg_status lay_out(ScanArgs* a, int scans, uint32_t** claims, const hg_decay_params* p, void* scratch, cudaStream_t s) {
+  ScanLayout L;
+  carve_scans(scratch, p, a->n, a->T, scans, &L);
+  for (int i = 0; i < scans; ++i) {
+    a[i].seg = L.seg[i];
+    a[i].nseg = L.nseg;
+    a[i].seg_len = L.seg_len;
   }
-  a->seg = c.take<float>(0);
-  plan_segments(p, a->n, a->T, &a->nseg, &a->seg_len);
+  *claims = a->lens ? L.claims : nullptr;
+  if (*claims) HG_CUDA(cudaMemsetAsync(*claims, 0, sizeof(uint32_t) * kClaims, s));
   return HG_OK;
 }
 
@@ -388,7 +408,9 @@ extern "C" hg_status hg_decay_workspace_size(const hg_decay_params* params, int6
   clear_error();
   HG_REQUIRE(fwd_bytes && bwd_bytes, "fwd_bytes and bwd_bytes must be non-null");
   HG_TRY(check_params(params, n, T));
-  *fwd_bytes = *bwd_bytes = seg_bytes(params, n, T);
+  ScanLayout L;
+  *fwd_bytes = carve_scans(nullptr, params, n, T, 1, &L);
+  *bwd_bytes = carve_scans(nullptr, params, n, T, 3, &L);
   return HG_OK;
 }
 
@@ -398,7 +420,8 @@ extern "C" hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q
   clear_error();
   HG_TRY(device_guard());
   HG_TRY(check_params(params, n, T));
-  const size_t need = seg_bytes(params, n, T);
+  ScanLayout L;
+  const size_t need = carve_scans(nullptr, params, n, T, 1, &L);
   HG_TRY(check_buffers(params, scratch, need > 0));
   if (n == 0) return HG_OK;
   const size_t esz = params->dtype == HG_BF16 ? 2 : 4;
@@ -426,8 +449,9 @@ extern "C" hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q
   a.c_in = 1.f;
   a.c_out = params->scale;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  HG_TRY(carve_scan(&a, params, scratch, s));
-  return scan(a, params, s);
+  uint32_t* claims;
+  HG_TRY(lay_out(&a, 1, &claims, params, scratch, s));
+  return scan(&a, 1, claims, params, s);
 }
 
 extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
@@ -437,7 +461,8 @@ extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q
   clear_error();
   HG_TRY(device_guard());
   HG_TRY(check_params(params, n, T));
-  const size_t need = seg_bytes(params, n, T);
+  ScanLayout L;
+  const size_t need = carve_scans(nullptr, params, n, T, 3, &L);
   HG_TRY(check_buffers(params, scratch, need > 0));
   if (n == 0) return HG_OK;
   const size_t esz = params->dtype == HG_BF16 ? 2 : 4;
@@ -469,37 +494,44 @@ extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q
   a.T = T;
   a.heads = params->heads;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  HG_TRY(carve_scan(&a, params, scratch, s));
-  // dq
-  a.q = ro;
-  a.k = rv;
-  a.v = rk;
-  a.o = gq;
-  a.init = S_in;
-  a.init_t = 1;
-  a.last = nullptr;
-  a.shift = 1;
-  a.c_in = 1.f;
-  a.c_out = params->scale;
-  if (T > 0) HG_TRY(scan(a, params, s));
-  // dk (before dv, whose run may overwrite dS_out with dS_in)
-  a.q = rv;
-  a.k = ro;
-  a.v = rq;
-  a.o = gk;
-  a.init = dS_out;
-  a.shift = 0;
-  a.reverse = 1;
-  a.c_in = params->scale;
-  a.c_out = 1.f;
-  if (T > 0) HG_TRY(scan(a, params, s));
-  a.q = rk;
-  a.k = rq;
-  a.v = ro;
-  a.o = gv;
-  a.init_t = 0;
-  a.last = dS_in;
-  return scan(a, params, s);
+  HG_REQUIRE(!dS_in || dS_in != S_in, "dS_in must not overlap S_in");
+  ScanArgs g[3] = {a, a, a};
+  ScanArgs &aq = g[0], &ak = g[1], &av = g[2];
+  aq.q = ro;  // dq
+  aq.k = rv;
+  aq.v = rk;
+  aq.o = gq;
+  aq.init = S_in;
+  aq.init_t = 1;
+  aq.shift = 1;
+  aq.c_in = 1.f;
+  aq.c_out = params->scale;
+  ak.q = rv;  // dk
+  ak.k = ro;
+  ak.v = rq;
+  ak.o = gk;
+  ak.init = dS_out;
+  ak.init_t = 1;
+  ak.reverse = 1;
+  ak.c_in = params->scale;
+  ak.c_out = 1.f;
+  av.q = rk;  // dv
+  av.k = rq;
+  av.v = ro;
+  av.o = gv;
+  av.init = dS_out;
+  av.last = dS_in;
+  av.reverse = 1;
+  av.c_in = params->scale;
+  av.c_out = 1.f;
+  uint32_t* claims;
+  HG_TRY(lay_out(g, 3, &claims, params, scratch, s));
+  if (T == 0) return scan(&av, 1, claims, params, s);
+  // side by side (three launches: 306 us for 400 histories of up to 515 events, d_h = 64), but dv by itself where it
+  // leaves dS_in in the place of dS_out, which dk reads
+  const int together = dS_in && dS_in == dS_out ? 2 : 3;
+  HG_TRY(scan(g, together, claims, params, s));
+  return together == 3 ? HG_OK : scan(&av, 1, claims, params, s);
 }
 
 namespace hg {

@@ -33,6 +33,12 @@ struct ScanArgs {
   float c_in, c_out;
 };
 
+// Scans over the same sequences (n, T, lens, ld, segments and claims agree), run side by side.
+struct ScanBatch {
+  ScanArgs s[3];
+  int count;
+};
+
 // log_decay as the kernels take it
 __device__ __forceinline__ float clamp_ld(float x) { return x < 0.f ? fmaxf(x, -200.f) : 0.f; }
 
@@ -48,7 +54,7 @@ __device__ __forceinline__ int64_t scan_len(const ScanArgs& a, int64_t i) {
 constexpr float kFrame = 5.f;
 
 // bf16 scan on the tensor cores (decay_mma.cu); local: the segments' own states into a.seg, no rows.
-hg_status scan_mma(const ScanArgs& a, int d_h, bool local, cudaStream_t s);
+hg_status scan_mma(const ScanBatch& b, int d_h, bool local, cudaStream_t s);
 // warps that scan_mma runs for one sequence and segment, and warps that an SM holds
 int scan_mma_warps(int heads, int d_h);
 int scan_mma_resident(int d_h);

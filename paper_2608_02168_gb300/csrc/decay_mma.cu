@@ -34,7 +34,7 @@ constexpr int kSms = 152;
 
 template <int DH>
 struct Cfg {
-  static constexpr int DS = DH < 32 ? DH : 32;       // value features of a warp
+  static constexpr int DS = DH <= 64 ? DH : 32;       // value features of a warp
   static constexpr int SL = DH / DS;                 // slices of a head
   static constexpr int ST = DH == 128 ? 2 : 3;       // chunks in the ring
   static constexpr int W = 4;                        // warps of a CTA
@@ -42,10 +42,11 @@ struct Cfg {
   static constexpr int kQ = kC * kRow, kV = kC * kVRow;
   static constexpr int kStage = 2 * kQ + kV;
   static constexpr int kSmem = W * (ST * kStage + 16);
-  static constexpr int kBlocks = DH == 16 ? 5 : DH == 32 ? 4 : DH == 64 ? 3 : 2;  // resident CTAs of an SM
+  static constexpr int kBlocks = DH == 16 ? 5 : DH == 32 ? 4 : DH == 64 ? 2 : 2;  // resident CTAs of an SM
 };
 
 // Byte offset of 16-byte piece c of row r, N pieces a row.
+// 2 x pieces further on is an XOR with 32 x, for rows' places that begin at a multiple of their size.
 template <int N>
 __device__ __forceinline__ uint32_t piece(int r, int c) {
   constexpr int sh = N == 2 ? 2 : N == 4 ? 1 : 0;
@@ -79,19 +80,21 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 struct Item {
   uint32_t id;  // at or past the number of items: none
   uint32_t seq;
-  int head, slice, segi;
+  int set, head, slice, segi;
   int64_t len, t0, t1;
 };
 
-template <int DH>
-__device__ __forceinline__ void locate(const ScanArgs& a, uint32_t items, uint32_t segs, Item& it) {
+template <int DH, bool kMany>
+__device__ __forceinline__ void locate(const ScanArgs& a, uint32_t items, uint32_t each, uint32_t segs, Item& it) {
   if (it.id >= items) {
     it.t0 = it.t1 = 0;
     return;
   }
   constexpr uint32_t SL = Cfg<DH>::SL;
-  it.slice = (int)(it.id % SL);
-  uint32_t x = it.id / SL;
+  it.set = kMany ? (int)(it.id / each) : 0;
+  const uint32_t id = kMany ? it.id % each : it.id;
+  it.slice = (int)(id % SL);
+  uint32_t x = id / SL;
   it.head = (int)(x % (uint32_t)a.heads);
   x /= (uint32_t)a.heads;
   it.segi = 0;
@@ -136,28 +139,52 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// x (a pair of bf16) times (f0, f1) as a sum of three bf16 pairs
-__device__ __forceinline__ void scale_split(uint32_t x, float f0, float f1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  float y0 = __uint_as_float(x << 16) * f0, y1 = __uint_as_float(x & 0xffff0000u) * f1;
-  hi = pack2_bf16(y0, y1);
-  y0 -= __uint_as_float(hi << 16);
-  y1 -= __uint_as_float(hi & 0xffff0000u);
-  mid = pack2_bf16(y0, y1);
-  lo = pack2_bf16(y0 - __uint_as_float(mid << 16), y1 - __uint_as_float(mid & 0xffff0000u));
+// two products, two differences
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(c.x), "=f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "sub.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(c.x), "=f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 wide(uint32_t x) {
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
 }
 
-template <int DH, bool kLocal>
-__global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_kernel(const __grid_constant__ ScanArgs a) {
+// x (a pair of bf16) times f as a sum of three bf16 pairs
+__device__ __forceinline__ void scale_split(uint32_t x, float2 f, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  float2 y = mul2(wide(x), f);
+  hi = pack2_bf16(y.x, y.y);
+  y = sub2(y, wide(hi));
+  mid = pack2_bf16(y.x, y.y);
+  y = sub2(y, wide(mid));
+  lo = pack2_bf16(y.x, y.y);
+}
+
+// kMany: the items of several scans over the same sequences, scan by scan.
+template <int DH, bool kLocal, bool kMany>
+__global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
+    scan_mma_kernel(const __grid_constant__ ScanBatch batch) {
   pdl_begin();
+  const ScanArgs& all = batch.s[0];  // what the scans have in common
+  auto scan_of = [&](const Item& it) -> const ScanArgs& { return batch.s[kMany ? it.set : 0]; };
   using C = Cfg<DH>;
   constexpr int DS = C::DS, MT = DS / 16, NT = DH / 8, KS = DH / 16, NV = DS / 8, N = DH / 8, ST = C::ST;
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   uint8_t* ring = smem + warp * (ST * C::kStage);
-  const uint32_t segs = kLocal ? a.nseg - 1 : a.nseg;
-  const uint32_t items = (uint32_t)a.n * segs * a.heads * C::SL;
+  const uint32_t segs = kLocal ? all.nseg - 1 : all.nseg;
+  const uint32_t each = (uint32_t)all.n * segs * all.heads * C::SL, items = kMany ? each * batch.count : each;
   const uint32_t stride = gridDim.x * C::W;
-  const int64_t qs = row_step(a.q, a), ks = row_step(a.k, a), vs = row_step(a.v, a), os = row_step(a.o, a);
   // lane addresses inside a tile of 16 x 16 for ldmatrix: rows by lane & 15 / pieces by lane >> 4, and the other order
   const int r16 = lane & 15, c16 = lane >> 4;
   const int r8 = (lane & 7) + ((lane >> 4) << 3), c8 = (lane >> 3) & 1;
@@ -167,26 +194,32 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
   uint32_t* queue = reinterpret_cast<uint32_t*>(smem + C::W * ST * C::kStage) + warp * 4;
   uint32_t queued = 0, taken = 0;
   auto next_id = [&](uint32_t id) -> uint32_t {
-    if (!a.claims) return id + stride;
+    if (!all.claims) return id + stride;
     uint32_t x = 0;
-    if (lane == 0) x = atomicAdd(a.claims, 1u);
+    if (lane == 0) x = atomicAdd(all.claims, 1u);
     x = __shfl_sync(0xffffffffu, x, 0) + stride;
     if (lane == 0) queue[queued & 3] = x;
     ++queued;
     __syncwarp();
     return x;
   };
-  auto follow = [&](uint32_t id) -> uint32_t { return a.claims ? queue[taken++ & 3] : id + stride; };
+  auto follow = [&](uint32_t id) -> uint32_t { return all.claims ? queue[taken++ & 3] : id + stride; };
   Item it{}, nx{};
   it.id = blockIdx.x * C::W + warp;
-  locate<DH>(a, items, segs, it);
+  locate<DH, kMany>(all, items, each, segs, it);
   // The loads run ahead: position nc of item nx is the next chunk to ask for.  An item without positions passes as one
   // empty chunk, so the loads are at most a ring ahead of the arithmetic.
   const uint8_t *qp = nullptr, *kp = nullptr, *vp = nullptr;
-  int64_t nc = 0;
+  int64_t nc = 0, qs = row_step(all.q, all), ks = row_step(all.k, all), vs = row_step(all.v, all);
   auto begin = [&]() {
     nc = nx.t0;
     if (nx.id >= items || nx.t0 >= nx.t1) return;
+    const ScanArgs& a = scan_of(nx);
+    if (kMany) {
+      qs = row_step(a.q, a);
+      ks = row_step(a.k, a);
+      vs = row_step(a.v, a);
+    }
     if (!kLocal) qp = lane_rows<N>(a.q, a, nx, nc, nx.head * DH, lane);
     kp = lane_rows<N>(a.k, a, nx, nc, nx.head * DH, lane);
     vp = lane_rows<NV>(a.v, a, nx, nc, nx.head * DH + nx.slice * DS, lane);
@@ -196,7 +229,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
   auto advance = [&](uint8_t* stage) {
     if (nx.id < items && nc >= max(nx.t1, nx.t0 + 1)) {
       nx.id = next_id(nx.id);
-      locate<DH>(a, items, segs, nx);
+      locate<DH, kMany>(all, items, each, segs, nx);
       begin();
     }
     if (nx.id < items) {
@@ -219,7 +252,9 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
     advance(ring + put * C::kStage);
     put = put + 1 == ST ? 0 : put + 1;
   }
-  for (; it.id < items; it.id = follow(it.id), locate<DH>(a, items, segs, it)) {
+  for (; it.id < items; it.id = follow(it.id), locate<DH, kMany>(all, items, each, segs, it)) {
+    const ScanArgs& a = scan_of(it);
+    const int64_t os = row_step(a.o, a);
     const float ld = clamp_ld(a.ld[it.head]), ld2 = ld * 1.4426950408889634f;
     const int64_t sh = (int64_t)it.seq * a.heads + it.head;
     float F[MT][NT][4];
@@ -279,7 +314,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
 #pragma unroll
       for (int x = 0; x < MT; ++x) {
         uint32_t b[4];
-        ldsm4t(sv + piece<NV>(r16, 2 * x + c16), b);
+        ldsm4t((sv + piece<NV>(r16, c16)) ^ (x * 32), b);
         vt[x][0] = b[0];
         vt[x][2] = b[1];
         vt[x][1] = b[2];
@@ -294,8 +329,8 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           uint32_t qa[4], kb[4];
-          ldsm4(sq + piece<N>(r16, 2 * s + c16), qa);
-          ldsm4(sk + piece<N>(r8, 2 * s + c8), kb);
+          ldsm4((sq + piece<N>(r16, c16)) ^ (s * 32), qa);
+          ldsm4((sk + piece<N>(r8, c8)) ^ (s * 32), kb);
           mma(p0, qa[0], qa[1], qa[2], qa[3], kb[0], kb[1]);
           mma(p1, qa[0], qa[1], qa[2], qa[3], kb[2], kb[3]);
           if (some) {
@@ -313,10 +348,12 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
           const float f0 = a.c_out * ex2(ld2 * x), f1 = a.c_out * ex2(ld2 * (x + 8.f));
 #pragma unroll
           for (int y = 0; y < NV; ++y) {
-            o[y][0] *= f0;
-            o[y][1] *= f0;
-            o[y][2] *= f1;
-            o[y][3] *= f1;
+            const float2 u = mul2(make_float2(o[y][0], o[y][1]), make_float2(f0, f0));
+            const float2 v = mul2(make_float2(o[y][2], o[y][3]), make_float2(f1, f1));
+            o[y][0] = u.x;
+            o[y][1] = u.y;
+            o[y][2] = v.x;
+            o[y][3] = v.y;
           }
         }
         const uint32_t a0 = pack2_bf16(keep0 ? p0[0] * w[0] : 0.f, keep1 ? p0[1] * w[1] : 0.f);
@@ -353,29 +390,36 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
           }
           base = target;
         }
-        float f[4];
+        float2 f[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 2 * t4 + (e & 1) + 8 * (e >> 1);
-          f[e] = r < m ? a.c_in * ex2(ld2 * (float)(base - tau0 - r)) : 0.f;
+        for (int e = 0; e < 2; ++e) {
+          const int r = 2 * t4 + 8 * e;
+          f[e].x = r < m ? a.c_in * ex2(ld2 * (float)(base - tau0 - r)) : 0.f;
+          f[e].y = r + 1 < m ? a.c_in * ex2(ld2 * (float)(base - tau0 - r - 1)) : 0.f;
         }
-        uint32_t hi[MT][4], mid[MT][4], lo[MT][4];
+        constexpr int XB = MT < 2 ? MT : 2;  // groups of 16 value features at a time: registers for their terms
 #pragma unroll
-        for (int x = 0; x < MT; ++x)
+        for (int x0 = 0; x0 < MT; x0 += XB) {
+          uint32_t hi[XB][4], mid[XB][4], lo[XB][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) scale_split(vt[x][e], f[e & 2], f[(e & 2) + 1], hi[x][e], mid[x][e], lo[x][e]);
+          for (int x = 0; x < XB; ++x)
 #pragma unroll
-        for (int y = 0; y < NT; y += 2) {
-          uint32_t kb[4];
-          ldsm4t(sk + piece<N>(r16, y + c16), kb);
+            for (int e = 0; e < 4; ++e) scale_split(vt[x0 + x][e], f[e >> 1], hi[x][e], mid[x][e], lo[x][e]);
 #pragma unroll
-          for (int x = 0; x < MT; ++x) {
-            mma(F[x][y], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[0], kb[1]);
-            mma(F[x][y + 1], hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[2], kb[3]);
-            mma(F[x][y], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[0], kb[1]);
-            mma(F[x][y + 1], mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[2], kb[3]);
-            mma(F[x][y], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
-            mma(F[x][y + 1], lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
+          for (int y = 0; y < NT; y += 2) {
+            uint32_t kb[4];
+            ldsm4t((sk + piece<N>(r16, c16)) ^ (y * 16), kb);
+#pragma unroll
+            for (int x = 0; x < XB; ++x) {
+              auto& f0 = F[x0 + x][y];
+              auto& f1 = F[x0 + x][y + 1];
+              mma(f0, hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[0], kb[1]);
+              mma(f1, hi[x][0], hi[x][1], hi[x][2], hi[x][3], kb[2], kb[3]);
+              mma(f0, mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[0], kb[1]);
+              mma(f1, mid[x][0], mid[x][1], mid[x][2], mid[x][3], kb[2], kb[3]);
+              mma(f0, lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[0], kb[1]);
+              mma(f1, lo[x][0], lo[x][1], lo[x][2], lo[x][3], kb[2], kb[3]);
+            }
           }
         }
         some = true;
@@ -404,30 +448,38 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks) scan_mma_ke
   cp_async_wait<0>();
 }
 
-template <int DH, bool kLocal>
-hg_status scan_mma_t(const ScanArgs& a, cudaStream_t s) {
+template <int DH, bool kLocal, bool kMany>
+hg_status scan_mma_t(const ScanBatch& b, cudaStream_t s) {
   using C = Cfg<DH>;
   static bool done = false;
   if (!done) {
-    HG_CUDA(cudaFuncSetAttribute(scan_mma_kernel<DH, kLocal>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    HG_CUDA(cudaFuncSetAttribute(scan_mma_kernel<DH, kLocal, kMany>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 C::kSmem));
     done = true;
   }
-  const int64_t items = a.n * (kLocal ? a.nseg - 1 : a.nseg) * a.heads * C::SL;
+  const ScanArgs& a = b.s[0];
+  const int64_t items = a.n * (kLocal ? a.nseg - 1 : a.nseg) * a.heads * C::SL * b.count;
   const int64_t grid = std::min<int64_t>(ceil_div(items, C::W), kSms * C::kBlocks);
-  return launch(kLocal ? "decay_scan_local_mma" : "decay_scan_mma", scan_mma_kernel<DH, kLocal>, dim3((unsigned)grid),
-                dim3(32 * C::W), C::kSmem, s, a);
+  return launch(kLocal ? "decay_scan_local_mma" : "decay_scan_mma", scan_mma_kernel<DH, kLocal, kMany>,
+                dim3((unsigned)grid), dim3(32 * C::W), C::kSmem, s, b);
+}
+
+template <int DH>
+hg_status scan_mma_d(const ScanBatch& b, bool local, cudaStream_t s) {
+  if (b.count > 1) return local ? scan_mma_t<DH, true, true>(b, s) : scan_mma_t<DH, false, true>(b, s);
+  return local ? scan_mma_t<DH, true, false>(b, s) : scan_mma_t<DH, false, false>(b, s);
 }
 
 }  // namespace
 
-hg_status scan_mma(const ScanArgs& a, int d_h, bool local, cudaStream_t s) {
-  if (d_h == 16) return local ? scan_mma_t<16, true>(a, s) : scan_mma_t<16, false>(a, s);
-  if (d_h == 32) return local ? scan_mma_t<32, true>(a, s) : scan_mma_t<32, false>(a, s);
-  if (d_h == 64) return local ? scan_mma_t<64, true>(a, s) : scan_mma_t<64, false>(a, s);
-  return local ? scan_mma_t<128, true>(a, s) : scan_mma_t<128, false>(a, s);
+hg_status scan_mma(const ScanBatch& b, int d_h, bool local, cudaStream_t s) {
+  if (d_h == 16) return scan_mma_d<16>(b, local, s);
+  if (d_h == 32) return scan_mma_d<32>(b, local, s);
+  if (d_h == 64) return scan_mma_d<64>(b, local, s);
+  return scan_mma_d<128>(b, local, s);
 }
 
-int scan_mma_warps(int heads, int d_h) { return heads * (d_h <= 32 ? 1 : d_h / 32); }
+int scan_mma_warps(int heads, int d_h) { return heads * (d_h <= 64 ? 1 : d_h / 32); }
 
 int scan_mma_resident(int d_h) {
   if (d_h == 16) return Cfg<16>::W * Cfg<16>::kBlocks;

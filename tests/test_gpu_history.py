@@ -275,6 +275,27 @@ def test_decay_layouts_and_states_in_place(dt):
     hg.hg_decay_fwd(p, z, z, z, None, None, z, None, None)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T,dh", [(3, 1300, 64), (5, 300, 128), (2, 2100, 16)])
+def test_decay_state_gradient_in_place_of_a_long_history(dt, n, T, dh):
+    """dS_in in the place of dS_out, which the gradient of the keys reads too: segments, claimed lengths."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    q, k, v, do, lens, S, dS = decay_problem(dt, n, T, 2, dh, T, True, True)
+    p = hg.DecayParams(dev(LD[:2]), dh, td, scale=0.25)
+    x = [dev(y, td) for y in (q, k, v)]
+    work = torch.empty(hg.hg_decay_workspace_size(p, n, T)[1], dtype=torch.uint8, device="cuda")
+    runs = []
+    for state, out in ((dev(dS), nans((n, 2, dh, dh), torch.float32)), (dev(dS), None)):
+        g = [nans((n, T, 2, dh), td) for _ in range(3)] + [state if out is None else out]
+        hg.hg_decay_bwd(p, *x, dev(lens), dev(S), dev(do, td), state, *g, work)
+        runs.append(g)
+    assert all(torch.equal(y, z) for y, z in zip(*runs))
+    with pytest.raises(hg.HGError, match="S_in"):
+        hg.hg_decay_bwd(p, *x, dev(lens), runs[0][3], dev(do, td), None, *runs[0], work)
+
+
 def test_decay_long_memory_keeps_its_decay():
     """gamma close to 1 over thousands of positions: keys that are zero after the first leave gamma^t q k v alone."""
     need_gpu()
