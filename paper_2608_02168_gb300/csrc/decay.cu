@@ -163,18 +163,25 @@ __global__ void __launch_bounds__(256) scan_join(const __grid_constant__ ScanBat
   const float ld = clamp_ld(a.ld[sh % a.heads]);
   float run = a.init ? a.init[sh * dd + (a.init_t ? j * dh + i : e)] : 0.f;
   float* seg = a.seg + sh * a.nseg * dd + e;
-  constexpr int U = 8;  // loads in flight: they do not depend on the running state
-  for (int s0 = 0; s0 < a.nseg; s0 += U) {
-    float own[U];
+  constexpr int U = 8;  // the next states are loaded while these are joined
+  float own[U];
+  auto fetch = [&](int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) own[u] = s0 + u + 1 < a.nseg ? seg[(s0 + u) * dd] : 0.f;
+  };
+  fetch(0);
+  for (int s0 = 0; s0 < a.nseg; s0 += U) {
+    float now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = own[u];
+    if (s0 + U < a.nseg) fetch(s0 + U);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int s = s0 + u;
       if (s >= a.nseg) break;
       seg[s * dd] = run;
       const int64_t m = min(a.seg_len, max(len - s * a.seg_len, (int64_t)0));
-      run = fmaf(run, expf(ld * (float)m), own[u]);
+      run = fmaf(run, expf(ld * (float)m), now[u]);
     }
   }
 }
