@@ -636,29 +636,31 @@ def _want(t, name: str, dtype, shape):
     """A contiguous device tensor of this type and shape (None passes NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}; got {t.dtype} {tuple(t.shape)}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape}; got {t.dtype} {tuple(t.shape)}")
     return _ptr(t)
 
 
 def _heads_of(t, name: str, dtype, shape):
-    """A device tensor [..., heads, d_h] whose rows of heads are contiguous; the other strides are free."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}; got {t.dtype} {tuple(t.shape)}")
+    """Strides of a device tensor [..., heads, d_h] whose rows of heads are contiguous; the other strides are free."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape}; got {t.dtype} {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError(f"libhg takes device memory; {name} is on {t.device}")
-    if (shape[-1] > 1 and t.stride(-1) != 1) or (shape[-2] > 1 and t.stride(-2) != shape[-1]):
-        raise ValueError(f"{name}: a row's heads must be contiguous; got strides {t.stride()}")
+    strides = t.stride()
+    if strides[-1] != 1 or (strides[-2] != shape[-1] and shape[-2] > 1):
+        raise ValueError(f"{name}: a row's heads must be contiguous; got strides {strides}")
+    return strides
 
 
 def _row_arg(t, name: str, dtype, shape):
-    _heads_of(t, name, dtype, shape)
-    return byref(hg_rows(t.data_ptr(), t.stride(0)))
+    strides = _heads_of(t, name, dtype, shape)
+    return byref(hg_rows(t.data_ptr(), strides[0]))
 
 
 def _seq_arg(t, name: str, dtype, shape):
-    _heads_of(t, name, dtype, shape)
-    return byref(hg_seq(t.data_ptr(), t.stride(0), t.stride(1)))
+    strides = _heads_of(t, name, dtype, shape)
+    return byref(hg_seq(t.data_ptr(), strides[0], strides[1]))
 
 
 def _work_ptr(t, need: int, name: str):
