@@ -79,9 +79,9 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 // One warp's piece of work: positions [t0, t1) of the scan of a head (segment segi), value features slice * DS on.
 struct Item {
   uint32_t id;  // at or past the number of items: none
-  uint32_t seq;
+  uint32_t seq, unit;
   int set, head, slice, segi;
-  int64_t len, t0, t1;
+  int len, t0, t1;
 };
 
 template <int DH, bool kMany>
@@ -103,33 +103,35 @@ __device__ __forceinline__ void locate(const ScanArgs& a, uint32_t items, uint32
     x /= segs;
   }
   it.seq = x;
-  it.len = scan_len(a, x);
-  it.t0 = it.segi * a.seg_len;
-  it.t1 = max(it.t0, min(it.t0 + a.seg_len, it.len));
+  it.len = (int)scan_len(a, x);
+  it.t0 = it.segi * (int)a.seg_len;
+  it.t1 = max(it.t0, min(it.t0 + (int)a.seg_len, it.len));
 }
 
 // Where a lane's 16-byte pieces of an array's rows start and how far apart the rows of the scan lie, in bytes
 // (negative in reverse).  P pieces a row: the lane takes piece lane % P of rows lane / P + i (32 / P).
 template <int P>
-__device__ __forceinline__ const uint8_t* lane_rows(const ScanRows& r, const ScanArgs& a, const Item& it, int64_t t,
+__device__ __forceinline__ const uint8_t* lane_rows(const ScanRows& r, const ScanArgs& a, const Item& it, int t,
                                                     int col, int lane) {
-  const int64_t row = a.reverse ? it.len - 1 - t - lane / P : t + lane / P;
+  const int row = a.reverse ? it.len - 1 - t - lane / P : t + lane / P;
   return static_cast<const uint8_t*>(r.p) + 2 * ((int64_t)it.seq * r.sn + row * r.st + col + lane % P * 8);
 }
 __device__ __forceinline__ int64_t row_step(const ScanRows& r, const ScanArgs& a) {
   return a.reverse ? -2 * r.st : 2 * r.st;
 }
 
-// The lane's pieces of kC rows, m of them in use (the others become zero), to dst.
+// The lane's pieces of kC rows, m of them in use (the others are not read and become zero), to dst.
 template <int P>
 __device__ __forceinline__ void load_rows(uint8_t* dst, const uint8_t* src, int64_t step, int m, int lane) {
   constexpr int RS = 32 / P;
 #pragma unroll
   for (int i = 0; i < kC / RS; ++i) {
     const int r = lane / P + i * RS;
-    // a row that is not in use is not read; its address is that of the first row
-    const int64_t off = (r < m ? i * RS : -(lane / P)) * step;
-    cp_async16(dst + piece<P>(r, lane % P), src + off, r < m);
+    uint8_t* at = dst + piece<P>(r, lane % P);
+    if (r < m)
+      cp_async16(at, src + i * (RS * step), true);
+    else
+      st16(at, make_uint4(0u, 0u, 0u, 0u));
   }
 }
 
@@ -189,28 +191,57 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
   const int r16 = lane & 15, c16 = lane >> 4;
   const int r8 = (lane & 7) + ((lane >> 4) << 3), c8 = (lane >> 3) & 1;
 
-  // Items by turns, or, where a counter is given, as they are claimed: the loads run ahead, so the claimed numbers
-  // wait in a queue for the arithmetic.
+  // Items by turns, or, where a counter is given, as they are claimed: the loads run ahead, so the claimed numbers (or,
+  // by turns, the lengths) wait in a queue for the arithmetic.
   uint32_t* queue = reinterpret_cast<uint32_t*>(smem + C::W * ST * C::kStage) + warp * 4;
   uint32_t queued = 0, taken = 0;
+  auto enqueue = [&](uint32_t x) {
+    if (lane == 0) queue[queued & 3] = x;
+    ++queued;
+    __syncwarp();
+  };
   auto next_id = [&](uint32_t id) -> uint32_t {
     if (!all.claims) return id + stride;
     uint32_t x = 0;
     if (lane == 0) x = atomicAdd(all.claims, 1u);
     x = __shfl_sync(0xffffffffu, x, 0) + stride;
-    if (lane == 0) queue[queued & 3] = x;
-    ++queued;
-    __syncwarp();
+    enqueue(x);
     return x;
   };
   auto follow = [&](uint32_t id) -> uint32_t { return all.claims ? queue[taken++ & 3] : id + stride; };
+  // Items dealt out without segments follow each other by steps in (scan, sequence, unit = head and slice): carries
+  // replace divisions, and the length of the item after the next is asked for early (40001 histories of up to 12
+  // positions, 4 heads of 32: 188 us, with divisions and lengths asked for when needed 222 us).
+  const bool steps = !kLocal && !all.claims && segs == 1;
+  const uint32_t units = all.heads * C::SL, step_seq = stride / units, step_unit = stride % units;
+  auto bump = [&](int& set, uint32_t& seq, uint32_t& unit) {
+    seq += step_seq;
+    unit += step_unit;
+    if (unit >= units) {
+      unit -= units;
+      ++seq;
+    }
+    if (kMany)
+      for (; seq >= (uint32_t)all.n && set < batch.count; ++set) seq -= (uint32_t)all.n;
+  };
+  auto use = [&](Item& x, int len) {
+    x.t1 = 0;
+    if (x.id >= items) return;
+    x.head = (int)(x.unit / C::SL);
+    x.slice = (int)(x.unit % C::SL);
+    x.len = x.t1 = min(max(len, 0), (int)all.T);
+  };
+  int far_set = 0, far_len = 0;
+  uint32_t far_seq = 0, far_unit = 0;
+  auto look = [&]() { far_len = !all.lens ? (int)all.T : far_seq < (uint32_t)all.n ? all.lens[far_seq] : 0; };
   Item it{}, nx{};
   it.id = blockIdx.x * C::W + warp;
   locate<DH, kMany>(all, items, each, segs, it);
   // The loads run ahead: position nc of item nx is the next chunk to ask for.  An item without positions passes as one
   // empty chunk, so the loads are at most a ring ahead of the arithmetic.
   const uint8_t *qp = nullptr, *kp = nullptr, *vp = nullptr;
-  int64_t nc = 0, qs = row_step(all.q, all), ks = row_step(all.k, all), vs = row_step(all.v, all);
+  int nc = 0;
+  int64_t qs = row_step(all.q, all), ks = row_step(all.k, all), vs = row_step(all.v, all);
   auto begin = [&]() {
     nc = nx.t0;
     if (nx.id >= items || nx.t0 >= nx.t1) return;
@@ -224,16 +255,35 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
     kp = lane_rows<N>(a.k, a, nx, nc, nx.head * DH, lane);
     vp = lane_rows<NV>(a.v, a, nx, nc, nx.head * DH + nx.slice * DS, lane);
   };
+  if (steps) {
+    it.unit = it.id % units;
+    far_set = it.set;
+    far_seq = it.seq;
+    far_unit = it.unit;
+    bump(far_set, far_seq, far_unit);
+    look();
+  }
   nx = it;
   begin();
   auto advance = [&](uint8_t* stage) {
     if (nx.id < items && nc >= max(nx.t1, nx.t0 + 1)) {
-      nx.id = next_id(nx.id);
-      locate<DH, kMany>(all, items, each, segs, nx);
+      if (steps) {
+        nx.id += stride;
+        nx.set = far_set;
+        nx.seq = far_seq;
+        nx.unit = far_unit;
+        use(nx, far_len);
+        enqueue((uint32_t)nx.t1);
+        bump(far_set, far_seq, far_unit);
+        look();
+      } else {
+        nx.id = next_id(nx.id);
+        locate<DH, kMany>(all, items, each, segs, nx);
+      }
       begin();
     }
     if (nx.id < items) {
-      const int m = (int)min((int64_t)kC, nx.t1 - nc);
+      const int m = min(kC, nx.t1 - nc);
       nc += kC;
       if (m > 0) {
         if (!kLocal) load_rows<N>(stage, qp, qs, m, lane);
@@ -252,7 +302,17 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
     advance(ring + put * C::kStage);
     put = put + 1 == ST ? 0 : put + 1;
   }
-  for (; it.id < items; it.id = follow(it.id), locate<DH, kMany>(all, items, each, segs, it)) {
+  auto go_on = [&]() {
+    if (steps) {
+      it.id += stride;
+      bump(it.set, it.seq, it.unit);
+      use(it, (int)queue[taken++ & 3]);
+    } else {
+      it.id = follow(it.id);
+      locate<DH, kMany>(all, items, each, segs, it);
+    }
+  };
+  for (; it.id < items; go_on()) {
     const ScanArgs& a = scan_of(it);
     const int64_t os = row_step(a.o, a);
     const float ld = clamp_ld(a.ld[it.head]), ld2 = ld * 1.4426950408889634f;
@@ -295,10 +355,10 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
       }
     }
     int base = 0;  // positions from t0
-    const bool leave = kLocal || (a.last && it.segi == (it.len > 0 ? (int)((it.len - 1) / a.seg_len) : 0));
+    const bool leave = kLocal || (a.last && it.segi == (it.len > 0 ? (it.len - 1) / (int)a.seg_len : 0));
     uint8_t* op = nullptr;
     if (!kLocal) op = const_cast<uint8_t*>(lane_rows<NV>(a.o, a, it, it.t0, it.head * DH + it.slice * DS, lane));
-    const int count = (int)(it.t1 - it.t0);
+    const int count = it.t1 - it.t0;
     for (int c0 = 0; c0 < max(count, 1); c0 += kC) {
       cp_async_wait<ST - 2>();
       __syncwarp();
@@ -378,7 +438,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
       }
       if (leave || c0 + kC < count) {
         const int target = tau0 + m - 1;
-        if ((float)(base - target) * ld > kFrame) {
+        if (c0 + kC >= count || (float)(base - target) * ld > kFrame) {  // a state that leaves ends its frame
           if (some) {
             const float f = ex2(ld2 * (float)(target - base));
 #pragma unroll
@@ -426,15 +486,23 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
       }
     }
     if (!kLocal) {
-      const int64_t tend = min(it.t0 + a.seg_len, a.T), first = max(it.t0, it.len);
+      const int tend = min(it.t0 + (int)a.seg_len, (int)a.T), first = max(it.t0, it.len);
       uint8_t* zp = static_cast<uint8_t*>(const_cast<void*>(a.o.p)) +
                     2 * ((int64_t)it.seq * a.o.sn + (first + lane / NV) * a.o.st + it.head * DH + it.slice * DS +
                          lane % NV * 8);
-      for (int64_t t = first + lane / NV; t < tend; t += 32 / NV, zp += (32 / NV) * 2 * a.o.st)
+      for (int t = first + lane / NV; t < tend; t += 32 / NV, zp += (32 / NV) * 2 * a.o.st)
         st16(zp, make_uint4(0u, 0u, 0u, 0u));
     }
     if (leave) {
-      const float f = ex2(ld2 * (float)(count - base));
+      if (base != count) {  // shift 0
+        const float f = ex2(ld2 * (float)(count - base));
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+#pragma unroll
+          for (int y = 0; y < NT; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) F[x][y][e] *= f;
+      }
       float* dst = kLocal ? a.seg + (sh * a.nseg + it.segi) * (int64_t)(DH * DH) : a.last + sh * (DH * DH);
 #pragma unroll
       for (int x = 0; x < MT; ++x)
@@ -442,7 +510,7 @@ __global__ void __launch_bounds__(32 * Cfg<DH>::W, Cfg<DH>::kBlocks)
         for (int y = 0; y < NT; ++y)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            dst[(k0 + 8 * y + (e & 1)) * DH + v0 + 16 * x + 8 * (e >> 1)] = F[x][y][e] * f;
+            dst[(k0 + 8 * y + (e & 1)) * DH + v0 + 16 * x + 8 * (e >> 1)] = F[x][y][e];
     }
   }
   cp_async_wait<0>();
