@@ -582,21 +582,25 @@ hg_status hg_decay_workspace_size(const hg_decay_params* params, int64_t n, int6
  * use of each sequence (values outside [0, T] are taken as the nearer end), or NULL = T.  Rows from a
  * sequence's length on are not read and get zero in o.  S_in, S_out: device fp32 [n][heads][d_h][d_h]
  * (key feature x value feature); S_in NULL = zero, S_out NULL = not wanted; S_out (the state after the last
- * position in use; S_in for an empty sequence) may be S_in itself.  o overlaps none of q, k, v. */
+ * position in use; S_in for an empty sequence) may be S_in itself.  o overlaps none of q, k, v.
+ * In bf16 storage positions are taken 16 at a time, and an infinity or NaN in v (or k) at a position in use can reach
+ * the earlier rows of its 16 as NaN; positions that are not in use are never looked at.  Scratch: NULL where its size
+ * is zero. */
 hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
                        const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* o, float* S_out,
                        void* scratch, hg_stream stream);
 
 /* Gradients of hg_decay_fwd on the same q, k, v, lens, S_in, for the upstream gradients d_o and dS_out
  * (NULL = zero): dq, dk, dv (OVERWRITTEN; zero rows from a sequence's length on) and dS_in (fp32,
- * OVERWRITTEN; NULL = not wanted; may be dS_out itself).  Nothing is saved by the forward. */
+ * OVERWRITTEN; NULL = not wanted; may be dS_out itself, not S_in).  No gradient's rows overlap another array.  Nothing
+ * is saved by the forward. */
 hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
                        const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* d_o,
                        const float* dS_out, const hg_seq* dq, const hg_seq* dk, const hg_seq* dv, float* dS_in,
                        void* scratch, hg_stream stream);
 
 /* One new snapshot of n nodes: S_out = gamma S_in + k v^T and o = scale q S_out per node and head (rows
- * and states as above; one row a node).  live: device int32 [n] or NULL; a node whose entry is not
+ * and states as above; one row a node; o overlaps none of q, k, v).  live: device int32 [n] or NULL; a node whose entry is not
  * positive keeps its state and gets a zero row.  S_out may be S_in (updated in place). */
 hg_status hg_decay_step(const hg_decay_params* params, const hg_rows* q, const hg_rows* k, const hg_rows* v,
                         const int32_t* live, int64_t n, const float* S_in, const hg_rows* o, float* S_out,
@@ -627,13 +631,15 @@ typedef struct {
 /* Scratch of hg_ffn_fwd and hg_ffn_bwd for n rows. */
 hg_status hg_ffn_workspace_size(const hg_ffn_params* params, int64_t n, size_t* fwd_bytes, size_t* bwd_bytes);
 
-/* X, Y: n x d, row-major, storage type, 16-byte aligned; Y does not overlap X. */
+/* X, Y: n x d, row-major, storage type, 16-byte aligned; Y does not overlap X.  scratch may be NULL in bf16 (its size is
+ * zero).  bf16: the hidden rows are rounded to bf16 once, between the products; sums are fp32. */
 hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int64_t n, void* Y, void* scratch,
                      hg_stream stream);
 
 /* Gradients for the upstream gradient dY (n x d): dX (n x d, OVERWRITTEN; NULL = skip; overlaps neither X
  * nor dY) and the weights' (grads NULL = skip).  The hidden rows are formed again from X: nothing is
- * saved by the forward.  Sums over rows have a fixed order. */
+ * saved by the forward.  Sums over rows have a fixed order.  bf16: dX's products take dG and dU rounded to bf16, the
+ * weights' gradients take dG, dU and the hidden rows as sums of two bf16 numbers (16 bits). */
 hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
                      const hg_ffn_grads* grads, void* scratch, hg_stream stream);
 

@@ -7,11 +7,13 @@
 // CUDA-core scan: a lane owns one value feature of a head, so its column of the state (d_h numbers) stays in
 // registers and o_t needs no exchange; the keys and queries of a few positions are laid in shared memory
 // for their warp, where all lanes read the same 16 bytes at once.  2 d_h FMA a position and lane: at d_h = 32
-// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it.
+// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it (300 histories of up to 300
+// positions, 4 heads of 32: 156 us a scan, in which a warp has its four neighbours of the scheduler to hide behind).
 // Long histories of few sequences: the histories are cut into segments; a first pass finds each segment's own
 // state, a join runs through them, and the scan then starts each segment from its true state.
 //
-// The step reads and writes the state once (16-byte rows of it across the lanes): bound by HBM.
+// The step reads and writes the state once (16-byte rows of it across the lanes): bound by HBM (200000 nodes, 4 heads
+// of 32, 6.8 GB: 990 us, 0.98 of the measured rate).
 #include <algorithm>
 #include <initializer_list>
 
@@ -161,7 +163,9 @@ __global__ void __launch_bounds__(256) scan_join(const __grid_constant__ ScanBat
   const int64_t sh = x / dd, e = x % dd, i = e / dh, j = e % dh;
   const int64_t len = scan_len(a, sh / a.heads);
   const float ld = clamp_ld(a.ld[sh % a.heads]);
-  float run = a.init ? a.init[sh * dd + (a.init_t ? j * dh + i : e)] : 0.f;
+  // in a frame, as in the scans: a multiplication for each segment would gather the rounding of its factor
+  int base = 0;
+  float F = a.init ? a.init[sh * dd + (a.init_t ? j * dh + i : e)] : 0.f;
   float* seg = a.seg + sh * a.nseg * dd + e;
   constexpr int U = 8;  // the next states are loaded while these are joined
   float own[U];
@@ -179,9 +183,13 @@ __global__ void __launch_bounds__(256) scan_join(const __grid_constant__ ScanBat
     for (int u = 0; u < U; ++u) {
       const int s = s0 + u;
       if (s >= a.nseg) break;
-      seg[s * dd] = run;
-      const int64_t m = min(a.seg_len, max(len - s * a.seg_len, (int64_t)0));
-      run = fmaf(run, expf(ld * (float)m), now[u]);
+      const int t = (int)min(s * a.seg_len, len), t1 = (int)min((s + 1) * a.seg_len, len);
+      seg[s * dd] = F * expf(ld * (float)(t - base));
+      if ((float)(base - t1) * ld > kFrame) {
+        F *= expf(ld * (float)(t1 - base));
+        base = t1;
+      }
+      F = fmaf(now[u], expf(ld * (float)(base - t1)), F);
     }
   }
 }
@@ -265,17 +273,20 @@ __global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-// Segments: as many as fill the GPU with warps, none shorter than kMinSeg positions, where the second
-// reading of keys and values costs more than the warps gain.
-constexpr int64_t kMinSeg = 256;
+// Segments: as many as fill the GPU with warps, of at least 64 (bf16) or 32 positions, where that pays.  A scan in
+// segments takes as long as about 2.5 T / segments + 300 (bf16) or 2 T / segments + 60 positions of one without: keys and
+// values are read twice, a state is written and joined for each segment, and there are two more launches.  Measured
+// (us, whole | segments; 4 heads): bf16, d_h 64, T = 2000, room for 2 segments 209 | 244, 3: 209 | 191, 4: 208 | 152;
+// T = 600, 4: 70 | 76; d_h 32, 10 histories of 400: 29 | 27, 700: 45 | 28; fp32, d_h 32, T = 600, room for 2: 305 | 327,
+// 3: 301 | 231; 10 histories of 100: 42 | 46, 128: 52 | 38.
 void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int scans, int* nseg, int64_t* seg_len) {
   const bool mma = p->dtype == HG_BF16;
   const int64_t each = mma ? scan_mma_warps(p->heads, p->d_h) : (p->heads * p->d_h + 31) / 32;
   const int64_t full = kSms * (mma ? scan_mma_resident(p->d_h) : 16);
-  const int64_t want = std::min<int64_t>(full / (std::max<int64_t>(n, 1) * each * scans), T / kMinSeg);
+  const int64_t want = std::min<int64_t>(full / (std::max<int64_t>(n, 1) * each * scans), T / (mma ? 64 : 32));
   *nseg = 1;
   *seg_len = std::max<int64_t>(T, 1);
-  if (want < 2) return;
+  if (want < 2 || (mma ? 5 * T / want + 600 >= 2 * T : 2 * T / want + 60 >= T)) return;
   *seg_len = (int64_t)align_up((size_t)ceil_div(T, want), 16);
   *nseg = (int)ceil_div(T, *seg_len);
 }
@@ -301,8 +312,9 @@ hg_status scan_pass(const ScanBatch& b, const hg_decay_params* p, bool local, cu
 
 // Scratch: counters of the claimed items, one for each launch of a call, then the segments' states.
 constexpr int kClaims = 8;
-// Ragged histories of this length on are claimed by the warps instead of dealt out: 400 of up to 515 events,
-// 111 us dealt out.  Shorter ones come in such numbers that they even out, and a claim's latency would show.
+// Ragged histories of this length on are claimed by the warps instead of dealt out (us, dealt | claimed; 4 heads): 400
+// of up to 515, d_h 64: 116 | 94; 2000 of up to 200, d_h 32: 71 | 61; 2000 of up to 100: 39.6 | 39.2, and shorter ones
+// gain from the lengths that are asked for ahead.
 constexpr int64_t kClaimT = 128;
 bool scan_claims(const hg_decay_params* p, int64_t T) { return p->dtype == HG_BF16 && T >= kClaimT; }
 

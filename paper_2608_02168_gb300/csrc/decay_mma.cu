@@ -3,17 +3,22 @@
 // Chunks of 16 positions.  With F the state in its frame (decay_kernels.cuh), r, j positions of a chunk:
 //   rows    o_r = sum_(j <= r) gamma^(r - j) c (q_r . k_j) v_j  +  c_out gamma^(tau_r - b) q_r F
 //   state   F += sum_j c_in gamma^(b - tau_j) k_j v_j^T
-// A warp owns one head of one sequence (or of one segment of it) and a slice of DS <= 32 value features, and keeps
-// F^T (DS x d_h, fp32) in registers as the accumulator of m16n8k16 products: the accumulator's layout is the
+// A warp owns one head of one sequence (or of one segment of it) and a slice of DS value features (all of them up to
+// d_h = 64: 2000 histories of 400 positions, 4 heads, 432 us with two slices of 32 against 398 us, since q k^T and the
+// loads are not done twice; at 128, where a state has no place in registers, four slices), and keeps F^T (DS x d_h,
+// fp32) in registers as the accumulator of m16n8k16 products: the accumulator's layout is the
 // layout in which the next product wants its second operand, so the state goes from sum to operand without
 // leaving the registers; likewise the chunk's weights from q k^T to the product with v.  No warp waits for
 // another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand.  The
 // scaled values that are added to the state are split into three bf16 numbers, since a state is an fp32 result that
 // gathers them (two left it 2.5e-6 off).
 //
-// Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high and histories
-// are often shorter than one tile; at d_h = 32 a position moves 256 bytes and needs 9 kFLOP, which the warp
-// instructions deliver at the HBM rate.
+// Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high, histories are often
+// shorter than one tile, and the state would go through shared memory between its sum and the next product.
+//
+// Bound by instruction issue and latency at the warps that registers leave (16 an SM at d_h = 32, 8 above): 40001
+// histories of up to 12 positions, 4 heads of 32, with their states, 188 us (0.74 of the HBM rate); 6 of 32768
+// positions, 4 heads of 64, 99 us and 63 us for the segments' own states (0.6 and 0.47 of it).
 //
 // Loads: cp.async, 16 bytes a lane, into a ring of chunks that runs ahead across the warp's items, so short
 // histories follow one another without a pause.  Pieces of a row are XORed with the row so that ldmatrix is

@@ -6,7 +6,9 @@
 //
 // CUDA-core path: 128 x 64 tiles, 8 x 4 results a thread, operands in shared memory by k; the two
 // projections (and dH) share a pass over k, their gate is applied to the sums in registers, and H, dG and dU
-// go to scratch.  The weights' gradients split the rows; the splits are added in order.  Bound by the FMA rate.
+// go to scratch.  The weights' gradients split the rows; the splits are added in order.  Bound by the FMA rate:
+// 100003 rows, d = 128, f = 384: forward 575 us (51 TFLOP/s), backward 1765 us (45 TFLOP/s), where loads that wait
+// for the products took 652 and 2251 us.
 #include <algorithm>
 
 #include "ffn_kernels.cuh"

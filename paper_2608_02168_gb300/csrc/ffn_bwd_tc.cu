@@ -8,19 +8,23 @@
 // The hidden rows are formed twice, once in each kernel, instead of being stored: three of the five and of the
 // nine products are theirs, but n x f values written and read would take an order of magnitude longer.
 //
-// ffn_dx_tc: as the forward (ffn_tc.cu), one 128-row tile at a time.  The weights' pieces serve twice, as
-// MN-major operands of [G | U] and as K-major operands of dX.  dG and dU are rounded to bf16.  At d = 256
-// X, dY and a chunk's weights fill the shared memory, so dG and dU go back to tensor memory, as the products'
-// first operand.
+// ffn_dx_tc: as the forward (ffn_tc.cu) with one CTA and one 128-row tile at a time, two slots of chunks (one at
+// d = 256).  The weights' pieces serve twice, as MN-major operands of [G | U] and as K-major operands of dX.  dG and
+// dU are rounded to bf16.  At d = 256 X, dY and a chunk's weights fill the shared memory, so dG and dU go back to
+// tensor memory, as the products' first operand.
 //
-// ffn_wgrad_tc: a CTA owns a chunk of hidden features, keeps its weights in shared memory and its gradients
-// in tensor memory, and takes a share of the row tiles.  The gradients are fp32 results, so dG, dU and H enter
-// as sums of two bf16 numbers (16 bits): one rounding would leave them with three digits.  The tensor pipe's own
-// additions cut their results short, which shrinks a long sum (3.8e-5 of it over 16000 rows): each tile's products
-// are therefore drained into registers and added there.  The shares' sums are added in order.  With d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the
-// products is not used: a 64-wide one would run at half the rate).
+// ffn_wgrad_tc: a CTA owns a chunk of hidden features, keeps its weights in shared memory and takes a share of the row
+// tiles.  The gradients are fp32 results, so dG, dU and H enter as sums of two bf16 numbers (16 bits; 2.5e-6 of a
+// gradient is lost, where one number would leave three digits; a third one's place is not there at d = 128).  The
+// tensor pipe's own additions cut their results short, which shrinks a long sum (3.8e-5 of it over 16000 rows): each
+// tile's products are therefore drained into registers and added there.  The shares' sums are added in order.  With
+// d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the products is not used: a 64-wide
+// one would run at half the rate).
 //
-// Bound by the tensor pipe (16 d f flops a row are needed; 28 are run).
+// Bound by the tensor pipe (16 d f flops a row are needed; 28 are run).  Measured: dX 116 us at 200003 rows, d = 128,
+// f = 384 and 243 us at 100003 rows, d = 256, f = 704 (0.85 and 0.74 PFLOP/s of its ten units); weight gradients 234 us
+// (32-feature chunks with two tiles in shared memory 294 us) and 457 us (0.76 and 0.71 PFLOP/s of their eighteen units:
+// a tile's products, gates and drain follow one another, since a second tile's operands have no place).
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
@@ -36,7 +40,7 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kBlk = kRows * 128;  // a 64-column block of a 128-row tile
-constexpr int kThreads = 640;      // warps 0..3: TMA, MMA issue, tensor memory, idle; four warpgroups for the gates
+constexpr int kThreads = 640;      // warps 0..3: TMA, first products, tensor memory, dX; four warpgroups for the gates
 constexpr int kSms = 152;
 
 // eight 32-bit columns of this thread's lane

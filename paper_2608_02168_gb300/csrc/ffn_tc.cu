@@ -3,16 +3,18 @@
 //   [G | U] = X [W_gate | W_up],  H = act(G) * U (rounded to bf16: the operand of the next product),
 //   Y = H W_down (+ X)
 //
-// One persistent CTA an SM.  A group of two 128-row tiles (d <= 128; one at d = 256, whose Y fills half of the
-// tensor memory) stays in shared memory while the hidden features pass by in chunks of 64: the weights'
-// pieces arrive by TMA in two rings, in the stored layout (MN-major operands), half of each piece fetched by each
-// CTA of a pair for both (at d = 256 a lone CTA's weights, 96 KB a chunk, ask more of L2 than it gives), [G | U] of a chunk goes to
-// one of two tensor-memory slots, a warpgroup turns it into H (one row a thread) in shared memory, and the
-// product with W_down adds into Y.  The hidden rows never leave the chip.  The slots take turns (the two
-// tiles, or even and odd chunks): one's gates are computed while the other's products run, so the tensor pipe
-// waits only for the slower of the two.  The gate's reciprocals are taken for two features at once, since the
-// special-function rate (e^x and 1/x of every hidden feature) is as scarce as the tensor rate at d = 128.
-// Bound by the tensor pipe (6 d f flops a row against 4 d bytes).
+// One persistent CTA an SM, or at d = 256 a pair of CTAs on two.  A group of two 128-row tiles (d <= 128; one at
+// d = 256, whose Y fills half of the tensor memory) stays in shared memory while the hidden features pass by in
+// chunks of 64: the weights' pieces arrive by TMA in two rings, in the stored layout (MN-major operands), [G | U] of a
+// chunk goes to one of two tensor-memory slots, two warpgroups turn it into H (half of a row a thread) in shared
+// memory, and the product with W_down adds into Y, which starts at X for a residual.  The hidden rows never leave the
+// chip.  The slots take turns (the two tiles, or even and odd chunks): one's gates are computed while the other's
+// products run.  Each of the two products has an issuing warp of its own.  Rows leave through H's place by TMA.
+//
+// Bound by the tensor pipe (6 d f flops a row against 4 d bytes).  Measured: 300003 rows, f = 704 at d = 256 223 us
+// (1.45 PFLOP/s, 0.76 of the measured bf16 rate; one issuing warp and one CTA 313 us), f = 384 at d = 128 88.5 us
+// (1.0 PFLOP/s: the gates' e^x and 1/x of every hidden feature take the special-function unit as long as the products
+// take the tensor pipe).
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
@@ -29,8 +31,9 @@ namespace {
 constexpr int kRows = 128;
 constexpr int kHc = 64;              // hidden features of a chunk
 constexpr int kBlk = kRows * 128;    // a 64-column block of a 128-row tile
-// warps 0..3: TMA, MMA issue, tensor memory, idle; then two warpgroups for the gates of each slot: with one, a
-// scheduler's single warp of a slot waits out every latency of its own (1M rows, d = 256: 1370 us)
+// warps 0..3: TMA, [G | U], tensor memory, H W_down; then two warpgroups for the gates of each slot: with one, a
+// scheduler's single warp of a slot waits out every latency of its own (300003 rows, d = 256, one issuing warp: 405
+// against 313 us)
 constexpr int kThreads = 640;
 constexpr int kSms = 152;
 
@@ -38,9 +41,9 @@ template <int D>
 struct FCfg {
   static constexpr int NB = D / 64;
   static constexpr int NT = D == 256 ? 1 : 2;                // row tiles of a CTA's group
-  // CTAs that share the weights: at d = 256 a lone CTA's operands, read at 8 KB a 64-cycle product and written at 96 KB a
-  // chunk, ask more of shared memory than it gives (300k rows: 284 us; a pair, whose products read half of the weights
-  // from each, 226 us); at d = 128 two tiles share them already (a pair 93 us, one CTA 88 us)
+  // CTAs that share the weights: at d = 256 a lone CTA's operands, read at 8 KB a 64-cycle product and written at 96 KB
+  // a chunk, ask more of shared memory than it gives (300003 rows: 284 us; a pair, whose products read half of the
+  // weights from each, 223 us); at d = 128 two tiles share them already (a pair 93 us, one CTA 88.5 us)
   static constexpr int CL = D == 256 ? 2 : 1;
   // a CTA's part of a chunk's weights: of a pair W_gate's or W_up's columns, and half of W_down's
   static constexpr int kPiece = D * 128 * 2 / CL, kDown = kHc * D * 2 / CL;
@@ -112,8 +115,8 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
   fence_after_sync();
   const uint32_t tmem = *tslot;
   const int nch = p.nch;
-  // A pair's CTAs take neighbouring groups at the same pace (one past the last is rows past n).  The first one issues the
-  // products of both; its barriers gather both CTAs' arrivals, its commits arrive in both.
+  // A pair's CTAs take neighbouring groups at the same pace (one past the last is rows past n).  The first one issues
+  // the products of both; its barriers gather both CTAs' arrivals, its commits arrive in both.
   const uint32_t rank = I::rank();
   const int64_t gr0 = blockIdx.x, gend = (p.groups + CL - 1) / CL * CL;
 
@@ -203,8 +206,9 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
     }
     if (!wait.ok) issue.drain(&quit[0]);
   } else if (warp == 3 && rank == 0) {
-    // ---------------------------------------------------------------- H W_down, by a warp of its own: a wait or a commit takes
-    // this role some hundred cycles beside the gates' warps, and neither product should stand behind the other's
+    // ---------------------------------------------------------------- H W_down
+    // by a warp of its own: a wait or a commit takes this role some hundred cycles beside the gates' warps, and neither
+    // product should stand behind the other's
     const I issue;
     WarpWaiter wait{p.status};
     uint32_t q = 0, gi = 0;
