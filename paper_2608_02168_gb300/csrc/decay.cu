@@ -7,8 +7,9 @@
 // CUDA-core scan: a lane owns one value feature of a head, so its column of the state (d_h numbers) stays in
 // registers and o_t needs no exchange; the keys and queries of a few positions are laid in shared memory
 // for their warp, where all lanes read the same 16 bytes at once.  2 d_h FMA a position and lane: at d_h = 32
-// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it (300 histories of up to 300
-// positions, 4 heads of 32: 156 us a scan, in which a warp has its four neighbours of the scheduler to hide behind).
+// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it.  Few histories leave an
+// SM few warps to hide a position's latency behind (300 of up to 300 positions, 4 heads of 32: 154 us a scan), so the
+// three scans of a gradient run side by side (230 us).
 // Long histories of few sequences: the histories are cut into segments; a first pass finds each segment's own
 // state, a join runs through them, and the scan then starts each segment from its true state.
 //
@@ -33,10 +34,11 @@ struct SimtCfg {
   static constexpr int TC = DH <= 32 ? 16 : 8;    // positions staged at a time
 };
 
-// blockIdx.x * kWarps + warp = ((sequence * nseg) + segment) * column blocks + column block
+// blockIdx.x * kWarps + warp = ((sequence * nseg) + segment) * column blocks + column block, blockIdx.y the scan
 template <int DH, bool kLocal>
-__global__ void __launch_bounds__(32 * kWarps) scan_simt(ScanArgs a) {
+__global__ void __launch_bounds__(32 * kWarps) scan_simt(const __grid_constant__ ScanBatch b) {
   pdl_begin();
+  const ScanArgs& a = b.s[blockIdx.y];
   using T = float;
   using C = SimtCfg<DH>;
   constexpr int W = C::W, TC = C::TC, VEC = VecTraits<T>::kElems;
@@ -292,22 +294,20 @@ void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int scans, in
 }
 
 template <int DH>
-hg_status scan_simt_t(const ScanArgs& a, bool local, cudaStream_t s) {
+hg_status scan_simt_t(const ScanBatch& b, bool local, cudaStream_t s) {
+  const ScanArgs& a = b.s[0];
   const int64_t items = a.n * a.nseg * (int64_t)((a.heads * DH + 31) / 32);
-  const dim3 grid((unsigned)ceil_div(items, kWarps));
-  if (local) return launch("decay_scan_local", scan_simt<DH, true>, grid, dim3(32 * kWarps), 0, s, a);
-  return launch("decay_scan", scan_simt<DH, false>, grid, dim3(32 * kWarps), 0, s, a);
+  const dim3 grid((unsigned)ceil_div(items, kWarps), (unsigned)b.count);
+  if (local) return launch("decay_scan_local", scan_simt<DH, true>, grid, dim3(32 * kWarps), 0, s, b);
+  return launch("decay_scan", scan_simt<DH, false>, grid, dim3(32 * kWarps), 0, s, b);
 }
 
 hg_status scan_pass(const ScanBatch& b, const hg_decay_params* p, bool local, cudaStream_t s) {
   if (p->dtype == HG_BF16) return scan_mma(b, p->d_h, local, s);
-  for (int i = 0; i < b.count; ++i) {
-    if (p->d_h == 16) HG_TRY(scan_simt_t<16>(b.s[i], local, s));
-    if (p->d_h == 32) HG_TRY(scan_simt_t<32>(b.s[i], local, s));
-    if (p->d_h == 64) HG_TRY(scan_simt_t<64>(b.s[i], local, s));
-    if (p->d_h == 128) HG_TRY(scan_simt_t<128>(b.s[i], local, s));
-  }
-  return HG_OK;
+  if (p->d_h == 16) return scan_simt_t<16>(b, local, s);
+  if (p->d_h == 32) return scan_simt_t<32>(b, local, s);
+  if (p->d_h == 64) return scan_simt_t<64>(b, local, s);
+  return scan_simt_t<128>(b, local, s);
 }
 
 // Scratch: counters of the claimed items, one for each launch of a call, then the segments' states.
