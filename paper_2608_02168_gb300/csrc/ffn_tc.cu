@@ -3,13 +3,13 @@
 //   [G | U] = X [W_gate | W_up],  H = act(G) * U (rounded to bf16: the operand of the next product),
 //   Y = H W_down (+ X)
 //
-// One persistent CTA an SM, or at d = 256 a pair of CTAs on two.  A group of two 128-row tiles (d <= 128; one at
-// d = 256, whose Y fills half of the tensor memory) stays in shared memory while the hidden features pass by in
-// chunks of 64: the weights' pieces arrive by TMA in two rings, in the stored layout (MN-major operands), [G | U] of a
-// chunk goes to one of two tensor-memory slots, two warpgroups turn it into H (half of a row a thread) in shared
-// memory, and the product with W_down adds into Y, which starts at X for a residual.  The hidden rows never leave the
-// chip.  The slots take turns (the two tiles, or even and odd chunks): one's gates are computed while the other's
-// products run.  Each of the two products has an issuing warp of its own.  Rows leave through H's place by TMA.
+// One persistent CTA an SM, or at d = 256 a pair of CTAs on two.  A group of two 128-row tiles (one at d = 256 and for
+// few rows) stays in shared memory while the hidden features pass by in chunks of 64: the weights' pieces arrive by TMA
+// in two rings, in the stored layout (MN-major operands), [G | U] of a chunk goes to one of two tensor-memory slots, two
+// warpgroups turn it into H (half of a row a thread) in shared memory, and the product with W_down adds into Y, which
+// starts at X for a residual.  The hidden rows never leave the chip.  The slots take turns (the two tiles, or even and
+// odd chunks): one's gates are computed while the other's products run.  Each of the two products has an issuing warp of
+// its own.  Rows leave through H's place by TMA.
 //
 // Bound by the tensor pipe (6 d f flops a row against 4 d bytes).  Measured: 300003 rows, f = 704 at d = 256 223 us
 // (1.45 PFLOP/s, 0.76 of the measured bf16 rate; one issuing warp and one CTA 313 us), f = 384 at d = 128 88.5 us
@@ -37,10 +37,14 @@ constexpr int kBlk = kRows * 128;    // a 64-column block of a 128-row tile
 constexpr int kThreads = 640;
 constexpr int kSms = 152;
 
-template <int D>
+// Row tiles of a CTA's group.  Up to a tile an SM one, whose even and odd chunks take turns in the slots (kernel with its
+// timing, d = 128, f = 384: 300 rows 17 | 13.5 us with two | one, 19400 rows 17.9 | 14.6, 30000 rows 18.4 | 21.2); at
+// d = 256, where Y fills half of the tensor memory, always one.
+int tiles_of(int d, int64_t n) { return d == 256 || n <= (int64_t)kSms * kRows ? 1 : 2; }
+
+template <int D, int NT>
 struct FCfg {
   static constexpr int NB = D / 64;
-  static constexpr int NT = D == 256 ? 1 : 2;                // row tiles of a CTA's group
   // CTAs that share the weights: at d = 256 a lone CTA's operands, read at 8 KB a 64-cycle product and written at 96 KB
   // a chunk, ask more of shared memory than it gives (300003 rows: 284 us; a pair, whose products read half of the
   // weights from each, 223 us); at d = 128 two tiles share them already (a pair 93 us, one CTA 88.5 us)
@@ -62,14 +66,14 @@ struct FwdP {
   int* status;
 };
 
-template <int D, int kAct>
-__cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 1)
+template <int D, int NT, int kAct>
+__cluster_dims__(FCfg<D, NT>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 1)
     ffn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_X, const __grid_constant__ CUtensorMap tm_G,
                       const __grid_constant__ CUtensorMap tm_U, const __grid_constant__ CUtensorMap tm_W,
                       const __grid_constant__ CUtensorMap tm_Y, FwdP p) {
   pdl_begin();
-  using C = FCfg<D>;
-  constexpr int NB = C::NB, NT = C::NT, NG = C::NG, ND = C::ND, CL = C::CL;
+  using C = FCfg<D, NT>;
+  constexpr int NB = C::NB, NG = C::NG, ND = C::ND, CL = C::CL;
   using I = Issuer<CL>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* Xs = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -246,7 +250,8 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
     uint32_t k = 0, gi = 0;
     // the slot's columns of Y: NT == 2 all of its tile's, else half of the tile's; 64 of them a round
     const int t = NT == 2 ? s : 0;
-    constexpr int RN = (NT == 2 ? D : D / 2) / 64;
+    constexpr int RN = NT == 2 ? D / 64 : D >= 128 ? D / 128 : 1;
+    const bool leaves = NT == 2 || D >= 128 || s == 0;  // one tile of 64 columns: the first slot's
     const int blk0 = NT == 2 ? 0 : s * RN;
     const uint32_t ycol = tmem + C::kYCol + t * D + lane_off + blk0 * 64 + half * 32;
     uint32_t rounds = 0;
@@ -254,7 +259,7 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
       if (p.residual) {  // Y starts at X, so that X's place can take the next group while this one is finished
         if (!wait(xfull, gi & 1)) break;
 #pragma unroll
-        for (int b = 0; b < RN; ++b) {
+        for (int b = 0; b < (leaves ? RN : 0); ++b) {
           const uint8_t* xb = Xs + (t * NB + blk0 + b) * kBlk;
 #pragma unroll
           for (int x = 0; x < 32; x += 16) {
@@ -299,7 +304,7 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
       const int64_t r0 = (gr * NT + t) * kRows;
       if (!wait(&yfull[t], gi & 1)) break;
 #pragma unroll 1
-      for (int b = 0; b < RN; ++b, ++rounds) {
+      for (int b = 0; b < (leaves ? RN : 0); ++b, ++rounds) {
         uint32_t y[32];
         ld16_issue(ycol + b * 64, reinterpret_cast<uint32_t(&)[16]>(y[0]));
         ld16_issue(ycol + b * 64 + 16, reinterpret_cast<uint32_t(&)[16]>(y[16]));
@@ -332,12 +337,13 @@ __cluster_dims__(FCfg<D>::CL, 1, 1) __global__ void __launch_bounds__(kThreads, 
   if (warp == 2) I::dealloc(tmem, 512);
 }
 
-template <int D, int kAct>
+template <int D, int NT, int kAct>
 hg_status fwd_t(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
-  using C = FCfg<D>;
+  using C = FCfg<D, NT>;
   static bool done = false;
   if (!done) {
-    HG_CUDA(cudaFuncSetAttribute(ffn_fwd_tc_kernel<D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    HG_CUDA(cudaFuncSetAttribute(ffn_fwd_tc_kernel<D, NT, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 C::kSmem));
     done = true;
   }
   CUtensorMap tm_X, tm_G, tm_U, tm_W, tm_Y;
@@ -346,19 +352,25 @@ hg_status fwd_t(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaS
   HG_TRY(make_tmap_bf16(&tm_U, w->W_up, D, (uint64_t)w->f, D));
   HG_TRY(make_tmap_bf16(&tm_W, w->W_down, (uint64_t)w->f, D, kHc));
   HG_TRY(make_tmap_bf16(&tm_Y, Y, (uint64_t)n, D, kRows));
-  FwdP p{n, (int)ceil_div(w->f, kHc), ceil_div(n, (int64_t)kRows * C::NT),
-         w->residual != 0, device_status_ptr()};
+  FwdP p{n, (int)ceil_div(w->f, kHc), ceil_div(n, (int64_t)kRows * NT), w->residual != 0, device_status_ptr()};
   const int grid = (int)std::min<int64_t>(ceil_div(p.groups, C::CL) * C::CL, kSms / C::CL * C::CL);
-  return launch("ffn_fwd_tc", ffn_fwd_tc_kernel<D, kAct>, dim3(grid), dim3(kThreads), C::kSmem, s, tm_X, tm_G, tm_U,
+  return launch("ffn_fwd_tc", ffn_fwd_tc_kernel<D, NT, kAct>, dim3(grid), dim3(kThreads), C::kSmem, s, tm_X, tm_G, tm_U,
                 tm_W, tm_Y, p);
+}
+
+template <int D, int NT>
+hg_status fwd_a(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
+  if (w->act == HG_ACT_RELU) return fwd_t<D, NT, HG_ACT_RELU>(w, X, n, Y, s);
+  if (w->act == HG_ACT_GELU_TANH) return fwd_t<D, NT, HG_ACT_GELU_TANH>(w, X, n, Y, s);
+  if (w->act == HG_ACT_SILU) return fwd_t<D, NT, HG_ACT_SILU>(w, X, n, Y, s);
+  return fwd_t<D, NT, HG_ACT_NONE>(w, X, n, Y, s);
 }
 
 template <int D>
 hg_status fwd_d(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s) {
-  if (w->act == HG_ACT_RELU) return fwd_t<D, HG_ACT_RELU>(w, X, n, Y, s);
-  if (w->act == HG_ACT_GELU_TANH) return fwd_t<D, HG_ACT_GELU_TANH>(w, X, n, Y, s);
-  if (w->act == HG_ACT_SILU) return fwd_t<D, HG_ACT_SILU>(w, X, n, Y, s);
-  return fwd_t<D, HG_ACT_NONE>(w, X, n, Y, s);
+  if constexpr (D != 256)
+    if (tiles_of(D, n) == 2) return fwd_a<D, 2>(w, X, n, Y, s);
+  return fwd_a<D, 1>(w, X, n, Y, s);
 }
 
 }  // namespace

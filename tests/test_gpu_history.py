@@ -499,6 +499,27 @@ def test_ffn_many_row_tiles(dt, d, f):
         assert np.linalg.norm(host(g[key]) - w) <= 1e-4 * np.linalg.norm(w), key
 
 
+@pytest.mark.parametrize("d,f", [(64, 40), (64, 136), (128, 72), (128, 200), (256, 64), (256, 264)])
+def test_ffn_many_row_tiles_with_a_residual(d, f):
+    """Y starts at X and dX at dY, whose places take the next tile early: rows of several tiles a CTA as those of one."""
+    need_gpu()
+    hg = lib()
+    n, m = 60_003, 331
+    td = torch.bfloat16
+    X, Wg, Wu, Wd, dY = ffn_problem("bf16", m, d, f, 7)
+    at = torch.arange(n, device="cuda") % m
+    p = hg.FfnParams(*(dev(w, td) for w in (Wg, Wu, Wd)), act="gelu_tanh", residual=True)
+    work = torch.empty(max(hg.hg_ffn_workspace_size(p, n)), dtype=torch.uint8, device="cuda")
+    few, many = nans((m, d), td), nans((n, d), td)
+    hg.hg_ffn_fwd(p, dev(X, td), few, None)
+    big, up = dev(X, td)[at].contiguous(), dev(dY, td)[at].contiguous()
+    hg.hg_ffn_fwd(p, big, many, None)
+    assert torch.equal(many, few[at])
+    hg.hg_ffn_bwd(p, dev(X, td), dev(dY, td), few, None, work)
+    hg.hg_ffn_bwd(p, big, up, many, None, work)
+    assert torch.equal(many, few[at])
+
+
 def test_ffn_empty():
     need_gpu()
     hg = lib()
