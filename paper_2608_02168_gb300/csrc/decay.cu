@@ -276,11 +276,11 @@ __global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q
 // host
 // ---------------------------------------------------------------------------------------------
 // Segments: as many as fill the GPU with warps, of at least 64 (bf16) or 32 positions, where that pays.  A scan in
-// segments takes as long as about 2.5 T / segments + 300 (bf16) or 2 T / segments + 60 positions of one without: keys and
-// values are read twice, a state is written and joined for each segment, and there are two more launches.  Measured
-// (us, whole | segments; 4 heads): bf16, d_h 64, T = 2000, room for 2 segments 209 | 244, 3: 209 | 191, 4: 208 | 152;
-// T = 600, 4: 70 | 76; d_h 32, 10 histories of 400: 29 | 27, 700: 45 | 28; fp32, d_h 32, T = 600, room for 2: 305 | 327,
-// 3: 301 | 231; 10 histories of 100: 42 | 46, 128: 52 | 38.
+// segments takes as long as about 2.5 T / segments + 300 (bf16) or 2 T / segments + 60 positions of one without: keys
+// and values are read twice, a state is written and joined for each segment, and there are two more launches.
+// Measured (us, whole | segments; 4 heads): bf16, d_h 64, T = 2000, room for 2 segments 209 | 244, 3: 209 | 191, 4:
+// 208 | 152; T = 600, 4: 70 | 76; d_h 32, 10 histories of 400: 29 | 27, 700: 45 | 28; fp32, d_h 32, T = 600, room for
+// 2: 305 | 327, 3: 301 | 231; 10 histories of 100: 42 | 46, 128: 52 | 38.
 void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int scans, int* nseg, int64_t* seg_len) {
   const bool mma = p->dtype == HG_BF16;
   const int64_t each = mma ? scan_mma_warps(p->heads, p->d_h) : (p->heads * p->d_h + 31) / 32;

@@ -13,7 +13,6 @@
 
 #include "ffn_kernels.cuh"
 #include "ffn_tc.cuh"
-#include "layer_kernels.cuh"
 
 namespace hg {
 
@@ -339,8 +338,8 @@ hg_status bwd_simt(const hg_ffn_params* p, const void* X, int64_t n, const void*
   const int sp = wg_splits(n, p->d, p->f);
   const Mat x{(const float*)X, d, n, d}, dg{L.dG, f, n, f}, du{L.dU, f, n, f}, h{L.H, f, n, f},
       dy{(const float*)dY, d, n, d};
-  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt, dim3((unsigned)wg_tiles(p->d, p->f), (unsigned)sp), dim3(kThr), 0, s, x,
-                dg, du, h, dy, (int64_t)align_up((size_t)ceil_div(n, sp), kBk), L.part));
+  HG_TRY(launch("ffn_wgrad_simt", ffn_wgrad_simt, dim3((unsigned)wg_tiles(p->d, p->f), (unsigned)sp), dim3(kThr), 0, s,
+                x, dg, du, h, dy, (int64_t)align_up((size_t)ceil_div(n, sp), kBk), L.part));
   return ffn_sum_shares(L.part, sp, d * f, g, s);
 }
 

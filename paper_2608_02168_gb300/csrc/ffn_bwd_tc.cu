@@ -247,7 +247,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int col0 = wg * CW;
     for (int64_t tile = blockIdx.x; wait.ok && tile < p.tiles; tile += gridDim.x, ++ti) {
       if (!C::kTs) {
-        if (p.residual) {  // dX starts at dY, so that X's and dY's places can take the next tile while this one is finished
+        // dX starts at dY, so that X's and dY's places can take the next tile while this one is finished
+        if (p.residual) {
           if (!wait(xfull, ti & 1)) break;
 #pragma unroll
           for (int c = 0; c < CW; c += 16) {
@@ -315,8 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         warp_arrive(ofull);
       }
       if (!wait.ok) break;
-      // Rows out, a TMA store each 64 columns (it leaves out the rows past n): through the operands' place, which the last
-      // product has read; kTs: dY's place takes dX (+ dY).
+      // Rows out, a TMA store each 64 columns (it leaves out the rows past n): through the operands' place, which the
+      // last product has read; kTs: dY's place takes dX (+ dY).
       uint8_t* ob = (C::kTs ? Ys : Os) + col0 / 64 * kBlk;
       if ((C::kTs && !wait(xfull, ti & 1)) || !wait(yfull, ti & 1)) break;
       if (!C::kTs && first && !wait(sdone, (ti - 1) & 1)) break;

@@ -5,11 +5,11 @@
 //
 // One persistent CTA an SM, or at d = 256 a pair of CTAs on two.  A group of two 128-row tiles (one at d = 256 and for
 // few rows) stays in shared memory while the hidden features pass by in chunks of 64: the weights' pieces arrive by TMA
-// in two rings, in the stored layout (MN-major operands), [G | U] of a chunk goes to one of two tensor-memory slots, two
-// warpgroups turn it into H (half of a row a thread) in shared memory, and the product with W_down adds into Y, which
-// starts at X for a residual.  The hidden rows never leave the chip.  The slots take turns (the two tiles, or even and
-// odd chunks): one's gates are computed while the other's products run.  Each of the two products has an issuing warp of
-// its own.  Rows leave through H's place by TMA.
+// in two rings, in the stored layout (MN-major operands), [G | U] of a chunk goes to one of two tensor-memory slots,
+// two warpgroups turn it into H (half of a row a thread) in shared memory, and the product with W_down adds into Y,
+// which starts at X for a residual.  The hidden rows never leave the chip.  The slots take turns (the two tiles, or
+// even and odd chunks): one's gates are computed while the other's products run.  Each of the two products has an
+// issuing warp of its own.  Rows leave through H's place by TMA.
 //
 // Bound by the tensor pipe (6 d f flops a row against 4 d bytes).  Measured: 300003 rows, f = 704 at d = 256 223 us
 // (1.45 PFLOP/s, 0.76 of the measured bf16 rate; one issuing warp and one CTA 313 us), f = 384 at d = 128 88.5 us
@@ -37,9 +37,9 @@ constexpr int kBlk = kRows * 128;    // a 64-column block of a 128-row tile
 constexpr int kThreads = 640;
 constexpr int kSms = 152;
 
-// Row tiles of a CTA's group.  Up to a tile an SM one, whose even and odd chunks take turns in the slots (kernel with its
-// timing, d = 128, f = 384: 300 rows 17 | 13.5 us with two | one, 19400 rows 17.9 | 14.6, 30000 rows 18.4 | 21.2); at
-// d = 256, where Y fills half of the tensor memory, always one.
+// Row tiles of a CTA's group.  Up to a tile an SM one, whose even and odd chunks take turns in the slots (kernel with
+// its timing, d = 128, f = 384: 300 rows 17 | 13.5 us with two | one, 19400 rows 17.9 | 14.6, 30000 rows 18.4 | 21.2);
+// at d = 256, where Y fills half of the tensor memory, always one.
 int tiles_of(int d, int64_t n) { return d == 256 || n <= (int64_t)kSms * kRows ? 1 : 2; }
 
 template <int D, int NT>

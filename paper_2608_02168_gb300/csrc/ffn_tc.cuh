@@ -5,6 +5,14 @@
 
 namespace hg {
 
+hg_status ffn_fwd_tc(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s);
+// dX null or g null: that part is left out
+hg_status ffn_bwd_tc(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
+                     void* scratch, cudaStream_t s);
+// the weights' gradients from the row shares' sums, part[splits] = [dW_gate | dW_up | dW_down] of df values each
+hg_status ffn_sum_shares(const float* part, int splits, int64_t df, const hg_ffn_grads* g, cudaStream_t s);
+size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n);
+
 // 16 consecutive 32-bit columns of this thread's tensor-memory lane; valid after ld_wait
 __device__ __forceinline__ void ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
@@ -20,15 +28,6 @@ __device__ __forceinline__ void ld8_issue(uint32_t taddr, uint32_t (&r)[8]) {
                : "r"(taddr));
 }
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-
-hg_status ffn_fwd_tc(const hg_ffn_params* w, const void* X, int64_t n, void* Y, cudaStream_t s);
-// dX null or g null: that part is left out
-hg_status ffn_bwd_tc(const hg_ffn_params* w, const void* X, int64_t n, const void* dY, void* dX, const hg_ffn_grads* g,
-                     void* scratch, cudaStream_t s);
-// the weights' gradients from the row shares' sums, part[splits] = [dW_gate | dW_up | dW_down] of df values each
-hg_status ffn_sum_shares(const float* part, int splits, int64_t df, const hg_ffn_grads* g, cudaStream_t s);
-size_t ffn_bwd_tc_scratch(const hg_ffn_params* w, int64_t n);
 
 __device__ __forceinline__ void st16_issue(uint32_t taddr, const float* v) {
   asm volatile(
@@ -50,9 +49,9 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 }
 
 // The issuing warp of a CTA (CL = 1) or of a pair of CTAs (CL = 2, a cluster): all its lanes run the role, so that
-// descriptors are warp-uniform values, and one elected lane issues.  A pair's product has 256 rows, 128 of each CTA from
-// the same places of its shared memory to the same columns of its tensor memory; the second operand lies half in each.
-// The first CTA issues, and a commit arrives at the same barrier of both.
+// descriptors are warp-uniform values, and one elected lane issues.  A pair's product has 256 rows, 128 of each CTA
+// from the same places of its shared memory to the same columns of its tensor memory; the second operand lies half in
+// each.  The first CTA issues, and a commit arrives at the same barrier of both.
 template <int CL>
 struct Issuer {
   uint32_t lead;
@@ -152,8 +151,8 @@ struct Issuer {
       tc::tma_load_2d(dst, map, x, y, bar);
     else
       asm volatile(
-          "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
-          "%3}], [%4];" ::"r"(tc::smem_u32(dst)),
+          "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, "
+          "{%2, %3}], [%4];" ::"r"(tc::smem_u32(dst)),
           "l"(map), "r"(x), "r"(y), "r"(first(bar))
           : "memory");
   }
@@ -161,7 +160,8 @@ struct Issuer {
     if constexpr (CL == 1) {
       tc::tmem_alloc(slot, ncols);
     } else {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(slot)), "r"(ncols)
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(slot)),
+                   "r"(ncols)
                    : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }

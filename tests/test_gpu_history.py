@@ -520,6 +520,79 @@ def test_ffn_many_row_tiles_with_a_residual(d, f):
     assert torch.equal(many, few[at])
 
 
+def far(x, stride):
+    """The rows of x, whose first index lies `stride` values apart."""
+    t = torch.empty(stride * (x.shape[0] - 1) + x[0].numel(), dtype=x.dtype, device="cuda")
+    v = t.as_strided(x.shape, (stride, *x.stride()[1:]))
+    v.copy_(x)
+    return v
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_offsets_past_32_bits_and_shared_rows(dt):
+    """Rows 2^31 values apart give the bits of rows side by side; so do inputs whose rows are one row (stride 0)."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    n, T, h, dh, step = 2, 19, 2, 32, (1 << 31) + 64
+    rng = np.random.default_rng(1)
+    x = [dev(draw(rng, dt, n, T, h, dh), td) for _ in range(4)]
+    p = hg.DecayParams(dev(LD[:h]), dh, td)
+    o = nans((n, T, h, dh), td)
+    hg.hg_decay_fwd(p, *x[:3], None, None, o, None, None)
+    g = [nans((n, T, h, dh), td) for _ in range(3)]
+    hg.hg_decay_bwd(p, *x[:3], None, None, x[3], None, *g, None, None)
+    fo = far(nans((n, T, h, dh), td), step)
+    fq, fk = far(x[0], step), far(x[1], step)
+    hg.hg_decay_fwd(p, fq, fk, x[2], None, None, fo, None, None)
+    assert torch.equal(fo, o)
+    fo.fill_(float("nan"))
+    hg.hg_decay_bwd(p, fq, fk, x[2], None, None, x[3], None, g[0].clone(), fo, g[2].clone(), None, None)
+    assert torch.equal(fo, g[1])
+    r = hg.QkRotParams(None, None, h, h, d_h=dh, dtype=td)
+    a, b = nans((n, h, dh), td), nans((n, h, dh), td)
+    hg.hg_qkrot_fwd(r, x[0][:, 1], x[1][:, 2], None, a, b)
+    hg.hg_qkrot_fwd(r, fq[:, 1], fk[:, 2], None, fo[:, 0], fo[:, 1])
+    assert torch.equal(fo[:, 0], a) and torch.equal(fo[:, 1], b)
+    del fq, fk, fo
+    one = x[0][:1, :1].expand(n, T, h, dh)
+    hg.hg_decay_fwd(p, one, one, x[2], None, None, o, None, None)
+    o2 = nans((n, T, h, dh), td)
+    hg.hg_decay_fwd(p, one.contiguous(), one.contiguous(), x[2], None, None, o2, None, None)
+    assert torch.equal(o, o2)
+    hg.hg_qkrot_fwd(r, one[:, 0], x[1][:, 2], None, a, b)
+    assert torch.equal(a[0], hg_rot(hg, r, x[0][:1, 0], h, dh, td)[0])
+
+
+def hg_rot(hg, r, q, h, dh, td):
+    a, b = nans((1, h, dh), td), nans((1, h, dh), td)
+    hg.hg_qkrot_fwd(r, q, q.clone(), None, a, b)
+    return a
+
+
+def test_states_past_32_bits():
+    """A step whose states hold more than 2^31 values: the last nodes' are those of a step on them alone."""
+    need_gpu()
+    hg = lib()
+    n, h, dh = 530_001, 4, 32
+    p = hg.DecayParams(dev(LD[:h]), dh, torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = (torch.randn(n, h, dh, device="cuda", generator=gen, dtype=torch.bfloat16) for _ in range(3))
+    S = torch.full((n, h, dh, dh), 0.5, device="cuda")
+    assert S.numel() > 1 << 31
+    o = nans((n, h, dh), torch.bfloat16)
+    hg.hg_decay_step(p, q, k, v, None, S, o)
+    few = torch.full((7, h, dh, dh), 0.5, device="cuda")
+    o2 = nans((7, h, dh), torch.bfloat16)
+    hg.hg_decay_step(p, q[-7:], k[-7:], v[-7:], None, few, o2)
+    assert torch.equal(S[-7:], few) and torch.equal(o[-7:], o2)
+    want = nans((7, 1, h, dh), torch.bfloat16)
+    S[-7:] = 0.5
+    hg.hg_decay_fwd(p, q[-7:, None], k[-7:, None], v[-7:, None], None, S[-7:], want, S[-7:], None)
+    # terms: the decayed 0.5 and products below 25 (two normal numbers of five deviations)
+    near(S[-7:], host(few), np.abs(host(few)) + 25, decay_rel("bf16", 1, dh, "state"), "scan of one")
+
+
 def test_ffn_empty():
     need_gpu()
     hg = lib()
