@@ -12,8 +12,10 @@
 // A group of d_h / (2 V) lanes holds one head (V = values in 16 bytes): each lane two 16-byte pieces that
 // contain both features of V pairs, so a turn needs no exchange and the norm is a shuffle over the group.
 // A group keeps its head for the whole run (the grid's stride is a multiple of the row's heads), so the
-// gain, its gradient's sum and the frequencies stay in registers.  Bound by HBM: a head is read once and
-// written once.
+// gain, its gradient's sum and the frequencies stay in registers.  The sines and cosines of a row are those of all its
+// heads: neighbouring heads share them out and exchange them by shuffles (8 + 2 heads of 64, 300001 rows: 169 us by
+// each for itself, 134 us).  Bound by HBM: a head is read once and written once (forward above 0.78 of the measured
+// rate, 1000003 rows backward 0.86; fp32, 200001 rows of 4 + 2 heads of 64, exact sines: 0.88).
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -28,7 +30,9 @@ constexpr int kThreads = 256;
 constexpr int kMaxHeads = 64;
 constexpr int kSms = 152;
 
-// CTAs of an SM.  A run has no more of them, since a second wave would find a part of the SMs' room empty.
+// CTAs of an SM (registers against rows in flight; bf16, 500003 rows of 4 + 4 heads of 32 forward: 2 104, 3 97, 4 101
+// us; 1000003 rows backward: 1 355, 2 262, 3 532 us).  A run has no more of them, since a second wave would find a part
+// of the SMs' room empty.
 constexpr int resident(bool bwd) { return bwd ? 2 : 3; }
 
 struct RotRows {
@@ -62,7 +66,7 @@ __device__ __forceinline__ void turn_sincos(uint64_t phase, float* s, float* c) 
   }
 }
 
-template <typename T, int DH, bool kInter, bool kBwd>
+template <typename T, int DH, bool kInter, bool kBwd, int K>
 __global__ void __launch_bounds__(kThreads, resident(kBwd)) qkrot_kernel(const __grid_constant__ RotArgs a) {
   pdl_begin();
   constexpr int V = VecTraits<T>::kElems;
@@ -91,12 +95,18 @@ __global__ void __launch_bounds__(kThreads, resident(kBwd)) qkrot_kernel(const _
     o1 = turned ? a.rot / 2 + l * V : o0 + V;
     f0 = l * V;
   }
-  uint64_t fr[V];
+  // This lane's share of its V pairs: those e with e % K == j.  The K lanes that follow each other by L have the same
+  // row and the same pairs.
+  const int lane = threadIdx.x & 31, j = lane / L % K, first = lane - j * L;
+  uint64_t fr[V / K];
   float gm[2 * V], acc[2 * V];
   const T* gamma = static_cast<const T*>(is_q ? a.gamma_q : a.gamma_k);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    fr[e] = turned ? a.freq[f0 + e] : 0;
+    if (e % K == 0) {
+      fr[e / K] = 0;
+      if (turned) fr[e / K] = a.freq[f0 + e + j];
+    }
     gm[e] = gamma ? to_f32(gamma[o0 + e]) : 1.f;
     gm[V + e] = gamma ? to_f32(gamma[o1 + e]) : 1.f;
     acc[e] = acc[V + e] = 0.f;
@@ -145,16 +155,24 @@ __global__ void __launch_bounds__(kThreads, resident(kBwd)) qkrot_kernel(const _
 #pragma unroll
       for (int e = 0; e < 2 * V; ++e) y[e] = x[e] * rn * gm[e];
     }
-    if (turned) {
+    if (a.rot) {
+      float sn[V / K], cs[V / K];
+#pragma unroll
+      for (int e = 0; e < V / K; ++e) turn_sincos<kExact>(at * fr[e], &sn[e], &cs[e]);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float s, c;
-        turn_sincos<kExact>(at * fr[e], &s, &c);
+        float s = sn[e / K], c = cs[e / K];
+        if (K > 1) {
+          s = __shfl_sync(0xffffffffu, s, first + e % K * L);
+          c = __shfl_sync(0xffffffffu, c, first + e % K * L);
+        }
         if (kBwd) s = -s;
-        const int ia = kInter ? 2 * e : e, ib = kInter ? 2 * e + 1 : V + e;
-        const float ya = y[ia], yb = y[ib];
-        y[ia] = ya * c - yb * s;
-        y[ib] = yb * c + ya * s;
+        if (turned) {
+          const int ia = kInter ? 2 * e : e, ib = kInter ? 2 * e + 1 : V + e;
+          const float ya = y[ia], yb = y[ib];
+          y[ia] = ya * c - yb * s;
+          y[ib] = yb * c + ya * s;
+        }
       }
     }
     if (kBwd) {
@@ -231,11 +249,23 @@ int rot_grid(int64_t n, int heads, int dh, hg_dtype dt, bool bwd) {
   return (int)std::max(ceil_div(heads, groups), std::min<int64_t>(want, kSms * resident(bwd)));
 }
 
+template <typename T, int DH, bool kBwd, int K>
+hg_status rot_pairs(const RotArgs& a, int grid, bool inter, cudaStream_t s) {
+  const char* name = kBwd ? "qkrot_bwd" : "qkrot_fwd";
+  if (inter) return launch(name, qkrot_kernel<T, DH, true, kBwd, K>, dim3(grid), dim3(kThreads), 0, s, a);
+  return launch(name, qkrot_kernel<T, DH, false, kBwd, K>, dim3(grid), dim3(kThreads), 0, s, a);
+}
+
+// Lanes that share their sines and cosines: those of neighbouring heads of a row, as far as every warp holds whole sets
+// of them (a power of two that divides the heads, and at most a warp).
 template <typename T, int DH, bool kBwd>
 hg_status rot_launch(const RotArgs& a, int grid, bool inter, cudaStream_t s) {
-  const char* name = kBwd ? "qkrot_bwd" : "qkrot_fwd";
-  if (inter) return launch(name, qkrot_kernel<T, DH, true, kBwd>, dim3(grid), dim3(kThreads), 0, s, a);
-  return launch(name, qkrot_kernel<T, DH, false, kBwd>, dim3(grid), dim3(kThreads), 0, s, a);
+  constexpr int L = DH / (2 * VecTraits<T>::kElems);
+  if constexpr (4 * L <= 32)
+    if (a.heads % 4 == 0) return rot_pairs<T, DH, kBwd, 4>(a, grid, inter, s);
+  if constexpr (2 * L <= 32)
+    if (a.heads % 2 == 0) return rot_pairs<T, DH, kBwd, 2>(a, grid, inter, s);
+  return rot_pairs<T, DH, kBwd, 1>(a, grid, inter, s);
 }
 
 template <typename T, bool kBwd>

@@ -278,9 +278,10 @@ def test_decay_layouts_and_states_in_place(dt):
 # Each warp takes several heads here (an SM holds 8 to 20 warps): the order in which they follow one another, dealt out
 # (carries past the last sequence and the last scan) and claimed.
 @pytest.mark.parametrize("n,T,h,dh,ragged", [(1201, 19, 8, 16, True), (997, 35, 5, 32, True), (1300, 3, 7, 32, False),
-                                             (1003, 18, 3, 64, True), (111, 17, 4, 128, True), (850, 130, 3, 32, True),
-                                             (320, 130, 4, 64, True)])
+                                             (1003, 18, 3, 64, True), (331, 17, 4, 128, True), (1100, 130, 3, 32, True),
+                                             (450, 130, 4, 64, True)])
 def test_decay_of_many_histories(n, T, h, dh, ragged):
+    """The same bits as those of the histories in small batches, in which a warp has one head."""
     need_gpu()
     hg = lib()
     td = torch.bfloat16
@@ -289,23 +290,22 @@ def test_decay_of_many_histories(n, T, h, dh, ragged):
         lens[5:9] = 0
         lens[-3:] = 0
     p = hg.DecayParams(dev(LD[:h]), dh, td, scale=dh ** -0.5)
-    fw, bw = hg.hg_decay_workspace_size(p, n, T)
-    work = torch.empty(max(fw, bw), dtype=torch.uint8, device="cuda")
     Q, K, V, DO = (strided(past(x, lens), td) for x in (q, k, v, do))
     L, S0, DS = (None if x is None else dev(x) for x in (lens, S, dS))
-    o, last = nans((n, T, h, dh), td), nans((n, h, dh, dh), torch.float32)
-    hg.hg_decay_fwd(p, Q, K, V, L, S0, o, last, work)
-    grads = [nans((n, T, h, dh), td) for _ in range(3)] + [nans((n, h, dh, dh), torch.float32)]
-    hg.hg_decay_bwd(p, Q, K, V, L, S0, DO, DS, *grads, work)
-    args = [f64(x) for x in (q, k, v)] + [f64(LD[:h]), np.float64(np.float32(dh ** -0.5))]
-    want = OH.decay_forward(*args, lens, f64(S))
-    terms = OH.decay_forward(*args, lens, f64(S), magnitude=True)
-    for got, w, t, name in ((o, want[0], terms[0], "rows"), (last, want[1], terms[1], "state")):
-        near(got, w, t, decay_rel("bf16", T, dh, name), name)
-    want = OH.decay_backward(*args, f64(do), lens, f64(S), f64(dS))
-    terms = OH.decay_backward(*args, f64(do), lens, f64(S), f64(dS), magnitude=True)
-    for got, w, t, name in zip(grads, want, terms, ("dq", "dk", "dv", "state")):
-        near(got, w, t, decay_rel("bf16", T, dh, "state" if name == "state" else "rows"), name)
+
+    def run(at):
+        some = [None if x is None else x[at] for x in (Q, K, V, L, S0, DO, DS)]
+        m = some[0].shape[0]
+        work = torch.empty(max(hg.hg_decay_workspace_size(p, m, T)), dtype=torch.uint8, device="cuda")
+        out = [nans((m, T, h, dh), td) for _ in range(4)] + [nans((m, h, dh, dh), torch.float32) for _ in range(2)]
+        hg.hg_decay_fwd(p, *some[:5], out[0], out[4], work)
+        hg.hg_decay_bwd(p, *some[:5], some[5], some[6], *out[1:4], out[5], work)
+        return out
+
+    whole = run(slice(None))
+    parts = [run(slice(i, i + 50)) for i in range(0, n, 50)]
+    for x, y in zip(whole, (torch.cat(z) for z in zip(*parts))):
+        assert torch.isfinite(x).all() and torch.equal(x, y)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
