@@ -671,7 +671,31 @@ def _work_ptr(t, need: int, name: str):
     return _ptr(t)
 
 
-class QkRotParams:
+class _Params:
+    """The C struct of an operator's parameters, filled from their tensors' addresses at the time of a call: a tensor
+    that was given another storage since is read there."""
+
+    def _hold(self, struct, values: tuple, tensors: tuple):
+        """struct(*values, *addresses); tensors: (tensor or None, name, dtype, shape)."""
+        self._struct, self._values, self._tensors = struct, values, tensors
+        self._held = [x[0] for x in tensors if x[0] is not None]
+        self._at = None
+        self.c()
+
+    def c(self):
+        # address and size of each, 0.15 us a tensor; its type and shape are looked at when one of them has changed
+        at = [(x.data_ptr(), x.nbytes) for x in self._held]
+        if at != self._at:
+            self._at = None
+            ptrs = [_want(*x) for x in self._tensors]
+            if 0 in ptrs:
+                raise ValueError(f"{type(self).__name__}: a tensor has no storage")
+            # a new struct: a call of another thread may be reading the one before
+            self._c, self._at = self._struct(*self._values, *ptrs), at
+        return self._c
+
+
+class QkRotParams(_Params):
     """Parameters of the norm and rotation (see hg_qkrot_params): gains [d_h] in the storage type, or None with
     d_h and dtype given."""
 
@@ -681,15 +705,10 @@ class QkRotParams:
         if some is not None:
             d_h, dtype = int(some.numel()), some.dtype
         self.t = [x.contiguous() if x is not None else None for x in (gamma_q, gamma_k)]
-        for x, name in zip(self.t, ("gamma_q", "gamma_k")):
-            _want(x, name, dtype, (d_h,))
         self.heads_q, self.heads_k, self.d_h, self.dtype = int(heads_q), int(heads_k), int(d_h), dtype
-        self._c = hg_qkrot_params(self.heads_q, self.heads_k, self.d_h, self.d_h if rot is None else int(rot),
-                                  1 if interleaved else 0, _storage(dtype), float(eps), float(base),
-                                  *(_ptr(x) for x in self.t))
-
-    def c(self) -> hg_qkrot_params:
-        return self._c
+        self._hold(hg_qkrot_params, (self.heads_q, self.heads_k, self.d_h, self.d_h if rot is None else int(rot),
+                                     1 if interleaved else 0, _storage(dtype), float(eps), float(base)),
+                   tuple((x, name, dtype, (self.d_h,)) for x, name in zip(self.t, ("gamma_q", "gamma_k"))))
 
 
 def hg_qkrot_workspace_size(params: QkRotParams, n: int) -> int:
@@ -724,17 +743,14 @@ def hg_qkrot_bwd(params: QkRotParams, q, k, pos, dq_out, dk_out, dq, dk, grads: 
                               a[5], g[0], g[1], w, _stream(stream)), "hg_qkrot_bwd")
 
 
-class DecayParams:
+class DecayParams(_Params):
     """Parameters of the linear attention with decay (see hg_decay_params); log_decay fp32 [heads]."""
 
     def __init__(self, log_decay, d_h: int, dtype, scale: float = 1.0):
         self.log_decay = log_decay.contiguous()
         self.heads, self.d_h, self.dtype = int(log_decay.numel()), int(d_h), dtype
-        self._c = hg_decay_params(self.heads, self.d_h, _storage(dtype), float(scale),
-                                  _want(self.log_decay, "log_decay", torch.float32, (self.heads,)))
-
-    def c(self) -> hg_decay_params:
-        return self._c
+        self._hold(hg_decay_params, (self.heads, self.d_h, _storage(dtype), float(scale)),
+                   ((self.log_decay, "log_decay", torch.float32, (self.heads,)),))
 
 
 def hg_decay_workspace_size(params: DecayParams, n: int, T: int) -> tuple:
@@ -775,7 +791,7 @@ def hg_decay_step(params: DecayParams, q, k, v, live, S_in, o, S_out=None, strea
                                r[3], st[1], _stream(stream)), "hg_decay_step")
 
 
-class FfnParams:
+class FfnParams(_Params):
     """Weights of the gated feed-forward block (see hg_ffn_params): W_gate, W_up [d, f], W_down [f, d]."""
 
     def __init__(self, W_gate, W_up, W_down, act: str = "silu", residual: bool = False):
@@ -783,12 +799,9 @@ class FfnParams:
         self.d, self.f = (int(x) for x in W_gate.shape)
         self.dtype = W_gate.dtype
         shapes = ((self.d, self.f), (self.d, self.f), (self.f, self.d))
-        ptrs = [_want(x, name, self.dtype, shape)
-                for x, name, shape in zip(self.t, ("W_gate", "W_up", "W_down"), shapes)]
-        self._c = hg_ffn_params(self.d, self.f, _storage(self.dtype), ACTS[act], 1 if residual else 0, *ptrs)
-
-    def c(self) -> hg_ffn_params:
-        return self._c
+        self._hold(hg_ffn_params, (self.d, self.f, _storage(self.dtype), ACTS[act], 1 if residual else 0),
+                   tuple((x, name, self.dtype, shape)
+                         for x, name, shape in zip(self.t, ("W_gate", "W_up", "W_down"), shapes)))
 
 
 def hg_ffn_workspace_size(params: FfnParams, n: int) -> tuple:

@@ -320,3 +320,56 @@ def test_decay_of_no_sequences_needs_no_scratch(hg):
     assert f.value == b.value == 0
     null = ctypes.POINTER(hg.hg_seq)()
     assert so.hg_decay_fwd(p, null, null, null, None, 0, 500, None, null, None, None, None) == 0
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that stands in for a device one: the binding reads its address, nothing is dereferenced."""
+    is_cuda = True
+
+
+def stand_in(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice)
+
+
+def some_params(hg):
+    """Each class of parameters with its tensors by the names of its C struct."""
+    f32 = torch.float32
+    t = {"gamma_q": stand_in(32), "gamma_k": stand_in(32)}
+    yield hg.QkRotParams(t["gamma_q"], t["gamma_k"], 4, 2), t
+    t = {"log_decay": stand_in(4, dtype=f32)}
+    yield hg.DecayParams(t["log_decay"], 32, torch.bfloat16), t
+    t = {"W_gate": stand_in(64, 96), "W_up": stand_in(64, 96), "W_down": stand_in(96, 64)}
+    yield hg.FfnParams(t["W_gate"], t["W_up"], t["W_down"]), t
+
+
+def test_parameters_follow_their_tensors(hg):
+    """A tensor that is given another storage is read at its new place by the next call, not where it was; another
+    shape is refused."""
+    for p, tensors in some_params(hg):
+        for name, x in tensors.items():
+            before, was = p.c(), x.data_ptr()
+            assert getattr(before, name) == was
+            x.data = torch.ones_like(x)
+            assert x.data_ptr() != was
+            assert all(getattr(p.c(), y) == tensors[y].data_ptr() for y in tensors), name
+            good = x.data
+            x.data = torch.zeros(*x.shape, 2, dtype=x.dtype)
+            with pytest.raises(ValueError, match="shape"):
+                p.c()
+            x.data = torch.zeros(0, dtype=x.dtype)
+            with pytest.raises(ValueError, match="shape"):
+                p.c()
+            x.data = good
+            assert getattr(p.c(), name) == good.data_ptr()
+
+
+def test_a_parameter_without_storage_is_refused(hg):
+    """Its address is null, which would stand for gains of one."""
+    for p, tensors in some_params(hg):
+        for x in tensors.values():
+            size = x.untyped_storage().nbytes()
+            x.untyped_storage().resize_(0)
+            with pytest.raises(ValueError, match="no storage"):
+                p.c()
+            x.untyped_storage().resize_(size)
+            p.c()
