@@ -340,7 +340,9 @@ def hg_graph_node_order(g: Graph, node_type: int) -> dict:
 # layer
 # ------------------------------------------------------------------------------------------------
 class LayerParams:
-    """Packed device parameters of one layer (see hg_layer_params)."""
+    """Packed device parameters of one layer (see hg_layer_params).
+
+    A tensor that is not contiguous is copied here, once: later changes of the original are not seen."""
 
     def __init__(self, W_rel, W_agg, b_agg, ln_gamma=None, ln_beta=None, act: str = "relu", layernorm: bool = True,
                  ln_eps: float = 1e-5, fused: bool = False):
@@ -511,7 +513,9 @@ def hg_overlap_build(src, dst, rel, type_offsets, K: int, k: int, theta: int, M:
 # prediction head and joint objective
 # ------------------------------------------------------------------------------------------------
 class HeadParams:
-    """Packed device parameters of the two-layer head (see hg_head_params)."""
+    """Packed device parameters of the two-layer head (see hg_head_params).
+
+    A tensor that is not contiguous is copied here, once: later changes of the original are not seen."""
 
     def __init__(self, W1, b1, w2, b2):
         self.W1, self.b1, self.w2, self.b2 = W1.contiguous(), b1.contiguous(), w2.contiguous(), b2.contiguous()
@@ -553,7 +557,9 @@ def hg_head_bwd(params: HeadParams, lab_idx, dloss: float, saved, dH, dH_rep, gr
 # temporal module
 # ------------------------------------------------------------------------------------------------
 class TemporalParams:
-    """Packed device parameters of the temporal module (see hg_temporal_params); w = context size."""
+    """Packed device parameters of the temporal module (see hg_temporal_params); w = context size.
+
+    A tensor that is not contiguous is copied here, once: later changes of the original are not seen."""
 
     def __init__(self, Wa, r, W_i, W_h, b_i, b_h, w: int):
         self.t = [x.contiguous() for x in (Wa, r, W_i, W_h, b_i, b_h)]
@@ -590,7 +596,9 @@ def hg_temporal_bwd(params: TemporalParams, X, C, saved, dH_out, dX, grads: dict
 # attention layer (Heterogeneous Graph Transformer)
 # ------------------------------------------------------------------------------------------------
 class HgtParams:
-    """Packed device parameters of one attention layer (see hg_hgt_params); mu is fp32."""
+    """Packed device parameters of one attention layer (see hg_hgt_params); mu is fp32.
+
+    A tensor that is not contiguous is copied here, once: later changes of the original are not seen."""
 
     def __init__(self, tensors: dict, heads: int, act: str = "relu", layernorm: bool = True, ln_eps: float = 1e-5):
         self.t = {k: (tensors[k].contiguous() if tensors.get(k) is not None else None) for k in HGT_KEYS}
@@ -672,13 +680,15 @@ def _work_ptr(t, need: int, name: str):
 
 
 class _Params:
-    """The C struct of an operator's parameters, filled from their tensors' addresses at the time of a call: a tensor
-    that was given another storage since is read there."""
+    """The C struct of an operator's parameters, filled from their tensors' addresses at the time of a call: updates
+    in place and another storage given to a tensor are seen.  The tensors are kept, never copied: one that is not
+    contiguous (the transpose of a weight, say) is refused."""
 
     def _hold(self, struct, values: tuple, tensors: tuple):
         """struct(*values, *addresses); tensors: (tensor or None, name, dtype, shape)."""
         self._struct, self._values, self._tensors = struct, values, tensors
-        self._held = [x[0] for x in tensors if x[0] is not None]
+        self.t = [x[0] for x in tensors]
+        self._held = [x for x in self.t if x is not None]
         self._at = None
         self.c()
 
@@ -704,11 +714,10 @@ class QkRotParams(_Params):
         some = gamma_q if gamma_q is not None else gamma_k
         if some is not None:
             d_h, dtype = int(some.numel()), some.dtype
-        self.t = [x.contiguous() if x is not None else None for x in (gamma_q, gamma_k)]
         self.heads_q, self.heads_k, self.d_h, self.dtype = int(heads_q), int(heads_k), int(d_h), dtype
         self._hold(hg_qkrot_params, (self.heads_q, self.heads_k, self.d_h, self.d_h if rot is None else int(rot),
                                      1 if interleaved else 0, _storage(dtype), float(eps), float(base)),
-                   tuple((x, name, dtype, (self.d_h,)) for x, name in zip(self.t, ("gamma_q", "gamma_k"))))
+                   tuple((x, name, dtype, (self.d_h,)) for x, name in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k"))))
 
 
 def hg_qkrot_workspace_size(params: QkRotParams, n: int) -> int:
@@ -747,7 +756,7 @@ class DecayParams(_Params):
     """Parameters of the linear attention with decay (see hg_decay_params); log_decay fp32 [heads]."""
 
     def __init__(self, log_decay, d_h: int, dtype, scale: float = 1.0):
-        self.log_decay = log_decay.contiguous()
+        self.log_decay = log_decay
         self.heads, self.d_h, self.dtype = int(log_decay.numel()), int(d_h), dtype
         self._hold(hg_decay_params, (self.heads, self.d_h, _storage(dtype), float(scale)),
                    ((self.log_decay, "log_decay", torch.float32, (self.heads,)),))
@@ -795,13 +804,12 @@ class FfnParams(_Params):
     """Weights of the gated feed-forward block (see hg_ffn_params): W_gate, W_up [d, f], W_down [f, d]."""
 
     def __init__(self, W_gate, W_up, W_down, act: str = "silu", residual: bool = False):
-        self.t = [x.contiguous() for x in (W_gate, W_up, W_down)]
         self.d, self.f = (int(x) for x in W_gate.shape)
         self.dtype = W_gate.dtype
         shapes = ((self.d, self.f), (self.d, self.f), (self.f, self.d))
         self._hold(hg_ffn_params, (self.d, self.f, _storage(self.dtype), ACTS[act], 1 if residual else 0),
                    tuple((x, name, self.dtype, shape)
-                         for x, name, shape in zip(self.t, ("W_gate", "W_up", "W_down"), shapes)))
+                         for x, name, shape in zip((W_gate, W_up, W_down), ("W_gate", "W_up", "W_down"), shapes)))
 
 
 def hg_ffn_workspace_size(params: FfnParams, n: int) -> tuple:

@@ -373,3 +373,20 @@ def test_a_parameter_without_storage_is_refused(hg):
                 p.c()
             x.untyped_storage().resize_(size)
             p.c()
+
+
+def test_parameters_that_would_be_copies_are_refused(hg):
+    """A copy of a tensor in another layout would keep the values of the moment; in-place updates reach what is taken."""
+    w, g = stand_in(96, 64).t(), stand_in(64)[::2]
+    assert not w.is_contiguous() and not g.is_contiguous()
+    ok = stand_in(64, 96)
+    for args in ((w, ok, stand_in(96, 64)), (ok, w, stand_in(96, 64)), (ok, ok.clone(), ok.t())):
+        with pytest.raises(ValueError, match="must be contiguous"):
+            hg.FfnParams(*args)
+    with pytest.raises(ValueError, match="must be contiguous"):
+        hg.QkRotParams(g, stand_in(32), 4, 4)
+    with pytest.raises(ValueError, match="must be contiguous"):
+        hg.QkRotParams(None, g, 4, 4)
+    with pytest.raises(ValueError, match="must be contiguous"):
+        hg.DecayParams(stand_in(8, dtype=torch.float32)[::2], 32, torch.bfloat16)
+    assert hg.FfnParams(w.contiguous(), ok, stand_in(96, 64)).c().W_gate != w.data_ptr()
