@@ -38,13 +38,13 @@ __device__ __forceinline__ float gate_half(float x) {
   return 0.7213475204444817f * x;
 }
 
-// kAct: hg_act.  The gate's value.
+// kAct: hg_act.  The gate's value; s r is at most 1/2, so no factor carries a large x past the largest number.
 template <int kAct>
 __device__ __forceinline__ float gate(float x) {
   if (kAct == HG_ACT_RELU) return x > 0.f ? x : 0.f;
   if (kAct == HG_ACT_NONE) return x;
   const Logistic l(gate_half<kAct>(x));
-  return (x * l.s) * (l.s * l.r);
+  return (x * (l.s * l.r)) * l.s;
 }
 
 // The gate's value and derivative.
@@ -63,7 +63,7 @@ __device__ __forceinline__ float gate_grad(float x, float* d) {
   float k = x * l.r;
   if (kAct == HG_ACT_GELU_TANH) k *= fmaf(x * x, 3.f * 0.044715f * 1.5957691216057308f, 1.5957691216057308f);
   *d = fmaf(p, k, p);
-  return (x * l.s) * sr;
+  return x * p;
 }
 
 }  // namespace hg
