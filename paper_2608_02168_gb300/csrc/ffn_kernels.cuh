@@ -17,12 +17,12 @@ __device__ __forceinline__ float gate_rcp(float x) {
 }
 
 // The logistic function of z as s (s r) and its complement as r, from s = e^(z / 2), r = 1 / (1 + s^2): the
-// exponent is halved, so a gate as small as the smallest fp32 number comes out as it is.  Above z = 41 the
-// logistic function is 1 to the last bit.
+// exponent is halved, so a gate as small as the smallest fp32 number comes out as it is.  Above z = 41 (half_log2 = 30,
+// where the caller ends it) the logistic function is 1 to the last bit.
 struct Logistic {
   float s, r;
   __device__ __forceinline__ explicit Logistic(float half_log2) {
-    s = gate_ex2(fminf(half_log2, 30.f));
+    s = gate_ex2(half_log2);
     r = gate_rcp(fmaf(s, s, 1.f));
   }
 };
@@ -43,11 +43,13 @@ template <int kAct>
 __device__ __forceinline__ float gate(float x) {
   if (kAct == HG_ACT_RELU) return x > 0.f ? x : 0.f;
   if (kAct == HG_ACT_NONE) return x;
-  const Logistic l(gate_half<kAct>(x));
+  const Logistic l(fminf(gate_half<kAct>(x), 30.f));
   return (x * (l.s * l.r)) * l.s;
 }
 
-// The gate's value and derivative.
+// The gate's value x p and derivative p (1 + r x dz/dx), p = s^2 r (one below 2^-126 loses bits here).  r ends at 2^-60 where it should go on to 0, and what it is
+// multiplied with grows like x, or x^3: the functions are taken at x's nearest in the range outside of which p is 1 or 0
+// to the last bit (NaN stays).
 template <int kAct>
 __device__ __forceinline__ float gate_grad(float x, float* d) {
   if (kAct == HG_ACT_RELU) {
@@ -58,10 +60,13 @@ __device__ __forceinline__ float gate_grad(float x, float* d) {
     *d = 1.f;
     return x;
   }
-  const Logistic l(gate_half<kAct>(x));
+  float xb = x;
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(xb) : "f"(kAct == HG_ACT_GELU_TANH ? 7.45f : 41.5f));
+  if (kAct == HG_ACT_GELU_TANH) asm("max.NaN.f32 %0, %0, %1;" : "+f"(xb) : "f"(-16.f));
+  const Logistic l(gate_half<kAct>(xb));
   const float sr = l.s * l.r, p = l.s * sr;
-  float k = x * l.r;
-  if (kAct == HG_ACT_GELU_TANH) k *= fmaf(x * x, 3.f * 0.044715f * 1.5957691216057308f, 1.5957691216057308f);
+  float k = xb * l.r;
+  if (kAct == HG_ACT_GELU_TANH) k *= fmaf(xb * xb, 3.f * 0.044715f * 1.5957691216057308f, 1.5957691216057308f);
   *d = fmaf(p, k, p);
   return x * p;
 }

@@ -66,3 +66,15 @@ def test_values_of_gates_of_every_size(dt, act):
     near(Y[:, g32], A[:, g32], np.abs(X[:, g32]), (U[dt], 30 * F32), "Y")
     s = (2.0**-16 if dt == "bf16" else 0) + (30 + 37) * F32
     near(g["W_up"][63, g32], (dY * A).sum(0)[g32], (np.abs(dY) * np.abs(X)).sum(0)[g32], (0, s), "W_up")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh", "relu", "none"])
+def test_derivatives_of_gates_of_every_size(dt, act):
+    """act' of the same gates: that of a large one is 1 or 0.  Within 70 steps of 1 (a slope below 2.3 times 30 steps where
+    it is neither 0 nor 1), in bf16 dG rounded once; dW_gate sums 37 rows, in bf16 of two terms."""
+    need_gpu()
+    X, dY, _, dA, _, dX, g = gates_run(lib(), dt, act)
+    near(dX[:, g32], (dY * dA)[:, g32], np.abs(dY[:, g32]), (U[dt], 70 * F32), "dX")
+    s = (2.0**-16 if dt == "bf16" else 0) + (70 + 37) * F32
+    near(g["W_gate"][:, g32], X.T @ (dY * dA)[:, g32], np.abs(X).T @ np.abs(dY[:, g32]), (0, s), "W_gate")
