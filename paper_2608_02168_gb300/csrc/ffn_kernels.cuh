@@ -38,10 +38,16 @@ __device__ __forceinline__ float gate_half(float x) {
   return 0.7213475204444817f * x;
 }
 
+// The positive part, NaN as it is.
+__device__ __forceinline__ float gate_relu(float x) {
+  asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(x));
+  return x;
+}
+
 // kAct: hg_act.  The gate's value; s r is at most 1/2, so no factor carries a large x past the largest number.
 template <int kAct>
 __device__ __forceinline__ float gate(float x) {
-  if (kAct == HG_ACT_RELU) return x > 0.f ? x : 0.f;
+  if (kAct == HG_ACT_RELU) return gate_relu(x);
   if (kAct == HG_ACT_NONE) return x;
   const Logistic l(fminf(gate_half<kAct>(x), 30.f));
   return (x * (l.s * l.r)) * l.s;
@@ -54,7 +60,7 @@ template <int kAct>
 __device__ __forceinline__ float gate_grad(float x, float* d) {
   if (kAct == HG_ACT_RELU) {
     *d = x > 0.f ? 1.f : 0.f;
-    return x > 0.f ? x : 0.f;
+    return gate_relu(x);
   }
   if (kAct == HG_ACT_NONE) {
     *d = 1.f;

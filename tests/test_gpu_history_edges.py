@@ -78,3 +78,24 @@ def test_derivatives_of_gates_of_every_size(dt, act):
     near(dX[:, g32], (dY * dA)[:, g32], np.abs(dY[:, g32]), (U[dt], 70 * F32), "dX")
     s = (2.0**-16 if dt == "bf16" else 0) + (70 + 37) * F32
     near(g["W_gate"][:, g32], X.T @ (dY * dA)[:, g32], np.abs(X).T @ np.abs(dY[:, g32]), (0, s), "W_gate")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh", "relu", "none"])
+def test_a_gate_that_is_nan_is_seen(dt, act):
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    X, Wg, Wu, Wd, dY = gates_problem(dt)
+    X[:, :32] = np.clip(X[:, :32], -4, 4)
+    Wg[63, 40] = np.nan  # one hidden feature's gate, of every row
+    n, d = X.shape
+    p = hg.FfnParams(*(dev(w, td) for w in (Wg, Wu, Wd)), act=act)
+    work = torch.empty(max(hg.hg_ffn_workspace_size(p, n)), dtype=torch.uint8, device="cuda")
+    Y, dX = torch.zeros(n, d, dtype=td, device="cuda"), torch.zeros(n, d, dtype=td, device="cuda")
+    g = {k: torch.zeros(d, d, device="cuda") for k in ("W_gate", "W_up", "W_down")}
+    hg.hg_ffn_fwd(p, dev(X, td), Y, work)
+    assert torch.isnan(Y).all()  # the feature is a term of every column
+    dY[:, 40] = 1
+    hg.hg_ffn_bwd(p, dev(X, td), dev(dY, td), dX, g, work)
+    assert torch.isnan(dX).all() and torch.isnan(g["W_up"][:, 40]).all() and torch.isnan(g["W_down"][40]).all()
