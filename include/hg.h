@@ -583,9 +583,9 @@ hg_status hg_decay_workspace_size(const hg_decay_params* params, int64_t n, int6
  * sequence's length on are not read and get zero in o.  S_in, S_out: device fp32 [n][heads][d_h][d_h]
  * (key feature x value feature); S_in NULL = zero, S_out NULL = not wanted; S_out (the state after the last
  * position in use; S_in for an empty sequence) may be S_in itself.  o overlaps none of q, k, v.
- * In bf16 storage positions are taken 16 at a time, and an infinity or NaN in v (or k) at a position in use can reach
- * the earlier rows of its 16 as NaN; positions that are not in use are never looked at.  Scratch: NULL where its size
- * is zero. */
+ * An infinity or NaN at a position in use reaches no earlier row, and in hg_decay_bwd no later row of dk and dv; what it
+ * does reach can be NaN where the definition has an infinity.  Positions that are not in use are never looked at.
+ * Scratch: NULL where its size is zero. */
 hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
                        const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* o, float* S_out,
                        void* scratch, hg_stream stream);

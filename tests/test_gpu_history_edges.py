@@ -7,7 +7,7 @@ import torch
 from hgsynth import bf16_round
 from oracle import history as OH
 from tests.gpu_util import dev, lib, need_gpu, tdtype
-from tests.test_gpu_history import F32, U, f64, near, nans
+from tests.test_gpu_history import F32, U, decay_problem, decay_rel, f64, host, nans, near, past, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +99,59 @@ def test_a_gate_that_is_nan_is_seen(dt, act):
     dY[:, 40] = 1
     hg.hg_ffn_bwd(p, dev(X, td), dev(dY, td), dX, g, work)
     assert torch.isnan(dX).all() and torch.isnan(g["W_up"][:, 40]).all() and torch.isnan(g["W_down"][40]).all()
+
+
+# ------------------------------------------------------------------------------------------------- decay
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("T,h,dh", [(40, 2, 32), (37, 1, 16), (40, 2, 64), (20, 1, 128), (900, 1, 64)])
+def test_decay_is_causal_whatever_the_values(dt, bad, T, h, dh):
+    """An infinity or NaN at one position of one head: o, dq at earlier positions and dk, dv at later ones are what they
+    are without it, and so are the other heads and, where it is a value feature, the other columns."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    at = [0, 5, 7, 15, 16, 23, T - 1]
+    n = len(at)
+    q, k, v, do, lens, S, dS = decay_problem(dt, n, T, h, dh, T + dh, False, True)
+    lens = np.full(n, T, np.int32)
+    lens[2] = 9
+    at = np.minimum(at, lens - 1)
+    c = np.float64(np.float32(0.3))
+    ld = np.array([-0.05, -0.4], np.float32)[:h]
+    p = hg.DecayParams(dev(ld), dh, td, scale=0.3)
+    work = torch.empty(max(hg.hg_decay_workspace_size(p, n, T)), dtype=torch.uint8, device="cuda")
+    args = [f64(x) for x in (q, k, v)] + [f64(ld), c]
+    names = ("o", "last", "dq", "dk", "dv", "dS")
+    want, terms = ({**dict(zip(names, OH.decay_forward(*args, lens, f64(S), magnitude=m))),
+                    **dict(zip(names[2:], OH.decay_backward(*args, f64(do), lens, f64(S), f64(dS), magnitude=m)))}
+                   for m in (False, True))
+    t = np.arange(T)[None]
+    before, after, own = t < at[:, None], t > at[:, None], t == at[:, None]
+    every, none = np.ones((n, T), bool), np.zeros((n, T), bool)
+    # which positions of the poisoned head an array's bad value leaves alone, and whether it is held to a column
+    reach = {"q": dict(o=~own, dq=every, dk=(after, True), dv=after), "k": dict(o=before, dq=(before, True), dk=every, dv=~own),
+             "v": dict(o=(before, True), dq=before, dk=~own, dv=every),
+             "do": dict(o=every, dq=~own, dk=after, dv=(after, True))}
+    for name, clean in reach.items():
+        x = {"q": q, "k": k, "v": v, "do": do}
+        x[name] = x[name].copy()
+        x[name][np.arange(n), at, 0, 3] = bad * (1 if name != "k" else -1)
+        Q, K, V, DO = (strided(past(y, lens), td) for y in x.values())
+        o = nans((n, T, h, dh), td)
+        hg.hg_decay_fwd(p, Q, K, V, dev(lens), dev(S), o, None, work)
+        g = [nans((n, T, h, dh), td) for _ in range(3)] + [nans((n, h, dh, dh), torch.float32)]
+        hg.hg_decay_bwd(p, Q, K, V, dev(lens), dev(S), DO, dev(dS), *g, work)
+        for out, got in zip(("o", "dq", "dk", "dv"), (o, *g[:3])):
+            rows = clean[out]
+            rows, column = rows if isinstance(rows, tuple) else (rows, False)
+            good = np.ones((n, T, h, dh), bool)
+            good[:, :, 0] = rows[..., None]
+            if column:
+                good[:, :, 0, np.arange(dh) != 3] = True
+            got = host(got)
+            live = np.broadcast_to((t < lens[:, None])[:, :, None, None], good.shape)
+            assert not np.isfinite(got[~good & live]).any(), (name, out)
+            assert (got[~live] == 0).all()
+            near(torch.from_numpy(np.where(good, got, 0)), np.where(good, want[out], 0), np.where(good, terms[out], 0),
+                 decay_rel(dt, T, dh, "rows"), (name, out))
