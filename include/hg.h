@@ -513,7 +513,9 @@ hg_status hg_temporal_bwd(const hg_temporal_params* params, const void* X, const
  * values of the storage type; rows lie `stride` values apart (for hg_seq: row t of sequence i at
  * p + i * stride_n + t * stride_t), so a slice of a wider projection row can be passed as it is.  p must
  * be 16-byte aligned and each stride a multiple of 16 bytes, non-negative, and (for arrays written) such
- * that no two rows overlap; a stride that no second row uses is not looked at. */
+ * that no two rows overlap; a stride that no second row uses is not looked at.  Arrays may share memory between their
+ * rows (all of them slices of one wide row); rows of an output that meet another array's are refused where both
+ * arrays have the same strides, or where the first or last row of one meets the other. */
 typedef struct {
   void* p;
   int64_t stride;

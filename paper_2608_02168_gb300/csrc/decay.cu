@@ -19,6 +19,7 @@
 #include <initializer_list>
 
 #include "decay_kernels.cuh"
+#include "row_sets.cuh"
 
 namespace hg {
 
@@ -368,9 +369,18 @@ hg_status check_seq(const hg_seq* r, const char* name, int64_t n, int64_t T, int
   return HG_OK;
 }
 
-// Rows that are written start at none of the rows that are read.
-hg_status check_apart(const hg_seq* out, const char* name, std::initializer_list<const hg_seq*> in) {
-  for (const hg_seq* r : in) HG_REQUIRE(out->p != r->p, "%s must not overlap an input", name);
+// Rows that are written meet none of the others.
+hg_status check_apart(const hg_seq* out, const char* name, int64_t n, int64_t T, int64_t width, size_t esz,
+                      std::initializer_list<const hg_seq*> others) {
+  auto set = [&](const hg_seq* r) { return row_set(r->p, n, T, r->stride_n, r->stride_t, width, esz); };
+  for (const hg_seq* r : others) HG_REQUIRE(!rows_meet(set(out), set(r)), "%s must not overlap another array", name);
+  return HG_OK;
+}
+
+// A state that is written is another one itself, or shares nothing with it.
+hg_status check_state(const hg_decay_params* p, int64_t n, const float* out, const float* in, const char* names) {
+  const size_t bytes = sizeof(float) * (size_t)n * p->heads * p->d_h * p->d_h;
+  HG_REQUIRE(!shifted(out, in, bytes), "%s must not overlap", names);
   return HG_OK;
 }
 
@@ -451,12 +461,13 @@ extern "C" hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q
     HG_TRY(check_seq(k, "k", n, T, w, esz, false));
     HG_TRY(check_seq(v, "v", n, T, w, esz, false));
     HG_TRY(check_seq(o, "o", n, T, w, esz, true));
-    HG_TRY(check_apart(o, "o", {q, k, v}));
+    HG_TRY(check_apart(o, "o", n, T, w, esz, {q, k, v}));
     a.q = rows_of(q, n, T);
     a.k = rows_of(k, n, T);
     a.v = rows_of(v, n, T);
     a.o = rows_of(o, n, T);
   }
+  HG_TRY(check_state(params, n, S_out, S_in, "S_out and S_in"));
   a.lens = lens;
   a.ld = params->log_decay;
   a.init = S_in;
@@ -496,9 +507,9 @@ extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q
     HG_TRY(check_seq(dq, "dq", n, T, w, esz, true));
     HG_TRY(check_seq(dk, "dk", n, T, w, esz, true));
     HG_TRY(check_seq(dv, "dv", n, T, w, esz, true));
-    HG_TRY(check_apart(dq, "dq", {q, k, v, d_o, dk, dv}));
-    HG_TRY(check_apart(dk, "dk", {q, k, v, d_o, dv}));
-    HG_TRY(check_apart(dv, "dv", {q, k, v, d_o}));
+    HG_TRY(check_apart(dq, "dq", n, T, w, esz, {q, k, v, d_o, dk, dv}));
+    HG_TRY(check_apart(dk, "dk", n, T, w, esz, {q, k, v, d_o, dv}));
+    HG_TRY(check_apart(dv, "dv", n, T, w, esz, {q, k, v, d_o}));
     rq = rows_of(q, n, T);
     rk = rows_of(k, n, T);
     rv = rows_of(v, n, T);
@@ -514,6 +525,8 @@ extern "C" hg_status hg_decay_bwd(const hg_decay_params* params, const hg_seq* q
   a.heads = params->heads;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   HG_REQUIRE(!dS_in || dS_in != S_in, "dS_in must not overlap S_in");
+  HG_TRY(check_state(params, n, dS_in, S_in, "dS_in and S_in"));
+  HG_TRY(check_state(params, n, dS_in, dS_out, "dS_in and dS_out"));
   ScanArgs g[3] = {a, a, a};
   ScanArgs &aq = g[0], &ak = g[1], &av = g[2];
   aq.q = ro;  // dq
@@ -592,10 +605,15 @@ extern "C" hg_status hg_decay_step(const hg_decay_params* params, const hg_rows*
     HG_REQUIRE(in[x] != nullptr, "%s must be non-null", names[x]);
     const hg_seq r{in[x]->p, in[x]->stride, 0};
     HG_TRY(check_seq(&r, names[x], n, 1, w, esz, x == 3));
-    HG_REQUIRE(x == 3 || !o || in[x]->p != o->p, "o must not overlap an input");
+  }
+  const hg_seq out{o->p, o->stride, 0};
+  for (int x = 0; x < 3; ++x) {
+    const hg_seq r{in[x]->p, in[x]->stride, 0};
+    HG_TRY(check_apart(&out, "o", n, 1, w, esz, {&r}));
   }
   HG_REQUIRE(S_in && S_out, "S_in and S_out must be non-null");
   HG_REQUIRE((((uintptr_t)S_in | (uintptr_t)S_out) & 15) == 0, "S_in and S_out must be 16-byte aligned");
+  HG_TRY(check_state(params, n, S_out, S_in, "S_out and S_in"));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (params->dtype == HG_F32) return step_w<float>(params, q, k, v, live, n, S_in, o, S_out, s);
   return step_w<__nv_bfloat16>(params, q, k, v, live, n, S_in, o, S_out, s);

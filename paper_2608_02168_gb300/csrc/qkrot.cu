@@ -21,6 +21,7 @@
 #include <initializer_list>
 
 #include "hg_internal.cuh"
+#include "row_sets.cuh"
 
 namespace hg {
 
@@ -302,11 +303,19 @@ hg_status check_rows(const hg_rows* r, const char* name, int64_t n, int64_t widt
   return HG_OK;
 }
 
-// An output may be its own input, rows at the same places; it starts at no other array's rows.
-hg_status check_apart(const hg_rows* out, const hg_rows* own, const char* name, int64_t n,
-                      std::initializer_list<const hg_rows*> others) {
-  HG_REQUIRE(out->p != own->p || n < 2 || out->stride == own->stride, "%s: in place, the strides must agree", name);
-  for (const hg_rows* r : others) HG_REQUIRE(!r || out->p != r->p, "%s must not overlap another array", name);
+// A call's rows with their width.
+struct Rows {
+  const hg_rows* r;
+  int64_t width;
+};
+
+// An output may be its own input, rows at the same places; it meets no other array's rows.
+hg_status check_apart(Rows out, Rows own, const char* name, int64_t n, size_t esz, std::initializer_list<Rows> others) {
+  auto set = [&](Rows x) { return row_set(x.r->p, n, 1, x.r->stride, 0, x.width, esz); };
+  const bool same = out.r->p == own.r->p;
+  HG_REQUIRE(!same || n < 2 || out.r->stride == own.r->stride, "%s: in place, the strides must agree", name);
+  HG_REQUIRE(same || !rows_meet(set(out), set(own)), "%s must not overlap an input but in place", name);
+  for (Rows x : others) HG_REQUIRE(!rows_meet(set(out), set(x)), "%s must not overlap another array", name);
   return HG_OK;
 }
 
@@ -362,10 +371,10 @@ extern "C" hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* 
   if (wk) {
     HG_TRY(check_rows(k, "k", n, wk, esz, false));
     HG_TRY(check_rows(k_out, "k_out", n, wk, esz, true));
-    HG_TRY(check_apart(q_out, q, "q_out", n, {k, k_out}));
-    HG_TRY(check_apart(k_out, k, "k_out", n, {q}));
+    HG_TRY(check_apart({q_out, wq}, {q, wq}, "q_out", n, esz, {{k, wk}, {k_out, wk}}));
+    HG_TRY(check_apart({k_out, wk}, {k, wk}, "k_out", n, esz, {{q, wq}}));
   } else {
-    HG_TRY(check_apart(q_out, q, "q_out", n, {}));
+    HG_TRY(check_apart({q_out, wq}, {q, wq}, "q_out", n, esz, {}));
   }
   RotArgs a;
   fill_args(&a, params, pos, n);
@@ -400,10 +409,10 @@ extern "C" hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* 
     HG_TRY(check_rows(k, "k", n, wk, esz, false));
     HG_TRY(check_rows(dk_out, "dk_out", n, wk, esz, false));
     HG_TRY(check_rows(dk, "dk", n, wk, esz, true));
-    HG_TRY(check_apart(dq, dq_out, "dq", n, {q, k, dk_out, dk}));
-    HG_TRY(check_apart(dk, dk_out, "dk", n, {q, k, dq_out}));
+    HG_TRY(check_apart({dq, wq}, {dq_out, wq}, "dq", n, esz, {{q, wq}, {k, wk}, {dk_out, wk}, {dk, wk}}));
+    HG_TRY(check_apart({dk, wk}, {dk_out, wk}, "dk", n, esz, {{q, wq}, {k, wk}, {dq_out, wq}}));
   } else {
-    HG_TRY(check_apart(dq, dq_out, "dq", n, {q}));
+    HG_TRY(check_apart({dq, wq}, {dq_out, wq}, "dq", n, esz, {{q, wq}}));
   }
   HG_REQUIRE(scratch != nullptr && ((uintptr_t)scratch & 255) == 0, "scratch must be non-null and 256-byte aligned");
   RotArgs a;

@@ -7,7 +7,7 @@ import torch
 from hgsynth import bf16_round
 from oracle import history as OH
 from tests.gpu_util import dev, lib, need_gpu, tdtype
-from tests.test_gpu_history import F32, U, decay_problem, decay_rel, f64, host, nans, near, past, strided
+from tests.test_gpu_history import F32, LD, U, decay_problem, decay_rel, f64, host, nans, near, past, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,39 @@ def test_decay_is_causal_whatever_the_values(dt, bad, T, h, dh):
             assert (got[~live] == 0).all()
             near(torch.from_numpy(np.where(good, got, 0)), np.where(good, want[out], 0), np.where(good, terms[out], 0),
                  decay_rel(dt, T, dh, "rows"), (name, out))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("swap", [False, True])
+def test_outputs_between_inputs_in_the_same_rows(dt, swap):
+    """Every array a slice of one wide row (or positions outside, sequences inside): accepted, the bits of arrays apart,
+    and nothing else written."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    n, T, h, dh = 5, 21, 2, 32
+    q, k, v, do, lens, S, dS = decay_problem(dt, n, T, h, dh, 4, True, True)
+    p, r = hg.DecayParams(dev(LD[:h]), dh, td), hg.QkRotParams(None, None, h, h, d_h=dh, dtype=td)
+    wide = nans((T, n, 11, h, dh) if swap else (n, T, 11, h, dh), td)
+    view = wide.transpose(0, 1) if swap else wide
+    x = [view[:, :, i] for i in (0, 2, 4, 6)]
+    out = [view[:, :, i] for i in (1, 3, 5, 7)]
+    for a, b in zip(x, (q, k, v, do)):
+        a.copy_(dev(b, td))
+    want = [nans((n, T, h, dh), td) for _ in range(4)]
+    for y, o in ((x, out), ([a.contiguous() for a in x], want)):
+        hg.hg_decay_fwd(p, *y[:3], dev(lens), dev(S), o[0], None, None)
+        hg.hg_decay_bwd(p, *y[:3], dev(lens), dev(S), y[3], dev(dS), *o[1:], None, None)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert all(torch.equal(a, dev(b, td)) for a, b in zip(x, (q, k, v, do))) and torch.isnan(view[:, :, 8:]).all()
+    rows = [wide.view(n * T, 11, h, dh)[:, i] for i in (8, 9, 0, 2)]
+    hg.hg_qkrot_fwd(r, rows[2], rows[3], None, rows[0], rows[1])
+    a, b = nans((n * T, h, dh), td), nans((n * T, h, dh), td)
+    hg.hg_qkrot_fwd(r, rows[2].contiguous(), rows[3].contiguous(), None, a, b)
+    assert torch.equal(rows[0], a) and torch.equal(rows[1], b)
+    hg.hg_qkrot_fwd(r, rows[2], rows[3], None, rows[2], rows[3])  # in place, side by side
+    assert torch.equal(rows[2], a) and torch.equal(rows[3], b) and torch.isnan(view[:, :, 10]).all()
+    with pytest.raises(hg.HGError, match="overlap"):
+        hg.hg_decay_fwd(p, *x[:3], dev(lens), None, view[:, :, 4:6].flatten(2, 3)[:, :, 1:3], None, None)
+    with pytest.raises(hg.HGError, match="overlap"):
+        hg.hg_qkrot_fwd(r, rows[2][:-1], rows[3][:-1], None, rows[2][1:], rows[3][:-1])

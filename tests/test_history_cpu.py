@@ -390,3 +390,73 @@ def test_parameters_that_would_be_copies_are_refused(hg):
     with pytest.raises(ValueError, match="must be contiguous"):
         hg.DecayParams(stand_in(8, dtype=torch.float32)[::2], 32, torch.bfloat16)
     assert hg.FfnParams(w.contiguous(), ok, stand_in(96, 64)).c().W_gate != w.data_ptr()
+
+
+def test_rows_that_meet_without_starting_together_are_refused(hg):
+    """Outputs a row, a sequence or a part of a row further on than another array; strides alike and not."""
+    so = hg.lib()
+    B = A + (1 << 28)
+
+    def refused(status):
+        return status == 1 and b"overlap" in so.hg_last_error()
+
+    # rotation, 10 rows of 256 bytes (q) and 128 (k), 1024 bytes apart
+    qp = ctypes.byref(hg.hg_qkrot_params(4, 2, 32, 32, 0, 1, 1e-6, 1e4, None, None))
+    far = [B + (i << 22) for i in range(6)]
+
+    def rot(q=far[0], k=far[1], qo=far[2], ko=far[3], stride=512, ostride=512):
+        return so.hg_qkrot_fwd(qp, rows(hg, q, stride), rows(hg, k, stride), None, 10, rows(hg, qo, ostride),
+                               rows(hg, ko, ostride), None)
+
+    for shift in (1024, -1024, 9 * 1024, -9 * 1024, 128, -128, 5 * 1024 + 240, -5 * 1024 - 240):
+        assert refused(rot(qo=far[0] + shift)), shift            # q_out over q, not in place
+    for shift in (1024, -1024, 9 * 1024, -9 * 1024, 128, -112, 5 * 1024 + 240, -5 * 1024 - 112):
+        assert refused(rot(ko=far[2] + shift)), shift            # k_out over q_out
+    assert refused(rot(qo=far[1] + 3 * 1024 + 112)) and refused(rot(ko=far[0] - 112))
+    assert refused(rot(qo=far[0] + 1024, ostride=256)) and refused(rot(qo=far[0] - 512, ostride=128))
+
+    def rot_bwd(**k):
+        p = {**dict(zip(("q", "k", "dqo", "dko", "dq", "dk"), far)), **k}
+        r = [rows(hg, x, 512) for x in p.values()]
+        return so.hg_qkrot_bwd(qp, r[0], r[1], None, 10, *r[2:], None, None, A, None)
+
+    assert refused(rot_bwd(dq=far[2] + 1024)) and refused(rot_bwd(dq=far[0] + 2048)) and refused(rot_bwd(dk=far[3] - 1024))
+    assert refused(rot_bwd(dk=far[4] + 1024)) and refused(rot_bwd(dk=far[2] + 9 * 1024))
+
+    # scan, 3 sequences 8192 bytes apart of 5 rows of 256 bytes 1024 apart; and the other way round
+    dp = ctypes.byref(hg.hg_decay_params(4, 32, 1, 1.0, A))
+    for sn, st, one in ((4096, 512, 1024), (512, 4096, 8192)):
+        def fwd(o, osn=sn, ost=st, q=far[0], sn=sn, st=st):
+            s = [seq(hg, x, sn, st) for x in (q, far[1], far[2])]
+            return so.hg_decay_fwd(dp, *s, None, 3, 5, None, seq(hg, o, osn, ost), None, None, None)
+
+        for x in far[:3]:
+            for shift in (one, -one, 8192, -8192, 1024, -1024, 112, -240, 2 * 8192 + 1024):
+                assert refused(fwd(x + shift)), (sn, shift)
+        assert refused(fwd(far[0] + 128, q=far[0], osn=640, ost=128)) and refused(fwd(far[1] + 2048, osn=128, ost=384))
+
+        def bwd(i, x):
+            p = [B + (j << 22) for j in range(7)]
+            p[i] = x
+            s = [seq(hg, y, sn, st) for y in p]
+            return so.hg_decay_bwd(dp, *s[:3], None, 3, 5, None, s[3], None, *s[4:], None, None, None)
+
+        for i in (4, 5, 6):
+            for j in range(7):
+                assert i == j or refused(bwd(i, B + (j << 22) + one)), (i, j)
+
+    # the step's rows; states that are moved, not the same
+    S, size = B + (1 << 26), 3 * 4 * 32 * 32 * 4
+
+    def step(o=far[3], S_in=S, S_out=S):
+        r = [rows(hg, x, 512) for x in far[:3]]
+        return so.hg_decay_step(dp, *r, None, 3, S_in, rows(hg, o, 512), S_out, None)
+
+    assert all(refused(step(o=x + y)) for x in far[:3] for y in (1024, -1024, 128))
+    for y in (16, -16, size - 16, 16 - size):
+        assert refused(step(S_out=S + y))
+        s = [seq(hg, x) for x in far[:4]]
+        assert refused(so.hg_decay_fwd(dp, *s[:3], None, 3, 5, S, s[3], S + y, None, None))
+        g = [seq(hg, B + (j << 22)) for j in range(7)]
+        for a, b in ((S, None), (None, S)):
+            assert refused(so.hg_decay_bwd(dp, *g[:3], None, 3, 5, a, g[3], b, *g[4:], S + y, None, None))
