@@ -558,7 +558,7 @@ hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* q, const hg
                        int64_t n, const hg_rows* q_out, const hg_rows* k_out, hg_stream stream);
 
 /* Gradients for the upstream gradients dq_out, dk_out: dq, dk (OVERWRITTEN, may be dq_out, dk_out
- * themselves) and dgamma_q, dgamma_k (device fp32 [d_h], OVERWRITTEN; NULL = not wanted).  q, k, pos are
+ * themselves) and dgamma_q, dgamma_k (device fp32 [d_h], apart, OVERWRITTEN; NULL = not wanted).  q, k, pos are
  * those of the forward (its inputs: nothing is saved).  The gains' sums have a fixed order. */
 hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* q, const hg_rows* k, const int64_t* pos,
                        int64_t n, const hg_rows* dq_out, const hg_rows* dk_out, const hg_rows* dq,
@@ -623,7 +623,7 @@ typedef struct {
   const void* W_down;
 } hg_ffn_params;
 
-/* Gradients, device fp32, OVERWRITTEN: dW_gate, dW_up [d x f], dW_down [f x d]. */
+/* Gradients, device fp32, apart, OVERWRITTEN: dW_gate, dW_up [d x f], dW_down [f x d]. */
 typedef struct {
   float* dW_gate;
   float* dW_up;

@@ -13,6 +13,7 @@
 
 #include "ffn_kernels.cuh"
 #include "ffn_tc.cuh"
+#include "row_sets.cuh"
 
 namespace hg {
 
@@ -367,9 +368,7 @@ hg_status check_params(const hg_ffn_params* p, int64_t n) {
 
 // Two arrays of n x d values share no byte.
 hg_status check_apart(const hg_ffn_params* p, int64_t n, const void* out, const void* in, const char* names) {
-  const size_t bytes = (size_t)n * p->d * (p->dtype == HG_BF16 ? 2 : 4);
-  const uintptr_t a = (uintptr_t)out, b = (uintptr_t)in;
-  HG_REQUIRE(a >= b + bytes || b >= a + bytes, "%s must not overlap", names);
+  HG_REQUIRE(!shared(out, in, (size_t)n * p->d * (p->dtype == HG_BF16 ? 2 : 4)), "%s must not overlap", names);
   return HG_OK;
 }
 
@@ -424,6 +423,9 @@ extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int6
              "gradients must be 16-byte aligned");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const size_t wbytes = sizeof(float) * (size_t)params->d * params->f;
+  HG_REQUIRE(!grads || !(shared(grads->dW_gate, grads->dW_up, wbytes) || shared(grads->dW_gate, grads->dW_down, wbytes) ||
+                         shared(grads->dW_up, grads->dW_down, wbytes)),
+             "the gradients must not overlap one another");
   if (n == 0) {
     if (grads) {
       HG_CUDA(cudaMemsetAsync(grads->dW_gate, 0, wbytes, s));

@@ -394,6 +394,7 @@ extern "C" hg_status hg_qkrot_bwd(const hg_qkrot_params* params, const hg_rows* 
   clear_error();
   HG_TRY(device_guard());
   HG_TRY(check_params(params, n));
+  HG_REQUIRE(!shared(dgamma_q, dgamma_k, sizeof(float) * params->d_h), "dgamma_q and dgamma_k must not overlap");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (n == 0) {
     if (dgamma_q) HG_CUDA(cudaMemsetAsync(dgamma_q, 0, sizeof(float) * params->d_h, s));

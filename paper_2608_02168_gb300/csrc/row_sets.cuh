@@ -60,10 +60,11 @@ inline bool rows_meet(const RowSet& out, const RowSet& in) {
   return false;
 }
 
-// Whether two arrays of the same size share memory without being the same.
-inline bool shifted(const void* a, const void* b, size_t bytes) {
+// Whether two arrays of the same size (null: none) share memory; whether they do without being the same.
+inline bool shared(const void* a, const void* b, size_t bytes) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return a && b && x != y && x < y + bytes && y < x + bytes;
+  return a && b && x < y + bytes && y < x + bytes;
 }
+inline bool shifted(const void* a, const void* b, size_t bytes) { return a != b && shared(a, b, bytes); }
 
 }  // namespace hg

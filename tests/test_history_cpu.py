@@ -460,3 +460,23 @@ def test_rows_that_meet_without_starting_together_are_refused(hg):
         g = [seq(hg, B + (j << 22)) for j in range(7)]
         for a, b in ((S, None), (None, S)):
             assert refused(so.hg_decay_bwd(dp, *g[:3], None, 3, 5, a, g[3], b, *g[4:], S + y, None, None))
+
+
+def test_gradients_of_two_parameters_in_one_place_are_refused(hg):
+    """Each is overwritten, none added to: one buffer for the gains of queries and keys would keep either."""
+    so = hg.lib()
+    P = [A + (i << 24) for i in range(8)]
+    qp = ctypes.byref(hg.hg_qkrot_params(4, 4, 32, 32, 0, 1, 1e-6, 1e4, None, None))
+    r = [rows(hg, x) for x in P[:6]]
+    for n in (10, 0):
+        for shift in (0, 4, -4, 124):
+            assert so.hg_qkrot_bwd(qp, r[0], r[1], None, n, *r[2:6], P[6], P[6] + shift, A, None) == 1
+            assert b"overlap" in so.hg_last_error()
+    fp = ctypes.byref(hg.hg_ffn_params(64, 96, 1, 3, 1, A, A, A))
+    for i, j in ((0, 1), (0, 2), (1, 2)):
+        for shift in (0, 16, 64 * 96 * 4 - 16):
+            g = P[:3]
+            g[j] = g[i] + shift
+            for n in (10, 0):
+                assert so.hg_ffn_bwd(fp, P[3], n, P[4], P[5], ctypes.byref(hg.hg_ffn_grads(*g)), A, None) == 1
+                assert b"overlap" in so.hg_last_error()
