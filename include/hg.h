@@ -630,7 +630,7 @@ typedef struct {
   float* dW_down;
 } hg_ffn_grads;
 
-/* Scratch of hg_ffn_fwd and hg_ffn_bwd for n rows. */
+/* Scratch of hg_ffn_fwd and hg_ffn_bwd for n rows.  hg_ffn_bwd in bf16 without weight gradients needs none (NULL). */
 hg_status hg_ffn_workspace_size(const hg_ffn_params* params, int64_t n, size_t* fwd_bytes, size_t* bwd_bytes);
 
 /* X, Y: n x d, row-major, storage type, 16-byte aligned; Y does not overlap X.  scratch may be NULL in bf16 (its size is

@@ -423,7 +423,8 @@ extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int6
              "gradients must be 16-byte aligned");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const size_t wbytes = sizeof(float) * (size_t)params->d * params->f;
-  HG_REQUIRE(!grads || !(shared(grads->dW_gate, grads->dW_up, wbytes) || shared(grads->dW_gate, grads->dW_down, wbytes) ||
+  HG_REQUIRE(!grads || !(shared(grads->dW_gate, grads->dW_up, wbytes) ||
+                         shared(grads->dW_gate, grads->dW_down, wbytes) ||
                          shared(grads->dW_up, grads->dW_down, wbytes)),
              "the gradients must not overlap one another");
   if (n == 0) {
@@ -434,7 +435,8 @@ extern "C" hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int6
     }
     return HG_OK;
   }
-  HG_REQUIRE(X && dY && scratch, "X, dY and scratch must be non-null");
+  HG_REQUIRE(X && dY, "X and dY must be non-null");
+  HG_REQUIRE(scratch || (params->dtype == HG_BF16 && !grads), "scratch must be non-null");
   HG_REQUIRE((((uintptr_t)X | (uintptr_t)dY | (uintptr_t)dX) & 15) == 0, "X, dY and dX must be 16-byte aligned");
   if (dX) {
     HG_TRY(check_apart(params, n, dX, X, "dX and X"));

@@ -826,14 +826,15 @@ def hg_ffn_fwd(params: FfnParams, X, Y, scratch, stream=None):
 
 
 def hg_ffn_bwd(params: FfnParams, X, dY, dX, grads: dict | None, scratch, stream=None):
-    """dX None or grads None skips that part; grads: W_gate, W_up, W_down (fp32)."""
+    """dX None or grads None skips that part; grads: W_gate, W_up, W_down (fp32).  bf16 without grads needs no scratch."""
     n, shape = X.shape[0], (X.shape[0], params.d)
     gr = None
     if grads is not None:
         df, fd = (params.d, params.f), (params.f, params.d)
         gr = byref(hg_ffn_grads(*(_want(grads[k], k, torch.float32, s)
                                   for k, s in (("W_gate", df), ("W_up", df), ("W_down", fd)))))
-    w = _work_ptr(scratch, hg_ffn_workspace_size(params, n)[1] if n else 0, "scratch")
+    none = n == 0 or (grads is None and params.dtype == torch.bfloat16)
+    w = _work_ptr(scratch, 0 if none else hg_ffn_workspace_size(params, n)[1], "scratch")
     _check(lib().hg_ffn_bwd(byref(params.c()), _want(X, "X", params.dtype, shape), n,
                             _want(dY, "dY", params.dtype, shape), _want(dX, "dX", params.dtype, shape), gr, w,
                             _stream(stream)), "hg_ffn_bwd")

@@ -191,3 +191,21 @@ def test_outputs_between_inputs_in_the_same_rows(dt, swap):
         hg.hg_decay_fwd(p, *x[:3], dev(lens), None, view[:, :, 4:6].flatten(2, 3)[:, :, 1:3], None, None)
     with pytest.raises(hg.HGError, match="overlap"):
         hg.hg_qkrot_fwd(r, rows[2][:-1], rows[3][:-1], None, rows[2][1:], rows[3][:-1])
+
+
+def test_ffn_input_gradient_alone_needs_no_scratch_in_bf16():
+    need_gpu()
+    hg = lib()
+    for td in (torch.bfloat16, torch.float32):
+        gen = torch.Generator(device="cuda").manual_seed(2)
+        new = lambda *s: torch.randn(*s, device="cuda", generator=gen).mul_(0.25).to(td)  # noqa: E731
+        X, dY, p = new(150, 64), new(150, 64), hg.FfnParams(new(64, 72), new(64, 72), new(72, 64))
+        work = torch.empty(hg.hg_ffn_workspace_size(p, 150)[1], dtype=torch.uint8, device="cuda")
+        a, b = nans((150, 64), td), nans((150, 64), td)
+        hg.hg_ffn_bwd(p, X, dY, a, None, work)
+        if td == torch.bfloat16:
+            hg.hg_ffn_bwd(p, X, dY, b, None, None)
+            assert torch.equal(a, b)
+        else:
+            with pytest.raises(ValueError, match="bytes are needed"):
+                hg.hg_ffn_bwd(p, X, dY, b, None, None)

@@ -480,3 +480,12 @@ def test_gradients_of_two_parameters_in_one_place_are_refused(hg):
             for n in (10, 0):
                 assert so.hg_ffn_bwd(fp, P[3], n, P[4], P[5], ctypes.byref(hg.hg_ffn_grads(*g)), A, None) == 1
                 assert b"overlap" in so.hg_last_error()
+
+
+def test_ffn_scratch_is_asked_for_where_it_is_used(hg):
+    so = hg.lib()
+    g = ctypes.byref(hg.hg_ffn_grads(A, A + (1 << 20), A + (2 << 20)))
+    for dt, grads in ((0, None), (0, g), (1, g)):
+        p = ctypes.byref(hg.hg_ffn_params(64, 96, dt, 3, 1, A, A, A))
+        assert so.hg_ffn_bwd(p, A, 10, A + (1 << 24), A + (2 << 24), grads, None, None) == 1
+        assert b"scratch" in so.hg_last_error()
