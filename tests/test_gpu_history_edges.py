@@ -7,7 +7,8 @@ import torch
 from hgsynth import bf16_round
 from oracle import history as OH
 from tests.gpu_util import dev, lib, need_gpu, tdtype
-from tests.test_gpu_history import F32, LD, U, decay_problem, decay_rel, f64, host, nans, near, past, strided
+from tests.test_gpu_history import (F32, LD, U, decay_problem, decay_rel, f64, host, nans, near, past, rot_problem,
+                                    rot_rel, strided)
 
 pytestmark = pytest.mark.gpu
 
@@ -59,8 +60,8 @@ g32 = slice(0, 32)
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["silu", "gelu_tanh", "relu", "none"])
 def test_values_of_gates_of_every_size(dt, act):
-    """act of gates from 0 to 1e30 of either sign.  G, U and dH are exact and a sum has one term: the functions within 30
-    steps of |x|, in bf16 H rounded once; dW_up sums 37 rows, in bf16 of two terms."""
+    """act of gates from 0 to 1e30 of either sign.  G, U and dH are exact and a sum has one term: the functions within
+    30 steps of |x|, in bf16 H rounded once; dW_up sums 37 rows, in bf16 of two terms."""
     need_gpu()
     X, dY, A, _, Y, _, g = gates_run(lib(), dt, act)
     near(Y[:, g32], A[:, g32], np.abs(X[:, g32]), (U[dt], 30 * F32), "Y")
@@ -71,8 +72,8 @@ def test_values_of_gates_of_every_size(dt, act):
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["silu", "gelu_tanh", "relu", "none"])
 def test_derivatives_of_gates_of_every_size(dt, act):
-    """act' of the same gates: that of a large one is 1 or 0.  Within 70 steps of 1 (a slope below 2.3 times 30 steps where
-    it is neither 0 nor 1), in bf16 dG rounded once; dW_gate sums 37 rows, in bf16 of two terms."""
+    """act' of the same gates: that of a large one is 1 or 0.  Within 70 steps of 1 (a slope below 2.3 times 30 steps
+    where it is neither 0 nor 1), in bf16 dG rounded once; dW_gate sums 37 rows, in bf16 of two terms."""
     need_gpu()
     X, dY, _, dA, _, dX, g = gates_run(lib(), dt, act)
     near(dX[:, g32], (dY * dA)[:, g32], np.abs(dY[:, g32]), (U[dt], 70 * F32), "dX")
@@ -99,6 +100,24 @@ def test_a_gate_that_is_nan_is_seen(dt, act):
     dY[:, 40] = 1
     hg.hg_ffn_bwd(p, dev(X, td), dev(dY, td), dX, g, work)
     assert torch.isnan(dX).all() and torch.isnan(g["W_up"][:, 40]).all() and torch.isnan(g["W_down"][40]).all()
+
+
+def test_ffn_input_gradient_alone_needs_no_scratch_in_bf16():
+    need_gpu()
+    hg = lib()
+    for td in (torch.bfloat16, torch.float32):
+        gen = torch.Generator(device="cuda").manual_seed(2)
+        new = lambda *s: torch.randn(*s, device="cuda", generator=gen).mul_(0.25).to(td)  # noqa: E731
+        X, dY, p = new(150, 64), new(150, 64), hg.FfnParams(new(64, 72), new(64, 72), new(72, 64))
+        work = torch.empty(hg.hg_ffn_workspace_size(p, 150)[1], dtype=torch.uint8, device="cuda")
+        a, b = nans((150, 64), td), nans((150, 64), td)
+        hg.hg_ffn_bwd(p, X, dY, a, None, work)
+        if td == torch.bfloat16:
+            hg.hg_ffn_bwd(p, X, dY, b, None, None)
+            assert torch.equal(a, b)
+        else:
+            with pytest.raises(ValueError, match="bytes are needed"):
+                hg.hg_ffn_bwd(p, X, dY, b, None, None)
 
 
 # ------------------------------------------------------------------------------------------------- decay
@@ -130,7 +149,8 @@ def test_decay_is_causal_whatever_the_values(dt, bad, T, h, dh):
     before, after, own = t < at[:, None], t > at[:, None], t == at[:, None]
     every, none = np.ones((n, T), bool), np.zeros((n, T), bool)
     # which positions of the poisoned head an array's bad value leaves alone, and whether it is held to a column
-    reach = {"q": dict(o=~own, dq=every, dk=(after, True), dv=after), "k": dict(o=before, dq=(before, True), dk=every, dv=~own),
+    reach = {"q": dict(o=~own, dq=every, dk=(after, True), dv=after),
+             "k": dict(o=before, dq=(before, True), dk=every, dv=~own),
              "v": dict(o=(before, True), dq=before, dk=~own, dv=every),
              "do": dict(o=every, dq=~own, dk=after, dv=(after, True))}
     for name, clean in reach.items():
@@ -193,19 +213,51 @@ def test_outputs_between_inputs_in_the_same_rows(dt, swap):
         hg.hg_qkrot_fwd(r, rows[2][:-1], rows[3][:-1], None, rows[2][1:], rows[3][:-1])
 
 
-def test_ffn_input_gradient_alone_needs_no_scratch_in_bf16():
+# ---------------------------------------------------------------------------------------------- rotation
+# A resident set of CTAs (three an SM, two backward) takes these rows in three rounds and more, the last one ragged:
+# heads in fours, in twos and odd, that divide a CTA's groups and that do not.
+MANY = [("bf16", 80_001, 2, 2, 16), ("bf16", 25_003, 2, 1, 64), ("bf16", 10_007, 5, 1, 64), ("bf16", 9_001, 5, 2, 64),
+        ("bf16", 13_003, 4, 0, 128), ("f32", 31_001, 2, 2, 32), ("f32", 21_001, 3, 0, 64), ("f32", 5_003, 5, 1, 128),
+        ("f32", 3_001, 6, 5, 128), ("bf16", 26_001, 3, 3, 32)]
+
+
+@pytest.mark.parametrize("dt,n,hq,hk,dh", MANY)
+def test_qkrot_of_many_rows(dt, n, hq, hk, dh):
+    """The bits of the rows in small batches, in which a group of lanes has one row, in place too; the gains' sums are
+    those of runs of at most ten rows a group, 256 groups a CTA and 57 CTAs a thread."""
     need_gpu()
     hg = lib()
-    for td in (torch.bfloat16, torch.float32):
-        gen = torch.Generator(device="cuda").manual_seed(2)
-        new = lambda *s: torch.randn(*s, device="cuda", generator=gen).mul_(0.25).to(td)  # noqa: E731
-        X, dY, p = new(150, 64), new(150, 64), hg.FfnParams(new(64, 72), new(64, 72), new(72, 64))
-        work = torch.empty(hg.hg_ffn_workspace_size(p, 150)[1], dtype=torch.uint8, device="cuda")
-        a, b = nans((150, 64), td), nans((150, 64), td)
-        hg.hg_ffn_bwd(p, X, dY, a, None, work)
-        if td == torch.bfloat16:
-            hg.hg_ffn_bwd(p, X, dY, b, None, None)
-            assert torch.equal(a, b)
-        else:
-            with pytest.raises(ValueError, match="bytes are needed"):
-                hg.hg_ffn_bwd(p, X, dY, b, None, None)
+    td = tdtype(dt)
+    rng, q, k, gq, gk, pos = rot_problem(dt, n, hq, hk, dh, n, True)
+    how = (dh, 1000.0, 1e-4, hq % 2 == 1)
+    p = hg.QkRotParams(dev(gq, td), dev(gk, td), hq, hk, rot=dh, base=1000.0, eps=1e-4, interleaved=how[3])
+    dy = [dev(x, td) for x in (rng.standard_normal((n, hq, dh)), rng.standard_normal((n, hk, dh)))]
+    Q, K, P = strided(q, td), strided(k, td), dev(pos)
+    work = torch.empty(hg.hg_qkrot_workspace_size(p, n), dtype=torch.uint8, device="cuda")
+    some = lambda x, s: x[s] if hk else None  # noqa: E731
+    out = [nans((n, hq, dh), td), nans((n, hk, dh), td), nans((n, hq, dh), td), nans((n, hk, dh), td)]
+    small = [x.clone() for x in out]
+    g = {"gamma_q": nans((dh,), torch.float32), "gamma_k": nans((dh,), torch.float32)}
+
+    def both(to, s, grads, work):
+        hg.hg_qkrot_fwd(p, Q[s], some(K, s), P[s], to[0][s], some(to[1], s))
+        hg.hg_qkrot_bwd(p, Q[s], some(K, s), P[s], dy[0][s], some(dy[1], s), to[2][s], some(to[3], s), grads, work)
+
+    both(out, slice(0, n), g, work)
+    for i in range(0, n, 997):
+        both(small, slice(i, min(i + 997, n)), {}, work)
+    assert all(torch.isfinite(x).all() and torch.equal(x, y) for x, y in zip(out, small))
+    e = rot_rel(dt)[1] + (10 + 256 + 57 + 8) * F32
+    for x, gain, d, key in ((q, gq, dy[0], "gamma_q"), (k, gk, dy[1], "gamma_k")):
+        x, gain, d = f64(x), f64(gain), host(d)
+        a, b = OH.pair_index(dh, how[3])
+        t = np.abs(d)
+        t[..., a] = t[..., b] = t[..., a] + t[..., b]
+        u = np.abs(x) / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-4)
+        near(g[key], OH.qkrot_backward(x, gain, pos, *how, d)[1], (t * u).sum((0, 1)), (0, e), key)
+    inq, ink = Q.contiguous(), K.contiguous()
+    hg.hg_qkrot_fwd(p, inq, ink if hk else None, P, inq, ink if hk else None)
+    assert torch.equal(inq, out[0]) and torch.equal(ink, out[1])
+    dq, dk = dy[0].clone(), dy[1].clone()
+    hg.hg_qkrot_bwd(p, Q, K if hk else None, P, dq, dk if hk else None, dq, dk if hk else None, {}, work)
+    assert torch.equal(dq, out[2]) and torch.equal(dk, out[3])
