@@ -120,6 +120,28 @@ def test_ffn_input_gradient_alone_needs_no_scratch_in_bf16():
                 hg.hg_ffn_bwd(p, X, dY, b, None, None)
 
 
+def test_long_sums_of_one_sign_do_not_shrink():
+    """Weight gradients of positive rows in one share of 157 row tiles (d 64, 152 chunks of hidden features).  Tensor
+    additions cut their results (2^-23 at most): 4 for each of U and dH (or G), 16 for a tile's rows, so the mean of the
+    relative errors is above -24 2^-23 = -2.9e-6.  The rest is rounded to nearest and does not lean: 157 tiles at 2^-24,
+    the two terms at 2^-17; all together below 2e-5 in any one value."""
+    need_gpu()
+    hg = lib()
+    n, d, f, td = 20_000, 64, 152 * 64, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda *s: torch.rand(*s, device="cuda", generator=gen).add_(0.5).to(td)  # noqa: E731
+    X, dY, Wg, Wu, Wd = new(n, d), new(n, d), new(d, f), new(d, f), new(f, d)
+    p = hg.FfnParams(Wg, Wu, Wd, act="none")
+    g = {k: nans(w.shape, torch.float32) for k, w in (("W_gate", Wg), ("W_up", Wu), ("W_down", Wd))}
+    hg.hg_ffn_bwd(p, X, dY, None, g, torch.empty(hg.hg_ffn_workspace_size(p, n)[1], dtype=torch.uint8, device="cuda"))
+    X, dY, Wg, Wu, Wd = (x.double() for x in (X, dY, Wg, Wu, Wd))
+    G, U_, dH = X @ Wg, X @ Wu, dY @ Wd.T
+    for key, want in (("W_gate", X.T @ (dH * U_)), ("W_up", X.T @ (dH * G)), ("W_down", (G * U_).T @ dY)):
+        off = g[key].double() / want - 1
+        assert off.abs().max() < 2e-5, (key, off.abs().max())
+        assert abs(off.mean()) < 4e-6, (key, off.mean())
+
+
 # ------------------------------------------------------------------------------------------------- decay
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
@@ -211,6 +233,36 @@ def test_outputs_between_inputs_in_the_same_rows(dt, swap):
         hg.hg_decay_fwd(p, *x[:3], dev(lens), None, view[:, :, 4:6].flatten(2, 3)[:, :, 1:3], None, None)
     with pytest.raises(hg.HGError, match="overlap"):
         hg.hg_qkrot_fwd(r, rows[2][:-1], rows[3][:-1], None, rows[2][1:], rows[3][:-1])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,dh", [(1, 16), (1, 32), (1, 128), (2, 64), (2, 32)])
+def test_decay_states_are_fp32_sums(dt, T, dh):
+    """States of one and two positions.  A term: its factor c gamma^t (the product 1, 2^x and x 6), the product with it
+    1, each of three tensor additions cut at 2^-23 (6), a last factor (7), and T such terms: 21 T steps of 2^-24 of
+    their sizes.  Two bf16 numbers for a scaled value, in place of three, would be seen: planted in the oracle here."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    n, h = 3, 2
+    q, k, v, do, *_ = decay_problem(dt, n, T, h, dh, T + dh, False, False)
+    c, ld = np.float64(np.float32(0.3)), np.array([0.0, -0.3], np.float32)
+    p = hg.DecayParams(dev(ld), dh, td, scale=0.3)
+    x = [dev(y, td) for y in (q, k, v)]
+    o, last, dlast = nans((n, T, h, dh), td), nans((n, h, dh, dh), torch.float32), nans((n, h, dh, dh), torch.float32)
+    work = torch.empty(max(hg.hg_decay_workspace_size(p, n, T)), dtype=torch.uint8, device="cuda")
+    hg.hg_decay_fwd(p, *x, None, None, o, last, work)
+    hg.hg_decay_bwd(p, *x, None, None, dev(do, td), None, *(nans((n, T, h, dh), td) for _ in range(3)), dlast, work)
+    args = [f64(y) for y in (q, k, v)] + [f64(ld), c]
+    rel = (0, 21 * T * F32)
+    near(last, OH.decay_forward(*args)[1], OH.decay_forward(*args, magnitude=True)[1], rel, "state")
+    want, size = (OH.decay_backward(*args, f64(do), magnitude=m)[3] for m in (False, True))
+    near(dlast, want, size, rel, "state's gradient")
+    y = (c * f64(do)).astype(np.float32)  # the planted mistake
+    hi = bf16_round(y)
+    two = f64(hi) + f64(bf16_round(y - hi))
+    off = OH.decay_backward(*args[:4], 1.0, two)[3]
+    assert (np.abs(off - want) > rel[1] * size).any()
 
 
 # ---------------------------------------------------------------------------------------------- rotation
