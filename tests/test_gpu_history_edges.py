@@ -265,6 +265,42 @@ def test_decay_states_are_fp32_sums(dt, T, dh):
     assert (np.abs(off - want) > rel[1] * size).any()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_every_call_repeats_its_bits(dt):
+    """Ragged histories that are claimed, segments, shares of rows: no sum's order depends on the run."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    n, T, h, dh = 60, 300, 4, 32
+    q, k, v, do, lens, S, dS = decay_problem(dt, n, T, h, dh, 1, True, True)
+    p = hg.DecayParams(dev(LD[:h]), dh, td, scale=0.25)
+    r = hg.QkRotParams(torch.ones(dh, dtype=td, device="cuda"), torch.ones(dh, dtype=td, device="cuda"), h, h)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    w = [torch.randn(*s, device="cuda", generator=gen).mul_(0.1).to(td) for s in ((128, 200), (128, 200), (200, 128))]
+    f = hg.FfnParams(*w)
+    Q, K, V, DO = (dev(x, td) for x in (q, k, v, do))
+    need = max(*hg.hg_decay_workspace_size(p, n, T), *hg.hg_ffn_workspace_size(f, n * T),
+               hg.hg_qkrot_workspace_size(r, n * T))
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    runs = []
+    for _ in range(4):
+        work.random_(0, 255)
+        new = lambda *s, dtype=td: nans(s, dtype)  # noqa: E731
+        out = [new(n, T, h, dh) for _ in range(6)] + [new(n, h, dh, dh, dtype=torch.float32) for _ in range(2)]
+        hg.hg_decay_fwd(p, Q, K, V, dev(lens), dev(S), out[0], out[6], work)
+        hg.hg_decay_bwd(p, Q, K, V, dev(lens), dev(S), DO, dev(dS), *out[1:4], out[7], work)
+        rows = [x.view(n * T, h, dh) for x in (Q, K, DO, V, out[4], out[5])]
+        g = {"gamma_q": new(dh, dtype=torch.float32), "gamma_k": new(dh, dtype=torch.float32)}
+        hg.hg_qkrot_bwd(r, rows[0], rows[1], None, *rows[2:], g, work)
+        y, dx = new(n * T, 128), new(n * T, 128)
+        fg = {x: nans(z.shape, torch.float32) for x, z in zip(("W_gate", "W_up", "W_down"), w)}
+        hg.hg_ffn_fwd(f, Q.view(n * T, 128), y, work)
+        hg.hg_ffn_bwd(f, Q.view(n * T, 128), DO.view(n * T, 128), dx, fg, work)
+        runs.append([*out, *g.values(), y, dx, *fg.values()])
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+
+
 # ---------------------------------------------------------------------------------------------- rotation
 # A resident set of CTAs (three an SM, two backward) takes these rows in three rounds and more, the last one ragged:
 # heads in fours, in twos and odd, that divide a CTA's groups and that do not.
