@@ -688,20 +688,23 @@ class _Params:
         """struct(*values, *addresses); tensors: (tensor or None, name, dtype, shape)."""
         self._struct, self._values, self._tensors = struct, values, tensors
         self.t = [x[0] for x in tensors]
-        self._held = [x for x in self.t if x is not None]
-        self._at = None
-        self.c()
+        self._fill()
+
+    def _fill(self):
+        self._at = ((None, 0, 0),)  # filled anew after a refusal
+        ptrs = [_want(*x) for x in self._tensors]
+        if 0 in ptrs:
+            raise ValueError(f"{type(self).__name__}: a tensor has no storage")
+        # a new struct: a call of another thread may be reading the one before
+        self._c = self._struct(*self._values, *ptrs)
+        self._at = tuple((x, x.data_ptr(), x.nbytes) for x in self.t if x is not None)
+        return self._c
 
     def c(self):
-        # address and size of each, 0.15 us a tensor; its type and shape are looked at when one of them has changed
-        at = [(x.data_ptr(), x.nbytes) for x in self._held]
-        if at != self._at:
-            self._at = None
-            ptrs = [_want(*x) for x in self._tensors]
-            if 0 in ptrs:
-                raise ValueError(f"{type(self).__name__}: a tensor has no storage")
-            # a new struct: a call of another thread may be reading the one before
-            self._c, self._at = self._struct(*self._values, *ptrs), at
+        # address and size of each (0.15 us a tensor); type and shape are looked at when one of them has changed
+        for x, at, size in self._at:
+            if x is None or x.data_ptr() != at or x.nbytes != size:
+                return self._fill()
         return self._c
 
 
@@ -720,10 +723,14 @@ class QkRotParams(_Params):
                    tuple((x, name, dtype, (self.d_h,)) for x, name in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k"))))
 
 
-def hg_qkrot_workspace_size(params: QkRotParams, n: int) -> int:
+def _qkrot_bytes(c, n: int) -> int:
     b = c_size_t(0)
-    _check(lib().hg_qkrot_workspace_size(byref(params.c()), int(n), byref(b)), "hg_qkrot_workspace_size")
+    _check(lib().hg_qkrot_workspace_size(byref(c), int(n), byref(b)), "hg_qkrot_workspace_size")
     return b.value
+
+
+def hg_qkrot_workspace_size(params: QkRotParams, n: int) -> int:
+    return _qkrot_bytes(params.c(), n)
 
 
 def _qkrot_rows(p: QkRotParams, n: int, qk):
@@ -747,8 +754,9 @@ def hg_qkrot_bwd(params: QkRotParams, q, k, pos, dq_out, dk_out, dq, dk, grads: 
     n = q.shape[0]
     a = _qkrot_rows(params, n, ((q, k, "%s"), (dq_out, dk_out, "d%s_out"), (dq, dk, "d%s")))
     g = [_want(grads.get(x), x, torch.float32, (params.d_h,)) for x in ("gamma_q", "gamma_k")]
-    w = _work_ptr(scratch, hg_qkrot_workspace_size(params, n) if n else 0, "scratch")
-    _check(lib().hg_qkrot_bwd(byref(params.c()), a[0], a[1], _want(pos, "pos", torch.int64, (n,)), n, a[2], a[3], a[4],
+    c = params.c()
+    w = _work_ptr(scratch, _qkrot_bytes(c, n) if n else 0, "scratch")
+    _check(lib().hg_qkrot_bwd(byref(c), a[0], a[1], _want(pos, "pos", torch.int64, (n,)), n, a[2], a[3], a[4],
                               a[5], g[0], g[1], w, _stream(stream)), "hg_qkrot_bwd")
 
 
@@ -762,11 +770,14 @@ class DecayParams(_Params):
                    ((self.log_decay, "log_decay", torch.float32, (self.heads,)),))
 
 
-def hg_decay_workspace_size(params: DecayParams, n: int, T: int) -> tuple:
+def _decay_bytes(c, n: int, T: int) -> tuple:
     f, b = c_size_t(0), c_size_t(0)
-    _check(lib().hg_decay_workspace_size(byref(params.c()), int(n), int(T), byref(f), byref(b)),
-           "hg_decay_workspace_size")
+    _check(lib().hg_decay_workspace_size(byref(c), int(n), int(T), byref(f), byref(b)), "hg_decay_workspace_size")
     return f.value, b.value
+
+
+def hg_decay_workspace_size(params: DecayParams, n: int, T: int) -> tuple:
+    return _decay_bytes(params.c(), n, T)
 
 
 def hg_decay_fwd(params: DecayParams, q, k, v, lens, S_in, o, S_out, scratch, stream=None):
@@ -774,8 +785,9 @@ def hg_decay_fwd(params: DecayParams, q, k, v, lens, S_in, o, S_out, scratch, st
     n, T, h, dh = q.shape[0], q.shape[1], params.heads, params.d_h
     r = [_seq_arg(t, x, params.dtype, (n, T, h, dh)) for t, x in ((q, "q"), (k, "k"), (v, "v"), (o, "o"))]
     st = [_want(t, x, torch.float32, (n, h, dh, dh)) for t, x in ((S_in, "S_in"), (S_out, "S_out"))]
-    w = _work_ptr(scratch, hg_decay_workspace_size(params, n, T)[0] if n else 0, "scratch")
-    _check(lib().hg_decay_fwd(byref(params.c()), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
+    c = params.c()
+    w = _work_ptr(scratch, _decay_bytes(c, n, T)[0] if n else 0, "scratch")
+    _check(lib().hg_decay_fwd(byref(c), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
                               r[3], st[1], w, _stream(stream)), "hg_decay_fwd")
 
 
@@ -785,8 +797,9 @@ def hg_decay_bwd(params: DecayParams, q, k, v, lens, S_in, d_o, dS_out, dq, dk, 
          for t, x in ((q, "q"), (k, "k"), (v, "v"), (d_o, "d_o"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
     st = [_want(t, x, torch.float32, (n, h, dh, dh))
           for t, x in ((S_in, "S_in"), (dS_out, "dS_out"), (dS_in, "dS_in"))]
-    w = _work_ptr(scratch, hg_decay_workspace_size(params, n, T)[1] if n else 0, "scratch")
-    _check(lib().hg_decay_bwd(byref(params.c()), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
+    c = params.c()
+    w = _work_ptr(scratch, _decay_bytes(c, n, T)[1] if n else 0, "scratch")
+    _check(lib().hg_decay_bwd(byref(c), r[0], r[1], r[2], _want(lens, "lens", torch.int32, (n,)), n, T, st[0],
                               r[3], st[1], r[4], r[5], r[6], st[2], w, _stream(stream)), "hg_decay_bwd")
 
 
@@ -812,16 +825,21 @@ class FfnParams(_Params):
                          for x, name, shape in zip((W_gate, W_up, W_down), ("W_gate", "W_up", "W_down"), shapes)))
 
 
-def hg_ffn_workspace_size(params: FfnParams, n: int) -> tuple:
+def _ffn_bytes(c, n: int) -> tuple:
     f, b = c_size_t(0), c_size_t(0)
-    _check(lib().hg_ffn_workspace_size(byref(params.c()), int(n), byref(f), byref(b)), "hg_ffn_workspace_size")
+    _check(lib().hg_ffn_workspace_size(byref(c), int(n), byref(f), byref(b)), "hg_ffn_workspace_size")
     return f.value, b.value
+
+
+def hg_ffn_workspace_size(params: FfnParams, n: int) -> tuple:
+    return _ffn_bytes(params.c(), n)
 
 
 def hg_ffn_fwd(params: FfnParams, X, Y, scratch, stream=None):
     n, shape = X.shape[0], (X.shape[0], params.d)
-    w = _work_ptr(scratch, hg_ffn_workspace_size(params, n)[0] if n else 0, "scratch")
-    _check(lib().hg_ffn_fwd(byref(params.c()), _want(X, "X", params.dtype, shape), n,
+    c = params.c()
+    w = _work_ptr(scratch, _ffn_bytes(c, n)[0] if n else 0, "scratch")
+    _check(lib().hg_ffn_fwd(byref(c), _want(X, "X", params.dtype, shape), n,
                             _want(Y, "Y", params.dtype, shape), w, _stream(stream)), "hg_ffn_fwd")
 
 
@@ -834,7 +852,8 @@ def hg_ffn_bwd(params: FfnParams, X, dY, dX, grads: dict | None, scratch, stream
         gr = byref(hg_ffn_grads(*(_want(grads[k], k, torch.float32, s)
                                   for k, s in (("W_gate", df), ("W_up", df), ("W_down", fd)))))
     none = n == 0 or (grads is None and params.dtype == torch.bfloat16)
-    w = _work_ptr(scratch, 0 if none else hg_ffn_workspace_size(params, n)[1], "scratch")
-    _check(lib().hg_ffn_bwd(byref(params.c()), _want(X, "X", params.dtype, shape), n,
+    c = params.c()
+    w = _work_ptr(scratch, 0 if none else _ffn_bytes(c, n)[1], "scratch")
+    _check(lib().hg_ffn_bwd(byref(c), _want(X, "X", params.dtype, shape), n,
                             _want(dY, "dY", params.dtype, shape), _want(dX, "dX", params.dtype, shape), gr, w,
                             _stream(stream)), "hg_ffn_bwd")
