@@ -551,8 +551,9 @@ typedef struct {
 hg_status hg_qkrot_workspace_size(const hg_qkrot_params* params, int64_t n, size_t* scratch_bytes);
 
 /* q_out, k_out = normed and turned rows of q, k (n rows each).  pos: device int64 [n], or NULL for
- * pos[i] = i; any value is taken (negative ones turn backwards), the angle is reduced exactly in 64-bit
- * fixed point and is within 4e-7 of the definition for |pos| < 2^31.  Computed in fp32, rounded once.
+ * pos[i] = i; any value is taken (negative ones turn backwards).  The angle is within 3.1e-7 + |pos| 2^-59 of
+ * the definition (its whole turns are left out exactly; 4e-7 for |pos| < 2^31, lost from 2^58 on).  Computed in fp32,
+ * rounded once; a head whose squares pass the largest fp32 number has no norm and becomes zeros.
  * An output may be its own input (same pointer and stride); other overlaps are not allowed. */
 hg_status hg_qkrot_fwd(const hg_qkrot_params* params, const hg_rows* q, const hg_rows* k, const int64_t* pos,
                        int64_t n, const hg_rows* q_out, const hg_rows* k_out, hg_stream stream);
@@ -585,9 +586,10 @@ hg_status hg_decay_workspace_size(const hg_decay_params* params, int64_t n, int6
  * sequence's length on are not read and get zero in o.  S_in, S_out: device fp32 [n][heads][d_h][d_h]
  * (key feature x value feature); S_in NULL = zero, S_out NULL = not wanted; S_out (the state after the last
  * position in use; S_in for an empty sequence) may be S_in itself.  o overlaps none of q, k, v.
- * An infinity or NaN at a position in use reaches no earlier row, and in hg_decay_bwd no later row of dk and dv; what it
- * does reach can be NaN where the definition has an infinity.  Positions that are not in use are never looked at.
- * Scratch: NULL where its size is zero. */
+ * bf16: the weights of a row (q k times their decay) and the state that it reads are rounded to bf16 once each; states
+ * are sums in fp32 of terms that are not rounded.  An infinity or NaN at a position in use reaches no earlier row, and
+ * in hg_decay_bwd no later row of dk and dv; what it does reach can be NaN where the definition has an infinity.
+ * Positions that are not in use are never looked at.  Scratch: NULL where its size is zero. */
 hg_status hg_decay_fwd(const hg_decay_params* params, const hg_seq* q, const hg_seq* k, const hg_seq* v,
                        const int32_t* lens, int64_t n, int64_t T, const float* S_in, const hg_seq* o, float* S_out,
                        void* scratch, hg_stream stream);
@@ -641,7 +643,8 @@ hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int64_t n, void
 /* Gradients for the upstream gradient dY (n x d): dX (n x d, OVERWRITTEN; NULL = skip; overlaps neither X
  * nor dY) and the weights' (grads NULL = skip).  The hidden rows are formed again from X: nothing is
  * saved by the forward.  Sums over rows have a fixed order.  bf16: dX's products take dG and dU rounded to bf16, the
- * weights' gradients take dG, dU and the hidden rows as sums of two bf16 numbers (16 bits). */
+ * weights' gradients take dG, dU and the hidden rows as sums of two bf16 numbers (16 bits; an infinity among them
+ * becomes NaN). */
 hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
                      const hg_ffn_grads* grads, void* scratch, hg_stream stream);
 

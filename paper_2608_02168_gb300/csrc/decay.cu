@@ -4,12 +4,12 @@
 //   S_t = gamma S_(t-1) + k_t v_t^T,  o_t = c q_t S_t;  the gradients are three scans of the same form
 //   (decay_kernels.cuh).
 //
-// CUDA-core scan: a lane owns one value feature of a head, so its column of the state (d_h numbers) stays in
-// registers and o_t needs no exchange; the keys and queries of a few positions are laid in shared memory
-// for their warp, where all lanes read the same 16 bytes at once.  2 d_h FMA a position and lane: at d_h = 32
-// that takes about as long as the rows' HBM traffic, above it the FMA rate bounds it.  Few histories leave an
-// SM few warps to hide a position's latency behind (300 of up to 300 positions, 4 heads of 32: 154 us a scan), so the
-// three scans of a gradient run side by side (230 us).
+// CUDA-core scan: a lane owns one value feature of a head, so its column of the state (d_h numbers) stays in registers
+// and o_t needs no exchange; the keys and queries of a few positions are laid in shared memory for their warp, where
+// all lanes read the same 16 bytes at once.  2 d_h FMA a position and lane.  Bound by latency: nothing is loaded ahead,
+// and the positions of a lane follow one another (300 histories of 300 positions, 4 heads: 81, 154, 487 and 1672 us at
+// d_h = 16, 32, 64 and 128, 4.5 to 14 TFLOP/s of 80 and 0.06 to 0.18 of HBM), so the three scans of a gradient run side
+// by side (133, 354, 1004, 4917 us).
 // Long histories of few sequences: the histories are cut into segments; a first pass finds each segment's own
 // state, a join runs through them, and the scan then starts each segment from its true state.
 //
@@ -281,7 +281,8 @@ __global__ void __launch_bounds__(256) decay_step_kernel(const T* __restrict__ q
 // and values are read twice, a state is written and joined for each segment, and there are two more launches.
 // Measured (us, whole | segments; 4 heads): bf16, d_h 64, T = 2000, room for 2 segments 209 | 244, 3: 209 | 191, 4:
 // 208 | 152; T = 600, 4: 70 | 76; d_h 32, 10 histories of 400: 29 | 27, 700: 45 | 28; fp32, d_h 32, T = 600, room for
-// 2: 305 | 327, 3: 301 | 231; 10 histories of 100: 42 | 46, 128: 52 | 38.
+// 2: 305 | 327, 3: 301 | 231; 10 histories of 100: 42 | 46, 128: 52 | 38.  fp32 was measured at d_h = 32 alone, and its
+// 16 warps an SM are taken for every width (registers leave room for 20, 16, 12 and 8 at d_h = 16 to 128).
 void plan_segments(const hg_decay_params* p, int64_t n, int64_t T, int scans, int* nseg, int64_t* seg_len) {
   const bool mma = p->dtype == HG_BF16;
   const int64_t each = mma ? scan_mma_warps(p->heads, p->d_h) : (p->heads * p->d_h + 31) / 32;

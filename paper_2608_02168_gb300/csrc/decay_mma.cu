@@ -9,16 +9,21 @@
 // fp32) in registers as the accumulator of m16n8k16 products: the accumulator's layout is the
 // layout in which the next product wants its second operand, so the state goes from sum to operand without
 // leaving the registers; likewise the chunk's weights from q k^T to the product with v.  No warp waits for
-// another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand.  The
-// scaled values that are added to the state are split into three bf16 numbers, since a state is an fp32 result that
-// gathers them (two left it 2.5e-6 off).
+// another.  Two roundings to bf16 lie inside a row: the chunk's weights, and the state as an operand; the state itself
+// stays fp32.  A row is off by 2.3e-3 of itself with them and by 1.7e-3 with its own rounding alone; a second term of
+// both would take 40 products more than a chunk's 144 at d_h = 64.  The scaled values that are added to the state are
+// split into three bf16 numbers, since a state is an fp32 result that gathers them (two left it 2.5e-6 off; 4e-7).
 //
 // Why not tcgen05: its tiles are 64 or 128 rows high, while the state of a head is d_h high, histories are often
-// shorter than one tile, and the state would go through shared memory between its sum and the next product.
+// shorter than one tile, and the state would go through shared memory between its sum and the next product.  The
+// segments' own states (kLocal) are hundreds of positions long and would suit it; they run on this kernel so far.
 //
 // Bound by instruction issue and latency at the warps that registers leave (16 an SM at d_h = 32, 8 above): 40001
 // histories of up to 12 positions, 4 heads of 32, with their states, 188 us (0.74 of the HBM rate); 6 of 32768
-// positions, 4 heads of 64, 99 us and 63 us for the segments' own states (0.6 and 0.47 of it).
+// positions, 4 heads of 64, 99 us and 63 us for the segments' own states (0.6 and 0.47 of it).  At d_h = 128 the four
+// slices of a head load q and k and form q k^T each for itself: 300 histories of 300, 4 heads, 181 us (0.30 of HBM; at
+// d_h = 64 51 us, 0.53).  The gradients' launch at d_h = 32 keeps 24 bytes of a lane in local memory, those of the
+// other widths none.
 //
 // Loads: cp.async, 16 bytes a lane, into a ring of chunks that runs ahead across the warp's items, so short
 // histories follow one another without a pause.  Pieces of a row are XORed with the row so that ldmatrix is

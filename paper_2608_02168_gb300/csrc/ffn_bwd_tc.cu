@@ -21,10 +21,13 @@
 // d = 64 the rows of X and dY stand side by side as one 128-wide operand (half of the products is not used: a 64-wide
 // one would run at half the rate).
 //
-// Bound by the tensor pipe (16 d f flops a row are needed; 28 are run).  Measured: dX 116 us at 200003 rows, d = 128,
-// f = 384 and 243 us at 100003 rows, d = 256, f = 704 (0.85 and 0.74 PFLOP/s of its ten units); weight gradients 234 us
-// (32-feature chunks with two tiles in shared memory 294 us) and 457 us (0.76 and 0.71 PFLOP/s of their eighteen units:
-// a tile's products, gates and drain follow one another, since a second tile's operands have no place).
+// Bound by the chain of a tile: products, gates and products (or a drain) follow one another, with the tensor pipe
+// active 40 % (dX) and 33 % (weight gradients) of the time, and 28 d f flops a row are run where 16 are needed.  In dX
+// the two slots share one place for dG and dU; a second row tile's operands have no place for the weight gradients.
+// Measured: dX 116 us at 200003 rows, d = 128, f = 384 and 243 us at 100003 rows, d = 256, f = 704 (0.85 and 0.74
+// PFLOP/s of its ten units); weight gradients 234 us (32-feature chunks with two tiles in shared memory 294 us) and 468
+// us (0.76 and 0.69 PFLOP/s of their eighteen units).  At 96 registers up to 56 bytes of a lane (dX) and 72 (weight
+// gradients, d = 256) lie in local memory.
 #include <algorithm>
 
 #include "ffn_kernels.cuh"

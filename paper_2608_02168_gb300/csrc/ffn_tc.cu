@@ -12,9 +12,11 @@
 // issuing warp of its own.  Rows leave through H's place by TMA.
 //
 // Bound by the tensor pipe (6 d f flops a row against 4 d bytes).  Measured: 300003 rows, f = 704 at d = 256 223 us
-// (1.45 PFLOP/s, 0.76 of the measured bf16 rate; one issuing warp and one CTA 313 us), f = 384 at d = 128 88.5 us
-// (1.0 PFLOP/s: the gates' e^x and 1/x of every hidden feature take the special-function unit as long as the products
-// take the tensor pipe).
+// (1.45 PFLOP/s, 0.76 of the measured bf16 rate; one issuing warp and one CTA 313 us), f = 384 at d = 128 88.5 us (1.0
+// PFLOP/s: the gates' e^x and 1/x of every hidden feature take the special-function unit 49 us, the products the tensor
+// pipe 46 us, and the two do not run wholly side by side), f = 200 at d = 64 62 us (0.37 PFLOP/s).  Few row tiles: a
+// tile's chunks follow one another in one CTA, so the time does not fall with the rows (300, 3000 and 10000 rows at
+// d = 128, f = 384: 14 us from a cold cache, 9 us in a replayed graph of such calls; at d = 256, f = 704: 22.5 us).
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
