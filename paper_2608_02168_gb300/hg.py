@@ -701,9 +701,9 @@ class _Params:
         return self._c
 
     def c(self):
-        # address and size of each (0.15 us a tensor); type and shape are looked at when one of them has changed
+        # address, size and layout of each (0.2 us a tensor); type and shape are looked at when one of them has changed
         for x, at, size in self._at:
-            if x is None or x.data_ptr() != at or x.nbytes != size:
+            if x is None or x.data_ptr() != at or x.nbytes != size or not x.is_contiguous():
                 return self._fill()
         return self._c
 

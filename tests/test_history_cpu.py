@@ -489,3 +489,12 @@ def test_ffn_scratch_is_asked_for_where_it_is_used(hg):
         p = ctypes.byref(hg.hg_ffn_params(64, 96, dt, 3, 1, A, A, A))
         assert so.hg_ffn_bwd(p, A, 10, A + (1 << 24), A + (2 << 24), grads, None, None) == 1
         assert b"scratch" in so.hg_last_error()
+
+
+def test_a_parameter_turned_in_its_place_is_refused(hg):
+    """The transpose of a weight has its address and size; read as it lies it would be another matrix."""
+    w = stand_in(64, 64)
+    p = hg.FfnParams(w, stand_in(64, 64), stand_in(64, 64))
+    w.data = w.data.t()
+    with pytest.raises(ValueError, match="must be contiguous"):
+        p.c()
