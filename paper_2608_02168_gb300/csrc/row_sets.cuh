@@ -44,7 +44,8 @@ inline bool step_within(__int128 d, Steps S, Steps s, int64_t lo, int64_t hi) {
 }
 
 // Whether the rows of an array that is written (its rows nest: positions within sequences or the other way round) meet
-// those of another: found wherever the two have the same strides, else where a corner row of one meets the other.
+// those of another: found wherever the two have the same strides, else where a corner row of one
+// meets the other.
 inline bool rows_meet(const RowSet& out, const RowSet& in) {
   auto end = [](const RowSet& r, int c) {  // place of a corner row, from the first
     return (c & 1 ? (__int128)(r.n - 1) * r.sn : 0) + (c & 2 ? (__int128)(r.T - 1) * r.st : 0);
@@ -53,9 +54,11 @@ inline bool rows_meet(const RowSet& out, const RowSet& in) {
   if (d >= end(out, 3) + out.w || -d >= end(in, 3) + in.w) return false;
   if (out.sn == in.sn && out.st == in.st)
     return step_within(d, {out.sn, 1 - out.n, out.n - 1}, {out.st, 1 - out.T, out.T - 1}, -in.w, out.w);
+  // rows of an input that lie over one another are not searched: too many come near a place
+  const bool search = (in.n < 2 || in.sn >= in.w) && (in.T < 2 || in.st >= in.w);
   for (int c = 0; c < 4; ++c) {
     if (step_within(d + end(in, c), {out.sn, 0, out.n - 1}, {out.st, 0, out.T - 1}, -in.w, out.w)) return true;
-    if (step_within(end(out, c) - d, {in.sn, 0, in.n - 1}, {in.st, 0, in.T - 1}, -out.w, in.w)) return true;
+    if (search && step_within(end(out, c) - d, {in.sn, 0, in.n - 1}, {in.st, 0, in.T - 1}, -out.w, in.w)) return true;
   }
   return false;
 }
