@@ -44,8 +44,7 @@ inline bool step_within(__int128 d, Steps S, Steps s, int64_t lo, int64_t hi) {
 }
 
 // Whether the rows of an array that is written (its rows nest: positions within sequences or the other way round) meet
-// those of another: found wherever the two have the same strides, else where a corner row of one
-// meets the other.
+// those of another: found wherever the two have the same strides, else where a corner row of one meets the other.
 inline bool rows_meet(const RowSet& out, const RowSet& in) {
   auto end = [](const RowSet& r, int c) {  // place of a corner row, from the first
     return (c & 1 ? (__int128)(r.n - 1) * r.sn : 0) + (c & 2 ? (__int128)(r.T - 1) * r.st : 0);
