@@ -648,6 +648,47 @@ hg_status hg_ffn_fwd(const hg_ffn_params* params, const void* X, int64_t n, void
 hg_status hg_ffn_bwd(const hg_ffn_params* params, const void* X, int64_t n, const void* dY, void* dX,
                      const hg_ffn_grads* grads, void* scratch, hg_stream stream);
 
+/* Gated linear recurrence: the linear form of the GRU (Eq. 13) over a whole history, with a state of d numbers.  Per
+ * sequence and channel, with the gate's logits g and a bias per channel:
+ *   z_t = sigmoid(g_t + bias),   h_t = h_(t-1) + z_t (x_t - h_(t-1)),   y_t = h_t       (h_(-1) = h_in, or zero).
+ * d: a multiple of 8 in [8, 16384].  bias: device [d] in the storage type, 16-byte aligned, or NULL = zero.  A row is d
+ * contiguous values; the strides of hg_rows and hg_seq are as above (x and g may be slices of one wide row). */
+typedef struct {
+  int32_t d;
+  hg_dtype dtype;
+  const void* bias;
+} hg_recur_params;
+
+/* Bytes of `saved` (written by hg_recur_fwd for hg_recur_bwd: the state before every 16th position; zero up to T = 16)
+ * and of the backward's scratch, for n sequences of up to T positions. */
+hg_status hg_recur_workspace_size(const hg_recur_params* params, int64_t n, int64_t T, size_t* saved_bytes,
+                                  size_t* scratch_bytes);
+
+/* Whole histories.  x, g, y: n sequences of T rows.  lens: device int32 [n], the positions in use of each sequence
+ * (values outside [0, T] are taken as the nearer end), or NULL = T.  Rows from a sequence's length on are not read and
+ * get zero in y.  h_in, h_out: device fp32 [n][d], 16-byte aligned; h_in NULL = zero, h_out NULL = not wanted; h_out
+ * (the state after the last position in use; h_in for an empty sequence) may be h_in itself.  saved: NULL where no
+ * backward pass follows.  No output overlaps another array otherwise.  Computed in fp32, y rounded once; the state is
+ * never rounded to bf16.  Differences x_t - h_(t-1) are formed in fp32: one past its largest number (two values of
+ * opposite signs above 1.7e38) is an infinity, and what an infinity reaches can be NaN where the definition has an
+ * infinity.  Neither reaches an earlier row. */
+hg_status hg_recur_fwd(const hg_recur_params* params, const hg_seq* x, const hg_seq* g, const int32_t* lens, int64_t n,
+                       int64_t T, const float* h_in, const hg_seq* y, float* h_out, void* saved, hg_stream stream);
+
+/* Gradients of hg_recur_fwd on the same x, g, lens, h_in, with its `saved`, for the upstream gradients d_y and dh_out
+ * (NULL = zero): dx, dg (OVERWRITTEN; zero rows from a sequence's length on), dh_in (fp32 [n][d], OVERWRITTEN; NULL =
+ * not wanted; may be dh_out itself) and dbias (fp32 [d], OVERWRITTEN; NULL = not wanted, and then scratch may be NULL).
+ * No output overlaps another array otherwise.  The bias's sums have a fixed order. */
+hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x, const hg_seq* g, const int32_t* lens, int64_t n,
+                       int64_t T, const float* h_in, const void* saved, const hg_seq* d_y, const float* dh_out,
+                       const hg_seq* dx, const hg_seq* dg, float* dh_in, float* dbias, void* scratch, hg_stream stream);
+
+/* One new snapshot of n nodes: h_out = h_in + z (x - h_in), y = h_out rounded, per node (one row a node).  live: device
+ * int32 [n] or NULL; a node whose entry is not positive keeps its state and gets a zero row.  h_out may be h_in
+ * (updated in place); no output overlaps another array otherwise. */
+hg_status hg_recur_step(const hg_recur_params* params, const hg_rows* x, const hg_rows* g, const int32_t* live,
+                        int64_t n, const float* h_in, const hg_rows* y, float* h_out, hg_stream stream);
+
 /* ------------------------------------------------------------------------------------------- */
 /* Kernel timing (measurement support; off by default)                                          */
 /* ------------------------------------------------------------------------------------------- */

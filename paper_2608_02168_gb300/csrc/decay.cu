@@ -352,29 +352,11 @@ hg_status check_params(const hg_decay_params* p, int64_t n, int64_t T) {
   return HG_OK;
 }
 
-hg_status check_seq(const hg_seq* r, const char* name, int64_t n, int64_t T, int64_t width, size_t esz, bool written) {
-  HG_REQUIRE(r != nullptr && r->p != nullptr, "%s must be non-null", name);
-  HG_REQUIRE(((uintptr_t)r->p & 15) == 0, "%s must be 16-byte aligned", name);
-  const int64_t lim = int64_t(1) << 40, st = r->stride_t, sn = r->stride_n, u = 16 / (int64_t)esz;
-  HG_REQUIRE(T < 2 || (st >= 0 && st < lim && st % u == 0),
-             "%s: stride_t must be a non-negative multiple of 16 bytes", name);
-  HG_REQUIRE(n < 2 || (sn >= 0 && sn < lim && sn % u == 0),
-             "%s: stride_n must be a non-negative multiple of 16 bytes", name);
-  if (written) {  // rows nest: positions within sequences, or sequences within positions
-    const bool ok_t = T < 2 || st >= width, ok_n = n < 2 || sn >= width;
-    // sn >= (T - 1) st + width, or st >= (n - 1) sn + width, without the products, which may pass 64 bits
-    const bool nest = n < 2 || T < 2 || (sn >= width && st <= (sn - width) / (T - 1)) ||
-                      (st >= width && sn <= (st - width) / (n - 1));
-    HG_REQUIRE(ok_t && ok_n && nest, "%s: rows that are written must not overlap", name);
-  }
-  return HG_OK;
-}
-
 // Rows that are written meet none of the others.
 hg_status check_apart(const hg_seq* out, const char* name, int64_t n, int64_t T, int64_t width, size_t esz,
                       std::initializer_list<const hg_seq*> others) {
-  auto set = [&](const hg_seq* r) { return row_set(r->p, n, T, r->stride_n, r->stride_t, width, esz); };
-  for (const hg_seq* r : others) HG_REQUIRE(!rows_meet(set(out), set(r)), "%s must not overlap another array", name);
+  for (const hg_seq* r : others)
+    HG_TRY(check_apart(seq_set(out, n, T, width, esz), name, {seq_set(r, n, T, width, esz)}));
   return HG_OK;
 }
 

@@ -1,6 +1,8 @@
 // Arrays of rows as the checks of a call's arguments see them (host only); not part of the public ABI.
 #pragma once
 
+#include <initializer_list>
+
 #include "hg_internal.cuh"
 
 namespace hg {
@@ -16,7 +18,9 @@ inline RowSet row_set(const void* p, int64_t n, int64_t T, int64_t sn, int64_t s
   return {(uintptr_t)p, n, T, n < 2 ? 0 : sn * b, T < 2 ? 0 : st * b, width * b};
 }
 
-// Whether lo < d - i S - t s < hi for some i, t within the given ends, where the inner steps stay within an outer one.
+// Whether lo < d - i S - t s < hi for some i, t within the given ends, where the inner steps stay within an outer one:
+// the outer steps that come near are tried, the inner ones follow by division.
+inline __int128 floor_div(__int128 a, __int128 b) { return a / b - (a % b != 0 && (a < 0) != (b < 0)); }
 struct Steps {
   __int128 step;
   int64_t first, last;
@@ -36,9 +40,12 @@ inline bool step_within(__int128 d, Steps S, Steps s, int64_t lo, int64_t hi) {
   const Steps I = near(d, S);
   for (int64_t i = I.first; i <= I.last; ++i) {
     const __int128 r = d - i * S.step;
-    const Steps K = near(r, s);
-    for (int64_t t = K.first; t <= K.last; ++t)
-      if (lo < r - t * s.step && r - t * s.step < hi) return true;
+    if (s.step == 0) {
+      if (lo < r && r < hi) return true;
+      continue;
+    }
+    const __int128 a = floor_div(r - hi, s.step) + 1, b = -floor_div(lo - r, s.step) - 1;  // a <= t <= b
+    if ((a < s.first ? s.first : a) <= (b > s.last ? s.last : b)) return true;
   }
   return false;
 }
@@ -60,6 +67,37 @@ inline bool rows_meet(const RowSet& out, const RowSet& in) {
     if (search && step_within(end(out, c) - d, {in.sn, 0, in.n - 1}, {in.st, 0, in.T - 1}, -out.w, in.w)) return true;
   }
   return false;
+}
+
+// A contiguous array (null: none); the rows of a sequence argument.
+inline RowSet block_set(const void* p, int64_t bytes) { return {(uintptr_t)p, 1, 1, 0, 0, p ? bytes : 0}; }
+inline RowSet seq_set(const hg_seq* r, int64_t n, int64_t T, int64_t width, size_t esz) {
+  return row_set(r->p, n, T, r->stride_n, r->stride_t, width, esz);
+}
+
+inline hg_status check_seq(const hg_seq* r, const char* name, int64_t n, int64_t T, int64_t width, size_t esz,
+                           bool written) {
+  HG_REQUIRE(r != nullptr && r->p != nullptr, "%s must be non-null", name);
+  HG_REQUIRE(((uintptr_t)r->p & 15) == 0, "%s must be 16-byte aligned", name);
+  const int64_t lim = int64_t(1) << 40, st = r->stride_t, sn = r->stride_n, u = 16 / (int64_t)esz;
+  HG_REQUIRE(T < 2 || (st >= 0 && st < lim && st % u == 0),
+             "%s: stride_t must be a non-negative multiple of 16 bytes", name);
+  HG_REQUIRE(n < 2 || (sn >= 0 && sn < lim && sn % u == 0),
+             "%s: stride_n must be a non-negative multiple of 16 bytes", name);
+  if (written) {  // rows nest: positions within sequences, or sequences within positions
+    const bool ok_t = T < 2 || st >= width, ok_n = n < 2 || sn >= width;
+    // sn >= (T - 1) st + width, or st >= (n - 1) sn + width, without the products, which may pass 64 bits
+    const bool nest = n < 2 || T < 2 || (sn >= width && st <= (sn - width) / (T - 1)) ||
+                      (st >= width && sn <= (st - width) / (n - 1));
+    HG_REQUIRE(ok_t && ok_n && nest, "%s: rows that are written must not overlap", name);
+  }
+  return HG_OK;
+}
+
+// Rows that are written meet none of the others.
+inline hg_status check_apart(const RowSet& out, const char* name, std::initializer_list<RowSet> others) {
+  for (const RowSet& r : others) HG_REQUIRE(!rows_meet(out, r), "%s must not overlap another array", name);
+  return HG_OK;
 }
 
 // Whether two arrays of the same size (null: none) share memory; whether they do without being the same.

@@ -109,6 +109,10 @@ class hg_ffn_grads(Structure):
     _fields_ = [("dW_gate", c_void_p), ("dW_up", c_void_p), ("dW_down", c_void_p)]
 
 
+class hg_recur_params(Structure):
+    _fields_ = [("d", c_int32), ("dtype", c_int32), ("bias", c_void_p)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "hg_status_string": (c_char_p, [c_int32]),
@@ -181,6 +185,15 @@ EXPORTS = {
     "hg_ffn_fwd": (c_int32, [POINTER(hg_ffn_params), c_void_p, c_int64, c_void_p, c_void_p, c_void_p]),
     "hg_ffn_bwd": (c_int32, [POINTER(hg_ffn_params), c_void_p, c_int64, c_void_p, c_void_p, POINTER(hg_ffn_grads),
                              c_void_p, c_void_p]),
+    "hg_recur_workspace_size": (c_int32, [POINTER(hg_recur_params), c_int64, c_int64, POINTER(c_size_t),
+                                          POINTER(c_size_t)]),
+    "hg_recur_fwd": (c_int32, [POINTER(hg_recur_params), POINTER(hg_seq), POINTER(hg_seq), c_void_p, c_int64, c_int64,
+                               c_void_p, POINTER(hg_seq), c_void_p, c_void_p, c_void_p]),
+    "hg_recur_bwd": (c_int32, [POINTER(hg_recur_params), POINTER(hg_seq), POINTER(hg_seq), c_void_p, c_int64, c_int64,
+                               c_void_p, c_void_p, POINTER(hg_seq), c_void_p, POINTER(hg_seq), POINTER(hg_seq),
+                               c_void_p, c_void_p, c_void_p, c_void_p]),
+    "hg_recur_step": (c_int32, [POINTER(hg_recur_params), POINTER(hg_rows), POINTER(hg_rows), c_void_p, c_int64,
+                                c_void_p, POINTER(hg_rows), c_void_p, c_void_p]),
     "hg_timing_enable": (c_int32, [c_int32]),
     "hg_timing_report": (c_int32, [c_char_p, c_size_t]),
 }
@@ -857,3 +870,83 @@ def hg_ffn_bwd(params: FfnParams, X, dY, dX, grads: dict | None, scratch, stream
     _check(lib().hg_ffn_bwd(byref(c), _want(X, "X", params.dtype, shape), n,
                             _want(dY, "dY", params.dtype, shape), _want(dX, "dX", params.dtype, shape), gr, w,
                             _stream(stream)), "hg_ffn_bwd")
+
+
+class RecurParams(_Params):
+    """Parameters of the gated linear recurrence (see hg_recur_params): bias [d] in the storage type, or None with d
+    and dtype given."""
+
+    def __init__(self, bias=None, d: int | None = None, dtype=None):
+        if bias is not None:
+            d, dtype = int(bias.numel()), bias.dtype
+        self.d, self.dtype = int(d), dtype
+        self._hold(hg_recur_params, (self.d, _storage(dtype)), ((bias, "bias", dtype, (self.d,)),))
+
+
+def _width_of(t, name: str, dtype, shape):
+    """Strides of a device tensor [..., d] whose rows are contiguous; the other strides are free."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape}; got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"libhg takes device memory; {name} is on {t.device}")
+    strides = t.stride()
+    if strides[-1] != 1:
+        raise ValueError(f"{name}: a row must be contiguous; got strides {strides}")
+    return strides
+
+
+def _flat_row_arg(t, name: str, dtype, shape):
+    strides = _width_of(t, name, dtype, shape)
+    return byref(hg_rows(t.data_ptr(), strides[0]))
+
+
+def _flat_seq_arg(t, name: str, dtype, shape):
+    strides = _width_of(t, name, dtype, shape)
+    return byref(hg_seq(t.data_ptr(), strides[0], strides[1]))
+
+
+def _recur_bytes(c, n: int, T: int) -> tuple:
+    s, b = c_size_t(0), c_size_t(0)
+    _check(lib().hg_recur_workspace_size(byref(c), int(n), int(T), byref(s), byref(b)), "hg_recur_workspace_size")
+    return s.value, b.value
+
+
+def hg_recur_workspace_size(params: RecurParams, n: int, T: int) -> tuple:
+    return _recur_bytes(params.c(), n, T)
+
+
+def hg_recur_fwd(params: RecurParams, x, g, lens, h_in, y, h_out, saved, stream=None):
+    """x, g, y [n, T, d]; lens int32 [n] or None; h_in, h_out fp32 [n, d] or None; saved None where no backward pass
+    follows."""
+    n, T, d = x.shape[0], x.shape[1], params.d
+    r = [_flat_seq_arg(t, k, params.dtype, (n, T, d)) for t, k in ((x, "x"), (g, "g"), (y, "y"))]
+    h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (h_out, "h_out"))]
+    c = params.c()
+    sv = None if saved is None else _work_ptr(saved, _recur_bytes(c, n, T)[0], "saved")
+    _check(lib().hg_recur_fwd(byref(c), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], r[2], h[1], sv,
+                              _stream(stream)), "hg_recur_fwd")
+
+
+def hg_recur_bwd(params: RecurParams, x, g, lens, h_in, saved, d_y, dh_out, dx, dg, dh_in, dbias, scratch, stream=None):
+    """saved: hg_recur_fwd's; dbias fp32 [d] or None (then scratch may be None)."""
+    n, T, d = x.shape[0], x.shape[1], params.d
+    r = [_flat_seq_arg(t, k, params.dtype, (n, T, d))
+         for t, k in ((x, "x"), (g, "g"), (d_y, "d_y"), (dx, "dx"), (dg, "dg"))]
+    h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (dh_out, "dh_out"), (dh_in, "dh_in"))]
+    c = params.c()
+    sb, wb = _recur_bytes(c, n, T)
+    sv = _work_ptr(saved, sb, "saved")
+    w = _work_ptr(scratch, wb if n and dbias is not None else 0, "scratch")
+    _check(lib().hg_recur_bwd(byref(c), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], sv, r[2], h[1],
+                              r[3], r[4], h[2], _want(dbias, "dbias", torch.float32, (d,)), w, _stream(stream)),
+           "hg_recur_bwd")
+
+
+def hg_recur_step(params: RecurParams, x, g, live, h_in, y, h_out=None, stream=None):
+    """One snapshot: x, g, y [n, d]; live int32 [n] or None; h_out None updates h_in in place."""
+    n, d = x.shape[0], params.d
+    r = [_flat_row_arg(t, k, params.dtype, (n, d)) for t, k in ((x, "x"), (g, "g"), (y, "y"))]
+    h_out = h_in if h_out is None else h_out
+    h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (h_out, "h_out"))]
+    _check(lib().hg_recur_step(byref(params.c()), r[0], r[1], _want(live, "live", torch.int32, (n,)), n, h[0], r[2],
+                               h[1], _stream(stream)), "hg_recur_step")
