@@ -689,6 +689,43 @@ hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x, const hg_
 hg_status hg_recur_step(const hg_recur_params* params, const hg_rows* x, const hg_rows* g, const int32_t* live,
                         int64_t n, const float* h_in, const hg_rows* y, float* h_out, hg_stream stream);
 
+/* A layer of experts for a few rows: gated feed-forward blocks (as in hg_ffn_*) of which a router chooses top_k a row.
+ *   l = x W_router  (W_router [d x experts]);  e_1 .. e_k = the experts of the top_k largest l, largest first, of equal
+ *   ones the lower index first;  w = softmax of l over the chosen ones (renorm != 0) or over all experts;
+ *   Y = sum_j w_j (act(x W_gate[e_j]) * (x W_up[e_j])) W_down[e_j]  (+ x where residual != 0).
+ * Device pointers of the storage type, 16-byte aligned, row-major: W_gate, W_up [experts][d][f], W_down
+ * [experts][f][d].  d in {64, 128, 256}, f a multiple of 8 up to 16384, 1 to 256 experts, top_k up to 8. */
+typedef struct {
+  int32_t d;
+  int32_t f;
+  int32_t experts;
+  int32_t top_k;
+  hg_dtype dtype;
+  hg_act act;
+  int32_t residual;
+  int32_t renorm;
+  const void* W_router;
+  const void* W_gate;
+  const void* W_up;
+  const void* W_down;
+} hg_moe_params;
+
+/* Scratch of hg_moe_fwd for n rows, 0 <= n <= 1024 (HG_ERR_UNSUPPORTED above: the kernel is made for rows so few that
+ * the weights are the work; a large batch is served by hg_ffn_fwd on each expert's rows, and so is training, by
+ * hg_ffn_bwd). */
+hg_status hg_moe_workspace_size(const hg_moe_params* params, int64_t n, size_t* scratch_bytes);
+
+/* X, Y: n x d, row-major, storage type, 16-byte aligned.  live: device int32 [n] or NULL; a row whose entry is not
+ * positive is not read, chooses no expert and gets a zero row in Y.  experts (device int32 [n][top_k]) and weights
+ * (device fp32 [n][top_k]) receive e_j and w_j (-1 and 0 for a row that is not live); NULL = not wanted.  No output
+ * overlaps another array.  The choice is that of logits without rounding (sums of two fp32 numbers, within d 2^-48 of
+ * the sum of their terms' sizes); a NaN counts as the largest logit, and an infinite one has the weights that the
+ * formula gives it (NaN).  Sums are fp32 in an order fixed by the choice; bf16: the hidden rows are rounded to bf16
+ * once, between the products, and Y once.  An infinity or NaN stays in its own row.  Weights of experts that no row
+ * chooses are not read. */
+hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, const int32_t* live, int64_t n, void* Y,
+                     int32_t* experts, float* weights, void* scratch, hg_stream stream);
+
 /* ------------------------------------------------------------------------------------------- */
 /* Kernel timing (measurement support; off by default)                                          */
 /* ------------------------------------------------------------------------------------------- */

@@ -1,0 +1,646 @@
+// A whole layer of experts for a few rows (hg_moe_fwd), two launches:
+//   moe_router    l = x W_router, the top_k largest, their weights; a CTA a row
+//   moe_experts   Y = sum_j w_j (act(x W_gate[e_j]) * (x W_up[e_j])) W_down[e_j] (+ x)
+//
+// With a few rows an expert the weights are the work: 3 d f values of every expert that a row chose are read once, and
+// what a row costs beside them is small (16 rows: 192 flops a byte of bf16 weights at most, a tenth of what the tensor
+// pipe does meanwhile).  So the second kernel is a stream of weights: the chosen experts' hidden features in chunks of
+// 64 bytes of a W_gate row are one list, cut into equal shares, a CTA a share, its loads some 100 KB ahead of the
+// products.  A share may begin and end inside an expert.  What a share gives an expert's rows (d sums each, fp32) goes
+// to scratch, and the CTA that brings a row's last share adds them up in the order of the list: the sum does not
+// depend on who comes last.
+#include <algorithm>
+
+#include "ffn_kernels.cuh"
+#include "row_sets.cuh"
+#include "tc_util.cuh"
+
+namespace hg {
+namespace {
+
+constexpr int kSms = 152;
+constexpr int kThr = 256;
+constexpr int kMaxRows = 1024, kMaxExperts = 256, kMaxTop = 8, kMaxF = 16384;
+constexpr int kGroup = 64;  // rows of an expert that a pass over its weights serves
+
+struct MoeArgs {
+  const void *x, *wr, *wg, *wu, *wd;
+  const int32_t* live;
+  void* y;
+  int32_t* experts_out;  // null: not wanted
+  float* weights_out;
+  int32_t* sel;      // [n][top] chosen expert, -1: none
+  float* w;          // [n][top]
+  int32_t* slot_in;  // [n][top] shares that have arrived
+  int32_t* row_in;   // [n] slots whose shares have all arrived
+  int32_t* place;    // [n][top] pass * group + row in it
+  float* part;       // [CTA + pass][group][d]
+  int32_t n, d, f, experts, top, renorm, residual, group;
+};
+
+// ------------------------------------------------------------------------------------------------------------
+// router
+// ------------------------------------------------------------------------------------------------------------
+// The choice hangs on differences of logits, so these are sums of two fp32 numbers: a product and what it lost, a sum
+// and what it lost.  Off by d 2^-48 of the sum of the terms' sizes.
+struct Two {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float v, float rest) {
+    const float s = __fadd_rn(hi, v), b = __fsub_rn(s, hi);
+    lo = __fadd_rn(lo, __fadd_rn(__fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b)), rest));
+    hi = s;
+  }
+  __device__ __forceinline__ void add_product(float a, float b) {
+    const float p = __fmul_rn(a, b);
+    add(p, fmaf(a, b, -p));
+  }
+  // As one number in two parts that do not overlap; an infinity has no rest, NaN counts as more than an infinity.
+  __device__ __forceinline__ float2 key() const {
+    if (isnan(hi)) return make_float2(INFINITY, INFINITY);
+    if (isinf(hi)) return make_float2(hi, 0.f);
+    const float s = __fadd_rn(hi, lo);
+    return make_float2(s, __fsub_rn(lo, __fsub_rn(s, hi)));
+  }
+};
+
+// A CTA a row: an expert's logit is summed by `parts` threads.
+template <typename T>
+__global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int parts) {
+  pdl_begin();
+  __shared__ float xs[256];
+  __shared__ float2 sums[kThr], keys[kMaxExperts];
+  __shared__ float warp_sum[kThr / 32];
+  __shared__ int chosen[kMaxTop];
+  __shared__ float pw[kMaxTop];
+  __shared__ float raw[kMaxExperts];
+  const int row = blockIdx.x, tid = threadIdx.x, d = a.d, E = a.experts, top = a.top;
+  if (tid < top) a.slot_in[row * top + tid] = 0;
+  if (tid == 0) a.row_in[row] = 0;
+  if (a.live && a.live[row] <= 0) {
+    if (tid < top) {
+      a.sel[row * top + tid] = -1;
+      if (a.experts_out) a.experts_out[row * top + tid] = -1;
+      if (a.weights_out) a.weights_out[row * top + tid] = 0.f;
+    }
+    for (int c = tid; c < d; c += kThr) static_cast<T*>(a.y)[(int64_t)row * d + c] = from_f32<T>(0.f);
+    return;
+  }
+  if (tid < d) xs[tid] = to_f32(static_cast<const T*>(a.x)[(int64_t)row * d + tid]);
+  __syncthreads();
+  const int e = tid % width, part = tid / width, per = d / parts;
+  if (part < parts && e < E) {
+    Two l;
+    const T* w = static_cast<const T*>(a.wr) + (int64_t)part * per * E + e;
+#pragma unroll 16
+    for (int k = 0; k < per; ++k) l.add_product(xs[part * per + k], to_f32(w[(int64_t)k * E]));
+    sums[tid] = make_float2(l.hi, l.lo);
+  }
+  __syncthreads();
+  if (tid < E) {
+    Two l;
+    for (int p = 0; p < parts; ++p) l.add(sums[p * width + tid].x, sums[p * width + tid].y);
+    raw[tid] = l.hi;
+    keys[tid] = l.key();
+  }
+  __syncthreads();
+  // an expert's place is the number of those before it
+  if (tid < E) {
+    const float2 me = keys[tid];
+    int before = 0;
+    for (int j = 0; j < E; ++j) {
+      const float2 o = keys[j];
+      before += o.x > me.x || (o.x == me.x && (o.y > me.y || (o.y == me.y && j < tid)));
+    }
+    if (before < top) chosen[before] = tid;
+  }
+  __syncthreads();
+  // the largest is taken off in both parts; with a NaN among the logits every weight is NaN
+  const float2 most = keys[chosen[0]];
+  const bool finite = isfinite(most.x);
+  auto power = [&](int j) {
+    const float2 l = keys[j];
+    return expf(finite ? (l.x - most.x) + (l.y - most.y) : raw[j] - raw[chosen[0]]);
+  };
+  if (tid < top) pw[tid] = power(chosen[tid]);
+  float sum = 0.f;
+  if (!a.renorm) {
+    sum = tid < E ? power(tid) : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (tid % 32 == 0) warp_sum[tid / 32] = sum;
+  }
+  __syncthreads();
+  if (tid >= top) return;
+  sum = 0.f;
+  if (a.renorm) {
+    for (int j = 0; j < top; ++j) sum += pw[j];
+  } else {
+    for (int j = 0; j < kThr / 32; ++j) sum += warp_sum[j];
+  }
+  const float w = pw[tid] / sum;
+  a.sel[row * top + tid] = chosen[tid];
+  a.w[row * top + tid] = w;
+  if (a.experts_out) a.experts_out[row * top + tid] = chosen[tid];
+  if (a.weights_out) a.weights_out[row * top + tid] = w;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// experts
+// ------------------------------------------------------------------------------------------------------------
+template <typename T, int D>
+struct MoeCfg {
+  static constexpr int FC = 64 / (int)sizeof(T);     // hidden features of a chunk: 64 bytes of a W_gate row
+  static constexpr int EP = 16 / (int)sizeof(T);     // values of a 16-byte piece
+  static constexpr int kGate = D * 64;               // bytes of a chunk of W_gate; W_up and W_down have as many
+  static constexpr int kStage = 3 * kGate;
+  static constexpr int XS = sizeof(T) == 2 ? D : D + 4;    // values between two rows of X, and of H (fp32: padded)
+  static constexpr int HS = sizeof(T) == 2 ? FC : FC + 4;
+  static constexpr int kX = kGroup * XS * (int)sizeof(T), kH = kGroup * HS * (int)sizeof(T);
+  static constexpr int kIdx = kMaxRows * kMaxTop * 2;
+  static constexpr int kFit = (220 * 1024 - kX - kH - kIdx) / kStage;
+  static constexpr int kStages = kFit > 8 ? 8 : kFit;
+  static constexpr size_t kSmem = (size_t)kStages * kStage + kX + kH + kIdx;
+};
+
+// Byte offset of piece c of row r, N pieces a row, such that eight rows' pieces lie in different banks.
+template <int N>
+__device__ __forceinline__ uint32_t place16(int r, int c) {
+  return (uint32_t)(r * N + (c ^ (N == 4 ? (r >> 1) & 3 : r & 7))) * 16u;
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// A CTA's sums of up to 64 rows: tensor instructions in bf16, FMAs in fp32.
+template <typename T, int D, int kAct>
+struct Sums;
+
+template <int D, int kAct>
+struct Sums<__nv_bfloat16, D, kAct> {
+  using C = MoeCfg<__nv_bfloat16, D>;
+  static constexpr int NT = D / 64;  // a warp has an eighth of the columns, in tiles of 8
+  float acc[kGroup / 16][NT][4];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kGroup / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
+  }
+  // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments.  H is
+  // rounded to bf16 once, the operand of the next product.
+  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
+    const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4, half = threadIdx.x / 128;
+    const uint32_t w = tc::smem_u32(st) + (lane < 16 ? 0 : C::kGate), xa = tc::smem_u32(X);
+    for (int rt = half; rt < tiles; rt += 2) {
+      float g[4] = {}, u[4] = {};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint32_t b[4], x[4];
+        ldsm4t(w + place16<4>(ks * 16 + lane % 16, ft), b);
+        ldsm4(xa + place16<D / 8>(rt * 16 + lane % 16, ks * 2 + lane / 16), x);
+        mma(g, x, b[0], b[1]);
+        mma(u, x, b[2], b[3]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t v = pack2_bf16(gate<kAct>(g[2 * h]) * u[2 * h], gate<kAct>(g[2 * h + 1]) * u[2 * h + 1]);
+        *reinterpret_cast<uint32_t*>(H + place16<4>(rt * 16 + lane / 4 + 8 * h, ft) + lane % 4 * 4) = v;
+      }
+    }
+  }
+  __device__ __forceinline__ void out(const char* st, const char* H, int tiles) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t w = tc::smem_u32(st) + 2 * C::kGate, ha = tc::smem_u32(H);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      uint32_t b[(NT + 1) / 2][4];
+#pragma unroll
+      for (int j = 0; j < (NT + 1) / 2; ++j)  // one tile: the second half of the fragment is not used
+        ldsm4t(w + place16<D / 8>(ks * 16 + lane % 16, warp * NT + 2 * j + (NT > 1 ? lane / 16 : 0)), b[j]);
+#pragma unroll
+      for (int rt = 0; rt < kGroup / 16; ++rt) {
+        if (rt >= tiles) break;
+        uint32_t h[4];
+        ldsm4(ha + place16<4>(rt * 16 + lane % 16, ks * 2 + lane / 16), h);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma(acc[rt][j], h, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float* part, int rows) const {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+#pragma unroll
+    for (int rt = 0; rt < kGroup / 16; ++rt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = rt * 16 + lane / 4 + 8 * h;
+        if (r >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          *reinterpret_cast<float2*>(part + r * D + (warp * NT + j) * 8 + lane % 4 * 2) =
+              make_float2(acc[rt][j][2 * h], acc[rt][j][2 * h + 1]);
+      }
+  }
+};
+
+template <int D, int kAct>
+struct Sums<float, D, kAct> {
+  using C = MoeCfg<float, D>;
+  static constexpr int kCols = kThr / D;            // rows side by side: thread t has column t % D of rows t / D + ...
+  static constexpr int kPer = kGroup / kCols;       // rows a thread
+  float acc[kPer];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+  }
+  // A thread has one feature of the rows t / 16 + 16 i.
+  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
+    const int ft = threadIdx.x % 16, r0 = threadIdx.x / 16;
+    const float *wg = reinterpret_cast<const float*>(st) + ft, *wu = wg + C::kGate / 4;
+    const float* x = reinterpret_cast<const float*>(X) + r0 * C::XS;
+    float* h = reinterpret_cast<float*>(H) + r0 * C::HS + ft;
+    float g[4] = {}, u[4] = {};
+#pragma unroll 4
+    for (int k = 0; k < D; k += 4) {
+      float a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = wg[(k + i) * 16];
+        b[i] = wu[(k + i) * 16];
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (t >= tiles) break;
+        const float4 v = *reinterpret_cast<const float4*>(x + t * 16 * C::XS + k);
+        g[t] = fmaf(v.x, a[0], fmaf(v.y, a[1], fmaf(v.z, a[2], fmaf(v.w, a[3], g[t]))));
+        u[t] = fmaf(v.x, b[0], fmaf(v.y, b[1], fmaf(v.z, b[2], fmaf(v.w, b[3], u[t]))));
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t < tiles) h[t * 16 * C::HS] = gate<kAct>(g[t]) * u[t];
+  }
+  __device__ __forceinline__ void out(const char* st, const char* H, int tiles) {
+    const int c = threadIdx.x % D, r0 = threadIdx.x / D;
+    const float* w = reinterpret_cast<const float*>(st + 2 * C::kGate) + c;
+    const float* h = reinterpret_cast<const float*>(H) + r0 * C::HS;
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+      const float w0 = w[k * D], w1 = w[(k + 1) * D], w2 = w[(k + 2) * D], w3 = w[(k + 3) * D];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (t >= tiles) break;
+#pragma unroll
+        for (int i = t * kPer / 4; i < (t + 1) * kPer / 4; ++i) {
+          const float4 v = *reinterpret_cast<const float4*>(h + i * kCols * C::HS + k);
+          acc[i] = fmaf(v.x, w0, fmaf(v.y, w1, fmaf(v.z, w2, fmaf(v.w, w3, acc[i]))));
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float* part, int rows) const {
+    const int c = threadIdx.x % D, r0 = threadIdx.x / D;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (r0 + i * kCols < rows) part[(r0 + i * kCols) * D + c] = acc[i];
+  }
+};
+
+// Shares of `items` chunks: CTA b of `ctas` has [first_of(b), first_of(b + 1)).
+__device__ __forceinline__ int first_of(int b, int items, int ctas) { return (int)((int64_t)b * items / ctas); }
+__device__ __forceinline__ int owner_of(int item, int items, int ctas) {
+  return (int)((((int64_t)item + 1) * ctas - 1) / items);
+}
+
+template <typename T, int D, int kAct>
+__global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
+  pdl_begin();
+  using C = MoeCfg<T, D>;
+  extern __shared__ __align__(128) char smem[];
+  char* const X = smem + C::kStages * C::kStage;
+  char* const H = X + C::kX;
+  uint16_t* const idx = reinterpret_cast<uint16_t*>(H + C::kH);
+  __shared__ int count[kMaxExperts];      // rows of an expert
+  __shared__ int first[kMaxExperts + 1];  // its first pass
+  __shared__ int warp_part[kThr / 32], list[kGroup];
+  __shared__ bool last[kGroup];
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, slots = a.n * a.top, E = a.experts, group = a.group;
+
+  // ---- the list: passes of up to `group` rows of an expert, experts in order; chunks of f in a pass
+  for (int i = tid; i < E; i += kThr) count[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < slots; i += kThr) {
+    const int e = a.sel[i];
+    idx[i] = (uint16_t)e;  // none: 0xFFFF
+    if (e >= 0) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  int passes = tid < E ? (count[tid] + group - 1) / group : 0;
+  int scan = passes;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_part[warp] = scan;
+  __syncthreads();
+  for (int k = 0; k < warp; ++k) scan += warp_part[k];
+  if (tid < E) first[tid + 1] = scan;
+  if (tid == 0) first[0] = 0;
+  __syncthreads();
+  const int chunks = (a.f + C::FC - 1) / C::FC, items = first[E] * chunks;
+  const int ctas = min((int)gridDim.x, items), b = blockIdx.x;
+  if (b >= ctas) return;
+  const int lo = first_of(b, items, ctas), hi = first_of(b + 1, items, ctas);
+
+  // ---- a cursor of the loads and one of the products
+  struct At {
+    int pass, chunk, e;
+  };
+  auto start = [&](int item) {
+    At c{item / chunks, item % chunks, 0};
+    while (first[c.e + 1] <= c.pass) ++c.e;
+    return c;
+  };
+  auto next = [&](At& c) {
+    if (++c.chunk < chunks) return;
+    c.chunk = 0;
+    ++c.pass;
+    while (c.e < E - 1 && first[c.e + 1] <= c.pass) ++c.e;
+  };
+  At ahead = start(lo), now = ahead;
+  int ahead_item = lo;
+  auto load = [&]() {  // the next chunk, into the place of its number
+    if (ahead_item < hi) {
+      char* st = smem + (ahead_item - lo) % C::kStages * C::kStage;
+      const int f0 = ahead.chunk * C::FC, use = min(C::FC, a.f - f0);
+      const T* wg = static_cast<const T*>(a.wg) + (int64_t)ahead.e * D * a.f + f0;
+      const T* wu = static_cast<const T*>(a.wu) + (int64_t)ahead.e * D * a.f + f0;
+      const T* wd = static_cast<const T*>(a.wd) + ((int64_t)ahead.e * a.f + f0) * D;
+#pragma unroll
+      for (int i = 0; i < D * 4 / kThr; ++i) {
+        const int p = tid + i * kThr, r = p / 4, q = p % 4;
+        const bool in = q * C::EP < use;
+        const int64_t at = in ? (int64_t)r * a.f + q * C::EP : 0;
+        const uint32_t to = sizeof(T) == 2 ? place16<4>(r, q) : (uint32_t)p * 16u;
+        tc::cp_async16(st + to, wg + at, in);
+        tc::cp_async16(st + C::kGate + to, wu + at, in);
+      }
+      constexpr int N = D / C::EP;  // pieces of a W_down row
+#pragma unroll
+      for (int i = 0; i < D * 4 / kThr; ++i) {
+        const int p = tid + i * kThr, r = p / N, q = p % N;
+        const bool in = r < use;
+        const uint32_t to = sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)p * 16u;
+        tc::cp_async16(st + 2 * C::kGate + to, wd + (in ? (int64_t)r * D + q * C::EP : 0), in);
+      }
+      ++ahead_item;
+      if (ahead_item < hi) next(ahead);
+    }
+    tc::cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < C::kStages - 1; ++i) load();
+
+  Sums<T, D, kAct> sums;
+  int rows = 0, tiles = 0;
+  for (int item = lo; item < hi; ++item) {
+    if (item == lo || now.chunk == 0) {  // a pass begins: its rows
+      const int skip = (now.pass - first[now.e]) * group;
+      rows = min(group, count[now.e] - skip);
+      tiles = (rows + 15) / 16;
+      const int per = (slots + kThr - 1) / kThr * 32, s0 = warp * per, s1 = min(slots, s0 + per);
+      int found = 0;
+      for (int s = s0; s < s1; s += 32)
+        found += __popc(__ballot_sync(0xffffffffu, s + lane < s1 && idx[s + lane] == now.e));
+      if (lane == 0) warp_part[warp] = found;
+      __syncthreads();
+      int at = -skip;
+      for (int k = 0; k < warp; ++k) at += warp_part[k];
+      for (int s = s0; s < s1; s += 32) {
+        const bool mine = s + lane < s1 && idx[s + lane] == now.e;
+        const uint32_t m = __ballot_sync(0xffffffffu, mine);
+        const int r = at + __popc(m & ((1u << lane) - 1));
+        if (mine && r >= 0 && r < group) list[r] = s + lane;
+        at += __popc(m);
+      }
+      __syncthreads();
+      constexpr int N = D / C::EP;
+      for (int p = tid; p < tiles * 16 * N; p += kThr) {
+        const int r = p / N, q = p % N;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < rows) v = ld16(static_cast<const T*>(a.x) + (int64_t)(list[r] / a.top) * D + q * C::EP);
+        st16(X + (sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)(r * C::XS + q * C::EP) * 4u), v);
+      }
+      sums.zero();
+    }
+    tc::cp_async_wait<C::kStages - 2>();
+    __syncthreads();  // the chunk and the rows are there; the place of the chunk before is free
+    load();
+    const char* st = smem + (item - lo) % C::kStages * C::kStage;
+    sums.hidden(st, X, H, tiles);
+    __syncthreads();
+    sums.out(st, H, tiles);
+    const At was = now;
+    if (item + 1 < hi) next(now);
+    if (item + 1 < hi && now.chunk != 0) continue;
+
+    // ---- the share's end of a pass: its sums, and whose last share this is
+    sums.store(a.part + (int64_t)(b + was.pass) * group * D, rows);
+    if (tid < rows) a.place[list[tid]] = was.pass * group + tid;
+    __threadfence();
+    __syncthreads();
+    if (tid < rows) {
+      const int shares = owner_of((was.pass + 1) * chunks - 1, items, ctas) - owner_of(was.pass * chunks, items, ctas) + 1;
+      bool done = false;
+      if (atomicAdd(&a.slot_in[list[tid]], 1) == shares - 1) {
+        __threadfence();
+        done = atomicAdd(&a.row_in[list[tid] / a.top], 1) == a.top - 1;
+      }
+      last[tid] = done;
+    }
+    __syncthreads();
+    __threadfence();
+    for (int r = tid / D; r < rows; r += kThr / D) {
+      if (!last[r]) continue;
+      const int row = list[r] / a.top, c = tid % D;
+      float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
+      for (int j = 0; j < a.top; ++j) {
+        const int at = __ldcg(&a.place[row * a.top + j]), pass = at / group;
+        const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
+        const float* p = a.part + ((int64_t)(b0 + pass) * group + at % group) * D + c;
+        float s = 0.f;
+#pragma unroll 8
+        for (int k = b0; k <= b1; ++k, p += group * D) s += __ldcg(p);
+        y = fmaf(a.w[row * a.top + j], s, y);
+      }
+      static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
+    }
+    __syncthreads();  // list, last and X are free
+  }
+  tc::cp_async_wait<0>();
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------------------------
+struct MoeLayout {
+  int32_t *sel, *slot_in, *row_in, *place;
+  float *w, *part;
+  int group;
+};
+size_t carve(void* scratch, const hg_moe_params* p, int64_t n, MoeLayout* L) {
+  Carve c(scratch);
+  const size_t slots = (size_t)n * p->top_k;
+  L->group = (int)std::min<int64_t>(kGroup, (n + 15) / 16 * 16);
+  L->sel = c.take<int32_t>(slots);
+  L->slot_in = c.take<int32_t>(slots);
+  L->row_in = c.take<int32_t>(n);
+  L->place = c.take<int32_t>(slots);
+  L->w = c.take<float>(slots);
+  // a pass has its own rows, or 64 of an expert's: at most that many, and a CTA begins at most one more
+  const size_t passes = n > 0 ? std::min<size_t>(p->experts, slots) + slots / L->group : 0;
+  L->part = c.take<float>((kSms + passes) * L->group * p->d);
+  return n > 0 ? c.used : 0;
+}
+
+hg_status check(const hg_moe_params* p, int64_t n) {
+  HG_REQUIRE(p != nullptr, "params must be non-null");
+  if (!(p->d == 64 || p->d == 128 || p->d == 256) || !(p->dtype == HG_F32 || p->dtype == HG_BF16)) {
+    set_error("unsupported d=%d / dtype=%d", p->d, (int)p->dtype);
+    return HG_ERR_UNSUPPORTED;
+  }
+  HG_REQUIRE(p->f >= 8 && p->f <= kMaxF && p->f % 8 == 0, "f must be a multiple of 8 in [8, %d]", kMaxF);
+  HG_REQUIRE(p->experts >= 1 && p->experts <= kMaxExperts, "experts must be in [1, %d]", kMaxExperts);
+  HG_REQUIRE(p->top_k >= 1 && p->top_k <= kMaxTop && p->top_k <= p->experts, "top_k must be in [1, %d], at most experts",
+             kMaxTop);
+  HG_REQUIRE(p->act == HG_ACT_RELU || p->act == HG_ACT_GELU_TANH || p->act == HG_ACT_NONE || p->act == HG_ACT_SILU,
+             "unknown activation %d", (int)p->act);
+  HG_REQUIRE(n >= 0, "n must not be negative");
+  if (n > kMaxRows) {
+    set_error("n=%lld: a call takes up to %d rows (larger batches: hg_ffn_fwd on each expert's rows)", (long long)n,
+              kMaxRows);
+    return HG_ERR_UNSUPPORTED;
+  }
+  return HG_OK;
+}
+
+template <typename T, int D, int kAct>
+hg_status experts_act(const MoeArgs& a, int grid, cudaStream_t s) {
+  using C = MoeCfg<T, D>;
+  static bool once = false;
+  if (!once) {
+    HG_CUDA(cudaFuncSetAttribute(moe_experts<T, D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem));
+    once = true;
+  }
+  return launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a);
+}
+template <typename T, int D>
+hg_status experts_d(const MoeArgs& a, hg_act act, int grid, cudaStream_t s) {
+  if (act == HG_ACT_RELU) return experts_act<T, D, HG_ACT_RELU>(a, grid, s);
+  if (act == HG_ACT_GELU_TANH) return experts_act<T, D, HG_ACT_GELU_TANH>(a, grid, s);
+  if (act == HG_ACT_SILU) return experts_act<T, D, HG_ACT_SILU>(a, grid, s);
+  return experts_act<T, D, HG_ACT_NONE>(a, grid, s);
+}
+template <typename T>
+hg_status layer(const MoeArgs& a, hg_act act, cudaStream_t s) {
+  int width = 1;  // threads side by side, an expert each
+  while (width < a.experts) width *= 2;
+  const int parts = std::min(kThr / width, 16);
+  HG_TRY(launch("moe_router", moe_router<T>, dim3(a.n), dim3(kThr), 0, s, a, width, parts));
+  // no more CTAs than chunks there can be
+  const int64_t slots = (int64_t)a.n * a.top, chunks = ceil_div(a.f, 64 / (int)sizeof(T));
+  const int64_t passes = std::min<int64_t>(a.experts, slots) + slots / a.group;
+  const int grid = (int)std::min<int64_t>(kSms, passes * chunks);
+  if (a.d == 64) return experts_d<T, 64>(a, act, grid, s);
+  if (a.d == 128) return experts_d<T, 128>(a, act, grid, s);
+  return experts_d<T, 256>(a, act, grid, s);
+}
+
+}  // namespace
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" hg_status hg_moe_workspace_size(const hg_moe_params* params, int64_t n, size_t* scratch_bytes) {
+  clear_error();
+  HG_REQUIRE(scratch_bytes != nullptr, "scratch_bytes must be non-null");
+  HG_TRY(check(params, n));
+  MoeLayout L;
+  *scratch_bytes = carve(nullptr, params, n, &L);
+  return HG_OK;
+}
+
+extern "C" hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, const int32_t* live, int64_t n, void* Y,
+                                int32_t* experts, float* weights, void* scratch, hg_stream stream) {
+  clear_error();
+  HG_TRY(device_guard());
+  HG_TRY(check(params, n));
+  const hg_moe_params& p = *params;
+  HG_REQUIRE(p.W_router && p.W_gate && p.W_up && p.W_down, "every weight pointer must be non-null");
+  HG_REQUIRE((((uintptr_t)p.W_router | (uintptr_t)p.W_gate | (uintptr_t)p.W_up | (uintptr_t)p.W_down) & 15) == 0,
+             "weights must be 16-byte aligned");
+  if (n == 0) return HG_OK;
+  HG_REQUIRE(X && Y && scratch, "X, Y and scratch must be non-null");
+  HG_REQUIRE((((uintptr_t)X | (uintptr_t)Y) & 15) == 0, "X and Y must be 16-byte aligned");
+  HG_REQUIRE((((uintptr_t)live | (uintptr_t)experts | (uintptr_t)weights) & 3) == 0,
+             "live, experts and weights must be 4-byte aligned");
+  HG_REQUIRE(((uintptr_t)scratch & 255) == 0, "scratch must be 256-byte aligned");
+  const int64_t esz = p.dtype == HG_BF16 ? 2 : 4, rows = n * p.d * esz, slots = n * p.top_k;
+  MoeLayout L;
+  const RowSet sc = block_set(scratch, (int64_t)carve(scratch, params, n, &L));
+  const RowSet x = block_set(X, rows), y = block_set(Y, rows), lv = block_set(live, 4 * n);
+  const RowSet oe = block_set(experts, 4 * slots), ow = block_set(weights, 4 * slots);
+  const RowSet r = block_set(p.W_router, p.experts * p.d * esz);
+  const int64_t w = esz * p.experts * p.d * p.f;
+  const RowSet g = block_set(p.W_gate, w), u = block_set(p.W_up, w), d = block_set(p.W_down, w);
+  HG_TRY(check_apart(y, "Y", {x, lv, oe, ow, sc, r, g, u, d}));
+  HG_TRY(check_apart(sc, "scratch", {x, lv, oe, ow, r, g, u, d}));
+  HG_TRY(check_apart(oe, "experts", {x, lv, ow, r, g, u, d}));
+  HG_TRY(check_apart(ow, "weights", {x, lv, r, g, u, d}));
+  MoeArgs a{};
+  a.x = X;
+  a.wr = p.W_router;
+  a.wg = p.W_gate;
+  a.wu = p.W_up;
+  a.wd = p.W_down;
+  a.live = live;
+  a.y = Y;
+  a.experts_out = experts;
+  a.weights_out = weights;
+  a.sel = L.sel;
+  a.w = L.w;
+  a.slot_in = L.slot_in;
+  a.row_in = L.row_in;
+  a.place = L.place;
+  a.part = L.part;
+  a.n = (int32_t)n;
+  a.d = p.d;
+  a.f = p.f;
+  a.experts = p.experts;
+  a.top = p.top_k;
+  a.renorm = p.renorm;
+  a.residual = p.residual;
+  a.group = L.group;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (p.dtype == HG_F32) return layer<float>(a, p.act, s);
+  return layer<__nv_bfloat16>(a, p.act, s);
+}

@@ -113,6 +113,12 @@ class hg_recur_params(Structure):
     _fields_ = [("d", c_int32), ("dtype", c_int32), ("bias", c_void_p)]
 
 
+class hg_moe_params(Structure):
+    _fields_ = [("d", c_int32), ("f", c_int32), ("experts", c_int32), ("top_k", c_int32), ("dtype", c_int32),
+                ("act", c_int32), ("residual", c_int32), ("renorm", c_int32), ("W_router", c_void_p),
+                ("W_gate", c_void_p), ("W_up", c_void_p), ("W_down", c_void_p)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "hg_status_string": (c_char_p, [c_int32]),
@@ -194,6 +200,9 @@ EXPORTS = {
                                c_void_p, c_void_p, c_void_p, c_void_p]),
     "hg_recur_step": (c_int32, [POINTER(hg_recur_params), POINTER(hg_rows), POINTER(hg_rows), c_void_p, c_int64,
                                 c_void_p, POINTER(hg_rows), c_void_p, c_void_p]),
+    "hg_moe_workspace_size": (c_int32, [POINTER(hg_moe_params), c_int64, POINTER(c_size_t)]),
+    "hg_moe_fwd": (c_int32, [POINTER(hg_moe_params), c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                             c_void_p, c_void_p]),
     "hg_timing_enable": (c_int32, [c_int32]),
     "hg_timing_report": (c_int32, [c_char_p, c_size_t]),
 }
@@ -950,3 +959,38 @@ def hg_recur_step(params: RecurParams, x, g, live, h_in, y, h_out=None, stream=N
     h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (h_out, "h_out"))]
     _check(lib().hg_recur_step(byref(params.c()), r[0], r[1], _want(live, "live", torch.int32, (n,)), n, h[0], r[2],
                                h[1], _stream(stream)), "hg_recur_step")
+
+
+class MoeParams(_Params):
+    """Weights of a layer of experts (see hg_moe_params): W_router [d, experts], W_gate, W_up [experts, d, f], W_down
+    [experts, f, d]."""
+
+    def __init__(self, W_router, W_gate, W_up, W_down, top_k: int, act: str = "silu", residual: bool = False,
+                 renorm: bool = True):
+        self.experts, self.d, self.f = (int(x) for x in W_gate.shape)
+        self.top_k, self.dtype = int(top_k), W_gate.dtype
+        shapes = ((self.d, self.experts), *[(self.experts, self.d, self.f)] * 2, (self.experts, self.f, self.d))
+        self._hold(hg_moe_params, (self.d, self.f, self.experts, self.top_k, _storage(self.dtype), ACTS[act],
+                                   1 if residual else 0, 1 if renorm else 0),
+                   tuple((x, name, self.dtype, shape) for x, name, shape in zip(
+                       (W_router, W_gate, W_up, W_down), ("W_router", "W_gate", "W_up", "W_down"), shapes)))
+
+
+def _moe_bytes(c, n: int) -> int:
+    b = c_size_t(0)
+    _check(lib().hg_moe_workspace_size(byref(c), int(n), byref(b)), "hg_moe_workspace_size")
+    return b.value
+
+
+def hg_moe_workspace_size(params: MoeParams, n: int) -> int:
+    return _moe_bytes(params.c(), n)
+
+
+def hg_moe_fwd(params: MoeParams, X, live, Y, experts, weights, scratch, stream=None):
+    """X, Y [n, d]; live int32 [n] or None; experts int32 and weights fp32 [n, top_k], or None."""
+    n, shape, chosen = X.shape[0], (X.shape[0], params.d), (X.shape[0], params.top_k)
+    c = params.c()
+    w = _work_ptr(scratch, _moe_bytes(c, n), "scratch")
+    _check(lib().hg_moe_fwd(byref(c), _want(X, "X", params.dtype, shape), _want(live, "live", torch.int32, (n,)), n,
+                            _want(Y, "Y", params.dtype, shape), _want(experts, "experts", torch.int32, chosen),
+                            _want(weights, "weights", torch.float32, chosen), w, _stream(stream)), "hg_moe_fwd")
