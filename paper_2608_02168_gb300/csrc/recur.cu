@@ -13,7 +13,7 @@
 // Few chains of many positions are split over time instead: see recur_fwd_split.
 #include <algorithm>
 
-#include "hg_internal.cuh"
+#include "ffn_kernels.cuh"
 #include "row_sets.cuh"
 #include "tc_util.cuh"
 
@@ -48,55 +48,107 @@ struct RecurArgs {
   int32_t d, blocks;    // split forms: blocks of channels
 };
 
-template <typename T>
-__device__ __forceinline__ uint32_t ld4(const T* p) {
-  return *reinterpret_cast<const uint32_t*>(p);
-}
-__device__ __forceinline__ void piece(uint32_t v, float* f, float) { f[0] = __uint_as_float(v); }
-__device__ __forceinline__ void piece(uint32_t v, float* f, __nv_bfloat16) {
-  f[0] = __uint_as_float(v << 16);
-  f[1] = __uint_as_float(v & 0xFFFF0000u);
-}
-template <typename T>
-__device__ __forceinline__ void st4(T* p, const float* f) {
-  uint32_t v;
-  if constexpr (sizeof(T) == 4)
-    v = __float_as_uint(f[0]);
-  else
-    v = pack2_bf16(f[0], f[1]);
-  *reinterpret_cast<uint32_t*>(p) = v;
-}
+// A piece's channels: two go through one instruction each where there is one for two fp32 numbers.
 template <int V>
-__device__ __forceinline__ void ldf(const float* p, float* f) {
-  if constexpr (V == 2) {
-    const float2 v = *reinterpret_cast<const float2*>(p);
-    f[0] = v.x;
-    f[1] = v.y;
-  } else {
-    f[0] = *p;
+struct Vec {
+  float v[V];
+};
+#define HG_TWO(name, op)                                                                                        \
+  __device__ __forceinline__ Vec<2> name(Vec<2> a, Vec<2> b) {                                                  \
+    Vec<2> r;                                                                                                   \
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t" op                       \
+        " z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"                                                               \
+        : "=f"(r.v[0]), "=f"(r.v[1])                                                                            \
+        : "f"(a.v[0]), "f"(a.v[1]), "f"(b.v[0]), "f"(b.v[1]));                                                  \
+    return r;                                                                                                   \
   }
+HG_TWO(add, "add.rn.f32x2")
+HG_TWO(mul, "mul.rn.f32x2")
+#undef HG_TWO
+__device__ __forceinline__ Vec<2> fma(Vec<2> a, Vec<2> b, Vec<2> c) {
+  Vec<2> r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.v[0]), "=f"(r.v[1])
+      : "f"(a.v[0]), "f"(a.v[1]), "f"(b.v[0]), "f"(b.v[1]), "f"(c.v[0]), "f"(c.v[1]));
+  return r;
+}
+__device__ __forceinline__ Vec<1> add(Vec<1> a, Vec<1> b) { return {a.v[0] + b.v[0]}; }
+__device__ __forceinline__ Vec<1> mul(Vec<1> a, Vec<1> b) { return {a.v[0] * b.v[0]}; }
+__device__ __forceinline__ Vec<1> fma(Vec<1> a, Vec<1> b, Vec<1> c) { return {fmaf(a.v[0], b.v[0], c.v[0])}; }
+template <int V>
+__device__ __forceinline__ Vec<V> all(float x) {
+  Vec<V> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i] = x;
+  return r;
 }
 template <int V>
-__device__ __forceinline__ void stf(float* p, const float* f) {
-  if constexpr (V == 2)
-    *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
-  else
-    *p = f[0];
+__device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {  // a - b, rounded once
+  return fma(b, all<V>(-1.f), a);
 }
 
 // A share z of [0, 1] and 1 - z in one number, each to a few steps of its own size: the smaller of the two, and the sign
 // says which: z where it is not negative, -(1 - z) where it is (the gate is open).
 __device__ __forceinline__ bool is_open(float code) { return __float_as_int(code) < 0; }
-__device__ __forceinline__ float share(float code) { return is_open(code) ? 1.f + code : code; }
-__device__ __forceinline__ float keep(float code) { return is_open(code) ? -code : 1.f - code; }
-__device__ __forceinline__ float encode(float z, float k) { return z < 0.5f ? z : -k; }
-__device__ __forceinline__ float gate(float a) {  // of sigmoid(a): e^-|a| / (1 + e^-|a|) is the smaller one
-  const float e = __expf(-fabsf(a)), s = __fdividef(e, 1.f + e);
-  return a >= 0.f ? -s : s;
+template <int V>
+__device__ __forceinline__ Vec<V> pick(Vec<V> code, Vec<V> open, Vec<V> shut) {
+  Vec<V> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i] = is_open(code.v[i]) ? open.v[i] : shut.v[i];
+  return r;
 }
-__device__ __forceinline__ float update(float h, float x, float code) {
-  return fmaf(code, x - h, is_open(code) ? x : h);
+template <int V>
+__device__ __forceinline__ Vec<V> size_of(Vec<V> code) {
+  Vec<V> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i] = fabsf(code.v[i]);
+  return r;
 }
+template <int V>
+__device__ __forceinline__ Vec<V> other_of(Vec<V> size) {
+  return minus(all<V>(1.f), size);
+}
+// Of sigmoid(a): e^-|a| / (1 + e^-|a|) is the smaller one (zero from |a| = 87 on).
+template <int V>
+__device__ __forceinline__ Vec<V> gate_of(Vec<V> a) {
+  Vec<V> e, r, c;
+#pragma unroll
+  for (int i = 0; i < V; ++i) e.v[i] = gate_ex2(fabsf(a.v[i]) * -1.4426950408889634f);
+  r = add(e, all<V>(1.f));
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.v[i] = gate_rcp(r.v[i]);
+  r = mul(e, r);
+#pragma unroll
+  for (int i = 0; i < V; ++i)  // the sign: that of -a; a NaN stays one
+    c.v[i] = __int_as_float(__float_as_int(r.v[i]) | (~__float_as_int(a.v[i]) & 0x80000000));
+  return c;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> update(Vec<V> h, Vec<V> x, Vec<V> code) {
+  return fma(code, minus(x, h), pick(code, x, h));
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t ld4(const T* p) {
+  return *reinterpret_cast<const uint32_t*>(p);
+}
+__device__ __forceinline__ Vec<1> piece(uint32_t v, float) { return {__uint_as_float(v)}; }
+__device__ __forceinline__ Vec<2> piece(uint32_t v, __nv_bfloat16) {
+  return {__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)};
+}
+__device__ __forceinline__ void st4(float* p, Vec<1> f) { *p = f.v[0]; }
+__device__ __forceinline__ void st4(__nv_bfloat16* p, Vec<2> f) {
+  *reinterpret_cast<uint32_t*>(p) = pack2_bf16(f.v[0], f.v[1]);
+}
+__device__ __forceinline__ void ldf(const float* p, Vec<1>& f) { f.v[0] = *p; }
+__device__ __forceinline__ void ldf(const float* p, Vec<2>& f) {
+  const float2 v = *reinterpret_cast<const float2*>(p);
+  f.v[0] = v.x;
+  f.v[1] = v.y;
+}
+__device__ __forceinline__ void stf(float* p, Vec<1> f) { *p = f.v[0]; }
+__device__ __forceinline__ void stf(float* p, Vec<2> f) { *reinterpret_cast<float2*>(p) = make_float2(f.v[0], f.v[1]); }
 
 __device__ __forceinline__ int64_t length(const RecurArgs& a, int64_t i) {
   if (!a.lens) return a.T;
@@ -114,12 +166,18 @@ __device__ __forceinline__ T* at_out(const Rows& r, int64_t i, int64_t t, int c)
 }
 
 template <typename T>
-__device__ __forceinline__ void bias_of(const RecurArgs& a, int c, float* b) {
-  if (a.bias) {
-    piece(ld4(static_cast<const T*>(a.bias) + c), b, T{});
-  } else {
-    for (int v = 0; v < kVec<T>; ++v) b[v] = 0.f;
-  }
+__device__ __forceinline__ Vec<kVec<T>> bias_of(const RecurArgs& a, int c) {
+  return a.bias ? piece(ld4(static_cast<const T*>(a.bias) + c), T{}) : all<kVec<T>>(0.f);
+}
+template <int V>
+__device__ __forceinline__ Vec<V> state_of(const float* h, const RecurArgs& a, int64_t i, int c) {  // null: zero
+  Vec<V> r = all<V>(0.f);
+  if (h) ldf(h + i * a.d + c, r);
+  return r;
+}
+// Where the state before position t0 is kept, t0 a multiple of kPos above zero.
+__device__ __forceinline__ float* kept(const RecurArgs& a, int64_t i, int64_t t0, int c) {
+  return a.saved + (i * a.spans + t0 / kPos - 1) * a.d + c;
 }
 
 // Positions in use of the kPos from t0 on.
@@ -142,8 +200,9 @@ __device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64
 // ------------------------------------------------------------------------------------------------------------
 // a chain a thread
 // ------------------------------------------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void recur_fwd(RecurArgs a) {
+// kAhead: the next rows' loads run under these ones' updates; histories of one batch do without their registers.
+template <typename T, bool kAhead>
+__global__ __launch_bounds__(256, kAhead ? 2 : 4) void recur_fwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
@@ -152,119 +211,110 @@ __global__ __launch_bounds__(256) void recur_fwd(RecurArgs a) {
   const int64_t len = length(a, i);
   const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c);
   T* y = at_out<T>(a.y, i, 0, c);
-  float b[V], h[V] = {};
-  bias_of<T>(a, c, b);
-  if (a.h_in) ldf<V>(a.h_in + i * a.d + c, h);
   uint32_t rx[kPos], rg[kPos];
   load_rows(rx, x, a.x.st, 0, len);
   load_rows(rg, g, a.g.st, 0, len);
+  const Vec<V> b = bias_of<T>(a, c);
+  Vec<V> h = state_of<V>(a.h_in, a, i, c);
   for (int64_t t0 = 0; t0 < len; t0 += kPos) {
     uint32_t nx[kPos], ng[kPos];
-    load_rows(nx, x, a.x.st, t0 + kPos, len);
-    load_rows(ng, g, a.g.st, t0 + kPos, len);
-    if (a.saved && t0 > 0) stf<V>(a.saved + (i * a.spans + t0 / kPos - 1) * a.d + c, h);
+    if (kAhead) {
+      load_rows(nx, x, a.x.st, t0 + kPos, len);
+      load_rows(ng, g, a.g.st, t0 + kPos, len);
+      if (a.saved && t0 > 0) stf(kept(a, i, t0, c), h);
+    }
     const int left = left_of(t0, len);
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
       if (u >= left) break;
-      float fx[V], fg[V];
-      piece(rx[u], fx, T{});
-      piece(rg[u], fg, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = update(h[v], fx[v], gate(fg[v] + b[v]));
+      h = update(h, piece(rx[u], T{}), gate_of(add(piece(rg[u], T{}), b)));
       st4(y, h);
       y += a.y.st;
     }
+    if (kAhead) {
 #pragma unroll
-    for (int u = 0; u < kPos; ++u) {
-      rx[u] = nx[u];
-      rg[u] = ng[u];
+      for (int u = 0; u < kPos; ++u) {
+        rx[u] = nx[u];
+        rg[u] = ng[u];
+      }
     }
   }
-  const float zero[V] = {};
-  for (int64_t t = len; t < a.T; ++t, y += a.y.st) st4(y, zero);
-  if (a.h_out) stf<V>(a.h_out + i * a.d + c, h);
+  for (int64_t t = len; t < a.T; ++t, y += a.y.st) st4(y, all<V>(0.f));
+  if (a.h_out) stf(a.h_out + i * a.d + c, h);
 }
 
 // Sums of a CTA's rows of threads (ty < rows), in a fixed order, to a row of partial sums.
 template <int V>
-__device__ __forceinline__ void part_sums(const float* sum, float* sh, int tx, int ty, int width, int rows, float* out,
+__device__ __forceinline__ void part_sums(Vec<V> sum, float* sh, int tx, int ty, int width, int rows, float* out,
                                           bool in) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) sh[(ty * width + tx) * V + v] = sum[v];
+  for (int v = 0; v < V; ++v) sh[(ty * width + tx) * V + v] = sum.v[v];
   __syncthreads();
   if (ty != 0 || !in) return;
-  float s[V] = {};
+  Vec<V> s = all<V>(0.f);
   for (int k = 0; k < rows; ++k) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) s[v] += sh[(k * width + tx) * V + v];
+    for (int v = 0; v < V; ++v) s.v[v] += sh[(k * width + tx) * V + v];
   }
-  stf<V>(out, s);
+  stf(out, s);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void recur_bwd(RecurArgs a) {
+// A position's part of the backward: what R gives dx and dg, and R for the position before.
+template <int V>
+__device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> diff, Vec<V>& dx, Vec<V>& dg) {
+  const Vec<V> s = size_of(code), o = other_of(s), keep = pick(code, s, o);
+  R = add(R, dy);
+  dx = mul(pick(code, o, s), R);
+  R = mul(keep, R);
+  dg = mul(mul(dx, diff), keep);
+}
+
+template <typename T, bool kAhead>
+__global__ __launch_bounds__(256, kAhead ? 1 : 2) void recur_bwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   __shared__ float sh[256 * V];
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   const bool in = c < a.d;
-  float b[V] = {}, sum[V] = {};
-  if (in) bias_of<T>(a, c, b);
+  const Vec<V> zero = all<V>(0.f), b = in ? bias_of<T>(a, c) : zero;
+  Vec<V> sum = zero;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; in && i < a.n;
        i += (int64_t)gridDim.x * blockDim.y) {
     const int64_t len = length(a, i);
     const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c), *dy = at<T>(a.dy, i, 0, c);
     T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
-    float R[V] = {};
-    if (a.dh_out) ldf<V>(a.dh_out + i * a.d + c, R);
-    const float zero[V] = {};
+    const int64_t last = len > 0 ? (len - 1) / kPos * kPos : 0;
+    uint32_t rx[kPos], rg[kPos], ry[kPos];
+    Vec<V> h;
+    auto load = [&](int64_t t0, int64_t end) {
+      load_rows(rx, x, a.x.st, t0, end);
+      load_rows(rg, g, a.g.st, t0, end);
+      load_rows(ry, dy, a.dy.st, t0, end);
+      if (t0 > 0)
+        ldf(kept(a, i, t0, c), h);
+      else
+        h = state_of<V>(a.h_in, a, i, c);
+    };
+    load(last, len);
+    Vec<V> R = state_of<V>(a.dh_out, a, i, c);
     for (int64_t t = len; t < a.T; ++t) {
       st4(dx + t * a.dx.st, zero);
       st4(dg + t * a.dg.st, zero);
     }
-    auto start = [&](int64_t t0, float* h) {  // the state before position t0
-      if (t0 > 0) {
-        ldf<V>(a.saved + (i * a.spans + t0 / kPos - 1) * a.d + c, h);
-      } else if (a.h_in) {
-        ldf<V>(a.h_in + i * a.d + c, h);
-      } else {
-        for (int v = 0; v < V; ++v) h[v] = 0.f;
-      }
-    };
-    const int64_t last = len > 0 ? (len - 1) / kPos * kPos : -1;
-    uint32_t rx[kPos], rg[kPos], ry[kPos];
-    float h[V] = {};
-    if (last >= 0) {
-      load_rows(rx, x, a.x.st, last, len);
-      load_rows(rg, g, a.g.st, last, len);
-      load_rows(ry, dy, a.dy.st, last, len);
-      start(last, h);
-    }
-    for (int64_t t0 = last; t0 >= 0; t0 -= kPos) {
-      float diff[kPos][V], code[kPos][V];
+    for (int64_t t0 = last; t0 >= 0 && len > 0; t0 -= kPos) {
+      Vec<V> diff[kPos], code[kPos];
 #pragma unroll
       for (int u = 0; u < kPos; ++u) {
-        float fx[V], fg[V];
-        piece(rx[u], fx, T{});
-        piece(rg[u], fg, T{});
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          code[u][v] = gate(fg[v] + b[v]);
-          diff[u][v] = fx[v] - h[v];
-          h[v] = update(h[v], fx[v], code[u][v]);
-        }
+        code[u] = gate_of(add(piece(rg[u], T{}), b));
+        const Vec<V> fx = piece(rx[u], T{});
+        diff[u] = minus(fx, h);
+        h = fma(code[u], diff[u], pick(code[u], fx, h));
       }
       uint32_t cy[kPos];
 #pragma unroll
       for (int u = 0; u < kPos; ++u) cy[u] = ry[u];
-      if (t0 > 0) {
-        load_rows(rx, x, a.x.st, t0 - kPos, t0);
-        load_rows(rg, g, a.g.st, t0 - kPos, t0);
-        load_rows(ry, dy, a.dy.st, t0 - kPos, t0);
-        start(t0 - kPos, h);
-      }
-      float here[V] = {};
+      if (kAhead && t0 > 0) load(t0 - kPos, t0);
+      Vec<V> here = zero;
       const int left = left_of(t0, len);
       T *px = dx + (t0 + kPos) * a.dx.st, *pg = dg + (t0 + kPos) * a.dg.st;
 #pragma unroll
@@ -272,25 +322,16 @@ __global__ __launch_bounds__(256) void recur_bwd(RecurArgs a) {
         px -= a.dx.st;
         pg -= a.dg.st;
         if (u < left) {
-          float fy[V], ox[V], og[V];
-          piece(cy[u], fy, T{});
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const float k = keep(code[u][v]);
-            R[v] += fy[v];
-            ox[v] = share(code[u][v]) * R[v];
-            og[v] = ox[v] * diff[u][v] * k;
-            here[v] += og[v];
-            R[v] *= k;
-          }
+          Vec<V> ox, og;
+          back(R, piece(cy[u], T{}), code[u], diff[u], ox, og);
+          here = add(here, og);
           st4(px, ox);
           st4(pg, og);
         }
       }
-#pragma unroll
-      for (int v = 0; v < V; ++v) sum[v] += here[v];
+      sum = add(sum, here);
     }
-    if (a.dh_in) stf<V>(a.dh_in + i * a.d + c, R);
+    if (a.dh_in) stf(a.dh_in + i * a.d + c, R);
   }
   if (a.part)
     part_sums<V>(sum, sh, threadIdx.x, threadIdx.y, blockDim.x, blockDim.y, a.part + (int64_t)blockIdx.x * a.d + c, in);
@@ -300,32 +341,45 @@ __global__ __launch_bounds__(256) void recur_bwd(RecurArgs a) {
 // a chain split over time
 // ------------------------------------------------------------------------------------------------------------
 // A cluster of CL CTAs takes 64 bytes of a sequence's rows through CL tiles of 256 positions a step; a thread has 16
-// positions of a 4-byte piece.  Positions compose: a run of them maps the state h before it to B + K h, with B = its
-// end from a zero state and K = prod(1 - z), Z = 1 - K (carried apart, so that the smaller one is known to a few steps
-// of its own size).  Threads form the runs of their 16 positions, a CTA that of its
-// tile, each CTA hands its tile's to all others of the cluster (distributed shared memory), and every CTA joins them
-// in the same order, so all carry the same state and a call repeats its bits.  One barrier of the cluster a step.
+// positions of a 4-byte piece.  Positions compose: a run of them maps the state h before it to B + K h, B its end from
+// a zero state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).
+// Threads form the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to
+// the cluster's others (distributed shared memory), and every CTA joins them in the same order, so all carry the same
+// state and a call repeats its bits.  One barrier of the cluster a step.
+template <int V>
+struct Run {
+  Vec<V> K, B;
+};
+template <int V>
+struct alignas(8 * V) Pair {  // as it lies in shared memory
+  float K[V], B[V];
+};
 template <int V>
 struct SplitSmem {
-  float2 agg[2][kSubs][kLanes * V];  // (share and keep, B) of the threads' runs
-  float2 tot[2][8][kLanes * V];      // and of the cluster's tiles
+  Pair<V> run[2][kSubs][kLanes];
+  Pair<V> tile[2][8][kLanes];
 };
-
-__device__ __forceinline__ float through(float h, float2 r) {
-  return fmaf(-r.x, h, is_open(r.x) ? 0.f : h) + r.y;
+template <int V>
+__device__ __forceinline__ void join(Run<V>& a, const Pair<V>& p) {  // a, then p
+  Vec<V> K, B;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    K.v[v] = p.K[v];
+    B.v[v] = p.B[v];
+  }
+  a.B = fma(K, a.B, B);
+  a.K = mul(a.K, K);
 }
-struct Run {
-  float Z = 0.f, K = 1.f, B = 0.f;
-  __device__ __forceinline__ void add(float code) {
-    Z = fmaf(share(code), K, Z);
-    K *= keep(code);
+template <int V>
+__device__ __forceinline__ Pair<V> pair_of(const Run<V>& r) {
+  Pair<V> p;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    p.K[v] = r.K.v[v];
+    p.B[v] = r.B.v[v];
   }
-  __device__ __forceinline__ void add(float2 r) {  // this run, then r
-    B = through(B, r);
-    add(r.x);
-  }
-  __device__ __forceinline__ float2 pair() const { return make_float2(encode(Z, K), B); }
-};
+  return p;
+}
 
 template <int CL>
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -344,244 +398,188 @@ __device__ __forceinline__ void cluster_wait() {
   else
     __syncthreads();
 }
-template <int CL>
-__device__ __forceinline__ void hand_out(float2* slot, float2 v) {  // to the same place of every CTA of the cluster
+template <int CL, int V>
+__device__ __forceinline__ void hand_out(Pair<V>* slot, const Pair<V>& p) {  // to the same place of every CTA
   if constexpr (CL > 1) {
     const uint32_t own = tc::smem_u32(slot);
 #pragma unroll
     for (int r = 0; r < CL; ++r) {
       uint32_t there;
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(r));
-      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * v), "f"(p.K[v]) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * (V + v)), "f"(p.B[v]) : "memory");
+      }
     }
   } else {
-    *slot = v;
+    *slot = p;
   }
+}
+
+// The joined run of the tiles and threads before this one, from a step's runs: in the order of positions, or from the
+// end.  State is carried on to the next step; what enters this thread's positions is returned.
+template <int CL, int V, bool kBack>
+__device__ __forceinline__ Vec<V> enter(SplitSmem<V>& sm, const Run<V>& mine, Vec<V>& state, int buf, int rank, int sub,
+                                        int tx) {
+  auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
+  sm.run[buf][sub][tx] = pair_of(mine);
+  __syncthreads();
+  Run<V> before{all<V>(1.f), all<V>(0.f)};
+  if (threadIdx.x < kLanes) {
+    Run<V> whole = before;
+#pragma unroll
+    for (int k = 0; k < kSubs; ++k) join(whole, sm.run[buf][at(k, kSubs)][threadIdx.x]);
+    hand_out<CL>(&sm.tile[buf][rank][threadIdx.x], pair_of(whole));
+  }
+  __syncwarp();
+  cluster_arrive<CL>();
+  const int ahead = at(sub, kSubs);
+  for (int k = 0; k < ahead; ++k) join(before, sm.run[buf][at(k, kSubs)][tx]);
+  __syncwarp();
+  cluster_wait<CL>();
+  Vec<V> got = state;
+#pragma unroll
+  for (int k = 0; k < CL; ++k) {
+    const int r = at(k, CL);
+    if (r == rank) got = fma(before.K, state, before.B);
+    Run<V> s{all<V>(1.f), state};
+    join(s, sm.tile[buf][r][tx]);
+    state = s.B;
+  }
+  return got;
 }
 
 template <typename T, int CL>
 __cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 2) recur_fwd_split(RecurArgs a) {
   pdl_begin();
-  constexpr int V = kVec<T>, W = kLanes * V;
+  constexpr int V = kVec<T>;
   __shared__ SplitSmem<V> sm;
   const int rank = cluster_rank<CL>(), tx = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c = (int)(item % a.blocks) * W + tx * V;
+  const int c = (int)(item % a.blocks) * kLanes * V + tx * V;
   const bool in = c < a.d;
   const int64_t len = length(a, i);
   const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c);
   T* y = at_out<T>(a.y, i, 0, c);
-  float b[V] = {}, h[V] = {};
-  if (in) {
-    bias_of<T>(a, c, b);
-    if (a.h_in) ldf<V>(a.h_in + i * a.d + c, h);
-  }
   const int64_t end = in ? len : 0;  // lanes past the row load and store nothing
   const int64_t steps = (len + CL * kTile - 1) / (CL * kTile);
   const int64_t own = (int64_t)rank * kTile + sub * kPos;
   uint32_t rx[kPos], rg[kPos];
   load_rows(rx, x, a.x.st, own, end);
   load_rows(rg, g, a.g.st, own, end);
+  const Vec<V> b = in ? bias_of<T>(a, c) : all<V>(0.f);
+  Vec<V> h = in ? state_of<V>(a.h_in, a, i, c) : all<V>(0.f);
   cluster_arrive<CL>();  // every CTA runs before another one writes to it
   cluster_wait<CL>();
   for (int64_t s = 0; s < steps; ++s) {
     const int64_t t0 = s * CL * kTile + own;
-    const int buf = s & 1;
     const int left = left_of(t0, end);
-    float code[kPos][V];
-    uint32_t cx[kPos];
-    Run run[V];
+    Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      float fx[V], fg[V];
-      cx[u] = rx[u];
-      piece(rx[u], fx, T{});
-      piece(rg[u], fg, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        code[u][v] = u < left ? gate(fg[v] + b[v]) : 0.f;  // zero: a position that is not in use
-        run[v].B = update(run[v].B, fx[v], code[u][v]);
-        run[v].add(code[u][v]);
-      }
+      const Vec<V> code = gate_of(add(piece(rg[u], T{}), b)), sz = size_of(code);
+      const Vec<V> B = update(now.B, piece(rx[u], T{}), code), K = mul(now.K, pick(code, sz, other_of(sz)));
+      if (u < left) now = Run<V>{K, B};
+      run[u] = now;
     }
     load_rows(rx, x, a.x.st, t0 + CL * kTile, end);
     load_rows(rg, g, a.g.st, t0 + CL * kTile, end);
-#pragma unroll
-    for (int v = 0; v < V; ++v) sm.agg[buf][sub][tx * V + v] = run[v].pair();
-    __syncthreads();
-    if (threadIdx.x < W) {
-      Run all;
-#pragma unroll
-      for (int k = 0; k < kSubs; ++k) all.add(sm.agg[buf][k][threadIdx.x]);
-      hand_out<CL>(&sm.tot[buf][rank][threadIdx.x], all.pair());
-    }
-    __syncwarp();
-    cluster_arrive<CL>();
-    Run before[V];
-    for (int k = 0; k < sub; ++k) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) before[v].add(sm.agg[buf][k][tx * V + v]);
-    }
-    __syncwarp();
-    cluster_wait<CL>();
-    float hh[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int r = 0; r < CL; ++r) {
-        if (r == rank) hh[v] = through(h[v], before[v].pair());
-        h[v] = through(h[v], sm.tot[buf][r][tx * V + v]);
-      }
-    }
-    if (a.saved && t0 > 0 && left > 0) stf<V>(a.saved + (i * a.spans + t0 / kPos - 1) * a.d + c, hh);
+    const Vec<V> h0 = enter<CL, V, false>(sm, now, h, s & 1, rank, sub, tx);
+    if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
     T* py = y + t0 * a.y.st;
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      float fx[V];
-      piece(cx[u], fx, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) hh[v] = update(hh[v], fx[v], code[u][v]);
-      if (u < left) st4(py, hh);
+      if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
       py += a.y.st;
     }
   }
   if (!in) return;
-  const float zero[V] = {};
-  for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) st4(y + t * a.y.st, zero);
-  if (a.h_out && rank == 0 && sub == 0) stf<V>(a.h_out + i * a.d + c, h);
+  for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) st4(y + t * a.y.st, all<V>(0.f));
+  if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
 }
 
-// The same from the end: a run of positions maps the R that enters from the right to B + (1 - Z) R.  The states
-// before each thread's 16 positions are the forward's.
+// The same from the end: a run of positions maps the R that enters from the right to B + K R.  The states before each
+// thread's 16 positions are the forward's.
 template <typename T, int CL>
 __cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 1) recur_bwd_split(RecurArgs a) {
   pdl_begin();
-  constexpr int V = kVec<T>, W = kLanes * V;
+  constexpr int V = kVec<T>;
   __shared__ SplitSmem<V> sm;
   __shared__ float sh[256 * V];
   const int rank = cluster_rank<CL>(), tx = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c = (int)(item % a.blocks) * W + tx * V;
+  const int c = (int)(item % a.blocks) * kLanes * V + tx * V;
   const bool in = c < a.d;
   const int64_t len = length(a, i);
   const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c), *dy = at<T>(a.dy, i, 0, c);
   T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
-  float b[V] = {}, R[V] = {}, sum[V] = {};
-  if (in) {
-    bias_of<T>(a, c, b);
-    if (a.dh_out) ldf<V>(a.dh_out + i * a.d + c, R);
-  }
   const int64_t end = in ? len : 0;
   const int64_t steps = (len + CL * kTile - 1) / (CL * kTile);
   const int64_t own = (int64_t)rank * kTile + sub * kPos;
+  const Vec<V> zero = all<V>(0.f);
   uint32_t rx[kPos], rg[kPos], ry[kPos];
-  float h[V];
+  Vec<V> h;
   auto load = [&](int64_t t0) {
     load_rows(rx, x, a.x.st, t0, end);
     load_rows(rg, g, a.g.st, t0, end);
     load_rows(ry, dy, a.dy.st, t0, end);
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = 0.f;
+    h = zero;
     if (t0 < end) {
       if (t0 > 0)
-        ldf<V>(a.saved + (i * a.spans + t0 / kPos - 1) * a.d + c, h);
-      else if (a.h_in)
-        ldf<V>(a.h_in + i * a.d + c, h);
+        ldf(kept(a, i, t0, c), h);
+      else
+        h = state_of<V>(a.h_in, a, i, c);
     }
   };
   if (steps > 0) load((steps - 1) * CL * kTile + own);
+  const Vec<V> b = in ? bias_of<T>(a, c) : zero;
+  Vec<V> R = in ? state_of<V>(a.dh_out, a, i, c) : zero, sum = zero;
   cluster_arrive<CL>();
   cluster_wait<CL>();
   for (int64_t s = steps - 1; s >= 0; --s) {
     const int64_t t0 = s * CL * kTile + own;
-    const int buf = s & 1;
-    float diff[kPos][V], code[kPos][V];
     const int left = left_of(t0, end);
+    Vec<V> diff[kPos], code[kPos];
     uint32_t cy[kPos];
-    Run run[V];
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      float fx[V], fg[V];
+      const Vec<V> fx = piece(rx[u], T{}), z = gate_of(add(piece(rg[u], T{}), b));
       cy[u] = ry[u];
-      piece(rx[u], fx, T{});
-      piece(rg[u], fg, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        code[u][v] = u < left ? gate(fg[v] + b[v]) : 0.f;
-        diff[u][v] = fx[v] - h[v];
-        h[v] = update(h[v], fx[v], code[u][v]);
-      }
+      code[u] = u < left ? z : zero;  // zero: a position that is not in use
+      diff[u] = minus(fx, h);
+      h = fma(code[u], diff[u], pick(code[u], fx, h));
     }
+    Run<V> run{all<V>(1.f), zero};
 #pragma unroll
     for (int u = kPos - 1; u >= 0; --u) {
-      float fy[V];
-      piece(cy[u], fy, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        run[v].B = keep(code[u][v]) * (run[v].B + fy[v]);
-        run[v].add(code[u][v]);
-      }
+      const Vec<V> sz = size_of(code[u]), k = pick(code[u], sz, other_of(sz));
+      run.B = mul(k, add(run.B, piece(cy[u], T{})));
+      run.K = mul(run.K, k);
     }
     if (s > 0) load(t0 - CL * kTile);
-#pragma unroll
-    for (int v = 0; v < V; ++v) sm.agg[buf][sub][tx * V + v] = run[v].pair();
-    __syncthreads();
-    if (threadIdx.x < W) {
-      Run all;
-#pragma unroll
-      for (int k = kSubs - 1; k >= 0; --k) all.add(sm.agg[buf][k][threadIdx.x]);
-      hand_out<CL>(&sm.tot[buf][rank][threadIdx.x], all.pair());
-    }
-    __syncwarp();
-    cluster_arrive<CL>();
-    Run after[V];
-    for (int k = kSubs - 1; k > sub; --k) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) after[v].add(sm.agg[buf][k][tx * V + v]);
-    }
-    __syncwarp();
-    cluster_wait<CL>();
-    float RR[V], here[V] = {};
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int r = CL - 1; r >= 0; --r) {
-        if (r == rank) RR[v] = through(R[v], after[v].pair());
-        R[v] = through(R[v], sm.tot[buf][r][tx * V + v]);
-      }
-    }
+    Vec<V> r = enter<CL, V, true>(sm, run, R, s & 1, rank, sub, tx), here = zero;
     T *px = dx + (t0 + kPos) * a.dx.st, *pg = dg + (t0 + kPos) * a.dg.st;
 #pragma unroll
     for (int u = kPos - 1; u >= 0; --u) {
-      float fy[V], ox[V], og[V];
       px -= a.dx.st;
       pg -= a.dg.st;
-      piece(cy[u], fy, T{});
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float k = keep(code[u][v]);
-        RR[v] += fy[v];
-        ox[v] = share(code[u][v]) * RR[v];
-        og[v] = ox[v] * diff[u][v] * k;
-        RR[v] *= k;
-      }
+      Vec<V> ox, og;
+      back(r, piece(cy[u], T{}), code[u], diff[u], ox, og);
       if (u < left) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) here[v] += og[v];
+        here = add(here, og);
         st4(px, ox);
         st4(pg, og);
       }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] += here[v];
+    sum = add(sum, here);
   }
   if (in) {
-    const float zero[V] = {};
     for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) {
       st4(dx + t * a.dx.st, zero);
       st4(dg + t * a.dg.st, zero);
     }
-    if (a.dh_in && rank == 0 && sub == 0) stf<V>(a.dh_in + i * a.d + c, R);
+    if (a.dh_in && rank == 0 && sub == 0) stf(a.dh_in + i * a.d + c, R);
   }
   if (a.part) part_sums<V>(sum, sh, tx, sub, kLanes, kSubs, a.part + (i * CL + rank) * a.d + c, in);
 }
@@ -629,7 +627,7 @@ __global__ __launch_bounds__(256) void recur_step(RecurArgs a) {
       if (a.bias) unpack(ld16(static_cast<const T*>(a.bias) + c + q * E / Q), b + q * E / Q, T{});
     }
 #pragma unroll
-    for (int v = 0; v < E; ++v) o[v] = h[v] = update(h[v], x[v], gate(g[v] + b[v]));
+    for (int v = 0; v < E; ++v) o[v] = h[v] = update(Vec<1>{h[v]}, Vec<1>{x[v]}, gate_of(Vec<1>{g[v] + b[v]})).v[0];
   }
   T* yp = at_out<T>(a.y, i, 0, c);
 #pragma unroll
@@ -700,7 +698,9 @@ template <typename T>
 hg_status forward(const RecurArgs& a, int cl, cudaStream_t s) {
   if (cl == 0) {
     const Shape sh = shape_of(a.d / kVec<T>);
-    return launch("recur_fwd", recur_fwd<T>, dim3((unsigned)ceil_div(a.n, sh.block.y), sh.across), sh.block, 0, s, a);
+    const dim3 grid((unsigned)ceil_div(a.n, sh.block.y), sh.across);
+    if (a.T <= kPos) return launch("recur_fwd", recur_fwd<T, false>, grid, sh.block, 0, s, a);
+    return launch("recur_fwd", recur_fwd<T, true>, grid, sh.block, 0, s, a);
   }
   const dim3 grid((unsigned)(a.n * a.blocks * cl)), block(256);
   if (cl == 1) return launch("recur_fwd_split", recur_fwd_split<T, 1>, grid, block, 0, s, a);
@@ -713,7 +713,9 @@ template <typename T>
 hg_status backward(const RecurArgs& a, int cl, int64_t rows, cudaStream_t s) {
   if (cl == 0) {
     const Shape sh = shape_of(a.d / kVec<T>);
-    return launch("recur_bwd", recur_bwd<T>, dim3((unsigned)rows, sh.across), sh.block, 0, s, a);
+    const dim3 grid((unsigned)rows, sh.across);
+    if (a.T <= kPos) return launch("recur_bwd", recur_bwd<T, false>, grid, sh.block, 0, s, a);
+    return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
   }
   const dim3 grid((unsigned)(a.n * a.blocks * cl)), block(256);
   if (cl == 1) return launch("recur_bwd_split", recur_bwd_split<T, 1>, grid, block, 0, s, a);
