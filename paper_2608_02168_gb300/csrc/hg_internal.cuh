@@ -83,20 +83,24 @@ __device__ __forceinline__ void pdl_begin() { asm volatile("griddepcontrol.wait;
 // 4.83 -> 4.43 ms; fp32 layer on 112k nodes 509 -> 449 us).  No kernel asks for its successor early
 // (griddepcontrol.launch_dependents): the successor's waiting CTAs then take the SMs' shared memory, and with it
 // the L1 of the gather kernels, for their whole run (10M-node layer 10.4 -> 11.3 ms).
+// launch_clusters: clusters of `cluster` CTAs along x.
 template <typename... KArgs, typename... Args>
-hg_status launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
-                 cudaStream_t s, Args&&... args) {
+hg_status launch_clusters(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                          cudaStream_t s, int cluster, Args&&... args) {
   if (grid.x == 0 || grid.y == 0 || grid.z == 0) return HG_OK;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;  // none: the kernel's own, if it has any
   int slot = timing_begin(name, s);
   cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
   timing_end(slot, s);
@@ -106,6 +110,12 @@ hg_status launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 blo
     return HG_ERR_CUDA;
   }
   return HG_OK;
+}
+
+template <typename... KArgs, typename... Args>
+hg_status launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                 Args&&... args) {
+  return launch_clusters(name, kernel, grid, block, smem, s, 0, std::forward<Args>(args)...);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
+#include "layer_kernels.cuh"
 #include "row_sets.cuh"
 #include "tc_util.cuh"
 
@@ -25,6 +26,7 @@ constexpr int kMaxWidth = 16384;  // channels of a row
 constexpr int kLanes = 16;        // split forms: lanes across a row's piece, so 64 bytes of it
 constexpr int kSubs = 16;         // ... and threads along time, kPos positions each
 constexpr int kTile = kSubs * kPos;
+constexpr int kMaxCluster = 8;
 
 template <typename T>
 constexpr int kVec = 4 / (int)sizeof(T);  // channels of a 4-byte piece
@@ -43,6 +45,7 @@ struct RecurArgs {
   const float* dh_out;  // backward
   float* dh_in;
   float* saved;         // [n][(T - 1) / kPos][d]: the states before positions kPos, 2 kPos, ...
+  int* status;          // split forms: the library's device status word
   float* part;          // backward: partial sums of the bias's gradient, [rows of CTAs][d]
   int64_t n, T, spans;  // spans = (T - 1) / kPos
   int32_t d, blocks;    // split forms: blocks of channels
@@ -88,45 +91,54 @@ __device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {  // a - b, rounded
   return fma(b, all<V>(-1.f), a);
 }
 
-// A share z of [0, 1] and 1 - z in one number, each to a few steps of its own size: the smaller of the two, and the sign
-// says which: z where it is not negative, -(1 - z) where it is (the gate is open).
-__device__ __forceinline__ bool is_open(float code) { return __float_as_int(code) < 0; }
+// z = sigmoid(a) and k = 1 - z, each to a few steps of its own size: s = e^-|a| / (1 + e^-|a|) is the smaller of the two
+// (zero from |a| = 87 on), 1 - s the other.
 template <int V>
-__device__ __forceinline__ Vec<V> pick(Vec<V> code, Vec<V> open, Vec<V> shut) {
-  Vec<V> r;
+struct Gate {
+  Vec<V> s, big;
+  bool open[V];
+  __device__ __forceinline__ explicit Gate(Vec<V> a) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) r.v[i] = is_open(code.v[i]) ? open.v[i] : shut.v[i];
-  return r;
+    for (int i = 0; i < V; ++i) s.v[i] = gate_ex2(fabsf(a.v[i]) * -1.4426950408889634f);
+    Vec<V> r = add(s, all<V>(1.f));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      r.v[i] = gate_rcp(r.v[i]);
+      open[i] = a.v[i] >= 0.f;
+    }
+    s = mul(s, r);
+    big = minus(all<V>(1.f), s);
+  }
+  __device__ __forceinline__ Vec<V> pick(Vec<V> x, Vec<V> y) const {  // x of an open gate, y of a shut one
+    Vec<V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = open[i] ? x.v[i] : y.v[i];
+    return r;
+  }
+  __device__ __forceinline__ Vec<V> z() const { return pick(big, s); }
+  __device__ __forceinline__ Vec<V> k() const { return pick(s, big); }
+  // Both in one number: z where it is not negative, -k where it is.
+  __device__ __forceinline__ Vec<V> code() const {
+    Vec<V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = open[i] ? -s.v[i] : s.v[i];
+    return r;
+  }
+};
+template <int V>
+__device__ __forceinline__ void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float s = fabsf(code.v[i]), big = 1.f - s;
+    const bool open = __float_as_int(code.v[i]) < 0;
+    z.v[i] = open ? big : s;
+    k.v[i] = open ? s : big;
+  }
 }
+// The next state: the nearer end and the smaller share of the difference.
 template <int V>
-__device__ __forceinline__ Vec<V> size_of(Vec<V> code) {
-  Vec<V> r;
-#pragma unroll
-  for (int i = 0; i < V; ++i) r.v[i] = fabsf(code.v[i]);
-  return r;
-}
-template <int V>
-__device__ __forceinline__ Vec<V> other_of(Vec<V> size) {
-  return minus(all<V>(1.f), size);
-}
-// Of sigmoid(a): e^-|a| / (1 + e^-|a|) is the smaller one (zero from |a| = 87 on).
-template <int V>
-__device__ __forceinline__ Vec<V> gate_of(Vec<V> a) {
-  Vec<V> e, r, c;
-#pragma unroll
-  for (int i = 0; i < V; ++i) e.v[i] = gate_ex2(fabsf(a.v[i]) * -1.4426950408889634f);
-  r = add(e, all<V>(1.f));
-#pragma unroll
-  for (int i = 0; i < V; ++i) r.v[i] = gate_rcp(r.v[i]);
-  r = mul(e, r);
-#pragma unroll
-  for (int i = 0; i < V; ++i)  // the sign: that of -a; a NaN stays one
-    c.v[i] = __int_as_float(__float_as_int(r.v[i]) | (~__float_as_int(a.v[i]) & 0x80000000));
-  return c;
-}
-template <int V>
-__device__ __forceinline__ Vec<V> update(Vec<V> h, Vec<V> x, Vec<V> code) {
-  return fma(code, minus(x, h), pick(code, x, h));
+__device__ __forceinline__ Vec<V> update(Vec<V> h, Vec<V> x, const Gate<V>& g) {
+  return fma(g.code(), minus(x, h), g.pick(x, h));
 }
 
 template <typename T>
@@ -165,9 +177,17 @@ __device__ __forceinline__ T* at_out(const Rows& r, int64_t i, int64_t t, int c)
   return const_cast<T*>(at<T>(r, i, t, c));
 }
 
+// An infinite bias is a large one, so that -infinity plus it stays what it is (NaN too).
+__device__ __forceinline__ float far_bias(float b) {
+  return isinf(b) ? copysignf(1e30f, b) : b;
+}
 template <typename T>
 __device__ __forceinline__ Vec<kVec<T>> bias_of(const RecurArgs& a, int c) {
-  return a.bias ? piece(ld4(static_cast<const T*>(a.bias) + c), T{}) : all<kVec<T>>(0.f);
+  Vec<kVec<T>> b = all<kVec<T>>(0.f);
+  if (a.bias) b = piece(ld4(static_cast<const T*>(a.bias) + c), T{});
+#pragma unroll
+  for (int v = 0; v < kVec<T>; ++v) b.v[v] = far_bias(b.v[v]);
+  return b;
 }
 template <int V>
 __device__ __forceinline__ Vec<V> state_of(const float* h, const RecurArgs& a, int64_t i, int c) {  // null: zero
@@ -185,62 +205,139 @@ __device__ __forceinline__ int left_of(int64_t t0, int64_t end) {
   const int64_t l = end - t0;
   return l < 0 ? 0 : l > kPos ? kPos : (int)l;
 }
-// kPos rows' pieces from position t0 on, zeros from `end` on.
+// kPos rows' pieces from position t0 on; from `end` on x and dy are zero and the gates' logits -infinity: z = 0, a position
+// that leaves every sum as it is.
 template <typename T>
-__device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64_t st, int64_t t0, int64_t end) {
+__device__ __forceinline__ uint32_t shut() {
+  return sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+}
+template <typename T>
+__device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64_t st, int64_t t0, int64_t end,
+                                          uint32_t fill = 0u) {
   const int left = left_of(t0, end);
   p += t0 * st;
+  if (left == kPos) {
 #pragma unroll
-  for (int u = 0; u < kPos; ++u) {
-    r[u] = u < left ? ld4(p) : 0u;
-    p += st;
+    for (int u = 0; u < kPos; ++u, p += st) r[u] = ld4(p);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kPos; ++u, p += st) r[u] = u < left ? ld4(p) : fill;
   }
 }
 
 // ------------------------------------------------------------------------------------------------------------
 // a chain a thread
 // ------------------------------------------------------------------------------------------------------------
-// kAhead: the next rows' loads run under these ones' updates; histories of one batch do without their registers.
-template <typename T, bool kAhead>
-__global__ __launch_bounds__(256, kAhead ? 2 : 4) void recur_fwd(RecurArgs a) {
-  pdl_begin();
-  constexpr int V = kVec<T>;
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
-  const int64_t i = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  if (c >= a.d || i >= a.n) return;
-  const int64_t len = length(a, i);
-  const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c);
-  T* y = at_out<T>(a.y, i, 0, c);
-  uint32_t rx[kPos], rg[kPos];
-  load_rows(rx, x, a.x.st, 0, len);
-  load_rows(rg, g, a.g.st, 0, len);
-  const Vec<V> b = bias_of<T>(a, c);
-  Vec<V> h = state_of<V>(a.h_in, a, i, c);
-  for (int64_t t0 = 0; t0 < len; t0 += kPos) {
-    uint32_t nx[kPos], ng[kPos];
-    if (kAhead) {
-      load_rows(nx, x, a.x.st, t0 + kPos, len);
-      load_rows(ng, g, a.g.st, t0 + kPos, len);
-      if (a.saved && t0 > 0) stf(kept(a, i, t0, c), h);
-    }
-    const int left = left_of(t0, len);
+// Forward: a thread has 16 bytes of a row, so that loads, stores and their addresses are few beside the gates, and four
+// positions, the next four's loads in flight.
+constexpr int kWide = 4;
+template <typename T>
+struct Wide {
+  static constexpr int E = 16 / (int)sizeof(T), N = E / 2;
+  Vec<2> v[N];
+  __device__ __forceinline__ void unpacked(const uint4& r) {
+    float f[E];
+    unpack(r, f, T{});
 #pragma unroll
-    for (int u = 0; u < kPos; ++u) {
-      if (u >= left) break;
-      h = update(h, piece(rx[u], T{}), gate_of(add(piece(rg[u], T{}), b)));
-      st4(y, h);
-      y += a.y.st;
-    }
-    if (kAhead) {
+    for (int k = 0; k < N; ++k) v[k] = {f[2 * k], f[2 * k + 1]};
+  }
+  __device__ __forceinline__ uint4 packed() const {
+    float f[E];
 #pragma unroll
-      for (int u = 0; u < kPos; ++u) {
-        rx[u] = nx[u];
-        rg[u] = ng[u];
-      }
+    for (int k = 0; k < E; ++k) f[k] = v[k / 2].v[k % 2];
+    return pack(f, T{});
+  }
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      float f[4];
+      unpack(ld16(p + 2 * k), f, 0.f);
+      v[k] = {f[0], f[1]};
+      v[k + 1] = {f[2], f[3]};
     }
   }
-  for (int64_t t = len; t < a.T; ++t, y += a.y.st) st4(y, all<V>(0.f));
-  if (a.h_out) stf(a.h_out + i * a.d + c, h);
+  __device__ __forceinline__ void store(float* p) const {
+#pragma unroll
+    for (int k = 0; k < N; k += 2)
+      *reinterpret_cast<float4*>(p + 2 * k) = make_float4(v[k].v[0], v[k].v[1], v[k + 1].v[0], v[k + 1].v[1]);
+  }
+};
+
+// A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's length
+// and state, are on their way while these ones' gates are computed.
+template <typename T>
+__global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
+  pdl_begin();
+  using W = Wide<T>;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W::E;
+  const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
+  if (c >= a.d || first >= a.n) return;
+  uint4 rx[2][kWide], rg[2][kWide];
+  int64_t lens[2];  // of the sequence that a place's rows are of
+  W b, h, enter;
+#pragma unroll
+  for (int k = 0; k < W::N; ++k) b.v[k] = enter.v[k] = all<2>(0.f);
+  if (a.bias) {
+    b.unpacked(ld16(static_cast<const T*>(a.bias) + c));
+#pragma unroll
+    for (int k = 0; k < W::N; ++k) b.v[k] = {far_bias(b.v[k].v[0]), far_bias(b.v[k].v[1])};
+  }
+  // the loads' place: sequence, position, rows
+  int64_t li = first, lt = 0, llen = length(a, li), after = li + step < a.n ? length(a, li + step) : 0;
+  const T *x = at<T>(a.x, li, 0, c), *g = at<T>(a.g, li, 0, c);
+  auto load = [&](int buf) {
+    if (li >= a.n) return;
+    lens[buf] = llen;
+    if (lt == 0 && a.h_in) enter.load(a.h_in + li * a.d + c);
+#pragma unroll
+    for (int u = 0; u < kWide; ++u)
+      if (lt + u < llen) {
+        rx[buf][u] = ld16(x);
+        rg[buf][u] = ld16(g);
+        x += a.x.st;
+        g += a.g.st;
+      }
+    lt += kWide;
+    if (lt < llen) return;
+    li += step;
+    lt = 0;
+    llen = after;
+    if (li >= a.n) return;
+    x = at<T>(a.x, li, 0, c);
+    g = at<T>(a.g, li, 0, c);
+    if (li + step < a.n) after = length(a, li + step);
+  };
+  int64_t i = first, t = 0;
+  T* y = at_out<T>(a.y, i, 0, c);
+  auto batch = [&](int buf) {
+    if (i >= a.n) return;
+    if (t == 0) h = enter;
+    load(buf ^ 1);
+    if (a.saved && t > 0 && t % kPos == 0) h.store(kept(a, i, t, c));
+#pragma unroll
+    for (int u = 0; u < kWide; ++u)
+      if (t + u < lens[buf]) {
+        W fx, fg;
+        fx.unpacked(rx[buf][u]);
+        fg.unpacked(rg[buf][u]);
+#pragma unroll
+        for (int k = 0; k < W::N; ++k) h.v[k] = update(h.v[k], fx.v[k], Gate<2>(add(fg.v[k], b.v[k])));
+        st16(y, h.packed());
+        y += a.y.st;
+      }
+    t += kWide;
+    if (t < lens[buf]) return;
+    for (int64_t u = lens[buf]; u < a.T; ++u, y += a.y.st) st16(y, make_uint4(0, 0, 0, 0));
+    if (a.h_out) h.store(a.h_out + i * a.d + c);
+    i += step;
+    t = 0;
+    y = at_out<T>(a.y, i, 0, c);
+  };
+  load(0);
+  while (i < a.n) {
+    batch(0);
+    batch(1);
+  }
 }
 
 // Sums of a CTA's rows of threads (ty < rows), in a fixed order, to a row of partial sums.
@@ -259,18 +356,26 @@ __device__ __forceinline__ void part_sums(Vec<V> sum, float* sh, int tx, int ty,
   stf(out, s);
 }
 
-// A position's part of the backward: what R gives dx and dg, and R for the position before.
+// The backward's forward half: a position's state, and what its gate's gradient is of R: (x - h) z k.
 template <int V>
-__device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> diff, Vec<V>& dx, Vec<V>& dg) {
-  const Vec<V> s = size_of(code), o = other_of(s), keep = pick(code, s, o);
+__device__ __forceinline__ Vec<V> slope(Vec<V>& h, Vec<V> x, const Gate<V>& g) {
+  const Vec<V> diff = minus(x, h);
+  h = fma(g.code(), diff, g.pick(x, h));
+  return mul(diff, mul(g.s, g.big));
+}
+// And its half from the end: what R gives dx and dg, and R for the position before.
+template <int V>
+__device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> slope, Vec<V>& dx, Vec<V>& dg) {
+  Vec<V> z, k;
+  decode(code, z, k);
   R = add(R, dy);
-  dx = mul(pick(code, o, s), R);
-  R = mul(keep, R);
-  dg = mul(mul(dx, diff), keep);
+  dx = mul(z, R);
+  dg = mul(slope, R);
+  R = mul(k, R);
 }
 
 template <typename T, bool kAhead>
-__global__ __launch_bounds__(256, kAhead ? 1 : 2) void recur_bwd(RecurArgs a) {
+__global__ __launch_bounds__(256, 1) void recur_bwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   __shared__ float sh[256 * V];
@@ -288,7 +393,7 @@ __global__ __launch_bounds__(256, kAhead ? 1 : 2) void recur_bwd(RecurArgs a) {
     Vec<V> h;
     auto load = [&](int64_t t0, int64_t end) {
       load_rows(rx, x, a.x.st, t0, end);
-      load_rows(rg, g, a.g.st, t0, end);
+      load_rows(rg, g, a.g.st, t0, end, shut<T>());
       load_rows(ry, dy, a.dy.st, t0, end);
       if (t0 > 0)
         ldf(kept(a, i, t0, c), h);
@@ -302,13 +407,12 @@ __global__ __launch_bounds__(256, kAhead ? 1 : 2) void recur_bwd(RecurArgs a) {
       st4(dg + t * a.dg.st, zero);
     }
     for (int64_t t0 = last; t0 >= 0 && len > 0; t0 -= kPos) {
-      Vec<V> diff[kPos], code[kPos];
+      Vec<V> sl[kPos], code[kPos];
 #pragma unroll
       for (int u = 0; u < kPos; ++u) {
-        code[u] = gate_of(add(piece(rg[u], T{}), b));
-        const Vec<V> fx = piece(rx[u], T{});
-        diff[u] = minus(fx, h);
-        h = fma(code[u], diff[u], pick(code[u], fx, h));
+        const Gate<V> gt(add(piece(rg[u], T{}), b));
+        code[u] = gt.code();
+        sl[u] = slope(h, piece(rx[u], T{}), gt);
       }
       uint32_t cy[kPos];
 #pragma unroll
@@ -323,7 +427,7 @@ __global__ __launch_bounds__(256, kAhead ? 1 : 2) void recur_bwd(RecurArgs a) {
         pg -= a.dg.st;
         if (u < left) {
           Vec<V> ox, og;
-          back(R, piece(cy[u], T{}), code[u], diff[u], ox, og);
+          back(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
           here = add(here, og);
           st4(px, ox);
           st4(pg, og);
@@ -357,7 +461,8 @@ struct alignas(8 * V) Pair {  // as it lies in shared memory
 template <int V>
 struct SplitSmem {
   Pair<V> run[2][kSubs][kLanes];
-  Pair<V> tile[2][8][kLanes];
+  Pair<V> tile[2][kMaxCluster][kLanes];
+  uint64_t bar[2];  // a step's tiles have come
 };
 template <int V>
 __device__ __forceinline__ void join(Run<V>& a, const Pair<V>& p) {  // a, then p
@@ -381,119 +486,208 @@ __device__ __forceinline__ Pair<V> pair_of(const Run<V>& r) {
   return p;
 }
 
-template <int CL>
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r = 0;
-  if constexpr (CL > 1) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
+__device__ __forceinline__ int cluster_reg_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return (int)r;
 }
-template <int CL>
-__device__ __forceinline__ void cluster_arrive() {
-  if constexpr (CL > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+__device__ __forceinline__ int cluster_reg_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return (int)r;
 }
-template <int CL>
-__device__ __forceinline__ void cluster_wait() {
-  if constexpr (CL > 1)
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  else
-    __syncthreads();
+// Every CTA runs before another one writes to it, and is there until the last one has.
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-template <int CL, int V>
-__device__ __forceinline__ void hand_out(Pair<V>* slot, const Pair<V>& p) {  // to the same place of every CTA
-  if constexpr (CL > 1) {
-    const uint32_t own = tc::smem_u32(slot);
-#pragma unroll
-    for (int r = 0; r < CL; ++r) {
-      uint32_t there;
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(r));
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * v), "f"(p.K[v]) : "memory");
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * (V + v)), "f"(p.B[v]) : "memory");
-      }
-    }
-  } else {
-    *slot = p;
+// To the same place of every CTA of the cluster, counted by the barrier at the same place there.  (A barrier of the
+// whole cluster a step would wait for the rows' stores as well: 1.4 of 6.7 stall cycles an instruction.)
+template <int V>
+__device__ __forceinline__ void hand_out(Pair<V>* slot, uint64_t* bar, const Run<V>& p, int cl) {
+  const uint32_t own = tc::smem_u32(slot), own_bar = tc::smem_u32(bar);
+  for (int r = 0; r < cl; ++r) {
+    uint32_t there, there_bar;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(r));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(own_bar), "r"(r));
+    if constexpr (V == 2)
+      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                       there),
+                   "f"(p.K.v[0]), "f"(p.K.v[1]), "f"(p.B.v[0]), "f"(p.B.v[1]), "r"(there_bar)
+                   : "memory");
+    else
+      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there),
+                   "f"(p.K.v[0]), "f"(p.B.v[0]), "r"(there_bar)
+                   : "memory");
   }
 }
 
 // The joined run of the tiles and threads before this one, from a step's runs: in the order of positions, or from the
 // end.  State is carried on to the next step; what enters this thread's positions is returned.
-template <int CL, int V, bool kBack>
-__device__ __forceinline__ Vec<V> enter(SplitSmem<V>& sm, const Run<V>& mine, Vec<V>& state, int buf, int rank, int sub,
-                                        int tx) {
-  auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
-  sm.run[buf][sub][tx] = pair_of(mine);
-  __syncthreads();
-  Run<V> before{all<V>(1.f), all<V>(0.f)};
-  if (threadIdx.x < kLanes) {
-    Run<V> whole = before;
-#pragma unroll
-    for (int k = 0; k < kSubs; ++k) join(whole, sm.run[buf][at(k, kSubs)][threadIdx.x]);
-    hand_out<CL>(&sm.tile[buf][rank][threadIdx.x], pair_of(whole));
+__device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity) {
+  const uint32_t addr = tc::smem_u32(bar);
+  for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    if (done) return true;
   }
-  __syncwarp();
-  cluster_arrive<CL>();
-  const int ahead = at(sub, kSubs);
-  for (int k = 0; k < ahead; ++k) join(before, sm.run[buf][at(k, kSubs)][tx]);
-  __syncwarp();
-  cluster_wait<CL>();
-  Vec<V> got = state;
-#pragma unroll
-  for (int k = 0; k < CL; ++k) {
-    const int r = at(k, CL);
-    if (r == rank) got = fma(before.K, state, before.B);
-    Run<V> s{all<V>(1.f), state};
-    join(s, sm.tile[buf][r][tx]);
-    state = s.B;
-  }
-  return got;
+  return false;
 }
 
-template <typename T, int CL>
-__cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 2) recur_fwd_split(RecurArgs a) {
+template <int V>
+struct Split {
+  SplitSmem<V>& sm;
+  int* status;
+  int cl, rank, tx, ty;
+  uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
+
+  __device__ __forceinline__ Split(SplitSmem<V>& s, int* st)
+      : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % kLanes),
+        ty(threadIdx.x / kLanes) {
+    if (threadIdx.x == 0) {
+      tc::mbar_init(&sm.bar[0], 1);
+      tc::mbar_init(&sm.bar[1], 1);
+      tc::fence_mbar_init();
+    }
+    __syncthreads();
+  }
+  // A CTA hands out step s + 1 after all its threads have read step s, and enters s + 2 after every other one has
+  // handed out s + 1: two places are enough.
+  // `then` is done by all threads when all have formed their runs.
+  template <bool kBack, typename F>
+  __device__ __forceinline__ Vec<V> enter(const Run<V>& mine, Vec<V>& state, int buf, F then) {
+    auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
+    sm.run[buf][ty][tx] = pair_of(mine);
+    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * kLanes * sizeof(Pair<V>)));
+    __syncthreads();
+    Run<V> before{all<V>(1.f), all<V>(0.f)};
+    if (threadIdx.x < kLanes) {
+      Run<V> whole = before;
+#pragma unroll
+      for (int k = 0; k < kSubs; ++k) join(whole, sm.run[buf][at(k, kSubs)][threadIdx.x]);
+      if (cl > 1)
+        hand_out(&sm.tile[buf][rank][threadIdx.x], &sm.bar[buf], whole, cl);
+      else
+        sm.tile[buf][0][threadIdx.x] = pair_of(whole);
+    }
+    then();
+    const int ahead = at(ty, kSubs);
+    for (int k = 0; k < ahead; ++k) join(before, sm.run[buf][at(k, kSubs)][tx]);
+    // (a wait that gave up leaves this call's results invalid; every loop ends all the same)
+    if (cl == 1)
+      __syncthreads();
+    else if (!tiles_here(&sm.bar[buf], phase >> buf & 1))
+      record_device_error(status, tc::kErrTimeout);
+    phase ^= 1u << buf;
+    Vec<V> got = state;
+    for (int k = 0; k < cl; ++k) {
+      const int r = at(k, cl);
+      if (r == rank) got = fma(before.K, state, before.B);
+      Run<V> s{all<V>(1.f), state};
+      join(s, sm.tile[buf][r][tx]);
+      state = s.B;
+    }
+    return got;
+  }
+};
+
+// A tile of rows' pieces in shared memory, 64 bytes a row: neighbouring rows are swapped in every other thread's 16, which
+// puts the rows that a warp's two threads along time read together into different banks.
+constexpr int kTileBytes = kTile * 64;
+__device__ __forceinline__ int tile_row(int r) { return (r ^ (r / kPos & 1)) * 64; }
+struct Piece16 {  // a thread's 16 rows
+  const char *even, *odd;
+  __device__ __forceinline__ Piece16(const char* tile, int sub, int tx)
+      : even(tile + sub * kPos * 64 + (sub & 1) * 64 + tx * 4), odd(tile + sub * kPos * 64 - (sub & 1) * 64 + tx * 4) {}
+  __device__ __forceinline__ uint32_t operator[](int u) const {
+    return *reinterpret_cast<const uint32_t*>((u & 1 ? odd : even) + u * 64);
+  }
+};
+
+// kStreams arrays' tiles of `stages` steps, asked for that many steps ahead.
+template <typename T, int kStreams, int kStages>
+struct Stages {
+  static constexpr size_t kBytes = (size_t)kStages * kStreams * kTileBytes;
+  char* smem;
+  __device__ __forceinline__ const char* of(int64_t s, int stream) const {
+    return smem + ((int)(s % kStages) * kStreams + stream) * kTileBytes;
+  }
+  // Step s's rows t0 .. t0 + 255; from `len` on, and past the row's end, zeros.
+  __device__ __forceinline__ void ask(int64_t s, const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t len, int c0,
+                                      int d) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int q = threadIdx.x % 4, r0 = threadIdx.x / 4, c = c0 + q * E;
+    const int64_t left = c < d ? len - t0 : 0;
+#pragma unroll
+    for (int k = 0; k < kStreams; ++k) {
+      char* to = smem + ((int)(s % kStages) * kStreams + k) * kTileBytes + q * 16;
+      const T* p = at<T>(r[k], i, t0 + r0, c);
+#pragma unroll
+      for (int m = 0; m < kTile / 64; ++m) {
+        const int row = r0 + 64 * m;
+        tc::cp_async16(to + tile_row(row), row < left ? p + 64 * m * r[k].st : static_cast<const T*>(r[k].p), row < left);
+      }
+    }
+  }
+};
+
+constexpr int kFwdStages = 3, kBwdStages = 4;
+
+template <typename T>
+__global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
+  extern __shared__ __align__(128) char smem[];
   __shared__ SplitSmem<V> sm;
-  const int rank = cluster_rank<CL>(), tx = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
+  Split<V> sp(sm, a.status);
+  Stages<T, 2, kFwdStages> tiles{smem};
+  const Rows in_rows[2] = {a.x, a.g};
+  const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c = (int)(item % a.blocks) * kLanes * V + tx * V;
+  const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
   const bool in = c < a.d;
-  const int64_t len = length(a, i);
-  const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c);
+  const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
+  auto ask = [&](int64_t s) {
+    if (s < steps) tiles.ask(s, in_rows, i, (s * CL + rank) * kTile, len, c0, a.d);
+    tc::cp_async_commit();
+  };
+  for (int s = 0; s < kFwdStages - 1; ++s) ask(s);
   T* y = at_out<T>(a.y, i, 0, c);
-  const int64_t end = in ? len : 0;  // lanes past the row load and store nothing
-  const int64_t steps = (len + CL * kTile - 1) / (CL * kTile);
-  const int64_t own = (int64_t)rank * kTile + sub * kPos;
-  uint32_t rx[kPos], rg[kPos];
-  load_rows(rx, x, a.x.st, own, end);
-  load_rows(rg, g, a.g.st, own, end);
   const Vec<V> b = in ? bias_of<T>(a, c) : all<V>(0.f);
   Vec<V> h = in ? state_of<V>(a.h_in, a, i, c) : all<V>(0.f);
-  cluster_arrive<CL>();  // every CTA runs before another one writes to it
-  cluster_wait<CL>();
+  tc::cp_async_wait<kFwdStages - 2>();
+  cluster_meet();
   for (int64_t s = 0; s < steps; ++s) {
-    const int64_t t0 = s * CL * kTile + own;
-    const int left = left_of(t0, end);
+    const int64_t t0 = (s * CL + rank) * kTile + sub * kPos;
+    const int left = left_of(t0, len);
+    const Piece16 px(tiles.of(s, 0), sub, tx), pg(tiles.of(s, 1), sub, tx);
     Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      const Vec<V> code = gate_of(add(piece(rg[u], T{}), b)), sz = size_of(code);
-      const Vec<V> B = update(now.B, piece(rx[u], T{}), code), K = mul(now.K, pick(code, sz, other_of(sz)));
-      if (u < left) now = Run<V>{K, B};
+      const Gate<V> gt(add(piece(u < left ? pg[u] : shut<T>(), T{}), b));
+      const Vec<V> k = gt.k();
+      now.B = fma(k, now.B, mul(gt.z(), piece(px[u], T{})));
+      now.K = mul(now.K, k);
       run[u] = now;
     }
-    load_rows(rx, x, a.x.st, t0 + CL * kTile, end);
-    load_rows(rg, g, a.g.st, t0 + CL * kTile, end);
-    const Vec<V> h0 = enter<CL, V, false>(sm, now, h, s & 1, rank, sub, tx);
-    if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
-    T* py = y + t0 * a.y.st;
+    tc::cp_async_wait<kFwdStages - 3>();
+    const Vec<V> h0 = sp.template enter<false>(now, h, s & 1, [&] { ask(s + kFwdStages - 1); });
+    if (in) {
+      if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
+      T* py = y + t0 * a.y.st;
 #pragma unroll
-    for (int u = 0; u < kPos; ++u) {
-      if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
-      py += a.y.st;
+      for (int u = 0; u < kPos; ++u) {
+        if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
+        py += a.y.st;
+      }
     }
   }
+  cluster_meet();
   if (!in) return;
   for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) st4(y + t * a.y.st, all<V>(0.f));
   if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
@@ -501,72 +695,70 @@ __cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 2) recur_fwd_s
 
 // The same from the end: a run of positions maps the R that enters from the right to B + K R.  The states before each
 // thread's 16 positions are the forward's.
-template <typename T, int CL>
-__cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 1) recur_bwd_split(RecurArgs a) {
+template <typename T>
+__global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
+  extern __shared__ __align__(128) char smem[];
   __shared__ SplitSmem<V> sm;
   __shared__ float sh[256 * V];
-  const int rank = cluster_rank<CL>(), tx = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
+  Split<V> sp(sm, a.status);
+  Stages<T, 3, kBwdStages> tiles{smem};
+  const Rows in_rows[3] = {a.x, a.g, a.dy};
+  const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c = (int)(item % a.blocks) * kLanes * V + tx * V;
+  const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
   const bool in = c < a.d;
-  const int64_t len = length(a, i);
-  const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c), *dy = at<T>(a.dy, i, 0, c);
-  T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
-  const int64_t end = in ? len : 0;
-  const int64_t steps = (len + CL * kTile - 1) / (CL * kTile);
-  const int64_t own = (int64_t)rank * kTile + sub * kPos;
+  const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
+  auto start = [&](int64_t s) { return ((steps - 1 - s) * CL + rank) * kTile; };  // steps from the end
+  auto ask = [&](int64_t s) {
+    if (s < steps) tiles.ask(s, in_rows, i, start(s), len, c0, a.d);
+    tc::cp_async_commit();
+  };
   const Vec<V> zero = all<V>(0.f);
-  uint32_t rx[kPos], rg[kPos], ry[kPos];
-  Vec<V> h;
-  auto load = [&](int64_t t0) {
-    load_rows(rx, x, a.x.st, t0, end);
-    load_rows(rg, g, a.g.st, t0, end);
-    load_rows(ry, dy, a.dy.st, t0, end);
-    h = zero;
-    if (t0 < end) {
+  auto before = [&](int64_t t0) {  // the state before this thread's positions
+    Vec<V> h = zero;
+    if (in && t0 < len) {
       if (t0 > 0)
         ldf(kept(a, i, t0, c), h);
       else
         h = state_of<V>(a.h_in, a, i, c);
     }
+    return h;
   };
-  if (steps > 0) load((steps - 1) * CL * kTile + own);
+  for (int s = 0; s < kBwdStages - 1; ++s) ask(s);
+  T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
   const Vec<V> b = in ? bias_of<T>(a, c) : zero;
   Vec<V> R = in ? state_of<V>(a.dh_out, a, i, c) : zero, sum = zero;
-  cluster_arrive<CL>();
-  cluster_wait<CL>();
-  for (int64_t s = steps - 1; s >= 0; --s) {
-    const int64_t t0 = s * CL * kTile + own;
-    const int left = left_of(t0, end);
-    Vec<V> diff[kPos], code[kPos];
-    uint32_t cy[kPos];
+  Vec<V> ahead = steps > 0 ? before(start(0) + sub * kPos) : zero;
+  tc::cp_async_wait<kBwdStages - 2>();
+  cluster_meet();
+  for (int64_t s = 0; s < steps; ++s) {
+    const int64_t t0 = start(s) + sub * kPos;
+    const int left = left_of(t0, len);
+    const Piece16 qx(tiles.of(s, 0), sub, tx), qg(tiles.of(s, 1), sub, tx), qy(tiles.of(s, 2), sub, tx);
+    Vec<V> h = ahead;
+    if (s + 1 < steps) ahead = before(start(s + 1) + sub * kPos);
+    Vec<V> sl[kPos], code[kPos];
+    Run<V> run{all<V>(1.f), zero};  // B = sum of dy_u times the product of k up to u
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      const Vec<V> fx = piece(rx[u], T{}), z = gate_of(add(piece(rg[u], T{}), b));
-      cy[u] = ry[u];
-      code[u] = u < left ? z : zero;  // zero: a position that is not in use
-      diff[u] = minus(fx, h);
-      h = fma(code[u], diff[u], pick(code[u], fx, h));
+      const Gate<V> gt(add(piece(u < left ? qg[u] : shut<T>(), T{}), b));
+      code[u] = gt.code();
+      sl[u] = slope(h, piece(qx[u], T{}), gt);
+      run.K = mul(run.K, gt.k());
+      run.B = fma(run.K, piece(qy[u], T{}), run.B);
     }
-    Run<V> run{all<V>(1.f), zero};
-#pragma unroll
-    for (int u = kPos - 1; u >= 0; --u) {
-      const Vec<V> sz = size_of(code[u]), k = pick(code[u], sz, other_of(sz));
-      run.B = mul(k, add(run.B, piece(cy[u], T{})));
-      run.K = mul(run.K, k);
-    }
-    if (s > 0) load(t0 - CL * kTile);
-    Vec<V> r = enter<CL, V, true>(sm, run, R, s & 1, rank, sub, tx), here = zero;
+    tc::cp_async_wait<kBwdStages - 3>();
+    Vec<V> r = sp.template enter<true>(run, R, s & 1, [&] { ask(s + kBwdStages - 1); }), here = zero;
     T *px = dx + (t0 + kPos) * a.dx.st, *pg = dg + (t0 + kPos) * a.dg.st;
 #pragma unroll
     for (int u = kPos - 1; u >= 0; --u) {
       px -= a.dx.st;
       pg -= a.dg.st;
       Vec<V> ox, og;
-      back(r, piece(cy[u], T{}), code[u], diff[u], ox, og);
-      if (u < left) {
+      back(r, piece(qy[u], T{}), code[u], sl[u], ox, og);
+      if (in && u < left) {
         here = add(here, og);
         st4(px, ox);
         st4(pg, og);
@@ -574,6 +766,7 @@ __cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 1) recur_bwd_s
     }
     sum = add(sum, here);
   }
+  cluster_meet();
   if (in) {
     for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) {
       st4(dx + t * a.dx.st, zero);
@@ -587,20 +780,20 @@ __cluster_dims__(CL, 1, 1) __global__ void __launch_bounds__(256, 1) recur_bwd_s
 // ------------------------------------------------------------------------------------------------------------
 // the bias's gradient, one snapshot
 // ------------------------------------------------------------------------------------------------------------
-// Column sums of `rows` partial rows: eight runs a CTA of 32 columns, joined in order.
-__global__ __launch_bounds__(256) void recur_bias_sum(const float* part, int64_t rows, int32_t d, float* out) {
+// Column sums of `rows` partial rows: 32 runs a CTA of 32 columns, joined in order.
+__global__ __launch_bounds__(1024) void recur_bias_sum(const float* part, int64_t rows, int32_t d, float* out) {
   pdl_begin();
-  __shared__ float sh[8][32];
+  __shared__ float sh[32][32];
   const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, c = blockIdx.x * 32 + tx;
   float s = 0.f;
   if (c < d) {
 #pragma unroll 8
-    for (int64_t r = ty; r < rows; r += 8) s += part[r * d + c];
+    for (int64_t r = ty; r < rows; r += 32) s += part[r * d + c];
   }
   sh[ty][tx] = s;
   __syncthreads();
   if (ty != 0 || c >= d) return;
-  for (int k = 1; k < 8; ++k) s += sh[k][tx];
+  for (int k = 1; k < 32; ++k) s += sh[k][tx];
   out[c] = s;
 }
 
@@ -627,7 +820,7 @@ __global__ __launch_bounds__(256) void recur_step(RecurArgs a) {
       if (a.bias) unpack(ld16(static_cast<const T*>(a.bias) + c + q * E / Q), b + q * E / Q, T{});
     }
 #pragma unroll
-    for (int v = 0; v < E; ++v) o[v] = h[v] = update(Vec<1>{h[v]}, Vec<1>{x[v]}, gate_of(Vec<1>{g[v] + b[v]})).v[0];
+    for (int v = 0; v < E; ++v) o[v] = h[v] = update(Vec<1>{h[v]}, Vec<1>{x[v]}, Gate<1>(Vec<1>{g[v] + b[v]})).v[0];
   }
   T* yp = at_out<T>(a.y, i, 0, c);
 #pragma unroll
@@ -656,9 +849,16 @@ int split_of(const hg_recur_params* p, int64_t n, int64_t T) {
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
   if (n * lanes >= 152 * 256 || T <= 4 * kPos) return 0;
   const int64_t items = n * ceil_div(lanes, kLanes);
-  int cl = 1;
-  while (cl < 8 && items * cl < 2 * 152 && cl * kTile < T) cl *= 2;
-  return cl;
+  int best = 1;
+  int64_t cost = INT64_MAX;
+  for (int cl = 1; cl <= kMaxCluster; ++cl) {
+    const int64_t at_once = 8 * (38 / cl), waves = ceil_div(items, at_once), steps = ceil_div(T, cl * kTile);
+    if (waves * steps < cost) {
+      cost = waves * steps;
+      best = cl;
+    }
+  }
+  return best;
 }
 
 // Rows of partial sums of the bias's gradient.
@@ -694,19 +894,26 @@ Rows rows_of(const hg_seq* r, int64_t n, int64_t T) {
 
 size_t esize(const hg_recur_params* p) { return p->dtype == HG_BF16 ? 2 : 4; }
 
+// A kernel's dynamic shared memory, allowed once for each kernel.
+template <auto* kKernel>
+hg_status allow_smem(size_t bytes) {
+  static bool done = false;
+  if (!done) HG_CUDA(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  done = true;
+  return HG_OK;
+}
+
 template <typename T>
 hg_status forward(const RecurArgs& a, int cl, cudaStream_t s) {
   if (cl == 0) {
-    const Shape sh = shape_of(a.d / kVec<T>);
-    const dim3 grid((unsigned)ceil_div(a.n, sh.block.y), sh.across);
-    if (a.T <= kPos) return launch("recur_fwd", recur_fwd<T, false>, grid, sh.block, 0, s, a);
-    return launch("recur_fwd", recur_fwd<T, true>, grid, sh.block, 0, s, a);
+    const Shape sh = shape_of(a.d / Wide<T>::E);
+    const int64_t groups = ceil_div(a.n, sh.block.y), most = std::max<int64_t>(1, 2 * 152 / sh.across);
+    return launch("recur_fwd", recur_fwd<T>, dim3((unsigned)std::min(groups, most), sh.across), sh.block, 0, s, a);
   }
-  const dim3 grid((unsigned)(a.n * a.blocks * cl)), block(256);
-  if (cl == 1) return launch("recur_fwd_split", recur_fwd_split<T, 1>, grid, block, 0, s, a);
-  if (cl == 2) return launch("recur_fwd_split", recur_fwd_split<T, 2>, grid, block, 0, s, a);
-  if (cl == 4) return launch("recur_fwd_split", recur_fwd_split<T, 4>, grid, block, 0, s, a);
-  return launch("recur_fwd_split", recur_fwd_split<T, 8>, grid, block, 0, s, a);
+  constexpr size_t smem = Stages<T, 2, kFwdStages>::kBytes;
+  HG_TRY(allow_smem<recur_fwd_split<T>>(smem));
+  return launch_clusters("recur_fwd_split", recur_fwd_split<T>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(256), smem, s,
+                         cl, a);
 }
 
 template <typename T>
@@ -717,11 +924,10 @@ hg_status backward(const RecurArgs& a, int cl, int64_t rows, cudaStream_t s) {
     if (a.T <= kPos) return launch("recur_bwd", recur_bwd<T, false>, grid, sh.block, 0, s, a);
     return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
   }
-  const dim3 grid((unsigned)(a.n * a.blocks * cl)), block(256);
-  if (cl == 1) return launch("recur_bwd_split", recur_bwd_split<T, 1>, grid, block, 0, s, a);
-  if (cl == 2) return launch("recur_bwd_split", recur_bwd_split<T, 2>, grid, block, 0, s, a);
-  if (cl == 4) return launch("recur_bwd_split", recur_bwd_split<T, 4>, grid, block, 0, s, a);
-  return launch("recur_bwd_split", recur_bwd_split<T, 8>, grid, block, 0, s, a);
+  constexpr size_t smem = Stages<T, 3, kBwdStages>::kBytes;
+  HG_TRY(allow_smem<recur_bwd_split<T>>(smem));
+  return launch_clusters("recur_bwd_split", recur_bwd_split<T>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(256), smem, s,
+                         cl, a);
 }
 
 RecurArgs args_of(const hg_recur_params* p, int64_t n, int64_t T) {
@@ -731,6 +937,7 @@ RecurArgs args_of(const hg_recur_params* p, int64_t n, int64_t T) {
   a.T = T;
   a.spans = T > 0 ? (T - 1) / kPos : 0;
   a.d = p->d;
+  a.status = device_status_ptr();
   a.blocks = (int32_t)ceil_div(p->d * (int64_t)esize(p) / 4, kLanes);
   return a;
 }
@@ -848,7 +1055,7 @@ extern "C" hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x
     HG_TRY(params->dtype == HG_BF16 ? backward<__nv_bfloat16>(a, cl, rows, s) : backward<float>(a, cl, rows, s));
   }
   if (!dbias) return HG_OK;
-  return launch("recur_bias_sum", recur_bias_sum, dim3((unsigned)ceil_div(w, 32)), dim3(256), 0, s, a.part,
+  return launch("recur_bias_sum", recur_bias_sum, dim3((unsigned)ceil_div(w, 32)), dim3(1024), 0, s, a.part,
                 n > 0 ? rows : 0, params->d, dbias);
 }
 
