@@ -32,25 +32,29 @@ def forward(x, g, bias=None, lens=None, h_in=None):
     return y, h, before, most
 
 
-def backward(x, g, dy, bias=None, lens=None, h_in=None, dh_out=None):
-    """dx, dg, dbias, dh_in, and the same sums with every term's absolute value (x - h becomes |x| + the state's most)."""
+def backward(x, g, dy, bias=None, lens=None, h_in=None, dh_out=None, held=False):
+    """dx, dg, dbias, dh_in, and the same sums with every term's absolute value (x - h becomes |x| + the state's most);
+    held: with R's most so far in the place of R's."""
     n, T, d = x.shape
     z, k = gates(g, bias)
     _, _, before, most = forward(x, g, bias, lens, h_in)
     R = np.zeros((n, d)) if dh_out is None else np.asarray(dh_out, np.float64).copy()
-    N = np.abs(R)
+    own = np.abs(R)
+    N = own.copy()
     out = {q: np.zeros((n, T, d)) for q in ("dx", "dg")}
     mag = {q: np.zeros((n, T, d)) for q in ("dx", "dg")}
     for t in reversed(range(T)):
         m = np.ones(n, bool) if lens is None else t < lens
         R[m] += dy[m, t]
-        N[m] += np.abs(dy[m, t])
+        own[m] = own[m] + np.abs(dy[m, t])
+        N[m] = np.maximum(N[m], own[m]) if held else own[m]
         out["dx"][m, t] = z[m, t] * R[m]
         mag["dx"][m, t] = z[m, t] * N[m]
         out["dg"][m, t] = R[m] * (x[m, t] - before[m, t]) * z[m, t] * k[m, t]
         mag["dg"][m, t] = N[m] * (np.abs(x[m, t]) + most[m]) * z[m, t] * k[m, t]
         R[m] *= k[m, t]
-        N[m] *= k[m, t]
+        own[m] *= k[m, t]
+        N[m] = N[m] if held else own[m]
     for q, r in ((out, R), (mag, N)):
         q["dbias"], q["dh_in"] = q["dg"].sum((0, 1)), r
     return out, mag

@@ -51,34 +51,30 @@ struct RecurArgs {
   int32_t d, blocks;    // split forms: blocks of channels
 };
 
-// A piece's channels: two go through one instruction each where there is one for two fp32 numbers.
+// A piece's channels.  (Instructions on two fp32 numbers at once cost more moves into register pairs, 16 a position of
+// two channels, than they save.)
 template <int V>
 struct Vec {
   float v[V];
 };
-#define HG_TWO(name, op)                                                                                        \
-  __device__ __forceinline__ Vec<2> name(Vec<2> a, Vec<2> b) {                                                  \
-    Vec<2> r;                                                                                                   \
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t" op                       \
-        " z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"                                                               \
-        : "=f"(r.v[0]), "=f"(r.v[1])                                                                            \
-        : "f"(a.v[0]), "f"(a.v[1]), "f"(b.v[0]), "f"(b.v[1]));                                                  \
-    return r;                                                                                                   \
-  }
-HG_TWO(add, "add.rn.f32x2")
-HG_TWO(mul, "mul.rn.f32x2")
-#undef HG_TWO
-__device__ __forceinline__ Vec<2> fma(Vec<2> a, Vec<2> b, Vec<2> c) {
-  Vec<2> r;
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
-      : "=f"(r.v[0]), "=f"(r.v[1])
-      : "f"(a.v[0]), "f"(a.v[1]), "f"(b.v[0]), "f"(b.v[1]), "f"(c.v[0]), "f"(c.v[1]));
-  return r;
+template <int V>
+__device__ __forceinline__ Vec<V> add(Vec<V> a, Vec<V> b) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) a.v[i] += b.v[i];
+  return a;
 }
-__device__ __forceinline__ Vec<1> add(Vec<1> a, Vec<1> b) { return {a.v[0] + b.v[0]}; }
-__device__ __forceinline__ Vec<1> mul(Vec<1> a, Vec<1> b) { return {a.v[0] * b.v[0]}; }
-__device__ __forceinline__ Vec<1> fma(Vec<1> a, Vec<1> b, Vec<1> c) { return {fmaf(a.v[0], b.v[0], c.v[0])}; }
+template <int V>
+__device__ __forceinline__ Vec<V> mul(Vec<V> a, Vec<V> b) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) a.v[i] *= b.v[i];
+  return a;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> fma(Vec<V> a, Vec<V> b, Vec<V> c) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) c.v[i] = fmaf(a.v[i], b.v[i], c.v[i]);
+  return c;
+}
 template <int V>
 __device__ __forceinline__ Vec<V> all(float x) {
   Vec<V> r;
@@ -87,24 +83,31 @@ __device__ __forceinline__ Vec<V> all(float x) {
   return r;
 }
 template <int V>
-__device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {  // a - b, rounded once
-  return fma(b, all<V>(-1.f), a);
+__device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) a.v[i] -= b.v[i];
+  return a;
 }
 
-// z = sigmoid(a) and k = 1 - z, each to a few steps of its own size: s = e^-|a| / (1 + e^-|a|) is the smaller of the two
-// (zero from |a| = 87 on), 1 - s the other.
-template <int V>
+// z = sigmoid(g + b) and k = 1 - z.  The logit's product with -log2 e and the sum with the bias's are one instruction.
+constexpr float kLog2e = 1.4426950408889634f;
+
+// fp32 rows: each to a few steps of its own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero from
+// |a| = 87 on), 1 - s the other, and an update is the nearer end plus the smaller share of the difference: a state that
+// an open gate has just left does not leave its rounding behind.
+template <int V, bool kExact>
 struct Gate {
   Vec<V> s, big;
   bool open[V];
-  __device__ __forceinline__ explicit Gate(Vec<V> a) {
+  __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
+    const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
 #pragma unroll
-    for (int i = 0; i < V; ++i) s.v[i] = gate_ex2(fabsf(a.v[i]) * -1.4426950408889634f);
+    for (int i = 0; i < V; ++i) s.v[i] = gate_ex2(-fabsf(a.v[i]));
     Vec<V> r = add(s, all<V>(1.f));
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       r.v[i] = gate_rcp(r.v[i]);
-      open[i] = a.v[i] >= 0.f;
+      open[i] = a.v[i] <= 0.f;
     }
     s = mul(s, r);
     big = minus(all<V>(1.f), s);
@@ -117,6 +120,8 @@ struct Gate {
   }
   __device__ __forceinline__ Vec<V> z() const { return pick(big, s); }
   __device__ __forceinline__ Vec<V> k() const { return pick(s, big); }
+  __device__ __forceinline__ Vec<V> zk() const { return mul(s, big); }
+  __device__ __forceinline__ Vec<V> next(Vec<V> h, Vec<V> x) const { return fma(code(), minus(x, h), pick(x, h)); }
   // Both in one number: z where it is not negative, -k where it is.
   __device__ __forceinline__ Vec<V> code() const {
     Vec<V> r;
@@ -124,22 +129,50 @@ struct Gate {
     for (int i = 0; i < V; ++i) r.v[i] = open[i] ? -s.v[i] : s.v[i];
     return r;
   }
-};
-template <int V>
-__device__ __forceinline__ void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
+  __device__ __forceinline__ static void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const float s = fabsf(code.v[i]), big = 1.f - s;
-    const bool open = __float_as_int(code.v[i]) < 0;
-    z.v[i] = open ? big : s;
-    k.v[i] = open ? s : big;
+    for (int i = 0; i < V; ++i) {
+      const float s = fabsf(code.v[i]), big = 1.f - s;
+      const bool open = __float_as_int(code.v[i]) < 0;
+      z.v[i] = open ? big : s;
+      k.v[i] = open ? s : big;
+    }
   }
-}
-// The next state: the nearer end and the smaller share of the difference.
+};
+
+// bf16 rows, whose bytes are half as many and whose instructions therefore count: z to a few steps of its own size, 1 - z
+// to a step of one, which is a rounding of the state that it keeps.
 template <int V>
-__device__ __forceinline__ Vec<V> update(Vec<V> h, Vec<V> x, const Gate<V>& g) {
-  return fma(g.code(), minus(x, h), g.pick(x, h));
-}
+struct Gate<V, false> {
+  Vec<V> e, r;
+  __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
+    const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
+#pragma unroll
+    for (int i = 0; i < V; ++i) e.v[i] = gate_ex2(a.v[i]);
+    r = add(e, all<V>(1.f));
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = gate_rcp(r.v[i]);
+  }
+  __device__ __forceinline__ Vec<V> z() const { return r; }
+  __device__ __forceinline__ Vec<V> k() const { return minus(all<V>(1.f), r); }
+  __device__ __forceinline__ Vec<V> zk() const {  // of its own size, as a gradient that it is
+    Vec<V> x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x.v[i] = e.v[i];
+      asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.v[i]) : "f"(3e38f));  // r is zero where e is infinite
+    }
+    return mul(mul(x, r), r);
+  }
+  __device__ __forceinline__ Vec<V> next(Vec<V> h, Vec<V> x) const { return fma(r, minus(x, h), h); }
+  __device__ __forceinline__ Vec<V> code() const { return r; }
+  __device__ __forceinline__ static void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
+    z = code;
+    k = minus(all<V>(1.f), code);
+  }
+};
+template <typename T>
+using GateOf = Gate<4 / (int)sizeof(T), sizeof(T) == 4>;
 
 template <typename T>
 __device__ __forceinline__ uint32_t ld4(const T* p) {
@@ -177,16 +210,16 @@ __device__ __forceinline__ T* at_out(const Rows& r, int64_t i, int64_t t, int c)
   return const_cast<T*>(at<T>(r, i, t, c));
 }
 
-// An infinite bias is a large one, so that -infinity plus it stays what it is (NaN too).
-__device__ __forceinline__ float far_bias(float b) {
-  return isinf(b) ? copysignf(1e30f, b) : b;
+// As the gates take it.  An infinite bias is a large one, so that -infinity plus it stays what it is (NaN too).
+__device__ __forceinline__ float gate_bias(float b) {
+  return -kLog2e * (isinf(b) ? copysignf(1e30f, b) : b);
 }
 template <typename T>
 __device__ __forceinline__ Vec<kVec<T>> bias_of(const RecurArgs& a, int c) {
   Vec<kVec<T>> b = all<kVec<T>>(0.f);
   if (a.bias) b = piece(ld4(static_cast<const T*>(a.bias) + c), T{});
 #pragma unroll
-  for (int v = 0; v < kVec<T>; ++v) b.v[v] = far_bias(b.v[v]);
+  for (int v = 0; v < kVec<T>; ++v) b.v[v] = gate_bias(b.v[v]);
   return b;
 }
 template <int V>
@@ -280,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   if (a.bias) {
     b.unpacked(ld16(static_cast<const T*>(a.bias) + c));
 #pragma unroll
-    for (int k = 0; k < W::N; ++k) b.v[k] = {far_bias(b.v[k].v[0]), far_bias(b.v[k].v[1])};
+    for (int k = 0; k < W::N; ++k) b.v[k] = {gate_bias(b.v[k].v[0]), gate_bias(b.v[k].v[1])};
   }
   // the loads' place: sequence, position, rows
   int64_t li = first, lt = 0, llen = length(a, li), after = li + step < a.n ? length(a, li + step) : 0;
@@ -321,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
         fx.unpacked(rx[buf][u]);
         fg.unpacked(rg[buf][u]);
 #pragma unroll
-        for (int k = 0; k < W::N; ++k) h.v[k] = update(h.v[k], fx.v[k], Gate<2>(add(fg.v[k], b.v[k])));
+        for (int k = 0; k < W::N; ++k) h.v[k] = Gate<2, sizeof(T) == 4>(fg.v[k], b.v[k]).next(h.v[k], fx.v[k]);
         st16(y, h.packed());
         y += a.y.st;
       }
@@ -357,17 +390,17 @@ __device__ __forceinline__ void part_sums(Vec<V> sum, float* sh, int tx, int ty,
 }
 
 // The backward's forward half: a position's state, and what its gate's gradient is of R: (x - h) z k.
-template <int V>
-__device__ __forceinline__ Vec<V> slope(Vec<V>& h, Vec<V> x, const Gate<V>& g) {
+template <int V, bool kExact>
+__device__ __forceinline__ Vec<V> slope(Vec<V>& h, Vec<V> x, const Gate<V, kExact>& g) {
   const Vec<V> diff = minus(x, h);
-  h = fma(g.code(), diff, g.pick(x, h));
-  return mul(diff, mul(g.s, g.big));
+  h = g.next(h, x);
+  return mul(diff, g.zk());
 }
 // And its half from the end: what R gives dx and dg, and R for the position before.
-template <int V>
+template <typename T, int V>
 __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> slope, Vec<V>& dx, Vec<V>& dg) {
   Vec<V> z, k;
-  decode(code, z, k);
+  GateOf<T>::decode(code, z, k);
   R = add(R, dy);
   dx = mul(z, R);
   dg = mul(slope, R);
@@ -410,7 +443,7 @@ __global__ __launch_bounds__(256, 1) void recur_bwd(RecurArgs a) {
       Vec<V> sl[kPos], code[kPos];
 #pragma unroll
       for (int u = 0; u < kPos; ++u) {
-        const Gate<V> gt(add(piece(rg[u], T{}), b));
+        const GateOf<T> gt(piece(rg[u], T{}), b);
         code[u] = gt.code();
         sl[u] = slope(h, piece(rx[u], T{}), gt);
       }
@@ -427,7 +460,7 @@ __global__ __launch_bounds__(256, 1) void recur_bwd(RecurArgs a) {
         pg -= a.dg.st;
         if (u < left) {
           Vec<V> ox, og;
-          back(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
+          back<T>(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
           here = add(here, og);
           st4(px, ox);
           st4(pg, og);
@@ -460,7 +493,7 @@ struct alignas(8 * V) Pair {  // as it lies in shared memory
 };
 template <int V>
 struct SplitSmem {
-  Pair<V> run[2][kSubs][kLanes];
+  Pair<V> run[2][kSubs][kLanes];  // the threads' runs, then what is before each
   Pair<V> tile[2][kMaxCluster][kLanes];
   uint64_t bar[2];  // a step's tiles have come
 };
@@ -474,6 +507,12 @@ __device__ __forceinline__ void join(Run<V>& a, const Pair<V>& p) {  // a, then 
   }
   a.B = fma(K, a.B, B);
   a.K = mul(a.K, K);
+}
+template <int V>
+__device__ __forceinline__ Vec<V> through(Vec<V> h, const Pair<V>& p) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) h.v[v] = fmaf(p.K[v], h.v[v], p.B[v]);
+  return h;
 }
 template <int V>
 __device__ __forceinline__ Pair<V> pair_of(const Run<V>& r) {
@@ -550,8 +589,8 @@ struct Split {
       : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % kLanes),
         ty(threadIdx.x / kLanes) {
     if (threadIdx.x == 0) {
-      tc::mbar_init(&sm.bar[0], 1);
-      tc::mbar_init(&sm.bar[1], 1);
+      tc::mbar_init(&sm.bar[0], 1 + kLanes);
+      tc::mbar_init(&sm.bar[1], 1 + kLanes);
       tc::fence_mbar_init();
     }
     __syncthreads();
@@ -565,33 +604,34 @@ struct Split {
     sm.run[buf][ty][tx] = pair_of(mine);
     if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * kLanes * sizeof(Pair<V>)));
     __syncthreads();
-    Run<V> before{all<V>(1.f), all<V>(0.f)};
     if (threadIdx.x < kLanes) {
-      Run<V> whole = before;
+      Run<V> whole{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
-      for (int k = 0; k < kSubs; ++k) join(whole, sm.run[buf][at(k, kSubs)][threadIdx.x]);
-      if (cl > 1)
+      for (int k = 0; k < kSubs; ++k) {
+        Pair<V>& p = sm.run[buf][at(k, kSubs)][threadIdx.x];
+        const Pair<V> own = p, before = pair_of(whole);
+        join(whole, own);
+        p = before;
+      }
+      if (cl > 1) {
         hand_out(&sm.tile[buf][rank][threadIdx.x], &sm.bar[buf], whole, cl);
-      else
+        tc::mbar_arrive(&sm.bar[buf]);
+      } else {
         sm.tile[buf][0][threadIdx.x] = pair_of(whole);
+      }
     }
     then();
-    const int ahead = at(ty, kSubs);
-    for (int k = 0; k < ahead; ++k) join(before, sm.run[buf][at(k, kSubs)][tx]);
     // (a wait that gave up leaves this call's results invalid; every loop ends all the same)
     if (cl == 1)
       __syncthreads();
     else if (!tiles_here(&sm.bar[buf], phase >> buf & 1))
       record_device_error(status, tc::kErrTimeout);
     phase ^= 1u << buf;
-    Vec<V> got = state;
-    for (int k = 0; k < cl; ++k) {
-      const int r = at(k, cl);
-      if (r == rank) got = fma(before.K, state, before.B);
-      Run<V> s{all<V>(1.f), state};
-      join(s, sm.tile[buf][r][tx]);
-      state = s.B;
-    }
+    const Pair<V>* t = &sm.tile[buf][0][tx];
+    int k = 0;
+    for (; at(k, cl) != rank; ++k) state = through(state, t[at(k, cl) * kLanes]);
+    const Vec<V> got = through(state, sm.run[buf][ty][tx]);
+    for (; k < cl; ++k) state = through(state, t[at(k, cl) * kLanes]);
     return got;
   }
 };
@@ -609,30 +649,55 @@ struct Piece16 {  // a thread's 16 rows
   }
 };
 
-// kStreams arrays' tiles of `stages` steps, asked for that many steps ahead.
+// kStreams arrays' tiles, each step's asked for kStages - 1 steps ahead.  Array 1 is the gates': from the sequence's
+// length on its logits are -infinity and the others' values zero, so no position needs a look at the length.
 template <typename T, int kStreams, int kStages>
 struct Stages {
   static constexpr size_t kBytes = (size_t)kStages * kStreams * kTileBytes;
-  char* smem;
-  __device__ __forceinline__ const char* of(int64_t s, int stream) const {
-    return smem + ((int)(s % kStages) * kStreams + stream) * kTileBytes;
-  }
-  // Step s's rows t0 .. t0 + 255; from `len` on, and past the row's end, zeros.
-  __device__ __forceinline__ void ask(int64_t s, const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t len, int c0,
-                                      int d) {
-    constexpr int E = 16 / (int)sizeof(T);
-    const int q = threadIdx.x % 4, r0 = threadIdx.x / 4, c = c0 + q * E;
-    const int64_t left = c < d ? len - t0 : 0;
+  static constexpr int kRows = kTile / 64;  // a thread's rows of a tile, 64 apart
+  char* smem;                               // of this thread's first row
+  const char* p[kStreams];
+  int64_t row[kStreams], tile[kStreams];    // bytes from row to row, and from step to step
+  int64_t left, step;                       // rows in use from this thread's first one on, and their change
+  int stage = 0;
+  bool in;
+  // First tile at t0; from step to step `by` rows on.
+  __device__ __forceinline__ Stages(char* base, const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t by, int64_t len,
+                                    int c0, int d) {
+    const int q = threadIdx.x % 4, r0 = threadIdx.x / 4, c = c0 + q * (16 / (int)sizeof(T));
+    smem = base + tile_row(r0) + q * 16;
+    in = c < d;
+    left = len - t0 - r0;
+    step = by;
 #pragma unroll
     for (int k = 0; k < kStreams; ++k) {
-      char* to = smem + ((int)(s % kStages) * kStreams + k) * kTileBytes + q * 16;
-      const T* p = at<T>(r[k], i, t0 + r0, c);
-#pragma unroll
-      for (int m = 0; m < kTile / 64; ++m) {
-        const int row = r0 + 64 * m;
-        tc::cp_async16(to + tile_row(row), row < left ? p + 64 * m * r[k].st : static_cast<const T*>(r[k].p), row < left);
-      }
+      p[k] = reinterpret_cast<const char*>(at<T>(r[k], i, t0 + r0, c));
+      row[k] = 64 * r[k].st * (int64_t)sizeof(T);
+      tile[k] = by * r[k].st * (int64_t)sizeof(T);
     }
+  }
+  __device__ __forceinline__ void ask() {
+    char* const to = smem + stage * kStreams * kTileBytes;
+#pragma unroll
+    for (int k = 0; k < kStreams; ++k) {
+      const char* from = p[k];
+      if (in && left > 64 * (kRows - 1)) {
+#pragma unroll
+        for (int m = 0; m < kRows; ++m, from += row[k]) tc::cp_async16(to + k * kTileBytes + m * 64 * 64, from, true);
+      } else {
+        const uint32_t f = k == 1 ? shut<T>() : 0u;
+#pragma unroll
+        for (int m = 0; m < kRows; ++m, from += row[k]) {
+          if (in && left > 64 * m)
+            tc::cp_async16(to + k * kTileBytes + m * 64 * 64, from, true);
+          else
+            st16(to + k * kTileBytes + m * 64 * 64, make_uint4(f, f, f, f));
+        }
+      }
+      p[k] += tile[k];
+    }
+    left -= step;
+    stage = stage + 1 == kStages ? 0 : stage + 1;
   }
 };
 
@@ -645,15 +710,15 @@ __global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
   extern __shared__ __align__(128) char smem[];
   __shared__ SplitSmem<V> sm;
   Split<V> sp(sm, a.status);
-  Stages<T, 2, kFwdStages> tiles{smem};
-  const Rows in_rows[2] = {a.x, a.g};
+  using Tiles = Stages<T, 2, kFwdStages>;
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
   const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
   const bool in = c < a.d;
   const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
+  Tiles tiles(smem, {a.x, a.g}, i, rank * kTile, CL * kTile, len, c0, a.d);
   auto ask = [&](int64_t s) {
-    if (s < steps) tiles.ask(s, in_rows, i, (s * CL + rank) * kTile, len, c0, a.d);
+    if (s < steps) tiles.ask();
     tc::cp_async_commit();
   };
   for (int s = 0; s < kFwdStages - 1; ++s) ask(s);
@@ -662,14 +727,16 @@ __global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
   Vec<V> h = in ? state_of<V>(a.h_in, a, i, c) : all<V>(0.f);
   tc::cp_async_wait<kFwdStages - 2>();
   cluster_meet();
+  int stage = 0;
   for (int64_t s = 0; s < steps; ++s) {
     const int64_t t0 = (s * CL + rank) * kTile + sub * kPos;
-    const int left = left_of(t0, len);
-    const Piece16 px(tiles.of(s, 0), sub, tx), pg(tiles.of(s, 1), sub, tx);
+    const char* const tile = smem + stage * 2 * kTileBytes;
+    stage = stage + 1 == kFwdStages ? 0 : stage + 1;
+    const Piece16 px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
     Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      const Gate<V> gt(add(piece(u < left ? pg[u] : shut<T>(), T{}), b));
+      const GateOf<T> gt(piece(pg[u], T{}), b);
       const Vec<V> k = gt.k();
       now.B = fma(k, now.B, mul(gt.z(), piece(px[u], T{})));
       now.K = mul(now.K, k);
@@ -677,14 +744,16 @@ __global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
     }
     tc::cp_async_wait<kFwdStages - 3>();
     const Vec<V> h0 = sp.template enter<false>(now, h, s & 1, [&] { ask(s + kFwdStages - 1); });
-    if (in) {
-      if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
-      T* py = y + t0 * a.y.st;
+    const int left = in ? left_of(t0, len) : 0;
+    if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
+    T* py = y + t0 * a.y.st;
+    if (left == kPos) {
 #pragma unroll
-      for (int u = 0; u < kPos; ++u) {
+      for (int u = 0; u < kPos; ++u, py += a.y.st) st4(py, fma(run[u].K, h0, run[u].B));
+    } else {
+#pragma unroll
+      for (int u = 0; u < kPos; ++u, py += a.y.st)
         if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
-        py += a.y.st;
-      }
     }
   }
   cluster_meet();
@@ -703,16 +772,16 @@ __global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
   __shared__ SplitSmem<V> sm;
   __shared__ float sh[256 * V];
   Split<V> sp(sm, a.status);
-  Stages<T, 3, kBwdStages> tiles{smem};
-  const Rows in_rows[3] = {a.x, a.g, a.dy};
+  using Tiles = Stages<T, 3, kBwdStages>;
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
   const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
   const bool in = c < a.d;
   const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
   auto start = [&](int64_t s) { return ((steps - 1 - s) * CL + rank) * kTile; };  // steps from the end
+  Tiles tiles(smem, {a.x, a.g, a.dy}, i, start(0), -CL * kTile, len, c0, a.d);
   auto ask = [&](int64_t s) {
-    if (s < steps) tiles.ask(s, in_rows, i, start(s), len, c0, a.d);
+    if (s < steps) tiles.ask();
     tc::cp_async_commit();
   };
   const Vec<V> zero = all<V>(0.f);
@@ -733,17 +802,20 @@ __global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
   Vec<V> ahead = steps > 0 ? before(start(0) + sub * kPos) : zero;
   tc::cp_async_wait<kBwdStages - 2>();
   cluster_meet();
+  int stage = 0;
   for (int64_t s = 0; s < steps; ++s) {
     const int64_t t0 = start(s) + sub * kPos;
-    const int left = left_of(t0, len);
-    const Piece16 qx(tiles.of(s, 0), sub, tx), qg(tiles.of(s, 1), sub, tx), qy(tiles.of(s, 2), sub, tx);
+    const int left = in ? left_of(t0, len) : 0;
+    const char* const tile = smem + stage * 3 * kTileBytes;
+    stage = stage + 1 == kBwdStages ? 0 : stage + 1;
+    const Piece16 qx(tile, sub, tx), qg(tile + kTileBytes, sub, tx), qy(tile + 2 * kTileBytes, sub, tx);
     Vec<V> h = ahead;
     if (s + 1 < steps) ahead = before(start(s + 1) + sub * kPos);
     Vec<V> sl[kPos], code[kPos];
     Run<V> run{all<V>(1.f), zero};  // B = sum of dy_u times the product of k up to u
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
-      const Gate<V> gt(add(piece(u < left ? qg[u] : shut<T>(), T{}), b));
+      const GateOf<T> gt(piece(qg[u], T{}), b);
       code[u] = gt.code();
       sl[u] = slope(h, piece(qx[u], T{}), gt);
       run.K = mul(run.K, gt.k());
@@ -757,8 +829,8 @@ __global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
       px -= a.dx.st;
       pg -= a.dg.st;
       Vec<V> ox, og;
-      back(r, piece(qy[u], T{}), code[u], sl[u], ox, og);
-      if (in && u < left) {
+      back<T>(r, piece(qy[u], T{}), code[u], sl[u], ox, og);
+      if (u < left) {
         here = add(here, og);
         st4(px, ox);
         st4(pg, og);
@@ -820,7 +892,7 @@ __global__ __launch_bounds__(256) void recur_step(RecurArgs a) {
       if (a.bias) unpack(ld16(static_cast<const T*>(a.bias) + c + q * E / Q), b + q * E / Q, T{});
     }
 #pragma unroll
-    for (int v = 0; v < E; ++v) o[v] = h[v] = update(Vec<1>{h[v]}, Vec<1>{x[v]}, Gate<1>(Vec<1>{g[v] + b[v]})).v[0];
+    for (int v = 0; v < E; ++v) o[v] = h[v] = Gate<1, true>(Vec<1>{g[v]}, Vec<1>{gate_bias(b[v])}).next(Vec<1>{h[v]}, Vec<1>{x[v]}).v[0];
   }
   T* yp = at_out<T>(a.y, i, 0, c);
 #pragma unroll

@@ -6,6 +6,9 @@ Tolerances, element by element, with u = half a step of the storage type (2^-24 
      z and 1 - z right to (2.4 |a| + 10) s of itself (exponential, reciprocal, the sum with the bias), and what follows is
      off by that times z |x - h| <= 2 z M with z's weights summing to at most one: below 100 s M, as |a| <= 12 where T
      gates matter at all;
+  bf16 rows: 1 - z is right to 4 s of one, not of itself (z to that of itself): what it keeps, the state or R, is off by
+     that of its size; summed over steps as above where z is small, and where it is not 1 - z < 1/2 keeps less than 8 s
+     in all.  M is the most so far; R's sums are held at their most so far as well.
   dx                   u |want| + (2 T + 140) s A: R, a sum of at most T terms times gates, and one product;
   dg, dbias            u |want| + (4 T + 400) s A, where A takes |x| + M for the difference; dbias adds n T s A.
 bf16 states and dbias are fp32: their u is 2^-24.
@@ -67,7 +70,7 @@ def check(o, dt, x, g, dy, b, lens, h, dh):
     e = (2 * T + 100) * F32
     near(o["y"], y, np.broadcast_to(most[:, None], y.shape), (U[dt], e), "y")
     near(o["h"], last, most, (F32, e), "h_out")
-    want, mag = OR.backward(x, g, dy, b, lens, h, dh)
+    want, mag = OR.backward(x, g, dy, b, lens, h, dh, held=dt == "bf16")
     near(o["dx"], want["dx"], mag["dx"], (U[dt], e + 40 * F32), "dx")
     near(o["dg"], want["dg"], mag["dg"], (U[dt], 2 * e + 200 * F32), "dg")
     near(o["dh"], want["dh_in"], mag["dh_in"], (F32, e), "dh_in")
