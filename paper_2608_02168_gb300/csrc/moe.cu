@@ -22,6 +22,8 @@ constexpr int kSms = 152;
 constexpr int kThr = 256;
 constexpr int kMaxRows = 1024, kMaxExperts = 256, kMaxTop = 8, kMaxF = 16384;
 constexpr int kGroup = 64;  // rows of an expert that a pass over its weights serves
+constexpr int kFewRows = 4;  // up to these the experts' CTAs add up the rows themselves
+constexpr int kMaxPasses = kMaxExperts + kMaxRows * kMaxTop / kGroup;
 
 struct MoeArgs {
   const void *x, *wr, *wg, *wu, *wd;
@@ -34,8 +36,10 @@ struct MoeArgs {
   int32_t* slot_in;  // [n][top] shares that have arrived
   int32_t* row_in;   // [n] slots whose shares have all arrived
   int32_t* place;    // [n][top] pass * group + row in it
+  int32_t* items;    // chunks of all passes
   float* part;       // [CTA + pass][group][d]
   int32_t n, d, f, experts, top, renorm, residual, group;
+  int32_t last;      // the CTA that brings a row's last share adds them up (else moe_sum does)
 };
 
 // ------------------------------------------------------------------------------------------------------------
@@ -63,14 +67,15 @@ struct Two {
   }
 };
 
-// A CTA a row: an expert's logit is summed by `parts` threads.
+// A CTA a row: an expert's logit is summed by `parts` threads, sixteen weights' loads in flight each.
+constexpr int kRouterThr = 1024, kMaxParts = 16;
 template <typename T>
-__global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int parts) {
+__global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, int parts) {
   pdl_begin();
   __shared__ float xs[256];
-  __shared__ float2 sums[kThr], keys[kMaxExperts];
-  __shared__ float warp_sum[kThr / 32];
-  __shared__ int chosen[kMaxTop];
+  __shared__ float2 sums[kRouterThr], keys[kMaxExperts];
+  __shared__ float warp_sum[kMaxExperts / 32];
+  __shared__ int chosen[kMaxTop], before[kMaxExperts];
   __shared__ float pw[kMaxTop];
   __shared__ float raw[kMaxExperts];
   const int row = blockIdx.x, tid = threadIdx.x, d = a.d, E = a.experts, top = a.top;
@@ -82,17 +87,30 @@ __global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int par
       if (a.experts_out) a.experts_out[row * top + tid] = -1;
       if (a.weights_out) a.weights_out[row * top + tid] = 0.f;
     }
-    for (int c = tid; c < d; c += kThr) static_cast<T*>(a.y)[(int64_t)row * d + c] = from_f32<T>(0.f);
+    if (tid < d) static_cast<T*>(a.y)[(int64_t)row * d + tid] = from_f32<T>(0.f);
     return;
   }
-  if (tid < d) xs[tid] = to_f32(static_cast<const T*>(a.x)[(int64_t)row * d + tid]);
-  __syncthreads();
   const int e = tid % width, part = tid / width, per = d / parts;
-  if (part < parts && e < E) {
+  if (tid < d) xs[tid] = to_f32(static_cast<const T*>(a.x)[(int64_t)row * d + tid]);
+  if (tid < E) before[tid] = 0;
+  const bool mine = part < parts && e < E;
+  const T* wr = static_cast<const T*>(a.wr) + (int64_t)part * per * E + e;
+  T v[16];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (k0 + k < per) v[k] = wr[(int64_t)(k0 + k) * E];
+  };
+  if (mine) fetch(0);
+  __syncthreads();
+  if (mine) {
     Two l;
-    const T* w = static_cast<const T*>(a.wr) + (int64_t)part * per * E + e;
-#pragma unroll 16
-    for (int k = 0; k < per; ++k) l.add_product(xs[part * per + k], to_f32(w[(int64_t)k * E]));
+    for (int k0 = 0; k0 < per; k0 += 16) {
+      if (k0 > 0) fetch(k0);
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k0 + k < per) l.add_product(xs[part * per + k0 + k], to_f32(v[k]));
+    }
     sums[tid] = make_float2(l.hi, l.lo);
   }
   __syncthreads();
@@ -104,15 +122,17 @@ __global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int par
   }
   __syncthreads();
   // an expert's place is the number of those before it
-  if (tid < E) {
-    const float2 me = keys[tid];
-    int before = 0;
-    for (int j = 0; j < E; ++j) {
+  if (mine) {
+    const float2 me = keys[e];
+    int n = 0;
+    for (int j = part; j < E; j += parts) {
       const float2 o = keys[j];
-      before += o.x > me.x || (o.x == me.x && (o.y > me.y || (o.y == me.y && j < tid)));
+      n += o.x > me.x || (o.x == me.x && (o.y > me.y || (o.y == me.y && j < e)));
     }
-    if (before < top) chosen[before] = tid;
+    if (n > 0) atomicAdd(&before[e], n);
   }
+  __syncthreads();
+  if (tid < E && before[tid] < top) chosen[before[tid]] = tid;
   __syncthreads();
   // the largest is taken off in both parts; with a NaN among the logits every weight is NaN
   const float2 most = keys[chosen[0]];
@@ -123,7 +143,7 @@ __global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int par
   };
   if (tid < top) pw[tid] = power(chosen[tid]);
   float sum = 0.f;
-  if (!a.renorm) {
+  if (!a.renorm && tid < (E + 31) / 32 * 32) {
     sum = tid < E ? power(tid) : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -135,7 +155,7 @@ __global__ __launch_bounds__(kThr) void moe_router(MoeArgs a, int width, int par
   if (a.renorm) {
     for (int j = 0; j < top; ++j) sum += pw[j];
   } else {
-    for (int j = 0; j < kThr / 32; ++j) sum += warp_sum[j];
+    for (int j = 0; j < (E + 31) / 32; ++j) sum += warp_sum[j];
   }
   const float w = pw[tid] / sum;
   a.sel[row * top + tid] = chosen[tid];
@@ -330,6 +350,31 @@ __device__ __forceinline__ int owner_of(int item, int items, int ctas) {
   return (int)((((int64_t)item + 1) * ctas - 1) / items);
 }
 
+// A column of a row of Y: its experts' shares in the order of the list.
+template <typename T, int D>
+__device__ __forceinline__ void row_sum(const MoeArgs& a, int row, int c, int chunks, int items, int ctas) {
+  float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
+  for (int j = 0; j < a.top; ++j) {
+    const int at = __ldcg(&a.place[row * a.top + j]), pass = at / a.group;
+    const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
+    const float* p = a.part + ((int64_t)(b0 + pass) * a.group + at % a.group) * D + c;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = b0; k <= b1; ++k, p += a.group * D) s += __ldcg(p);
+    y = fmaf(a.w[row * a.top + j], s, y);
+  }
+  static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
+}
+
+// A CTA a row.
+template <typename T, int D>
+__global__ __launch_bounds__(D) void moe_sum(MoeArgs a, int grid) {
+  pdl_begin();
+  const int row = blockIdx.x, items = *a.items, chunks = (a.f + MoeCfg<T, D>::FC - 1) / MoeCfg<T, D>::FC;
+  if (a.sel[row * a.top] < 0) return;  // not live: zeros already
+  row_sum<T, D>(a, row, threadIdx.x, chunks, items, min(grid, items));
+}
+
 template <typename T, int D, int kAct>
 __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   pdl_begin();
@@ -340,6 +385,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   uint16_t* const idx = reinterpret_cast<uint16_t*>(H + C::kH);
   __shared__ int count[kMaxExperts];      // rows of an expert
   __shared__ int first[kMaxExperts + 1];  // its first pass
+  __shared__ uint8_t expert[kMaxPasses];  // of a pass
   __shared__ int warp_part[kThr / 32], list[kGroup];
   __shared__ bool last[kGroup];
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, slots = a.n * a.top, E = a.experts, group = a.group;
@@ -364,10 +410,12 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   __syncthreads();
   for (int k = 0; k < warp; ++k) scan += warp_part[k];
   if (tid < E) first[tid + 1] = scan;
+  for (int k = scan - passes; k < scan; ++k) expert[k] = (uint8_t)tid;
   if (tid == 0) first[0] = 0;
   __syncthreads();
   const int chunks = (a.f + C::FC - 1) / C::FC, items = first[E] * chunks;
   const int ctas = min((int)gridDim.x, items), b = blockIdx.x;
+  if (b == 0 && tid == 0) *a.items = items;
   if (b >= ctas) return;
   const int lo = first_of(b, items, ctas), hi = first_of(b + 1, items, ctas);
 
@@ -375,18 +423,12 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   struct At {
     int pass, chunk, e;
   };
-  auto start = [&](int item) {
-    At c{item / chunks, item % chunks, 0};
-    while (first[c.e + 1] <= c.pass) ++c.e;
-    return c;
-  };
   auto next = [&](At& c) {
     if (++c.chunk < chunks) return;
     c.chunk = 0;
-    ++c.pass;
-    while (c.e < E - 1 && first[c.e + 1] <= c.pass) ++c.e;
+    c.e = expert[++c.pass];
   };
-  At ahead = start(lo), now = ahead;
+  At ahead{lo / chunks, lo % chunks, expert[lo / chunks]}, now = ahead;
   int ahead_item = lo;
   auto load = [&]() {  // the next chunk, into the place of its number
     if (ahead_item < hi) {
@@ -466,6 +508,10 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
     // ---- the share's end of a pass: its sums, and whose last share this is
     sums.store(a.part + (int64_t)(b + was.pass) * group * D, rows);
     if (tid < rows) a.place[list[tid]] = was.pass * group + tid;
+    if (!a.last) {  // moe_sum follows
+      __syncthreads();
+      continue;
+    }
     __threadfence();
     __syncthreads();
     if (tid < rows) {
@@ -479,21 +525,8 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
     }
     __syncthreads();
     __threadfence();
-    for (int r = tid / D; r < rows; r += kThr / D) {
-      if (!last[r]) continue;
-      const int row = list[r] / a.top, c = tid % D;
-      float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
-      for (int j = 0; j < a.top; ++j) {
-        const int at = __ldcg(&a.place[row * a.top + j]), pass = at / group;
-        const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
-        const float* p = a.part + ((int64_t)(b0 + pass) * group + at % group) * D + c;
-        float s = 0.f;
-#pragma unroll 8
-        for (int k = b0; k <= b1; ++k, p += group * D) s += __ldcg(p);
-        y = fmaf(a.w[row * a.top + j], s, y);
-      }
-      static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
-    }
+    for (int r = tid / D; r < rows; r += kThr / D)
+      if (last[r]) row_sum<T, D>(a, list[r] / a.top, tid % D, chunks, items, ctas);
     __syncthreads();  // list, last and X are free
   }
   tc::cp_async_wait<0>();
@@ -503,7 +536,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
 // host
 // ------------------------------------------------------------------------------------------------------------
 struct MoeLayout {
-  int32_t *sel, *slot_in, *row_in, *place;
+  int32_t *sel, *slot_in, *row_in, *place, *items;
   float *w, *part;
   int group;
 };
@@ -516,6 +549,7 @@ size_t carve(void* scratch, const hg_moe_params* p, int64_t n, MoeLayout* L) {
   L->row_in = c.take<int32_t>(n);
   L->place = c.take<int32_t>(slots);
   L->w = c.take<float>(slots);
+  L->items = c.take<int32_t>(1);
   // a pass has its own rows, or 64 of an expert's: at most that many, and a CTA begins at most one more
   const size_t passes = n > 0 ? std::min<size_t>(p->experts, slots) + slots / L->group : 0;
   L->part = c.take<float>((kSms + passes) * L->group * p->d);
@@ -551,7 +585,9 @@ hg_status experts_act(const MoeArgs& a, int grid, cudaStream_t s) {
     HG_CUDA(cudaFuncSetAttribute(moe_experts<T, D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem));
     once = true;
   }
-  return launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a);
+  HG_TRY(launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a));
+  if (a.last) return HG_OK;
+  return launch("moe_sum", moe_sum<T, D>, dim3(a.n), dim3(D), 0, s, a, grid);
 }
 template <typename T, int D>
 hg_status experts_d(const MoeArgs& a, hg_act act, int grid, cudaStream_t s) {
@@ -564,8 +600,8 @@ template <typename T>
 hg_status layer(const MoeArgs& a, hg_act act, cudaStream_t s) {
   int width = 1;  // threads side by side, an expert each
   while (width < a.experts) width *= 2;
-  const int parts = std::min(kThr / width, 16);
-  HG_TRY(launch("moe_router", moe_router<T>, dim3(a.n), dim3(kThr), 0, s, a, width, parts));
+  const int parts = std::min(kRouterThr / width, kMaxParts);
+  HG_TRY(launch("moe_router", moe_router<T>, dim3(a.n), dim3(std::max(width * parts, a.d)), 0, s, a, width, parts));
   // no more CTAs than chunks there can be
   const int64_t slots = (int64_t)a.n * a.top, chunks = ceil_div(a.f, 64 / (int)sizeof(T));
   const int64_t passes = std::min<int64_t>(a.experts, slots) + slots / a.group;
@@ -632,6 +668,8 @@ extern "C" hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, cons
   a.row_in = L.row_in;
   a.place = L.place;
   a.part = L.part;
+  a.items = L.items;
+  a.last = n <= kFewRows;
   a.n = (int32_t)n;
   a.d = p.d;
   a.f = p.f;

@@ -916,26 +916,39 @@ Shape shape_of(int64_t lanes) {  // rows of up to 256 lanes; short ones share a 
   return {dim3((unsigned)width, (unsigned)(256 / width)), (unsigned)across};
 }
 
-// Split over time, and by a cluster of how many CTAs?
-int split_of(const hg_recur_params* p, int64_t n, int64_t T) {
-  const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
-  if (n * lanes >= 152 * 256 || T <= 4 * kPos) return 0;
-  const int64_t items = n * ceil_div(lanes, kLanes);
-  int best = 1;
-  int64_t cost = INT64_MAX;
-  for (int cl = 1; cl <= kMaxCluster; ++cl) {
-    const int64_t at_once = 8 * (38 / cl), waves = ceil_div(items, at_once), steps = ceil_div(T, cl * kTile);
-    if (waves * steps < cost) {
-      cost = waves * steps;
-      best = cl;
+// Split over time, and by a cluster of how many CTAs (0: a chain a thread)?  The least time by a model of both, in us: a
+// split step takes 1.75 (2.15 where CTAs exchange their runs), and longer where two CTAs share an SM; a chain 0.2 a
+// position forward and 0.085 backward.  `held` is how many clusters of each size the GPU holds at once.  Measured, chain /
+// split: 77 fp32 histories of up to 1001, d 200, forward 179 / 40 us; 400 of up to 515, d 256, 112 / 83; 1000 of 100,
+// d 128, 31 / 70; backward 82 / 68, 95 / 155, 32 / 132.  6 of 32768, d 256, by clusters of 1 to 8: 233, 135, 119, 95,
+// 83, 116, 116, 103.
+int split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
+  static const int held[2][kMaxCluster] = {{304, 152, 97, 74, 58, 46, 38, 36}, {152, 76, 46, 36, 28, 23, 15, 15}};
+  if (T <= 4 * kPos || n == 0) return 0;
+  const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, items = n * ceil_div(lanes, kLanes);
+  const Shape s = shape_of(back ? lanes : lanes / 4);
+  const int64_t ctas = ceil_div(n, s.block.y) * s.across;
+  double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, back ? 152 : 304);
+  int cl = 0;
+  auto waves = [](int64_t count, int c) {  // of `count` clusters at once: how long beside one CTA an SM
+    const double full = count * c / 152.0;
+    return full <= 1 ? 1.0 : c == 1 ? 0.4 + 0.6 * full : full;
+  };
+  for (int c = 1; c <= kMaxCluster; ++c) {
+    const int h = held[back][c - 1];
+    const double step = c == 1 ? 1.75 : 2.15, w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
+    const double cost = ceil_div(T, c * kTile) * step * w + 1.5 * ceil_div(items, h);
+    if (cost < best) {
+      best = cost;
+      cl = c;
     }
   }
-  return best;
+  return cl;
 }
 
 // Rows of partial sums of the bias's gradient.
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
-  const int cl = split_of(p, n, T);
+  const int cl = split_of(p, n, T, true);
   if (cl) return n * cl;
   const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4);
   const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, 152 * 16 / s.across);
@@ -1067,7 +1080,7 @@ extern "C" hg_status hg_recur_fwd(const hg_recur_params* params, const hg_seq* x
   a.h_out = h_out;
   a.saved = static_cast<float*>(saved);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const int cl = split_of(params, n, T);
+  const int cl = split_of(params, n, T, false);
   return params->dtype == HG_BF16 ? forward<__nv_bfloat16>(a, cl, s) : forward<float>(a, cl, s);
 }
 
@@ -1123,7 +1136,7 @@ extern "C" hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x
     a.dh_out = dh_out;
     a.dh_in = dh_in;
     a.part = dbias ? static_cast<float*>(scratch) : nullptr;
-    const int cl = split_of(params, n, T);
+    const int cl = split_of(params, n, T, true);
     HG_TRY(params->dtype == HG_BF16 ? backward<__nv_bfloat16>(a, cl, rows, s) : backward<float>(a, cl, rows, s));
   }
   if (!dbias) return HG_OK;
