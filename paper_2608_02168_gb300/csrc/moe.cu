@@ -345,34 +345,48 @@ struct Sums<float, D, kAct> {
 };
 
 // Shares of `items` chunks: CTA b of `ctas` has [first_of(b), first_of(b + 1)).
-__device__ __forceinline__ int first_of(int b, int items, int ctas) { return (int)((int64_t)b * items / ctas); }
-__device__ __forceinline__ int owner_of(int item, int items, int ctas) {
-  return (int)((((int64_t)item + 1) * ctas - 1) / items);
+__device__ __forceinline__ int first_of(int b, int items, int ctas) {
+  return (int)((uint32_t)b * (uint32_t)items / (uint32_t)ctas);
+}
+__device__ __forceinline__ int owner_of(int item, int items, int ctas) {  // (at most 384 passes of 1024 chunks)
+  return (int)(((uint32_t)(item + 1) * (uint32_t)ctas - 1u) / (uint32_t)items);
 }
 
-// A column of a row of Y: its experts' shares in the order of the list.
+// A column of what expert j of a row gave it: its shares in the order of the list.
+template <typename T, int D>
+__device__ __forceinline__ float share_sum(const MoeArgs& a, int row, int j, int c, int chunks, int items, int ctas) {
+  const int at = __ldcg(&a.place[row * a.top + j]), pass = at / a.group;
+  const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
+  const float* p = a.part + ((int64_t)(b0 + pass) * a.group + at % a.group) * D + c;
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = b0; k <= b1; ++k, p += a.group * D) s += __ldcg(p);
+  return s;
+}
+// A column of a row of Y.
 template <typename T, int D>
 __device__ __forceinline__ void row_sum(const MoeArgs& a, int row, int c, int chunks, int items, int ctas) {
   float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
-  for (int j = 0; j < a.top; ++j) {
-    const int at = __ldcg(&a.place[row * a.top + j]), pass = at / a.group;
-    const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
-    const float* p = a.part + ((int64_t)(b0 + pass) * a.group + at % a.group) * D + c;
-    float s = 0.f;
-#pragma unroll 8
-    for (int k = b0; k <= b1; ++k, p += a.group * D) s += __ldcg(p);
-    y = fmaf(a.w[row * a.top + j], s, y);
-  }
+  for (int j = 0; j < a.top; ++j)
+    y = fmaf(a.w[row * a.top + j], share_sum<T, D>(a, row, j, c, chunks, items, ctas), y);
   static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
 }
 
-// A CTA a row.
+// The same, a CTA a row: a thread has a column of one of the row's experts, so that all their shares' loads are in
+// flight together.
 template <typename T, int D>
-__global__ __launch_bounds__(D) void moe_sum(MoeArgs a, int grid) {
+__global__ __launch_bounds__(D * kMaxTop > 1024 ? 1024 : D * kMaxTop) void moe_sum(MoeArgs a, int grid) {
   pdl_begin();
-  const int row = blockIdx.x, items = *a.items, chunks = (a.f + MoeCfg<T, D>::FC - 1) / MoeCfg<T, D>::FC;
+  __shared__ float sums[kMaxTop][D];
+  const int row = blockIdx.x, c = threadIdx.x, chunks = (a.f + MoeCfg<T, D>::FC - 1) / MoeCfg<T, D>::FC;
+  const int items = *a.items, ctas = min(grid, items);
   if (a.sel[row * a.top] < 0) return;  // not live: zeros already
-  row_sum<T, D>(a, row, threadIdx.x, chunks, items, min(grid, items));
+  for (int j = threadIdx.y; j < a.top; j += blockDim.y) sums[j][c] = share_sum<T, D>(a, row, j, c, chunks, items, ctas);
+  __syncthreads();
+  if (threadIdx.y != 0) return;
+  float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
+  for (int j = 0; j < a.top; ++j) y = fmaf(a.w[row * a.top + j], sums[j][c], y);
+  static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
 }
 
 template <typename T, int D, int kAct>
@@ -393,10 +407,23 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   // ---- the list: passes of up to `group` rows of an expert, experts in order; chunks of f in a pass
   for (int i = tid; i < E; i += kThr) count[i] = 0;
   __syncthreads();
-  for (int i = tid; i < slots; i += kThr) {
-    const int e = a.sel[i];
-    idx[i] = (uint16_t)e;  // none: 0xFFFF
-    if (e >= 0) atomicAdd(&count[e], 1);
+  for (int i0 = tid * 4; i0 < slots; i0 += kThr * 16) {  // four loads of four in flight
+    int4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = make_int4(-1, -1, -1, -1);
+      if (i0 + k * kThr * 4 < slots) v[k] = *reinterpret_cast<const int4*>(a.sel + i0 + k * kThr * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e[4] = {v[k].x, v[k].y, v[k].z, v[k].w}, i = i0 + k * kThr * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + j < slots) {
+          idx[i + j] = (uint16_t)e[j];  // none: 0xFFFF
+          if (e[j] >= 0) atomicAdd(&count[e[j]], 1);
+        }
+    }
   }
   __syncthreads();
   int passes = tid < E ? (count[tid] + group - 1) / group : 0;
@@ -485,12 +512,19 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
         at += __popc(m);
       }
       __syncthreads();
-      constexpr int N = D / C::EP;
-      for (int p = tid; p < tiles * 16 * N; p += kThr) {
-        const int r = p / N, q = p % N;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < rows) v = ld16(static_cast<const T*>(a.x) + (int64_t)(list[r] / a.top) * D + q * C::EP);
-        st16(X + (sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)(r * C::XS + q * C::EP) * 4u), v);
+      constexpr int N = D / C::EP, kTileLoads = 16 * N / kThr > 0 ? 16 * N / kThr : 1;  // a thread's of 16 rows
+      uint4 v[4 * kTileLoads];
+#pragma unroll
+      for (int m = 0; m < 4 * kTileLoads; ++m) {
+        const int p = tid + m * kThr, r = p / N, q = p % N;
+        v[m] = make_uint4(0, 0, 0, 0);
+        if (r < rows) v[m] = ld16(static_cast<const T*>(a.x) + (int64_t)(list[r] / a.top) * D + q * C::EP);
+      }
+#pragma unroll
+      for (int m = 0; m < 4 * kTileLoads; ++m) {
+        const int p = tid + m * kThr, r = p / N, q = p % N;
+        if (r < tiles * 16)
+          st16(X + (sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)(r * C::XS + q * C::EP) * 4u), v[m]);
       }
       sums.zero();
     }
@@ -587,7 +621,7 @@ hg_status experts_act(const MoeArgs& a, int grid, cudaStream_t s) {
   }
   HG_TRY(launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a));
   if (a.last) return HG_OK;
-  return launch("moe_sum", moe_sum<T, D>, dim3(a.n), dim3(D), 0, s, a, grid);
+  return launch("moe_sum", moe_sum<T, D>, dim3(a.n), dim3(D, std::min(a.top, 1024 / D)), 0, s, a, grid);
 }
 template <typename T, int D>
 hg_status experts_d(const MoeArgs& a, hg_act act, int grid, cudaStream_t s) {
