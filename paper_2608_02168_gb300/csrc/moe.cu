@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
+#include "layer_kernels.cuh"
 #include "row_sets.cuh"
 #include "tc_util.cuh"
 
@@ -37,6 +38,7 @@ struct MoeArgs {
   int32_t* row_in;   // [n] slots whose shares have all arrived
   int32_t* place;    // [n][top] pass * group + row in it
   int32_t* items;    // chunks of all passes
+  int* status;       // the library's device status word
   float* part;       // [CTA + pass][group][d]
   int32_t n, d, f, experts, top, renorm, residual, group;
   int32_t last;      // the CTA that brings a row's last share adds them up (else moe_sum does)
@@ -175,17 +177,23 @@ struct MoeCfg {
   static constexpr int kStage = 3 * kGate;
   static constexpr int XS = sizeof(T) == 2 ? D : D + 4;    // values between two rows of X, and of H (fp32: padded)
   static constexpr int HS = sizeof(T) == 2 ? FC : FC + 4;
-  static constexpr int kX = kGroup * XS * (int)sizeof(T), kH = kGroup * HS * (int)sizeof(T);
+  static constexpr int kX = kGroup * XS * (int)sizeof(T);
+  static constexpr int kH = kGroup * HS * (int)sizeof(T);  // of one of two places
   static constexpr int kIdx = kMaxRows * kMaxTop * 2;
-  static constexpr int kFit = (220 * 1024 - kX - kH - kIdx) / kStage;
+  static constexpr int kFit = (222 * 1024 - kX - 2 * kH - kIdx) / kStage;
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr size_t kSmem = (size_t)kStages * kStage + kX + kH + kIdx;
+  static constexpr size_t kSmem = (size_t)kStages * kStage + kX + 2 * kH + kIdx;
 };
 
-// Byte offset of piece c of row r, N pieces a row, such that eight rows' pieces lie in different banks.
+// Byte offset of piece c of row r, N pieces a row, such that eight rows' pieces lie in different banks (N = 4: as the
+// 64-byte swizzle of a copied box has them).
 template <int N>
 __device__ __forceinline__ uint32_t place16(int r, int c) {
   return (uint32_t)(r * N + (c ^ (N == 4 ? (r >> 1) & 3 : r & 7))) * 16u;
+}
+// Of W_down's chunk, which comes in boxes of 128 bytes a row.
+__device__ __forceinline__ uint32_t down16(int r, int c) {
+  return (uint32_t)(c / 8 * 32 * 128 + r * 128 + ((c % 8) ^ (r & 7)) * 16);
 }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -254,7 +262,7 @@ struct Sums<__nv_bfloat16, D, kAct> {
       uint32_t b[(NT + 1) / 2][4];
 #pragma unroll
       for (int j = 0; j < (NT + 1) / 2; ++j)  // one tile: the second half of the fragment is not used
-        ldsm4t(w + place16<D / 8>(ks * 16 + lane % 16, warp * NT + 2 * j + (NT > 1 ? lane / 16 : 0)), b[j]);
+        ldsm4t(w + down16(ks * 16 + lane % 16, warp * NT + 2 * j + (NT > 1 ? lane / 16 : 0)), b[j]);
 #pragma unroll
       for (int rt = 0; rt < kGroup / 16; ++rt) {
         if (rt >= tiles) break;
@@ -390,22 +398,29 @@ __global__ __launch_bounds__(D * kMaxTop > 1024 ? 1024 : D * kMaxTop) void moe_s
 }
 
 template <typename T, int D, int kAct>
-__global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
+__global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_constant__ CUtensorMap wg,
+                                                       const __grid_constant__ CUtensorMap wu,
+                                                       const __grid_constant__ CUtensorMap wd) {
   pdl_begin();
   using C = MoeCfg<T, D>;
-  extern __shared__ __align__(128) char smem[];
+  extern __shared__ __align__(1024) char smem[];
   char* const X = smem + C::kStages * C::kStage;
   char* const H = X + C::kX;
-  uint16_t* const idx = reinterpret_cast<uint16_t*>(H + C::kH);
+  uint16_t* const idx = reinterpret_cast<uint16_t*>(H + 2 * C::kH);
   __shared__ int count[kMaxExperts];      // rows of an expert
   __shared__ int first[kMaxExperts + 1];  // its first pass
   __shared__ uint8_t expert[kMaxPasses];  // of a pass
   __shared__ int warp_part[kThr / 32], list[kGroup];
   __shared__ bool last[kGroup];
+  __shared__ uint64_t full[C::kStages];  // a chunk has come
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, slots = a.n * a.top, E = a.experts, group = a.group;
 
   // ---- the list: passes of up to `group` rows of an expert, experts in order; chunks of f in a pass
   for (int i = tid; i < E; i += kThr) count[i] = 0;
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) tc::mbar_init(&full[i], 1);
+    tc::fence_mbar_init();
+  }
   __syncthreads();
   for (int i0 = tid * 4; i0 < slots; i0 += kThr * 16) {  // four loads of four in flight
     int4 v[4];
@@ -457,40 +472,25 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
   };
   At ahead{lo / chunks, lo % chunks, expert[lo / chunks]}, now = ahead;
   int ahead_item = lo;
-  auto load = [&]() {  // the next chunk, into the place of its number
-    if (ahead_item < hi) {
-      char* st = smem + (ahead_item - lo) % C::kStages * C::kStage;
-      const int f0 = ahead.chunk * C::FC, use = min(C::FC, a.f - f0);
-      const T* wg = static_cast<const T*>(a.wg) + (int64_t)ahead.e * D * a.f + f0;
-      const T* wu = static_cast<const T*>(a.wu) + (int64_t)ahead.e * D * a.f + f0;
-      const T* wd = static_cast<const T*>(a.wd) + ((int64_t)ahead.e * a.f + f0) * D;
+  auto load = [&]() {  // thread 0: the next chunk, into the place of its number; columns and rows past f are zeros
+    if (ahead_item >= hi) return;
+    const int stage = (ahead_item - lo) % C::kStages, f0 = ahead.chunk * C::FC;
+    char* st = smem + stage * C::kStage;
+    tc::mbar_expect_tx(&full[stage], C::kStage);
+    tc::tma_load_2d(st, &wg, f0, ahead.e * D, &full[stage]);
+    tc::tma_load_2d(st + C::kGate, &wu, f0, ahead.e * D, &full[stage]);
+    constexpr int kBox = sizeof(T) == 2 ? 64 : D;
 #pragma unroll
-      for (int i = 0; i < D * 4 / kThr; ++i) {
-        const int p = tid + i * kThr, r = p / 4, q = p % 4;
-        const bool in = q * C::EP < use;
-        const int64_t at = in ? (int64_t)r * a.f + q * C::EP : 0;
-        const uint32_t to = sizeof(T) == 2 ? place16<4>(r, q) : (uint32_t)p * 16u;
-        tc::cp_async16(st + to, wg + at, in);
-        tc::cp_async16(st + C::kGate + to, wu + at, in);
-      }
-      constexpr int N = D / C::EP;  // pieces of a W_down row
-#pragma unroll
-      for (int i = 0; i < D * 4 / kThr; ++i) {
-        const int p = tid + i * kThr, r = p / N, q = p % N;
-        const bool in = r < use;
-        const uint32_t to = sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)p * 16u;
-        tc::cp_async16(st + 2 * C::kGate + to, wd + (in ? (int64_t)r * D + q * C::EP : 0), in);
-      }
-      ++ahead_item;
-      if (ahead_item < hi) next(ahead);
-    }
-    tc::cp_async_commit();
+    for (int k = 0; k < D / kBox; ++k)
+      tc::tma_load_3d(st + 2 * C::kGate + k * 32 * 128, &wd, k * kBox, f0, ahead.e, &full[stage]);
+    if (++ahead_item < hi) next(ahead);
   };
-#pragma unroll
-  for (int i = 0; i < C::kStages - 1; ++i) load();
+  if (tid == 0)
+    for (int i = 0; i < C::kStages; ++i) load();
 
   Sums<T, D, kAct> sums;
   int rows = 0, tiles = 0;
+  bool gave_up = false;
   for (int item = lo; item < hi; ++item) {
     if (item == lo || now.chunk == 0) {  // a pass begins: its rows
       const int skip = (now.pass - first[now.e]) * group;
@@ -527,14 +527,19 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
           st16(X + (sizeof(T) == 2 ? place16<N>(r, q) : (uint32_t)(r * C::XS + q * C::EP) * 4u), v[m]);
       }
       sums.zero();
+      __syncthreads();
     }
-    tc::cp_async_wait<C::kStages - 2>();
-    __syncthreads();  // the chunk and the rows are there; the place of the chunk before is free
-    load();
-    const char* st = smem + (item - lo) % C::kStages * C::kStage;
-    sums.hidden(st, X, H, tiles);
-    __syncthreads();
-    sums.out(st, H, tiles);
+    const int at = item - lo, stage = at % C::kStages;
+    const char* st = smem + stage * C::kStage;
+    char* const h = H + at % 2 * C::kH;
+    const bool here = tc::mbar_wait(&full[stage], at / C::kStages & 1);
+    sums.hidden(st, X, h, tiles);
+    if (__syncthreads_or(!here)) {  // H is there, and nobody reads the chunk before any more
+      gave_up = true;
+      break;
+    }
+    if (tid == 0 && at > 0) load();
+    sums.out(st, h, tiles);
     const At was = now;
     if (item + 1 < hi) next(now);
     if (item + 1 < hi && now.chunk != 0) continue;
@@ -542,10 +547,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
     // ---- the share's end of a pass: its sums, and whose last share this is
     sums.store(a.part + (int64_t)(b + was.pass) * group * D, rows);
     if (tid < rows) a.place[list[tid]] = was.pass * group + tid;
-    if (!a.last) {  // moe_sum follows
-      __syncthreads();
-      continue;
-    }
+    if (!a.last) continue;  // moe_sum follows
     __threadfence();
     __syncthreads();
     if (tid < rows) {
@@ -563,7 +565,11 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a) {
       if (last[r]) row_sum<T, D>(a, list[r] / a.top, tid % D, chunks, items, ctas);
     __syncthreads();  // list, last and X are free
   }
-  tc::cp_async_wait<0>();
+  if (gave_up && tid == 0) {  // a copy did not come: nor wait for the others without end
+    record_device_error(a.status, tc::kErrTimeout);
+    for (int at = max(0, ahead_item - lo - C::kStages); at < ahead_item - lo; ++at)
+      tc::mbar_wait(&full[at % C::kStages], at / C::kStages & 1);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -611,6 +617,20 @@ hg_status check(const hg_moe_params* p, int64_t n) {
   return HG_OK;
 }
 
+struct MoeMaps {
+  CUtensorMap wg, wu, wd;
+};
+template <typename T, int D>
+hg_status encode(const MoeArgs& a, MoeMaps* m) {
+  using C = MoeCfg<T, D>;
+  const bool f32 = sizeof(T) == 4;
+  const uint64_t gate[2] = {(uint64_t)a.f, (uint64_t)a.experts * D}, down[3] = {D, (uint64_t)a.f, (uint64_t)a.experts};
+  const uint32_t gate_box[2] = {C::FC, D}, down_box[3] = {f32 ? D : 64, C::FC, 1};
+  HG_TRY(make_tmap(&m->wg, a.wg, f32, 2, gate, gate_box, f32 ? 0 : 64));
+  HG_TRY(make_tmap(&m->wu, a.wu, f32, 2, gate, gate_box, f32 ? 0 : 64));
+  return make_tmap(&m->wd, a.wd, f32, 3, down, down_box, f32 ? 0 : 128);
+}
+
 template <typename T, int D, int kAct>
 hg_status experts_act(const MoeArgs& a, int grid, cudaStream_t s) {
   using C = MoeCfg<T, D>;
@@ -619,7 +639,9 @@ hg_status experts_act(const MoeArgs& a, int grid, cudaStream_t s) {
     HG_CUDA(cudaFuncSetAttribute(moe_experts<T, D, kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem));
     once = true;
   }
-  HG_TRY(launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a));
+  MoeMaps m;
+  HG_TRY((encode<T, D>(a, &m)));
+  HG_TRY(launch("moe_experts", moe_experts<T, D, kAct>, dim3(grid), dim3(kThr), C::kSmem, s, a, m.wg, m.wu, m.wd));
   if (a.last) return HG_OK;
   return launch("moe_sum", moe_sum<T, D>, dim3(a.n), dim3(D, std::min(a.top, 1024 / D)), 0, s, a, grid);
 }
@@ -703,6 +725,7 @@ extern "C" hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, cons
   a.place = L.place;
   a.part = L.part;
   a.items = L.items;
+  a.status = device_status_ptr();
   a.last = n <= kFewRows;
   a.n = (int32_t)n;
   a.d = p.d;

@@ -62,6 +62,35 @@ hg_status make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
   return HG_OK;
 }
 
+hg_status make_tmap(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims, const uint32_t* box,
+                    int swizzle) {
+  auto fn = encode_fn();
+  if (!fn) {
+    set_error("cuTensorMapEncodeTiled is not available from the driver");
+    return HG_ERR_CUDA;
+  }
+  cuuint64_t d[3], strides[2];
+  cuuint32_t b[3], estr[3] = {1, 1, 1};
+  cuuint64_t bytes = f32 ? 4 : 2;
+  for (int k = 0; k < rank; ++k) {
+    d[k] = dims[k];
+    b[k] = box[k];
+    bytes *= dims[k];
+    if (k + 1 < rank) strides[k] = bytes;
+  }
+  CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+                  const_cast<void*>(base), d, strides, b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                  : swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                  : CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled failed (%d) for an array of %d dimensions", (int)r, rank);
+    return HG_ERR_CUDA;
+  }
+  return HG_OK;
+}
+
 // Self-test of the bounded waits: thread 0 of one CTA waits `polls` times on an mbarrier that
 // nothing arrives at (no copy, store or MMA is in flight) and records the give-up in the status
 // word, as every tensor-core kernel does when one of its waits runs out.

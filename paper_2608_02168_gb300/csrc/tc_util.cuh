@@ -69,6 +69,12 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, i
       ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
       : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
 // Four rows r0..r3 of 64 columns from column x (x a multiple of 64 elements here) of a 2-D tensor
 // map whose box is one row high, written one after another (512 B for bf16) at dst; a row index at
 // or past the map's row extent reads zeros.  The 128-byte swizzle follows the destination address,
@@ -271,5 +277,8 @@ __device__ __forceinline__ void record_device_error(int* status, int code) { ato
 // Host: 2-D bf16 tensor map over a row-major [rows x cols] array with a [box_rows x 64] box and
 // 128-byte swizzle.  cols * 2 bytes must be a multiple of 16.
 hg_status make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+// A contiguous array of bf16 or fp32 values of up to three dimensions, innermost first; box and swizzle in bytes (0: none).
+hg_status make_tmap(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims, const uint32_t* box,
+                    int swizzle);
 
 }  // namespace hg
