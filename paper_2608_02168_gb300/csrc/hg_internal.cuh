@@ -78,10 +78,14 @@ void timing_end(int slot, cudaStream_t s);
 // memory, or leave, before it.
 __device__ __forceinline__ void pdl_begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// In a short kernel whose successor needs little of an SM: the successor's CTAs are set up while this one runs (they
+// still wait for its end in pdl_begin()).
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // A launch that may overlap the end of the kernel before it in the stream, up to pdl_begin(): the chains of
 // short kernels gain the set-up time between two of them (step on 10k nodes 1451 -> 1016 us, on 1M nodes
-// 4.83 -> 4.43 ms; fp32 layer on 112k nodes 509 -> 449 us).  No kernel asks for its successor early
-// (griddepcontrol.launch_dependents): the successor's waiting CTAs then take the SMs' shared memory, and with it
+// 4.83 -> 4.43 ms; fp32 layer on 112k nodes 509 -> 449 us).  Kernels of some length do not ask for their
+// successor early (griddepcontrol.launch_dependents): the successor's waiting CTAs then take the SMs' shared memory, and with it
 // the L1 of the gather kernels, for their whole run (10M-node layer 10.4 -> 11.3 ms).
 // launch_clusters: clusters of `cluster` CTAs along x.
 template <typename... KArgs, typename... Args>

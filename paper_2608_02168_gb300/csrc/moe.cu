@@ -34,8 +34,7 @@ struct MoeArgs {
   float* weights_out;
   int32_t* sel;      // [n][top] chosen expert, -1: none
   float* w;          // [n][top]
-  int32_t* slot_in;  // [n][top] shares that have arrived
-  int32_t* row_in;   // [n] slots whose shares have all arrived
+  int32_t* row_in;   // [n] shares that have arrived
   int32_t* place;    // [n][top] pass * group + row in it
   int32_t* items;    // chunks of all passes
   int* status;       // the library's device status word
@@ -56,9 +55,16 @@ struct Two {
     lo = __fadd_rn(lo, __fadd_rn(__fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b)), rest));
     hi = s;
   }
+  template <bool kExact>  // the product of two bf16 numbers is an fp32 number
   __device__ __forceinline__ void add_product(float a, float b) {
     const float p = __fmul_rn(a, b);
-    add(p, fmaf(a, b, -p));
+    if constexpr (kExact) {
+      const float s = __fadd_rn(hi, p), c = __fsub_rn(s, hi);
+      lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, c)), __fsub_rn(p, c)));
+      hi = s;
+    } else {
+      add(p, fmaf(a, b, -p));
+    }
   }
   // As one number in two parts that do not overlap; an infinity has no rest, NaN counts as more than an infinity.
   __device__ __forceinline__ float2 key() const {
@@ -74,14 +80,14 @@ constexpr int kRouterThr = 1024, kMaxParts = 16;
 template <typename T>
 __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, int parts) {
   pdl_begin();
-  __shared__ float xs[256];
+  pdl_next();
+  __shared__ __align__(16) float xs[256];
   __shared__ float2 sums[kRouterThr], keys[kMaxExperts];
   __shared__ float warp_sum[kMaxExperts / 32];
   __shared__ int chosen[kMaxTop], before[kMaxExperts];
   __shared__ float pw[kMaxTop];
   __shared__ float raw[kMaxExperts];
   const int row = blockIdx.x, tid = threadIdx.x, d = a.d, E = a.experts, top = a.top;
-  if (tid < top) a.slot_in[row * top + tid] = 0;
   if (tid == 0) a.row_in[row] = 0;
   if (a.live && a.live[row] <= 0) {
     if (tid < top) {
@@ -98,10 +104,13 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
   const bool mine = part < parts && e < E;
   const T* wr = static_cast<const T*>(a.wr) + (int64_t)part * per * E + e;
   T v[16];
-  auto fetch = [&](int k0) {
+  auto fetch = [&](int k0) {  // per is a multiple of four
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-      if (k0 + k < per) v[k] = wr[(int64_t)(k0 + k) * E];
+    for (int k = 0; k < 16; k += 4)
+      if (k0 + k < per) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[k + j] = wr[(k0 + k + j) * E];
+      }
   };
   if (mine) fetch(0);
   __syncthreads();
@@ -110,8 +119,14 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
     for (int k0 = 0; k0 < per; k0 += 16) {
       if (k0 > 0) fetch(k0);
 #pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (k0 + k < per) l.add_product(xs[part * per + k0 + k], to_f32(v[k]));
+      for (int k = 0; k < 16; k += 4)
+        if (k0 + k < per) {
+          const float4 x = *reinterpret_cast<const float4*>(&xs[part * per + k0 + k]);
+          l.add_product<sizeof(T) == 2>(x.x, to_f32(v[k]));
+          l.add_product<sizeof(T) == 2>(x.y, to_f32(v[k + 1]));
+          l.add_product<sizeof(T) == 2>(x.z, to_f32(v[k + 2]));
+          l.add_product<sizeof(T) == 2>(x.w, to_f32(v[k + 3]));
+        }
     }
     sums[tid] = make_float2(l.hi, l.lo);
   }
@@ -179,6 +194,7 @@ struct MoeCfg {
   static constexpr int HS = sizeof(T) == 2 ? FC : FC + 4;
   static constexpr int kX = kGroup * XS * (int)sizeof(T);
   static constexpr int kH = kGroup * HS * (int)sizeof(T);  // of one of two places
+  static_assert(2 * kH >= kMaxTop * D * 4, "a row's experts' sums have the same place");
   static constexpr int kIdx = kMaxRows * kMaxTop * 2;
   static constexpr int kFit = (222 * 1024 - kX - 2 * kH - kIdx) / kStage;
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
@@ -273,7 +289,9 @@ struct Sums<__nv_bfloat16, D, kAct> {
       }
     }
   }
-  __device__ __forceinline__ void store(float* part, int rows) const {
+  // Row r of the pass to row at(r) of `part`.
+  template <typename F>
+  __device__ __forceinline__ void store(float* part, int rows, F at) const {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
 #pragma unroll
     for (int rt = 0; rt < kGroup / 16; ++rt)
@@ -283,7 +301,7 @@ struct Sums<__nv_bfloat16, D, kAct> {
         if (r >= rows) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-          *reinterpret_cast<float2*>(part + r * D + (warp * NT + j) * 8 + lane % 4 * 2) =
+          *reinterpret_cast<float2*>(part + at(r) * D + (warp * NT + j) * 8 + lane % 4 * 2) =
               make_float2(acc[rt][j][2 * h], acc[rt][j][2 * h + 1]);
       }
   }
@@ -344,11 +362,12 @@ struct Sums<float, D, kAct> {
       }
     }
   }
-  __device__ __forceinline__ void store(float* part, int rows) const {
+  template <typename F>
+  __device__ __forceinline__ void store(float* part, int rows, F at) const {
     const int c = threadIdx.x % D, r0 = threadIdx.x / D;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (r0 + i * kCols < rows) part[(r0 + i * kCols) * D + c] = acc[i];
+      if (r0 + i * kCols < rows) part[at(r0 + i * kCols) * D + c] = acc[i];
   }
 };
 
@@ -360,41 +379,47 @@ __device__ __forceinline__ int owner_of(int item, int items, int ctas) {  // (at
   return (int)(((uint32_t)(item + 1) * (uint32_t)ctas - 1u) / (uint32_t)items);
 }
 
-// A column of what expert j of a row gave it: its shares in the order of the list.
-template <typename T, int D>
-__device__ __forceinline__ float share_sum(const MoeArgs& a, int row, int j, int c, int chunks, int items, int ctas) {
-  const int at = __ldcg(&a.place[row * a.top + j]), pass = at / a.group;
+// A column of what an expert gave a row: the shares of its pass, in the order of the list, at row r of each.
+template <int D>
+__device__ __forceinline__ float share_sum(const MoeArgs& a, int pass, int r, int c, int chunks, int items, int ctas) {
   const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
-  const float* p = a.part + ((int64_t)(b0 + pass) * a.group + at % a.group) * D + c;
+  const float* p = a.part + ((int64_t)(b0 + pass) * a.group + r) * D + c;
   float s = 0.f;
-#pragma unroll 8
-  for (int k = b0; k <= b1; ++k, p += a.group * D) s += __ldcg(p);
+  for (int k = b0; k <= b1; k += 8, p += 8 * a.group * D) {
+    float v[8];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) v[m] = k + m <= b1 ? __ldcg(p + m * a.group * D) : 0.f;
+#pragma unroll
+    for (int m = 0; m < 8; ++m) s += v[m];
+  }
   return s;
 }
 // A column of a row of Y.
 template <typename T, int D>
-__device__ __forceinline__ void row_sum(const MoeArgs& a, int row, int c, int chunks, int items, int ctas) {
-  float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
-  for (int j = 0; j < a.top; ++j)
-    y = fmaf(a.w[row * a.top + j], share_sum<T, D>(a, row, j, c, chunks, items, ctas), y);
-  static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
+__device__ __forceinline__ void row_out(const MoeArgs& a, int row, int c, const float* sums, float x) {
+  for (int j = 0; j < a.top; ++j) x = fmaf(a.w[row * a.top + j], sums[j * D + c], x);
+  static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(x);
+}
+template <typename T, int D>
+__device__ __forceinline__ float row_in(const MoeArgs& a, int row, int c) {
+  return a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
 }
 
-// The same, a CTA a row: a thread has a column of one of the row's experts, so that all their shares' loads are in
-// flight together.
+// A CTA a row: a thread has a column of one of the row's experts, so that all their shares' loads are in flight together.
 template <typename T, int D>
 __global__ __launch_bounds__(D * kMaxTop > 1024 ? 1024 : D * kMaxTop) void moe_sum(MoeArgs a, int grid) {
   pdl_begin();
-  __shared__ float sums[kMaxTop][D];
+  __shared__ float sums[kMaxTop * D];
   const int row = blockIdx.x, c = threadIdx.x, chunks = (a.f + MoeCfg<T, D>::FC - 1) / MoeCfg<T, D>::FC;
   const int items = *a.items, ctas = min(grid, items);
   if (a.sel[row * a.top] < 0) return;  // not live: zeros already
-  for (int j = threadIdx.y; j < a.top; j += blockDim.y) sums[j][c] = share_sum<T, D>(a, row, j, c, chunks, items, ctas);
+  const float x = row_in<T, D>(a, row, c);
+  for (int j = threadIdx.y; j < a.top; j += blockDim.y) {
+    const int at = a.place[row * a.top + j];
+    sums[j * D + c] = share_sum<D>(a, at / a.group, at % a.group, c, chunks, items, ctas);
+  }
   __syncthreads();
-  if (threadIdx.y != 0) return;
-  float y = a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
-  for (int j = 0; j < a.top; ++j) y = fmaf(a.w[row * a.top + j], sums[j][c], y);
-  static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(y);
+  if (threadIdx.y == 0) row_out<T, D>(a, row, c, sums, x);
 }
 
 template <typename T, int D, int kAct>
@@ -459,6 +484,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
   const int ctas = min((int)gridDim.x, items), b = blockIdx.x;
   if (b == 0 && tid == 0) *a.items = items;
   if (b >= ctas) return;
+  if (!a.last) pdl_next();
   const int lo = first_of(b, items, ctas), hi = first_of(b + 1, items, ctas);
 
   // ---- a cursor of the loads and one of the products
@@ -544,25 +570,39 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
     if (item + 1 < hi) next(now);
     if (item + 1 < hi && now.chunk != 0) continue;
 
-    // ---- the share's end of a pass: its sums, and whose last share this is
-    sums.store(a.part + (int64_t)(b + was.pass) * group * D, rows);
-    if (tid < rows) a.place[list[tid]] = was.pass * group + tid;
-    if (!a.last) continue;  // moe_sum follows
+    // ---- the share's end of a pass: its sums
+    float* part = a.part + (int64_t)(b + was.pass) * group * D;
+    if (!a.last) {  // moe_sum follows
+      sums.store(part, rows, [](int r) { return r; });
+      if (tid < rows) a.place[list[tid]] = was.pass * group + tid;
+      continue;
+    }
+    // few rows: one pass an expert, at the rows' own places; whose last share this is
+    sums.store(part, rows, [&](int r) { return list[r] / a.top; });
     __threadfence();
     __syncthreads();
     if (tid < rows) {
-      const int shares = owner_of((was.pass + 1) * chunks - 1, items, ctas) - owner_of(was.pass * chunks, items, ctas) + 1;
-      bool done = false;
-      if (atomicAdd(&a.slot_in[list[tid]], 1) == shares - 1) {
-        __threadfence();
-        done = atomicAdd(&a.row_in[list[tid] / a.top], 1) == a.top - 1;
+      const int row = list[tid] / a.top;
+      int shares = 0;
+      for (int j = 0; j < a.top; ++j) {
+        const int pass = first[idx[row * a.top + j]];
+        shares += owner_of((pass + 1) * chunks - 1, items, ctas) - owner_of(pass * chunks, items, ctas) + 1;
       }
-      last[tid] = done;
+      last[tid] = atomicAdd(&a.row_in[row], 1) == shares - 1;
     }
     __syncthreads();
     __threadfence();
-    for (int r = tid / D; r < rows; r += kThr / D)
-      if (last[r]) row_sum<T, D>(a, list[r] / a.top, tid % D, chunks, items, ctas);
+    for (int r = 0; r < rows; ++r) {
+      if (!last[r]) continue;
+      const int row = list[r] / a.top, c = tid % D;
+      float* const all = reinterpret_cast<float*>(H);
+      const float x = row_in<T, D>(a, row, c);
+      for (int j = tid / D; j < a.top; j += kThr / D)
+        all[j * D + c] = share_sum<D>(a, first[idx[row * a.top + j]], row, c, chunks, items, ctas);
+      __syncthreads();
+      if (tid < D) row_out<T, D>(a, row, c, all, x);
+      __syncthreads();
+    }
     __syncthreads();  // list, last and X are free
   }
   if (gave_up && tid == 0) {  // a copy did not come: nor wait for the others without end
@@ -576,7 +616,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
 // host
 // ------------------------------------------------------------------------------------------------------------
 struct MoeLayout {
-  int32_t *sel, *slot_in, *row_in, *place, *items;
+  int32_t *sel, *row_in, *place, *items;
   float *w, *part;
   int group;
 };
@@ -585,7 +625,6 @@ size_t carve(void* scratch, const hg_moe_params* p, int64_t n, MoeLayout* L) {
   const size_t slots = (size_t)n * p->top_k;
   L->group = (int)std::min<int64_t>(kGroup, (n + 15) / 16 * 16);
   L->sel = c.take<int32_t>(slots);
-  L->slot_in = c.take<int32_t>(slots);
   L->row_in = c.take<int32_t>(n);
   L->place = c.take<int32_t>(slots);
   L->w = c.take<float>(slots);
@@ -720,7 +759,6 @@ extern "C" hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, cons
   a.weights_out = weights;
   a.sel = L.sel;
   a.w = L.w;
-  a.slot_in = L.slot_in;
   a.row_in = L.row_in;
   a.place = L.place;
   a.part = L.part;
