@@ -116,6 +116,7 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
   __syncthreads();
   if (mine) {
     Two l;
+#pragma unroll 1
     for (int k0 = 0; k0 < per; k0 += 16) {
       if (k0 > 0) fetch(k0);
 #pragma unroll
@@ -133,6 +134,7 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
   __syncthreads();
   if (tid < E) {
     Two l;
+#pragma unroll 4
     for (int p = 0; p < parts; ++p) l.add(sums[p * width + tid].x, sums[p * width + tid].y);
     raw[tid] = l.hi;
     keys[tid] = l.key();
@@ -142,6 +144,7 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
   if (mine) {
     const float2 me = keys[e];
     int n = 0;
+#pragma unroll 4
     for (int j = part; j < E; j += parts) {
       const float2 o = keys[j];
       n += o.x > me.x || (o.x == me.x && (o.y > me.y || (o.y == me.y && j < e)));
@@ -170,8 +173,10 @@ __global__ __launch_bounds__(kRouterThr) void moe_router(MoeArgs a, int width, i
   if (tid >= top) return;
   sum = 0.f;
   if (a.renorm) {
+#pragma unroll 1
     for (int j = 0; j < top; ++j) sum += pw[j];
   } else {
+#pragma unroll 1
     for (int j = 0; j < (E + 31) / 32; ++j) sum += warp_sum[j];
   }
   const float w = pw[tid] / sum;
@@ -253,9 +258,10 @@ struct Sums<__nv_bfloat16, D, kAct> {
   __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
     const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4, half = threadIdx.x / 128;
     const uint32_t w = tc::smem_u32(st) + (lane < 16 ? 0 : C::kGate), xa = tc::smem_u32(X);
+#pragma unroll 1
     for (int rt = half; rt < tiles; rt += 2) {
       float g[4] = {}, u[4] = {};
-#pragma unroll
+#pragma unroll 4
       for (int ks = 0; ks < D / 16; ++ks) {
         uint32_t b[4], x[4];
         ldsm4t(w + place16<4>(ks * 16 + lane % 16, ft), b);
@@ -324,7 +330,7 @@ struct Sums<float, D, kAct> {
     const float* x = reinterpret_cast<const float*>(X) + r0 * C::XS;
     float* h = reinterpret_cast<float*>(H) + r0 * C::HS + ft;
     float g[4] = {}, u[4] = {};
-#pragma unroll 4
+#pragma unroll 2
     for (int k = 0; k < D; k += 4) {
       float a[4], b[4];
 #pragma unroll
@@ -348,7 +354,7 @@ struct Sums<float, D, kAct> {
     const int c = threadIdx.x % D, r0 = threadIdx.x / D;
     const float* w = reinterpret_cast<const float*>(st + 2 * C::kGate) + c;
     const float* h = reinterpret_cast<const float*>(H) + r0 * C::HS;
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 16; k += 4) {
       const float w0 = w[k * D], w1 = w[(k + 1) * D], w2 = w[(k + 2) * D], w3 = w[(k + 3) * D];
 #pragma unroll
@@ -385,6 +391,7 @@ __device__ __forceinline__ float share_sum(const MoeArgs& a, int pass, int r, in
   const int b0 = owner_of(pass * chunks, items, ctas), b1 = owner_of((pass + 1) * chunks - 1, items, ctas);
   const float* p = a.part + ((int64_t)(b0 + pass) * a.group + r) * D + c;
   float s = 0.f;
+#pragma unroll 1
   for (int k = b0; k <= b1; k += 8, p += 8 * a.group * D) {
     float v[8];
 #pragma unroll
@@ -397,6 +404,7 @@ __device__ __forceinline__ float share_sum(const MoeArgs& a, int pass, int r, in
 // A column of a row of Y.
 template <typename T, int D>
 __device__ __forceinline__ void row_out(const MoeArgs& a, int row, int c, const float* sums, float x) {
+#pragma unroll 1
   for (int j = 0; j < a.top; ++j) x = fmaf(a.w[row * a.top + j], sums[j * D + c], x);
   static_cast<T*>(a.y)[(int64_t)row * D + c] = from_f32<T>(x);
 }
@@ -414,6 +422,7 @@ __global__ __launch_bounds__(D * kMaxTop > 1024 ? 1024 : D * kMaxTop) void moe_s
   const int items = *a.items, ctas = min(grid, items);
   if (a.sel[row * a.top] < 0) return;  // not live: zeros already
   const float x = row_in<T, D>(a, row, c);
+#pragma unroll 1
   for (int j = threadIdx.y; j < a.top; j += blockDim.y) {
     const int at = a.place[row * a.top + j];
     sums[j * D + c] = share_sum<D>(a, at / a.group, at % a.group, c, chunks, items, ctas);
@@ -435,27 +444,30 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
   __shared__ int count[kMaxExperts];      // rows of an expert
   __shared__ int first[kMaxExperts + 1];  // its first pass
   __shared__ uint8_t expert[kMaxPasses];  // of a pass
-  __shared__ int warp_part[kThr / 32], list[kGroup];
+  __shared__ int warp_part[kThr / 32], list[kGroup], row_of[kGroup];  // a pass's slots, and their rows
   __shared__ bool last[kGroup];
   __shared__ uint64_t full[C::kStages];  // a chunk has come
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, slots = a.n * a.top, E = a.experts, group = a.group;
 
   // ---- the list: passes of up to `group` rows of an expert, experts in order; chunks of f in a pass
+#pragma unroll 1
   for (int i = tid; i < E; i += kThr) count[i] = 0;
   if (tid == 0) {
+#pragma unroll 1
     for (int i = 0; i < C::kStages; ++i) tc::mbar_init(&full[i], 1);
     tc::fence_mbar_init();
   }
   __syncthreads();
-  for (int i0 = tid * 4; i0 < slots; i0 += kThr * 16) {  // four loads of four in flight
-    int4 v[4];
+#pragma unroll 1
+  for (int i0 = tid * 4; i0 < slots; i0 += kThr * 8) {  // two loads of four in flight
+    int4 v[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       v[k] = make_int4(-1, -1, -1, -1);
       if (i0 + k * kThr * 4 < slots) v[k] = *reinterpret_cast<const int4*>(a.sel + i0 + k * kThr * 4);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       const int e[4] = {v[k].x, v[k].y, v[k].z, v[k].w}, i = i0 + k * kThr * 4;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -475,8 +487,10 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
   }
   if (lane == 31) warp_part[warp] = scan;
   __syncthreads();
+#pragma unroll 1
   for (int k = 0; k < warp; ++k) scan += warp_part[k];
   if (tid < E) first[tid + 1] = scan;
+#pragma unroll 1
   for (int k = scan - passes; k < scan; ++k) expert[k] = (uint8_t)tid;
   if (tid == 0) first[0] = 0;
   __syncthreads();
@@ -512,11 +526,13 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
     if (++ahead_item < hi) next(ahead);
   };
   if (tid == 0)
+#pragma unroll 1
     for (int i = 0; i < C::kStages; ++i) load();
 
   Sums<T, D, kAct> sums;
   int rows = 0, tiles = 0;
   bool gave_up = false;
+#pragma unroll 1
   for (int item = lo; item < hi; ++item) {
     if (item == lo || now.chunk == 0) {  // a pass begins: its rows
       const int skip = (now.pass - first[now.e]) * group;
@@ -524,17 +540,23 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
       tiles = (rows + 15) / 16;
       const int per = (slots + kThr - 1) / kThr * 32, s0 = warp * per, s1 = min(slots, s0 + per);
       int found = 0;
+#pragma unroll 1
       for (int s = s0; s < s1; s += 32)
         found += __popc(__ballot_sync(0xffffffffu, s + lane < s1 && idx[s + lane] == now.e));
       if (lane == 0) warp_part[warp] = found;
       __syncthreads();
       int at = -skip;
+#pragma unroll 1
       for (int k = 0; k < warp; ++k) at += warp_part[k];
+#pragma unroll 1
       for (int s = s0; s < s1; s += 32) {
         const bool mine = s + lane < s1 && idx[s + lane] == now.e;
         const uint32_t m = __ballot_sync(0xffffffffu, mine);
         const int r = at + __popc(m & ((1u << lane) - 1));
-        if (mine && r >= 0 && r < group) list[r] = s + lane;
+        if (mine && r >= 0 && r < group) {
+          list[r] = s + lane;
+          row_of[r] = (s + lane) / a.top;
+        }
         at += __popc(m);
       }
       __syncthreads();
@@ -544,7 +566,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
       for (int m = 0; m < 4 * kTileLoads; ++m) {
         const int p = tid + m * kThr, r = p / N, q = p % N;
         v[m] = make_uint4(0, 0, 0, 0);
-        if (r < rows) v[m] = ld16(static_cast<const T*>(a.x) + (int64_t)(list[r] / a.top) * D + q * C::EP);
+        if (r < rows) v[m] = ld16(static_cast<const T*>(a.x) + (int64_t)row_of[r] * D + q * C::EP);
       }
 #pragma unroll
       for (int m = 0; m < 4 * kTileLoads; ++m) {
@@ -578,12 +600,13 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
       continue;
     }
     // few rows: one pass an expert, at the rows' own places; whose last share this is
-    sums.store(part, rows, [&](int r) { return list[r] / a.top; });
+    sums.store(part, rows, [&](int r) { return row_of[r]; });
     __threadfence();
     __syncthreads();
     if (tid < rows) {
-      const int row = list[tid] / a.top;
+      const int row = row_of[tid];
       int shares = 0;
+#pragma unroll 1
       for (int j = 0; j < a.top; ++j) {
         const int pass = first[idx[row * a.top + j]];
         shares += owner_of((pass + 1) * chunks - 1, items, ctas) - owner_of(pass * chunks, items, ctas) + 1;
@@ -592,11 +615,13 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
     }
     __syncthreads();
     __threadfence();
+#pragma unroll 1
     for (int r = 0; r < rows; ++r) {
       if (!last[r]) continue;
-      const int row = list[r] / a.top, c = tid % D;
+      const int row = row_of[r], c = tid % D;
       float* const all = reinterpret_cast<float*>(H);
       const float x = row_in<T, D>(a, row, c);
+#pragma unroll 1
       for (int j = tid / D; j < a.top; j += kThr / D)
         all[j * D + c] = share_sum<D>(a, first[idx[row * a.top + j]], row, c, chunks, items, ctas);
       __syncthreads();
@@ -607,6 +632,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
   }
   if (gave_up && tid == 0) {  // a copy did not come: nor wait for the others without end
     record_device_error(a.status, tc::kErrTimeout);
+#pragma unroll 1
     for (int at = max(0, ahead_item - lo - C::kStages); at < ahead_item - lo; ++at)
       tc::mbar_wait(&full[at % C::kStages], at / C::kStages & 1);
   }
