@@ -253,28 +253,40 @@ struct Sums<__nv_bfloat16, D, kAct> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
   }
-  // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments.  H is
-  // rounded to bf16 once, the operand of the next product.
-  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
-    const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4, half = threadIdx.x / 128;
+  // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments, two tiles
+  // the weights'.  H is rounded to bf16 once, the operand of the next product.
+  template <int NR>
+  __device__ __forceinline__ void hidden_of(const char* st, const char* X, char* H, int rt) {
+    const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4;
     const uint32_t w = tc::smem_u32(st) + (lane < 16 ? 0 : C::kGate), xa = tc::smem_u32(X);
-#pragma unroll 1
-    for (int rt = half; rt < tiles; rt += 2) {
-      float g[4] = {}, u[4] = {};
-#pragma unroll 4
-      for (int ks = 0; ks < D / 16; ++ks) {
-        uint32_t b[4], x[4];
-        ldsm4t(w + place16<4>(ks * 16 + lane % 16, ft), b);
-        ldsm4(xa + place16<D / 8>(rt * 16 + lane % 16, ks * 2 + lane / 16), x);
-        mma(g, x, b[0], b[1]);
-        mma(u, x, b[2], b[3]);
-      }
+    float g[NR][4] = {}, u[NR][4] = {};
+#pragma unroll(D / 16 < 8 / NR ? D / 16 : 8 / NR)
+    for (int ks = 0; ks < D / 16; ++ks) {
+      uint32_t b[4], x[NR][4];
+      ldsm4t(w + place16<4>(ks * 16 + lane % 16, ft), b);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t v = pack2_bf16(gate<kAct>(g[2 * h]) * u[2 * h], gate<kAct>(g[2 * h + 1]) * u[2 * h + 1]);
-        *reinterpret_cast<uint32_t*>(H + place16<4>(rt * 16 + lane / 4 + 8 * h, ft) + lane % 4 * 4) = v;
+      for (int i = 0; i < NR; ++i) ldsm4(xa + place16<D / 8>((rt + 2 * i) * 16 + lane % 16, ks * 2 + lane / 16), x[i]);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        mma(g[i], x[i], b[0], b[1]);
+        mma(u[i], x[i], b[2], b[3]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t v =
+            pack2_bf16(gate<kAct>(g[i][2 * h]) * u[i][2 * h], gate<kAct>(g[i][2 * h + 1]) * u[i][2 * h + 1]);
+        *reinterpret_cast<uint32_t*>(H + place16<4>((rt + 2 * i) * 16 + lane / 4 + 8 * h, ft) + lane % 4 * 4) = v;
+      }
+  }
+  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
+    const int half = threadIdx.x / 128;
+    if (half + 2 < tiles)
+      hidden_of<2>(st, X, H, half);
+    else if (half < tiles)
+      hidden_of<1>(st, X, H, half);
   }
   __device__ __forceinline__ void out(const char* st, const char* H, int tiles) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -453,6 +465,9 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
 #pragma unroll 1
   for (int i = tid; i < E; i += kThr) count[i] = 0;
   if (tid == 0) {
+    tc::prefetch_tmap(&wg);
+    tc::prefetch_tmap(&wu);
+    tc::prefetch_tmap(&wd);
 #pragma unroll 1
     for (int i = 0; i < C::kStages; ++i) tc::mbar_init(&full[i], 1);
     tc::fence_mbar_init();
@@ -525,10 +540,6 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
       tc::tma_load_3d(st + 2 * C::kGate + k * 32 * 128, &wd, k * kBox, f0, ahead.e, &full[stage]);
     if (++ahead_item < hi) next(ahead);
   };
-  if (tid == 0)
-#pragma unroll 1
-    for (int i = 0; i < C::kStages; ++i) load();
-
   Sums<T, D, kAct> sums;
   int rows = 0, tiles = 0;
   bool gave_up = false;
@@ -568,6 +579,9 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
         v[m] = make_uint4(0, 0, 0, 0);
         if (r < rows) v[m] = ld16(static_cast<const T*>(a.x) + (int64_t)row_of[r] * D + q * C::EP);
       }
+      if (item == lo && tid == 0)  // the first chunks: behind the rows' loads, which would wait for them some 3 us
+#pragma unroll 1
+        for (int i = 0; i < C::kStages; ++i) load();
 #pragma unroll
       for (int m = 0; m < 4 * kTileLoads; ++m) {
         const int p = tid + m * kThr, r = p / N, q = p % N;
