@@ -305,8 +305,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W::E;
   const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
   if (c >= a.d || first >= a.n) return;
-  uint4 rx[2][kWide], rg[2][kWide];
-  int64_t lens[2];  // of the sequence that a place's rows are of
+  uint4 rx[kWide], rg[kWide], nx[kWide], ng[kWide];  // this batch's rows, and the next one's
   W b, h, enter;
 #pragma unroll
   for (int k = 0; k < W::N; ++k) b.v[k] = enter.v[k] = all<2>(0.f);
@@ -318,15 +317,16 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   // the loads' place: sequence, position, rows
   int64_t li = first, lt = 0, llen = length(a, li), after = li + step < a.n ? length(a, li + step) : 0;
   const T *x = at<T>(a.x, li, 0, c), *g = at<T>(a.g, li, 0, c);
-  auto load = [&](int buf) {
+  int64_t next_len = 0;  // of the sequence that the next batch is of
+  auto load = [&]() {
     if (li >= a.n) return;
-    lens[buf] = llen;
+    next_len = llen;
     if (lt == 0 && a.h_in) enter.load(a.h_in + li * a.d + c);
 #pragma unroll
     for (int u = 0; u < kWide; ++u)
       if (lt + u < llen) {
-        rx[buf][u] = ld16(x);
-        rg[buf][u] = ld16(g);
+        nx[u] = ld16(x);
+        ng[u] = ld16(g);
         x += a.x.st;
         g += a.g.st;
       }
@@ -342,34 +342,38 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   };
   int64_t i = first, t = 0;
   T* y = at_out<T>(a.y, i, 0, c);
-  auto batch = [&](int buf) {
-    if (i >= a.n) return;
+  load();
+#pragma unroll 1
+  while (true) {
+    const int64_t len = next_len;
+#pragma unroll
+    for (int u = 0; u < kWide; ++u) {
+      rx[u] = nx[u];
+      rg[u] = ng[u];
+    }
     if (t == 0) h = enter;
-    load(buf ^ 1);
+    load();
     if (a.saved && t > 0 && t % kPos == 0) h.store(kept(a, i, t, c));
 #pragma unroll
     for (int u = 0; u < kWide; ++u)
-      if (t + u < lens[buf]) {
+      if (t + u < len) {
         W fx, fg;
-        fx.unpacked(rx[buf][u]);
-        fg.unpacked(rg[buf][u]);
+        fx.unpacked(rx[u]);
+        fg.unpacked(rg[u]);
 #pragma unroll
         for (int k = 0; k < W::N; ++k) h.v[k] = Gate<2, sizeof(T) == 4>(fg.v[k], b.v[k]).next(h.v[k], fx.v[k]);
         st16(y, h.packed());
         y += a.y.st;
       }
     t += kWide;
-    if (t < lens[buf]) return;
-    for (int64_t u = lens[buf]; u < a.T; ++u, y += a.y.st) st16(y, make_uint4(0, 0, 0, 0));
+    if (t < len) continue;
+#pragma unroll 1
+    for (int64_t u = len; u < a.T; ++u, y += a.y.st) st16(y, make_uint4(0, 0, 0, 0));
     if (a.h_out) h.store(a.h_out + i * a.d + c);
     i += step;
+    if (i >= a.n) return;
     t = 0;
     y = at_out<T>(a.y, i, 0, c);
-  };
-  load(0);
-  while (i < a.n) {
-    batch(0);
-    batch(1);
   }
 }
 
@@ -407,11 +411,13 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
   R = mul(k, R);
 }
 
+// (CTAs of 128 threads, two an SM: ragged histories leave fewer threads waiting for the longest one than in 256)
+constexpr int kBwdThr = 128;
 template <typename T, bool kAhead>
-__global__ __launch_bounds__(256, 1) void recur_bwd(RecurArgs a) {
+__global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
-  __shared__ float sh[256 * V];
+  __shared__ float sh[kBwdThr * V];
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   const bool in = c < a.d;
   const Vec<V> zero = all<V>(0.f), b = in ? bias_of<T>(a, c) : zero;
@@ -911,9 +917,9 @@ struct Shape {
   dim3 block;
   unsigned across;  // CTAs across a row
 };
-Shape shape_of(int64_t lanes) {  // rows of up to 256 lanes; short ones share a CTA
-  const int64_t across = ceil_div(lanes, 256), width = ceil_div(lanes, across);
-  return {dim3((unsigned)width, (unsigned)(256 / width)), (unsigned)across};
+Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` lanes; short ones share a CTA
+  const int64_t across = ceil_div(lanes, threads), width = ceil_div(lanes, across);
+  return {dim3((unsigned)width, (unsigned)(threads / width)), (unsigned)across};
 }
 
 // Split over time, and by a cluster of how many CTAs (0: a chain a thread)?  The least time by a model of both, in us: a
@@ -926,9 +932,9 @@ int split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   static const int held[2][kMaxCluster] = {{304, 152, 97, 74, 58, 46, 38, 36}, {152, 76, 46, 36, 28, 23, 15, 15}};
   if (T <= 4 * kPos || n == 0) return 0;
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, items = n * ceil_div(lanes, kLanes);
-  const Shape s = shape_of(back ? lanes : lanes / 4);
+  const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
   const int64_t ctas = ceil_div(n, s.block.y) * s.across;
-  double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, back ? 152 : 304);
+  double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, 304);
   int cl = 0;
   auto waves = [](int64_t count, int c) {  // of `count` clusters at once: how long beside one CTA an SM
     const double full = count * c / 152.0;
@@ -950,7 +956,7 @@ int split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const int cl = split_of(p, n, T, true);
   if (cl) return n * cl;
-  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4);
+  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr);
   const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, 152 * 16 / s.across);
   return std::min(groups, most);
 }
@@ -1004,7 +1010,7 @@ hg_status forward(const RecurArgs& a, int cl, cudaStream_t s) {
 template <typename T>
 hg_status backward(const RecurArgs& a, int cl, int64_t rows, cudaStream_t s) {
   if (cl == 0) {
-    const Shape sh = shape_of(a.d / kVec<T>);
+    const Shape sh = shape_of(a.d / kVec<T>, kBwdThr);
     const dim3 grid((unsigned)rows, sh.across);
     if (a.T <= kPos) return launch("recur_bwd", recur_bwd<T, false>, grid, sh.block, 0, s, a);
     return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
