@@ -3,14 +3,16 @@
 //   z_t = sigmoid(g_t + b),  h_t = h_(t-1) + z_t (x_t - h_(t-1)),
 // and, from the end, with R_t = dy_t + (1 - z_(t+1)) R_(t+1):
 //   dx_t = z_t R_t,  dg_t = R_t (x_t - h_(t-1)) z_t (1 - z_t),  db = sum of dg.
-// An update is the nearer end plus a share of the difference, h + z (x - h) or x + (1 - z) (h - x), whichever share is
-// below a half: no 1 - z is rounded (at z = 1e-5 that alone would change the mean's weight by 0.3 %), and a state that
-// an open gate has just left does not leave its rounding behind.
+// The difference form's share z is known to a few steps of its own size, so long memories (z = 1e-5) keep their weights.
 //
 // Each value is read and written once and costs two special functions and some ten other instructions: all forms are
-// bound by HBM, or by latency where there are few chains.  A thread owns the chain of one 4-byte piece of a row (two
-// bf16 channels or one fp32 channel), walks its positions 16 at a time and holds the next 16 rows' loads in flight.
-// Few chains of many positions are split over time instead: see recur_fwd_split.
+// bound by HBM, or by latency where there are few chains.
+//   recur_fwd, recur_bwd              a thread walks a chain (split_of says when)
+//   recur_fwd_split, recur_bwd_split  a few long histories: time is split over threads, CTAs and clusters
+//   recur_bias_sum                    the CTAs' parts of the bias's gradient, in a fixed order
+//   recur_step                        one new snapshot: 1000003 nodes of d 128, one in eight not live, 242 us (the copy rate)
+// The backward reads x, g, dy and every 16th state, which the forward kept, and forms the states between anew: 0.25 bytes
+// a value more in either pass, where reading the states (4 bytes) or a second forward pass (2 b) would be more.
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
@@ -92,7 +94,7 @@ __device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {
 // z = sigmoid(g + b) and k = 1 - z.  The logit's product with -log2 e and the sum with the bias's are one instruction.
 constexpr float kLog2e = 1.4426950408889634f;
 
-// fp32 rows: each to a few steps of its own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero from
+// fp32 rows: z and k each to a few steps of their own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero from
 // |a| = 87 on), 1 - s the other, and an update is the nearer end plus the smaller share of the difference: a state that
 // an open gate has just left does not leave its rounding behind.
 template <int V, bool kExact>
@@ -140,8 +142,8 @@ struct Gate {
   }
 };
 
-// bf16 rows, whose bytes are half as many and whose instructions therefore count: z to a few steps of its own size, 1 - z
-// to a step of one, which is a rounding of the state that it keeps.
+// bf16 rows, whose bytes are half as many and whose instructions therefore count (5 a gate instead of 9): z to a few steps
+// of its own size, 1 - z to a few of one, which is a rounding of the state that it keeps.
 template <int V>
 struct Gate<V, false> {
   Vec<V> e, r;
@@ -238,12 +240,12 @@ __device__ __forceinline__ int left_of(int64_t t0, int64_t end) {
   const int64_t l = end - t0;
   return l < 0 ? 0 : l > kPos ? kPos : (int)l;
 }
-// kPos rows' pieces from position t0 on; from `end` on x and dy are zero and the gates' logits -infinity: z = 0, a position
-// that leaves every sum as it is.
+// What stands for logits from a sequence's length on: -infinity, so that z = 0 and a position leaves every sum as it is.
 template <typename T>
 __device__ __forceinline__ uint32_t shut() {
   return sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
 }
+// kPos rows' pieces from position t0 on, `fill` from `end` on.
 template <typename T>
 __device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64_t st, int64_t t0, int64_t end,
                                           uint32_t fill = 0u) {
@@ -261,8 +263,8 @@ __device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64
 // ------------------------------------------------------------------------------------------------------------
 // a chain a thread
 // ------------------------------------------------------------------------------------------------------------
-// Forward: a thread has 16 bytes of a row, so that loads, stores and their addresses are few beside the gates, and four
-// positions, the next four's loads in flight.
+// Forward: a thread has 16 bytes of a row, so that loads, stores and their addresses are few beside the gates (4 bytes a
+// thread: 240 us where this takes 203), and four positions, the next four's loads in flight.
 constexpr int kWide = 4;
 template <typename T>
 struct Wide {
@@ -297,7 +299,8 @@ struct Wide {
 };
 
 // A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's length
-// and state, are on their way while these ones' gates are computed.
+// and state, are on their way while these ones' gates are computed (a sequence a thread: 203 us).  Bound by HBM: 150001
+// ragged histories of up to 12, d 128, bf16, 156 us, 0.94 of the copy rate.
 template <typename T>
 __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   pdl_begin();
@@ -411,7 +414,10 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
   R = mul(k, R);
 }
 
-// (CTAs of 128 threads, two an SM: ragged histories leave fewer threads waiting for the longest one than in 256)
+// Backward: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one kept before them; kAhead: the
+// 16 before them are loaded meanwhile (histories of one batch do without).  CTAs of 128 threads, two an SM: ragged
+// histories leave fewer threads waiting for the longest one than in 256 (400 of up to 515, d 256, 99 -> 85 us; 2000 of
+// them 316 us, 0.86 of the copy rate).  Registers bound it: 16 positions' gates and slopes, and the next rows.
 constexpr int kBwdThr = 128;
 template <typename T, bool kAhead>
 __global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
@@ -488,7 +494,12 @@ __global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
 // a zero state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).
 // Threads form the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to
 // the cluster's others (distributed shared memory), and every CTA joins them in the same order, so all carry the same
-// state and a call repeats its bits.  One barrier of the cluster a step.
+// state and a call repeats its bits.
+//
+// A step of a CTA alone takes 1.75 us, one after another: copies into shared memory 0.55, gates 0.5, the join 0.4, stores
+// 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6 histories
+// of 32768, d 256, bf16: 86 us forward (HBM: 44).  Half as many positions a thread and twice as many threads took 97 us
+// where this took 83, instructions on bf16 pairs and more registers in flight changed nothing.
 template <int V>
 struct Run {
   Vec<V> K, B;
@@ -543,6 +554,7 @@ __device__ __forceinline__ int cluster_reg_size() {
 }
 // Every CTA runs before another one writes to it, and is there until the last one has.
 __device__ __forceinline__ void cluster_meet() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // To the same place of every CTA of the cluster, counted by the barrier at the same place there.  (A barrier of the
@@ -566,8 +578,7 @@ __device__ __forceinline__ void hand_out(Pair<V>* slot, uint64_t* bar, const Run
   }
 }
 
-// The joined run of the tiles and threads before this one, from a step's runs: in the order of positions, or from the
-// end.  State is carried on to the next step; what enters this thread's positions is returned.
+// A bounded wait for a step's tiles: false when it ran out.
 __device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity) {
   const uint32_t addr = tc::smem_u32(bar);
   for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
@@ -590,6 +601,7 @@ struct Split {
   int* status;
   int cl, rank, tx, ty;
   uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
+  bool ok = true;      // no wait has run out
 
   __device__ __forceinline__ Split(SplitSmem<V>& s, int* st)
       : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % kLanes),
@@ -601,9 +613,9 @@ struct Split {
     }
     __syncthreads();
   }
-  // A CTA hands out step s + 1 after all its threads have read step s, and enters s + 2 after every other one has
-  // handed out s + 1: two places are enough.
-  // `then` is done by all threads when all have formed their runs.
+  // The state that enters this thread's run, in the order of positions or from the end; `state`, of the step before, is
+  // carried on.  `then` is done by all threads when all have formed their runs.  A CTA hands out step s + 1 after all its
+  // threads have read step s, and enters s + 2 after every other one has handed out s + 1: two places are enough.
   template <bool kBack, typename F>
   __device__ __forceinline__ Vec<V> enter(const Run<V>& mine, Vec<V>& state, int buf, F then) {
     auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
@@ -627,11 +639,12 @@ struct Split {
       }
     }
     then();
-    // (a wait that gave up leaves this call's results invalid; every loop ends all the same)
-    if (cl == 1)
+    if (cl == 1) {
       __syncthreads();
-    else if (!tiles_here(&sm.bar[buf], phase >> buf & 1))
+    } else if (ok && !tiles_here(&sm.bar[buf], phase >> buf & 1)) {
+      ok = false;  // this call's results are invalid; nothing waits any more, and every loop ends
       record_device_error(status, tc::kErrTimeout);
+    }
     phase ^= 1u << buf;
     const Pair<V>* t = &sm.tile[buf][0][tx];
     int k = 0;

@@ -914,14 +914,24 @@ def _flat_seq_arg(t, name: str, dtype, shape):
     return byref(hg_seq(t.data_ptr(), strides[0], strides[1]))
 
 
-def _recur_bytes(c, n: int, T: int) -> tuple:
-    s, b = c_size_t(0), c_size_t(0)
-    _check(lib().hg_recur_workspace_size(byref(c), int(n), int(T), byref(s), byref(b)), "hg_recur_workspace_size")
-    return s.value, b.value
+def _sizes(params, key, ask):
+    """What a size query of these parameters gave, asked for once a shape (sizes hang on the struct's numbers alone)."""
+    known = params.__dict__.setdefault("_known", {})
+    if key not in known:
+        if len(known) >= 64:
+            known.clear()
+        known[key] = ask()
+    return known[key]
 
 
 def hg_recur_workspace_size(params: RecurParams, n: int, T: int) -> tuple:
-    return _recur_bytes(params.c(), n, T)
+    def ask():
+        s, b = c_size_t(0), c_size_t(0)
+        _check(lib().hg_recur_workspace_size(byref(params.c()), int(n), int(T), byref(s), byref(b)),
+               "hg_recur_workspace_size")
+        return s.value, b.value
+
+    return _sizes(params, (n, T), ask)
 
 
 def hg_recur_fwd(params: RecurParams, x, g, lens, h_in, y, h_out, saved, stream=None):
@@ -930,9 +940,8 @@ def hg_recur_fwd(params: RecurParams, x, g, lens, h_in, y, h_out, saved, stream=
     n, T, d = x.shape[0], x.shape[1], params.d
     r = [_flat_seq_arg(t, k, params.dtype, (n, T, d)) for t, k in ((x, "x"), (g, "g"), (y, "y"))]
     h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (h_out, "h_out"))]
-    c = params.c()
-    sv = None if saved is None else _work_ptr(saved, _recur_bytes(c, n, T)[0], "saved")
-    _check(lib().hg_recur_fwd(byref(c), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], r[2], h[1], sv,
+    sv = None if saved is None else _work_ptr(saved, hg_recur_workspace_size(params, n, T)[0], "saved")
+    _check(lib().hg_recur_fwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], r[2], h[1], sv,
                               _stream(stream)), "hg_recur_fwd")
 
 
@@ -942,11 +951,10 @@ def hg_recur_bwd(params: RecurParams, x, g, lens, h_in, saved, d_y, dh_out, dx, 
     r = [_flat_seq_arg(t, k, params.dtype, (n, T, d))
          for t, k in ((x, "x"), (g, "g"), (d_y, "d_y"), (dx, "dx"), (dg, "dg"))]
     h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (dh_out, "dh_out"), (dh_in, "dh_in"))]
-    c = params.c()
-    sb, wb = _recur_bytes(c, n, T)
+    sb, wb = hg_recur_workspace_size(params, n, T)
     sv = _work_ptr(saved, sb, "saved")
     w = _work_ptr(scratch, wb if n and dbias is not None else 0, "scratch")
-    _check(lib().hg_recur_bwd(byref(c), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], sv, r[2], h[1],
+    _check(lib().hg_recur_bwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], sv, r[2], h[1],
                               r[3], r[4], h[2], _want(dbias, "dbias", torch.float32, (d,)), w, _stream(stream)),
            "hg_recur_bwd")
 
@@ -976,21 +984,19 @@ class MoeParams(_Params):
                        (W_router, W_gate, W_up, W_down), ("W_router", "W_gate", "W_up", "W_down"), shapes)))
 
 
-def _moe_bytes(c, n: int) -> int:
-    b = c_size_t(0)
-    _check(lib().hg_moe_workspace_size(byref(c), int(n), byref(b)), "hg_moe_workspace_size")
-    return b.value
-
-
 def hg_moe_workspace_size(params: MoeParams, n: int) -> int:
-    return _moe_bytes(params.c(), n)
+    def ask():
+        b = c_size_t(0)
+        _check(lib().hg_moe_workspace_size(byref(params.c()), int(n), byref(b)), "hg_moe_workspace_size")
+        return b.value
+
+    return _sizes(params, n, ask)
 
 
 def hg_moe_fwd(params: MoeParams, X, live, Y, experts, weights, scratch, stream=None):
     """X, Y [n, d]; live int32 [n] or None; experts int32 and weights fp32 [n, top_k], or None."""
     n, shape, chosen = X.shape[0], (X.shape[0], params.d), (X.shape[0], params.top_k)
-    c = params.c()
-    w = _work_ptr(scratch, _moe_bytes(c, n), "scratch")
-    _check(lib().hg_moe_fwd(byref(c), _want(X, "X", params.dtype, shape), _want(live, "live", torch.int32, (n,)), n,
+    w = _work_ptr(scratch, hg_moe_workspace_size(params, n), "scratch")
+    _check(lib().hg_moe_fwd(byref(params.c()), _want(X, "X", params.dtype, shape), _want(live, "live", torch.int32, (n,)), n,
                             _want(Y, "Y", params.dtype, shape), _want(experts, "experts", torch.int32, chosen),
                             _want(weights, "weights", torch.float32, chosen), w, _stream(stream)), "hg_moe_fwd")
