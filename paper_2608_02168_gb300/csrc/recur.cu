@@ -25,10 +25,12 @@ namespace {
 
 constexpr int kPos = 16;          // positions a thread holds at a time; the forward keeps every 16th state
 constexpr int kMaxWidth = 16384;  // channels of a row
-constexpr int kLanes = 16;        // split forms: lanes across a row's piece, so 64 bytes of it
-constexpr int kSubs = 16;         // ... and threads along time, kPos positions each
-constexpr int kTile = kSubs * kPos;
+constexpr int kSplitThr = 256;    // split forms: threads, L across a piece of a row and the others along time
 constexpr int kMaxCluster = 8;
+template <int L>
+constexpr int kSubs = kSplitThr / L;       // threads along time, kPos positions each
+template <int L>
+constexpr int kTile = kSubs<L> * kPos;     // positions of a CTA's step
 
 template <typename T>
 constexpr int kVec = 4 / (int)sizeof(T);  // channels of a 4-byte piece
@@ -489,17 +491,18 @@ __global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
 // ------------------------------------------------------------------------------------------------------------
 // a chain split over time
 // ------------------------------------------------------------------------------------------------------------
-// A cluster of CL CTAs takes 64 bytes of a sequence's rows through CL tiles of 256 positions a step; a thread has 16
-// positions of a 4-byte piece.  Positions compose: a run of them maps the state h before it to B + K h, B its end from
-// a zero state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).
-// Threads form the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to
-// the cluster's others (distributed shared memory), and every CTA joins them in the same order, so all carry the same
-// state and a call repeats its bits.
+// A cluster of CL CTAs takes a piece of a sequence's rows (L lanes of 4 bytes) through CL tiles of positions a step: 64
+// bytes and 256 positions a tile, or, where even eight CTAs a piece leave SMs idle, 32 bytes and 512.  A thread has 16
+// positions of 4 bytes.  Positions compose: a run of them maps the state h before it to B + K h, B its end from a zero
+// state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).  Threads form
+// the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to the cluster's
+// others (distributed shared memory), and every CTA joins them in the same order, so all carry the same state and a call
+// repeats its bits.
 //
 // A step of a CTA alone takes 1.75 us, one after another: copies into shared memory 0.55, gates 0.5, the join 0.4, stores
 // 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6 histories
 // of 32768, d 256, bf16: 86 us forward (HBM: 44).  Half as many positions a thread and twice as many threads took 97 us
-// where this took 83, instructions on bf16 pairs and more registers in flight changed nothing.
+// where this took 83; instructions on two numbers at once changed nothing.
 template <int V>
 struct Run {
   Vec<V> K, B;
@@ -508,10 +511,12 @@ template <int V>
 struct alignas(8 * V) Pair {  // as it lies in shared memory
   float K[V], B[V];
 };
-template <int V>
+constexpr int kJoin = 16;  // runs that a lane joins one after another; with twice as many, two lanes do, and join theirs
+template <int V, int L>
 struct SplitSmem {
-  Pair<V> run[2][kSubs][kLanes];  // the threads' runs, then what is before each
-  Pair<V> tile[2][kMaxCluster][kLanes];
+  Pair<V> run[2][kSubs<L>][L];  // the threads' runs, then what is before each among its sixteen
+  Pair<V> half[2][L];           // of the first sixteen of 32
+  Pair<V> tile[2][kMaxCluster][L];
   uint64_t bar[2];  // a step's tiles have come
 };
 template <int V>
@@ -595,20 +600,21 @@ __device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity) {
   return false;
 }
 
-template <int V>
+template <int V, int L>
 struct Split {
-  SplitSmem<V>& sm;
+  SplitSmem<V, L>& sm;
   int* status;
   int cl, rank, tx, ty;
   uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
   bool ok = true;      // no wait has run out
+  static constexpr int kGroups = kSubs<L> / kJoin, kJoiners = L * kGroups;
+  static_assert(kJoiners == 16, "the joining lanes are half a warp");
 
-  __device__ __forceinline__ Split(SplitSmem<V>& s, int* st)
-      : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % kLanes),
-        ty(threadIdx.x / kLanes) {
+  __device__ __forceinline__ Split(SplitSmem<V, L>& s, int* st)
+      : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % L), ty(threadIdx.x / L) {
     if (threadIdx.x == 0) {
-      tc::mbar_init(&sm.bar[0], 1 + kLanes);
-      tc::mbar_init(&sm.bar[1], 1 + kLanes);
+      tc::mbar_init(&sm.bar[0], 1 + kJoiners);
+      tc::mbar_init(&sm.bar[1], 1 + kJoiners);
       tc::fence_mbar_init();
     }
     __syncthreads();
@@ -620,23 +626,36 @@ struct Split {
   __device__ __forceinline__ Vec<V> enter(const Run<V>& mine, Vec<V>& state, int buf, F then) {
     auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
     sm.run[buf][ty][tx] = pair_of(mine);
-    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * kLanes * sizeof(Pair<V>)));
+    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * L * sizeof(Pair<V>)));
     __syncthreads();
-    if (threadIdx.x < kLanes) {
+    if (threadIdx.x < kJoiners) {
+      const int group = threadIdx.x / L;
       Run<V> whole{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
-      for (int k = 0; k < kSubs; ++k) {
-        Pair<V>& p = sm.run[buf][at(k, kSubs)][threadIdx.x];
+      for (int k = 0; k < kJoin; ++k) {
+        Pair<V>& p = sm.run[buf][at(group * kJoin + k, kSubs<L>)][tx];
         const Pair<V> own = p, before = pair_of(whole);
         join(whole, own);
         p = before;
       }
-      if (cl > 1) {
-        hand_out(&sm.tile[buf][rank][threadIdx.x], &sm.bar[buf], whole, cl);
-        tc::mbar_arrive(&sm.bar[buf]);
-      } else {
-        sm.tile[buf][0][threadIdx.x] = pair_of(whole);
+      if constexpr (kGroups == 2) {
+        if (group == 0) sm.half[buf][tx] = pair_of(whole);
+        Run<V> first;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          first.K.v[v] = __shfl_xor_sync(0xffffu, whole.K.v[v], L);
+          first.B.v[v] = __shfl_xor_sync(0xffffu, whole.B.v[v], L);
+        }
+        join(first, pair_of(whole));
+        whole = first;
       }
+      if (group == kGroups - 1) {
+        if (cl > 1)
+          hand_out(&sm.tile[buf][rank][tx], &sm.bar[buf], whole, cl);
+        else
+          sm.tile[buf][0][tx] = pair_of(whole);
+      }
+      if (cl > 1) tc::mbar_arrive(&sm.bar[buf]);
     }
     then();
     if (cl == 1) {
@@ -648,32 +667,42 @@ struct Split {
     phase ^= 1u << buf;
     const Pair<V>* t = &sm.tile[buf][0][tx];
     int k = 0;
-    for (; at(k, cl) != rank; ++k) state = through(state, t[at(k, cl) * kLanes]);
-    const Vec<V> got = through(state, sm.run[buf][ty][tx]);
-    for (; k < cl; ++k) state = through(state, t[at(k, cl) * kLanes]);
+    for (; at(k, cl) != rank; ++k) state = through(state, t[at(k, cl) * L]);
+    Vec<V> got = state;
+    if (kGroups == 2 && at(ty, kSubs<L>) >= kJoin) got = through(got, sm.half[buf][tx]);
+    got = through(got, sm.run[buf][ty][tx]);
+    for (; k < cl; ++k) state = through(state, t[at(k, cl) * L]);
     return got;
   }
 };
 
-// A tile of rows' pieces in shared memory, 64 bytes a row: neighbouring rows are swapped in every other thread's 16, which
-// puts the rows that a warp's two threads along time read together into different banks.
-constexpr int kTileBytes = kTile * 64;
-__device__ __forceinline__ int tile_row(int r) { return (r ^ (r / kPos & 1)) * 64; }
-struct Piece16 {  // a thread's 16 rows
-  const char *even, *odd;
-  __device__ __forceinline__ Piece16(const char* tile, int sub, int tx)
-      : even(tile + sub * kPos * 64 + (sub & 1) * 64 + tx * 4), odd(tile + sub * kPos * 64 - (sub & 1) * 64 + tx * 4) {}
+// A tile of rows' pieces in shared memory, 4 L bytes a row: rows change places within groups of 32 / L by the thread along
+// time that they are of, which puts the rows that a warp's threads along time read together into different banks.
+constexpr int kTileBytes = kSplitThr * kPos * 4;
+template <int L>
+__device__ __forceinline__ int tile_row(int r) {
+  return (r ^ (r / kPos & (32 / L - 1))) * L * 4;
+}
+template <int L>
+struct RunRows {  // a thread's rows
+  static constexpr int M = 32 / L;
+  const char* p[M];
+  __device__ __forceinline__ RunRows(const char* tile, int ty, int tx) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) p[m] = tile + (ty * kPos + (m ^ (ty & (M - 1)))) * L * 4 + tx * 4;
+  }
   __device__ __forceinline__ uint32_t operator[](int u) const {
-    return *reinterpret_cast<const uint32_t*>((u & 1 ? odd : even) + u * 64);
+    return *reinterpret_cast<const uint32_t*>(p[u % M] + u / M * M * L * 4);
   }
 };
 
 // kStreams arrays' tiles, each step's asked for kStages - 1 steps ahead.  Array 1 is the gates': from the sequence's
 // length on its logits are -infinity and the others' values zero, so no position needs a look at the length.
-template <typename T, int kStreams, int kStages>
+template <typename T, int L, int kStreams, int kStages>
 struct Stages {
   static constexpr size_t kBytes = (size_t)kStages * kStreams * kTileBytes;
-  static constexpr int kRows = kTile / 64;  // a thread's rows of a tile, 64 apart
+  static constexpr int kPieces = L / 4, kApart = kSplitThr / kPieces;  // 16-byte pieces of a row; a thread's rows' distance
+  static constexpr int kRows = kTile<L> / kApart;                       // ... and number
   char* smem;                               // of this thread's first row
   const char* p[kStreams];
   int64_t row[kStreams], tile[kStreams];    // bytes from row to row, and from step to step
@@ -683,15 +712,15 @@ struct Stages {
   // First tile at t0; from step to step `by` rows on.
   __device__ __forceinline__ Stages(char* base, const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t by, int64_t len,
                                     int c0, int d) {
-    const int q = threadIdx.x % 4, r0 = threadIdx.x / 4, c = c0 + q * (16 / (int)sizeof(T));
-    smem = base + tile_row(r0) + q * 16;
+    const int q = threadIdx.x % kPieces, r0 = threadIdx.x / kPieces, c = c0 + q * (16 / (int)sizeof(T));
+    smem = base + tile_row<L>(r0) + q * 16;
     in = c < d;
     left = len - t0 - r0;
     step = by;
 #pragma unroll
     for (int k = 0; k < kStreams; ++k) {
       p[k] = reinterpret_cast<const char*>(at<T>(r[k], i, t0 + r0, c));
-      row[k] = 64 * r[k].st * (int64_t)sizeof(T);
+      row[k] = kApart * r[k].st * (int64_t)sizeof(T);
       tile[k] = by * r[k].st * (int64_t)sizeof(T);
     }
   }
@@ -700,17 +729,17 @@ struct Stages {
 #pragma unroll
     for (int k = 0; k < kStreams; ++k) {
       const char* from = p[k];
-      if (in && left > 64 * (kRows - 1)) {
+      if (in && left > kApart * (kRows - 1)) {
 #pragma unroll
-        for (int m = 0; m < kRows; ++m, from += row[k]) tc::cp_async16(to + k * kTileBytes + m * 64 * 64, from, true);
+        for (int m = 0; m < kRows; ++m, from += row[k]) tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
       } else {
         const uint32_t f = k == 1 ? shut<T>() : 0u;
 #pragma unroll
         for (int m = 0; m < kRows; ++m, from += row[k]) {
-          if (in && left > 64 * m)
-            tc::cp_async16(to + k * kTileBytes + m * 64 * 64, from, true);
+          if (in && left > kApart * m)
+            tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
           else
-            st16(to + k * kTileBytes + m * 64 * 64, make_uint4(f, f, f, f));
+            st16(to + k * kTileBytes + m * kApart * L * 4, make_uint4(f, f, f, f));
         }
       }
       p[k] += tile[k];
@@ -722,20 +751,20 @@ struct Stages {
 
 constexpr int kFwdStages = 3, kBwdStages = 4;
 
-template <typename T>
-__global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
+template <typename T, int L>
+__global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   extern __shared__ __align__(128) char smem[];
-  __shared__ SplitSmem<V> sm;
-  Split<V> sp(sm, a.status);
-  using Tiles = Stages<T, 2, kFwdStages>;
+  __shared__ SplitSmem<V, L> sm;
+  Split<V, L> sp(sm, a.status);
+  using Tiles = Stages<T, L, 2, kFwdStages>;
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
+  const int c0 = (int)(item % a.blocks) * L * V, c = c0 + tx * V;
   const bool in = c < a.d;
-  const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
-  Tiles tiles(smem, {a.x, a.g}, i, rank * kTile, CL * kTile, len, c0, a.d);
+  const int64_t len = length(a, i), steps = (len + CL * kTile<L> - 1) / (CL * kTile<L>);
+  Tiles tiles(smem, {a.x, a.g}, i, rank * kTile<L>, CL * kTile<L>, len, c0, a.d);
   auto ask = [&](int64_t s) {
     if (s < steps) tiles.ask();
     tc::cp_async_commit();
@@ -748,10 +777,10 @@ __global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
   cluster_meet();
   int stage = 0;
   for (int64_t s = 0; s < steps; ++s) {
-    const int64_t t0 = (s * CL + rank) * kTile + sub * kPos;
+    const int64_t t0 = (s * CL + rank) * kTile<L> + sub * kPos;
     const char* const tile = smem + stage * 2 * kTileBytes;
     stage = stage + 1 == kFwdStages ? 0 : stage + 1;
-    const Piece16 px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
+    const RunRows<L> px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
     Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
@@ -777,28 +806,28 @@ __global__ __launch_bounds__(256, 2) void recur_fwd_split(RecurArgs a) {
   }
   cluster_meet();
   if (!in) return;
-  for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) st4(y + t * a.y.st, all<V>(0.f));
+  for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) st4(y + t * a.y.st, all<V>(0.f));
   if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
 }
 
 // The same from the end: a run of positions maps the R that enters from the right to B + K R.  The states before each
 // thread's 16 positions are the forward's.
-template <typename T>
-__global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
+template <typename T, int L>
+__global__ __launch_bounds__(kSplitThr, 1) void recur_bwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   extern __shared__ __align__(128) char smem[];
-  __shared__ SplitSmem<V> sm;
+  __shared__ SplitSmem<V, L> sm;
   __shared__ float sh[256 * V];
-  Split<V> sp(sm, a.status);
-  using Tiles = Stages<T, 3, kBwdStages>;
+  Split<V, L> sp(sm, a.status);
+  using Tiles = Stages<T, L, 3, kBwdStages>;
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c0 = (int)(item % a.blocks) * kLanes * V, c = c0 + tx * V;
+  const int c0 = (int)(item % a.blocks) * L * V, c = c0 + tx * V;
   const bool in = c < a.d;
-  const int64_t len = length(a, i), steps = (len + CL * kTile - 1) / (CL * kTile);
-  auto start = [&](int64_t s) { return ((steps - 1 - s) * CL + rank) * kTile; };  // steps from the end
-  Tiles tiles(smem, {a.x, a.g, a.dy}, i, start(0), -CL * kTile, len, c0, a.d);
+  const int64_t len = length(a, i), steps = (len + CL * kTile<L> - 1) / (CL * kTile<L>);
+  auto start = [&](int64_t s) { return ((steps - 1 - s) * CL + rank) * kTile<L>; };  // steps from the end
+  Tiles tiles(smem, {a.x, a.g, a.dy}, i, start(0), -CL * kTile<L>, len, c0, a.d);
   auto ask = [&](int64_t s) {
     if (s < steps) tiles.ask();
     tc::cp_async_commit();
@@ -827,7 +856,7 @@ __global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
     const int left = in ? left_of(t0, len) : 0;
     const char* const tile = smem + stage * 3 * kTileBytes;
     stage = stage + 1 == kBwdStages ? 0 : stage + 1;
-    const Piece16 qx(tile, sub, tx), qg(tile + kTileBytes, sub, tx), qy(tile + 2 * kTileBytes, sub, tx);
+    const RunRows<L> qx(tile, sub, tx), qg(tile + kTileBytes, sub, tx), qy(tile + 2 * kTileBytes, sub, tx);
     Vec<V> h = ahead;
     if (s + 1 < steps) ahead = before(start(s + 1) + sub * kPos);
     Vec<V> sl[kPos], code[kPos];
@@ -859,13 +888,13 @@ __global__ __launch_bounds__(256, 1) void recur_bwd_split(RecurArgs a) {
   }
   cluster_meet();
   if (in) {
-    for (int64_t t = len + rank * kSubs + sub; t < a.T; t += CL * kSubs) {
+    for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) {
       st4(dx + t * a.dx.st, zero);
       st4(dg + t * a.dg.st, zero);
     }
     if (a.dh_in && rank == 0 && sub == 0) stf(a.dh_in + i * a.d + c, R);
   }
-  if (a.part) part_sums<V>(sum, sh, tx, sub, kLanes, kSubs, a.part + (i * CL + rank) * a.d + c, in);
+  if (a.part) part_sums<V>(sum, sh, tx, sub, L, kSubs<L>, a.part + (i * CL + rank) * a.d + c, in);
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -941,34 +970,41 @@ Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` l
 // split: 77 fp32 histories of up to 1001, d 200, forward 179 / 40 us; 400 of up to 515, d 256, 112 / 83; 1000 of 100,
 // d 128, 31 / 70; backward 82 / 68, 95 / 155, 32 / 132.  6 of 32768, d 256, by clusters of 1 to 8: 233, 135, 119, 95,
 // 83, 116, 116, 103.
-int split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
+struct SplitHow {
+  int lanes, cl;  // lanes 0: a chain a thread
+};
+SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   static const int held[2][kMaxCluster] = {{304, 152, 97, 74, 58, 46, 38, 36}, {152, 76, 46, 36, 28, 23, 15, 15}};
-  if (T <= 4 * kPos || n == 0) return 0;
-  const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, items = n * ceil_div(lanes, kLanes);
+  SplitHow how{0, 0};
+  if (T <= 4 * kPos || n == 0) return how;
+  const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
   const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
   const int64_t ctas = ceil_div(n, s.block.y) * s.across;
   double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, 304);
-  int cl = 0;
   auto waves = [](int64_t count, int c) {  // of `count` clusters at once: how long beside one CTA an SM
     const double full = count * c / 152.0;
     return full <= 1 ? 1.0 : c == 1 ? 0.4 + 0.6 * full : full;
   };
-  for (int c = 1; c <= kMaxCluster; ++c) {
-    const int h = held[back][c - 1];
-    const double step = c == 1 ? 1.75 : 2.15, w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
-    const double cost = ceil_div(T, c * kTile) * step * w + 1.5 * ceil_div(items, h);
-    if (cost < best) {
-      best = cost;
-      cl = c;
+  for (int L = 16; L >= 8; L /= 2) {
+    const int64_t items = n * ceil_div(lanes, L), tile = kSplitThr / L * kPos;
+    for (int c = 1; c <= kMaxCluster; ++c) {
+      const int h = held[back][c - 1];
+      const double step = (c == 1 ? 1.75 : 2.15) + (L == 8 ? 0.2 : 0);
+      const double w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
+      const double cost = ceil_div(T, c * tile) * step * w + 1.5 * ceil_div(items, h);
+      if (cost < best) {
+        best = cost;
+        how = {L, c};
+      }
     }
   }
-  return cl;
+  return how;
 }
 
 // Rows of partial sums of the bias's gradient.
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
-  const int cl = split_of(p, n, T, true);
-  if (cl) return n * cl;
+  const SplitHow how = split_of(p, n, T, true);
+  if (how.lanes) return n * how.cl;
   const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr);
   const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, 152 * 16 / s.across);
   return std::min(groups, most);
@@ -1007,31 +1043,43 @@ hg_status allow_smem(size_t bytes) {
   return HG_OK;
 }
 
+template <typename T, int L>
+hg_status forward_split(const RecurArgs& a, int cl, cudaStream_t s) {
+  constexpr size_t smem = Stages<T, L, 2, kFwdStages>::kBytes;
+  HG_TRY((allow_smem<recur_fwd_split<T, L>>(smem)));
+  return launch_clusters("recur_fwd_split", recur_fwd_split<T, L>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(kSplitThr),
+                         smem, s, cl, a);
+}
 template <typename T>
-hg_status forward(const RecurArgs& a, int cl, cudaStream_t s) {
-  if (cl == 0) {
+hg_status forward(RecurArgs& a, SplitHow how, cudaStream_t s) {
+  const int64_t lanes = a.d / kVec<T>;
+  if (how.lanes == 0) {
     const Shape sh = shape_of(a.d / Wide<T>::E);
     const int64_t groups = ceil_div(a.n, sh.block.y), most = std::max<int64_t>(1, 2 * 152 / sh.across);
     return launch("recur_fwd", recur_fwd<T>, dim3((unsigned)std::min(groups, most), sh.across), sh.block, 0, s, a);
   }
-  constexpr size_t smem = Stages<T, 2, kFwdStages>::kBytes;
-  HG_TRY(allow_smem<recur_fwd_split<T>>(smem));
-  return launch_clusters("recur_fwd_split", recur_fwd_split<T>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(256), smem, s,
-                         cl, a);
+  a.blocks = (int32_t)ceil_div(lanes, how.lanes);
+  return how.lanes == 16 ? forward_split<T, 16>(a, how.cl, s) : forward_split<T, 8>(a, how.cl, s);
 }
 
+template <typename T, int L>
+hg_status backward_split(const RecurArgs& a, int cl, cudaStream_t s) {
+  constexpr size_t smem = Stages<T, L, 3, kBwdStages>::kBytes;
+  HG_TRY((allow_smem<recur_bwd_split<T, L>>(smem)));
+  return launch_clusters("recur_bwd_split", recur_bwd_split<T, L>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(kSplitThr),
+                         smem, s, cl, a);
+}
 template <typename T>
-hg_status backward(const RecurArgs& a, int cl, int64_t rows, cudaStream_t s) {
-  if (cl == 0) {
-    const Shape sh = shape_of(a.d / kVec<T>, kBwdThr);
+hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
+  const int64_t lanes = a.d / kVec<T>;
+  if (how.lanes == 0) {
+    const Shape sh = shape_of(lanes, kBwdThr);
     const dim3 grid((unsigned)rows, sh.across);
     if (a.T <= kPos) return launch("recur_bwd", recur_bwd<T, false>, grid, sh.block, 0, s, a);
     return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
   }
-  constexpr size_t smem = Stages<T, 3, kBwdStages>::kBytes;
-  HG_TRY(allow_smem<recur_bwd_split<T>>(smem));
-  return launch_clusters("recur_bwd_split", recur_bwd_split<T>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(256), smem, s,
-                         cl, a);
+  a.blocks = (int32_t)ceil_div(lanes, how.lanes);
+  return how.lanes == 16 ? backward_split<T, 16>(a, how.cl, s) : backward_split<T, 8>(a, how.cl, s);
 }
 
 RecurArgs args_of(const hg_recur_params* p, int64_t n, int64_t T) {
@@ -1042,7 +1090,6 @@ RecurArgs args_of(const hg_recur_params* p, int64_t n, int64_t T) {
   a.spans = T > 0 ? (T - 1) / kPos : 0;
   a.d = p->d;
   a.status = device_status_ptr();
-  a.blocks = (int32_t)ceil_div(p->d * (int64_t)esize(p) / 4, kLanes);
   return a;
 }
 
@@ -1099,8 +1146,8 @@ extern "C" hg_status hg_recur_fwd(const hg_recur_params* params, const hg_seq* x
   a.h_out = h_out;
   a.saved = static_cast<float*>(saved);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const int cl = split_of(params, n, T, false);
-  return params->dtype == HG_BF16 ? forward<__nv_bfloat16>(a, cl, s) : forward<float>(a, cl, s);
+  const SplitHow how = split_of(params, n, T, false);
+  return params->dtype == HG_BF16 ? forward<__nv_bfloat16>(a, how, s) : forward<float>(a, how, s);
 }
 
 extern "C" hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x, const hg_seq* g, const int32_t* lens,
@@ -1155,8 +1202,8 @@ extern "C" hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x
     a.dh_out = dh_out;
     a.dh_in = dh_in;
     a.part = dbias ? static_cast<float*>(scratch) : nullptr;
-    const int cl = split_of(params, n, T, true);
-    HG_TRY(params->dtype == HG_BF16 ? backward<__nv_bfloat16>(a, cl, rows, s) : backward<float>(a, cl, rows, s));
+    const SplitHow how = split_of(params, n, T, true);
+    HG_TRY(params->dtype == HG_BF16 ? backward<__nv_bfloat16>(a, how, rows, s) : backward<float>(a, how, rows, s));
   }
   if (!dbias) return HG_OK;
   return launch("recur_bias_sum", recur_bias_sum, dim3((unsigned)ceil_div(w, 32)), dim3(1024), 0, s, a.part,
