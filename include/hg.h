@@ -720,8 +720,9 @@ hg_status hg_moe_workspace_size(const hg_moe_params* params, int64_t n, size_t* 
  * (device fp32 [n][top_k]) receive e_j and w_j (-1 and 0 for a row that is not live); NULL = not wanted.  No output
  * overlaps another array.  The choice is that of logits without rounding (sums of two fp32 numbers, within d 2^-48 of
  * the sum of their terms' sizes); a NaN counts as the largest logit, and an infinite one has the weights that the
- * formula gives it (NaN).  Sums are fp32 in an order fixed by the choice; bf16: the hidden rows are rounded to bf16
- * once, between the products, and Y once.  An infinity or NaN stays in its own row.  Weights of experts that no row
+ * formula gives it (NaN).  Sums are fp32 in an order fixed by the choice; bf16: the hidden rows enter the second
+ * product as sums of two bf16 numbers (16 bits; an infinity among them becomes NaN), Y is rounded once.  An infinity or
+ * NaN stays in its own row.  Weights of experts that no row
  * chooses are not read. */
 hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, const int32_t* live, int64_t n, void* Y,
                      int32_t* experts, float* weights, void* scratch, hg_stream stream);

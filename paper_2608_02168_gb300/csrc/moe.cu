@@ -198,12 +198,14 @@ struct MoeCfg {
   static constexpr int XS = sizeof(T) == 2 ? D : D + 4;    // values between two rows of X, and of H (fp32: padded)
   static constexpr int HS = sizeof(T) == 2 ? FC : FC + 4;
   static constexpr int kX = kGroup * XS * (int)sizeof(T);
-  static constexpr int kH = kGroup * HS * (int)sizeof(T);  // of one of two places
+  // H of one of two places; bf16: the rounded rows, then what they lost.  fp32: and 8 KB for the parts of its sums.
+  static constexpr int kTerm = kGroup * HS * (int)sizeof(T), kH = sizeof(T) == 2 ? 2 * kTerm : kTerm;
+  static constexpr int kRed = sizeof(T) == 2 ? 0 : 16 * 4 * 16 * 8;
   static_assert(2 * kH >= kMaxTop * D * 4, "a row's experts' sums have the same place");
   static constexpr int kIdx = kMaxRows * kMaxTop * 2;
-  static constexpr int kFit = (222 * 1024 - kX - 2 * kH - kIdx) / kStage;
+  static constexpr int kFit = (222 * 1024 - kX - 2 * kH - kIdx - kRed) / kStage;
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr size_t kSmem = (size_t)kStages * kStage + kX + 2 * kH + kIdx;
+  static constexpr size_t kSmem = (size_t)kStages * kStage + kX + 2 * kH + kIdx + kRed;
 };
 
 // Byte offset of piece c of row r, N pieces a row, such that eight rows' pieces lie in different banks (N = 4: as the
@@ -254,7 +256,8 @@ struct Sums<__nv_bfloat16, D, kAct> {
         for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
   }
   // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments, two tiles
-  // the weights'.  H is rounded to bf16 once, the operand of the next product.
+  // the weights'.  H is kept as a sum of two bf16 numbers (16 bits), the operands of the next product: rounded once to 8
+  // bits it would add 1.8e-3 of a row to the 1.7e-3 of Y's own rounding, and the product is not what takes the time.
   template <int NR>
   __device__ __forceinline__ void hidden_of(const char* st, const char* X, char* H, int rt) {
     const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4;
@@ -276,20 +279,23 @@ struct Sums<__nv_bfloat16, D, kAct> {
     for (int i = 0; i < NR; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t v =
-            pack2_bf16(gate<kAct>(g[i][2 * h]) * u[i][2 * h], gate<kAct>(g[i][2 * h + 1]) * u[i][2 * h + 1]);
-        *reinterpret_cast<uint32_t*>(H + place16<4>((rt + 2 * i) * 16 + lane / 4 + 8 * h, ft) + lane % 4 * 4) = v;
+        const float a = gate<kAct>(g[i][2 * h]) * u[i][2 * h], c = gate<kAct>(g[i][2 * h + 1]) * u[i][2 * h + 1];
+        const uint32_t v = pack2_bf16(a, c);
+        char* to = H + place16<4>((rt + 2 * i) * 16 + lane / 4 + 8 * h, ft) + lane % 4 * 4;
+        *reinterpret_cast<uint32_t*>(to) = v;
+        *reinterpret_cast<uint32_t*>(to + C::kTerm) =
+            pack2_bf16(a - __uint_as_float(v << 16), c - __uint_as_float(v & 0xFFFF0000u));
       }
   }
-  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
-    const int half = threadIdx.x / 128;
+  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int rows, float2*) {
+    const int half = threadIdx.x / 128, tiles = (rows + 15) / 16;
     if (half + 2 < tiles)
       hidden_of<2>(st, X, H, half);
     else if (half < tiles)
       hidden_of<1>(st, X, H, half);
   }
-  __device__ __forceinline__ void out(const char* st, const char* H, int tiles) {
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  __device__ __forceinline__ void out(const char* st, const char* H, int rows) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, tiles = (rows + 15) / 16;
     const uint32_t w = tc::smem_u32(st) + 2 * C::kGate, ha = tc::smem_u32(H);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
@@ -300,8 +306,11 @@ struct Sums<__nv_bfloat16, D, kAct> {
 #pragma unroll
       for (int rt = 0; rt < kGroup / 16; ++rt) {
         if (rt >= tiles) break;
-        uint32_t h[4];
+        uint32_t h[4], l[4];
         ldsm4(ha + place16<4>(rt * 16 + lane % 16, ks * 2 + lane / 16), h);
+        ldsm4(ha + C::kTerm + place16<4>(rt * 16 + lane % 16, ks * 2 + lane / 16), l);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma(acc[rt][j], l, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
 #pragma unroll
         for (int j = 0; j < NT; ++j) mma(acc[rt][j], h, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
       }
@@ -335,34 +344,48 @@ struct Sums<float, D, kAct> {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
   }
-  // A thread has one feature of the rows t / 16 + 16 i.
-  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int tiles) {
-    const int ft = threadIdx.x % 16, r0 = threadIdx.x / 16;
+  // Sixteen rows at a time.  A thread has one feature of four rows and a share of the sum, which is the finer the fewer
+  // rows there are (1, 2 or 4 times four rows: a 16th, an 8th or a 4th); the shares are added in shared memory.
+  __device__ __forceinline__ void hidden(const char* st, const char* X, char* H, int rows, float2* red) {
+    const int ft = threadIdx.x % 16, of = threadIdx.x / 16;
     const float *wg = reinterpret_cast<const float*>(st) + ft, *wu = wg + C::kGate / 4;
-    const float* x = reinterpret_cast<const float*>(X) + r0 * C::XS;
-    float* h = reinterpret_cast<float*>(H) + r0 * C::HS + ft;
-    float g[4] = {}, u[4] = {};
+#pragma unroll 1
+    for (int t0 = 0; t0 < rows; t0 += 16) {
+      const int left = rows - t0, blocks = left <= 4 ? 1 : left <= 8 ? 2 : 4, shares = 16 / blocks;
+      const float* x = reinterpret_cast<const float*>(X) + (t0 + of % blocks * 4) * C::XS;
+      float g[4] = {}, u[4] = {};
 #pragma unroll 2
-    for (int k = 0; k < D; k += 4) {
-      float a[4], b[4];
+      for (int k = of / blocks * 4; k < D; k += shares * 4) {
+        float a[4], b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        a[i] = wg[(k + i) * 16];
-        b[i] = wu[(k + i) * 16];
+        for (int i = 0; i < 4; ++i) {
+          a[i] = wg[(k + i) * 16];
+          b[i] = wu[(k + i) * 16];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 v = *reinterpret_cast<const float4*>(x + r * C::XS + k);
+          g[r] = fmaf(v.x, a[0], fmaf(v.y, a[1], fmaf(v.z, a[2], fmaf(v.w, a[3], g[r]))));
+          u[r] = fmaf(v.x, b[0], fmaf(v.y, b[1], fmaf(v.z, b[2], fmaf(v.w, b[3], u[r]))));
+        }
       }
+      if (t0 > 0) __syncthreads();  // the parts of the rows before have been added
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t >= tiles) break;
-        const float4 v = *reinterpret_cast<const float4*>(x + t * 16 * C::XS + k);
-        g[t] = fmaf(v.x, a[0], fmaf(v.y, a[1], fmaf(v.z, a[2], fmaf(v.w, a[3], g[t]))));
-        u[t] = fmaf(v.x, b[0], fmaf(v.y, b[1], fmaf(v.z, b[2], fmaf(v.w, b[3], u[t]))));
+      for (int r = 0; r < 4; ++r) red[(of * 4 + r) * 16 + ft] = make_float2(g[r], u[r]);
+      __syncthreads();
+      if (of < 4 * blocks) {  // row `of` of the sixteen
+        float2 s = make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (int q = 0; q < shares; ++q) {
+          const float2 p = red[((q * blocks + of / 4) * 4 + of % 4) * 16 + ft];
+          s.x += p.x;
+          s.y += p.y;
+        }
+        reinterpret_cast<float*>(H)[(t0 + of) * C::HS + ft] = gate<kAct>(s.x) * s.y;
       }
     }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (t < tiles) h[t * 16 * C::HS] = gate<kAct>(g[t]) * u[t];
   }
-  __device__ __forceinline__ void out(const char* st, const char* H, int tiles) {
+  __device__ __forceinline__ void out(const char* st, const char* H, int rows) {
     const int c = threadIdx.x % D, r0 = threadIdx.x / D;
     const float* w = reinterpret_cast<const float*>(st + 2 * C::kGate) + c;
     const float* h = reinterpret_cast<const float*>(H) + r0 * C::HS;
@@ -370,13 +393,10 @@ struct Sums<float, D, kAct> {
     for (int k = 0; k < 16; k += 4) {
       const float w0 = w[k * D], w1 = w[(k + 1) * D], w2 = w[(k + 2) * D], w3 = w[(k + 3) * D];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t >= tiles) break;
-#pragma unroll
-        for (int i = t * kPer / 4; i < (t + 1) * kPer / 4; ++i) {
-          const float4 v = *reinterpret_cast<const float4*>(h + i * kCols * C::HS + k);
-          acc[i] = fmaf(v.x, w0, fmaf(v.y, w1, fmaf(v.z, w2, fmaf(v.w, w3, acc[i]))));
-        }
+      for (int i = 0; i < kPer; ++i) {
+        if (i % 4 == 0 && i * kCols >= rows) break;
+        const float4 v = *reinterpret_cast<const float4*>(h + i * kCols * C::HS + k);
+        acc[i] = fmaf(v.x, w0, fmaf(v.y, w1, fmaf(v.z, w2, fmaf(v.w, w3, acc[i]))));
       }
     }
   }
@@ -453,6 +473,7 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
   char* const X = smem + C::kStages * C::kStage;
   char* const H = X + C::kX;
   uint16_t* const idx = reinterpret_cast<uint16_t*>(H + 2 * C::kH);
+  float2* const red = reinterpret_cast<float2*>(H + 2 * C::kH + C::kIdx);
   __shared__ int count[kMaxExperts];      // rows of an expert
   __shared__ int first[kMaxExperts + 1];  // its first pass
   __shared__ uint8_t expert[kMaxPasses];  // of a pass
@@ -595,13 +616,13 @@ __global__ __launch_bounds__(kThr, 1) void moe_experts(MoeArgs a, const __grid_c
     const char* st = smem + stage * C::kStage;
     char* const h = H + at % 2 * C::kH;
     const bool here = tc::mbar_wait(&full[stage], at / C::kStages & 1);
-    sums.hidden(st, X, h, tiles);
+    sums.hidden(st, X, h, rows, red);
     if (__syncthreads_or(!here)) {  // H is there, and nobody reads the chunk before any more
       gave_up = true;
       break;
     }
     if (tid == 0 && at > 0) load();
-    sums.out(st, h, tiles);
+    sums.out(st, h, rows);
     const At was = now;
     if (item + 1 < hi) next(now);
     if (item + 1 < hi && now.chunk != 0) continue;

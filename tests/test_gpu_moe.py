@@ -3,7 +3,7 @@
 Choices are equal.  Weights: within (264 + 2 |l - l_max|) steps 2^-24 of themselves (exponential, sum of up to 256, quotient;
 the differences of logits are exact to a step).  Rows, with u = half a step of the storage type and s = 2^-24:
   u |want| + r A + e B,  A = the sum of |w H W_down|, B = the same with G and U by their terms' absolute values, + |x|;
-r = u in bf16 (the hidden rows rounded once), 0 in fp32; e = (3 (d + f + 40) + 4 top + 60) s: the gated block's bound
+r = 2^-16 in bf16 (the hidden rows as sums of two bf16 numbers), 0 in fp32; e = (3 (d + f + 40) + 4 top + 60) s: the gated block's bound
 (test_gpu_history.py), the weights, and the sum over a row's experts.
 """
 from fractions import Fraction
@@ -46,7 +46,7 @@ def check(dt, got, x, ws, top, act, res, renorm, live=None):
     far = l.max(-1, keepdims=True) - np.take_along_axis(l, np.maximum(idx, 0), 1)
     near(w, wt, wt, (0, (264 + 2 * far.max(initial=0)) * F32), "weights")
     e = (3 * (d + f + 40) + 4 * top + 60) * F32
-    r = U["bf16"] if dt == "bf16" else 0
+    r = 2.0**-16 if dt == "bf16" else 0
     near(Y, want, (r * rounded + e * terms) / max(r + e, 1e-30), (U[dt], r + e), "Y")
 
 
