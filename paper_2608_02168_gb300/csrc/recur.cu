@@ -703,48 +703,44 @@ struct Stages {
   static constexpr size_t kBytes = (size_t)kStages * kStreams * kTileBytes;
   static constexpr int kPieces = L / 4, kApart = kSplitThr / kPieces;  // 16-byte pieces of a row; a thread's rows' distance
   static constexpr int kRows = kTile<L> / kApart;                       // ... and number
-  char* smem;                               // of this thread's first row
-  const char* p[kStreams];
-  int64_t row[kStreams], tile[kStreams];    // bytes from row to row, and from step to step
-  int64_t left, step;                       // rows in use from this thread's first one on, and their change
+  char* smem;               // of this thread's first row
+  const char* p[kStreams];  // its row of the next tile
+  int64_t left;             // rows in use from that row on
   int stage = 0;
   bool in;
-  // First tile at t0; from step to step `by` rows on.
-  __device__ __forceinline__ Stages(char* base, const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t by, int64_t len,
-                                    int c0, int d) {
-    const int q = threadIdx.x % kPieces, r0 = threadIdx.x / kPieces, c = c0 + q * (16 / (int)sizeof(T));
-    smem = base + tile_row<L>(r0) + q * 16;
+  __device__ __forceinline__ explicit Stages(char* base)
+      : smem(base + tile_row<L>(threadIdx.x / kPieces) + threadIdx.x % kPieces * 16) {}
+  // A sequence's tiles begin at t0.
+  __device__ __forceinline__ void begin(const Rows (&r)[kStreams], int64_t i, int64_t t0, int64_t len, int c0, int d) {
+    const int r0 = threadIdx.x / kPieces, c = c0 + threadIdx.x % kPieces * (16 / (int)sizeof(T));
     in = c < d;
     left = len - t0 - r0;
-    step = by;
 #pragma unroll
-    for (int k = 0; k < kStreams; ++k) {
-      p[k] = reinterpret_cast<const char*>(at<T>(r[k], i, t0 + r0, c));
-      row[k] = kApart * r[k].st * (int64_t)sizeof(T);
-      tile[k] = by * r[k].st * (int64_t)sizeof(T);
-    }
+    for (int k = 0; k < kStreams; ++k) p[k] = reinterpret_cast<const char*>(at<T>(r[k], i, t0 + r0, c));
   }
-  __device__ __forceinline__ void ask() {
+  // The next tile of each array, `by` rows before the one after it.
+  __device__ __forceinline__ void ask(const Rows (&rows)[kStreams], int64_t by) {
     char* const to = smem + stage * kStreams * kTileBytes;
 #pragma unroll
     for (int k = 0; k < kStreams; ++k) {
       const char* from = p[k];
+      const int64_t row = kApart * rows[k].st * (int64_t)sizeof(T);
       if (in && left > kApart * (kRows - 1)) {
 #pragma unroll
-        for (int m = 0; m < kRows; ++m, from += row[k]) tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
+        for (int m = 0; m < kRows; ++m, from += row) tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
       } else {
         const uint32_t f = k == 1 ? shut<T>() : 0u;
 #pragma unroll
-        for (int m = 0; m < kRows; ++m, from += row[k]) {
+        for (int m = 0; m < kRows; ++m, from += row) {
           if (in && left > kApart * m)
             tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
           else
             st16(to + k * kTileBytes + m * kApart * L * 4, make_uint4(f, f, f, f));
         }
       }
-      p[k] += tile[k];
+      p[k] += by * rows[k].st * (int64_t)sizeof(T);
     }
-    left -= step;
+    left -= by;
     stage = stage + 1 == kStages ? 0 : stage + 1;
   }
 };
@@ -758,56 +754,92 @@ __global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
   extern __shared__ __align__(128) char smem[];
   __shared__ SplitSmem<V, L> sm;
   Split<V, L> sp(sm, a.status);
-  using Tiles = Stages<T, L, 2, kFwdStages>;
+  const Rows in_rows[2] = {a.x, a.g};
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
-  const int64_t item = blockIdx.x / CL, i = item / a.blocks;
-  const int c0 = (int)(item % a.blocks) * L * V, c = c0 + tx * V;
-  const bool in = c < a.d;
-  const int64_t len = length(a, i), steps = (len + CL * kTile<L> - 1) / (CL * kTile<L>);
-  Tiles tiles(smem, {a.x, a.g}, i, rank * kTile<L>, CL * kTile<L>, len, c0, a.d);
-  auto ask = [&](int64_t s) {
-    if (s < steps) tiles.ask();
+  const int items = (int)(a.n * a.blocks), stride = gridDim.x / CL, first = blockIdx.x / CL;
+  auto steps_of = [&](int64_t len) { return (int)((len + CL * kTile<L> - 1) / (CL * kTile<L>)); };
+  // The loads run ahead from piece to piece; a piece's length, bias and state are asked for a piece ahead.
+  Stages<T, L, 2, kFwdStages> tiles(smem);
+  int l_item = first, l_steps = 0;
+  auto begin = [&]() {
+    const int64_t i = l_item / a.blocks, len = length(a, i);
+    l_steps = steps_of(len);
+    tiles.begin(in_rows, i, rank * kTile<L>, len, l_item % a.blocks * L * V, a.d);
+  };
+  if (l_item < items) begin();
+  auto ask = [&]() {
+    while (l_steps == 0 && l_item < items) {
+      l_item += stride;
+      if (l_item < items) begin();
+    }
+    if (l_item < items) {
+      tiles.ask(in_rows, CL * kTile<L>);
+      --l_steps;
+    }
     tc::cp_async_commit();
   };
-  for (int s = 0; s < kFwdStages - 1; ++s) ask(s);
-  T* y = at_out<T>(a.y, i, 0, c);
-  const Vec<V> b = in ? bias_of<T>(a, c) : all<V>(0.f);
-  Vec<V> h = in ? state_of<V>(a.h_in, a, i, c) : all<V>(0.f);
+  int64_t next_len = 0;
+  Vec<V> next_b = all<V>(0.f), next_h = next_b;
+  auto fetch = [&](int item) {
+    if (item >= items) return;
+    const int64_t i = item / a.blocks;
+    const int c = item % a.blocks * L * V + tx * V;
+    next_len = length(a, i);
+    if (c >= a.d) return;
+    next_b = bias_of<T>(a, c);
+    next_h = state_of<V>(a.h_in, a, i, c);
+  };
+  fetch(first);
+#pragma unroll 1
+  for (int s = 0; s < kFwdStages - 1; ++s) ask();
   tc::cp_async_wait<kFwdStages - 2>();
   cluster_meet();
-  int stage = 0;
-  for (int64_t s = 0; s < steps; ++s) {
-    const int64_t t0 = (s * CL + rank) * kTile<L> + sub * kPos;
-    const char* const tile = smem + stage * 2 * kTileBytes;
-    stage = stage + 1 == kFwdStages ? 0 : stage + 1;
-    const RunRows<L> px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
-    Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
+  int stage = 0, buf = 0;
+#pragma unroll 1
+  for (int item = first; item < items; item += stride) {
+    const int64_t i = item / a.blocks, len = next_len;
+    const int c = item % a.blocks * L * V + tx * V, steps = steps_of(len);
+    const bool in = c < a.d;
+    T* const y = at_out<T>(a.y, i, 0, c);
+    const Vec<V> b = next_b;
+    Vec<V> h = next_h;
+    fetch(item + stride);
+#pragma unroll 1
+    for (int s = 0; s < steps; ++s, buf ^= 1) {
+      const int64_t t0 = ((int64_t)s * CL + rank) * kTile<L> + sub * kPos;
+      const char* const tile = smem + stage * 2 * kTileBytes;
+      stage = stage + 1 == kFwdStages ? 0 : stage + 1;
+      const RunRows<L> px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
+      Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
-    for (int u = 0; u < kPos; ++u) {
-      const GateOf<T> gt(piece(pg[u], T{}), b);
-      const Vec<V> k = gt.k();
-      now.B = fma(k, now.B, mul(gt.z(), piece(px[u], T{})));
-      now.K = mul(now.K, k);
-      run[u] = now;
+      for (int u = 0; u < kPos; ++u) {
+        const GateOf<T> gt(piece(pg[u], T{}), b);
+        const Vec<V> k = gt.k();
+        now.B = fma(k, now.B, mul(gt.z(), piece(px[u], T{})));
+        now.K = mul(now.K, k);
+        run[u] = now;
+      }
+      tc::cp_async_wait<kFwdStages - 3>();
+      const Vec<V> h0 = sp.template enter<false>(now, h, buf, ask);
+      const int left = in ? left_of(t0, len) : 0;
+      if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
+      T* py = y + t0 * a.y.st;
+      if (left == kPos) {
+#pragma unroll
+        for (int u = 0; u < kPos; ++u, py += a.y.st) st4(py, fma(run[u].K, h0, run[u].B));
+      } else {
+#pragma unroll
+        for (int u = 0; u < kPos; ++u, py += a.y.st)
+          if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
+      }
     }
-    tc::cp_async_wait<kFwdStages - 3>();
-    const Vec<V> h0 = sp.template enter<false>(now, h, s & 1, [&] { ask(s + kFwdStages - 1); });
-    const int left = in ? left_of(t0, len) : 0;
-    if (a.saved && t0 > 0 && left > 0) stf(kept(a, i, t0, c), h0);
-    T* py = y + t0 * a.y.st;
-    if (left == kPos) {
-#pragma unroll
-      for (int u = 0; u < kPos; ++u, py += a.y.st) st4(py, fma(run[u].K, h0, run[u].B));
-    } else {
-#pragma unroll
-      for (int u = 0; u < kPos; ++u, py += a.y.st)
-        if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
-    }
+    if (!in) continue;
+#pragma unroll 1
+    for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) st4(y + t * a.y.st, all<V>(0.f));
+    if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
   }
+  __syncwarp();
   cluster_meet();
-  if (!in) return;
-  for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) st4(y + t * a.y.st, all<V>(0.f));
-  if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
 }
 
 // The same from the end: a run of positions maps the R that enters from the right to B + K R.  The states before each
@@ -820,16 +852,17 @@ __global__ __launch_bounds__(kSplitThr, 1) void recur_bwd_split(RecurArgs a) {
   __shared__ SplitSmem<V, L> sm;
   __shared__ float sh[256 * V];
   Split<V, L> sp(sm, a.status);
-  using Tiles = Stages<T, L, 3, kBwdStages>;
+  const Rows in_rows[3] = {a.x, a.g, a.dy};
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
   const int c0 = (int)(item % a.blocks) * L * V, c = c0 + tx * V;
   const bool in = c < a.d;
   const int64_t len = length(a, i), steps = (len + CL * kTile<L> - 1) / (CL * kTile<L>);
   auto start = [&](int64_t s) { return ((steps - 1 - s) * CL + rank) * kTile<L>; };  // steps from the end
-  Tiles tiles(smem, {a.x, a.g, a.dy}, i, start(0), -CL * kTile<L>, len, c0, a.d);
+  Stages<T, L, 3, kBwdStages> tiles(smem);
+  tiles.begin(in_rows, i, start(0), len, c0, a.d);
   auto ask = [&](int64_t s) {
-    if (s < steps) tiles.ask();
+    if (s < steps) tiles.ask(in_rows, -CL * kTile<L>);
     tc::cp_async_commit();
   };
   const Vec<V> zero = all<V>(0.f);
@@ -971,11 +1004,11 @@ Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` l
 // d 128, 31 / 70; backward 82 / 68, 95 / 155, 32 / 132.  6 of 32768, d 256, by clusters of 1 to 8: 233, 135, 119, 95,
 // 83, 116, 116, 103.
 struct SplitHow {
-  int lanes, cl;  // lanes 0: a chain a thread
+  int lanes, cl, held;  // lanes 0: a chain a thread
 };
 SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   static const int held[2][kMaxCluster] = {{304, 152, 97, 74, 58, 46, 38, 36}, {152, 76, 46, 36, 28, 23, 15, 15}};
-  SplitHow how{0, 0};
+  SplitHow how{0, 0, 0};
   if (T <= 4 * kPos || n == 0) return how;
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
   const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
@@ -987,14 +1020,15 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   };
   for (int L = 16; L >= 8; L /= 2) {
     const int64_t items = n * ceil_div(lanes, L), tile = kSplitThr / L * kPos;
+    if (items >= int64_t(1) << 28) break;
     for (int c = 1; c <= kMaxCluster; ++c) {
       const int h = held[back][c - 1];
       const double step = (c == 1 ? 1.75 : 2.15) + (L == 8 ? 0.2 : 0);
       const double w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
-      const double cost = ceil_div(T, c * tile) * step * w + 1.5 * ceil_div(items, h);
+      const double cost = ceil_div(T, c * tile) * step * w + (back ? 1.5 : 0.5) * ceil_div(items, h);
       if (cost < best) {
         best = cost;
-        how = {L, c};
+        how = {L, c, h};
       }
     }
   }
@@ -1044,10 +1078,11 @@ hg_status allow_smem(size_t bytes) {
 }
 
 template <typename T, int L>
-hg_status forward_split(const RecurArgs& a, int cl, cudaStream_t s) {
+hg_status forward_split(const RecurArgs& a, int cl, int held, cudaStream_t s) {
   constexpr size_t smem = Stages<T, L, 2, kFwdStages>::kBytes;
   HG_TRY((allow_smem<recur_fwd_split<T, L>>(smem)));
-  return launch_clusters("recur_fwd_split", recur_fwd_split<T, L>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(kSplitThr),
+  return launch_clusters("recur_fwd_split", recur_fwd_split<T, L>,
+                         dim3((unsigned)(std::min<int64_t>(a.n * a.blocks, held) * cl)), dim3(kSplitThr),
                          smem, s, cl, a);
 }
 template <typename T>
@@ -1059,7 +1094,7 @@ hg_status forward(RecurArgs& a, SplitHow how, cudaStream_t s) {
     return launch("recur_fwd", recur_fwd<T>, dim3((unsigned)std::min(groups, most), sh.across), sh.block, 0, s, a);
   }
   a.blocks = (int32_t)ceil_div(lanes, how.lanes);
-  return how.lanes == 16 ? forward_split<T, 16>(a, how.cl, s) : forward_split<T, 8>(a, how.cl, s);
+  return how.lanes == 16 ? forward_split<T, 16>(a, how.cl, how.held, s) : forward_split<T, 8>(a, how.cl, how.held, s);
 }
 
 template <typename T, int L>
