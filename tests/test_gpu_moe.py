@@ -58,7 +58,10 @@ CASES = [(1, 1, 1, 64, 8, "silu", False, True, False), (1, 16, 2, 128, 384, "sil
          (64, 64, 2, 256, 104, "silu", True, True, False), (100, 5, 4, 128, 136, "silu", False, False, True),
          (200, 2, 2, 64, 24, "silu", True, True, False), (300, 32, 4, 256, 88, "silu", True, False, True),
          (130, 256, 8, 64, 16, "relu", False, True, False), (1024, 7, 3, 64, 56, "silu", True, True, True),
-         (1000, 129, 8, 128, 32, "silu", False, False, False), (65, 1, 1, 256, 520, "silu", True, True, False)]
+         (1000, 129, 8, 128, 32, "silu", False, False, False), (65, 1, 1, 256, 520, "silu", True, True, False),
+         (4, 2, 2, 256, 136, "silu", True, True, True), (4, 9, 8, 64, 24, "gelu_tanh", False, False, False),
+         (5, 2, 2, 256, 136, "silu", True, True, True), (64, 1, 1, 128, 40, "none", False, False, False),
+         (128, 2, 2, 128, 264, "silu", False, True, False), (1024, 256, 8, 256, 8, "silu", True, False, True)]
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -279,3 +282,36 @@ def test_the_layer_is_the_blocks_on_each_experts_rows(dt):
     e = (3 * (d + f + 40) + 4 * top + 60) * F32
     r = U["bf16"] if dt == "bf16" else 0
     near(Y, host(total), 2 * (r * rounded + e * terms) + U[dt] * rounded, (U[dt], 1.0), "Y")
+
+
+def test_streams_given_and_two_calls_at_once():
+    need_gpu()
+    hg = lib()
+    td, n, E, d, f = torch.bfloat16, 90, 12, 128, 264
+    x, *ws = problem("bf16", n, E, d, f, 13)
+    p, X = hg.MoeParams(*(dev(w, td) for w in ws), 3), dev(x, td)
+    ref = call(hg, p, X)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    work = [torch.empty(hg.hg_moe_workspace_size(p, n), dtype=torch.uint8, device="cuda") for _ in streams]
+    out = [[nans(X.shape, td), torch.zeros_like(ref[1]), nans(ref[2].shape, torch.float32)] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, w, o in zip(streams, work, out):
+            hg.hg_moe_fwd(p, X, None, *o, w, stream=s)
+    for s, o in zip(streams, out):
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o, ref))
+    assert hg.hg_device_status() == 0
+
+
+def test_updated_weights_are_seen():
+    need_gpu()
+    hg = lib()
+    x, *ws = problem("f32", 9, 4, 64, 40, 14)
+    W = [dev(w) for w in ws]
+    p, X = hg.MoeParams(*W, 2), dev(x)
+    call(hg, p, X)
+    for w in W:
+        w.mul_(-0.5)
+    check("f32", call(hg, p, X), x, [w.cpu().numpy() for w in W], 2, "silu", False, True)

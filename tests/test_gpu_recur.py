@@ -338,3 +338,89 @@ def test_updated_bias_is_seen():
     hg.hg_recur_fwd(p, dev(x), dev(g), None, None, y, None, None)
     want, _, _, most = OR.forward(f64(x), f64(g), f64(B.cpu().numpy()), None, None)
     near(y, want, np.broadcast_to(most[:, None], want.shape), (F32, 118 * F32), "y")
+
+
+@pytest.mark.parametrize("n,T,d", [(40, 12, 64), (300, 70, 64), (3, 900, 40)])
+def test_infinite_biases(n, T, d):
+    """A channel that always takes its input and one that never does, with ragged histories."""
+    need_gpu()
+    hg = lib()
+    x, g, dy, _, lens, h, dh = problem("f32", n, T, d, 13, True, True)
+    b = np.zeros(d, np.float32)
+    b[1], b[2] = np.inf, -np.inf
+    L = dev(lens)
+    o = run(hg, hg.RecurParams(dev(b)), torch.float32, dev(x), dev(g), L, dev(h), dev(dy), dev(dh), n, T, d)
+    live = torch.arange(T, device="cuda") < L[:, None]
+    X, H = dev(x), dev(h)
+    assert torch.equal(o["y"][..., 1], X[..., 1] * live) and torch.equal(o["y"][..., 2], H[:, None, 2] * live)
+    at = (L.long() - 1).clamp(min=0)[:, None]
+    assert torch.equal(o["h"][:, 1], torch.where(L > 0, X[..., 1].gather(1, at)[:, 0], H[:, 1]))
+    assert torch.equal(o["h"][:, 2], H[:, 2])
+    assert (o["dg"][..., 1:3] == 0).all() and (o["dx"][..., 2] == 0).all() and (o["db"][1:3] == 0).all()
+    keep = np.ones(d, bool)
+    keep[1:3] = False
+    some = {k: v[..., keep].contiguous() for k, v in o.items()}
+    check(some, "f32", x[..., keep], g[..., keep], dy[..., keep], b[keep], lens, h[:, keep], dh[:, keep])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_very_long_history_and_very_many_short_ones(dt):
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    x, g, dy, b, _, h, dh = problem(dt, 1, 100_003, 8, 14, False, True)
+    o = run(hg, params(hg, b, 8, td), td, dev(x, td), dev(g, td), None, dev(h), dev(dy, td), dev(dh), 1, 100_003, 8)
+    check(o, dt, x, g, dy, b, None, h, dh)
+    n = 2_000_003
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    X, G = (torch.randn(n, 2, 8, device="cuda", generator=gen).to(td) for _ in range(2))
+    lens = torch.randint(0, 3, (n,), device="cuda", generator=gen).to(torch.int32)
+    y, last = nans((n, 2, 8), td), nans((n, 8), torch.float32)
+    hg.hg_recur_fwd(params(hg, None, 8, td), X, G, lens, None, y, last, None)
+    z = torch.sigmoid(G.double())
+    h0 = z[:, 0] * X[:, 0].double() * (lens > 0)[:, None]
+    h1 = torch.where((lens > 1)[:, None], h0 + z[:, 1] * (X[:, 1].double() - h0), h0)
+    most = X.double().abs().amax((1, 2))[:, None]
+    assert ((last.double() - h1).abs() <= (2 * 2 + 100) * F32 * most).all()
+    want = torch.stack([h0, h1 * (lens > 1)[:, None]], 1)
+    assert ((y.double() - want).abs() <= U[dt] * want.abs() + (2 * 2 + 100) * F32 * most[:, None]).all()
+
+
+def test_chains_with_offsets_past_32_bits():
+    need_gpu()
+    hg = lib()
+    td, T, d = torch.bfloat16, 20, 64
+    far = (1 << 32) + 64
+    x, g, dy, b, _, h, dh = problem("bf16", 2, T, d, 15, False, True)
+    big = torch.empty(far + 6 * T * d, dtype=td, device="cuda")
+    at = lambda k: torch.as_strided(big, (2, T, d), (far, d, 1), k * T * d)  # noqa: E731
+    X, G, DY, y, dx, dg = (at(k) for k in range(6))
+    for view, v in ((X, x), (G, g), (DY, dy)):
+        view.copy_(dev(v, td))
+    p = params(hg, b, d, td)
+    o = run(hg, p, td, X, G, None, dev(h), DY, dev(dh), 2, T, d, {"y": y, "dx": dx, "dg": dg})
+    ref = run(hg, p, td, dev(x, td), dev(g, td), None, dev(h), dev(dy, td), dev(dh), 2, T, d)
+    assert all(torch.equal(o[k], ref[k]) for k in ref)
+
+
+def test_streams_given_and_two_calls_at_once():
+    """The call's stream is the one given, not the current one; calls on two streams do not meet."""
+    need_gpu()
+    hg = lib()
+    td, n, T, d = torch.bfloat16, 3, 5000, 64
+    x, g, dy, b, lens, h, dh = problem("bf16", n, T, d, 16, True, True)
+    p = params(hg, b, d, td)
+    X, G, L, H = dev(x, td), dev(g, td), dev(lens), dev(h)
+    ref, last = nans((n, T, d), td), nans((n, d), torch.float32)
+    hg.hg_recur_fwd(p, X, G, L, H, ref, last, None)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    out = [[nans((n, T, d), td), nans((n, d), torch.float32)] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, (y, e) in zip(streams, out):
+            hg.hg_recur_fwd(p, X, G, L, H, y, e, None, stream=s)
+    for s, (y, e) in zip(streams, out):
+        s.synchronize()
+        assert torch.equal(y, ref) and torch.equal(e, last)
+    assert hg.hg_device_status() == 0
