@@ -492,7 +492,8 @@ __global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
 // a chain split over time
 // ------------------------------------------------------------------------------------------------------------
 // A cluster of CL CTAs takes a piece of a sequence's rows (L lanes of 4 bytes) through CL tiles of positions a step: 64
-// bytes and 256 positions a tile, or, where even eight CTAs a piece leave SMs idle, 32 bytes and 512.  A thread has 16
+// bytes and 256 positions a tile; where even eight CTAs a piece leave SMs idle, 32 bytes and 512; in the backward, whose
+// three arrays in and two out touch half as many lines so, mostly 128 bytes and 128 positions.  A thread has 16
 // positions of 4 bytes.  Positions compose: a run of them maps the state h before it to B + K h, B its end from a zero
 // state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).  Threads form
 // the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to the cluster's
@@ -511,7 +512,9 @@ template <int V>
 struct alignas(8 * V) Pair {  // as it lies in shared memory
   float K[V], B[V];
 };
-constexpr int kJoin = 16;  // runs that a lane joins one after another; with twice as many, two lanes do, and join theirs
+// Runs that a lane joins one after another; of 32, two lanes join sixteen each, and then theirs.
+template <int L>
+constexpr int kJoin = kSubs<L> < 16 ? kSubs<L> : 16;
 template <int V, int L>
 struct SplitSmem {
   Pair<V> run[2][kSubs<L>][L];  // the threads' runs, then what is before each among its sixteen
@@ -607,8 +610,8 @@ struct Split {
   int cl, rank, tx, ty;
   uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
   bool ok = true;      // no wait has run out
-  static constexpr int kGroups = kSubs<L> / kJoin, kJoiners = L * kGroups;
-  static_assert(kJoiners == 16, "the joining lanes are half a warp");
+  static constexpr int kGroups = kSubs<L> / kJoin<L>, kJoiners = L * kGroups;
+  static_assert(kJoiners <= 32, "the joining lanes are in one warp");
 
   __device__ __forceinline__ Split(SplitSmem<V, L>& s, int* st)
       : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % L), ty(threadIdx.x / L) {
@@ -632,8 +635,8 @@ struct Split {
       const int group = threadIdx.x / L;
       Run<V> whole{all<V>(1.f), all<V>(0.f)};
 #pragma unroll
-      for (int k = 0; k < kJoin; ++k) {
-        Pair<V>& p = sm.run[buf][at(group * kJoin + k, kSubs<L>)][tx];
+      for (int k = 0; k < kJoin<L>; ++k) {
+        Pair<V>& p = sm.run[buf][at(group * kJoin<L> + k, kSubs<L>)][tx];
         const Pair<V> own = p, before = pair_of(whole);
         join(whole, own);
         p = before;
@@ -669,7 +672,7 @@ struct Split {
     int k = 0;
     for (; at(k, cl) != rank; ++k) state = through(state, t[at(k, cl) * L]);
     Vec<V> got = state;
-    if (kGroups == 2 && at(ty, kSubs<L>) >= kJoin) got = through(got, sm.half[buf][tx]);
+    if (kGroups == 2 && at(ty, kSubs<L>) >= kJoin<L>) got = through(got, sm.half[buf][tx]);
     got = through(got, sm.run[buf][ty][tx]);
     for (; k < cl; ++k) state = through(state, t[at(k, cl) * L]);
     return got;
@@ -997,12 +1000,13 @@ Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` l
   return {dim3((unsigned)width, (unsigned)(threads / width)), (unsigned)across};
 }
 
-// Split over time, and by a cluster of how many CTAs (0: a chain a thread)?  The least time by a model of both, in us: a
-// split step takes 1.75 (2.15 where CTAs exchange their runs), and longer where two CTAs share an SM; a chain 0.2 a
-// position forward and 0.085 backward.  `held` is how many clusters of each size the GPU holds at once.  Measured, chain /
-// split: 77 fp32 histories of up to 1001, d 200, forward 179 / 40 us; 400 of up to 515, d 256, 112 / 83; 1000 of 100,
-// d 128, 31 / 70; backward 82 / 68, 95 / 155, 32 / 132.  6 of 32768, d 256, by clusters of 1 to 8: 233, 135, 119, 95,
-// 83, 116, 116, 103.
+// Split over time, and how (lanes 0: a chain a thread)?  The least time by a model of the measured parts, in us: a chain
+// takes 0.2 a position forward and 0.085 backward; a split step some 1.5 forward and 2 backward, longer with more CTAs to
+// hand runs to, and longer where two CTAs share an SM; a CTA's beginning 0.5 and 3 (the forward's go on to the next piece).
+// `held` is how many clusters of each size the GPU holds at once.  Measured, chain / split: 77 fp32 histories of up to
+// 1001, d 200, forward 192 / 36 us; 400 of up to 515, d 256, 112 / 66; 1000 of 100, d 128, 28 / 50; backward 80 / 57,
+// 85 / 109, 31 / 72.  By clusters of 1, 2, 3, 4, 6 and 8, 6 histories of 32768, d 256: forward 191, 105, 84, 77, 134, 99;
+// backward with pieces of 128 bytes 474, 246, 172, 132, 185, 148 (64 bytes: 262, 139, 146, 146, 168, 199).
 struct SplitHow {
   int lanes, cl, held;  // lanes 0: a chain a thread
 };
@@ -1018,14 +1022,14 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
     const double full = count * c / 152.0;
     return full <= 1 ? 1.0 : c == 1 ? 0.4 + 0.6 * full : full;
   };
-  for (int L = 16; L >= 8; L /= 2) {
+  for (int L = back ? 32 : 16; L >= 8; L /= 2) {
     const int64_t items = n * ceil_div(lanes, L), tile = kSplitThr / L * kPos;
     if (items >= int64_t(1) << 28) break;
     for (int c = 1; c <= kMaxCluster; ++c) {
       const int h = held[back][c - 1];
-      const double step = (c == 1 ? 1.75 : 2.15) + (L == 8 ? 0.2 : 0);
+      const double step = (back ? 2.05 + 0.06 * (c - 1) : 1.5 + 0.09 * (c - 1)) + (L == 8 ? 0.2 : L == 32 ? -0.2 : 0);
       const double w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
-      const double cost = ceil_div(T, c * tile) * step * w + (back ? 1.5 : 0.5) * ceil_div(items, h);
+      const double cost = ceil_div(T, c * tile) * step * w + (back ? 3 : 0.5) * ceil_div(items, h);
       if (cost < best) {
         best = cost;
         how = {L, c, h};
@@ -1114,6 +1118,7 @@ hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
     return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
   }
   a.blocks = (int32_t)ceil_div(lanes, how.lanes);
+  if (how.lanes == 32) return backward_split<T, 32>(a, how.cl, s);
   return how.lanes == 16 ? backward_split<T, 16>(a, how.cl, s) : backward_split<T, 8>(a, how.cl, s);
 }
 
