@@ -727,7 +727,8 @@ hg_status encode(const MoeArgs& a, MoeMaps* m) {
   const uint64_t gate[2] = {(uint64_t)a.f, (uint64_t)a.experts * D}, down[3] = {D, (uint64_t)a.f, (uint64_t)a.experts};
   const uint32_t gate_box[2] = {C::FC, D}, down_box[3] = {f32 ? D : 64, C::FC, 1};
   HG_TRY(make_tmap(&m->wg, a.wg, f32, 2, gate, gate_box, f32 ? 0 : 64));
-  HG_TRY(make_tmap(&m->wu, a.wu, f32, 2, gate, gate_box, f32 ? 0 : 64));
+  m->wu = m->wg;
+  HG_TRY(move_tmap(&m->wu, a.wu));
   return make_tmap(&m->wd, a.wd, f32, 3, down, down_box, f32 ? 0 : 128);
 }
 

@@ -62,6 +62,22 @@ hg_status make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
   return HG_OK;
 }
 
+hg_status move_tmap(CUtensorMap* map, const void* base) {
+  static PFN_cuTensorMapReplaceAddress_v12000 fn = nullptr;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapReplaceAddress", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapReplaceAddress_v12000>(p);
+  }
+  if (!fn || fn(map, const_cast<void*>(base)) != CUDA_SUCCESS) {
+    set_error("cuTensorMapReplaceAddress failed or is not available from the driver");
+    return HG_ERR_CUDA;
+  }
+  return HG_OK;
+}
+
 hg_status make_tmap(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims, const uint32_t* box,
                     int swizzle) {
   auto fn = encode_fn();

@@ -280,5 +280,7 @@ hg_status make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
 // A contiguous array of bf16 or fp32 values of up to three dimensions, innermost first; box and swizzle in bytes (0: none).
 hg_status make_tmap(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims, const uint32_t* box,
                     int swizzle);
+// The same map of another array of the same shape.
+hg_status move_tmap(CUtensorMap* map, const void* base);
 
 }  // namespace hg
