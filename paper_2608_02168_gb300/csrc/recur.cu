@@ -1002,7 +1002,8 @@ Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` l
 
 // Split over time, and how (lanes 0: a chain a thread)?  The least time by a model of the measured parts, in us: a chain
 // takes 0.2 a position forward and 0.085 backward; a split step some 1.5 forward and 2 backward, longer with more CTAs to
-// hand runs to, and longer where two CTAs share an SM; a CTA's beginning 0.5 and 3 (the forward's go on to the next piece).
+// hand runs to, and longer where two CTAs share an SM; a CTA's beginning 0.5 and 3 (the forward's go on to the next piece), and the
+// kernel's 2.5 more than a chain's.
 // `held` is how many clusters of each size the GPU holds at once.  Measured, chain / split: 77 fp32 histories of up to
 // 1001, d 200, forward 192 / 36 us; 400 of up to 515, d 256, 112 / 66; 1000 of 100, d 128, 28 / 50; backward 80 / 57,
 // 85 / 109, 31 / 72.  By clusters of 1, 2, 3, 4, 6 and 8, 6 histories of 32768, d 256: forward 191, 105, 84, 77, 134, 99;
@@ -1013,7 +1014,7 @@ struct SplitHow {
 SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   static const int held[2][kMaxCluster] = {{304, 152, 97, 74, 58, 46, 38, 36}, {152, 76, 46, 36, 28, 23, 15, 15}};
   SplitHow how{0, 0, 0};
-  if (T <= 4 * kPos || n == 0) return how;
+  if (T <= kPos || n == 0) return how;
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
   const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
   const int64_t ctas = ceil_div(n, s.block.y) * s.across;
@@ -1029,7 +1030,7 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
       const int h = held[back][c - 1];
       const double step = (back ? 2.05 + 0.06 * (c - 1) : 1.5 + 0.09 * (c - 1)) + (L == 8 ? 0.2 : L == 32 ? -0.2 : 0);
       const double w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
-      const double cost = ceil_div(T, c * tile) * step * w + (back ? 3 : 0.5) * ceil_div(items, h);
+      const double cost = ceil_div(T, c * tile) * step * w + (back ? 3 : 0.5) * ceil_div(items, h) + 2.5;
       if (cost < best) {
         best = cost;
         how = {L, c, h};
