@@ -416,13 +416,15 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
   R = mul(k, R);
 }
 
-// Backward: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one kept before them; kAhead: the
-// 16 before them are loaded meanwhile (histories of one batch do without).  CTAs of 128 threads, two an SM: ragged
-// histories leave fewer threads waiting for the longest one than in 256 (400 of up to 515, d 256, 99 -> 85 us; 2000 of
-// them 316 us, 0.86 of the copy rate).  Registers bound it: 16 positions' gates and slopes, and the next rows.
+// Backward: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one kept before them; the 16
+// before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128 threads, three an SM: ragged histories
+// leave fewer threads waiting for the longest one than in 256, and 12 warps hide more than 8 (400 of up to 515, d 256,
+// 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers bound it: 16 positions' gates and slopes, and
+// the next rows; short histories the 4-byte loads and stores (100000 of up to 12, d 128, 290 us, 0.54 of the copy rate; 364
+// without the next one's loads).
 constexpr int kBwdThr = 128;
-template <typename T, bool kAhead>
-__global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
+template <typename T>
+__global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   __shared__ float sh[kBwdThr * V];
@@ -430,59 +432,80 @@ __global__ __launch_bounds__(kBwdThr, 2) void recur_bwd(RecurArgs a) {
   const bool in = c < a.d;
   const Vec<V> zero = all<V>(0.f), b = in ? bias_of<T>(a, c) : zero;
   Vec<V> sum = zero;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; in && i < a.n;
-       i += (int64_t)gridDim.x * blockDim.y) {
-    const int64_t len = length(a, i);
-    const T *x = at<T>(a.x, i, 0, c), *g = at<T>(a.g, i, 0, c), *dy = at<T>(a.dy, i, 0, c);
-    T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
-    const int64_t last = len > 0 ? (len - 1) / kPos * kPos : 0;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t i = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (in && i < a.n) {
     uint32_t rx[kPos], rg[kPos], ry[kPos];
     Vec<V> h;
-    auto load = [&](int64_t t0, int64_t end) {
-      load_rows(rx, x, a.x.st, t0, end);
-      load_rows(rg, g, a.g.st, t0, end, shut<T>());
-      load_rows(ry, dy, a.dy.st, t0, end);
+    auto load = [&](int64_t s, int64_t t0, int64_t end) {
+      load_rows(rx, at<T>(a.x, s, 0, c), a.x.st, t0, end);
+      load_rows(rg, at<T>(a.g, s, 0, c), a.g.st, t0, end, shut<T>());
+      load_rows(ry, at<T>(a.dy, s, 0, c), a.dy.st, t0, end);
       if (t0 > 0)
-        ldf(kept(a, i, t0, c), h);
+        ldf(kept(a, s, t0, c), h);
       else
-        h = state_of<V>(a.h_in, a, i, c);
+        h = state_of<V>(a.h_in, a, s, c);
     };
-    load(last, len);
-    Vec<V> R = state_of<V>(a.dh_out, a, i, c);
-    for (int64_t t = len; t < a.T; ++t) {
-      st4(dx + t * a.dx.st, zero);
-      st4(dg + t * a.dg.st, zero);
-    }
-    for (int64_t t0 = last; t0 >= 0 && len > 0; t0 -= kPos) {
-      Vec<V> sl[kPos], code[kPos];
+    auto last_of = [](int64_t len) { return len > 0 ? (len - 1) / kPos * kPos : 0; };
+    int64_t len = length(a, i), after = i + step < a.n ? length(a, i + step) : 0;
+    load(i, last_of(len), len);
+    Vec<V> R = state_of<V>(a.dh_out, a, i, c), next_R = zero;
+#pragma unroll 1
+    while (true) {
+      T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
+#pragma unroll 1
+      for (int64_t t0 = last_of(len); t0 >= 0; t0 -= kPos) {
+        const int left = left_of(t0, len);
+        Vec<V> sl[kPos], code[kPos];
 #pragma unroll
-      for (int u = 0; u < kPos; ++u) {
-        const GateOf<T> gt(piece(rg[u], T{}), b);
-        code[u] = gt.code();
-        sl[u] = slope(h, piece(rx[u], T{}), gt);
-      }
-      uint32_t cy[kPos];
+        for (int half = 0; half < kPos; half += kPos / 2) {  // eight gates at a time: side by side
+          if (half > 0 && left <= half) break;
 #pragma unroll
-      for (int u = 0; u < kPos; ++u) cy[u] = ry[u];
-      if (kAhead && t0 > 0) load(t0 - kPos, t0);
-      Vec<V> here = zero;
-      const int left = left_of(t0, len);
-      T *px = dx + (t0 + kPos) * a.dx.st, *pg = dg + (t0 + kPos) * a.dg.st;
-#pragma unroll
-      for (int u = kPos - 1; u >= 0; --u) {
-        px -= a.dx.st;
-        pg -= a.dg.st;
-        if (u < left) {
-          Vec<V> ox, og;
-          back<T>(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
-          here = add(here, og);
-          st4(px, ox);
-          st4(pg, og);
+          for (int u = half; u < half + kPos / 2; ++u) {
+            const GateOf<T> gt(piece(rg[u], T{}), b);
+            code[u] = gt.code();
+            sl[u] = slope(h, piece(rx[u], T{}), gt);
+          }
         }
+        uint32_t cy[kPos];
+#pragma unroll
+        for (int u = 0; u < kPos; ++u) cy[u] = ry[u];
+        if (t0 > 0) {
+          load(i, t0 - kPos, t0);
+        } else if (i + step < a.n) {
+          load(i + step, last_of(after), after);
+          next_R = state_of<V>(a.dh_out, a, i + step, c);
+        }
+        Vec<V> here = zero;
+        T *px = dx + (t0 + kPos) * a.dx.st, *pg = dg + (t0 + kPos) * a.dg.st;
+#pragma unroll
+        for (int u = kPos - 1; u >= 0; --u) {
+          px -= a.dx.st;
+          pg -= a.dg.st;
+          if (u < left) {
+            Vec<V> ox, og;
+            back<T>(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
+            here = add(here, og);
+            st4(px, ox);
+            st4(pg, og);
+          }
+        }
+        sum = add(sum, here);
       }
-      sum = add(sum, here);
+      // zero rows, 16 bytes at a time: four neighbouring threads take every fourth row each
+      const int part = threadIdx.x % 4, back16 = part * V;
+#pragma unroll 1
+      for (int64_t t = len + part; t < a.T; t += 4) {
+        st16(dx + t * a.dx.st - back16, make_uint4(0, 0, 0, 0));
+        st16(dg + t * a.dg.st - back16, make_uint4(0, 0, 0, 0));
+      }
+      if (a.dh_in) stf(a.dh_in + i * a.d + c, R);
+      i += step;
+      if (i >= a.n) break;
+      R = next_R;
+      len = after;
+      if (i + step < a.n) after = length(a, i + step);
     }
-    if (a.dh_in) stf(a.dh_in + i * a.d + c, R);
   }
   if (a.part)
     part_sums<V>(sum, sh, threadIdx.x, threadIdx.y, blockDim.x, blockDim.y, a.part + (int64_t)blockIdx.x * a.d + c, in);
@@ -995,8 +1018,8 @@ struct Shape {
   dim3 block;
   unsigned across;  // CTAs across a row
 };
-Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` lanes; short ones share a CTA
-  const int64_t across = ceil_div(lanes, threads), width = ceil_div(lanes, across);
+Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` lanes, in fours; short ones share a CTA
+  const int64_t across = ceil_div(lanes, threads), width = lanes < 4 ? lanes : ceil_div(ceil_div(lanes, across), 4) * 4;
   return {dim3((unsigned)width, (unsigned)(threads / width)), (unsigned)across};
 }
 
@@ -1018,7 +1041,7 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
   const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
   const int64_t ctas = ceil_div(n, s.block.y) * s.across;
-  double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, 304);
+  double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, back ? 456 : 304);
   auto waves = [](int64_t count, int c) {  // of `count` clusters at once: how long beside one CTA an SM
     const double full = count * c / 152.0;
     return full <= 1 ? 1.0 : c == 1 ? 0.4 + 0.6 * full : full;
@@ -1045,7 +1068,8 @@ int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const SplitHow how = split_of(p, n, T, true);
   if (how.lanes) return n * how.cl;
   const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr);
-  const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, 152 * 16 / s.across);
+  // short histories: as many CTAs as run at once, each from one to the next; long ones differ too much for that
+  const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, (T <= 64 ? 152 * 3 : 152 * 16) / s.across);
   return std::min(groups, most);
 }
 
@@ -1115,8 +1139,7 @@ hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
   if (how.lanes == 0) {
     const Shape sh = shape_of(lanes, kBwdThr);
     const dim3 grid((unsigned)rows, sh.across);
-    if (a.T <= kPos) return launch("recur_bwd", recur_bwd<T, false>, grid, sh.block, 0, s, a);
-    return launch("recur_bwd", recur_bwd<T, true>, grid, sh.block, 0, s, a);
+    return launch("recur_bwd", recur_bwd<T>, grid, sh.block, 0, s, a);
   }
   a.blocks = (int32_t)ceil_div(lanes, how.lanes);
   if (how.lanes == 32) return backward_split<T, 32>(a, how.cl, s);
