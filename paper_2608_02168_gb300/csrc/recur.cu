@@ -1018,8 +1018,8 @@ struct Shape {
   dim3 block;
   unsigned across;  // CTAs across a row
 };
-Shape shape_of(int64_t lanes, int threads = 256) {  // rows of up to `threads` lanes, in fours; short ones share a CTA
-  const int64_t across = ceil_div(lanes, threads), width = lanes < 4 ? lanes : ceil_div(ceil_div(lanes, across), 4) * 4;
+Shape shape_of(int64_t lanes, int threads = 256, int unit = 1) {  // rows of up to `threads` lanes; short ones share a CTA
+  const int64_t across = ceil_div(lanes, threads), width = ceil_div(ceil_div(lanes, across), unit) * unit;
   return {dim3((unsigned)width, (unsigned)(threads / width)), (unsigned)across};
 }
 
@@ -1039,7 +1039,7 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   SplitHow how{0, 0, 0};
   if (T <= kPos || n == 0) return how;
   const int64_t lanes = p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4;
-  const Shape s = shape_of(back ? lanes : lanes / 4, back ? kBwdThr : 256);
+  const Shape s = back ? shape_of(lanes, kBwdThr, 4) : shape_of(lanes / 4);
   const int64_t ctas = ceil_div(n, s.block.y) * s.across;
   double best = 3 + (back ? 0.085 : 0.2) * T * ceil_div(ctas, back ? 456 : 304);
   auto waves = [](int64_t count, int c) {  // of `count` clusters at once: how long beside one CTA an SM
@@ -1067,7 +1067,7 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const SplitHow how = split_of(p, n, T, true);
   if (how.lanes) return n * how.cl;
-  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr);
+  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr, 4);
   // short histories: as many CTAs as run at once, each from one to the next; long ones differ too much for that
   const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, (T <= 64 ? 152 * 3 : 152 * 16) / s.across);
   return std::min(groups, most);
@@ -1137,7 +1137,7 @@ template <typename T>
 hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
   const int64_t lanes = a.d / kVec<T>;
   if (how.lanes == 0) {
-    const Shape sh = shape_of(lanes, kBwdThr);
+    const Shape sh = shape_of(lanes, kBwdThr, 4);
     const dim3 grid((unsigned)rows, sh.across);
     return launch("recur_bwd", recur_bwd<T>, grid, sh.block, 0, s, a);
   }

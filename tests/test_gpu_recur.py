@@ -424,3 +424,20 @@ def test_streams_given_and_two_calls_at_once():
         s.synchronize()
         assert torch.equal(y, ref) and torch.equal(e, last)
     assert hg.hg_device_status() == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T,d", [(700, 9, 520), (300, 16, 1032), (5000, 17, 24), (2000, 40, 264)])
+def test_many_short_histories_of_odd_widths(dt, n, T, d):
+    """More histories than threads run at once (each thread goes from one to the next), rows that several CTAs share."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    x, g, dy, b, lens, h, dh = problem(dt, n, T, d, 17, True, True)
+    X, G, DY = (wide(past(v, lens), td) for v in (x, g, dy))
+    out = {k: wide(np.full((n, T, d), np.nan, np.float32), td) for k in ("y", "dx", "dg")}
+    o = run(hg, params(hg, b, d, td), td, X, G, dev(lens), dev(h), DY, dev(dh), n, T, d, out)
+    check(o, dt, x, g, dy, b, lens, h, dh)
+    for k in ("y", "dx", "dg"):
+        w = o[k]._base.view(n, T, 2 * d + 8)
+        assert torch.isnan(w[..., :8]).all() and torch.isnan(w[..., 8 + d:]).all(), k
