@@ -1,14 +1,20 @@
-// A whole layer of experts for a few rows (hg_moe_fwd), two launches:
+// A whole layer of experts for a few rows (hg_moe_fwd):
 //   moe_router    l = x W_router, the top_k largest, their weights; a CTA a row
-//   moe_experts   Y = sum_j w_j (act(x W_gate[e_j]) * (x W_up[e_j])) W_down[e_j] (+ x)
+//   moe_experts   (act(x W_gate[e]) * (x W_up[e])) W_down[e] for each expert e and the rows that chose it
+//   moe_sum       Y = sum of a row's w_j times what expert e_j gave it (+ x); up to kFewRows rows moe_experts does it
 //
-// With a few rows an expert the weights are the work: 3 d f values of every expert that a row chose are read once, and
-// what a row costs beside them is small (16 rows: 192 flops a byte of bf16 weights at most, a tenth of what the tensor
-// pipe does meanwhile).  So the second kernel is a stream of weights: the chosen experts' hidden features in chunks of
-// 64 bytes of a W_gate row are one list, cut into equal shares, a CTA a share, its loads some 100 KB ahead of the
-// products.  A share may begin and end inside an expert.  What a share gives an expert's rows (d sums each, fp32) goes
-// to scratch, and the CTA that brings a row's last share adds them up in the order of the list: the sum does not
-// depend on who comes last.
+// With a few rows an expert the weights are the work: 3 d f values of every expert that a row chose are read once, with
+// one multiplication and addition a row for each (16 rows of bf16: 16 flops a byte, where the tensor pipe has 280 a byte of
+// HBM).  So moe_experts is a stream of weights: the chosen experts' hidden features in chunks of 64 bytes of a W_gate row
+// are one list, cut into equal shares, a CTA a share, with some 100 KB of copies ahead of the products.  A share may begin
+// and end inside an expert; a pass over an expert's chunks serves up to 64 of its rows.  What a share gives a pass's rows
+// (d sums each, fp32) goes to scratch and is added up in the order of the list, whichever CTA was last.  mma.sync has the
+// room: a tile of sixteen rows is what few rows fill, and an instruction on 128 would run at an eighth of its rate.
+//
+// 64 rows, two of 64 experts each, d 256, f 1024, bf16: 24 us for the 87 MB that they chose; of that 3 us for the list and
+// the rows, 2 us until the first chunks are there, 13 us of weights; f 4096: 66 us, so beyond the beginning the weights
+// come at 6.3 TB/s (0.93 of the copy rate).  300 rows, four of 32 experts each, f 704 (33 rows a pass): 21 us, bound by a
+// pass's products (1.4 us a chunk, half of it the second product with its two terms of H).
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
