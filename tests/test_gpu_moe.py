@@ -60,7 +60,8 @@ CASES = [(1, 1, 1, 64, 8, "silu", False, True, False), (1, 16, 2, 128, 384, "sil
          (130, 256, 8, 64, 16, "relu", False, True, False), (1024, 7, 3, 64, 56, "silu", True, True, True),
          (1000, 129, 8, 128, 32, "silu", False, False, False), (65, 1, 1, 256, 520, "silu", True, True, False),
          (4, 2, 2, 256, 136, "silu", True, True, True), (4, 9, 8, 64, 24, "gelu_tanh", False, False, False),
-         (5, 2, 2, 256, 136, "silu", True, True, True), (64, 1, 1, 128, 40, "none", False, False, False),
+         (2, 2, 2, 256, 1032, "silu", True, True, False), (2, 9, 8, 128, 24, "relu", False, False, True),
+         (3, 4, 3, 64, 200, "silu", True, True, False), (5, 2, 2, 256, 136, "silu", True, True, True), (64, 1, 1, 128, 40, "none", False, False, False),
          (128, 2, 2, 128, 264, "silu", False, True, False), (1024, 256, 8, 256, 8, "silu", True, False, True)]
 
 
