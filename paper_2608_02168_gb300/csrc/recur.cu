@@ -8,6 +8,7 @@
 // Each value is read and written once and costs two special functions and some ten other instructions: all forms are
 // bound by HBM, or by latency where there are few chains.
 //   recur_fwd, recur_bwd              a thread walks a chain (split_of says when)
+//   recur_bwd_short                   the same for histories of at most 16 positions
 //   recur_fwd_split, recur_bwd_split  a few long histories: time is split over threads, CTAs and clusters
 //   recur_bias_sum                    the CTAs' parts of the bias's gradient, in a fixed order
 //   recur_step                        one new snapshot: 1000003 nodes of d 128, one in eight not live, 242 us (the copy rate)
@@ -416,12 +417,11 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
   R = mul(k, R);
 }
 
-// Backward: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one kept before them; the 16
-// before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128 threads, three an SM: ragged histories
+// Backward of more than 16 positions: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one
+// kept before them; the 16 before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128 threads, three an SM: ragged histories
 // leave fewer threads waiting for the longest one than in 256, and 12 warps hide more than 8 (400 of up to 515, d 256,
-// 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers bound it: 16 positions' gates and slopes, and
-// the next rows; short histories the 4-byte loads and stores (100000 of up to 12, d 128, 290 us, 0.54 of the copy rate; 364
-// without the next one's loads).
+// 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers bound it:
+// 16 positions' gates and slopes, and the next rows.
 constexpr int kBwdThr = 128;
 template <typename T>
 __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
@@ -505,6 +505,151 @@ __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
       R = next_R;
       len = after;
       if (i + step < a.n) after = length(a, i + step);
+    }
+  }
+  if (a.part)
+    part_sums<V>(sum, sh, threadIdx.x, threadIdx.y, blockDim.x, blockDim.y, a.part + (int64_t)blockIdx.x * a.d + c, in);
+}
+
+// Backward of at most 16 positions: rows go through shared memory, 16 bytes a copy and a store, the next sequence's on
+// their way meanwhile; a thread reads its 4 bytes of them where its positions are, four positions at a time, and leaves
+// its gradients in their place.  Fewer instructions for addresses than with loads and stores of 4 bytes, a fourth CTA an
+// SM where the next rows were in registers, and only a quad of threads waits
+// for one another.  100000 ragged histories of up to 12, d 128, bf16, 221 us, 0.82 of the copy rate (the kernel above: 291);
+// 50000 in fp32 184 (364); 150000 of one 142 (347); 50000 of 16, none ragged, 186 (173).  A third stage 261 where two take
+// 223 (three CTAs an SM then), five CTAs 246 (96 registers).  Bound by the rows' bytes and by the instructions of gates.
+template <int V>
+struct ShortStage {  // of shared memory: a sequence's two states, then its rows of x, g and dy, position by position
+  static constexpr int kPitch = kBwdThr * 4, kRow = 3 * kPitch + 32;  // a quad's four 16-byte pieces: different banks
+  static constexpr int kStates = 2 * kBwdThr * 4 * V;
+};
+constexpr int kShortStages = 2, kShortCtas = 4, kGroup = 4;
+template <typename T>
+int short_bytes(int64_t T_) {
+  using S = ShortStage<kVec<T>>;
+  return kShortStages * (S::kStates + (int)ceil_div(T_, kGroup) * kGroup * S::kRow);
+}
+template <typename T>
+__global__ __launch_bounds__(kBwdThr, kShortCtas) void recur_bwd_short(RecurArgs a) {
+  pdl_begin();
+  constexpr int V = kVec<T>;
+  using S = ShortStage<V>;
+  extern __shared__ __align__(128) char smem[];
+  __shared__ float sh[kBwdThr * V];
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, tid = threadIdx.y * blockDim.x + threadIdx.x, part = tid % 4;
+  const bool in = c < a.d;
+  const uint32_t quad = 0xFu << (tid % 32 - part);
+  const Vec<V> zero = all<V>(0.f), b = in ? bias_of<T>(a, c) : zero;
+  Vec<V> sum = zero;
+  const int n = (int)a.n, T_ = (int)a.T, step = gridDim.x * blockDim.y;
+  const int stage_bytes = S::kStates + (T_ + kGroup - 1) / kGroup * kGroup * S::kRow;
+  int i = blockIdx.x * blockDim.y + threadIdx.y;
+  if (in && i < n) {
+    const int c16 = c - part * V;
+    auto length_at = [&](int64_t s) { return s < n ? (int)length(a, s) : 0; };
+    // a sequence's rows, a quad's 16 bytes of every fourth a thread, and the thread's own states
+    auto load = [&](int64_t s, int len, char* to) {
+      if (s < n) {
+        if (a.h_in) {
+          if constexpr (V == 2)
+            tc::cp_async8(to + tid * 8, a.h_in + s * a.d + c);
+          else
+            tc::cp_async4(to + tid * 4, a.h_in + s * a.d + c);
+        }
+        if (a.dh_out) {
+          if constexpr (V == 2)
+            tc::cp_async8(to + (kBwdThr + tid) * 8, a.dh_out + s * a.d + c);
+          else
+            tc::cp_async4(to + (kBwdThr + tid) * 4, a.dh_out + s * a.d + c);
+        }
+        if (part < len) {
+          const T *x = at<T>(a.x, s, part, c16), *g = at<T>(a.g, s, part, c16), *y = at<T>(a.dy, s, part, c16);
+          char* row = to + S::kStates + part * S::kRow + (tid - part) * 4;
+#pragma unroll
+          for (int u = 0; u < kPos; u += 4) {
+            if (part + u >= len) break;
+            tc::cp_async16(row + u * S::kRow, x, true);
+            tc::cp_async16(row + u * S::kRow + S::kPitch, g, true);
+            tc::cp_async16(row + u * S::kRow + 2 * S::kPitch, y, true);
+            x += 4 * a.x.st;
+            g += 4 * a.g.st;
+            y += 4 * a.dy.st;
+          }
+        }
+      }
+      tc::cp_async_commit();
+    };
+    int lens[kShortStages + 1];  // of this sequence, of those on their way, and of the next
+#pragma unroll
+    for (int k = 0; k <= kShortStages; ++k) lens[k] = length_at(i + (int64_t)k * step);
+    char *here = smem, *const end = smem + kShortStages * stage_bytes, *free_ = smem + (kShortStages - 1) * stage_bytes;
+#pragma unroll
+    for (int k = 0; k < kShortStages - 1; ++k) load(i + (int64_t)k * step, lens[k], smem + k * stage_bytes);
+#pragma unroll 1
+    for (; i < n; i += step) {
+      __syncwarp(quad);  // the quad has read its last sequence's gradients
+      load(i + (int64_t)(kShortStages - 1) * step, lens[kShortStages - 1], free_);
+      const int len = lens[0];
+#pragma unroll
+      for (int k = 0; k < kShortStages; ++k) lens[k] = lens[k + 1];
+      lens[kShortStages] = length_at(i + (int64_t)(kShortStages + 1) * step);
+      tc::cp_async_wait<kShortStages - 1>();
+      __syncwarp(quad);  // and its pieces of this one are here
+      char* const rows = here + S::kStates + tid * 4;
+      Vec<V> h = zero, R = zero;
+      if (a.h_in) ldf(reinterpret_cast<const float*>(here) + tid * V, h);
+      if (a.dh_out) ldf(reinterpret_cast<const float*>(here) + (kBwdThr + tid) * V, R);
+      // positions of a group from len on hold what they held before: they change nothing that is used
+      Vec<V> sl[kPos], code[kPos];
+#pragma unroll
+      for (int q = 0; q < kPos; q += kGroup) {
+        if (len <= q) break;
+#pragma unroll
+        for (int u = q; u < q + kGroup; ++u) {
+          const char* row = rows + u * S::kRow;
+          const GateOf<T> gt(piece(ld4(reinterpret_cast<const T*>(row + S::kPitch)), T{}), b);
+          code[u] = gt.code();
+          sl[u] = slope(h, piece(ld4(reinterpret_cast<const T*>(row)), T{}), gt);
+        }
+      }
+      Vec<V> partial = zero;
+#pragma unroll
+      for (int q = kPos - kGroup; q >= 0; q -= kGroup) {
+        if (len <= q) continue;
+#pragma unroll
+        for (int u = q + kGroup - 1; u >= q; --u)
+          if (u < len) {
+            char* row = rows + u * S::kRow;
+            Vec<V> ox, og;
+            back<T>(R, piece(ld4(reinterpret_cast<const T*>(row + 2 * S::kPitch)), T{}), code[u], sl[u], ox, og);
+            partial = add(partial, og);
+            st4(reinterpret_cast<T*>(row), ox);
+            st4(reinterpret_cast<T*>(row + S::kPitch), og);
+          }
+      }
+      sum = add(sum, partial);
+      if (a.dh_in) stf(a.dh_in + (int64_t)i * a.d + c, R);
+      __syncwarp(quad);
+      if (part < T_) {
+        T *dx = at_out<T>(a.dx, i, part, c16), *dg = at_out<T>(a.dg, i, part, c16);
+        const char* row = rows + part * S::kRow - part * 4;
+#pragma unroll
+        for (int u = 0; u < kPos; u += 4) {
+          if (part + u >= T_) break;
+          uint4 ox = make_uint4(0, 0, 0, 0), og = ox;
+          if (part + u < len) {
+            ox = *reinterpret_cast<const uint4*>(row + u * S::kRow);
+            og = *reinterpret_cast<const uint4*>(row + u * S::kRow + S::kPitch);
+          }
+          st16(dx, ox);
+          st16(dg, og);
+          dx += 4 * a.dx.st;
+          dg += 4 * a.dg.st;
+        }
+      }
+      free_ = here;
+      here += stage_bytes;
+      if (here == end) here = smem;
     }
   }
   if (a.part)
@@ -1063,13 +1208,18 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
   return how;
 }
 
+// CTAs of short histories that an SM holds.
+int short_ctas(const hg_recur_params* p, int64_t T) {
+  const int bytes = p->dtype == HG_BF16 ? short_bytes<__nv_bfloat16>(T) : short_bytes<float>(T);
+  return std::min(kShortCtas, (227 << 10) / (bytes + (2 << 10)));
+}
 // Rows of partial sums of the bias's gradient.
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const SplitHow how = split_of(p, n, T, true);
   if (how.lanes) return n * how.cl;
   const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr, 4);
   // short histories: as many CTAs as run at once, each from one to the next; long ones differ too much for that
-  const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, (T <= 64 ? 152 * 3 : 152 * 16) / s.across);
+  const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, (T <= kPos ? 152 * short_ctas(p, T) : T <= 64 ? 152 * 3 : 152 * 16) / s.across);
   return std::min(groups, most);
 }
 
@@ -1139,6 +1289,10 @@ hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
   if (how.lanes == 0) {
     const Shape sh = shape_of(lanes, kBwdThr, 4);
     const dim3 grid((unsigned)rows, sh.across);
+    if (a.T <= kPos) {
+      HG_TRY((allow_smem<recur_bwd_short<T>>((size_t)short_bytes<T>(kPos))));
+      return launch("recur_bwd_short", recur_bwd_short<T>, grid, sh.block, (size_t)short_bytes<T>(a.T), s, a);
+    }
     return launch("recur_bwd", recur_bwd<T>, grid, sh.block, 0, s, a);
   }
   a.blocks = (int32_t)ceil_div(lanes, how.lanes);

@@ -84,7 +84,8 @@ CASES = [(1, 1, 8, False, False), (3, 1, 64, True, True), (5, 2, 24, True, True)
          (9, 64, 16, True, True), (1400, 66, 64, True, True), (3, 1030, 16384, True, True),
          (1, 65, 8, False, True), (200, 80, 64, True, True), (3, 256, 40, True, True), (4, 257, 64, True, False),
          (1, 300, 96, False, True), (2, 513, 24, True, True), (2, 1024, 64, False, False), (3, 1100, 40, True, True),
-         (1, 2049, 64, False, True), (2, 4500, 8, True, True)]
+         (1, 2049, 64, False, True), (2, 4500, 8, True, True),
+         (3000, 16, 24, True, True), (5000, 1, 40, False, True), (2100, 5, 264, True, False)]
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -108,7 +109,7 @@ def test_forward_and_backward(dt, n, T, d, ragged, state):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("n,T,d", [(40, 20, 64), (3, 700, 48)])
+@pytest.mark.parametrize("n,T,d", [(40, 20, 64), (3, 700, 48), (700, 14, 48), (40, 7, 64)])
 def test_positions_within_sequences_or_the_other_way(dt, n, T, d):
     """Rows stored position by position, [T, n, d], and inputs that one sequence's row serves (stride zero)."""
     need_gpu()
@@ -123,7 +124,7 @@ def test_positions_within_sequences_or_the_other_way(dt, n, T, d):
     check(o, dt, x, g, dy, b, lens, h, dh)
 
 
-@pytest.mark.parametrize("n,T", [(30, 40), (2, 600)])
+@pytest.mark.parametrize("n,T", [(30, 40), (2, 600), (2000, 12)])
 def test_optional_arguments_change_nothing_else(n, T):
     need_gpu()
     hg = lib()
@@ -253,7 +254,7 @@ def test_shut_and_open_gates(n, T, d):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("n,T,d", [(6, 40, 64), (2, 900, 64), (3, 300, 8)])
+@pytest.mark.parametrize("n,T,d", [(6, 40, 64), (2, 900, 64), (3, 300, 8), (6, 12, 64)])
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 def test_a_bad_value_reaches_nothing_before_it(dt, n, T, d, bad):
     need_gpu()
@@ -279,7 +280,7 @@ def test_a_bad_value_reaches_nothing_before_it(dt, n, T, d, bad):
     assert torch.equal(o["dx"][~hit], ref["dx"][~hit]) and torch.equal(o["dg"][~hit], ref["dg"][~hit])
 
 
-@pytest.mark.parametrize("n,T,d", [(400, 30, 64), (2, 3000, 64), (1, 700, 40)])
+@pytest.mark.parametrize("n,T,d", [(400, 30, 64), (2, 3000, 64), (1, 700, 40), (4000, 13, 64)])
 def test_calls_repeat_their_bits_and_replay_in_a_graph(n, T, d):
     need_gpu()
     hg = lib()
@@ -386,10 +387,11 @@ def test_a_very_long_history_and_very_many_short_ones(dt):
     assert ((y.double() - want).abs() <= U[dt] * want.abs() + (2 * 2 + 100) * F32 * most[:, None]).all()
 
 
-def test_chains_with_offsets_past_32_bits():
+@pytest.mark.parametrize("T", [20, 12])
+def test_chains_with_offsets_past_32_bits(T):
     need_gpu()
     hg = lib()
-    td, T, d = torch.bfloat16, 20, 64
+    td, d = torch.bfloat16, 64
     far = (1 << 32) + 64
     x, g, dy, b, _, h, dh = problem("bf16", 2, T, d, 15, False, True)
     big = torch.empty(far + 6 * T * d, dtype=td, device="cuda")
