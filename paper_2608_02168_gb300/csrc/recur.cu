@@ -94,6 +94,20 @@ __device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {
   return a;
 }
 
+// a + rest as its sum and what that leaves of it.
+template <int V>
+__device__ __forceinline__ void settle(Vec<V>& a, Vec<V>& rest) {
+  const Vec<V> sum = add(a, rest);
+  rest = minus(rest, minus(sum, a));
+  a = sum;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> less(Vec<V> c, Vec<V> a, Vec<V> b) {  // c - a b
+#pragma unroll
+  for (int i = 0; i < V; ++i) c.v[i] = fmaf(-a.v[i], b.v[i], c.v[i]);
+  return c;
+}
+
 // z = sigmoid(g + b) and k = 1 - z.  The logit's product with -log2 e and the sum with the bias's are one instruction.
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -127,21 +141,38 @@ struct Gate {
   __device__ __forceinline__ Vec<V> k() const { return pick(s, big); }
   __device__ __forceinline__ Vec<V> zk() const { return mul(s, big); }
   __device__ __forceinline__ Vec<V> next(Vec<V> h, Vec<V> x) const { return fma(code(), minus(x, h), pick(x, h)); }
+  // The same of a state kept as h + rest, whose sum `sum` is.
+  __device__ __forceinline__ void next(Vec<V>& h, Vec<V>& rest, Vec<V> sum, Vec<V> x) const {
+    rest = fma(code(), minus(x, sum), pick(x, rest));
+    h = pick(all<V>(0.f), h);
+  }
+  // What a gate lets through of R, z R, and what it leaves, (1 - z) R: the smaller as a product, the other as R without it.
+  __device__ __forceinline__ static void part(Vec<V> code, Vec<V> R, Vec<V>& through, Vec<V>& left) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float s = fabsf(code.v[i]), small = s * R.v[i], rest = fmaf(-s, R.v[i], R.v[i]);
+      const bool open = __float_as_int(code.v[i]) < 0;
+      through.v[i] = open ? rest : small;
+      left.v[i] = open ? small : rest;
+    }
+  }
+  // The same of R + rest, whose sum `sum` is: what is left stays in two numbers.
+  __device__ __forceinline__ static void part(Vec<V> code, Vec<V>& R, Vec<V>& rest, Vec<V> sum, Vec<V>& through) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float s = fabsf(code.v[i]), small = s * sum.v[i];
+      const bool open = __float_as_int(code.v[i]) < 0;
+      through.v[i] = open ? sum.v[i] - small : small;
+      rest.v[i] = open ? small : fmaf(-s, sum.v[i], rest.v[i]);
+      R.v[i] = open ? 0.f : R.v[i];
+    }
+  }
   // Both in one number: z where it is not negative, -k where it is.
   __device__ __forceinline__ Vec<V> code() const {
     Vec<V> r;
 #pragma unroll
     for (int i = 0; i < V; ++i) r.v[i] = open[i] ? -s.v[i] : s.v[i];
     return r;
-  }
-  __device__ __forceinline__ static void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float s = fabsf(code.v[i]), big = 1.f - s;
-      const bool open = __float_as_int(code.v[i]) < 0;
-      z.v[i] = open ? big : s;
-      k.v[i] = open ? s : big;
-    }
   }
 };
 
@@ -159,7 +190,6 @@ struct Gate<V, false> {
     for (int i = 0; i < V; ++i) r.v[i] = gate_rcp(r.v[i]);
   }
   __device__ __forceinline__ Vec<V> z() const { return r; }
-  __device__ __forceinline__ Vec<V> k() const { return minus(all<V>(1.f), r); }
   __device__ __forceinline__ Vec<V> zk() const {  // of its own size, as a gradient that it is
     Vec<V> x;
 #pragma unroll
@@ -171,9 +201,9 @@ struct Gate<V, false> {
   }
   __device__ __forceinline__ Vec<V> next(Vec<V> h, Vec<V> x) const { return fma(r, minus(x, h), h); }
   __device__ __forceinline__ Vec<V> code() const { return r; }
-  __device__ __forceinline__ static void decode(Vec<V> code, Vec<V>& z, Vec<V>& k) {
-    z = code;
-    k = minus(all<V>(1.f), code);
+  __device__ __forceinline__ static void part(Vec<V> code, Vec<V> R, Vec<V>& through, Vec<V>& left) {
+    through = mul(code, R);
+    left = less(R, code, R);
   }
 };
 template <typename T>
@@ -304,7 +334,7 @@ struct Wide {
 // A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's length
 // and state, are on their way while these ones' gates are computed (a sequence a thread: 203 us).  Bound by HBM: 150001
 // ragged histories of up to 12, d 128, bf16, 156 us, 0.94 of the copy rate.
-template <typename T>
+template <typename T, bool kTwo>
 __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   pdl_begin();
   using W = Wide<T>;
@@ -312,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
   if (c >= a.d || first >= a.n) return;
   uint4 rx[kWide], rg[kWide], nx[kWide], ng[kWide];  // this batch's rows, and the next one's
-  W b, h, enter;
+  W b, h, enter, rest;
 #pragma unroll
   for (int k = 0; k < W::N; ++k) b.v[k] = enter.v[k] = all<2>(0.f);
   if (a.bias) {
@@ -357,7 +387,11 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
       rx[u] = nx[u];
       rg[u] = ng[u];
     }
-    if (t == 0) h = enter;
+    if (t == 0) {
+      h = enter;
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) rest.v[k] = all<2>(0.f);
+    }
     load();
     if (a.saved && t > 0 && t % kPos == 0) h.store(kept(a, i, t, c));
 #pragma unroll
@@ -367,10 +401,22 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
         fx.unpacked(rx[u]);
         fg.unpacked(rg[u]);
 #pragma unroll
-        for (int k = 0; k < W::N; ++k) h.v[k] = Gate<2, sizeof(T) == 4>(fg.v[k], b.v[k]).next(h.v[k], fx.v[k]);
-        st16(y, h.packed());
+        for (int k = 0; k < W::N; ++k) {
+          const Gate<2, sizeof(T) == 4> gt(fg.v[k], b.v[k]);
+          if constexpr (kTwo) {
+            gt.next(h.v[k], rest.v[k], add(h.v[k], rest.v[k]), fx.v[k]);
+            fx.v[k] = add(h.v[k], rest.v[k]);
+          } else {
+            fx.v[k] = h.v[k] = gt.next(h.v[k], fx.v[k]);
+          }
+        }
+        st16(y, fx.packed());
         y += a.y.st;
       }
+    if constexpr (kTwo) {
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) settle(h.v[k], rest.v[k]);
+    }
     t += kWide;
     if (t < len) continue;
 #pragma unroll 1
@@ -409,12 +455,9 @@ __device__ __forceinline__ Vec<V> slope(Vec<V>& h, Vec<V> x, const Gate<V, kExac
 // And its half from the end: what R gives dx and dg, and R for the position before.
 template <typename T, int V>
 __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> slope, Vec<V>& dx, Vec<V>& dg) {
-  Vec<V> z, k;
-  GateOf<T>::decode(code, z, k);
   R = add(R, dy);
-  dx = mul(z, R);
   dg = mul(slope, R);
-  R = mul(k, R);
+  GateOf<T>::part(code, R, dx, R);
 }
 
 // Backward of more than 16 positions: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one
@@ -427,6 +470,7 @@ template <typename T>
 __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
+  constexpr bool kTwo = sizeof(T) == 4;
   __shared__ float sh[kBwdThr * V];
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   const bool in = c < a.d;
@@ -449,7 +493,7 @@ __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
     auto last_of = [](int64_t len) { return len > 0 ? (len - 1) / kPos * kPos : 0; };
     int64_t len = length(a, i), after = i + step < a.n ? length(a, i + step) : 0;
     load(i, last_of(len), len);
-    Vec<V> R = state_of<V>(a.dh_out, a, i, c), next_R = zero;
+    Vec<V> R = state_of<V>(a.dh_out, a, i, c), rest = zero, next_R = zero;
 #pragma unroll 1
     while (true) {
       T *dx = at_out<T>(a.dx, i, 0, c), *dg = at_out<T>(a.dg, i, 0, c);
@@ -484,12 +528,20 @@ __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
           pg -= a.dg.st;
           if (u < left) {
             Vec<V> ox, og;
-            back<T>(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
+            if constexpr (kTwo) {
+              rest = add(rest, piece(cy[u], T{}));
+              const Vec<V> both = add(R, rest);
+              og = mul(sl[u], both);
+              GateOf<T>::part(code[u], R, rest, both, ox);
+            } else {
+              back<T>(R, piece(cy[u], T{}), code[u], sl[u], ox, og);
+            }
             here = add(here, og);
             st4(px, ox);
             st4(pg, og);
           }
         }
+        if constexpr (kTwo) settle(R, rest);
         sum = add(sum, here);
       }
       // zero rows, 16 bytes at a time: four neighbouring threads take every fourth row each
@@ -503,6 +555,7 @@ __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
       i += step;
       if (i >= a.n) break;
       R = next_R;
+      rest = zero;
       len = after;
       if (i + step < a.n) after = length(a, i + step);
     }
@@ -672,51 +725,90 @@ __global__ __launch_bounds__(kBwdThr, kShortCtas) void recur_bwd_short(RecurArgs
 // 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6 histories
 // of 32768, d 256, bf16: 86 us forward (HBM: 44).  Half as many positions a thread and twice as many threads took 97 us
 // where this took 83; instructions on two numbers at once changed nothing.
-template <int V>
-struct Run {
-  Vec<V> K, B;
+//
+// K itself would not do for a state: 1 - z or K rounded, a step of one at every position and of one sign where gates hardly
+// change, makes a memory of 10^5 positions a thousandth off.  So a run is kept as B and Q = 1 - K, both to some steps of
+// themselves (rounded shares of 1 - z only weigh what has been added), and a state goes to h + (B - Q h).  In fp32 K of its own
+// size too, and the state goes to B + K h where K is at most a half, as behind an open gate, which leaves no rounding of h.
+template <typename T>
+struct Run;
+template <>
+struct Run<__nv_bfloat16> {
+  using G = GateOf<__nv_bfloat16>;
+  using Kept = Run;
+  Vec<2> Q = all<2>(0.f), B = all<2>(0.f);
+  __device__ __forceinline__ Vec<2> of(Vec<2> h) const { return add(h, less(B, Q, h)); }
+  __device__ __forceinline__ void position(const G& g, Vec<2> x) {  // then this one
+    const Vec<2> k = minus(all<2>(1.f), g.z());
+    B = fma(k, B, mul(g.z(), x));
+    Q = fma(k, Q, g.z());
+  }
+  __device__ __forceinline__ void before(const G& g, Vec<2> dy) {  // from the end: before it this one
+    Q = fma(g.z(), minus(all<2>(1.f), Q), Q);
+    B = fma(minus(all<2>(1.f), Q), dy, B);
+  }
+  __device__ __forceinline__ void join(const Run& p) {  // this, then p
+    const Vec<2> k = minus(all<2>(1.f), p.Q);
+    B = fma(k, B, p.B);
+    Q = fma(k, Q, p.Q);
+  }
+  __device__ __forceinline__ Kept kept() const { return *this; }
+  __device__ __forceinline__ float4 packed() const { return make_float4(Q.v[0], Q.v[1], B.v[0], B.v[1]); }
+  __device__ __forceinline__ static Run from(const float4& p) {
+    Run r;
+    r.Q = {p.x, p.y};
+    r.B = {p.z, p.w};
+    return r;
+  }
 };
-template <int V>
-struct alignas(8 * V) Pair {  // as it lies in shared memory
-  float K[V], B[V];
+template <>
+struct Run<float> {
+  using G = GateOf<float>;
+  float K = 1.f, Q = 0.f, B = 0.f;
+  struct Kept {  // in two numbers: share is Q, or -K where K is at most a half
+    float share, B;
+    __device__ __forceinline__ Vec<1> of(Vec<1> h) const {
+      const float t = fmaf(-share, h.v[0], B);
+      return {t + (__float_as_int(share) < 0 ? 0.f : h.v[0])};
+    }
+  };
+  __device__ __forceinline__ Kept kept() const { return {K <= 0.5f ? -K : Q, B}; }
+  __device__ __forceinline__ Vec<1> of(Vec<1> h) const { return kept().of(h); }
+  __device__ __forceinline__ float gate(const G& g) {
+    const float z = g.z().v[0], k = g.k().v[0];
+    K *= k;
+    Q = fmaf(k, Q, z);
+    return k;
+  }
+  __device__ __forceinline__ void position(const G& g, Vec<1> x) { B = fmaf(gate(g), B, g.z().v[0] * x.v[0]); }
+  __device__ __forceinline__ void before(const G& g, Vec<1> dy) {
+    gate(g);
+    B = fmaf(K, dy.v[0], B);
+  }
+  __device__ __forceinline__ void join(const Run& p) {
+    B = fmaf(p.K, B, p.B);
+    Q = fmaf(p.K, Q, p.Q);
+    K *= p.K;
+  }
+  __device__ __forceinline__ float4 packed() const { return make_float4(Q < 0.5f ? 1.f - Q : K, Q, B, 0.f); }
+  __device__ __forceinline__ static Run from(const float4& p) {
+    Run r;
+    r.K = p.x;
+    r.Q = p.y;
+    r.B = p.z;
+    return r;
+  }
 };
 // Runs that a lane joins one after another; of 32, two lanes join sixteen each, and then theirs.
 template <int L>
 constexpr int kJoin = kSubs<L> < 16 ? kSubs<L> : 16;
-template <int V, int L>
+template <int L>
 struct SplitSmem {
-  Pair<V> run[2][kSubs<L>][L];  // the threads' runs, then what is before each among its sixteen
-  Pair<V> half[2][L];           // of the first sixteen of 32
-  Pair<V> tile[2][kMaxCluster][L];
+  float4 run[2][kSubs<L>][L];  // the threads' runs, then what is before each among its sixteen
+  float4 half[2][L];           // of the first sixteen of 32
+  float4 tile[2][kMaxCluster][L];
   uint64_t bar[2];  // a step's tiles have come
 };
-template <int V>
-__device__ __forceinline__ void join(Run<V>& a, const Pair<V>& p) {  // a, then p
-  Vec<V> K, B;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    K.v[v] = p.K[v];
-    B.v[v] = p.B[v];
-  }
-  a.B = fma(K, a.B, B);
-  a.K = mul(a.K, K);
-}
-template <int V>
-__device__ __forceinline__ Vec<V> through(Vec<V> h, const Pair<V>& p) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) h.v[v] = fmaf(p.K[v], h.v[v], p.B[v]);
-  return h;
-}
-template <int V>
-__device__ __forceinline__ Pair<V> pair_of(const Run<V>& r) {
-  Pair<V> p;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    p.K[v] = r.K.v[v];
-    p.B[v] = r.B.v[v];
-  }
-  return p;
-}
 
 __device__ __forceinline__ int cluster_reg_rank() {
   uint32_t r;
@@ -735,22 +827,15 @@ __device__ __forceinline__ void cluster_meet() {
 }
 // To the same place of every CTA of the cluster, counted by the barrier at the same place there.  (A barrier of the
 // whole cluster a step would wait for the rows' stores as well: 1.4 of 6.7 stall cycles an instruction.)
-template <int V>
-__device__ __forceinline__ void hand_out(Pair<V>* slot, uint64_t* bar, const Run<V>& p, int cl) {
+__device__ __forceinline__ void hand_out(float4* slot, uint64_t* bar, const float4& p, int cl) {
   const uint32_t own = tc::smem_u32(slot), own_bar = tc::smem_u32(bar);
   for (int r = 0; r < cl; ++r) {
     uint32_t there, there_bar;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(r));
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(own_bar), "r"(r));
-    if constexpr (V == 2)
-      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
-                       there),
-                   "f"(p.K.v[0]), "f"(p.K.v[1]), "f"(p.B.v[0]), "f"(p.B.v[1]), "r"(there_bar)
-                   : "memory");
-    else
-      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there),
-                   "f"(p.K.v[0]), "f"(p.B.v[0]), "r"(there_bar)
-                   : "memory");
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(there),
+                 "f"(p.x), "f"(p.y), "f"(p.z), "f"(p.w), "r"(there_bar)
+                 : "memory");
   }
 }
 
@@ -771,9 +856,10 @@ __device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity) {
   return false;
 }
 
-template <int V, int L>
+template <typename T, int L>
 struct Split {
-  SplitSmem<V, L>& sm;
+  static constexpr int V = kVec<T>;
+  SplitSmem<L>& sm;
   int* status;
   int cl, rank, tx, ty;
   uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
@@ -781,7 +867,7 @@ struct Split {
   static constexpr int kGroups = kSubs<L> / kJoin<L>, kJoiners = L * kGroups;
   static_assert(kJoiners <= 32, "the joining lanes are in one warp");
 
-  __device__ __forceinline__ Split(SplitSmem<V, L>& s, int* st)
+  __device__ __forceinline__ Split(SplitSmem<L>& s, int* st)
       : sm(s), status(st), cl(cluster_reg_size()), rank(cluster_reg_rank()), tx(threadIdx.x % L), ty(threadIdx.x / L) {
     if (threadIdx.x == 0) {
       tc::mbar_init(&sm.bar[0], 1 + kJoiners);
@@ -794,37 +880,37 @@ struct Split {
   // carried on.  `then` is done by all threads when all have formed their runs.  A CTA hands out step s + 1 after all its
   // threads have read step s, and enters s + 2 after every other one has handed out s + 1: two places are enough.
   template <bool kBack, typename F>
-  __device__ __forceinline__ Vec<V> enter(const Run<V>& mine, Vec<V>& state, int buf, F then) {
+  __device__ __forceinline__ Vec<V> enter(const Run<T>& mine, Vec<V>& state, int buf, F then) {
     auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
-    sm.run[buf][ty][tx] = pair_of(mine);
-    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * L * sizeof(Pair<V>)));
+    sm.run[buf][ty][tx] = mine.packed();
+    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * L * sizeof(float4)));
     __syncthreads();
     if (threadIdx.x < kJoiners) {
       const int group = threadIdx.x / L;
-      Run<V> whole{all<V>(1.f), all<V>(0.f)};
+      Run<T> whole;
 #pragma unroll
       for (int k = 0; k < kJoin<L>; ++k) {
-        Pair<V>& p = sm.run[buf][at(group * kJoin<L> + k, kSubs<L>)][tx];
-        const Pair<V> own = p, before = pair_of(whole);
-        join(whole, own);
-        p = before;
+        float4& p = sm.run[buf][at(group * kJoin<L> + k, kSubs<L>)][tx];
+        const Run<T> own = Run<T>::from(p);
+        p = whole.packed();
+        whole.join(own);
       }
       if constexpr (kGroups == 2) {
-        if (group == 0) sm.half[buf][tx] = pair_of(whole);
-        Run<V> first;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          first.K.v[v] = __shfl_xor_sync(0xffffu, whole.K.v[v], L);
-          first.B.v[v] = __shfl_xor_sync(0xffffu, whole.B.v[v], L);
-        }
-        join(first, pair_of(whole));
+        float4 w = whole.packed();
+        if (group == 0) sm.half[buf][tx] = w;
+        w.x = __shfl_xor_sync(0xffffu, w.x, L);
+        w.y = __shfl_xor_sync(0xffffu, w.y, L);
+        w.z = __shfl_xor_sync(0xffffu, w.z, L);
+        w.w = __shfl_xor_sync(0xffffu, w.w, L);
+        Run<T> first = Run<T>::from(w);
+        first.join(whole);
         whole = first;
       }
       if (group == kGroups - 1) {
         if (cl > 1)
-          hand_out(&sm.tile[buf][rank][tx], &sm.bar[buf], whole, cl);
+          hand_out(&sm.tile[buf][rank][tx], &sm.bar[buf], whole.packed(), cl);
         else
-          sm.tile[buf][0][tx] = pair_of(whole);
+          sm.tile[buf][0][tx] = whole.packed();
       }
       if (cl > 1) tc::mbar_arrive(&sm.bar[buf]);
     }
@@ -836,13 +922,14 @@ struct Split {
       record_device_error(status, tc::kErrTimeout);
     }
     phase ^= 1u << buf;
-    const Pair<V>* t = &sm.tile[buf][0][tx];
+    const float4* t = &sm.tile[buf][0][tx];
+    auto tile = [&](int k) { return Run<T>::from(t[at(k, cl) * L]); };
     int k = 0;
-    for (; at(k, cl) != rank; ++k) state = through(state, t[at(k, cl) * L]);
+    for (; at(k, cl) != rank; ++k) state = tile(k).of(state);
     Vec<V> got = state;
-    if (kGroups == 2 && at(ty, kSubs<L>) >= kJoin<L>) got = through(got, sm.half[buf][tx]);
-    got = through(got, sm.run[buf][ty][tx]);
-    for (; k < cl; ++k) state = through(state, t[at(k, cl) * L]);
+    if (kGroups == 2 && at(ty, kSubs<L>) >= kJoin<L>) got = Run<T>::from(sm.half[buf][tx]).of(got);
+    got = Run<T>::from(sm.run[buf][ty][tx]).of(got);
+    for (; k < cl; ++k) state = tile(k).of(state);
     return got;
   }
 };
@@ -923,8 +1010,8 @@ __global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   extern __shared__ __align__(128) char smem[];
-  __shared__ SplitSmem<V, L> sm;
-  Split<V, L> sp(sm, a.status);
+  __shared__ SplitSmem<L> sm;
+  Split<T, L> sp(sm, a.status);
   const Rows in_rows[2] = {a.x, a.g};
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int items = (int)(a.n * a.blocks), stride = gridDim.x / CL, first = blockIdx.x / CL;
@@ -981,14 +1068,12 @@ __global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
       const char* const tile = smem + stage * 2 * kTileBytes;
       stage = stage + 1 == kFwdStages ? 0 : stage + 1;
       const RunRows<L> px(tile, sub, tx), pg(tile + kTileBytes, sub, tx);
-      Run<V> run[kPos], now{all<V>(1.f), all<V>(0.f)};
+      Run<T> now;
+      typename Run<T>::Kept run[kPos];
 #pragma unroll
       for (int u = 0; u < kPos; ++u) {
-        const GateOf<T> gt(piece(pg[u], T{}), b);
-        const Vec<V> k = gt.k();
-        now.B = fma(k, now.B, mul(gt.z(), piece(px[u], T{})));
-        now.K = mul(now.K, k);
-        run[u] = now;
+        now.position(GateOf<T>(piece(pg[u], T{}), b), piece(px[u], T{}));
+        run[u] = now.kept();
       }
       tc::cp_async_wait<kFwdStages - 3>();
       const Vec<V> h0 = sp.template enter<false>(now, h, buf, ask);
@@ -997,11 +1082,11 @@ __global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
       T* py = y + t0 * a.y.st;
       if (left == kPos) {
 #pragma unroll
-        for (int u = 0; u < kPos; ++u, py += a.y.st) st4(py, fma(run[u].K, h0, run[u].B));
+        for (int u = 0; u < kPos; ++u, py += a.y.st) st4(py, run[u].of(h0));
       } else {
 #pragma unroll
         for (int u = 0; u < kPos; ++u, py += a.y.st)
-          if (u < left) st4(py, fma(run[u].K, h0, run[u].B));
+          if (u < left) st4(py, run[u].of(h0));
       }
     }
     if (!in) continue;
@@ -1020,9 +1105,9 @@ __global__ __launch_bounds__(kSplitThr, 1) void recur_bwd_split(RecurArgs a) {
   pdl_begin();
   constexpr int V = kVec<T>;
   extern __shared__ __align__(128) char smem[];
-  __shared__ SplitSmem<V, L> sm;
+  __shared__ SplitSmem<L> sm;
   __shared__ float sh[256 * V];
-  Split<V, L> sp(sm, a.status);
+  Split<T, L> sp(sm, a.status);
   const Rows in_rows[3] = {a.x, a.g, a.dy};
   const int CL = sp.cl, rank = sp.rank, tx = sp.tx, sub = sp.ty;
   const int64_t item = blockIdx.x / CL, i = item / a.blocks;
@@ -1064,14 +1149,13 @@ __global__ __launch_bounds__(kSplitThr, 1) void recur_bwd_split(RecurArgs a) {
     Vec<V> h = ahead;
     if (s + 1 < steps) ahead = before(start(s + 1) + sub * kPos);
     Vec<V> sl[kPos], code[kPos];
-    Run<V> run{all<V>(1.f), zero};  // B = sum of dy_u times the product of k up to u
+    Run<T> run;  // B = sum of dy_u times the product of 1 - z up to u
 #pragma unroll
     for (int u = 0; u < kPos; ++u) {
       const GateOf<T> gt(piece(qg[u], T{}), b);
       code[u] = gt.code();
       sl[u] = slope(h, piece(qx[u], T{}), gt);
-      run.K = mul(run.K, gt.k());
-      run.B = fma(run.K, piece(qy[u], T{}), run.B);
+      run.before(gt, piece(qy[u], T{}));
     }
     tc::cp_async_wait<kBwdStages - 3>();
     Vec<V> r = sp.template enter<true>(run, R, s & 1, [&] { ask(s + kBwdStages - 1); }), here = zero;
@@ -1270,7 +1354,10 @@ hg_status forward(RecurArgs& a, SplitHow how, cudaStream_t s) {
   if (how.lanes == 0) {
     const Shape sh = shape_of(a.d / Wide<T>::E);
     const int64_t groups = ceil_div(a.n, sh.block.y), most = std::max<int64_t>(1, 2 * 152 / sh.across);
-    return launch("recur_fwd", recur_fwd<T>, dim3((unsigned)std::min(groups, most), sh.across), sh.block, 0, s, a);
+    const dim3 grid((unsigned)std::min(groups, most), sh.across);
+    if constexpr (sizeof(T) == 4)
+      if (a.T > kPos) return launch("recur_fwd", recur_fwd<T, true>, grid, sh.block, 0, s, a);
+    return launch("recur_fwd", recur_fwd<T, false>, grid, sh.block, 0, s, a);
   }
   a.blocks = (int32_t)ceil_div(lanes, how.lanes);
   return how.lanes == 16 ? forward_split<T, 16>(a, how.cl, how.held, s) : forward_split<T, 8>(a, how.cl, how.held, s);
