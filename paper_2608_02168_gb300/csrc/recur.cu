@@ -3,7 +3,8 @@
 //   z_t = sigmoid(g_t + b),  h_t = h_(t-1) + z_t (x_t - h_(t-1)),
 // and, from the end, with R_t = dy_t + (1 - z_(t+1)) R_(t+1):
 //   dx_t = z_t R_t,  dg_t = R_t (x_t - h_(t-1)) z_t (1 - z_t),  db = sum of dg.
-// The difference form's share z is known to a few steps of its own size, so long memories (z = 1e-5) keep their weights.
+// A share z is known to a few steps of its own size, and a state or R goes on by what z changes of it, never by a product
+// with a rounded 1 - z, so long memories (z = 1e-5) keep their weights.
 //
 // Each value is read and written once and costs two special functions and some ten other instructions: all forms are
 // bound by HBM, or by latency where there are few chains.
@@ -94,7 +95,7 @@ __device__ __forceinline__ Vec<V> minus(Vec<V> a, Vec<V> b) {
   return a;
 }
 
-// a + rest as its sum and what that leaves of it.
+// A sum kept as a + rest: as one number and what that leaves of it.
 template <int V>
 __device__ __forceinline__ void settle(Vec<V>& a, Vec<V>& rest) {
   const Vec<V> sum = add(a, rest);
@@ -331,6 +332,10 @@ struct Wide {
   }
 };
 
+// kTwo (fp32 of more than 16 positions): the state in two numbers, joined every four positions, so that what a small z adds is
+// not rounded to a step of the state every time (an equal sign there makes z = 1e-6 some 1e-3 off in 30000 positions; 3000
+// histories of 1000, d 128: no change in time).  In bf16 that takes 20 % more time (registers), and a state is rounded at
+// every position.
 // A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's length
 // and state, are on their way while these ones' gates are computed (a sequence a thread: 203 us).  Bound by HBM: 150001
 // ragged histories of up to 12, d 128, bf16, 156 us, 0.94 of the copy rate.
@@ -464,7 +469,8 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
 // kept before them; the 16 before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128 threads, three an SM: ragged histories
 // leave fewer threads waiting for the longest one than in 256, and 12 warps hide more than 8 (400 of up to 515, d 256,
 // 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers bound it:
-// 16 positions' gates and slopes, and the next rows.
+// 16 positions' gates and slopes, and the next rows (bf16: 64 bytes of them are spilled).  In fp32 R is kept in two numbers,
+// joined every 16 positions, as the forward's state is (3000 of 1000, d 128: 1.21 -> 1.24 ms; not in bf16).
 constexpr int kBwdThr = 128;
 template <typename T>
 __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
@@ -716,20 +722,20 @@ __global__ __launch_bounds__(kBwdThr, kShortCtas) void recur_bwd_short(RecurArgs
 // bytes and 256 positions a tile; where even eight CTAs a piece leave SMs idle, 32 bytes and 512; in the backward, whose
 // three arrays in and two out touch half as many lines so, mostly 128 bytes and 128 positions.  A thread has 16
 // positions of 4 bytes.  Positions compose: a run of them maps the state h before it to B + K h, B its end from a zero
-// state, K the product of its 1 - z (off by a step each, as a state is that is rounded at every position).  Threads form
-// the runs of their 16 positions and keep B and K of each, a CTA forms that of its tile and hands it to the cluster's
-// others (distributed shared memory), and every CTA joins them in the same order, so all carry the same state and a call
-// repeats its bits.
+// state, K the product of its 1 - z.  Threads form the runs of their 16 positions and keep each, a CTA forms that of its
+// tile and hands it to the cluster's others (distributed shared memory), and every CTA joins them in the same order, so all
+// carry the same state and a call repeats its bits.
 //
 // A step of a CTA alone takes 1.75 us, one after another: copies into shared memory 0.55, gates 0.5, the join 0.4, stores
 // 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6 histories
 // of 32768, d 256, bf16: 86 us forward (HBM: 44).  Half as many positions a thread and twice as many threads took 97 us
 // where this took 83; instructions on two numbers at once changed nothing.
 //
-// K itself would not do for a state: 1 - z or K rounded, a step of one at every position and of one sign where gates hardly
-// change, makes a memory of 10^5 positions a thousandth off.  So a run is kept as B and Q = 1 - K, both to some steps of
-// themselves (rounded shares of 1 - z only weigh what has been added), and a state goes to h + (B - Q h).  In fp32 K of its own
-// size too, and the state goes to B + K h where K is at most a half, as behind an open gate, which leaves no rounding of h.
+// K itself would not do for a state: 1 - z rounded, a step of one at every position and of one sign where gates hardly
+// change, makes a memory of 10^5 positions a thousandth off (an eighth more instructions an output; 6 histories of 32768, d
+// 256, bf16: 85 -> 87 us).  So a run is kept as B and Q = 1 - K, both to some steps of themselves (rounded shares of 1 - z only
+// weigh what has been added), and a state goes to h + (B - Q h).  In fp32 K of its own size too, and the state goes to B + K h
+// where K is at most a half, as behind an open gate, which leaves no rounding of h.
 template <typename T>
 struct Run;
 template <>
