@@ -16,6 +16,7 @@
 // The backward reads x, g, dy and every 16th state, which the forward kept, and forms the states between anew: 0.25 bytes
 // a value more in either pass, where reading the states (4 bytes) or a second forward pass (2 b) would be more.
 #include <algorithm>
+#include <cfloat>
 
 #include "ffn_kernels.cuh"
 #include "layer_kernels.cuh"
@@ -109,18 +110,21 @@ __device__ __forceinline__ Vec<V> less(Vec<V> c, Vec<V> a, Vec<V> b) {  // c - a
   return c;
 }
 
-// z = sigmoid(g + b) and k = 1 - z.  The logit's product with -log2 e and the sum with the bias's are one instruction.
+// z = sigmoid(g + b) and k = 1 - z, with a bias as Gate::bias gives it.
 constexpr float kLog2e = 1.4426950408889634f;
 
 // fp32 rows: z and k each to a few steps of their own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero from
 // |a| = 87 on), 1 - s the other, and an update is the nearer end plus the smaller share of the difference: a state that
-// an open gate has just left does not leave its rounding behind.
+// an open gate has just left does not leave its rounding behind.  The bias is added first: its product with log2 e, rounded,
+// would be |b| 2^-24 of z off, also where g and b cancel.
 template <int V, bool kExact>
 struct Gate {
   Vec<V> s, big;
   bool open[V];
+  // An infinite bias is the largest, so that -infinity plus it stays what it is (NaN too).
+  __device__ __forceinline__ static float bias(float b) { return isinf(b) ? copysignf(FLT_MAX, b) : b; }
   __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
-    const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
+    const Vec<V> a = mul(add(g, bias), all<V>(-kLog2e));
 #pragma unroll
     for (int i = 0; i < V; ++i) s.v[i] = gate_ex2(-fabsf(a.v[i]));
     Vec<V> r = add(s, all<V>(1.f));
@@ -178,10 +182,13 @@ struct Gate {
 };
 
 // bf16 rows, whose bytes are half as many and whose instructions therefore count (5 a gate instead of 9): z to a few steps
-// of its own size, 1 - z to a few of one, which is a rounding of the state that it keeps.
+// of its own size (and |b| 2^-24), 1 - z to a few of one, which is a rounding of the state that it keeps.  The logit's product
+// with -log2 e and the sum with the bias's are one instruction.
 template <int V>
 struct Gate<V, false> {
   Vec<V> e, r;
+  // An infinite bias is a large one.
+  __device__ __forceinline__ static float bias(float b) { return -kLog2e * (isinf(b) ? copysignf(1e30f, b) : b); }
   __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
     const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
 #pragma unroll
@@ -246,16 +253,12 @@ __device__ __forceinline__ T* at_out(const Rows& r, int64_t i, int64_t t, int c)
   return const_cast<T*>(at<T>(r, i, t, c));
 }
 
-// As the gates take it.  An infinite bias is a large one, so that -infinity plus it stays what it is (NaN too).
-__device__ __forceinline__ float gate_bias(float b) {
-  return -kLog2e * (isinf(b) ? copysignf(1e30f, b) : b);
-}
 template <typename T>
 __device__ __forceinline__ Vec<kVec<T>> bias_of(const RecurArgs& a, int c) {
   Vec<kVec<T>> b = all<kVec<T>>(0.f);
   if (a.bias) b = piece(ld4(static_cast<const T*>(a.bias) + c), T{});
 #pragma unroll
-  for (int v = 0; v < kVec<T>; ++v) b.v[v] = gate_bias(b.v[v]);
+  for (int v = 0; v < kVec<T>; ++v) b.v[v] = GateOf<T>::bias(b.v[v]);
   return b;
 }
 template <int V>
@@ -343,6 +346,7 @@ template <typename T, bool kTwo>
 __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   pdl_begin();
   using W = Wide<T>;
+  using G = Gate<2, sizeof(T) == 4>;
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W::E;
   const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
   if (c >= a.d || first >= a.n) return;
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   if (a.bias) {
     b.unpacked(ld16(static_cast<const T*>(a.bias) + c));
 #pragma unroll
-    for (int k = 0; k < W::N; ++k) b.v[k] = {gate_bias(b.v[k].v[0]), gate_bias(b.v[k].v[1])};
+    for (int k = 0; k < W::N; ++k) b.v[k] = {G::bias(b.v[k].v[0]), G::bias(b.v[k].v[1])};
   }
   // the loads' place: sequence, position, rows
   int64_t li = first, lt = 0, llen = length(a, li), after = li + step < a.n ? length(a, li + step) : 0;
@@ -407,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
         fg.unpacked(rg[u]);
 #pragma unroll
         for (int k = 0; k < W::N; ++k) {
-          const Gate<2, sizeof(T) == 4> gt(fg.v[k], b.v[k]);
+          const G gt(fg.v[k], b.v[k]);
           if constexpr (kTwo) {
             gt.next(h.v[k], rest.v[k], add(h.v[k], rest.v[k]), fx.v[k]);
             fx.v[k] = add(h.v[k], rest.v[k]);
@@ -1234,7 +1238,10 @@ __global__ __launch_bounds__(256) void recur_step(RecurArgs a) {
       if (a.bias) unpack(ld16(static_cast<const T*>(a.bias) + c + q * E / Q), b + q * E / Q, T{});
     }
 #pragma unroll
-    for (int v = 0; v < E; ++v) o[v] = h[v] = Gate<1, true>(Vec<1>{g[v]}, Vec<1>{gate_bias(b[v])}).next(Vec<1>{h[v]}, Vec<1>{x[v]}).v[0];
+    for (int v = 0; v < E; ++v) {
+      using G = Gate<1, true>;
+      o[v] = h[v] = G(Vec<1>{g[v]}, Vec<1>{G::bias(b[v])}).next(Vec<1>{h[v]}, Vec<1>{x[v]}).v[0];
+    }
   }
   T* yp = at_out<T>(a.y, i, 0, c);
 #pragma unroll

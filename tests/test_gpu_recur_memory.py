@@ -84,3 +84,40 @@ def test_gates_of_small_spread(dt, T):
     near(o["dx"], want["dx"], mag["dx"], (U[dt], e + 40 * F32), "dx")
     near(o["dg"], want["dg"], mag["dg"], (U[dt], 2 * e + 200 * F32), "dg")
     near(o["dh"], want["dh_in"], mag["dh_in"], (F32, e), "dh_in")
+
+
+@pytest.mark.parametrize("T", [1, 40, 700])
+def test_biases_and_logits_that_cancel(T):
+    """fp32: a gate is that of the sum of logit and bias, to (3 |a| + 12) s of itself (the sum's rounding, and as above),
+    however large the two are.  With inputs of one and a state of zero, y_t = 1 - (1 - z)^(t + 1), and a run's own roundings
+    (100 s)."""
+    need_gpu()
+    hg = lib()
+    pairs = [(60.3, -60.3), (-77.3, -3.1), (-3.1, -77.3), (1000.1, -1000.1), (-1000.1, 990.0), (70.7, -75.2), (5e8, -5e8),
+             (-1e6, 1e6 + 4)]
+    g, b = (np.array(v, np.float32) for v in zip(*pairs))
+    d, n = 8, 2
+    p = hg.RecurParams(dev(b))
+    G, X = dev(g).expand(n, T, d), torch.ones(n, T, d, device="cuda")
+    y, h = nans((n, T, d), torch.float32), nans((n, d), torch.float32)
+    hg.hg_recur_fwd(p, X, G, None, None, y, h, None)
+    a = f64(g) + f64(b)
+    z = 1 / (1 + np.exp(-a))
+    t = np.arange(1, T + 1)[:, None]
+    want = -np.expm1(t * np.log1p(-z))
+    rel = (3 * np.abs(a) + 112) * F32
+    assert (np.abs(y.double().cpu().numpy() - want) <= rel * want).all()
+    # the state goes through whole tiles, a row through its own run: other sums, each within the same bound
+    assert (np.abs(h.double().cpu().numpy() - want[-1]) <= rel[None] * want[-1]).all()
+    s = torch.zeros(n, d, device="cuda")
+    hg.hg_recur_step(p, X[:, 0], G[:, 0], None, s, y[:, 0])
+    assert (np.abs(s.double().cpu().numpy() - z) <= (3 * np.abs(a) + 12) * F32 * z).all()
+    # and the gradients: of ones at the end z (1 - z)^(T - 1 - t) is left, whose logarithm follows z by T - t times its share
+    saved, scratch = (torch.empty(v, dtype=torch.uint8, device="cuda") for v in hg.hg_recur_workspace_size(p, n, T))
+    hg.hg_recur_fwd(p, X, G, None, None, y, h, saved)
+    dx, dg, dh = nans((n, T, d), torch.float32), nans((n, T, d), torch.float32), nans((n, d), torch.float32)
+    one = torch.ones(n, d, device="cuda")
+    hg.hg_recur_bwd(p, X, G, None, None, saved, torch.zeros(n, T, d, device="cuda"), one, dx, dg, dh, None, None)
+    left = np.exp((T - t) * np.log1p(-z))
+    off = rel * (1 + 2 * (T - t) * z)
+    assert (np.abs(dx.double().cpu().numpy() - z * left) <= (off + rel) * z * left + 1e-37).all()
