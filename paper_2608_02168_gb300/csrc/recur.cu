@@ -187,8 +187,8 @@ struct Gate {
 template <int V>
 struct Gate<V, false> {
   Vec<V> e, r;
-  // An infinite bias is a large one.
-  __device__ __forceinline__ static float bias(float b) { return -kLog2e * (isinf(b) ? copysignf(1e30f, b) : b); }
+  // One above 1e38 is as good as that, and its product stays finite, so that -infinity plus it stays what it is (NaN too).
+  __device__ __forceinline__ static float bias(float b) { return -kLog2e * (fabsf(b) > 1e38f ? copysignf(1e38f, b) : b); }
   __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
     const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
 #pragma unroll

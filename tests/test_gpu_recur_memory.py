@@ -121,3 +121,29 @@ def test_biases_and_logits_that_cancel(T):
     left = np.exp((T - t) * np.log1p(-z))
     off = rel * (1 + 2 * (T - t) * z)
     assert (np.abs(dx.double().cpu().numpy() - z * left) <= (off + rel) * z * left + 1e-37).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T,d", [(40, 12, 64), (300, 70, 64), (3, 900, 40)])
+def test_biases_near_the_largest_number(dt, n, T, d):
+    """A bias of +-3e38 is one that no logit moves, with ragged histories: z is 1 or 0."""
+    need_gpu()
+    hg = lib()
+    td = tdtype(dt)
+    rng = np.random.default_rng(7)
+    x, g, dy = (draw(rng, dt, n, T, d) for _ in range(3))
+    h, dh = rng.standard_normal((2, n, d)).astype(np.float32)
+    lens = rng.integers(0, T + 1, n).astype(np.int32)
+    lens[0], lens[-1] = 0, T
+    b = np.zeros(d, np.float32)
+    b[1], b[2] = 3e38, -3e38
+    X, H, L = dev(x, td), dev(h), dev(lens)
+    o = run(hg, hg.RecurParams(dev(b, td)), td, X, dev(g, td), L, H, dev(dy, td), dev(dh), n, T, d)
+    live = torch.arange(T, device="cuda") < L[:, None]
+    assert all(torch.isfinite(v).all() for v in o.values())
+    assert torch.equal(o["y"][..., 2], (H[:, None, 2] * live).to(td)) and torch.equal(o["h"][:, 2], H[:, 2])
+    # an open gate leaves the value to a step of it, or in bf16 of what was there (x, state and their difference: 6 steps)
+    most = max(np.abs(x).max(), np.abs(h).max())
+    want = X[..., 1].double() * live
+    assert ((o["y"][..., 1].double() - want).abs() <= U[dt] * want.abs() + (6 * F32 * most if dt == "bf16" else 0)).all()
+    assert (o["dx"][..., 2] == 0).all() and (o["dg"][..., 1:3] == 0).all() and (o["db"][1:3] == 0).all()
