@@ -274,34 +274,53 @@ def _places(rows_sorted, ids, n):
     return table[ids]
 
 
-def _row_aggregates(src, dst, rel, valid, rows_sorted, H, R, chunk=1 << 20):
+def _among(ids, rows, n):
+    """Mask of the ids that are among `rows` (an id out of range counts as the nearest in it: valid_edges drops it)."""
+    table = np.zeros(max(n, 1), bool)
+    table[rows] = True
+    return np.take(table, ids, mode="clip")
+
+
+def _edges(src, dst, rel, pick, type_offsets, rels):
+    """Ends and relation of the valid edges among the picked ones, in their order."""
+    e = np.flatnonzero(pick)
+    s, t, r = (np.asarray(x)[e].astype(np.int64) for x in (src, dst, rel))
+    ok = valid_edges(s, t, r, type_offsets, rels)
+    return s[ok], t[ok], r[ok]
+
+
+def _sums(keys, values, n, d, chunk=1 << 20):
+    """Sums of values(edges), one row an edge, by key in [0, n)."""
+    S = np.zeros((n, d), F64)
+    order = np.argsort(keys, kind="stable")
+    for s in range(0, order.shape[0], chunk):
+        o = order[s:s + chunk]
+        k = keys[o]
+        v = values(o)
+        at = np.flatnonzero(np.concatenate([[True], k[1:] != k[:-1]]))
+        for key, i, j in zip(k[at], at, np.append(at[1:], o.shape[0])):  # (reduceat takes eight times as long)
+            S[key] += v[i:j].sum(axis=0, dtype=F64)
+    return S
+
+
+def _row_aggregates(src, dst, rel, type_offsets, rels, rows_sorted, H):
     """For sorted node ids `rows_sorted`: S[k, r] = sum of H[src] over valid in-edges of relation r
     into rows_sorted[k], and deg[k, r] their count."""
-    n = rows_sorted.shape[0]
-    d = H.shape[1]
-    S = np.zeros((n, R, d), F64)
-    deg = np.zeros((n, R), np.int64)
-    pos_c = _places(rows_sorted, np.where(valid, dst, 0), H.shape[0])
-    e = np.flatnonzero(valid & (pos_c >= 0))
-    np.add.at(deg, (pos_c[e], rel[e]), 1)
-    for s in range(0, e.shape[0], chunk):
-        ec = e[s:s + chunk]
-        np.add.at(S, (pos_c[ec], rel[ec]), np.asarray(H[src[ec]], F64))
-    return S, deg
+    n, R, d, N = rows_sorted.shape[0], len(rels), H.shape[1], int(type_offsets[-1])
+    s, t, r = _edges(src, dst, rel, _among(dst, rows_sorted, N), type_offsets, rels)
+    key = _places(rows_sorted, t, N).astype(np.int64) * R + r
+    S = _sums(key, lambda e: H[s[e]], n * R, d)
+    return S.reshape(n, R, d), np.bincount(key, minlength=n * R).reshape(n, R)
 
 
 def layer_forward_rows(src, dst, rel, type_offsets, rels, params, H, rows, act="relu",
                        layernorm=True, ln_eps=1e-5, store="f64") -> tuple:
     """layer_forward evaluated only at node ids `rows` (sorted, unique), straight from the COO list.
     Returns (H_out[rows], cache) with per-row M (n x R x d), Z, U, deg, Xh, rstd."""
-    src = np.asarray(src, np.int64)
-    dst = np.asarray(dst, np.int64)
-    rel = np.asarray(rel, np.int64)
     p = _p64(params)
     rows = np.asarray(rows, np.int64)
-    valid = valid_edges(src, dst, rel, type_offsets, rels)
     R = len(rels)
-    S, deg = _row_aggregates(src, dst, rel, valid, rows, H, R)
+    S, deg = _row_aggregates(src, dst, rel, type_offsets, rels, rows, H)
     M = _stored(np.where(deg[:, :, None] > 0, S / np.maximum(deg, 1)[:, :, None], 0.0), store)
     ty = node_type(rows, type_offsets)
     d = H.shape[1]
@@ -310,8 +329,11 @@ def layer_forward_rows(src, dst, rel, type_offsets, rels, params, H, rows, act="
     for r in range(R):
         m = ty == rt[r]
         Z[m] += M[m, r] @ p["W_rel"][r]
-    U = _stored(np.einsum("nk,nkj->nj", Z, p["W_agg"][ty]), store) + p["b_agg"][ty]
-    Y = act_fwd(U, act) + np.asarray(H, F64)[rows]
+    U = np.zeros_like(Z)
+    for t in range(len(type_offsets) - 1):
+        m = ty == t
+        U[m] = _stored(Z[m] @ p["W_agg"][t], store) + p["b_agg"][t]
+    Y = act_fwd(U, act) + np.asarray(H[rows], F64)
     cache = dict(M=M, Z=Z, U=U, Y=Y, deg=deg, ty=ty)
     if layernorm:
         mu = Y.mean(axis=1, keepdims=True)
@@ -328,9 +350,6 @@ def layer_backward_rows(src, dst, rel, type_offsets, rels, params, H, S_rows, dH
     """layer_backward for an upstream gradient that is zero except on the sorted node ids S_rows
     (values dH_S).  Returns (dH_in[query_rows], grads); the weight gradients are complete because
     only rows in S_rows contribute to them."""
-    src = np.asarray(src, np.int64)
-    dst = np.asarray(dst, np.int64)
-    rel = np.asarray(rel, np.int64)
     p = _p64(params)
     S_rows = np.asarray(S_rows, np.int64)
     query_rows = np.asarray(query_rows, np.int64)
@@ -352,7 +371,10 @@ def layer_backward_rows(src, dst, rel, type_offsets, rels, params, H, S_rows, dH
     else:
         dY = dout
     dU = dY * act_grad(c["U"], act)
-    dZ = np.einsum("nj,nkj->nk", dU, p["W_agg"][ty])
+    dZ = np.zeros_like(dU)
+    for t in range(T):
+        m = ty == t
+        dZ[m] = dU[m] @ p["W_agg"][t].T
     rt = np.array([r[1] for r in rels])
     dMs = np.zeros((S_rows.shape[0], R, d), F64)  # dM_r[j] / deg_r(j)
     for t in range(T):
@@ -371,12 +393,11 @@ def layer_backward_rows(src, dst, rel, type_offsets, rels, params, H, S_rows, dH
     kc = np.minimum(k, S_rows.shape[0] - 1)
     ins = S_rows[kc] == query_rows
     out[ins] += dY[kc[ins]]
-    valid = valid_edges(src, dst, rel, type_offsets, rels)
     N = int(type_offsets[-1])
-    qc = _places(query_rows, np.where(valid, src, 0), N)
-    sc = _places(S_rows, np.where(valid, dst, 0), N)
-    e = np.flatnonzero(valid & (qc >= 0) & (sc >= 0))
-    np.add.at(out, qc[e], dMs[sc[e], rel[e]])
+    pick = _among(dst, S_rows, N) & _among(src, query_rows, N)
+    s, t, r = _edges(src, dst, rel, pick, type_offsets, rels)
+    sc = _places(S_rows, t, N)
+    out += _sums(_places(query_rows, s, N), lambda e: dMs[sc[e], r[e]], query_rows.shape[0], d)
     return out, g
 
 
@@ -388,33 +409,43 @@ def standardise(X: np.ndarray, eps: float) -> tuple:
     added to the variance.  Returns (H_hat, mu, s) with s = sqrt(var + eps)."""
     n = X.shape[0]
     mu = X.mean(axis=0)
-    var = ((X - mu) ** 2).mean(axis=0)
-    s = np.sqrt(var + eps)
-    return (X - mu) / (s * np.sqrt(n)), mu, s
+    Z = X - mu
+    s = np.sqrt(np.einsum("ij,ij->j", Z, Z) / n + eps)
+    Z /= s * np.sqrt(n)
+    return Z, mu, s
 
 
 def align_forward(Ha, idx_a, Hb, idx_b, lambda_n: float = 2e-4, eps: float = 1e-8) -> tuple:
     """L_CCA = ||Z_a - Z_b||_F^2 + lambda_n (||Z_a^T Z_a - I||_F^2 + ||Z_b^T Z_b - I||_F^2)
     (Eq. 15, 16, 17) on Z = standardised overlap rows (Eq. 14).  Returns (L, L_inv, L_dec)."""
-    A = np.asarray(Ha, F64)[np.asarray(idx_a, np.int64)]
-    B = np.asarray(Hb, F64)[np.asarray(idx_b, np.int64)]
-    Za, _, _ = standardise(A, eps)
-    Zb, _, _ = standardise(B, eps)
-    I = np.eye(A.shape[1])
-    l_inv = float(((Za - Zb) ** 2).sum())
+    Za, _, _ = standardise(np.asarray(Ha, F64)[np.asarray(idx_a, np.int64)], eps)
+    Zb, _, _ = standardise(np.asarray(Hb, F64)[np.asarray(idx_b, np.int64)], eps)
+    I = np.eye(Za.shape[1])
     l_dec = float(((Za.T @ Za - I) ** 2).sum() + ((Zb.T @ Zb - I) ** 2).sum())
+    Za -= Zb
+    l_inv = float(np.einsum("ij,ij->", Za, Za))
     return l_inv + lambda_n * l_dec, l_inv, l_dec
 
 
 def _standardise_backward(X: np.ndarray, G: np.ndarray, eps: float) -> np.ndarray:
-    """Gradient through Eq. 14: with x_hat = (h - mu)/s and g = dL/dx_hat = G / sqrt(n),
+    """Gradient through Eq. 14 for G = dL/dZ at the rows X."""
+    Z, _, s = standardise(X, eps)
+    return _through(Z, s, np.array(G, F64))
+
+
+def _through(Z: np.ndarray, s: np.ndarray, G: np.ndarray) -> np.ndarray:
+    """The same from Z, G overwritten: with x_hat = sqrt(n) Z and g = dL/dx_hat = G / sqrt(n),
     dL/dh = (1/s) (g - mean(g) - x_hat * mean(g * x_hat)) per column (s depends on h through var)."""
-    n = X.shape[0]
-    mu = X.mean(axis=0)
-    s = np.sqrt(((X - mu) ** 2).mean(axis=0) + eps)
-    xh = (X - mu) / s
-    g = G / np.sqrt(n)
-    return (g - g.mean(axis=0) - xh * (g * xh).mean(axis=0)) / s
+    along, mean = np.einsum("ij,ij->j", G, Z), G.mean(axis=0)
+    for b in _blocks(Z.shape[0]):
+        G[b] -= mean + Z[b] * along
+        G[b] /= s * np.sqrt(Z.shape[0])
+    return G
+
+
+def _blocks(n, rows=1 << 13):
+    """Rows a few at a time: what is made of them stays in the cache."""
+    return (slice(i, i + rows) for i in range(0, n, rows))
 
 
 def align_backward(Ha, idx_a, Hb, idx_b, lambda_n: float = 2e-4, eps: float = 1e-8,
@@ -424,18 +455,19 @@ def align_backward(Ha, idx_a, Hb, idx_b, lambda_n: float = 2e-4, eps: float = 1e
     with the sign of the invariance term flipped."""
     idx_a = np.asarray(idx_a, np.int64)
     idx_b = np.asarray(idx_b, np.int64)
-    A = np.asarray(Ha, F64)[idx_a]
-    B = np.asarray(Hb, F64)[idx_b]
-    Za, _, _ = standardise(A, eps)
-    Zb, _, _ = standardise(B, eps)
-    I = np.eye(A.shape[1])
-    Ga = dloss * (2.0 * (Za - Zb) + 4.0 * lambda_n * Za @ (Za.T @ Za - I))
-    Gb = dloss * (-2.0 * (Za - Zb) + 4.0 * lambda_n * Zb @ (Zb.T @ Zb - I))
-    dHa = np.zeros(np.shape(Ha), F64)
-    dHb = np.zeros(np.shape(Hb), F64)
-    dHa[idx_a] = _standardise_backward(A, Ga, eps)
-    dHb[idx_b] = _standardise_backward(B, Gb, eps)
-    return dHa, dHb
+    Za, _, sa = standardise(np.asarray(Ha, F64)[idx_a], eps)
+    Zb, _, sb = standardise(np.asarray(Hb, F64)[idx_b], eps)
+    I = np.eye(Za.shape[1])
+    out = []
+    for H, idx, Z, other, s in ((Ha, idx_a, Za, Zb, sa), (Hb, idx_b, Zb, Za, sb)):
+        P = dloss * (2.0 * I + 4.0 * lambda_n * (Z.T @ Z - I))
+        G = np.empty_like(Z)
+        for b in _blocks(Z.shape[0]):
+            G[b] = Z[b] @ P - 2.0 * dloss * other[b]
+        dH = np.zeros(np.shape(H), F64)
+        dH[idx] = _through(Z, s, G)
+        out.append(dH)
+    return tuple(out)
 
 
 def overlap_intersect(gid_a, gid_b) -> tuple:
