@@ -660,7 +660,7 @@ typedef struct {
 } hg_recur_params;
 
 /* Bytes of `saved` (written by hg_recur_fwd for hg_recur_bwd: the state before every 16th position; zero up to T = 16)
- * and of the backward's scratch, for n sequences of up to T positions. */
+ * and of the backward's scratch, for n sequences of up to T positions; enough for fewer and for smaller T as well. */
 hg_status hg_recur_workspace_size(const hg_recur_params* params, int64_t n, int64_t T, size_t* saved_bytes,
                                   size_t* scratch_bytes);
 

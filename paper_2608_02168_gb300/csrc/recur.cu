@@ -1273,6 +1273,7 @@ Shape shape_of(int64_t lanes, int threads = 256, int unit = 1) {  // rows of up 
 // 1001, d 200, forward 192 / 36 us; 400 of up to 515, d 256, 112 / 66; 1000 of 100, d 128, 28 / 50; backward 80 / 57,
 // 85 / 109, 31 / 72.  By clusters of 1, 2, 3, 4, 6 and 8, 6 histories of 32768, d 256: forward 191, 105, 84, 77, 134, 99;
 // backward with pieces of 128 bytes 474, 246, 172, 132, 185, 148 (64 bytes: 262, 139, 146, 146, 168, 199).
+constexpr int64_t kMaxPartRows = 4096;  // of the split backward (some 3000 sequences and more are faster as chains)
 struct SplitHow {
   int lanes, cl, held;  // lanes 0: a chain a thread
 };
@@ -1292,6 +1293,7 @@ SplitHow split_of(const hg_recur_params* p, int64_t n, int64_t T, bool back) {
     const int64_t items = n * ceil_div(lanes, L), tile = kSplitThr / L * kPos;
     if (items >= int64_t(1) << 28) break;
     for (int c = 1; c <= kMaxCluster; ++c) {
+      if (back && n * c > kMaxPartRows) break;
       const int h = held[back][c - 1];
       const double step = (back ? 2.05 + 0.06 * (c - 1) : 1.5 + 0.09 * (c - 1)) + (L == 8 ? 0.2 : L == 32 ? -0.2 : 0);
       const double w = items / h * waves(h, c) + (items % h ? waves(items % h, c) : 0);
@@ -1310,14 +1312,22 @@ int short_ctas(const hg_recur_params* p, int64_t T) {
   const int bytes = p->dtype == HG_BF16 ? short_bytes<__nv_bfloat16>(T) : short_bytes<float>(T);
   return std::min(kShortCtas, (227 << 10) / (bytes + (2 << 10)));
 }
-// Rows of partial sums of the bias's gradient.
+// Rows of partial sums of the bias's gradient: chains' CTAs.  Short histories: as many as run at once, each from one to the
+// next; long ones differ too much for that.
+int64_t chain_rows(const hg_recur_params* p, int64_t n, int64_t T) {
+  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr, 4);
+  const int64_t most = T <= kPos ? 152 * short_ctas(p, T) : T <= 64 ? 152 * 3 : 152 * 16;
+  return std::min(ceil_div(n, s.block.y), std::max<int64_t>(1, most / s.across));
+}
 int64_t part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const SplitHow how = split_of(p, n, T, true);
-  if (how.lanes) return n * how.cl;
-  const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr, 4);
-  // short histories: as many CTAs as run at once, each from one to the next; long ones differ too much for that
-  const int64_t groups = ceil_div(n, s.block.y), most = std::max<int64_t>(1, (T <= kPos ? 152 * short_ctas(p, T) : T <= 64 ? 152 * 3 : 152 * 16) / s.across);
-  return std::min(groups, most);
+  return how.lanes ? n * how.cl : chain_rows(p, n, T);
+}
+// No fewer than of any n and T up to these.
+int64_t most_part_rows(const hg_recur_params* p, int64_t n, int64_t T) {
+  int64_t rows = std::max(chain_rows(p, n, std::min<int64_t>(T, 1)), chain_rows(p, n, T));
+  if (T > kPos) rows = std::max(rows, std::min(n * kMaxCluster, kMaxPartRows));
+  return rows;
 }
 
 hg_status check(const hg_recur_params* p, int64_t n, int64_t T) {
@@ -1426,7 +1436,7 @@ extern "C" hg_status hg_recur_workspace_size(const hg_recur_params* params, int6
   HG_REQUIRE(saved_bytes && scratch_bytes, "saved_bytes and scratch_bytes must be non-null");
   HG_TRY(check(params, n, T));
   *saved_bytes = align_up(saved_bytes_of(params, n, T));
-  *scratch_bytes = align_up(sizeof(float) * (size_t)part_rows(params, n, T) * params->d);
+  *scratch_bytes = align_up(sizeof(float) * (size_t)most_part_rows(params, n, T) * params->d);
   return HG_OK;
 }
 

@@ -163,3 +163,24 @@ def test_binding_refuses_what_it_would_read_wrongly(hg):  # noqa: F811
         hg.hg_recur_fwd(p, x[..., :4], x, None, None, x, None, None)
     with pytest.raises(ValueError, match="shape"):
         hg.hg_recur_step(p, x[:, 0].double(), x[:, 0], None, x[:, 0], x[:, 0])
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+def test_sizes_serve_smaller_calls(hg, dt):  # noqa: F811
+    """What is enough for n sequences of up to T positions is enough for fewer or shorter ones."""
+    so = hg.lib()
+    s, w = ctypes.c_size_t(), ctypes.c_size_t()
+
+    def query(n, T, d):
+        assert so.hg_recur_workspace_size(params(hg, d, dt), n, T, ctypes.byref(s), ctypes.byref(w)) == 0
+        return s.value, w.value
+
+    Ts = [0, 1, 2, 12, 16, 17, 40, 64, 65, 300, 515, 1001, 4096, 32768, 1 << 20]
+    ns = [1, 2, 3, 7, 40, 77, 400, 1000, 2000, 2700, 3000, 5000, 20000, 150001, 1 << 21]
+    for d in (8, 64, 128, 264, 1024, 16384):
+        grid = {(n, T): query(n, T, d) for n in ns for T in Ts}
+        for i, n in enumerate(ns):
+            for j, T in enumerate(Ts):
+                here = grid[n, T]
+                for less in ([(ns[i - 1], T)] if i else []) + ([(n, Ts[j - 1])] if j else []):
+                    assert all(a >= b for a, b in zip(here, grid[less])), (d, n, T, less)
