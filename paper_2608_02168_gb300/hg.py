@@ -921,11 +921,12 @@ def _flat_seq_arg(t, name: str, dtype, shape):
 def _sizes(params, key, ask):
     """What a size query of these parameters gave, asked for once a shape (sizes hang on the struct's numbers alone)."""
     known = params.__dict__.setdefault("_known", {})
-    if key not in known:
+    size = known.get(key)  # (another thread may clear them at any time)
+    if size is None:
         if len(known) >= 64:
             known.clear()
-        known[key] = ask()
-    return known[key]
+        size = known[key] = ask()
+    return size
 
 
 def hg_recur_workspace_size(params: RecurParams, n: int, T: int) -> tuple:

@@ -184,3 +184,18 @@ def test_sizes_serve_smaller_calls(hg, dt):  # noqa: F811
                 here = grid[n, T]
                 for less in ([(ns[i - 1], T)] if i else []) + ([(n, Ts[j - 1])] if j else []):
                     assert all(a >= b for a, b in zip(here, grid[less])), (d, n, T, less)
+
+
+def test_sizes_asked_for_by_several_threads(hg):  # noqa: F811
+    """Sizes of more shapes than are kept, of parameters that threads share: one that another thread drops between its
+    asking and its return is still returned."""
+    p = hg.RecurParams(d=8, dtype=torch.float32)
+
+    class Dropping(dict):
+        def __setitem__(self, key, value):
+            dict.__setitem__(self, key, value)
+            self.clear()  # as the other thread would
+
+    p.__dict__["_known"] = Dropping()
+    want = [(0, hg.hg_recur_workspace_size(hg.RecurParams(d=8, dtype=torch.float32), n, 3)[1]) for n in (1, 5, 900)]
+    assert [hg.hg_recur_workspace_size(p, n, 3) for n in (1, 5, 900)] == want
