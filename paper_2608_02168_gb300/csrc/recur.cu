@@ -850,9 +850,9 @@ __device__ __forceinline__ void hand_out(float4* slot, uint64_t* bar, const floa
 }
 
 // A bounded wait for a step's tiles: false when it ran out.
-__device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool tiles_here(uint64_t* bar, uint32_t parity, uint32_t polls = tc::kSpinLimit) {
   const uint32_t addr = tc::smem_u32(bar);
-  for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
+  for (uint32_t i = 0; i < polls; ++i) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -872,8 +872,7 @@ struct Split {
   SplitSmem<L>& sm;
   int* status;
   int cl, rank, tx, ty;
-  uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next
-  bool ok = true;      // no wait has run out
+  uint32_t phase = 0;  // bit b: the parity that bar[b] comes to next; bit 2: a wait has run out
   static constexpr int kGroups = kSubs<L> / kJoin<L>, kJoiners = L * kGroups;
   static_assert(kJoiners <= 32, "the joining lanes are in one warp");
 
@@ -893,7 +892,7 @@ struct Split {
   __device__ __forceinline__ Vec<V> enter(const Run<T>& mine, Vec<V>& state, int buf, F then) {
     auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
     sm.run[buf][ty][tx] = mine.packed();
-    if (cl > 1 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * L * sizeof(float4)));
+    if (cl > 1 && phase < 4 && threadIdx.x == 0) tc::mbar_expect_tx(&sm.bar[buf], (uint32_t)(cl * L * sizeof(float4)));
     __syncthreads();
     if (threadIdx.x < kJoiners) {
       const int group = threadIdx.x / L;
@@ -916,22 +915,24 @@ struct Split {
         first.join(whole);
         whole = first;
       }
-      if (group == kGroups - 1) {
-        if (cl > 1)
-          hand_out(&sm.tile[buf][rank][tx], &sm.bar[buf], whole.packed(), cl);
-        else
-          sm.tile[buf][0][tx] = whole.packed();
+      if (cl == 1) {
+        if (group == kGroups - 1) sm.tile[buf][0][tx] = whole.packed();
+      } else if (phase < 4) {
+        if (group == kGroups - 1) hand_out(&sm.tile[buf][rank][tx], &sm.bar[buf], whole.packed(), cl);
+        tc::mbar_arrive(&sm.bar[buf]);
       }
-      if (cl > 1) tc::mbar_arrive(&sm.bar[buf]);
     }
     then();
     if (cl == 1) {
       __syncthreads();
-    } else if (ok && !tiles_here(&sm.bar[buf], phase >> buf & 1)) {
-      ok = false;  // this call's results are invalid; nothing waits any more, and every loop ends
-      record_device_error(status, tc::kErrTimeout);
+    } else if (phase < 4) {
+      if (tiles_here(&sm.bar[buf], phase >> buf & 1)) {
+        phase ^= 1u << buf;
+      } else {  // this call's results are invalid; this thread neither waits nor arrives any more, and every loop ends
+        phase |= 4;
+        record_device_error(status, tc::kErrTimeout);
+      }
     }
-    phase ^= 1u << buf;
     const float4* t = &sm.tile[buf][0][tx];
     auto tile = [&](int k) { return Run<T>::from(t[at(k, cl) * L]); };
     int k = 0;
@@ -941,6 +942,14 @@ struct Split {
     got = Run<T>::from(sm.run[buf][ty][tx]).of(got);
     for (; k < cl; ++k) state = tile(k).of(state);
     return got;
+  }
+  // When every CTA has handed out its last: what is on its way to this one comes before it ends.  (Each step has waited for
+  // it; after a wait that ran out, a while.)
+  __device__ __forceinline__ void finish() {
+    __syncwarp();
+    cluster_meet();
+    if (phase >= 4)
+      for (int b = 0; b < 2; ++b) tiles_here(&sm.bar[b], phase >> b & 1, 1u << 12);
   }
 };
 
@@ -1104,8 +1113,7 @@ __global__ __launch_bounds__(kSplitThr, 2) void recur_fwd_split(RecurArgs a) {
     for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) st4(y + t * a.y.st, all<V>(0.f));
     if (a.h_out && rank == 0 && sub == 0) stf(a.h_out + i * a.d + c, h);
   }
-  __syncwarp();
-  cluster_meet();
+  sp.finish();
 }
 
 // The same from the end: a run of positions maps the R that enters from the right to B + K R.  The states before each
@@ -1184,7 +1192,7 @@ __global__ __launch_bounds__(kSplitThr, 1) void recur_bwd_split(RecurArgs a) {
     }
     sum = add(sum, here);
   }
-  cluster_meet();
+  sp.finish();
   if (in) {
     for (int64_t t = len + rank * kSubs<L> + sub; t < a.T; t += CL * kSubs<L>) {
       st4(dx + t * a.dx.st, zero);
