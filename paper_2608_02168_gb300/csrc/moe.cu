@@ -1,7 +1,7 @@
 // A whole layer of experts for a few rows (hg_moe_fwd):
 //   moe_router    l = x W_router, the top_k largest, their weights; a CTA a row
 //   moe_experts   (act(x W_gate[e]) * (x W_up[e])) W_down[e] for each expert e and the rows that chose it
-//   moe_sum       Y = sum of a row's w_j times what expert e_j gave it (+ x); up to kFewRows rows moe_experts does it
+//   moe_sum       Y = sum of a row's w_j times what expert e_j gave it (+ x); for one or two rows mostly moe_experts does it
 //
 // With a few rows an expert the weights are the work: 3 d f values of every expert that a row chose are read once, with
 // one multiplication and addition a row for each (16 rows of bf16: 16 flops a byte, where the tensor pipe has 280 a byte of
@@ -29,10 +29,15 @@ constexpr int kSms = 152;
 constexpr int kThr = 256;
 constexpr int kMaxRows = 1024, kMaxExperts = 256, kMaxTop = 8, kMaxF = 16384;
 constexpr int kGroup = 64;  // rows of an expert that a pass over its weights serves
-// Up to these the CTA that brings a row's last share adds its shares up (one launch less, but the rows one after another in
-// one CTA).  Calls, without / with a launch of their own: one row of 16 experts, d 128, f 384: 10.3 / 12.6 us; two rows of 64
-// experts, d 256, f 1024: 13.0 / 14.7, of two experts 15.0 / 12.8; four rows of these 21.1 / 12.9; 64 rows of 64: 30.7 / 25.6.
-constexpr int kFewRows = 2;
+// The CTA that brings a row's last share adds the shares up, one launch less, where the rows that may come to one CTA take it
+// at most two rounds: it has one row after another, and kThr / d of a row's experts at a time, of which a launch of its own has
+// all at once.  Calls in a graph, weights from HBM, without / with that launch, f 1024 and 4096 (and 16384):
+//   one row     two of 8 experts, d 128 (one round): 17.5 / 19.6, 21.6 / 25.8 (25.7 / 29.9) us;  d 256 (two): 19.6 / 19.6,
+//               25.7 / 25.8 (33.9 / 34.0);  eight of 64, d 128 (four): 21.6 / 19.6, 27.7 / 25.8 (44 / 40), d 256: 28 / 26, 38 / 34
+//   two rows    one of two, d 256 (two): 17.5 / 18.6, 21.7 / 26.8 (34 / 35);  two of two, d 128 (two): 19.6 / 19.6,
+//               25.7 / 24.7 (29.9 / 29.8), d 256 (four): 21.6 / 19.6, 31.9 / 25.7 (40 / 34)
+//   three rows  of one expert, d 128 (three): 19.6 / 17.6, 29.8 / 25.8 (36 / 30) us
+constexpr int kMaxRounds = 2;
 constexpr int kMaxPasses = kMaxExperts + kMaxRows * kMaxTop / kGroup;
 
 struct MoeArgs {
@@ -837,7 +842,7 @@ extern "C" hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, cons
   a.part = L.part;
   a.items = L.items;
   a.status = device_status_ptr();
-  a.last = n <= kFewRows;
+  a.last = n * ceil_div((int64_t)p.top_k * p.d, kThr) <= kMaxRounds;
   a.n = (int32_t)n;
   a.d = p.d;
   a.f = p.f;
