@@ -669,9 +669,13 @@ hg_status hg_recur_workspace_size(const hg_recur_params* params, int64_t n, int6
  * get zero in y.  h_in, h_out: device fp32 [n][d], 16-byte aligned; h_in NULL = zero, h_out NULL = not wanted; h_out
  * (the state after the last position in use; h_in for an empty sequence) may be h_in itself.  saved: NULL where no
  * backward pass follows.  No output overlaps another array otherwise.  Computed in fp32, y rounded once; the state is
- * never rounded to bf16.  Differences x_t - h_(t-1) are formed in fp32: one past its largest number (two values of
- * opposite signs above 1.7e38) is an infinity, and what an infinity reaches can be NaN where the definition has an
- * infinity.  Neither reaches an earlier row. */
+ * never rounded to bf16.  z is right to some (3 |a| + 12) 2^-24 of itself, a = g + bias (bf16: and |bias| 2^-24; a bias
+ * above 1e38 counts as that), zero below 2^-126, and so are long memories: a state or a gradient goes on by what z changes
+ * of it.  fp32: 1 - z is right to as much of itself as well.  bf16: to some 2^-22 of one, so what an open gate leaves of
+ * a state or of a gradient is off by that of the whole (dh_in of a first gate above 16 may be zero), and where many
+ * histories are a chain each, a state is rounded at every position.  Differences x_t - h_(t-1) are formed in fp32: one
+ * past its largest number (two values of opposite signs above 1.7e38) is an infinity, and what an infinity reaches can
+ * be NaN where the definition has an infinity.  Neither reaches an earlier row. */
 hg_status hg_recur_fwd(const hg_recur_params* params, const hg_seq* x, const hg_seq* g, const int32_t* lens, int64_t n,
                        int64_t T, const float* h_in, const hg_seq* y, float* h_out, void* saved, hg_stream stream);
 
@@ -719,10 +723,10 @@ hg_status hg_moe_workspace_size(const hg_moe_params* params, int64_t n, size_t* 
  * positive is not read, chooses no expert and gets a zero row in Y.  experts (device int32 [n][top_k]) and weights
  * (device fp32 [n][top_k]) receive e_j and w_j (-1 and 0 for a row that is not live); NULL = not wanted.  No output
  * overlaps another array.  The choice is that of logits without rounding (sums of two fp32 numbers, within d 2^-48 of
- * the sum of their terms' sizes); a NaN counts as the largest logit, and an infinite one has the weights that the
- * formula gives it (NaN).  Sums are fp32 in an order fixed by the choice; bf16: the hidden rows enter the second
- * product as sums of two bf16 numbers (16 bits; an infinity among them becomes NaN), Y is rounded once.  An infinity or
- * NaN stays in its own row.  Weights of experts that no row
+ * the sum of their terms' sizes); a product or a sum past fp32's largest number is an infinity; a NaN counts as the
+ * largest logit, and an infinite one has the weights that the formula gives it (NaN).  Sums are fp32 in an order fixed by
+ * the choice; bf16: the hidden rows enter the second product as sums of two bf16 numbers (16 bits; an infinity among
+ * them becomes NaN), Y is rounded once.  An infinity or NaN stays in its own row.  Weights of experts that no row
  * chooses are not read. */
 hg_status hg_moe_fwd(const hg_moe_params* params, const void* X, const int32_t* live, int64_t n, void* Y,
                      int32_t* experts, float* weights, void* scratch, hg_stream stream);

@@ -1,20 +1,21 @@
 // A whole layer of experts for a few rows (hg_moe_fwd):
 //   moe_router    l = x W_router, the top_k largest, their weights; a CTA a row
 //   moe_experts   (act(x W_gate[e]) * (x W_up[e])) W_down[e] for each expert e and the rows that chose it
-//   moe_sum       Y = sum of a row's w_j times what expert e_j gave it (+ x); for one or two rows mostly moe_experts does it
+//   moe_sum       Y = sum of a row's w_j times what expert e_j gave it (+ x); one or two rows: often moe_experts
 //
 // With a few rows an expert the weights are the work: 3 d f values of every expert that a row chose are read once, with
-// one multiplication and addition a row for each (16 rows of bf16: 16 flops a byte, where the tensor pipe has 280 a byte of
-// HBM).  So moe_experts is a stream of weights: the chosen experts' hidden features in chunks of 64 bytes of a W_gate row
-// are one list, cut into equal shares, a CTA a share, with some 100 KB of copies ahead of the products.  A share may begin
-// and end inside an expert; a pass over an expert's chunks serves up to 64 of its rows.  What a share gives a pass's rows
-// (d sums each, fp32) goes to scratch and is added up in the order of the list, whichever CTA was last.  mma.sync has the
-// room: a tile of sixteen rows is what few rows fill, and an instruction on 128 would run at an eighth of its rate.
+// one multiplication and addition a row for each (16 rows of bf16: 16 flops a byte, where the tensor pipe has 280 a
+// byte of HBM).  So moe_experts is a stream of weights: the chosen experts' hidden features in chunks of 64 bytes of a
+// W_gate row are one list, cut into equal shares, a CTA a share, with some 100 KB of copies ahead of the products.  A
+// share may begin and end inside an expert; a pass over an expert's chunks serves up to 64 of its rows.  What a share
+// gives a pass's rows (d sums each, fp32) goes to scratch and is added up in the order of the list, whichever CTA was
+// last.  mma.sync has the room: a tile of sixteen rows is what few rows fill, and an instruction on 128 would run at an
+// eighth of its rate.
 //
-// 64 rows, two of 64 experts each, d 256, f 1024, bf16: 24 us for the 87 MB that they chose; of that 3 us for the list and
-// the rows, 2 us until the first chunks are there, 13 us of weights; f 4096: 66 us, so beyond the beginning the weights
-// come at 6.3 TB/s (0.93 of the copy rate).  300 rows, four of 32 experts each, f 704 (33 rows a pass): 21 us, bound by a
-// pass's products (1.4 us a chunk, half of it the second product with its two terms of H).
+// 64 rows, two of 64 experts each, d 256, f 1024, bf16: 24 us for the 87 MB that they chose; of that 3 us for the list
+// and the rows, 2 us until the first chunks are there, 13 us of weights; f 4096: 66 us, so beyond the beginning the
+// weights come at 6.3 TB/s (0.93 of the copy rate).  300 rows, four of 32 experts each, f 704 (33 rows a pass): 21 us,
+// bound by a pass's products (1.4 us a chunk, half of it the second product with its two terms of H).
 #include <algorithm>
 
 #include "ffn_kernels.cuh"
@@ -29,11 +30,13 @@ constexpr int kSms = 152;
 constexpr int kThr = 256;
 constexpr int kMaxRows = 1024, kMaxExperts = 256, kMaxTop = 8, kMaxF = 16384;
 constexpr int kGroup = 64;  // rows of an expert that a pass over its weights serves
-// The CTA that brings a row's last share adds the shares up, one launch less, where the rows that may come to one CTA take it
-// at most two rounds: it has one row after another, and kThr / d of a row's experts at a time, of which a launch of its own has
-// all at once.  Calls in a graph, weights from HBM, without / with that launch, f 1024 and 4096 (and 16384):
-//   one row     two of 8 experts, d 128 (one round): 17.5 / 19.6, 21.6 / 25.8 (25.7 / 29.9) us;  d 256 (two): 19.6 / 19.6,
-//               25.7 / 25.8 (33.9 / 34.0);  eight of 64, d 128 (four): 21.6 / 19.6, 27.7 / 25.8 (44 / 40), d 256: 28 / 26, 38 / 34
+// The CTA that brings a row's last share adds the shares up, one launch less, where the rows that may come to one CTA
+// take it at most two rounds: it has one row after another, and kThr / d of a row's experts at a time, of which a
+// launch of its own has all at once.  Calls in a graph, weights from HBM, without / with that launch, f 1024 and 4096
+// (and 16384):
+//   one row     two of 8 experts, d 128 (one round): 17.5 / 19.6, 21.6 / 25.8 (25.7 / 29.9) us;  d 256 (two): 19.6 /
+//               19.6, 25.7 / 25.8 (33.9 / 34.0);  eight of 64, d 128 (four): 21.6 / 19.6, 27.7 / 25.8 (44 / 40), d 256
+//               (eight): 28 / 26, 38 / 34
 //   two rows    one of two, d 256 (two): 17.5 / 18.6, 21.7 / 26.8 (34 / 35);  two of two, d 128 (two): 19.6 / 19.6,
 //               25.7 / 24.7 (29.9 / 29.8), d 256 (four): 21.6 / 19.6, 31.9 / 25.7 (40 / 34)
 //   three rows  of one expert, d 128 (three): 19.6 / 17.6, 29.8 / 25.8 (36 / 30) us
@@ -269,9 +272,10 @@ struct Sums<__nv_bfloat16, D, kAct> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
   }
-  // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments, two tiles
-  // the weights'.  H is kept as a sum of two bf16 numbers (16 bits), the operands of the next product: rounded once to 8
-  // bits it would add 1.8e-3 of a row to the 1.7e-3 of Y's own rounding, and the product is not what takes the time.
+  // H: a warp has 8 of the chunk's features, of every other tile of 16 rows; G and U share the rows' fragments, two
+  // tiles the weights'.  H is kept as a sum of two bf16 numbers (16 bits), the operands of the next product: rounded
+  // once to 8 bits it would add 1.8e-3 of a row to the 1.7e-3 of Y's own rounding, and the product is not what takes
+  // the time.
   template <int NR>
   __device__ __forceinline__ void hidden_of(const char* st, const char* X, char* H, int rt) {
     const int lane = threadIdx.x % 32, ft = threadIdx.x / 32 % 4;
@@ -459,7 +463,8 @@ __device__ __forceinline__ float row_in(const MoeArgs& a, int row, int c) {
   return a.residual ? to_f32(static_cast<const T*>(a.x)[(int64_t)row * D + c]) : 0.f;
 }
 
-// A CTA a row: a thread has a column of one of the row's experts, so that all their shares' loads are in flight together.
+// A CTA a row: a thread has a column of one of the row's experts, so that all their shares' loads are in flight
+// together.
 template <typename T, int D>
 __global__ __launch_bounds__(D * kMaxTop > 1024 ? 1024 : D * kMaxTop) void moe_sum(MoeArgs a, int grid) {
   pdl_begin();
@@ -720,8 +725,8 @@ hg_status check(const hg_moe_params* p, int64_t n) {
   }
   HG_REQUIRE(p->f >= 8 && p->f <= kMaxF && p->f % 8 == 0, "f must be a multiple of 8 in [8, %d]", kMaxF);
   HG_REQUIRE(p->experts >= 1 && p->experts <= kMaxExperts, "experts must be in [1, %d]", kMaxExperts);
-  HG_REQUIRE(p->top_k >= 1 && p->top_k <= kMaxTop && p->top_k <= p->experts, "top_k must be in [1, %d], at most experts",
-             kMaxTop);
+  HG_REQUIRE(p->top_k >= 1 && p->top_k <= kMaxTop && p->top_k <= p->experts,
+             "top_k must be in [1, %d], at most experts", kMaxTop);
   HG_REQUIRE(p->act == HG_ACT_RELU || p->act == HG_ACT_GELU_TANH || p->act == HG_ACT_NONE || p->act == HG_ACT_SILU,
              "unknown activation %d", (int)p->act);
   HG_REQUIRE(n >= 0, "n must not be negative");

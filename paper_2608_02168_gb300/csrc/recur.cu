@@ -3,8 +3,8 @@
 //   z_t = sigmoid(g_t + b),  h_t = h_(t-1) + z_t (x_t - h_(t-1)),
 // and, from the end, with R_t = dy_t + (1 - z_(t+1)) R_(t+1):
 //   dx_t = z_t R_t,  dg_t = R_t (x_t - h_(t-1)) z_t (1 - z_t),  db = sum of dg.
-// A share z is known to a few steps of its own size, and a state or R goes on by what z changes of it, never by a product
-// with a rounded 1 - z, so long memories (z = 1e-5) keep their weights.
+// A share z is known to a few steps of its own size, and a state or R goes on by what z changes of it, never by a
+// product with a rounded 1 - z, so long memories (z = 1e-5) keep their weights.
 //
 // Each value is read and written once and costs two special functions and some ten other instructions: all forms are
 // bound by HBM, or by latency where there are few chains.
@@ -12,9 +12,9 @@
 //   recur_bwd_short                   the same for histories of at most 16 positions
 //   recur_fwd_split, recur_bwd_split  a few long histories: time is split over threads, CTAs and clusters
 //   recur_bias_sum                    the CTAs' parts of the bias's gradient, in a fixed order
-//   recur_step                        one new snapshot: 1000003 nodes of d 128, one in eight not live, 242 us (the copy rate)
-// The backward reads x, g, dy and every 16th state, which the forward kept, and forms the states between anew: 0.25 bytes
-// a value more in either pass, where reading the states (4 bytes) or a second forward pass (2 b) would be more.
+//   recur_step                        one new snapshot: 1000003 nodes of d 128, one in eight not live: 242 us
+// The backward reads x, g, dy and every 16th state, which the forward kept, and forms the states between anew: 0.25
+// bytes a value more in either pass, where reading the states (4 bytes) or a second forward pass (2 b) would be more.
 #include <algorithm>
 #include <cfloat>
 
@@ -113,10 +113,10 @@ __device__ __forceinline__ Vec<V> less(Vec<V> c, Vec<V> a, Vec<V> b) {  // c - a
 // z = sigmoid(g + b) and k = 1 - z, with a bias as Gate::bias gives it.
 constexpr float kLog2e = 1.4426950408889634f;
 
-// fp32 rows: z and k each to a few steps of their own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero from
-// |a| = 87 on), 1 - s the other, and an update is the nearer end plus the smaller share of the difference: a state that
-// an open gate has just left does not leave its rounding behind.  The bias is added first: its product with log2 e, rounded,
-// would be |b| 2^-24 of z off, also where g and b cancel.
+// fp32 rows: z and k each to a few steps of their own size.  s = e^-|a| / (1 + e^-|a|) is the smaller of the two (zero
+// from |a| = 87 on), 1 - s the other, and an update is the nearer end plus the smaller share of the difference: a state
+// that an open gate has just left does not leave its rounding behind.  The bias is added first: its product with log2
+// e, rounded, would be |b| 2^-24 of z off, also where g and b cancel.
 template <int V, bool kExact>
 struct Gate {
   Vec<V> s, big;
@@ -151,7 +151,8 @@ struct Gate {
     rest = fma(code(), minus(x, sum), pick(x, rest));
     h = pick(all<V>(0.f), h);
   }
-  // What a gate lets through of R, z R, and what it leaves, (1 - z) R: the smaller as a product, the other as R without it.
+  // What a gate lets through of R, z R, and what it leaves, (1 - z) R: the smaller as a product, the other as R without
+  // it.
   __device__ __forceinline__ static void part(Vec<V> code, Vec<V> R, Vec<V>& through, Vec<V>& left) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -181,14 +182,17 @@ struct Gate {
   }
 };
 
-// bf16 rows, whose bytes are half as many and whose instructions therefore count (5 a gate instead of 9): z to a few steps
-// of its own size (and |b| 2^-24), 1 - z to a few of one, which is a rounding of the state that it keeps.  The logit's product
-// with -log2 e and the sum with the bias's are one instruction.
+// bf16 rows, whose bytes are half as many and whose instructions therefore count (5 a gate instead of 9): z to a few
+// steps of its own size (and |b| 2^-24), 1 - z to a few of one, which is a rounding of the state that it keeps.  The
+// logit's product with -log2 e and the sum with the bias's are one instruction.
 template <int V>
 struct Gate<V, false> {
   Vec<V> e, r;
-  // One above 1e38 is as good as that, and its product stays finite, so that -infinity plus it stays what it is (NaN too).
-  __device__ __forceinline__ static float bias(float b) { return -kLog2e * (fabsf(b) > 1e38f ? copysignf(1e38f, b) : b); }
+  // One above 1e38 is as good as that, and its product stays finite, so that -infinity plus it stays what it is (NaN
+  // too).
+  __device__ __forceinline__ static float bias(float b) {
+    return -kLog2e * (fabsf(b) > 1e38f ? copysignf(1e38f, b) : b);
+  }
   __device__ __forceinline__ Gate(Vec<V> g, Vec<V> bias) {
     const Vec<V> a = fma(g, all<V>(-kLog2e), bias);
 #pragma unroll
@@ -277,7 +281,8 @@ __device__ __forceinline__ int left_of(int64_t t0, int64_t end) {
   const int64_t l = end - t0;
   return l < 0 ? 0 : l > kPos ? kPos : (int)l;
 }
-// What stands for logits from a sequence's length on: -infinity, so that z = 0 and a position leaves every sum as it is.
+// What stands for logits from a sequence's length on: -infinity, so that z = 0 and a position leaves every sum as it
+// is.
 template <typename T>
 __device__ __forceinline__ uint32_t shut() {
   return sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
@@ -300,8 +305,8 @@ __device__ __forceinline__ void load_rows(uint32_t (&r)[kPos], const T* p, int64
 // ------------------------------------------------------------------------------------------------------------
 // a chain a thread
 // ------------------------------------------------------------------------------------------------------------
-// Forward: a thread has 16 bytes of a row, so that loads, stores and their addresses are few beside the gates (4 bytes a
-// thread: 240 us where this takes 203), and four positions, the next four's loads in flight.
+// Forward: a thread has 16 bytes of a row, so that loads, stores and their addresses are few beside the gates (4 bytes
+// a thread: 240 us where this takes 203), and four positions, the next four's loads in flight.
 constexpr int kWide = 4;
 template <typename T>
 struct Wide {
@@ -335,13 +340,13 @@ struct Wide {
   }
 };
 
-// kTwo (fp32 of more than 16 positions): the state in two numbers, joined every four positions, so that what a small z adds is
-// not rounded to a step of the state every time (an equal sign there makes z = 1e-6 some 1e-3 off in 30000 positions; 3000
-// histories of 1000, d 128: no change in time).  In bf16 that takes 20 % more time (registers), and a state is rounded at
-// every position.
-// A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's length
-// and state, are on their way while these ones' gates are computed (a sequence a thread: 203 us).  Bound by HBM: 150001
-// ragged histories of up to 12, d 128, bf16, 156 us, 0.94 of the copy rate.
+// kTwo (fp32 of more than 16 positions): the state in two numbers, joined every four positions, so that what a small z
+// adds is not rounded to a step of the state every time (an equal sign there makes z = 1e-6 some 1e-3 off in 30000
+// positions; 3000 histories of 1000, d 128: no change in time).  In bf16 that takes 20 % more time (registers), and a
+// state is rounded at every position.
+// A thread takes sequence after sequence, four positions at a time; the next four's loads, and the next sequence's
+// length and state, are on their way while these ones' gates are computed (a sequence a thread: 203 us).  Bound by HBM:
+// 150001 ragged histories of up to 12, d 128, bf16, 156 us, 0.94 of the copy rate.
 template <typename T, bool kTwo>
 __global__ __launch_bounds__(256, 2) void recur_fwd(RecurArgs a) {
   pdl_begin();
@@ -469,12 +474,13 @@ __device__ __forceinline__ void back(Vec<V>& R, Vec<V> dy, Vec<V> code, Vec<V> s
   GateOf<T>::part(code, R, dx, R);
 }
 
-// Backward of more than 16 positions: a thread has 4 bytes of a row and 16 positions, whose states it forms from the one
-// kept before them; the 16 before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128 threads, three an SM: ragged histories
-// leave fewer threads waiting for the longest one than in 256, and 12 warps hide more than 8 (400 of up to 515, d 256,
-// 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers bound it:
-// 16 positions' gates and slopes, and the next rows (bf16: 64 bytes of them are spilled).  In fp32 R is kept in two numbers,
-// joined every 16 positions, as the forward's state is (3000 of 1000, d 128: 1.21 -> 1.24 ms; not in bf16).
+// Backward of more than 16 positions: a thread has 4 bytes of a row and 16 positions, whose states it forms from the
+// one kept before them; the 16 before them, or the next sequence's last ones, are loaded meanwhile.  CTAs of 128
+// threads, three an SM: ragged histories leave fewer threads waiting for the longest one than in 256, and 12 warps hide
+// more than 8 (400 of up to 515, d 256, 99 -> 84 us; 2000 of them 347 -> 310 us, 0.88 of the copy rate).  Registers
+// bound it: 16 positions' gates and slopes, and the next rows (bf16: 64 bytes of them are spilled).  In fp32 R is kept
+// in two numbers, joined every 16 positions, as the forward's state is (3000 of 1000, d 128: 1.21 -> 1.24 ms; not in
+// bf16).
 constexpr int kBwdThr = 128;
 template <typename T>
 __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
@@ -576,11 +582,11 @@ __global__ __launch_bounds__(kBwdThr, 3) void recur_bwd(RecurArgs a) {
 
 // Backward of at most 16 positions: rows go through shared memory, 16 bytes a copy and a store, the next sequence's on
 // their way meanwhile; a thread reads its 4 bytes of them where its positions are, four positions at a time, and leaves
-// its gradients in their place.  Fewer instructions for addresses than with loads and stores of 4 bytes, a fourth CTA an
-// SM where the next rows were in registers, and only a quad of threads waits
-// for one another.  100000 ragged histories of up to 12, d 128, bf16, 221 us, 0.82 of the copy rate (the kernel above: 291);
-// 50000 in fp32 184 (364); 150000 of one 142 (347); 50000 of 16, none ragged, 186 (173).  A third stage 261 where two take
-// 223 (three CTAs an SM then), five CTAs 246 (96 registers).  Bound by the rows' bytes and by the instructions of gates.
+// its gradients in their place.  Fewer instructions for addresses than with loads and stores of 4 bytes, a fourth CTA
+// an SM where the next rows were in registers, and only a quad of threads waits for one another.  100000 ragged
+// histories of up to 12, d 128, bf16, 221 us, 0.82 of the copy rate (the kernel above: 291); 50000 in fp32 184 (364);
+// 150000 of one 142 (347); 50000 of 16, none ragged, 186 (173).  A third stage 261 where two take 223 (three CTAs an SM
+// then), five CTAs 246 (96 registers).  Bound by the rows' bytes and by the instructions of gates.
 template <int V>
 struct ShortStage {  // of shared memory: a sequence's two states, then its rows of x, g and dy, position by position
   static constexpr int kPitch = kBwdThr * 4, kRow = 3 * kPitch + 32;  // a quad's four 16-byte pieces: different banks
@@ -599,7 +605,8 @@ __global__ __launch_bounds__(kBwdThr, kShortCtas) void recur_bwd_short(RecurArgs
   using S = ShortStage<V>;
   extern __shared__ __align__(128) char smem[];
   __shared__ float sh[kBwdThr * V];
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, tid = threadIdx.y * blockDim.x + threadIdx.x, part = tid % 4;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x, part = tid % 4;
   const bool in = c < a.d;
   const uint32_t quad = 0xFu << (tid % 32 - part);
   const Vec<V> zero = all<V>(0.f), b = in ? bias_of<T>(a, c) : zero;
@@ -723,23 +730,23 @@ __global__ __launch_bounds__(kBwdThr, kShortCtas) void recur_bwd_short(RecurArgs
 // a chain split over time
 // ------------------------------------------------------------------------------------------------------------
 // A cluster of CL CTAs takes a piece of a sequence's rows (L lanes of 4 bytes) through CL tiles of positions a step: 64
-// bytes and 256 positions a tile; where even eight CTAs a piece leave SMs idle, 32 bytes and 512; in the backward, whose
-// three arrays in and two out touch half as many lines so, mostly 128 bytes and 128 positions.  A thread has 16
+// bytes and 256 positions a tile; where even eight CTAs a piece leave SMs idle, 32 bytes and 512; in the backward,
+// whose three arrays in and two out touch half as many lines so, mostly 128 bytes and 128 positions.  A thread has 16
 // positions of 4 bytes.  Positions compose: a run of them maps the state h before it to B + K h, B its end from a zero
-// state, K the product of its 1 - z.  Threads form the runs of their 16 positions and keep each, a CTA forms that of its
-// tile and hands it to the cluster's others (distributed shared memory), and every CTA joins them in the same order, so all
-// carry the same state and a call repeats its bits.
+// state, K the product of its 1 - z.  Threads form the runs of their 16 positions and keep each, a CTA forms that of
+// its tile and hands it to the cluster's others (distributed shared memory), and every CTA joins them in the same
+// order, so all carry the same state and a call repeats its bits.
 //
-// A step of a CTA alone takes 1.75 us, one after another: copies into shared memory 0.55, gates 0.5, the join 0.4, stores
-// 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6 histories
-// of 32768, d 256, bf16: 86 us forward (HBM: 44).  Half as many positions a thread and twice as many threads took 97 us
-// where this took 83; instructions on two numbers at once changed nothing.
+// A step of a CTA alone takes 1.75 us, one after another: copies into shared memory 0.55, gates 0.5, the join 0.4,
+// stores 0.57, barriers 0.6, overlapping in part; two CTAs an SM take 1.3 each.  That bounds it where chains are few: 6
+// histories of 32768, d 256, bf16: 82 us forward (HBM: 44).  Half as many positions a thread and twice as many threads
+// took 97 us where this took 83; instructions on two numbers at once changed nothing.
 //
 // K itself would not do for a state: 1 - z rounded, a step of one at every position and of one sign where gates hardly
-// change, makes a memory of 10^5 positions a thousandth off (an eighth more instructions an output; 6 histories of 32768, d
-// 256, bf16: 85 -> 87 us).  So a run is kept as B and Q = 1 - K, both to some steps of themselves (rounded shares of 1 - z only
-// weigh what has been added), and a state goes to h + (B - Q h).  In fp32 K of its own size too, and the state goes to B + K h
-// where K is at most a half, as behind an open gate, which leaves no rounding of h.
+// change, makes a memory of 10^5 positions a thousandth off (an eighth more instructions an output; 6 histories of
+// 32768, d 256, bf16: 78 -> 82 us).  So a run is kept as B and Q = 1 - K, both to some steps of themselves (rounded
+// shares of 1 - z only weigh what has been added), and a state goes to h + (B - Q h).  In fp32 K of its own size too,
+// and the state goes to B + K h where K is at most a half, as behind an open gate, which leaves no rounding of h.
 template <typename T>
 struct Run;
 template <>
@@ -843,8 +850,8 @@ __device__ __forceinline__ void hand_out(float4* slot, uint64_t* bar, const floa
     uint32_t there, there_bar;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(r));
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(own_bar), "r"(r));
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(there),
-                 "f"(p.x), "f"(p.y), "f"(p.z), "f"(p.w), "r"(there_bar)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(there), "f"(p.x), "f"(p.y), "f"(p.z), "f"(p.w), "r"(there_bar)
                  : "memory");
   }
 }
@@ -886,8 +893,8 @@ struct Split {
     __syncthreads();
   }
   // The state that enters this thread's run, in the order of positions or from the end; `state`, of the step before, is
-  // carried on.  `then` is done by all threads when all have formed their runs.  A CTA hands out step s + 1 after all its
-  // threads have read step s, and enters s + 2 after every other one has handed out s + 1: two places are enough.
+  // carried on.  `then` is done by all threads when all have formed their runs.  A CTA hands out step s + 1 after all
+  // its threads have read step s, and enters s + 2 after every other one has handed out s + 1: two places are enough.
   template <bool kBack, typename F>
   __device__ __forceinline__ Vec<V> enter(const Run<T>& mine, Vec<V>& state, int buf, F then) {
     auto at = [](int k, int count) { return kBack ? count - 1 - k : k; };
@@ -943,8 +950,8 @@ struct Split {
     for (; k < cl; ++k) state = tile(k).of(state);
     return got;
   }
-  // When every CTA has handed out its last: what is on its way to this one comes before it ends.  (Each step has waited for
-  // it; after a wait that ran out, a while.)
+  // When every CTA has handed out its last: what is on its way to this one comes before it ends.  (Each step has waited
+  // for it; after a wait that ran out, a while.)
   __device__ __forceinline__ void finish() {
     __syncwarp();
     cluster_meet();
@@ -953,8 +960,8 @@ struct Split {
   }
 };
 
-// A tile of rows' pieces in shared memory, 4 L bytes a row: rows change places within groups of 32 / L by the thread along
-// time that they are of, which puts the rows that a warp's threads along time read together into different banks.
+// A tile of rows' pieces in shared memory, 4 L bytes a row: rows change places within groups of 32 / L by the thread
+// along time that they are of, which puts the rows that a warp's threads along time read together into different banks.
 constexpr int kTileBytes = kSplitThr * kPos * 4;
 template <int L>
 __device__ __forceinline__ int tile_row(int r) {
@@ -978,8 +985,9 @@ struct RunRows {  // a thread's rows
 template <typename T, int L, int kStreams, int kStages>
 struct Stages {
   static constexpr size_t kBytes = (size_t)kStages * kStreams * kTileBytes;
-  static constexpr int kPieces = L / 4, kApart = kSplitThr / kPieces;  // 16-byte pieces of a row; a thread's rows' distance
-  static constexpr int kRows = kTile<L> / kApart;                       // ... and number
+  static constexpr int kPieces = L / 4;                 // 16-byte pieces of a row
+  static constexpr int kApart = kSplitThr / kPieces;    // a thread's rows' distance
+  static constexpr int kRows = kTile<L> / kApart;       // ... and number
   char* smem;               // of this thread's first row
   const char* p[kStreams];  // its row of the next tile
   int64_t left;             // rows in use from that row on
@@ -1004,7 +1012,8 @@ struct Stages {
       const int64_t row = kApart * rows[k].st * (int64_t)sizeof(T);
       if (in && left > kApart * (kRows - 1)) {
 #pragma unroll
-        for (int m = 0; m < kRows; ++m, from += row) tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
+        for (int m = 0; m < kRows; ++m, from += row)
+          tc::cp_async16(to + k * kTileBytes + m * kApart * L * 4, from, true);
       } else {
         const uint32_t f = k == 1 ? shut<T>() : 0u;
 #pragma unroll
@@ -1268,19 +1277,20 @@ struct Shape {
   dim3 block;
   unsigned across;  // CTAs across a row
 };
-Shape shape_of(int64_t lanes, int threads = 256, int unit = 1) {  // rows of up to `threads` lanes; short ones share a CTA
+// Rows of up to `threads` lanes a CTA; short ones share it.
+Shape shape_of(int64_t lanes, int threads = 256, int unit = 1) {
   const int64_t across = ceil_div(lanes, threads), width = ceil_div(ceil_div(lanes, across), unit) * unit;
   return {dim3((unsigned)width, (unsigned)(threads / width)), (unsigned)across};
 }
 
-// Split over time, and how (lanes 0: a chain a thread)?  The least time by a model of the measured parts, in us: a chain
-// takes 0.2 a position forward and 0.085 backward; a split step some 1.5 forward and 2 backward, longer with more CTAs to
-// hand runs to, and longer where two CTAs share an SM; a CTA's beginning 0.5 and 3 (the forward's go on to the next piece), and the
-// kernel's 2.5 more than a chain's.
-// `held` is how many clusters of each size the GPU holds at once.  Measured, chain / split: 77 fp32 histories of up to
-// 1001, d 200, forward 192 / 36 us; 400 of up to 515, d 256, 112 / 66; 1000 of 100, d 128, 28 / 50; backward 80 / 57,
-// 85 / 109, 31 / 72.  By clusters of 1, 2, 3, 4, 6 and 8, 6 histories of 32768, d 256: forward 191, 105, 84, 77, 134, 99;
-// backward with pieces of 128 bytes 474, 246, 172, 132, 185, 148 (64 bytes: 262, 139, 146, 146, 168, 199).
+// Split over time, and how (lanes 0: a chain a thread)?  The least time by a model of the measured parts, in us: a
+// chain takes 0.2 a position forward and 0.085 backward; a split step some 1.5 forward and 2 backward, longer with more
+// CTAs to hand runs to, and longer where two CTAs share an SM; a CTA's beginning 0.5 and 3 (the forward's go on to the
+// next piece), and the kernel's 2.5 more than a chain's.  `held` is how many clusters of each size the GPU holds at
+// once.  Measured, chain / split: 77 fp32 histories of up to 1001, d 200, forward 192 / 36 us; 400 of up to 515, d 256,
+// 112 / 66; 1000 of 100, d 128, 28 / 50; backward 80 / 57, 85 / 109, 31 / 72.  By clusters of 1, 2, 3, 4, 6 and 8, 6
+// histories of 32768, d 256: forward 191, 105, 84, 77 (with runs as 1 - K: 82), 134, 99; backward with pieces of 128
+// bytes 474, 246, 172, 132, 185, 148 (64 bytes: 262, 139, 146, 146, 168, 199).
 constexpr int64_t kMaxPartRows = 4096;  // of the split backward (some 3000 sequences and more are faster as chains)
 struct SplitHow {
   int lanes, cl, held;  // lanes 0: a chain a thread
@@ -1320,8 +1330,8 @@ int short_ctas(const hg_recur_params* p, int64_t T) {
   const int bytes = p->dtype == HG_BF16 ? short_bytes<__nv_bfloat16>(T) : short_bytes<float>(T);
   return std::min(kShortCtas, (227 << 10) / (bytes + (2 << 10)));
 }
-// Rows of partial sums of the bias's gradient: chains' CTAs.  Short histories: as many as run at once, each from one to the
-// next; long ones differ too much for that.
+// Rows of partial sums of the bias's gradient: chains' CTAs.  Short histories: as many as run at once, each from one to
+// the next; long ones differ too much for that.
 int64_t chain_rows(const hg_recur_params* p, int64_t n, int64_t T) {
   const Shape s = shape_of(p->d * (p->dtype == HG_BF16 ? 2 : 4) / 4, kBwdThr, 4);
   const int64_t most = T <= kPos ? 152 * short_ctas(p, T) : T <= 64 ? 152 * 3 : 152 * 16;
@@ -1398,8 +1408,8 @@ template <typename T, int L>
 hg_status backward_split(const RecurArgs& a, int cl, cudaStream_t s) {
   constexpr size_t smem = Stages<T, L, 3, kBwdStages>::kBytes;
   HG_TRY((allow_smem<recur_bwd_split<T, L>>(smem)));
-  return launch_clusters("recur_bwd_split", recur_bwd_split<T, L>, dim3((unsigned)(a.n * a.blocks * cl)), dim3(kSplitThr),
-                         smem, s, cl, a);
+  return launch_clusters("recur_bwd_split", recur_bwd_split<T, L>, dim3((unsigned)(a.n * a.blocks * cl)),
+                         dim3(kSplitThr), smem, s, cl, a);
 }
 template <typename T>
 hg_status backward(RecurArgs& a, SplitHow how, int64_t rows, cudaStream_t s) {
@@ -1507,8 +1517,8 @@ extern "C" hg_status hg_recur_bwd(const hg_recur_params* params, const hg_seq* x
     HG_TRY(check_state(dh_in, "dh_in"));
     const RowSet hi = block_set(h_in, 4 * n * w), ro = block_set(dh_out, 4 * n * w), ri = block_set(dh_in, 4 * n * w);
     const RowSet sv = block_set(saved, (int64_t)saved_bytes), db = block_set(dbias, 4 * w);
-    const RowSet sc = block_set(dbias ? scratch : nullptr, 4 * rows * w), bias = block_set(params->bias, w * (int64_t)esz);
-    const RowSet ln = block_set(lens, 4 * n);
+    const RowSet sc = block_set(dbias ? scratch : nullptr, 4 * rows * w), ln = block_set(lens, 4 * n);
+    const RowSet bias = block_set(params->bias, w * (int64_t)esz);
     HG_REQUIRE(dh_in == dh_out || !rows_meet(ri, ro), "dh_in and dh_out must not overlap");
     HG_TRY(check_apart(ri, "dh_in", {hi, sv, db, sc, bias, ln}));
     HG_TRY(check_apart(db, "dbias", {hi, ro, sv, sc, bias, ln}));

@@ -277,7 +277,8 @@ __device__ __forceinline__ void record_device_error(int* status, int code) { ato
 // Host: 2-D bf16 tensor map over a row-major [rows x cols] array with a [box_rows x 64] box and
 // 128-byte swizzle.  cols * 2 bytes must be a multiple of 16.
 hg_status make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
-// A contiguous array of bf16 or fp32 values of up to three dimensions, innermost first; box and swizzle in bytes (0: none).
+// A contiguous array of bf16 or fp32 values of up to three dimensions, innermost first; the box in values, the
+// swizzle in bytes (0: none).
 hg_status make_tmap(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims, const uint32_t* box,
                     int swizzle);
 // The same map of another array of the same shape.

@@ -946,8 +946,8 @@ def hg_recur_fwd(params: RecurParams, x, g, lens, h_in, y, h_out, saved, stream=
     r = [_flat_seq_arg(t, k, params.dtype, (n, T, d)) for t, k in ((x, "x"), (g, "g"), (y, "y"))]
     h = [_want(t, k, torch.float32, (n, d)) for t, k in ((h_in, "h_in"), (h_out, "h_out"))]
     sv = None if saved is None else _work_ptr(saved, hg_recur_workspace_size(params, n, T)[0], "saved")
-    _check(lib().hg_recur_fwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], r[2], h[1], sv,
-                              _stream(stream)), "hg_recur_fwd")
+    _check(lib().hg_recur_fwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], r[2],
+                              h[1], sv, _stream(stream)), "hg_recur_fwd")
 
 
 def hg_recur_bwd(params: RecurParams, x, g, lens, h_in, saved, d_y, dh_out, dx, dg, dh_in, dbias, scratch, stream=None):
@@ -959,8 +959,8 @@ def hg_recur_bwd(params: RecurParams, x, g, lens, h_in, saved, d_y, dh_out, dx, 
     sb, wb = hg_recur_workspace_size(params, n, T)
     sv = _work_ptr(saved, sb, "saved")
     w = _work_ptr(scratch, wb if n and dbias is not None else 0, "scratch")
-    _check(lib().hg_recur_bwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], sv, r[2], h[1],
-                              r[3], r[4], h[2], _want(dbias, "dbias", torch.float32, (d,)), w, _stream(stream)),
+    _check(lib().hg_recur_bwd(byref(params.c()), r[0], r[1], _want(lens, "lens", torch.int32, (n,)), n, T, h[0], sv, r[2],
+                              h[1], r[3], r[4], h[2], _want(dbias, "dbias", torch.float32, (d,)), w, _stream(stream)),
            "hg_recur_bwd")
 
 
@@ -1002,6 +1002,7 @@ def hg_moe_fwd(params: MoeParams, X, live, Y, experts, weights, scratch, stream=
     """X, Y [n, d]; live int32 [n] or None; experts int32 and weights fp32 [n, top_k], or None."""
     n, shape, chosen = X.shape[0], (X.shape[0], params.d), (X.shape[0], params.top_k)
     w = _work_ptr(scratch, hg_moe_workspace_size(params, n), "scratch")
-    _check(lib().hg_moe_fwd(byref(params.c()), _want(X, "X", params.dtype, shape), _want(live, "live", torch.int32, (n,)), n,
-                            _want(Y, "Y", params.dtype, shape), _want(experts, "experts", torch.int32, chosen),
+    _check(lib().hg_moe_fwd(byref(params.c()), _want(X, "X", params.dtype, shape),
+                            _want(live, "live", torch.int32, (n,)), n, _want(Y, "Y", params.dtype, shape),
+                            _want(experts, "experts", torch.int32, chosen),
                             _want(weights, "weights", torch.float32, chosen), w, _stream(stream)), "hg_moe_fwd")
